@@ -197,9 +197,10 @@ def prepare(case, seed):
     state = {"case": case, "z": z, "targets": targets}
     if op == "logp_bwd":
         z32 = z.float()
-        lse = torch.logsumexp(z32, dim=1)
-        lp = z32 - lse[:, None]
-        state |= {"lse": lse, "entropy": -(torch.exp(lp) * lp.clamp(min=-1e4)).sum(dim=1),
+        peak = z32.amax(dim=1)
+        log_sum = torch.log(torch.exp(z32 - peak[:, None]).sum(dim=1))
+        lp = (z32 - peak[:, None]) - log_sum[:, None]
+        state |= {"peak": peak, "log_sum": log_sum, "entropy": -(torch.exp(lp) * lp.clamp(min=-1e4)).sum(dim=1),
                   "g_logp": torch.randn(rows, device="cuda", generator=g) / 64,
                   "g_entropy": torch.randn(rows, device="cuda", generator=g) / 256 if case["entropy"] else None}
     return state
@@ -312,9 +313,8 @@ def _plain_logp(s):
     e = torch.exp(c)
     total = e.sum(dim=1)
     log_total = torch.log(total)
-    lse = big[:, 0] + log_total
-    lp = z.gather(1, t.clamp(min=0)[:, None])[:, 0] - lse
-    out = {"logp": torch.where(t >= 0, lp, 0.0), "lse": lse,
+    lp = c.gather(1, t.clamp(min=0)[:, None])[:, 0] - log_total
+    out = {"logp": torch.where(t >= 0, lp, 0.0), "peak": big[:, 0], "log_sum": log_total,
            "entropy": log_total - torch.where(e > 0, e * c, 0.0).sum(dim=1) / total}
     if k:
         # the k largest, of equal ones the first: one 64-bit key of the value's order and the index
@@ -322,13 +322,13 @@ def _plain_logp(s):
         order = torch.where(b >= 0, b, b ^ 0x7FFFFFFF).long()
         key = (order << 32) + (0xFFFFFFFF - torch.arange(z.shape[1], device="cuda"))
         ids = 0xFFFFFFFF - (torch.topk(key, k, dim=1).values & 0xFFFFFFFF)
-        out |= {"top_ids": ids, "top_logp": z.gather(1, ids) - lse[:, None]}
+        out |= {"top_ids": ids, "top_logp": c.gather(1, ids) - log_total[:, None]}
     return out
 
 
 def _plain_logp_bwd(s):
     z, t = s["z"].float(), s["targets"]
-    lp = z - s["lse"][:, None]
+    lp = (z - s["peak"][:, None]) - s["log_sum"][:, None]
     p = torch.exp(lp)
     g = torch.where(t >= 0, s["g_logp"], 0.0)[:, None]
     hit = t[:, None] == torch.arange(z.shape[1], device="cuda")
@@ -358,10 +358,10 @@ def run(state):
     if op == "logp":
         k = state["case"]["top"]
         r = binding.solon_token_logprobs(state["z"], state["targets"], top_k=k)
-        out = {"logp": r.logp, "lse": r.lse, "entropy": r.entropy}
+        out = {"logp": r.logp, "peak": r.peak, "log_sum": r.log_sum, "entropy": r.entropy}
         return out | {"top_ids": r.top_ids, "top_logp": r.top_logp} if k else out
-    return {"dz": binding.solon_token_logprobs_backward(state["z"], state["targets"], state["lse"], state["g_logp"], state["entropy"],
-                                                        state["g_entropy"])}
+    return {"dz": binding.solon_token_logprobs_backward(state["z"], state["targets"], state["peak"], state["log_sum"], state["g_logp"],
+                                                        state["entropy"], state["g_entropy"])}
 
 
 # ------------------------------------------------------------------------------------------ in 64 bits
@@ -422,22 +422,23 @@ def exact(case, seed):
         return {"dx": torch.cat(dx), "dw": torch.stack(dw), "db": torch.stack(db)}
     z, t = s["z"], s["targets"]
     if op == "logp":
-        logp, lse, ent, top = [], [], [], []
+        logp, lse, peak, ent, top = [], [], [], [], []
         for r in range(0, z.shape[0], 512):
             a = z[r:r + 512].to(f8)
             l = torch.logsumexp(a, dim=1)
             p = torch.softmax(a, dim=1)
             ent.append(-torch.special.xlogy(p, p).sum(dim=1))
-            lse.append(l)
+            peak.append(a.max(dim=1).values)
+            lse.append(l - peak[-1])
             u = t[r:r + 512]
             logp.append(torch.where(u < 0, 0.0, a[torch.arange(len(u), device="cuda"), u.clamp(min=0)] - l))
             top.append(a.topk(max(1, case["top"]), dim=1).values - l[:, None])
-        out = {"logp": torch.cat(logp), "lse": torch.cat(lse), "entropy": torch.cat(ent)}
+        out = {"logp": torch.cat(logp), "peak": torch.cat(peak), "log_sum": torch.cat(lse), "entropy": torch.cat(ent)}
         return out | {"top_ids": None, "top_logp": torch.cat(top)} if case["top"] else out
     dz = []
     for r in range(0, z.shape[0], 512):
         a, u = z[r:r + 512].to(f8), t[r:r + 512]
-        lp = a - s["lse"][r:r + 512, None].to(f8)
+        lp = a - (s["peak"][r:r + 512, None].to(f8) + s["log_sum"][r:r + 512, None].to(f8))
         p = lp.exp()
         g = s["g_logp"][r:r + 512].to(f8) * (u >= 0)
         part = -p * g[:, None]
