@@ -43,11 +43,16 @@ typedef enum solon_status {
 #define SOLON_MAX_M 32            /* compression ratio (the paper reports trouble above 14)   */
 #define SOLON_MAX_S 16            /* adversaries per group                                    */
 #define SOLON_MAX_PROJECTIONS 4   /* random projections K                                     */
+#define SOLON_MAX_COLS (1 << 24)  /* width of a layer norm's row; vocabulary                  */
+#define SOLON_MAX_TOP 32          /* likeliest tokens solon_token_logprobs reports            */
+#define SOLON_ADAMW_MAX_NUMEL (1LL << 40)
 
 /* Element type of partition gradients, coded vectors and aggregate (a property of the plan). */
 typedef enum solon_dtype {
   SOLON_F32 = 0, /* float32 at the boundary (solon_encode, solon_decode, ...)                                   */
-  SOLON_F64 = 1  /* float64 at the boundary, the paper's wire format (Table 2): the calls with the suffix _f64 */
+  SOLON_F64 = 1, /* float64 at the boundary, the paper's wire format (Table 2): the calls with the suffix _f64 */
+  SOLON_BF16 = 2, /* bfloat16 and float16: tensors of the token-model operators only, no plan has them        */
+  SOLON_F16 = 3
 } solon_dtype;
 
 typedef struct solon_plan solon_plan;
@@ -294,6 +299,117 @@ int solon_overwrite_rows(solon_plan* plan, float* matrix, int n_rows, const int*
 int solon_step_host_f64(solon_plan* plan, const double* grads_host, int n_byz, const int* byz_nodes,
                         const double* byz_rows_host, double* agg_host, uint8_t* mask_host);
 int solon_overwrite_rows_f64(solon_plan* plan, double* matrix, int n_rows, const int* nodes, const double* rows);
+
+/* ------------------------------------------------------------------------------------------
+ * Token-model operators: what stands on either side of the path when the partitions' gradients are
+ * those of a language model.  Layer norm and token log probabilities (the loss) produce partition
+ * gradients, solon_adamw_* applies the aggregate.  They need no plan, compute in float32, enqueue on
+ * `cuda_stream` (a cudaStream_t passed as void*) of the current device and never synchronise unless
+ * stated otherwise.  A matrix is given by its first element and its pitch, the distance of two rows'
+ * starts in elements (>= cols): rows need not be contiguous, and elements need their natural alignment
+ * only; 16-byte-aligned rows take wider accesses.
+ * ---------------------------------------------------------------------------------------- */
+
+/* Layer norm: y = w (x - mu) rstd + b with mu and rstd = 1 / sqrt(var + eps) of each row.
+ *   x, y          device, rows x cols of `dtype` (SOLON_F32, SOLON_BF16 or SOLON_F16); y may be x
+ *   weight, bias  device, cols of `param_dtype` (SOLON_F32 or dtype); NULL: 1 and 0
+ *   mean, rstd    device, rows float32 (outputs for the backward pass; NULL: not wanted)
+ * eps > 0.  rows = 0 does nothing.  Values are rounded to the element type once, when stored. */
+int solon_layernorm_forward(const void* x, int64_t x_pitch, int dtype, const void* weight, const void* bias, int param_dtype, int64_t rows, int64_t cols,
+                            double eps, void* y, int64_t y_pitch, float* mean, float* rstd, void* cuda_stream);
+
+/* Its gradients.  Partition k owns rows [k n, (k + 1) n), n = rows / partitions (which must divide rows), as in
+ * solon_lsq_grads; the parameters' gradients are summed within each partition, in an order that depends on the sizes
+ * alone, and written straight into row k of the partition-gradient matrix.
+ *   dy, x            device, rows x cols of `dtype`           mean, rstd   device, rows float32 (forward's)
+ *   dx               device, rows x cols of `dtype` (output; NULL: not wanted; may be dy or x)
+ *   dweight, dbias   device (outputs; NULL: not wanted): the gradient of weight c in partition k goes to
+ *                    dweight[k * grad_pitch + c], elements of `grad_dtype` (SOLON_F32 or SOLON_F64)
+ *   workspace        device, 16-byte aligned, solon_layernorm_backward_workspace(...) bytes (may be NULL where that is 0,
+ *                    or where neither dweight nor dbias is wanted); its contents need not survive the call
+ * A partition without rows (rows = 0) gets gradients of 0. */
+int64_t solon_layernorm_backward_workspace(int64_t rows, int64_t cols, int partitions);
+int solon_layernorm_backward(const void* dy, int64_t dy_pitch, const void* x, int64_t x_pitch, int dtype, const void* weight, int param_dtype,
+                             const float* mean, const float* rstd, int64_t rows, int64_t cols, int partitions, void* dx, int64_t dx_pitch, void* dweight,
+                             void* dbias, int64_t grad_pitch, int grad_dtype, void* workspace, int64_t workspace_bytes, void* cuda_stream);
+
+/* Log probabilities of given tokens under the softmax of each row of logits (a cross-entropy loss is -logp).
+ *   logits    device, rows x vocab of `dtype` (SOLON_F32, SOLON_BF16 or SOLON_F16)
+ *   targets   device, rows int64 (NULL: none): negative = no target in this row, logp 0
+ *   logp      device, rows float32 (output): log p of the target          (NULL: not wanted)
+ *   entropy   device, rows float32 (output): -sum p log p                 (NULL: not wanted)
+ *   peak, log_sum  device, rows float32 (outputs): M, the largest logit, and log sum e^(z - M), for the backward pass: log p =
+ *             (z - M) - log_sum, lse = M + log_sum                        (NULL: not wanted)
+ *   top_ids   device, rows x top_k int64, top_logp device, rows x top_k float32 (outputs, top_k > 0): the top_k
+ *             likeliest tokens in falling order, of equal logits the lower token first; top_k <= SOLON_MAX_TOP, vocab
+ * A logit of -infinity is a token masked out: p = 0.  A row with nothing left has peak = logp =
+ * -infinity and log_sum = entropy = 0.
+ * A target >= vocab is not read; its logp is NaN.  NaN or +infinity among the logits make the row's results NaN; NaN
+ * ranks above every number among the likeliest tokens. */
+int solon_token_logprobs(const void* logits, int64_t pitch, int dtype, const int64_t* targets, int64_t rows, int64_t vocab, int top_k, float* logp,
+                         float* entropy, float* peak, float* log_sum, int64_t* top_ids, float* top_logp, void* cuda_stream);
+
+/* Gradient with respect to the logits of sum_rows (grad_logp logp + grad_entropy entropy):
+ *   dlogits_j = grad_logp (1[j = target] - p_j) - grad_entropy p_j (log p_j + entropy)
+ *   peak, log_sum, entropy   device, rows float32: the forward's (entropy may be NULL without grad_entropy)
+ *   grad_logp, grad_entropy  device, rows float32 (NULL: 0; grad_logp needs targets)
+ *   dlogits                  device, rows x vocab of `dtype` (output); may be the logits, with their pitch
+ * Rows with peak = -infinity, and rows whose two factors are 0 (a row without target has grad_logp 0), get gradients of 0. */
+int solon_token_logprobs_backward(const void* logits, int64_t pitch, int dtype, const int64_t* targets, int64_t rows, int64_t vocab, const float* peak,
+                                  const float* log_sum, const float* entropy, const float* grad_logp, const float* grad_entropy, void* dlogits, int64_t dlogits_pitch,
+                                  void* cuda_stream);
+
+/* AdamW over all tensors of a model at once: per weight, with g' = grad_scale * clip * gradient and t the step's number,
+ *   m <- beta1 m + (1 - beta1) g'        v <- beta2 v + (1 - beta2) g'^2
+ *   p <- p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * The state is laid out in blocks of 256 elements; every tensor starts a block of its own (tensor i at block
+ * solon_adamw_state_blocks(i, numel), 0 for i = 0) and its last block is padded, with zeros.
+ *   state_bits 32: exp_avg, exp_avg_sq are blocks x 256 float32; base is not used.
+ *   state_bits 8:  exp_avg, exp_avg_sq are blocks x 256 bytes, base blocks x 2 int16.  Code c > 0 of a block stands for the
+ *                  float32 with bits (c + base) << 20 (three mantissa bits), code 0 for 0; exp_avg's codes have seven bits
+ *                  and the sign on top, base[0] is exp_avg's and base[1] exp_avg_sq's.  Rounded at random (from seed, step and
+ *                  place; without bias); exp_avg values more than 15.9 binades below their block's largest become 0,
+ *                  exp_avg_sq values more than 31.9 below it the smallest code, never 0. */
+typedef struct solon_adamw solon_adamw;
+
+/* Blocks of the state of n_tensors tensors of numel[i] elements (host array), or SOLON_ERR_INVALID_ARG. */
+int64_t solon_adamw_state_blocks(int n_tensors, const int64_t* numel);
+
+/* A handle on parameters and state, all owned by the caller and used in place by every step until the handle is destroyed.
+ *   params        host array of n_tensors device pointers, float32       numel    host array of n_tensors sizes (0: an empty tensor)
+ *   copies        host array of device pointers, bfloat16 (NULL, or entries NULL: none): every step also writes the rounded
+ *                 parameters there, for a forward pass in bfloat16
+ *   weight_decay  host array of n_tensors factors (NULL: 0)
+ *   exp_avg, exp_avg_sq (16-byte aligned), base (4-byte aligned): the state, zero before the first step
+ * 0 <= beta < 1, eps > 0.  Uses the current device and synchronises it. */
+int solon_adamw_create(int n_tensors, const int64_t* numel, float* const* params, void* const* copies, const float* weight_decay, int state_bits,
+                       void* exp_avg, void* exp_avg_sq, int16_t* base, double beta1, double beta2, double eps, uint64_t seed, solon_adamw** out);
+int solon_adamw_destroy(solon_adamw* opt);
+
+/* Gradients that live in tensors of their own (host array of device pointers, SOLON_F32, SOLON_F64 or SOLON_BF16), read in
+ * place by the steps that are given no flat gradient.  Synchronises. */
+int solon_adamw_bind_grads(solon_adamw* opt, const void* const* grads, int grad_dtype);
+
+/* One step.
+ *   grad        device: the gradients of all tensors one after the other - the aggregate that solon_decode returns -, of
+ *               `grad_dtype` (SOLON_F32, SOLON_F64 or SOLON_BF16); NULL: the bound gradients
+ *   grad_scale  factor on the gradient (1 / P turns a sum over partitions into their mean)
+ *   max_norm    > 0: the scaled gradient is scaled down to this 2-norm if it is longer (clip = max_norm / (norm + 1e-6));
+ *               0: no clipping
+ *   grad_norm   device, one float32 (output; NULL: not wanted; needs max_norm > 0): the norm before clipping
+ *   guard       a plan whose last decode the step depends on (NULL: none): if that decode was undecodable, or a wait in it
+ *               ran out, the step changes nothing.  Enqueue the step after the decode, on its stream or ordered behind it.
+ * A norm that is not finite also makes the step change nothing; without clipping a gradient that is not finite goes into its
+ * weight as the formulas have it.  Steps are counted on the device, only those that were applied count: a captured step may be replayed. */
+int solon_adamw_step(solon_adamw* opt, const void* grad, int grad_dtype, double grad_scale, double lr, double max_norm, float* grad_norm,
+                     const solon_plan* guard, void* cuda_stream);
+
+/* Number of steps applied (a resumed run sets it), and of steps that changed nothing.  Both synchronise the device. */
+int solon_adamw_set_step(solon_adamw* opt, int64_t step);
+int solon_adamw_get_steps(solon_adamw* opt, int64_t* applied, int64_t* skipped);
+
+/* What an 8-bit state stands for: blocks x 256 bfloat16 each (exact), 8-byte aligned.  Enqueued on cuda_stream. */
+int solon_adamw_moments(solon_adamw* opt, void* exp_avg_out, void* exp_avg_sq_out, void* cuda_stream);
 
 /* ------------------------------------------------------------------------------------------
  * Introspection of the last decode (for parity tests and diagnostics; each synchronises).

@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import os
 from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int, c_int64, c_uint8, c_uint64, c_void_p
+from typing import NamedTuple
 
 import numpy as np
 
@@ -24,6 +25,8 @@ ERR_INTERNAL = -5
 ERR_NOMEM = -6
 F32 = 0
 F64 = 1
+BF16 = 2
+F16 = 3
 
 # name -> (restype, argtypes); every symbol the header declares
 SIGNATURES = {
@@ -75,6 +78,24 @@ SIGNATURES = {
     "solon_plan_kernel_launches": (c_int64, [c_void_p]),
     "solon_plan_set_profiling": (c_int, [c_void_p, c_int]),
     "solon_plan_get_timings": (c_int, [c_void_p, POINTER(c_float)]),
+    "solon_layernorm_forward": (c_int, [c_void_p, c_int64, c_int, c_void_p, c_void_p, c_int, c_int64, c_int64, c_double, c_void_p, c_int64, c_void_p,
+                                        c_void_p, c_void_p]),
+    "solon_layernorm_backward_workspace": (c_int64, [c_int64, c_int64, c_int]),
+    "solon_layernorm_backward": (c_int, [c_void_p, c_int64, c_void_p, c_int64, c_int, c_void_p, c_int, c_void_p, c_void_p, c_int64, c_int64, c_int,
+                                         c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_int, c_void_p, c_int64, c_void_p]),
+    "solon_token_logprobs": (c_int, [c_void_p, c_int64, c_int, c_void_p, c_int64, c_int64, c_int, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                     c_void_p, c_void_p]),
+    "solon_token_logprobs_backward": (c_int, [c_void_p, c_int64, c_int, c_void_p, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                              c_void_p, c_int64, c_void_p]),
+    "solon_adamw_state_blocks": (c_int64, [c_int, POINTER(c_int64)]),
+    "solon_adamw_create": (c_int, [c_int, POINTER(c_int64), POINTER(c_void_p), POINTER(c_void_p), POINTER(c_float), c_int, c_void_p, c_void_p, c_void_p,
+                                   c_double, c_double, c_double, c_uint64, POINTER(c_void_p)]),
+    "solon_adamw_destroy": (c_int, [c_void_p]),
+    "solon_adamw_bind_grads": (c_int, [c_void_p, POINTER(c_void_p), c_int]),
+    "solon_adamw_step": (c_int, [c_void_p, c_void_p, c_int, c_double, c_double, c_double, c_void_p, c_void_p, c_void_p]),
+    "solon_adamw_set_step": (c_int, [c_void_p, c_int64]),
+    "solon_adamw_get_steps": (c_int, [c_void_p, POINTER(c_int64), POINTER(c_int64)]),
+    "solon_adamw_moments": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p]),
     "solon_project_noalloc": (c_int, [c_void_p, c_void_p, c_int64, c_int, c_int64, c_int, c_void_p, c_void_p, c_void_p]),
 }
 
@@ -172,6 +193,317 @@ def solon_project_noalloc(received, f, rho, nu, stream=None) -> int:
     stream = stream if stream is not None else torch.cuda.current_stream()
     return lib().solon_project_noalloc(c_void_p(received.data_ptr()), c_void_p(f.data_ptr()), f_pitch, P, d_c, K,
                                        c_void_p(rho.data_ptr()), c_void_p(nu.data_ptr()), c_void_p(stream.cuda_stream))
+
+
+# ------------------------------------------------------------------ token-model operators (no plan needed)
+#
+# All of them enqueue on the current stream of the current device, which the tensors have to be on, and return without
+# synchronising.  Outputs may be given (to be reused from step to step) or are allocated.
+
+_torch_dtypes = {}
+
+
+def _dtype_code(dtype) -> int:
+    if not _torch_dtypes:
+        import torch
+
+        _torch_dtypes.update({torch.float32: F32, torch.float64: F64, torch.bfloat16: BF16, torch.float16: F16})
+    code = _torch_dtypes.get(dtype)
+    if code is None:
+        raise ValueError(f"unsupported element type {dtype}")
+    return code
+
+
+def _current_stream(device) -> int:
+    import torch
+
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _matrix(t, name: str, shape=None, dtype=None, device=None):
+    """(pointer, pitch) of a CUDA matrix whose rows are contiguous."""
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA matrix (rows x columns)")
+    if (shape is not None and tuple(t.shape) != tuple(shape)) or (dtype is not None and t.dtype != dtype) or (device is not None and t.device != device):
+        raise ValueError(f"{name}: expected {tuple(shape) if shape else 'any shape'} {dtype} on {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    rows, cols = t.shape
+    pitch, step = t.stride()
+    if (step != 1 and cols > 1) or (pitch < cols and rows > 1):
+        raise ValueError(f"{name}: the elements of a row must be contiguous and rows must not overlap (strides {tuple(t.stride())})")
+    return t.data_ptr(), pitch if rows > 1 else cols
+
+
+def _vector(t, name: str, n: int, dtype, device) -> int:
+    if t.dim() != 1 or t.shape[0] != n or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous vector of {n} {dtype} on {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+def _params(weight, bias, cols: int, x):
+    """(weight pointer, bias pointer, type code) of layer norm parameters in float32 or x's type."""
+    given = weight if weight is not None else bias
+    if given is None:
+        return None, None, F32
+    code = _dtype_code(given.dtype)
+    return (None if weight is None else _vector(weight, "weight", cols, given.dtype, x.device),
+            None if bias is None else _vector(bias, "bias", cols, given.dtype, x.device), code)
+
+
+def solon_layernorm_forward(x, weight=None, bias=None, eps: float = 1e-5, y=None, mean=None, rstd=None):
+    """Layer norm of the rows of x (rows x cols; float32, bfloat16 or float16).  Returns (y, mean, rstd): y in x's type, the
+    rows' means and reciprocal standard deviations in float32 for the backward pass."""
+    import torch
+
+    px, x_pitch = _matrix(x, "x")
+    rows, cols = x.shape
+    stream = _current_stream(x.device)
+    if y is None:
+        y = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    if mean is None:
+        mean = torch.empty(rows, dtype=torch.float32, device=x.device)
+    if rstd is None:
+        rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
+    py, y_pitch = _matrix(y, "y", x.shape, x.dtype, x.device)
+    pw, pb, code = _params(weight, bias, cols, x)
+    _check(lib().solon_layernorm_forward(px, x_pitch, _dtype_code(x.dtype), pw, pb, code, rows, cols, eps, py, y_pitch,
+                                         _vector(mean, "mean", rows, torch.float32, x.device),
+                                         _vector(rstd, "rstd", rows, torch.float32, x.device), stream), "solon_layernorm_forward")
+    return y, mean, rstd
+
+
+def solon_layernorm_backward(dy, x, mean, rstd, weight=None, partitions: int = 1, dx=None, dweight=None, dbias=None, param_grads: bool = True):
+    """Gradients of layer norm.  Returns (dx, dweight, dbias); dweight and dbias are partitions x cols, row k summed over the
+    rows of partition k (rows / partitions consecutive ones).  They may be views into the partition-gradient matrix
+    (float32 or float64, as the plan's type), e.g. grads[:, a:a + cols].  param_grads=False: dx only."""
+    import torch
+
+    px, x_pitch = _matrix(x, "x")
+    rows, cols = x.shape
+    pdy, dy_pitch = _matrix(dy, "dy", x.shape, x.dtype, x.device)
+    stream = _current_stream(x.device)
+    if dx is None:
+        dx = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    pdx, dx_pitch = _matrix(dx, "dx", x.shape, x.dtype, x.device)
+    pw, _, code = _params(weight, None, cols, x)
+    pdw = pdb = workspace = None
+    grad_pitch, grad_code, n_bytes = cols, F32, 0
+    if param_grads:
+        like = dweight if dweight is not None else dbias
+        if like is None:
+            dweight, dbias = torch.empty((2, partitions, cols), dtype=torch.float32, device=x.device).unbind(0)
+        elif dweight is None:
+            dweight = torch.empty_strided(like.shape, like.stride(), dtype=like.dtype, device=x.device)
+        elif dbias is None:
+            dbias = torch.empty_strided(like.shape, like.stride(), dtype=like.dtype, device=x.device)
+        pdw, grad_pitch = _matrix(dweight, "dweight", (partitions, cols), None, x.device)
+        pdb, other_pitch = _matrix(dbias, "dbias", (partitions, cols), dweight.dtype, x.device)
+        if grad_pitch != other_pitch:
+            raise ValueError("dweight and dbias must have the same row pitch")
+        grad_code = _dtype_code(dweight.dtype)
+        n_bytes = lib().solon_layernorm_backward_workspace(rows, cols, partitions)
+        if n_bytes > 0:
+            workspace = torch.empty(n_bytes // 4, dtype=torch.float32, device=x.device)
+    _check(lib().solon_layernorm_backward(pdy, dy_pitch, px, x_pitch, _dtype_code(x.dtype), pw, code,
+                                          _vector(mean, "mean", rows, torch.float32, x.device), _vector(rstd, "rstd", rows, torch.float32, x.device),
+                                          rows, cols, partitions, pdx, dx_pitch, pdw, pdb, grad_pitch, grad_code,
+                                          None if workspace is None else workspace.data_ptr(), n_bytes, stream), "solon_layernorm_backward")
+    return dx, dweight, dbias
+
+
+class TokenLogprobs(NamedTuple):
+    """What solon_token_logprobs returns; what was not asked for is None."""
+
+    logp: object       # rows, float32: log probability of the target (None without targets)
+    entropy: object    # rows, float32
+    peak: object       # rows, float32: the largest logit
+    log_sum: object    # rows, float32: log sum e^(z - peak); log p = (z - peak) - log_sum
+    top_ids: object    # rows x top_k, int64
+    top_logp: object   # rows x top_k, float32
+
+
+def solon_token_logprobs(logits, targets=None, top_k: int = 0) -> TokenLogprobs:
+    """Log probabilities of the targets (int64; negative: none in this row) under the softmax of each row of logits
+    (rows x vocabulary; float32, bfloat16 or float16), the rows' entropy and their top_k likeliest tokens."""
+    import torch
+
+    pz, pitch = _matrix(logits, "logits")
+    rows, vocab = logits.shape
+    device = logits.device
+    stream = _current_stream(device)
+    stats = torch.empty((4, rows), dtype=torch.float32, device=device)
+    base, row_bytes = stats.data_ptr(), 4 * rows
+    top_ids = torch.empty((rows, top_k), dtype=torch.int64, device=device) if top_k > 0 else None
+    top_logp = torch.empty((rows, top_k), dtype=torch.float32, device=device) if top_k > 0 else None
+    _check(lib().solon_token_logprobs(pz, pitch, _dtype_code(logits.dtype),
+                                      None if targets is None else _vector(targets, "targets", rows, torch.int64, device), rows, vocab, top_k,
+                                      None if targets is None else base, base + row_bytes, base + 2 * row_bytes, base + 3 * row_bytes,
+                                      None if top_ids is None else top_ids.data_ptr(), None if top_logp is None else top_logp.data_ptr(), stream),
+           "solon_token_logprobs")
+    logp, entropy, peak, log_sum = stats.unbind(0)
+    return TokenLogprobs(None if targets is None else logp, entropy, peak, log_sum, top_ids, top_logp)
+
+
+def solon_token_logprobs_backward(logits, targets, peak, log_sum, grad_logp=None, entropy=None, grad_entropy=None, out=None):
+    """Gradient of sum(grad_logp * logp + grad_entropy * entropy) with respect to the logits, in their type; `out` may be
+    the logits themselves."""
+    import torch
+
+    pz, pitch = _matrix(logits, "logits")
+    rows, vocab = logits.shape
+    device = logits.device
+    stream = _current_stream(device)
+    if out is None:
+        out = torch.empty((rows, vocab), dtype=logits.dtype, device=device)
+    po, out_pitch = _matrix(out, "out", logits.shape, logits.dtype, device)
+
+    def row_vector(t, name):
+        return None if t is None else _vector(t, name, rows, torch.float32, device)
+
+    _check(lib().solon_token_logprobs_backward(pz, pitch, _dtype_code(logits.dtype),
+                                               None if targets is None else _vector(targets, "targets", rows, torch.int64, device), rows, vocab,
+                                               row_vector(peak, "peak"), row_vector(log_sum, "log_sum"),
+                                               row_vector(entropy if grad_entropy is not None else None, "entropy"), row_vector(grad_logp, "grad_logp"),
+                                               row_vector(grad_entropy, "grad_entropy"), po, out_pitch, stream),
+           "solon_token_logprobs_backward")
+    return out
+
+
+class AdamW:
+    """Owner of a solon_adamw*: AdamW over a list of float32 CUDA tensors, updated in place by step().
+
+    bits: 32 or 8, the state's width.  weight_decay: one factor, or one per tensor.  copies: bfloat16 tensors of the same
+    sizes (entries may be None) that every step fills with the rounded parameters.  state: (exp_avg, exp_avg_sq, base) as
+    an earlier handle's `state` had it, taken over in place; by default zeros.  step: steps already applied to it."""
+
+    def __init__(self, params, bits: int = 32, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.0, seed: int = 0, step: int = 0, copies=None,
+                 state=None):
+        import torch
+
+        self._h = None
+        params = list(params)
+        if not params:
+            raise ValueError("no parameters")
+        self.device = params[0].device
+        _current_stream(self.device)
+        n = len(params)
+        for p in params:
+            if not (p.is_cuda and p.is_contiguous() and p.dtype == torch.float32 and p.device == self.device):
+                raise ValueError("parameters must be contiguous float32 CUDA tensors on one device")
+        copies = [None] * n if copies is None else list(copies)
+        decay = list(weight_decay) if hasattr(weight_decay, "__len__") else [float(weight_decay)] * n
+        if len(copies) != n or len(decay) != n:
+            raise ValueError("copies and weight_decay need an entry for each parameter")
+        for p, c in zip(params, copies):
+            if c is not None and not (c.is_contiguous() and c.dtype == torch.bfloat16 and c.device == self.device and c.numel() == p.numel()):
+                raise ValueError("copies must be contiguous bfloat16 tensors of the parameters' sizes")
+        self.params, self.copies, self.bits = params, copies, bits
+        self.numel = [p.numel() for p in params]
+        self.total = sum(self.numel)
+        sizes = (c_int64 * n)(*self.numel)
+        blocks = int(lib().solon_adamw_state_blocks(n, sizes))
+        if blocks < 0:
+            raise SolonError(blocks, "solon_adamw_state_blocks")
+        if bits not in (8, 32):
+            raise ValueError("bits must be 8 or 32")
+        dtype = torch.float32 if bits == 32 else torch.uint8
+        if state is None:
+            state = (torch.zeros((blocks, 256), dtype=dtype, device=self.device), torch.zeros((blocks, 256), dtype=dtype, device=self.device),
+                     None if bits == 32 else torch.zeros((blocks, 2), dtype=torch.int16, device=self.device))
+        exp_avg, exp_avg_sq, base = state
+        for t, want, kind in ((exp_avg, (blocks, 256), dtype), (exp_avg_sq, (blocks, 256), dtype), (base, (blocks, 2), torch.int16)):
+            if t is base and bits == 32:
+                continue
+            if t is None or not (t.is_contiguous() and t.dtype == kind and t.device == self.device and tuple(t.shape) == want):
+                raise ValueError(f"state: expected contiguous {kind} tensors of shape {want} on {self.device}")
+        self.state = (exp_avg, exp_avg_sq, None if bits == 32 else base)
+        self._norm = torch.zeros((), dtype=torch.float32, device=self.device)
+        self._grads = None
+        handle = c_void_p()
+        torch.cuda.current_stream().synchronize()        # the state may just have been made
+        _check(lib().solon_adamw_create(n, sizes, self._pointers(params), self._pointers(copies), (c_float * n)(*decay), bits,
+                                        exp_avg.data_ptr() or 16, exp_avg_sq.data_ptr() or 16,
+                                        None if bits == 32 else base.data_ptr() or 16,
+                                        betas[0], betas[1], eps, seed, byref(handle)), "solon_adamw_create")
+        self._h = handle
+        if step:
+            self.set_step(step)
+
+    @staticmethod
+    def _pointers(tensors):
+        return (c_void_p * len(tensors))(*[None if t is None or t.numel() == 0 else t.data_ptr() for t in tensors])
+
+    def close(self) -> None:
+        if getattr(self, "_h", None):
+            lib().solon_adamw_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def bind_grads(self, grads) -> None:
+        """Gradients in tensors of their own (one type: float32, float64 or bfloat16), read in place by step(None, ...)."""
+        grads = list(grads)
+        if len(grads) != len(self.numel):
+            raise ValueError("one gradient for each parameter")
+        for g, n in zip(grads, self.numel):
+            if not (g.is_cuda and g.is_contiguous() and g.device == self.device and g.numel() == n and g.dtype == grads[0].dtype):
+                raise ValueError("gradients must be contiguous CUDA tensors of the parameters' sizes and of one type")
+        _check(lib().solon_adamw_bind_grads(self._h, self._pointers(grads), _dtype_code(grads[0].dtype)), "solon_adamw_bind_grads")
+        self._grads = grads
+
+    def step(self, grad=None, lr: float = 1e-3, grad_scale: float = 1.0, max_norm: float = 0.0, plan=None):
+        """One step on the current stream.  grad: the gradients of all parameters one after the other (the aggregate that
+        decode returns; float32, float64 or bfloat16), or None for the bound ones.  max_norm > 0 clips the norm of
+        grad_scale * grad and returns that norm (a device scalar, overwritten by the next step).  plan: the Plan whose
+        decode made grad; the step changes nothing if that decode failed."""
+        stream = _current_stream(self.device)
+        code = F32
+        if grad is not None:
+            if not (grad.is_cuda and grad.is_contiguous() and grad.device == self.device and grad.numel() == self.total):
+                raise ValueError(f"grad must be a contiguous CUDA tensor of {self.total} elements on {self.device}")
+            code = _dtype_code(grad.dtype)
+        if plan is not None and plan.stream_handle != stream:
+            raise ValueError("the plan's calls go to another stream than the current one")
+        _check(lib().solon_adamw_step(self._h, None if grad is None else grad.data_ptr() or 16, code, grad_scale, lr, max_norm,
+                                      self._norm.data_ptr() if max_norm > 0 else None, None if plan is None else plan._h, stream), "solon_adamw_step")
+        return self._norm if max_norm > 0 else None
+
+    def set_step(self, step: int) -> None:
+        _check(lib().solon_adamw_set_step(self._h, step), "solon_adamw_set_step")
+
+    def steps(self) -> tuple[int, int]:
+        """(steps applied, steps that changed nothing); synchronises."""
+        applied, skipped = c_int64(0), c_int64(0)
+        _check(lib().solon_adamw_get_steps(self._h, byref(applied), byref(skipped)), "solon_adamw_get_steps")
+        return applied.value, skipped.value
+
+    def moments(self):
+        """(exp_avg, exp_avg_sq), blocks x 256: the state itself with 32 bits, what it stands for in bfloat16 with 8."""
+        import torch
+
+        if self.bits == 32:
+            return self.state[0], self.state[1]
+        out = [torch.empty(self.state[0].shape, dtype=torch.bfloat16, device=self.device) for _ in range(2)]
+        stream = _current_stream(self.device)
+        if out[0].numel():
+            _check(lib().solon_adamw_moments(self._h, out[0].data_ptr(), out[1].data_ptr(), stream), "solon_adamw_moments")
+        return out[0], out[1]
+
+    def of_tensor(self, blocked, i: int):
+        """The entries of parameter i in a blocks x 256 tensor (a state or what moments() returns), as a flat view."""
+        first = sum(-(-n // 256) for n in self.numel[:i]) * 256
+        return blocked.view(-1)[first:first + self.numel[i]]
 
 
 # ------------------------------------------------------------------ plan

@@ -9,7 +9,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsolon.so")
-SOURCES = ["plan.cu", "encode.cu", "project.cu", "locate.cu", "recover.cu", "decode.cu", "lsq.cu"]
+SOURCES = ["plan.cu", "encode.cu", "project.cu", "locate.cu", "recover.cu", "decode.cu", "lsq.cu",
+           "layernorm.cu", "logprobs.cu", "adamw.cu"]
 
 
 def _nvcc() -> str:
@@ -43,7 +44,7 @@ def build(verbose: bool = False, force: bool = False) -> str:
             tmp = f"{LIB}.{os.getpid()}.tmp"
             cmd = [
                 _nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-                "-shared", "-Xcompiler", "-fPIC", "-cudart", "static",
+                "-shared", "-Xcompiler", "-fPIC", "-cudart", "static", "--threads", "0",
             ]
             if verbose:
                 cmd += ["-Xptxas", "-v"]

@@ -1,0 +1,633 @@
+// AdamW over all tensors of a model at once (solon_adamw_*): what a parameter server does with the aggregate that
+// solon_decode returns.  Per weight, with g' = grad_scale * clip * g:
+//     m <- b1 m + (1 - b1) g'          v <- b2 v + (1 - b2) g'^2
+//     p <- p (1 - lr wd) - lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)
+// All of it in float32; b1^t and b2^t are kept in float64 on the device, so that a replayed CUDA graph counts its steps.
+//
+// Bound by memory: a weight with float32 gradient moves 28 bytes (32-bit states) or 16 (8-bit states) against about 20 flops.
+//
+// Work: the state is laid out in blocks of 256 elements, every tensor starting a block of its own; one warp owns a block, one
+// CTA eight consecutive blocks of a tensor (a chunk).  Three launches at most: the gradient's squared norm (only when it is
+// clipped), one CTA that turns it into the clip factor, checks the guard and counts the step, and the update itself.
+#include <math.h>
+
+#include <new>
+
+#include "elements.cuh"
+#include "solon_internal.h"
+
+namespace solon {
+
+constexpr int kAdamBlock = 256;                        // elements of a state block (one warp, eight per lane)
+constexpr int kAdamChunkBlocks = 8;                    // blocks of a chunk (one CTA of eight warps)
+constexpr int kAdamThreads = 32 * kAdamChunkBlocks;
+
+struct AdamTensor {
+  float* p;
+  __nv_bfloat16* copy;       // nullptr: none
+  const void* grad;          // bound gradient (nullptr: the gradient is the flat vector of the call)
+  int64_t offset;            // first element in the concatenated order
+  int64_t numel;
+  int64_t first_block;
+  float weight_decay;
+  int pad;
+};
+
+struct AdamChunk {
+  int tensor;
+  int index;                 // chunk inside the tensor
+};
+
+// What the update reads, written by the control kernel of the same step.
+struct AdamScalars {
+  double b1t, b2t;           // b1^t, b2^t of the last step that was applied
+  long long applied, skipped;
+  float inv_bc1, inv_sqrt_bc2, grad_scale;
+  int skip;
+  unsigned key;              // of the step's random words
+};
+
+}  // namespace solon
+
+struct solon_adamw {
+  int n_tensors, bits, device, num_sms;
+  double beta1, beta2, eps;
+  uint64_t seed;
+  int64_t total, n_blocks, n_chunks;
+  int grads_bound, grad_dtype;             // bound gradients and their type
+  void *exp_avg, *exp_avg_sq;
+  int16_t* base;
+  std::vector<solon::AdamTensor> tensors;
+  solon::AdamTensor* d_tensors;
+  solon::AdamChunk* d_chunks;
+  solon::AdamScalars* d_scalars;
+  double* d_partials;                      // norm kernel: one sum per CTA
+  int norm_grid;
+};
+
+namespace solon {
+
+// MurmurHash3's 32-bit finaliser (Appleby): every input bit reaches every output bit.
+__host__ __device__ __forceinline__ uint32_t mix32(uint32_t h) {
+  h ^= h >> 16;
+  h *= 0x85EBCA6Bu;
+  h ^= h >> 13;
+  h *= 0xC2B2AE35u;
+  return h ^ (h >> 16);
+}
+
+// The 32 random bits of a state slot in a step (key: step and seed): the low half rounds m, the high half v.
+__device__ __forceinline__ uint32_t slot_random(uint32_t key, int64_t slot) {
+  return mix32(((uint32_t)slot * 0x9E3779B1u + (uint32_t)((uint64_t)slot >> 32) * 0x85EBCA77u) ^ key);
+}
+
+// ---- the 8-bit state -------------------------------------------------------------------------------------------
+// The float32 numbers with three mantissa bits are those whose low 20 bits are zero; their rank is bits >> 20.  A block
+// of 256 values holds `base` and, per value, an 8-bit code: rank - base, 0 for zero.  The window of 127 (m, beside its
+// sign) or 255 (v) ranks ends at the block's largest magnitude, rounded up: 15.9 and 31.9 binades, the same range of
+// gradients for both.  Because the grid is the same for every block, a window that moves with the block's maximum
+// re-rounds nothing.
+//
+// Rounding is stochastic: adding 20 random bits before the cut is unbiased (within a binade, and across its end, a float's
+// value is linear in its bits).  Rounding to nearest would leave v standing still: with b2 = 0.999 a step moves it by up to
+// 0.1 %, half a grid step is 3 - 6 %.  Two exceptions: what lies below the window becomes 0 for m and the smallest code for
+// v, which is never 0 unless v is - a zero v under a moving m would divide by eps.  Non-finite values take the top code
+// and have no part in the choice of the window, so they spoil no other element of their block.
+constexpr uint32_t kTopFinite = 0x7F7u;                // rank of the largest finite value of the grid
+
+__device__ __forceinline__ float state_value(uint32_t code, int base) {
+  return code ? __uint_as_float((code + (uint32_t)base) << 20) : 0.0f;
+}
+
+// Largest finite magnitude of the block as bits (float order = integer order for non-negative floats).
+__device__ __forceinline__ uint32_t finite_bits(uint32_t bits) { return bits < 0x7F800000u ? bits : 0u; }
+
+__device__ __forceinline__ int window_base(uint32_t max_bits, uint32_t levels) {
+  uint32_t top = (max_bits + 0xFFFFFu) >> 20;
+  top = top < kTopFinite ? top : kTopFinite;
+  return top > levels ? (int)(top - levels) : 0;
+}
+
+__device__ __forceinline__ int state_code(uint32_t bits, uint32_t random20, int base, int levels) {
+  const int code = (int)((bits + random20) >> 20) - base;
+  return code < levels ? code : levels;
+}
+
+// ---- control: one CTA before the update -----------------------------------------------------------------------------
+
+struct AdamControlArgs {
+  AdamScalars* s;
+  const double* partials;      // squared norm of the unscaled gradient, per CTA of the norm kernel
+  int n_partials;              // 0: no clipping
+  float* norm_out;             // nullptr: not wanted
+  double grad_scale, max_norm, beta1, beta2;
+  uint64_t seed;
+  const int* guard_status;     // plan's status words (nullptr: no guard)
+  const int* guard_t;          // per group: accepted error count, -1 undecodable
+  int guard_groups;
+};
+
+__global__ void __launch_bounds__(256) adam_control_kernel(AdamControlArgs a) {
+  __shared__ double part_s[8];
+  pdl_trigger();
+  pdl_wait();
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < a.n_partials; i += 256) sum += a.partials[i];
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+  if ((threadIdx.x & 31) == 0) part_s[threadIdx.x >> 5] = sum;
+  int bad = 0;
+  if (a.guard_t) {
+    for (int i = threadIdx.x; i < a.guard_groups; i += 256) bad |= a.guard_t[i] < 0;
+    if (threadIdx.x < 2) bad |= a.guard_status[threadIdx.x] & kStatusWaitExpired;
+  }
+  bad = __syncthreads_or(bad);
+  if (threadIdx.x != 0) return;
+  double scale = a.grad_scale;
+  if (a.n_partials > 0) {
+    sum = 0.0;
+    for (int w = 0; w < 8; ++w) sum += part_s[w];
+    const double norm = sqrt(sum) * fabs(a.grad_scale);
+    if (a.norm_out) *a.norm_out = (float)norm;
+    if (!(norm < INFINITY)) bad = 1;               // NaN or infinite: there is nothing to clip to
+    const double clip = a.max_norm / (norm + 1e-6);
+    if (clip < 1.0) scale *= clip;
+  }
+  AdamScalars* s = a.s;
+  s->skip = bad;
+  if (bad) {
+    s->skipped += 1;
+    return;
+  }
+  const double b1t = s->b1t * a.beta1, b2t = s->b2t * a.beta2;
+  const long long t = s->applied + 1;
+  s->b1t = b1t;
+  s->b2t = b2t;
+  s->applied = t;
+  s->inv_bc1 = (float)(1.0 / (1.0 - b1t));
+  s->inv_sqrt_bc2 = (float)(1.0 / sqrt(1.0 - b2t));
+  s->grad_scale = (float)scale;
+  s->key = mix32((uint32_t)t * 0x9E3779B1u + (uint32_t)a.seed) ^ (uint32_t)(a.seed >> 32);
+}
+
+// ---- squared norm of the gradient ----------------------------------------------------------------------------------
+// Squares and sums of at most eight of them in float32, everything further in float64, in an order that depends on the
+// sizes alone.  A square that overflows float32 counts as infinite.
+
+template <typename G>
+__global__ void __launch_bounds__(kAdamThreads) adam_norm_kernel(const AdamTensor* __restrict__ tensors, const AdamChunk* __restrict__ chunks,
+                                                                 int64_t n_chunks, const G* __restrict__ flat, double* __restrict__ partials) {
+  __shared__ double part_s[kAdamChunkBlocks];
+  pdl_trigger();
+  pdl_wait();
+  double acc = 0.0;
+  for (int64_t c = blockIdx.x; c < n_chunks; c += gridDim.x) {
+    const AdamChunk ch = chunks[c];
+    const AdamTensor* t = tensors + ch.tensor;
+    const G* g = flat ? flat + t->offset : static_cast<const G*>(t->grad);
+    const int64_t first = (int64_t)ch.index * (kAdamBlock * kAdamChunkBlocks);
+    const int64_t left = t->numel - first;
+    g += first;
+    float sum = 0.0f;
+    if (left >= kAdamBlock * kAdamChunkBlocks && ((uintptr_t)g & 15) == 0) {
+      constexpr int kVec = 16 / sizeof(G);
+      constexpr int kLoads = 8 / kVec;
+      Pack<G, kVec> v[kLoads];
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) v[i] = load_pack<G, kVec>(g + ((int64_t)i * kAdamThreads + threadIdx.x) * kVec);
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+        for (int k = 0; k < kVec; ++k) {
+          const float x = to_float(v[i].e[k]);
+          sum = fmaf(x, x, sum);
+        }
+    } else {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int e = i * kAdamThreads + threadIdx.x;
+        x[i] = e < left ? to_float(g[e]) : 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], sum);
+    }
+    acc += (double)sum;
+  }
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, off);
+  if ((threadIdx.x & 31) == 0) part_s[threadIdx.x >> 5] = acc;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double total = 0.0;
+    for (int w = 0; w < kAdamChunkBlocks; ++w) total += part_s[w];
+    partials[blockIdx.x] = total;
+  }
+}
+
+// ---- the update ------------------------------------------------------------------------------------------------------
+
+struct AdamStepArgs {
+  const AdamTensor* tensors;
+  const AdamChunk* chunks;
+  const void* flat;            // nullptr: the tensors' bound gradients
+  void* exp_avg;
+  void* exp_avg_sq;
+  int16_t* base;               // two per block: m's, v's (8-bit states)
+  const AdamScalars* scalars;
+  float beta1, one_minus_beta1, beta2, one_minus_beta2, eps, lr;
+};
+
+// A lane's eight elements of its warp's block: two groups of four consecutive ones (VEC), or every 32nd (any alignment,
+// and blocks that the tensor does not fill).
+template <bool VEC>
+__device__ __forceinline__ int lane_element(int lane, int i) {
+  return VEC ? ((i >> 2) * 32 + lane) * 4 + (i & 3) : i * 32 + lane;
+}
+
+template <bool VEC, typename T>
+__device__ __forceinline__ void load8(T (&x)[8], const T* p, int lane, int n) {
+  if constexpr (VEC) {
+    constexpr int kVec = sizeof(T) <= 4 ? 4 : 2;       // at most 16 bytes an access
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int q = 0; q < 4 / kVec; ++q) {
+        const Pack<T, kVec> v = load_pack<T, kVec>(p + (h * 32 + lane) * 4 + q * kVec);
+#pragma unroll
+        for (int k = 0; k < kVec; ++k) x[h * 4 + q * kVec + k] = v.e[k];
+      }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int e = i * 32 + lane;
+      x[i] = e < n ? p[e] : T(0.0f);
+    }
+  }
+}
+
+template <bool VEC, typename T>
+__device__ __forceinline__ void store8(T* p, const T (&x)[8], int lane, int n) {
+  if constexpr (VEC) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      Pack<T, 4> v;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v.e[k] = x[h * 4 + k];
+      store_pack<T, 4>(p + (h * 32 + lane) * 4, v);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int e = i * 32 + lane;
+      if (e < n) p[e] = x[i];
+    }
+  }
+}
+
+template <int BITS, typename G, bool VEC>
+__device__ __forceinline__ void adam_block(const AdamStepArgs& a, const AdamTensor& t, const AdamScalars& s, const G* grad, int64_t first, int64_t block,
+                                           int lane, int n) {
+  float p[8], m[8], v[8];
+  G g[8];
+  load8<VEC>(p, (const float*)t.p + first, lane, n);
+  load8<VEC>(g, grad + first, lane, n);
+  const int64_t slot = block * kAdamBlock;
+  if constexpr (BITS == 32) {
+    load8<VEC>(m, (const float*)a.exp_avg + slot, lane, kAdamBlock);
+    load8<VEC>(v, (const float*)a.exp_avg_sq + slot, lane, kAdamBlock);
+  } else {
+    uint8_t mc[8], vc[8];
+    load8<VEC>(mc, (const uint8_t*)a.exp_avg + slot, lane, kAdamBlock);
+    load8<VEC>(vc, (const uint8_t*)a.exp_avg_sq + slot, lane, kAdamBlock);
+    const Pack<int16_t, 2> base = load_pack<int16_t, 2>(a.base + 2 * block);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float mag = state_value(mc[i] & 127u, base.e[0]);
+      m[i] = (mc[i] & 128u) ? -mag : mag;
+      v[i] = state_value(vc[i], base.e[1]);
+    }
+  }
+  const float decay = 1.0f - a.lr * t.weight_decay;
+  const float step = a.lr * s.inv_bc1;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float gi = to_float(g[i]) * s.grad_scale;
+    m[i] = a.beta1 * m[i] + a.one_minus_beta1 * gi;
+    v[i] = a.beta2 * v[i] + a.one_minus_beta2 * gi * gi;
+    p[i] = p[i] * decay - step * m[i] / (sqrtf(v[i]) * s.inv_sqrt_bc2 + a.eps);
+  }
+  store8<VEC>(t.p + first, p, lane, n);
+  if (t.copy) {
+    __nv_bfloat16 c[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = from_float<__nv_bfloat16>(p[i]);
+    store8<VEC>(t.copy + first, c, lane, n);
+  }
+  if constexpr (BITS == 32) {
+    store8<VEC>((float*)a.exp_avg + slot, m, lane, kAdamBlock);
+    store8<VEC>((float*)a.exp_avg_sq + slot, v, lane, kAdamBlock);
+  } else {
+    uint32_t mbits = 0, vbits = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      mbits = max(mbits, finite_bits(__float_as_uint(m[i]) & 0x7FFFFFFFu));
+      vbits = max(vbits, finite_bits(__float_as_uint(v[i]) & 0x7FFFFFFFu));
+    }
+    const int mbase = window_base(__reduce_max_sync(0xffffffffu, mbits), 127u);
+    const int vbase = window_base(__reduce_max_sync(0xffffffffu, vbits), 255u);
+    uint8_t mc[8], vc[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t r = slot_random(s.key, slot + lane_element<VEC>(lane, i));
+      const uint32_t sign = __float_as_uint(m[i]) >> 31;
+      const int cm = max(state_code(__float_as_uint(m[i]) & 0x7FFFFFFFu, (r & 0xFFFFu) << 4, mbase, 127), 0);
+      const int cv = max(state_code(__float_as_uint(v[i]) & 0x7FFFFFFFu, (r >> 16) << 4, vbase, 255), v[i] != 0.0f ? 1 : 0);
+      mc[i] = (uint8_t)(cm | (cm ? sign << 7 : 0u));
+      vc[i] = (uint8_t)cv;
+    }
+    store8<VEC>((uint8_t*)a.exp_avg + slot, mc, lane, kAdamBlock);
+    store8<VEC>((uint8_t*)a.exp_avg_sq + slot, vc, lane, kAdamBlock);
+    if (lane == 0) {
+      Pack<int16_t, 2> base;
+      base.e[0] = (int16_t)mbase;
+      base.e[1] = (int16_t)vbase;
+      store_pack<int16_t, 2>(a.base + 2 * block, base);
+    }
+  }
+}
+
+template <int BITS, typename G>
+__global__ void __launch_bounds__(kAdamThreads) adam_step_kernel(AdamStepArgs a) {
+  const AdamChunk ch = a.chunks[blockIdx.x];
+  const AdamTensor t = a.tensors[ch.tensor];
+  const int lane = threadIdx.x & 31;
+  const int64_t local = (int64_t)ch.index * kAdamChunkBlocks + (threadIdx.x >> 5);     // block inside the tensor
+  const int64_t first = local * kAdamBlock;
+  const int64_t left = t.numel - first;
+  pdl_wait();
+  if (left <= 0 || a.scalars->skip) return;
+  const AdamScalars s = *a.scalars;
+  const G* grad = a.flat ? static_cast<const G*>(a.flat) + t.offset : static_cast<const G*>(t.grad);
+  const bool vec = left >= kAdamBlock && ((uintptr_t)t.p & 15) == 0 && ((uintptr_t)t.copy & 7) == 0 &&
+                   ((uintptr_t)grad & (sizeof(G) < 4 ? 7 : 15)) == 0;
+  if (vec) adam_block<BITS, G, true>(a, t, s, grad, first, t.first_block + local, lane, kAdamBlock);
+  else adam_block<BITS, G, false>(a, t, s, grad, first, t.first_block + local, lane, left < kAdamBlock ? (int)left : kAdamBlock);
+}
+
+// What the 8-bit state stands for, as bfloat16 (every value of the grid is one): blocks x 256.
+__global__ void __launch_bounds__(256) adam_moments_kernel(const uint8_t* __restrict__ m, const uint8_t* __restrict__ v, const int16_t* __restrict__ base,
+                                                           int64_t n_quads, __nv_bfloat16* __restrict__ m_out, __nv_bfloat16* __restrict__ v_out) {
+  for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < n_quads; q += (int64_t)gridDim.x * 256) {
+    const Pack<int16_t, 2> b = load_pack<int16_t, 2>(base + 2 * (q / (kAdamBlock / 4)));
+    const Pack<uint8_t, 4> mc = load_pack<uint8_t, 4>(m + 4 * q), vc = load_pack<uint8_t, 4>(v + 4 * q);
+    Pack<__nv_bfloat16, 4> mo, vo;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float mag = state_value(mc.e[k] & 127u, b.e[0]);
+      mo.e[k] = from_float<__nv_bfloat16>((mc.e[k] & 128u) ? -mag : mag);
+      vo.e[k] = from_float<__nv_bfloat16>(state_value(vc.e[k], b.e[1]));
+    }
+    store_pack<__nv_bfloat16, 4>(m_out + 4 * q, mo);
+    store_pack<__nv_bfloat16, 4>(v_out + 4 * q, vo);
+  }
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------
+
+static int adam_upload_scalars(solon_adamw* o, int64_t step) {
+  AdamScalars s = {};
+  s.b1t = pow(o->beta1, (double)step);
+  s.b2t = pow(o->beta2, (double)step);
+  s.applied = step;
+  SOLON_CUDA_TRY(cudaMemcpy(o->d_scalars, &s, sizeof(s), cudaMemcpyHostToDevice));
+  return SOLON_OK;
+}
+
+static void adam_free(solon_adamw* o) {
+  cudaFree(o->d_tensors);
+  cudaFree(o->d_chunks);
+  cudaFree(o->d_scalars);
+  cudaFree(o->d_partials);
+  (void)cudaGetLastError();
+}
+
+template <typename T>
+static int adam_alloc(T** ptr, size_t count) {
+  cudaError_t err = cudaMalloc((void**)ptr, (count ? count : 1) * sizeof(T));
+  if (err == cudaSuccess) return SOLON_OK;
+  (void)cudaGetLastError();
+  *ptr = nullptr;
+  return err == cudaErrorMemoryAllocation ? SOLON_ERR_NOMEM : SOLON_ERR_CUDA;
+}
+
+static int64_t adam_blocks(int64_t numel) { return (numel + kAdamBlock - 1) / kAdamBlock; }
+
+static int adam_create(solon_adamw* o, const int64_t* numel, float* const* params, void* const* copies, const float* weight_decay) {
+  std::vector<AdamChunk> chunks;
+  o->tensors.resize((size_t)o->n_tensors);
+  for (int i = 0; i < o->n_tensors; ++i) {
+    AdamTensor& t = o->tensors[(size_t)i];
+    t = AdamTensor();
+    t.p = params[i];
+    t.copy = copies ? static_cast<__nv_bfloat16*>(copies[i]) : nullptr;
+    t.offset = o->total;
+    t.numel = numel[i];
+    t.first_block = o->n_blocks;
+    t.weight_decay = weight_decay ? weight_decay[i] : 0.0f;
+    o->total += numel[i];
+    o->n_blocks += adam_blocks(numel[i]);
+    const int64_t n = (adam_blocks(numel[i]) + kAdamChunkBlocks - 1) / kAdamChunkBlocks;
+    for (int64_t c = 0; c < n; ++c) chunks.push_back({i, (int)c});
+  }
+  o->n_chunks = (int64_t)chunks.size();
+  if (o->n_chunks > 0x7fffffffLL) return SOLON_ERR_INVALID_ARG;
+  o->norm_grid = o->num_sms * 4;
+  if (o->norm_grid > o->n_chunks) o->norm_grid = o->n_chunks ? (int)o->n_chunks : 1;
+  int rc;
+  if ((rc = adam_alloc(&o->d_tensors, o->tensors.size()))) return rc;
+  if ((rc = adam_alloc(&o->d_chunks, chunks.size()))) return rc;
+  if ((rc = adam_alloc(&o->d_scalars, 1))) return rc;
+  if ((rc = adam_alloc(&o->d_partials, (size_t)o->norm_grid))) return rc;
+  SOLON_CUDA_TRY(cudaMemcpy(o->d_tensors, o->tensors.data(), o->tensors.size() * sizeof(AdamTensor), cudaMemcpyHostToDevice));
+  if (!chunks.empty()) SOLON_CUDA_TRY(cudaMemcpy(o->d_chunks, chunks.data(), chunks.size() * sizeof(AdamChunk), cudaMemcpyHostToDevice));
+  return adam_upload_scalars(o, 0);
+}
+
+template <typename G>
+static int adam_norm(solon_adamw* o, const void* flat, cudaStream_t stream) {
+  return launch_dependent(adam_norm_kernel<G>, dim3((unsigned)o->norm_grid), dim3(kAdamThreads), 0, stream, (const AdamTensor*)o->d_tensors,
+                          (const AdamChunk*)o->d_chunks, o->n_chunks, static_cast<const G*>(flat), o->d_partials);
+}
+
+template <typename G>
+static int adam_update(solon_adamw* o, const AdamStepArgs& a, cudaStream_t stream) {
+  const dim3 grid((unsigned)o->n_chunks), block(kAdamThreads);
+  if (o->bits == 32) return launch_dependent(adam_step_kernel<32, G>, grid, block, 0, stream, a);
+  return launch_dependent(adam_step_kernel<8, G>, grid, block, 0, stream, a);
+}
+
+}  // namespace solon
+
+using namespace solon;
+
+extern "C" {
+
+int64_t solon_adamw_state_blocks(int n_tensors, const int64_t* numel) {
+  if (n_tensors < 1 || !numel) return SOLON_ERR_INVALID_ARG;
+  int64_t blocks = 0;
+  for (int i = 0; i < n_tensors; ++i) {
+    if (numel[i] < 0 || numel[i] > SOLON_ADAMW_MAX_NUMEL || blocks > SOLON_ADAMW_MAX_NUMEL) return SOLON_ERR_INVALID_ARG;
+    blocks += adam_blocks(numel[i]);
+  }
+  return blocks;
+}
+
+int solon_adamw_create(int n_tensors, const int64_t* numel, float* const* params, void* const* copies, const float* weight_decay, int state_bits,
+                       void* exp_avg, void* exp_avg_sq, int16_t* base, double beta1, double beta2, double eps, uint64_t seed, solon_adamw** out) {
+  if (!out) return SOLON_ERR_INVALID_ARG;
+  *out = nullptr;
+  if (!params || !exp_avg || !exp_avg_sq || (state_bits != 32 && state_bits != 8) || (state_bits == 8 && !base)) return SOLON_ERR_INVALID_ARG;
+  if (solon_adamw_state_blocks(n_tensors, numel) < 0) return SOLON_ERR_INVALID_ARG;
+  if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !((float)eps > 0.0f && eps < INFINITY)) return SOLON_ERR_INVALID_ARG;
+  if (((uintptr_t)exp_avg | (uintptr_t)exp_avg_sq) & 15 || ((uintptr_t)base & 3)) return SOLON_ERR_INVALID_ARG;
+  for (int i = 0; i < n_tensors; ++i) {
+    if (numel[i] > 0 && (!params[i] || ((uintptr_t)params[i] & 3))) return SOLON_ERR_INVALID_ARG;
+    if (copies && copies[i] && ((uintptr_t)copies[i] & 1)) return SOLON_ERR_INVALID_ARG;
+    if (weight_decay && !(weight_decay[i] >= 0.0f && weight_decay[i] < INFINITY)) return SOLON_ERR_INVALID_ARG;
+  }
+  int device = 0, sms = 0;
+  SOLON_CUDA_TRY(cudaGetDevice(&device));
+  SOLON_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
+  solon_adamw* o = new (std::nothrow) solon_adamw();
+  if (!o) return SOLON_ERR_NOMEM;
+  o->n_tensors = n_tensors;
+  o->bits = state_bits;
+  o->device = device;
+  o->num_sms = sms;
+  o->beta1 = beta1;
+  o->beta2 = beta2;
+  o->eps = eps;
+  o->seed = seed;
+  o->exp_avg = exp_avg;
+  o->exp_avg_sq = exp_avg_sq;
+  o->base = base;
+  int rc;
+  try {
+    rc = adam_create(o, numel, params, copies, weight_decay);
+  } catch (...) {
+    rc = SOLON_ERR_NOMEM;
+  }
+  if (rc) {
+    adam_free(o);
+    delete o;
+    return rc;
+  }
+  *out = o;
+  return SOLON_OK;
+}
+
+int solon_adamw_destroy(solon_adamw* opt) {
+  if (!opt) return SOLON_ERR_INVALID_ARG;
+  adam_free(opt);      // cudaFree waits for work in flight
+  delete opt;
+  return SOLON_OK;
+}
+
+int solon_adamw_bind_grads(solon_adamw* opt, const void* const* grads, int grad_dtype) {
+  if (!opt || !grads || (grad_dtype != SOLON_F32 && grad_dtype != SOLON_F64 && grad_dtype != SOLON_BF16)) return SOLON_ERR_INVALID_ARG;
+  const uintptr_t size = grad_dtype == SOLON_F64 ? 8 : grad_dtype == SOLON_F32 ? 4 : 2;
+  for (int i = 0; i < opt->n_tensors; ++i)
+    if (opt->tensors[(size_t)i].numel > 0 && (!grads[i] || ((uintptr_t)grads[i] & (size - 1)))) return SOLON_ERR_INVALID_ARG;
+  for (int i = 0; i < opt->n_tensors; ++i) opt->tensors[(size_t)i].grad = grads[i];
+  SOLON_CUDA_TRY(cudaDeviceSynchronize());     // steps in flight read the table
+  SOLON_CUDA_TRY(cudaMemcpy(opt->d_tensors, opt->tensors.data(), opt->tensors.size() * sizeof(AdamTensor), cudaMemcpyHostToDevice));
+  opt->grads_bound = 1;
+  opt->grad_dtype = grad_dtype;
+  return SOLON_OK;
+}
+
+int solon_adamw_set_step(solon_adamw* opt, int64_t step) {
+  if (!opt || step < 0) return SOLON_ERR_INVALID_ARG;
+  SOLON_CUDA_TRY(cudaDeviceSynchronize());
+  return adam_upload_scalars(opt, step);
+}
+
+int solon_adamw_get_steps(solon_adamw* opt, int64_t* applied, int64_t* skipped) {
+  if (!opt || !applied || !skipped) return SOLON_ERR_INVALID_ARG;
+  AdamScalars s;
+  SOLON_CUDA_TRY(cudaDeviceSynchronize());
+  SOLON_CUDA_TRY(cudaMemcpy(&s, opt->d_scalars, sizeof(s), cudaMemcpyDeviceToHost));
+  *applied = s.applied;
+  *skipped = s.skipped;
+  return SOLON_OK;
+}
+
+int solon_adamw_step(solon_adamw* opt, const void* grad, int grad_dtype, double grad_scale, double lr, double max_norm, float* grad_norm,
+                     const solon_plan* guard, void* cuda_stream) {
+  if (!opt) return SOLON_ERR_INVALID_ARG;
+  if (!grad) {
+    if (!opt->grads_bound) return SOLON_ERR_INVALID_ARG;
+    grad_dtype = opt->grad_dtype;
+  }
+  if (grad_dtype != SOLON_F32 && grad_dtype != SOLON_F64 && grad_dtype != SOLON_BF16) return SOLON_ERR_INVALID_ARG;
+  const uintptr_t size = grad_dtype == SOLON_F64 ? 8 : grad_dtype == SOLON_F32 ? 4 : 2;
+  if ((uintptr_t)grad & (size - 1) || ((uintptr_t)grad_norm & 3)) return SOLON_ERR_INVALID_ARG;
+  if (!(fabs(grad_scale) < INFINITY) || !(lr >= 0.0 && lr < INFINITY) || !(max_norm >= 0.0 && max_norm < INFINITY)) return SOLON_ERR_INVALID_ARG;
+  if (grad_norm && max_norm == 0.0) return SOLON_ERR_INVALID_ARG;
+  if (guard && guard->device != opt->device) return SOLON_ERR_INVALID_ARG;
+  cudaStream_t stream = (cudaStream_t)cuda_stream;
+  int rc;
+  AdamControlArgs c = {};
+  c.s = opt->d_scalars;
+  c.partials = opt->d_partials;
+  c.n_partials = max_norm > 0.0 ? opt->norm_grid : 0;
+  c.norm_out = grad_norm;
+  c.grad_scale = grad_scale;
+  c.max_norm = max_norm;
+  c.beta1 = opt->beta1;
+  c.beta2 = opt->beta2;
+  c.seed = opt->seed;
+  if (guard) {
+    c.guard_status = guard->d_status;
+    c.guard_t = guard->d_t_acc;
+    c.guard_groups = guard->q;
+  }
+  if (max_norm > 0.0) {
+    rc = grad_dtype == SOLON_F32 ? adam_norm<float>(opt, grad, stream) : grad_dtype == SOLON_F64 ? adam_norm<double>(opt, grad, stream)
+                                                                                                  : adam_norm<__nv_bfloat16>(opt, grad, stream);
+    if (rc) return rc;
+  }
+  if ((rc = launch_dependent(adam_control_kernel, dim3(1), dim3(256), 0, stream, c))) return rc;
+  if (opt->n_chunks == 0) return SOLON_OK;
+  AdamStepArgs a = {};
+  a.tensors = opt->d_tensors;
+  a.chunks = opt->d_chunks;
+  a.flat = grad;
+  a.exp_avg = opt->exp_avg;
+  a.exp_avg_sq = opt->exp_avg_sq;
+  a.base = opt->base;
+  a.scalars = opt->d_scalars;
+  a.beta1 = (float)opt->beta1;
+  a.one_minus_beta1 = (float)(1.0 - opt->beta1);
+  a.beta2 = (float)opt->beta2;
+  a.one_minus_beta2 = (float)(1.0 - opt->beta2);
+  a.eps = (float)opt->eps;
+  a.lr = (float)lr;
+  return grad_dtype == SOLON_F32 ? adam_update<float>(opt, a, stream) : grad_dtype == SOLON_F64 ? adam_update<double>(opt, a, stream)
+                                                                                                 : adam_update<__nv_bfloat16>(opt, a, stream);
+}
+
+int solon_adamw_moments(solon_adamw* opt, void* exp_avg_out, void* exp_avg_sq_out, void* cuda_stream) {
+  if (!opt || opt->bits != 8 || !exp_avg_out || !exp_avg_sq_out) return SOLON_ERR_INVALID_ARG;
+  if (((uintptr_t)exp_avg_out | (uintptr_t)exp_avg_sq_out) & 7) return SOLON_ERR_INVALID_ARG;
+  const int64_t quads = opt->n_blocks * (kAdamBlock / 4);
+  if (quads == 0) return SOLON_OK;
+  const int64_t want = (quads + 255) / 256, cap = (int64_t)opt->num_sms * 16;
+  adam_moments_kernel<<<(unsigned)(want < cap ? want : cap), 256, 0, (cudaStream_t)cuda_stream>>>(
+      (const uint8_t*)opt->exp_avg, (const uint8_t*)opt->exp_avg_sq, opt->base, quads, (__nv_bfloat16*)exp_avg_out, (__nv_bfloat16*)exp_avg_sq_out);
+  SOLON_CUDA_TRY(cudaGetLastError());
+  return SOLON_OK;
+}
+
+}  // extern "C"
