@@ -39,4 +39,143 @@ __device__ __forceinline__ void store_pack(T* p, const Pack<T, N>& v) {
   *reinterpret_cast<Pack<T, N>*>(p) = v;
 }
 
+// ---- 16 bytes of a row that is read once -----------------------------------------------------------------------------
+
+__device__ __forceinline__ uint4 load16_once(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+
+// The elements of 16 bytes as float32, and their largest value (NaN if there is one).
+template <typename T>
+struct Word16;
+
+template <>
+struct Word16<float> {
+  static constexpr int kCount = 4;
+  static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[4]) {
+    x[0] = __uint_as_float(v.x);
+    x[1] = __uint_as_float(v.y);
+    x[2] = __uint_as_float(v.z);
+    x[3] = __uint_as_float(v.w);
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&x)[4]) {
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  }
+  static __device__ __forceinline__ float largest(const uint4& v) {
+    float m;
+    asm("{\n\t.reg .f32 a, b;\n\tmax.NaN.f32 a, %1, %2;\n\tmax.NaN.f32 b, %3, %4;\n\tmax.NaN.f32 %0, a, b;\n\t}"
+        : "=f"(m)
+        : "f"(__uint_as_float(v.x)), "f"(__uint_as_float(v.y)), "f"(__uint_as_float(v.z)), "f"(__uint_as_float(v.w)));
+    return m;
+  }
+};
+
+template <>
+struct Word16<__nv_bfloat16> {
+  static constexpr int kCount = 8;
+  static __device__ __forceinline__ void pair(uint32_t w, float& a, float& b) {
+    a = __uint_as_float(w << 16);
+    b = __uint_as_float(w & 0xFFFF0000u);
+  }
+  static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[8]) {
+    pair(v.x, x[0], x[1]);
+    pair(v.y, x[2], x[3]);
+    pair(v.z, x[4], x[5]);
+    pair(v.w, x[6], x[7]);
+  }
+  static __device__ __forceinline__ uint32_t join(float a, float b) {
+    uint32_t w;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(b), "f"(a));
+    return w;
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&x)[8]) { return make_uint4(join(x[0], x[1]), join(x[2], x[3]), join(x[4], x[5]), join(x[6], x[7])); }
+  static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+    uint32_t m;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
+    return m;
+  }
+  static __device__ __forceinline__ float largest(const uint4& v) {
+    const uint32_t m = max2(max2(v.x, v.y), max2(v.z, v.w));
+    float a, b, r;
+    pair(m, a, b);
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+  }
+};
+
+template <>
+struct Word16<__half> {
+  static constexpr int kCount = 8;
+  static __device__ __forceinline__ void pair(uint32_t w, float& a, float& b) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    a = f.x;
+    b = f.y;
+  }
+  static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[8]) {
+    pair(v.x, x[0], x[1]);
+    pair(v.y, x[2], x[3]);
+    pair(v.z, x[4], x[5]);
+    pair(v.w, x[6], x[7]);
+  }
+  static __device__ __forceinline__ uint32_t join(float a, float b) {
+    uint32_t w;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(b), "f"(a));
+    return w;
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&x)[8]) { return make_uint4(join(x[0], x[1]), join(x[2], x[3]), join(x[4], x[5]), join(x[6], x[7])); }
+  static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+    uint32_t m;
+    asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
+    return m;
+  }
+  static __device__ __forceinline__ float largest(const uint4& v) {
+    const uint32_t m = max2(max2(v.x, v.y), max2(v.z, v.w));
+    float a, b, r;
+    pair(m, a, b);
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+  }
+};
+
+// Two float32 at a time (one instruction each on sm_100).
+struct Float2 {
+  unsigned long long v;
+};
+__device__ __forceinline__ Float2 pack2(float a, float b) {
+  Float2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpack2(Float2 x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v)); }
+__device__ __forceinline__ Float2 add2(Float2 a, Float2 b) {
+  Float2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Float2 mul2(Float2 a, Float2 b) {
+  Float2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Float2 fma2(Float2 a, Float2 b, Float2 c) {
+  Float2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+
+// 2^x by the hardware's approximation (two units in the last place), 0 below 2^-126.
+__device__ __forceinline__ float exp2_fast(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
 }  // namespace solon
