@@ -217,17 +217,20 @@ def _dtype_code(dtype) -> int:
 def _current_stream(device) -> int:
     import torch
 
-    if device.index != torch.cuda.current_device():
+    index = device.index
+    if index != torch.cuda.current_device():
         raise ValueError(f"tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
-    return torch.cuda.current_stream().cuda_stream
+    return torch._C._cuda_getCurrentRawStream(index)      # torch.cuda.current_stream().cuda_stream, a Stream object less (3 us)
 
 
-def _matrix(t, name: str, shape=None, dtype=None, device=None):
-    """(pointer, pitch) of a CUDA matrix whose rows are contiguous."""
+def _matrix(t, name: str, like=None):
+    """(pointer, pitch) of a CUDA matrix whose rows are contiguous; `like`: a matrix it has to equal in shape, type and place."""
+    if like is not None and (t.shape != like.shape or t.dtype != like.dtype or t.device != like.device):
+        raise ValueError(f"{name}: expected {tuple(like.shape)} {like.dtype} on {like.device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
     if t.dim() != 2 or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA matrix (rows x columns)")
-    if (shape is not None and tuple(t.shape) != tuple(shape)) or (dtype is not None and t.dtype != dtype) or (device is not None and t.device != device):
-        raise ValueError(f"{name}: expected {tuple(shape) if shape else 'any shape'} {dtype} on {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    if t.is_contiguous():
+        return t.data_ptr(), t.shape[1]
     rows, cols = t.shape
     pitch, step = t.stride()
     if (step != 1 and cols > 1) or (pitch < cols and rows > 1):
@@ -258,18 +261,19 @@ def solon_layernorm_forward(x, weight=None, bias=None, eps: float = 1e-5, y=None
 
     px, x_pitch = _matrix(x, "x")
     rows, cols = x.shape
-    stream = _current_stream(x.device)
+    device, f32 = x.device, torch.float32
+    stream = _current_stream(device)
     if y is None:
-        y = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+        y = x.new_empty((rows, cols))
     if mean is None:
-        mean = torch.empty(rows, dtype=torch.float32, device=x.device)
+        mean = x.new_empty((rows,), dtype=f32)
     if rstd is None:
-        rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
-    py, y_pitch = _matrix(y, "y", x.shape, x.dtype, x.device)
+        rstd = x.new_empty((rows,), dtype=f32)
+    py, y_pitch = _matrix(y, "y", x)
     pw, pb, code = _params(weight, bias, cols, x)
     _check(lib().solon_layernorm_forward(px, x_pitch, _dtype_code(x.dtype), pw, pb, code, rows, cols, eps, py, y_pitch,
-                                         _vector(mean, "mean", rows, torch.float32, x.device),
-                                         _vector(rstd, "rstd", rows, torch.float32, x.device), stream), "solon_layernorm_forward")
+                                         _vector(mean, "mean", rows, f32, device), _vector(rstd, "rstd", rows, f32, device), stream),
+           "solon_layernorm_forward")
     return y, mean, rstd
 
 
@@ -281,34 +285,37 @@ def solon_layernorm_backward(dy, x, mean, rstd, weight=None, partitions: int = 1
 
     px, x_pitch = _matrix(x, "x")
     rows, cols = x.shape
-    pdy, dy_pitch = _matrix(dy, "dy", x.shape, x.dtype, x.device)
-    stream = _current_stream(x.device)
+    device, f32 = x.device, torch.float32
+    pdy, dy_pitch = _matrix(dy, "dy", x)
+    stream = _current_stream(device)
     if dx is None:
-        dx = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-    pdx, dx_pitch = _matrix(dx, "dx", x.shape, x.dtype, x.device)
+        dx = x.new_empty((rows, cols))
+    pdx, dx_pitch = _matrix(dx, "dx", x)
     pw, _, code = _params(weight, None, cols, x)
     pdw = pdb = workspace = None
     grad_pitch, grad_code, n_bytes = cols, F32, 0
     if param_grads:
         like = dweight if dweight is not None else dbias
         if like is None:
-            dweight, dbias = torch.empty((2, partitions, cols), dtype=torch.float32, device=x.device).unbind(0)
+            dweight, dbias = x.new_empty((2, partitions, cols), dtype=f32).unbind(0)
         elif dweight is None:
-            dweight = torch.empty_strided(like.shape, like.stride(), dtype=like.dtype, device=x.device)
+            dweight = torch.empty_strided(like.shape, like.stride(), dtype=like.dtype, device=device)
         elif dbias is None:
-            dbias = torch.empty_strided(like.shape, like.stride(), dtype=like.dtype, device=x.device)
-        pdw, grad_pitch = _matrix(dweight, "dweight", (partitions, cols), None, x.device)
-        pdb, other_pitch = _matrix(dbias, "dbias", (partitions, cols), dweight.dtype, x.device)
+            dbias = torch.empty_strided(like.shape, like.stride(), dtype=like.dtype, device=device)
+        if dweight.shape[0] != partitions or dweight.shape[-1] != cols or dweight.device != device:
+            raise ValueError(f"dweight: expected {partitions} x {cols} on {device}, got {tuple(dweight.shape)} on {dweight.device}")
+        pdw, grad_pitch = _matrix(dweight, "dweight")
+        pdb, other_pitch = _matrix(dbias, "dbias", dweight)
         if grad_pitch != other_pitch:
             raise ValueError("dweight and dbias must have the same row pitch")
         grad_code = _dtype_code(dweight.dtype)
         n_bytes = lib().solon_layernorm_backward_workspace(rows, cols, partitions)
         if n_bytes > 0:
-            workspace = torch.empty(n_bytes // 4, dtype=torch.float32, device=x.device)
-    _check(lib().solon_layernorm_backward(pdy, dy_pitch, px, x_pitch, _dtype_code(x.dtype), pw, code,
-                                          _vector(mean, "mean", rows, torch.float32, x.device), _vector(rstd, "rstd", rows, torch.float32, x.device),
-                                          rows, cols, partitions, pdx, dx_pitch, pdw, pdb, grad_pitch, grad_code,
-                                          None if workspace is None else workspace.data_ptr(), n_bytes, stream), "solon_layernorm_backward")
+            workspace = x.new_empty((n_bytes // 4,), dtype=f32)
+    _check(lib().solon_layernorm_backward(pdy, dy_pitch, px, x_pitch, _dtype_code(x.dtype), pw, code, _vector(mean, "mean", rows, f32, device),
+                                          _vector(rstd, "rstd", rows, f32, device), rows, cols, partitions, pdx, dx_pitch, pdw, pdb, grad_pitch,
+                                          grad_code, None if workspace is None else workspace.data_ptr(), n_bytes, stream),
+           "solon_layernorm_backward")
     return dx, dweight, dbias
 
 
@@ -332,10 +339,10 @@ def solon_token_logprobs(logits, targets=None, top_k: int = 0) -> TokenLogprobs:
     rows, vocab = logits.shape
     device = logits.device
     stream = _current_stream(device)
-    stats = torch.empty((4, rows), dtype=torch.float32, device=device)
+    stats = logits.new_empty((4, rows), dtype=torch.float32)
     base, row_bytes = stats.data_ptr(), 4 * rows
-    top_ids = torch.empty((rows, top_k), dtype=torch.int64, device=device) if top_k > 0 else None
-    top_logp = torch.empty((rows, top_k), dtype=torch.float32, device=device) if top_k > 0 else None
+    top_ids = logits.new_empty((rows, top_k), dtype=torch.int64) if top_k > 0 else None
+    top_logp = logits.new_empty((rows, top_k), dtype=torch.float32) if top_k > 0 else None
     _check(lib().solon_token_logprobs(pz, pitch, _dtype_code(logits.dtype),
                                       None if targets is None else _vector(targets, "targets", rows, torch.int64, device), rows, vocab, top_k,
                                       None if targets is None else base, base + row_bytes, base + 2 * row_bytes, base + 3 * row_bytes,
@@ -355,8 +362,8 @@ def solon_token_logprobs_backward(logits, targets, peak, log_sum, grad_logp=None
     device = logits.device
     stream = _current_stream(device)
     if out is None:
-        out = torch.empty((rows, vocab), dtype=logits.dtype, device=device)
-    po, out_pitch = _matrix(out, "out", logits.shape, logits.dtype, device)
+        out = logits.new_empty((rows, vocab))
+    po, out_pitch = _matrix(out, "out", logits)
 
     def row_vector(t, name):
         return None if t is None else _vector(t, name, rows, torch.float32, device)

@@ -7,11 +7,15 @@
 //
 // Bound by memory: 2 (forward) and 3 (backward) accesses of the matrix against about 8 and 14 flops an element.
 //
-// Layout: a row belongs to a team of TPR threads that hold it in registers, up to 16 elements each (VEC neighbours an access);
-// teams of one warp meet in shuffles only, larger ones also in shared memory.  CTAs stay for many rows, so that weight and
-// bias are read once a CTA and the weight's gradient is summed in registers; only one partial sum per CTA and column leaves
-// it, added up per partition by a second kernel in a fixed order.
+// Layout: a row belongs to a team of TPR threads, 64 bytes of it each (four 16-byte words; fewer in rows of less than 2 KB), so
+// that a team's two reductions cost little beside the work on the elements.  Teams of one warp meet in shuffles only, larger ones
+// also in shared memory.  CTAs stay for many rows; every thread copies its own words of the next rows into shared memory
+// ahead of time (cp.async: it waits for its own copies only, no barrier), which keeps enough bytes on the way without registers
+// for them.  The weight's gradient is summed in registers over all rows of a CTA; only one partial sum per CTA and column
+// leaves it, added up per partition by a second kernel in a fixed order.
 #include <math.h>
+
+#include <type_traits>
 
 #include "elements.cuh"
 #include "solon_internal.h"
@@ -19,16 +23,19 @@
 
 namespace solon {
 
-constexpr int kLnElems = 16;                 // elements of a row per thread
-constexpr int kLnMaxTeam = 1024;
-constexpr int kLnMaxCols = kLnElems * kLnMaxTeam;      // wider rows take the streaming kernels
+constexpr int kLnThreads = 256;                // threads of a CTA, or one team if that is larger
+constexpr int kLnMaxCols = 16384;              // 1024 threads of 16 float32; wider rows take the streaming kernels
+constexpr int kLnForwardStages = 2;            // rows on the way per team beside the one that is worked on
+// Rows in shared memory per team in the backward pass, the one that is worked on among them.
+template <int TPR>
+constexpr int ln_backward_stages = TPR < 1024 ? 3 : 1;
 
 // Sum over the team, the result in every thread.  Teams of several warps alternate between two slots, so one barrier a
 // sum is enough: a slot is written again only after everybody has passed the barrier of the sum in between.
 template <int TPR, int N>
 __device__ __forceinline__ void team_sum(float (&v)[N], float* slots, int& turn, int team) {
 #pragma unroll
-  for (int off = (TPR < 32 ? TPR : 32) / 2; off > 0; off >>= 1)
+  for (int off = 16; off > 0; off >>= 1)
 #pragma unroll
     for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], off);
   if constexpr (TPR > 32) {
@@ -38,63 +45,57 @@ __device__ __forceinline__ void team_sum(float (&v)[N], float* slots, int& turn,
     turn ^= 1;
     if ((threadIdx.x & 31) == 0) {
 #pragma unroll
-      for (int k = 0; k < N; ++k) s[warp * N + k] = v[k];
+      for (int k = 0; k < N; ++k) s[k * kWarps + warp] = v[k];
     }
     asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "n"(TPR) : "memory");
 #pragma unroll
     for (int k = 0; k < N; ++k) {
       float sum = 0.0f;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) sum += s[w * N + k];
+      for (int w = 0; w < kWarps; ++w) sum += s[k * kWarps + w];
       v[k] = sum;
     }
   }
 }
 
-template <typename T, int VEC>
-__device__ __forceinline__ void load_row(float (&x)[kLnElems], const T* row, int64_t cols, int tid, int tpr) {
+__device__ __forceinline__ void copy16_async(void* dst_smem, const void* src, bool inside) {
+  const int bytes = inside ? 16 : 0;           // 0: the 16 bytes are filled with zeros, nothing is read
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst_smem)), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Weight or bias of N neighbouring columns: float32 or the matrix's type, at any alignment.
+template <typename T, int N>
+__device__ __forceinline__ void param_words(float (&w)[N], const void* p, bool f32, bool aligned, int c) {
+  const float* q = static_cast<const float*>(p) + c;
+  const T* r = static_cast<const T*>(p) + c;
+  if constexpr (N % 4 == 0) {
+    if (aligned) {
+      if (f32) {
 #pragma unroll
-  for (int i = 0; i < kLnElems / VEC; ++i) {
-    const int64_t c = ((int64_t)i * tpr + tid) * VEC;
-    if (c < cols) {
-      const Pack<T, VEC> v = load_pack<T, VEC>(row + c);
+        for (int i = 0; i < N; i += 4) {
+          const Pack<float, 4> v = load_pack<float, 4>(q + i);
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) x[i * VEC + k] = to_float(v.e[k]);
-    } else {
+          for (int k = 0; k < 4; ++k) w[i + k] = v.e[k];
+        }
+      } else {
+        const Pack<T, N> v = load_pack<T, N>(r);
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) x[i * VEC + k] = 0.0f;
+        for (int i = 0; i < N; ++i) w[i] = to_float(v.e[i]);
+      }
+      return;
     }
   }
+#pragma unroll
+  for (int i = 0; i < N; ++i) w[i] = f32 ? q[i] : to_float(r[i]);
 }
 
-template <typename T, int VEC>
-__device__ __forceinline__ void store_row(T* row, const float (&x)[kLnElems], int64_t cols, int tid, int tpr) {
-#pragma unroll
-  for (int i = 0; i < kLnElems / VEC; ++i) {
-    const int64_t c = ((int64_t)i * tpr + tid) * VEC;
-    if (c < cols) {
-      Pack<T, VEC> v;
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) v.e[k] = from_float<T>(x[i * VEC + k]);
-      store_pack<T, VEC>(row + c, v);
-    }
-  }
-}
-
-// Weight or bias of a thread's columns: float32 or the matrix's type, read element by element (once per CTA).
 __device__ __forceinline__ float param_at(const void* p, int is_f32, int dtype, int64_t c) {
   if (is_f32) return static_cast<const float*>(p)[c];
   if (dtype == SOLON_BF16) return to_float(static_cast<const __nv_bfloat16*>(p)[c]);
   return to_float(static_cast<const __half*>(p)[c]);
-}
-
-template <int VEC>
-__device__ __forceinline__ void load_params(float (&w)[kLnElems], const void* p, int is_f32, int dtype, float absent, int64_t cols, int tid, int tpr) {
-#pragma unroll
-  for (int i = 0; i < kLnElems; ++i) {
-    const int64_t c = ((int64_t)(i / VEC) * tpr + tid) * VEC + i % VEC;
-    w[i] = c < cols ? (p ? param_at(p, is_f32, dtype, c) : absent) : 0.0f;
-  }
 }
 
 struct LnForwardArgs {
@@ -106,40 +107,95 @@ struct LnForwardArgs {
   float* rstd;
   int64_t rows, cols, x_pitch, y_pitch;
   float eps;
-  int param_f32, dtype;
+  int param_f32, dtype, weight_aligned, bias_aligned;
 };
 
-template <typename T, int VEC, int TPR>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) ln_forward_kernel(LnForwardArgs a) {
-  __shared__ float slots[2 * 32];
-  const int tid = threadIdx.x & (TPR - 1), team = threadIdx.x / TPR, teams = blockDim.x / TPR;
+// VEC: neighbouring elements an access moves - 16 bytes, or one where rows are not made of 16-byte words at 16-byte
+// boundaries; those are loaded straight into registers.
+template <typename T, int VEC, int TPR, int ELEMS>
+__global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, TPR < 512 ? 4 : TPR < 1024 ? 2 : 1) ln_forward_kernel(LnForwardArgs a) {
+  constexpr int kGroups = ELEMS / VEC;         // accesses (with VEC > 1 words of 16 bytes)
+  constexpr int kBlock = TPR < kLnThreads ? kLnThreads : TPR;
+  extern __shared__ __align__(16) uint4 ring[];           // stages x words x threads
+  __shared__ __align__(16) float slots[2 * 32];
+  const int tid = threadIdx.x & (TPR - 1), team = threadIdx.x / TPR;
+  constexpr int kTeams = kBlock / TPR;
+  const int cols = (int)a.cols;
   const T* x = static_cast<const T*>(a.x);
   T* y = static_cast<T*>(a.y);
-  float w[kLnElems], b[kLnElems];
-  load_params<VEC>(w, a.weight, a.param_f32, a.dtype, 1.0f, a.cols, tid, TPR);
-  load_params<VEC>(b, a.bias, a.param_f32, a.dtype, 0.0f, a.cols, tid, TPR);
-  const float inv_n = 1.0f / (float)a.cols;
+  const float inv_n = 1.0f / (float)cols;
   int turn = 0;
-  for (int64_t row = (int64_t)blockIdx.x * teams + team; row < a.rows; row += (int64_t)gridDim.x * teams) {
-    float v[kLnElems];
-    load_row<T, VEC>(v, x + row * a.x_pitch, a.cols, tid, TPR);
+  const int64_t stride = (int64_t)gridDim.x * kTeams;
+  auto issue = [&](int64_t row, int stage) {
+    if constexpr (VEC > 1) {
+      if (row < a.rows) {
+        const T* from = x + row * a.x_pitch + tid * VEC;
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i) {
+          const bool inside = (i * TPR + tid) * VEC < cols;
+          copy16_async(ring + (stage * kGroups + i) * kBlock + threadIdx.x, inside ? from + i * TPR * VEC : x, inside);
+        }
+      }
+      copies_commit();
+    }
+  };
+  int64_t row = (int64_t)blockIdx.x * kTeams + team;
+  int stage = 0;
+#pragma unroll
+  for (int s = 0; s < kLnForwardStages; ++s) issue(row + s * stride, s);
+  for (; row < a.rows; row += stride) {
+    float v[ELEMS];
+    if constexpr (VEC > 1) {
+      copies_wait<kLnForwardStages - 1>();
+#pragma unroll
+      for (int i = 0; i < kGroups; ++i) {
+        float part[VEC];
+        Word16<T>::unpack(ring[(stage * kGroups + i) * kBlock + threadIdx.x], part);
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) v[i * VEC + k] = part[k];
+      }
+      issue(row + kLnForwardStages * stride, stage);      // into the words just read
+      stage = stage + 1 == kLnForwardStages ? 0 : stage + 1;
+    } else {
+      const T* from = x + row * a.x_pitch;
+#pragma unroll
+      for (int i = 0; i < ELEMS; ++i) v[i] = i * TPR + tid < cols ? to_float(from[i * TPR + tid]) : 0.0f;
+    }
     float sum[1] = {0.0f};
 #pragma unroll
-    for (int i = 0; i < kLnElems; ++i) sum[0] += v[i];
+    for (int i = 0; i < ELEMS; ++i) sum[0] += v[i];
     team_sum<TPR>(sum, slots, turn, team);
     const float mean = sum[0] * inv_n;
     float sq[1] = {0.0f};
 #pragma unroll
-    for (int i = 0; i < kLnElems; ++i) {
-      const int64_t c = ((int64_t)(i / VEC) * TPR + tid) * VEC;      // (VEC divides cols: a group is inside or outside)
-      v[i] -= mean;
-      if (c < a.cols) sq[0] = fmaf(v[i], v[i], sq[0]);
+    for (int i = 0; i < kGroups; ++i) {
+      if ((i * TPR + tid) * VEC < cols) {
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+          v[i * VEC + k] -= mean;
+          sq[0] = fmaf(v[i * VEC + k], v[i * VEC + k], sq[0]);
+        }
+      }
     }
     team_sum<TPR>(sq, slots, turn, team);
     const float rstd = rsqrtf(sq[0] * inv_n + a.eps);
+    T* to = y + row * a.y_pitch;
 #pragma unroll
-    for (int i = 0; i < kLnElems; ++i) v[i] = fmaf(v[i] * rstd, w[i], b[i]);
-    store_row<T, VEC>(y + row * a.y_pitch, v, a.cols, tid, TPR);
+    for (int i = 0; i < kGroups; ++i) {
+      const int c = (i * TPR + tid) * VEC;
+      if (c < cols) {
+        float w[VEC], b[VEC], out[VEC];
+        if (a.weight) param_words<T>(w, a.weight, a.param_f32, a.weight_aligned, c);
+        if (a.bias) param_words<T>(b, a.bias, a.param_f32, a.bias_aligned, c);
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+          out[k] = v[i * VEC + k] * rstd;
+          out[k] = fmaf(out[k], a.weight ? w[k] : 1.0f, a.bias ? b[k] : 0.0f);
+        }
+        if constexpr (VEC > 1) *reinterpret_cast<uint4*>(to + c) = Word16<T>::pack(out);
+        else to[c] = from_float<T>(out[0]);
+      }
+    }
     if (tid == 0) {
       if (a.mean) a.mean[row] = mean;
       if (a.rstd) a.rstd[row] = rstd;
@@ -158,7 +214,7 @@ struct LnBackwardArgs {
   void* dbias;
   float* partials;             // partitions x splits x 2 x cols (splits > 1)
   int64_t rows_per_part, cols, dy_pitch, x_pitch, dx_pitch, grad_pitch;
-  int splits, param_f32, dtype, grad_f64;
+  int splits, param_f32, dtype, grad_f64, weight_aligned;
 };
 
 __device__ __forceinline__ void store_grad(void* p, int f64, int64_t i, float v) {
@@ -166,60 +222,144 @@ __device__ __forceinline__ void store_grad(void* p, int f64, int64_t i, float v)
   else static_cast<float*>(p)[i] = v;
 }
 
-// CTA (split, partition): rows split * teams + team, stepping by splits * teams, of its partition.
-template <typename T, int VEC, int TPR>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) ln_backward_kernel(LnBackwardArgs a) {
-  extern __shared__ float combine[];           // teams x TPR x kLnElems (teams > 1)
-  __shared__ float slots[2 * 32 * 2];
-  const int tid = threadIdx.x & (TPR - 1), team = threadIdx.x / TPR, teams = blockDim.x / TPR;
-  const int split = blockIdx.x, part = blockIdx.y;
+// CTA (split, partition): rows split * teams + team, stepping by splits * teams, of its partition.  A row is gone through
+// twice, for the sums and for dx: its words stay in shared memory in between, which is what the registers could not hold
+// beside the sums of the weight's gradient.
+template <typename T, int VEC, int TPR, int ELEMS>
+__global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, TPR < 512 ? 2 : 1) ln_backward_kernel(LnBackwardArgs a) {
+  constexpr int kGroups = ELEMS / VEC;         // accesses (with VEC > 1 words of 16 bytes)
+  constexpr int kBlock = TPR < kLnThreads ? kLnThreads : TPR;
+  constexpr int kTeams = kBlock / TPR;
+  constexpr int kStages = ln_backward_stages<TPR>;
+  extern __shared__ __align__(16) uint4 ring[];           // stages x 2 (x, dy) x words x threads; teams' sums at the end
+  __shared__ __align__(16) float slots[2 * 32 * 2];
+  const int tid = threadIdx.x & (TPR - 1), team = threadIdx.x / TPR;
+  const int split = blockIdx.x, part = blockIdx.y, cols = (int)a.cols;
   const T* x = static_cast<const T*>(a.x);
   const T* dy = static_cast<const T*>(a.dy);
   T* dx = static_cast<T*>(a.dx);
-  float w[kLnElems], dw[kLnElems], db[kLnElems];
-  load_params<VEC>(w, a.weight, a.param_f32, a.dtype, 1.0f, a.cols, tid, TPR);
+  float dw[ELEMS], db[ELEMS];
 #pragma unroll
-  for (int i = 0; i < kLnElems; ++i) dw[i] = db[i] = 0.0f;
-  const float inv_n = 1.0f / (float)a.cols;
+  for (int i = 0; i < ELEMS; ++i) dw[i] = db[i] = 0.0f;
+  const float inv_n = 1.0f / (float)cols;
   int turn = 0;
-  for (int64_t r = (int64_t)split * teams + team; r < a.rows_per_part; r += (int64_t)a.splits * teams) {
-    const int64_t row = (int64_t)part * a.rows_per_part + r;
-    float xv[kLnElems], g[kLnElems];
-    load_row<T, VEC>(xv, x + row * a.x_pitch, a.cols, tid, TPR);
-    load_row<T, VEC>(g, dy + row * a.dy_pitch, a.cols, tid, TPR);
-    const float mean = a.mean[row], rstd = a.rstd[row];
+  const int64_t stride = (int64_t)a.splits * kTeams, end = (int64_t)(part + 1) * a.rows_per_part;
+  int64_t row = (int64_t)part * a.rows_per_part + (int64_t)split * kTeams + team;
+  float next_mean = 0.0f, next_rstd = 0.0f;               // of the row after the one that is worked on
+  auto issue = [&](int64_t at, int stage) {
+    if constexpr (VEC > 1) {
+      if (at < end) {
+        const T* from_x = x + at * a.x_pitch + tid * VEC;
+        const T* from_dy = dy + at * a.dy_pitch + tid * VEC;
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i) {
+          const bool inside = (i * TPR + tid) * VEC < cols;
+          uint4* to = ring + (stage * 2 * kGroups + i) * kBlock + threadIdx.x;
+          copy16_async(to, inside ? from_x + i * TPR * VEC : x, inside);
+          copy16_async(to + kGroups * kBlock, inside ? from_dy + i * TPR * VEC : x, inside);
+        }
+      }
+      copies_commit();
+    }
+  };
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s) issue(row + s * stride, s);
+  if (row < end) {
+    next_mean = a.mean[row];
+    next_rstd = a.rstd[row];
+  }
+  int stage = 0;
+  for (; row < end; row += stride) {
+    const float mean = next_mean, rstd = next_rstd;
+    if (row + stride < end) {
+      next_mean = a.mean[row + stride];
+      next_rstd = a.rstd[row + stride];
+    }
+    const T* row_x = x + row * a.x_pitch;
+    const T* row_dy = dy + row * a.dy_pitch;
+    float hold_x[VEC > 1 ? 1 : ELEMS], hold_g[VEC > 1 ? 1 : ELEMS];       // rows without words are held in registers
+    if constexpr (VEC == 1) {
+#pragma unroll
+      for (int i = 0; i < ELEMS; ++i) {
+        const int c = i * TPR + tid;
+        hold_x[i] = c < cols ? to_float(row_x[c]) : mean;
+        hold_g[i] = c < cols ? to_float(row_dy[c]) : 0.0f;
+      }
+    } else {
+      const int ahead = stage == 0 ? kStages - 1 : stage - 1;     // the words of the row before
+      issue(row + (kStages - 1) * stride, ahead);
+      copies_wait<kStages - 1>();
+    }
+    // group i of the row: xh, dy and w dy
+    auto group = [&](int i, float (&xh)[VEC], float (&g)[VEC], float (&wg)[VEC]) {
+      if constexpr (VEC > 1) {
+        Word16<T>::unpack(ring[(stage * 2 * kGroups + i) * kBlock + threadIdx.x], xh);
+        Word16<T>::unpack(ring[((stage * 2 + 1) * kGroups + i) * kBlock + threadIdx.x], g);
+      } else {
+        xh[0] = hold_x[i];
+        g[0] = hold_g[i];
+      }
+      if (a.weight) {
+        float w[VEC];
+        const int c = (i * TPR + tid) * VEC;
+        param_words<T>(w, a.weight, a.param_f32, a.weight_aligned, c < cols ? c : 0);
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) wg[k] = g[k] * w[k];
+      } else {
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) wg[k] = g[k];
+      }
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) xh[k] = (xh[k] - mean) * rstd;
+    };
     float s[2] = {0.0f, 0.0f};
 #pragma unroll
-    for (int i = 0; i < kLnElems; ++i) {       // (outside the row g and w are 0)
-      xv[i] = (xv[i] - mean) * rstd;
-      dw[i] = fmaf(g[i], xv[i], dw[i]);
-      db[i] += g[i];
-      g[i] *= w[i];
-      s[0] += g[i];
-      s[1] = fmaf(g[i], xv[i], s[1]);
+    for (int i = 0; i < kGroups; ++i) {        // (outside the row dy is 0)
+      float xh[VEC], g[VEC], wg[VEC];
+      group(i, xh, g, wg);
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) {
+        dw[i * VEC + k] = fmaf(g[k], xh[k], dw[i * VEC + k]);
+        db[i * VEC + k] += g[k];
+        s[0] += wg[k];
+        s[1] = fmaf(wg[k], xh[k], s[1]);
+      }
     }
     if (dx) {
       team_sum<TPR>(s, slots, turn, team);
       const float m0 = s[0] * inv_n, m1 = s[1] * inv_n;
+      T* to = dx + row * a.dx_pitch;
 #pragma unroll
-      for (int i = 0; i < kLnElems; ++i) g[i] = rstd * (g[i] - m0 - xv[i] * m1);
-      store_row<T, VEC>(dx + row * a.dx_pitch, g, a.cols, tid, TPR);
+      for (int i = 0; i < kGroups; ++i) {
+        const int c = (i * TPR + tid) * VEC;
+        if (c < cols) {
+          float xh[VEC], g[VEC], out[VEC];
+          group(i, xh, g, out);
+#pragma unroll
+          for (int k = 0; k < VEC; ++k) out[k] = rstd * (out[k] - m0 - xh[k] * m1);
+          if constexpr (VEC > 1) *reinterpret_cast<uint4*>(to + c) = Word16<T>::pack(out);
+          else to[c] = from_float<T>(out[0]);
+        }
+      }
     }
+    stage = stage + 1 == kStages ? 0 : stage + 1;
   }
   if (!a.dweight && !a.dbias) return;
-  if constexpr (TPR < 256) {                   // add the teams' sums, in team order
+  if constexpr (kTeams > 1) {                  // add the teams' sums, in team order
+    float* combine = reinterpret_cast<float*>(ring);
+    if constexpr (VEC > 1) copies_wait<0>();
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
       float* mine = which ? db : dw;
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < kLnElems; ++i) combine[(team * kLnElems + i) * TPR + tid] = mine[i];
+      for (int i = 0; i < ELEMS; ++i) combine[(team * ELEMS + i) * TPR + tid] = mine[i];
       __syncthreads();
       if (team == 0) {
 #pragma unroll
-        for (int i = 0; i < kLnElems; ++i) {
-          float sum = 0.0f;
-          for (int t = 0; t < teams; ++t) sum += combine[(t * kLnElems + i) * TPR + tid];
+        for (int i = 0; i < ELEMS; ++i) {
+          float sum = mine[i];
+          for (int t = 1; t < kTeams; ++t) sum += combine[(t * ELEMS + i) * TPR + tid];
           mine[i] = sum;
         }
       }
@@ -228,7 +368,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) ln_backward_kernel(LnBa
   }
   float* out = a.splits > 1 ? a.partials + ((int64_t)part * a.splits + split) * 2 * a.cols : nullptr;
 #pragma unroll
-  for (int i = 0; i < kLnElems; ++i) {
+  for (int i = 0; i < ELEMS; ++i) {
     const int64_t c = ((int64_t)(i / VEC) * TPR + tid) * VEC + i % VEC;
     if (c >= a.cols) continue;
     if (out) {
@@ -249,8 +389,10 @@ __global__ void __launch_bounds__(256) ln_param_grad_kernel(LnBackwardArgs a) {
   pdl_wait();
   const float* src = a.partials + (int64_t)part * a.splits * 2 * a.cols + c2;
   float sum = 0.0f;
-  if (c2 < 2 * a.cols)
+  if (c2 < 2 * a.cols) {
+#pragma unroll 4
     for (int s = warp; s < a.splits; s += 8) sum += src[(int64_t)s * 2 * a.cols];
+  }
   part_s[warp][lane] = sum;
   __syncthreads();
   if (warp != 0 || c2 >= 2 * a.cols) return;
@@ -349,18 +491,28 @@ __global__ void __launch_bounds__(256) ln_param_partials_wide_kernel(LnBackwardA
 
 // ---- host ------------------------------------------------------------------------------------------------------------
 
-static int ln_team(int64_t cols) {
+// Threads of a team for rows of `cols` elements, `most` of which a thread takes at most; short rows take a half or a quarter.
+struct LnTeam {
+  int threads, elems;
+};
+static LnTeam ln_team(int64_t cols, int most) {
+  if (cols <= 32 * (most / 4)) return {32, most / 4};
+  if (cols <= 32 * (most / 2)) return {32, most / 2};
   int team = 32;
-  while ((int64_t)team * kLnElems < cols) team *= 2;
-  return team;
+  while ((int64_t)team * most < cols) team *= 2;
+  return {team, most};
 }
 
 static int64_t ln_min(int64_t a, int64_t b) { return a < b ? a : b; }
 
-// CTAs that share a partition's rows: two per SM over all partitions, as long as every CTA has a row for each of its teams.
+// CTAs that share a partition's rows: as many as run at once (two per SM of 256 threads, one of more), shared by the
+// partitions - one more and the last would run alone after all others -, as long as every CTA has a row for each of its teams.
+constexpr int kLnSms = 148;
 static int ln_splits(int64_t rows_per_part, int64_t cols, int partitions) {
-  const int teams = cols > kLnMaxCols ? 1 : (ln_team(cols) < 256 ? 256 / ln_team(cols) : 1);
-  const int64_t want = (2 * 148 + partitions - 1) / partitions;
+  // (the workspace does not depend on type and alignment, so the number of teams is taken as of the smallest ones)
+  const int team = cols > kLnMaxCols ? 1024 : ln_team(cols, 32).threads;
+  const int teams = team < kLnThreads ? kLnThreads / team : 1;
+  const int64_t want = 2 * kLnSms / partitions;
   const int64_t most = (rows_per_part + teams - 1) / teams;
   const int64_t splits = ln_min(want, most);
   return splits < 1 ? 1 : (int)splits;
@@ -371,25 +523,47 @@ static bool vector_rows(const void* p, int64_t pitch, int64_t cols, int dtype) {
   return ((uintptr_t)p & 15) == 0 && pitch % vec == 0 && cols % vec == 0;
 }
 
-template <typename T, int VEC, int TPR>
+template <typename T, int VEC, int TPR, int ELEMS>
 static int ln_forward_launch(const LnForwardArgs& a, int sms, cudaStream_t stream) {
-  constexpr int kThreads = TPR < 256 ? 256 : TPR;
-  constexpr int kTeams = kThreads / TPR;
-  const int64_t want = (a.rows + kTeams - 1) / kTeams, cap = (int64_t)sms * (2048 / kThreads);
-  ln_forward_kernel<T, VEC, TPR><<<(unsigned)ln_min(want, cap), kThreads, 0, stream>>>(a);
+  constexpr int kBlock = TPR < kLnThreads ? kLnThreads : TPR;
+  constexpr int kTeams = kBlock / TPR;
+  constexpr size_t kSmem = VEC > 1 ? (size_t)kLnForwardStages * (ELEMS / VEC) * 16 * kBlock : 0;
+  if constexpr (kSmem > 40 * 1024) SOLON_CUDA_TRY(cudaFuncSetAttribute(ln_forward_kernel<T, VEC, TPR, ELEMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem));
+  const int64_t want = (a.rows + kTeams - 1) / kTeams, cap = (int64_t)sms * (TPR < 512 ? 4 : TPR < 1024 ? 2 : 1);
+  ln_forward_kernel<T, VEC, TPR, ELEMS><<<(unsigned)ln_min(want, cap), kBlock, kSmem, stream>>>(a);
   SOLON_CUDA_TRY(cudaGetLastError());
   return SOLON_OK;
 }
 
-template <typename T, int VEC>
-static int ln_forward_team(const LnForwardArgs& a, int sms, cudaStream_t stream) {
-  switch (ln_team(a.cols)) {
-    case 32: return ln_forward_launch<T, VEC, 32>(a, sms, stream);
-    case 64: return ln_forward_launch<T, VEC, 64>(a, sms, stream);
-    case 128: return ln_forward_launch<T, VEC, 128>(a, sms, stream);
-    case 256: return ln_forward_launch<T, VEC, 256>(a, sms, stream);
-    case 512: return ln_forward_launch<T, VEC, 512>(a, sms, stream);
-    default: return ln_forward_launch<T, VEC, 1024>(a, sms, stream);
+template <typename T, int VEC, int TPR, int ELEMS>
+static int ln_backward_launch(const LnBackwardArgs& a, int partitions, cudaStream_t stream) {
+  constexpr int kBlock = TPR < kLnThreads ? kLnThreads : TPR;
+  constexpr size_t kRing = VEC > 1 ? (size_t)ln_backward_stages<TPR> * 2 * (ELEMS / VEC) * 16 * kBlock : 0;
+  constexpr size_t kCombine = TPR < kBlock ? (size_t)kBlock * ELEMS * sizeof(float) : 0;
+  constexpr size_t kSmem = kRing > kCombine ? kRing : kCombine;
+  if constexpr (kSmem > 40 * 1024) SOLON_CUDA_TRY(cudaFuncSetAttribute(ln_backward_kernel<T, VEC, TPR, ELEMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem));
+  ln_backward_kernel<T, VEC, TPR, ELEMS><<<dim3((unsigned)a.splits, (unsigned)partitions), kBlock, kSmem, stream>>>(a);
+  SOLON_CUDA_TRY(cudaGetLastError());
+  return SOLON_OK;
+}
+
+// f(team size, elements of a thread), both as compile-time constants.  16 elements with 4-byte types, and where elements are
+// loaded one by one; 32 with 16-byte words of two-byte types.
+template <int MOST, typename F>
+static int ln_by_team(int64_t cols, F f) {
+  const LnTeam t = ln_team(cols, MOST);
+  switch (t.threads) {
+    case 32:
+      if (t.elems == MOST / 4) return f(std::integral_constant<int, 32>(), std::integral_constant<int, MOST / 4>());
+      if (t.elems == MOST / 2) return f(std::integral_constant<int, 32>(), std::integral_constant<int, MOST / 2>());
+      return f(std::integral_constant<int, 32>(), std::integral_constant<int, MOST>());
+    case 64: return f(std::integral_constant<int, 64>(), std::integral_constant<int, MOST>());
+    case 128: return f(std::integral_constant<int, 128>(), std::integral_constant<int, MOST>());
+    case 256: return f(std::integral_constant<int, 256>(), std::integral_constant<int, MOST>());
+    case 512: return f(std::integral_constant<int, 512>(), std::integral_constant<int, MOST>());
+    default:
+      if constexpr (MOST * 1024 <= kLnMaxCols) return f(std::integral_constant<int, 1024>(), std::integral_constant<int, MOST>());
+      else return SOLON_ERR_INTERNAL;          // 512 threads of 32 elements hold the widest row
   }
 }
 
@@ -401,30 +575,12 @@ static int ln_forward_t(const LnForwardArgs& a, int sms, cudaStream_t stream) {
     SOLON_CUDA_TRY(cudaGetLastError());
     return SOLON_OK;
   }
-  if (vector_rows(a.x, a.x_pitch, a.cols, a.dtype) && vector_rows(a.y, a.y_pitch, a.cols, a.dtype))
-    return ln_forward_team<T, 16 / (int)sizeof(T)>(a, sms, stream);
-  return ln_forward_team<T, 1>(a, sms, stream);
-}
-
-template <typename T, int VEC, int TPR>
-static int ln_backward_launch(const LnBackwardArgs& a, int partitions, cudaStream_t stream) {
-  constexpr int kThreads = TPR < 256 ? 256 : TPR;
-  const size_t smem = TPR < 256 ? (size_t)kThreads * kLnElems * sizeof(float) : 0;
-  ln_backward_kernel<T, VEC, TPR><<<dim3((unsigned)a.splits, (unsigned)partitions), kThreads, smem, stream>>>(a);
-  SOLON_CUDA_TRY(cudaGetLastError());
-  return SOLON_OK;
-}
-
-template <typename T, int VEC>
-static int ln_backward_team(const LnBackwardArgs& a, int partitions, cudaStream_t stream) {
-  switch (ln_team(a.cols)) {
-    case 32: return ln_backward_launch<T, VEC, 32>(a, partitions, stream);
-    case 64: return ln_backward_launch<T, VEC, 64>(a, partitions, stream);
-    case 128: return ln_backward_launch<T, VEC, 128>(a, partitions, stream);
-    case 256: return ln_backward_launch<T, VEC, 256>(a, partitions, stream);
-    case 512: return ln_backward_launch<T, VEC, 512>(a, partitions, stream);
-    default: return ln_backward_launch<T, VEC, 1024>(a, partitions, stream);
-  }
+  const bool vec = vector_rows(a.x, a.x_pitch, a.cols, a.dtype) && vector_rows(a.y, a.y_pitch, a.cols, a.dtype);
+  if (vec)
+    return ln_by_team<64 / (int)sizeof(T)>(a.cols, [&](auto team, auto elems) {
+      return ln_forward_launch<T, 16 / (int)sizeof(T), team.value, elems.value>(a, sms, stream);
+    });
+  return ln_by_team<16>(a.cols, [&](auto team, auto elems) { return ln_forward_launch<T, 1, team.value, elems.value>(a, sms, stream); });
 }
 
 template <typename T>
@@ -443,7 +599,12 @@ static int ln_backward_t(const LnBackwardArgs& a, int partitions, int sms, cudaS
   } else {
     const bool vec = vector_rows(a.x, a.x_pitch, a.cols, a.dtype) && vector_rows(a.dy, a.dy_pitch, a.cols, a.dtype) &&
                      (!a.dx || vector_rows(a.dx, a.dx_pitch, a.cols, a.dtype));
-    rc = vec ? ln_backward_team<T, 16 / (int)sizeof(T)>(a, partitions, stream) : ln_backward_team<T, 1>(a, partitions, stream);
+    if (vec)
+      rc = ln_by_team<64 / (int)sizeof(T)>(a.cols, [&](auto team, auto elems) {
+        return ln_backward_launch<T, 16 / (int)sizeof(T), team.value, elems.value>(a, partitions, stream);
+      });
+    else
+      rc = ln_by_team<16>(a.cols, [&](auto team, auto elems) { return ln_backward_launch<T, 1, team.value, elems.value>(a, partitions, stream); });
   }
   if (rc || a.splits == 1 || (!a.dweight && !a.dbias)) return rc;
   return launch_dependent(ln_param_grad_kernel, dim3((unsigned)((2 * a.cols + 31) / 32), (unsigned)partitions), dim3(256), 0, stream, a);
@@ -464,7 +625,8 @@ int solon_layernorm_forward(const void* x, int64_t x_pitch, int dtype, const voi
   if (!param_ok(weight, param_dtype) || !param_ok(bias, param_dtype) || ((uintptr_t)mean | (uintptr_t)rstd) & 3) return SOLON_ERR_INVALID_ARG;
   int sms = 0, rc;
   if ((rc = current_sms(&sms))) return rc;
-  LnForwardArgs a = {x, weight, bias, y, mean, rstd, rows, cols, x_pitch, y_pitch, (float)eps, param_dtype == SOLON_F32, dtype};
+  LnForwardArgs a = {x, weight, bias, y, mean, rstd, rows, cols, x_pitch, y_pitch, (float)eps, param_dtype == SOLON_F32, dtype,
+                     ((uintptr_t)weight & 15) == 0, ((uintptr_t)bias & 15) == 0};
   cudaStream_t stream = (cudaStream_t)cuda_stream;
   if (dtype == SOLON_F32) return ln_forward_t<float>(a, sms, stream);
   if (dtype == SOLON_BF16) return ln_forward_t<__nv_bfloat16>(a, sms, stream);
@@ -517,6 +679,7 @@ int solon_layernorm_backward(const void* dy, int64_t dy_pitch, const void* x, in
   a.param_f32 = param_dtype == SOLON_F32;
   a.dtype = dtype;
   a.grad_f64 = grad_dtype == SOLON_F64;
+  a.weight_aligned = ((uintptr_t)weight & 15) == 0;
   cudaStream_t stream = (cudaStream_t)cuda_stream;
   if (dtype == SOLON_F32) return ln_backward_t<float>(a, partitions, sms, stream);
   if (dtype == SOLON_BF16) return ln_backward_t<__nv_bfloat16>(a, partitions, sms, stream);
