@@ -7,8 +7,8 @@
 //
 // Bound by memory: 2 (forward) and 3 (backward) accesses of the matrix against about 8 and 14 flops an element.
 //
-// Layout: a row belongs to a team of TPR threads, 64 bytes of it each (four 16-byte words; fewer in rows of less than 2 KB), so
-// that a team's two reductions cost little beside the work on the elements.  Teams of one warp meet in shuffles only, larger ones
+// Layout: a row belongs to a team of TPR threads that hold 16 or 32 elements each (fewer in short rows), so that a team's
+// reductions cost little beside the work on the elements.  Teams of one warp meet in shuffles only, larger ones
 // also in shared memory.  CTAs stay for many rows; every thread copies its own words of the next rows into shared memory
 // ahead of time (cp.async: it waits for its own copies only, no barrier), which keeps enough bytes on the way without registers
 // for them.  The weight's gradient is summed in registers over all rows of a CTA; only one partial sum per CTA and column
@@ -25,11 +25,15 @@ namespace solon {
 
 constexpr int kLnThreads = 256;                // threads of a CTA, or one team if that is larger
 constexpr int kLnMaxCols = 16384;              // 1024 threads of 16 float32; wider rows take the streaming kernels
-constexpr int kLnForwardStages = 2;            // rows on the way per team beside the one that is worked on
-// Rows in shared memory per team in the backward pass, the one that is worked on among them.
-template <int TPR>
-constexpr int ln_backward_stages = TPR < 1024 ? 3 : 1;
 
+// Rows on the way per team beside the one that is worked on: four, or what 96 KB (of a CTA of which two share an SM) or 192 KB
+// of shared memory hold.
+constexpr int ln_stages_for(int threads, int row_bytes_per_thread) {
+  const int fit = (threads <= kLnThreads ? 98304 : 196608) / (threads * row_bytes_per_thread);
+  return fit < 1 ? 1 : fit < 4 ? fit : 4;
+}
+template <typename T, int TPR, int ELEMS, int ROWS>
+constexpr int ln_stages = ln_stages_for(TPR < kLnThreads ? kLnThreads : TPR, ROWS * ELEMS * (int)sizeof(T));
 // Sum over the team, the result in every thread.  Teams of several warps alternate between two slots, so one barrier a
 // sum is enough: a slot is written again only after everybody has passed the barrier of the sum in between.
 template <int TPR, int N>
@@ -48,11 +52,16 @@ __device__ __forceinline__ void team_sum(float (&v)[N], float* slots, int& turn,
       for (int k = 0; k < N; ++k) s[k * kWarps + warp] = v[k];
     }
     asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "n"(TPR) : "memory");
+    constexpr int kRead = kWarps < 4 ? kWarps : 4;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
       float sum = 0.0f;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) sum += s[k * kWarps + w];
+      for (int w = 0; w < kWarps; w += kRead) {
+        const Pack<float, kRead> q = load_pack<float, kRead>(s + k * kWarps + w);
+#pragma unroll
+        for (int j = 0; j < kRead; ++j) sum += q.e[j];
+      }
       v[k] = sum;
     }
   }
@@ -65,32 +74,6 @@ __device__ __forceinline__ void copy16_async(void* dst_smem, const void* src, bo
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
-// Weight or bias of N neighbouring columns: float32 or the matrix's type, at any alignment.
-template <typename T, int N>
-__device__ __forceinline__ void param_words(float (&w)[N], const void* p, bool f32, bool aligned, int c) {
-  const float* q = static_cast<const float*>(p) + c;
-  const T* r = static_cast<const T*>(p) + c;
-  if constexpr (N % 4 == 0) {
-    if (aligned) {
-      if (f32) {
-#pragma unroll
-        for (int i = 0; i < N; i += 4) {
-          const Pack<float, 4> v = load_pack<float, 4>(q + i);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) w[i + k] = v.e[k];
-        }
-      } else {
-        const Pack<T, N> v = load_pack<T, N>(r);
-#pragma unroll
-        for (int i = 0; i < N; ++i) w[i] = to_float(v.e[i]);
-      }
-      return;
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < N; ++i) w[i] = f32 ? q[i] : to_float(r[i]);
-}
 
 __device__ __forceinline__ float param_at(const void* p, int is_f32, int dtype, int64_t c) {
   if (is_f32) return static_cast<const float*>(p)[c];
@@ -107,95 +90,143 @@ struct LnForwardArgs {
   float* rstd;
   int64_t rows, cols, x_pitch, y_pitch;
   float eps;
-  int param_f32, dtype, weight_aligned, bias_aligned;
+  int param_f32, dtype;
 };
 
-// VEC: neighbouring elements an access moves - 16 bytes, or one where rows are not made of 16-byte words at 16-byte
-// boundaries; those are loaded straight into registers.
+// How a thread sees a row: ELEMS elements in groups of VEC neighbours - 16-byte words, or single elements where rows are not
+// made of 16-byte words at 16-byte boundaries; those are loaded straight into registers.  Pairs of elements share an instruction.
 template <typename T, int VEC, int TPR, int ELEMS>
-__global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, TPR < 512 ? 4 : TPR < 1024 ? 2 : 1) ln_forward_kernel(LnForwardArgs a) {
-  constexpr int kGroups = ELEMS / VEC;         // accesses (with VEC > 1 words of 16 bytes)
-  constexpr int kBlock = TPR < kLnThreads ? kLnThreads : TPR;
-  extern __shared__ __align__(16) uint4 ring[];           // stages x words x threads
-  __shared__ __align__(16) float slots[2 * 32];
-  const int tid = threadIdx.x & (TPR - 1), team = threadIdx.x / TPR;
-  constexpr int kTeams = kBlock / TPR;
-  const int cols = (int)a.cols;
-  const T* x = static_cast<const T*>(a.x);
-  T* y = static_cast<T*>(a.y);
-  const float inv_n = 1.0f / (float)cols;
-  int turn = 0;
-  const int64_t stride = (int64_t)gridDim.x * kTeams;
-  auto issue = [&](int64_t row, int stage) {
-    if constexpr (VEC > 1) {
-      if (row < a.rows) {
-        const T* from = x + row * a.x_pitch + tid * VEC;
+struct LnRow {
+  static constexpr int kGroups = ELEMS / VEC;
+  static constexpr int kBlock = TPR < kLnThreads ? kLnThreads : TPR;
+  static constexpr int kTeams = kBlock / TPR;
+
+  static __device__ __forceinline__ int column(int group, int tid) { return (group * TPR + tid) * VEC; }
+
+  // the copies of a row's words into a stage of the ring (words x threads)
+  static __device__ __forceinline__ void issue(uint4* stage, const T* row, int cols, int tid) {
 #pragma unroll
-        for (int i = 0; i < kGroups; ++i) {
-          const bool inside = (i * TPR + tid) * VEC < cols;
-          copy16_async(ring + (stage * kGroups + i) * kBlock + threadIdx.x, inside ? from + i * TPR * VEC : x, inside);
-        }
-      }
-      copies_commit();
+    for (int i = 0; i < kGroups; ++i) {
+      const int c = column(i, tid);
+      copy16_async(stage + i * kBlock + threadIdx.x, c < cols ? row + c : row, c < cols);
     }
-  };
-  int64_t row = (int64_t)blockIdx.x * kTeams + team;
-  int stage = 0;
-#pragma unroll
-  for (int s = 0; s < kLnForwardStages; ++s) issue(row + s * stride, s);
-  for (; row < a.rows; row += stride) {
-    float v[ELEMS];
+  }
+  static __device__ __forceinline__ void take(Float2 (&v)[ELEMS / 2], const uint4* stage, const T* row, int cols, int tid) {
     if constexpr (VEC > 1) {
-      copies_wait<kLnForwardStages - 1>();
 #pragma unroll
       for (int i = 0; i < kGroups; ++i) {
         float part[VEC];
-        Word16<T>::unpack(ring[(stage * kGroups + i) * kBlock + threadIdx.x], part);
+        Word16<T>::unpack(stage[i * kBlock + threadIdx.x], part);
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) v[i * VEC + k] = part[k];
+        for (int k = 0; k < VEC; k += 2) v[(i * VEC + k) / 2] = pack2(part[k], part[k + 1]);
       }
-      issue(row + kLnForwardStages * stride, stage);      // into the words just read
-      stage = stage + 1 == kLnForwardStages ? 0 : stage + 1;
     } else {
-      const T* from = x + row * a.x_pitch;
+      T part[ELEMS];
 #pragma unroll
-      for (int i = 0; i < ELEMS; ++i) v[i] = i * TPR + tid < cols ? to_float(from[i * TPR + tid]) : 0.0f;
+      for (int i = 0; i < ELEMS; ++i) part[i] = column(i, tid) < cols ? row[column(i, tid)] : from_float<T>(0.0f);
+#pragma unroll
+      for (int i = 0; i < ELEMS; i += 2) v[i / 2] = pack2(to_float(part[i]), to_float(part[i + 1]));
     }
-    float sum[1] = {0.0f};
+  }
+  static __device__ __forceinline__ void store(T* row, const Float2 (&v)[ELEMS / 2], int cols, int tid) {
 #pragma unroll
-    for (int i = 0; i < ELEMS; ++i) sum[0] += v[i];
+    for (int i = 0; i < kGroups; ++i) {
+      if constexpr (VEC > 1) {
+        float part[VEC];
+#pragma unroll
+        for (int k = 0; k < VEC; k += 2) unpack2(v[(i * VEC + k) / 2], part[k], part[k + 1]);
+        if (column(i, tid) < cols) *reinterpret_cast<uint4*>(row + column(i, tid)) = Word16<T>::pack(part);
+      } else {
+        float part[2];
+        unpack2(v[i / 2], part[0], part[1]);
+        if (column(i, tid) < cols) row[column(i, tid)] = from_float<T>(part[i % 2]);
+      }
+    }
+  }
+  // weight or bias of the thread's columns (once per CTA)
+  static __device__ __forceinline__ void params(Float2 (&w)[ELEMS / 2], const void* p, int is_f32, int dtype, float absent, int cols, int tid) {
+    float e[ELEMS];
+#pragma unroll
+    for (int i = 0; i < ELEMS; ++i) {
+      const int c = column(i / VEC, tid) + i % VEC;
+      e[i] = c < cols ? (p ? param_at(p, is_f32, dtype, c) : absent) : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < ELEMS; i += 2) w[i / 2] = pack2(e[i], e[i + 1]);
+  }
+};
+
+__device__ __forceinline__ Float2 both(float x) { return pack2(x, x); }
+__device__ __forceinline__ float sum_of(Float2 x) {
+  float a, b;
+  unpack2(x, a, b);
+  return a + b;
+}
+
+template <typename T, int VEC, int TPR, int ELEMS>
+__global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, TPR < 512 ? 2 : 1) ln_forward_kernel(LnForwardArgs a) {
+  using Row = LnRow<T, VEC, TPR, ELEMS>;
+  constexpr int kStages = ln_stages<T, TPR, ELEMS, 1>;
+  constexpr int kStageWords = Row::kGroups * Row::kBlock;
+  extern __shared__ __align__(16) uint4 ring[];           // stages x words x threads
+  __shared__ __align__(16) float slots[2 * 32];
+  const int tid = threadIdx.x & (TPR - 1), team = threadIdx.x / TPR, cols = (int)a.cols;
+  const T* x = static_cast<const T*>(a.x);
+  T* y = static_cast<T*>(a.y);
+  const float inv_n = 1.0f / (float)cols;
+  const int64_t stride = (int64_t)gridDim.x * Row::kTeams;
+  int64_t row = (int64_t)blockIdx.x * Row::kTeams + team;
+  if constexpr (VEC > 1) {
+#pragma unroll
+    for (int s = 0; s < kStages; ++s) {
+      if (row + s * stride < a.rows) Row::issue(ring + s * kStageWords, x + (row + s * stride) * a.x_pitch, cols, tid);
+      copies_commit();
+    }
+  }
+  Float2 w[ELEMS / 2], b[ELEMS / 2];
+  Row::params(w, a.weight, a.param_f32, a.dtype, 1.0f, cols, tid);
+  Row::params(b, a.bias, a.param_f32, a.dtype, 0.0f, cols, tid);
+  int turn = 0, stage = 0;
+  for (; row < a.rows; row += stride) {
+    Float2 v[ELEMS / 2];
+    uint4* words = ring + stage * kStageWords;
+    if constexpr (VEC > 1) copies_wait<kStages - 1>();
+    Row::take(v, words, x + row * a.x_pitch, cols, tid);
+    if constexpr (VEC > 1) {
+      const int64_t ahead = row + kStages * stride;       // into the words just read
+      if (ahead < a.rows) Row::issue(words, x + ahead * a.x_pitch, cols, tid);
+      copies_commit();
+      stage = stage + 1 == kStages ? 0 : stage + 1;
+    }
+    Float2 acc = both(0.0f);
+#pragma unroll
+    for (int i = 0; i < ELEMS / 2; ++i) acc = add2(acc, v[i]);
+    float sum[1] = {sum_of(acc)};
     team_sum<TPR>(sum, slots, turn, team);
     const float mean = sum[0] * inv_n;
-    float sq[1] = {0.0f};
+    const Float2 minus_mean = both(-mean);
+    acc = both(0.0f);
 #pragma unroll
-    for (int i = 0; i < kGroups; ++i) {
-      if ((i * TPR + tid) * VEC < cols) {
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) {
-          v[i * VEC + k] -= mean;
-          sq[0] = fmaf(v[i * VEC + k], v[i * VEC + k], sq[0]);
-        }
+    for (int i = 0; i < ELEMS / 2; ++i) {
+      v[i] = add2(v[i], minus_mean);
+      if constexpr (VEC > 1) {                            // a group lies inside the row or outside
+        if (Row::column(2 * i / VEC, tid) < cols) acc = fma2(v[i], v[i], acc);
+      } else {
+        float e0, e1;
+        unpack2(v[i], e0, e1);
+        e0 = Row::column(2 * i, tid) < cols ? e0 : 0.0f;
+        e1 = Row::column(2 * i + 1, tid) < cols ? e1 : 0.0f;
+        const Float2 e = pack2(e0, e1);
+        acc = fma2(e, e, acc);
       }
     }
+    float sq[1] = {sum_of(acc)};
     team_sum<TPR>(sq, slots, turn, team);
     const float rstd = rsqrtf(sq[0] * inv_n + a.eps);
-    T* to = y + row * a.y_pitch;
+    const Float2 scale = both(rstd);
 #pragma unroll
-    for (int i = 0; i < kGroups; ++i) {
-      const int c = (i * TPR + tid) * VEC;
-      if (c < cols) {
-        float w[VEC], b[VEC], out[VEC];
-        if (a.weight) param_words<T>(w, a.weight, a.param_f32, a.weight_aligned, c);
-        if (a.bias) param_words<T>(b, a.bias, a.param_f32, a.bias_aligned, c);
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) {
-          out[k] = v[i * VEC + k] * rstd;
-          out[k] = fmaf(out[k], a.weight ? w[k] : 1.0f, a.bias ? b[k] : 0.0f);
-        }
-        if constexpr (VEC > 1) *reinterpret_cast<uint4*>(to + c) = Word16<T>::pack(out);
-        else to[c] = from_float<T>(out[0]);
-      }
-    }
+    for (int i = 0; i < ELEMS / 2; ++i) v[i] = fma2(mul2(v[i], scale), w[i], b[i]);
+    Row::store(y + row * a.y_pitch, v, cols, tid);
     if (tid == 0) {
       if (a.mean) a.mean[row] = mean;
       if (a.rstd) a.rstd[row] = rstd;
@@ -214,7 +245,7 @@ struct LnBackwardArgs {
   void* dbias;
   float* partials;             // partitions x splits x 2 x cols (splits > 1)
   int64_t rows_per_part, cols, dy_pitch, x_pitch, dx_pitch, grad_pitch;
-  int splits, param_f32, dtype, grad_f64, weight_aligned;
+  int splits, param_f32, dtype, grad_f64;
 };
 
 __device__ __forceinline__ void store_grad(void* p, int f64, int64_t i, float v) {
@@ -222,146 +253,104 @@ __device__ __forceinline__ void store_grad(void* p, int f64, int64_t i, float v)
   else static_cast<float*>(p)[i] = v;
 }
 
-// CTA (split, partition): rows split * teams + team, stepping by splits * teams, of its partition.  A row is gone through
-// twice, for the sums and for dx: its words stay in shared memory in between, which is what the registers could not hold
-// beside the sums of the weight's gradient.
+// CTA (split, partition): rows split * teams + team, stepping by splits * teams, of its partition.
 template <typename T, int VEC, int TPR, int ELEMS>
 __global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, TPR < 512 ? 2 : 1) ln_backward_kernel(LnBackwardArgs a) {
-  constexpr int kGroups = ELEMS / VEC;         // accesses (with VEC > 1 words of 16 bytes)
-  constexpr int kBlock = TPR < kLnThreads ? kLnThreads : TPR;
-  constexpr int kTeams = kBlock / TPR;
-  constexpr int kStages = ln_backward_stages<TPR>;
+  using Row = LnRow<T, VEC, TPR, ELEMS>;
+  constexpr int kTeams = Row::kTeams;
+  constexpr int kStages = ln_stages<T, TPR, ELEMS, 2>;
+  constexpr int kRowWords = Row::kGroups * Row::kBlock;
   extern __shared__ __align__(16) uint4 ring[];           // stages x 2 (x, dy) x words x threads; teams' sums at the end
   __shared__ __align__(16) float slots[2 * 32 * 2];
-  const int tid = threadIdx.x & (TPR - 1), team = threadIdx.x / TPR;
-  const int split = blockIdx.x, part = blockIdx.y, cols = (int)a.cols;
+  const int tid = threadIdx.x & (TPR - 1), team = threadIdx.x / TPR, cols = (int)a.cols;
+  const int split = blockIdx.x, part = blockIdx.y;
   const T* x = static_cast<const T*>(a.x);
   const T* dy = static_cast<const T*>(a.dy);
   T* dx = static_cast<T*>(a.dx);
-  float dw[ELEMS], db[ELEMS];
-#pragma unroll
-  for (int i = 0; i < ELEMS; ++i) dw[i] = db[i] = 0.0f;
   const float inv_n = 1.0f / (float)cols;
-  int turn = 0;
   const int64_t stride = (int64_t)a.splits * kTeams, end = (int64_t)(part + 1) * a.rows_per_part;
   int64_t row = (int64_t)part * a.rows_per_part + (int64_t)split * kTeams + team;
-  float next_mean = 0.0f, next_rstd = 0.0f;               // of the row after the one that is worked on
-  auto issue = [&](int64_t at, int stage) {
-    if constexpr (VEC > 1) {
-      if (at < end) {
-        const T* from_x = x + at * a.x_pitch + tid * VEC;
-        const T* from_dy = dy + at * a.dy_pitch + tid * VEC;
+  if constexpr (VEC > 1) {
 #pragma unroll
-        for (int i = 0; i < kGroups; ++i) {
-          const bool inside = (i * TPR + tid) * VEC < cols;
-          uint4* to = ring + (stage * 2 * kGroups + i) * kBlock + threadIdx.x;
-          copy16_async(to, inside ? from_x + i * TPR * VEC : x, inside);
-          copy16_async(to + kGroups * kBlock, inside ? from_dy + i * TPR * VEC : x, inside);
-        }
+    for (int s = 0; s < kStages; ++s) {
+      const int64_t at = row + s * stride;
+      if (at < end) {
+        Row::issue(ring + s * 2 * kRowWords, x + at * a.x_pitch, cols, tid);
+        Row::issue(ring + (s * 2 + 1) * kRowWords, dy + at * a.dy_pitch, cols, tid);
       }
       copies_commit();
     }
-  };
-#pragma unroll
-  for (int s = 0; s < kStages - 1; ++s) issue(row + s * stride, s);
+  }
+  float next_mean = 0.0f, next_rstd = 0.0f;               // of the row after the one that is worked on
   if (row < end) {
     next_mean = a.mean[row];
     next_rstd = a.rstd[row];
   }
-  int stage = 0;
+  Float2 w[ELEMS / 2], dw[ELEMS / 2], db[ELEMS / 2];
+  Row::params(w, a.weight, a.param_f32, a.dtype, 1.0f, cols, tid);
+#pragma unroll
+  for (int i = 0; i < ELEMS / 2; ++i) dw[i] = db[i] = both(0.0f);
+  int turn = 0, stage = 0;
   for (; row < end; row += stride) {
     const float mean = next_mean, rstd = next_rstd;
     if (row + stride < end) {
       next_mean = a.mean[row + stride];
       next_rstd = a.rstd[row + stride];
     }
-    const T* row_x = x + row * a.x_pitch;
-    const T* row_dy = dy + row * a.dy_pitch;
-    float hold_x[VEC > 1 ? 1 : ELEMS], hold_g[VEC > 1 ? 1 : ELEMS];       // rows without words are held in registers
-    if constexpr (VEC == 1) {
-#pragma unroll
-      for (int i = 0; i < ELEMS; ++i) {
-        const int c = i * TPR + tid;
-        hold_x[i] = c < cols ? to_float(row_x[c]) : mean;
-        hold_g[i] = c < cols ? to_float(row_dy[c]) : 0.0f;
+    Float2 xh[ELEMS / 2], g[ELEMS / 2];
+    uint4* words = ring + stage * 2 * kRowWords;
+    if constexpr (VEC > 1) copies_wait<kStages - 1>();
+    Row::take(xh, words, x + row * a.x_pitch, cols, tid);
+    Row::take(g, words + kRowWords, dy + row * a.dy_pitch, cols, tid);
+    if constexpr (VEC > 1) {
+      const int64_t ahead = row + kStages * stride;       // into the words just read
+      if (ahead < end) {
+        Row::issue(words, x + ahead * a.x_pitch, cols, tid);
+        Row::issue(words + kRowWords, dy + ahead * a.dy_pitch, cols, tid);
       }
-    } else {
-      const int ahead = stage == 0 ? kStages - 1 : stage - 1;     // the words of the row before
-      issue(row + (kStages - 1) * stride, ahead);
-      copies_wait<kStages - 1>();
+      copies_commit();
+      stage = stage + 1 == kStages ? 0 : stage + 1;
     }
-    // group i of the row: xh, dy and w dy
-    auto group = [&](int i, float (&xh)[VEC], float (&g)[VEC], float (&wg)[VEC]) {
-      if constexpr (VEC > 1) {
-        Word16<T>::unpack(ring[(stage * 2 * kGroups + i) * kBlock + threadIdx.x], xh);
-        Word16<T>::unpack(ring[((stage * 2 + 1) * kGroups + i) * kBlock + threadIdx.x], g);
-      } else {
-        xh[0] = hold_x[i];
-        g[0] = hold_g[i];
-      }
-      if (a.weight) {
-        float w[VEC];
-        const int c = (i * TPR + tid) * VEC;
-        param_words<T>(w, a.weight, a.param_f32, a.weight_aligned, c < cols ? c : 0);
+    const Float2 minus_mean = both(-mean), scale = both(rstd);
+    Float2 s0 = both(0.0f), s1 = both(0.0f);
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) wg[k] = g[k] * w[k];
-      } else {
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) wg[k] = g[k];
-      }
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) xh[k] = (xh[k] - mean) * rstd;
-    };
-    float s[2] = {0.0f, 0.0f};
-#pragma unroll
-    for (int i = 0; i < kGroups; ++i) {        // (outside the row dy is 0)
-      float xh[VEC], g[VEC], wg[VEC];
-      group(i, xh, g, wg);
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) {
-        dw[i * VEC + k] = fmaf(g[k], xh[k], dw[i * VEC + k]);
-        db[i * VEC + k] += g[k];
-        s[0] += wg[k];
-        s[1] = fmaf(wg[k], xh[k], s[1]);
-      }
+    for (int i = 0; i < ELEMS / 2; ++i) {                 // (outside the row dy and w are 0)
+      xh[i] = mul2(add2(xh[i], minus_mean), scale);
+      dw[i] = fma2(g[i], xh[i], dw[i]);
+      db[i] = add2(db[i], g[i]);
+      g[i] = mul2(g[i], w[i]);
+      s0 = add2(s0, g[i]);
+      s1 = fma2(g[i], xh[i], s1);
     }
     if (dx) {
+      float s[2] = {sum_of(s0), sum_of(s1)};
       team_sum<TPR>(s, slots, turn, team);
-      const float m0 = s[0] * inv_n, m1 = s[1] * inv_n;
-      T* to = dx + row * a.dx_pitch;
+      const Float2 minus_m0 = both(-s[0] * inv_n), minus_m1 = both(-s[1] * inv_n);
 #pragma unroll
-      for (int i = 0; i < kGroups; ++i) {
-        const int c = (i * TPR + tid) * VEC;
-        if (c < cols) {
-          float xh[VEC], g[VEC], out[VEC];
-          group(i, xh, g, out);
-#pragma unroll
-          for (int k = 0; k < VEC; ++k) out[k] = rstd * (out[k] - m0 - xh[k] * m1);
-          if constexpr (VEC > 1) *reinterpret_cast<uint4*>(to + c) = Word16<T>::pack(out);
-          else to[c] = from_float<T>(out[0]);
-        }
-      }
+      for (int i = 0; i < ELEMS / 2; ++i) g[i] = mul2(fma2(xh[i], minus_m1, add2(g[i], minus_m0)), scale);
+      Row::store(dx + row * a.dx_pitch, g, cols, tid);
     }
-    stage = stage + 1 == kStages ? 0 : stage + 1;
   }
   if (!a.dweight && !a.dbias) return;
+  float sums[2][ELEMS];                        // weight, bias
+#pragma unroll
+  for (int i = 0; i < ELEMS; i += 2) {
+    unpack2(dw[i / 2], sums[0][i], sums[0][i + 1]);
+    unpack2(db[i / 2], sums[1][i], sums[1][i + 1]);
+  }
   if constexpr (kTeams > 1) {                  // add the teams' sums, in team order
     float* combine = reinterpret_cast<float*>(ring);
     if constexpr (VEC > 1) copies_wait<0>();
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
-      float* mine = which ? db : dw;
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < ELEMS; ++i) combine[(team * ELEMS + i) * TPR + tid] = mine[i];
+      for (int i = 0; i < ELEMS; ++i) combine[(team * ELEMS + i) * TPR + tid] = sums[which][i];
       __syncthreads();
       if (team == 0) {
 #pragma unroll
-        for (int i = 0; i < ELEMS; ++i) {
-          float sum = mine[i];
-          for (int t = 1; t < kTeams; ++t) sum += combine[(t * ELEMS + i) * TPR + tid];
-          mine[i] = sum;
-        }
+        for (int i = 0; i < ELEMS; ++i)
+          for (int t = 1; t < kTeams; ++t) sums[which][i] += combine[(t * ELEMS + i) * TPR + tid];
       }
     }
     if (team != 0) return;
@@ -369,14 +358,14 @@ __global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, TPR < 512
   float* out = a.splits > 1 ? a.partials + ((int64_t)part * a.splits + split) * 2 * a.cols : nullptr;
 #pragma unroll
   for (int i = 0; i < ELEMS; ++i) {
-    const int64_t c = ((int64_t)(i / VEC) * TPR + tid) * VEC + i % VEC;
-    if (c >= a.cols) continue;
+    const int c = Row::column(i / VEC, tid) + i % VEC;
+    if (c >= cols) continue;
     if (out) {
-      out[c] = dw[i];
-      out[a.cols + c] = db[i];
+      out[c] = sums[0][i];
+      out[cols + c] = sums[1][i];
     } else {
-      if (a.dweight) store_grad(a.dweight, a.grad_f64, part * a.grad_pitch + c, dw[i]);
-      if (a.dbias) store_grad(a.dbias, a.grad_f64, part * a.grad_pitch + c, db[i]);
+      if (a.dweight) store_grad(a.dweight, a.grad_f64, part * a.grad_pitch + c, sums[0][i]);
+      if (a.dbias) store_grad(a.dbias, a.grad_f64, part * a.grad_pitch + c, sums[1][i]);
     }
   }
 }
@@ -509,8 +498,7 @@ static int64_t ln_min(int64_t a, int64_t b) { return a < b ? a : b; }
 // partitions - one more and the last would run alone after all others -, as long as every CTA has a row for each of its teams.
 constexpr int kLnSms = 148;
 static int ln_splits(int64_t rows_per_part, int64_t cols, int partitions) {
-  // (the workspace does not depend on type and alignment, so the number of teams is taken as of the smallest ones)
-  const int team = cols > kLnMaxCols ? 1024 : ln_team(cols, 32).threads;
+  const int team = cols > kLnMaxCols ? 1024 : ln_team(cols, 16).threads;
   const int teams = team < kLnThreads ? kLnThreads / team : 1;
   const int64_t want = 2 * kLnSms / partitions;
   const int64_t most = (rows_per_part + teams - 1) / teams;
@@ -527,9 +515,9 @@ template <typename T, int VEC, int TPR, int ELEMS>
 static int ln_forward_launch(const LnForwardArgs& a, int sms, cudaStream_t stream) {
   constexpr int kBlock = TPR < kLnThreads ? kLnThreads : TPR;
   constexpr int kTeams = kBlock / TPR;
-  constexpr size_t kSmem = VEC > 1 ? (size_t)kLnForwardStages * (ELEMS / VEC) * 16 * kBlock : 0;
+  constexpr size_t kSmem = VEC > 1 ? (size_t)ln_stages<T, TPR, ELEMS, 1> * (ELEMS / VEC) * 16 * kBlock : 0;
   if constexpr (kSmem > 40 * 1024) SOLON_CUDA_TRY(cudaFuncSetAttribute(ln_forward_kernel<T, VEC, TPR, ELEMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem));
-  const int64_t want = (a.rows + kTeams - 1) / kTeams, cap = (int64_t)sms * (TPR < 512 ? 4 : TPR < 1024 ? 2 : 1);
+  const int64_t want = (a.rows + kTeams - 1) / kTeams, cap = (int64_t)sms * (TPR < 512 ? 2 : 1);
   ln_forward_kernel<T, VEC, TPR, ELEMS><<<(unsigned)ln_min(want, cap), kBlock, kSmem, stream>>>(a);
   SOLON_CUDA_TRY(cudaGetLastError());
   return SOLON_OK;
@@ -538,7 +526,7 @@ static int ln_forward_launch(const LnForwardArgs& a, int sms, cudaStream_t strea
 template <typename T, int VEC, int TPR, int ELEMS>
 static int ln_backward_launch(const LnBackwardArgs& a, int partitions, cudaStream_t stream) {
   constexpr int kBlock = TPR < kLnThreads ? kLnThreads : TPR;
-  constexpr size_t kRing = VEC > 1 ? (size_t)ln_backward_stages<TPR> * 2 * (ELEMS / VEC) * 16 * kBlock : 0;
+  constexpr size_t kRing = VEC > 1 ? (size_t)ln_stages<T, TPR, ELEMS, 2> * 2 * (ELEMS / VEC) * 16 * kBlock : 0;
   constexpr size_t kCombine = TPR < kBlock ? (size_t)kBlock * ELEMS * sizeof(float) : 0;
   constexpr size_t kSmem = kRing > kCombine ? kRing : kCombine;
   if constexpr (kSmem > 40 * 1024) SOLON_CUDA_TRY(cudaFuncSetAttribute(ln_backward_kernel<T, VEC, TPR, ELEMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem));
@@ -547,14 +535,15 @@ static int ln_backward_launch(const LnBackwardArgs& a, int partitions, cudaStrea
   return SOLON_OK;
 }
 
-// f(team size, elements of a thread), both as compile-time constants.  16 elements with 4-byte types, and where elements are
-// loaded one by one; 32 with 16-byte words of two-byte types.
-template <int MOST, typename F>
+// f(team size, elements of a thread), both as compile-time constants.  A thread takes up to 16 elements; 32 in the forward
+// pass over 16-byte words of two-byte types.
+template <int MOST, int VEC, typename F>
 static int ln_by_team(int64_t cols, F f) {
   const LnTeam t = ln_team(cols, MOST);
+  constexpr int kLeast = MOST / 4 < VEC ? VEC : MOST / 4;
   switch (t.threads) {
     case 32:
-      if (t.elems == MOST / 4) return f(std::integral_constant<int, 32>(), std::integral_constant<int, MOST / 4>());
+      if (t.elems == MOST / 4) return f(std::integral_constant<int, 32>(), std::integral_constant<int, kLeast>());
       if (t.elems == MOST / 2) return f(std::integral_constant<int, 32>(), std::integral_constant<int, MOST / 2>());
       return f(std::integral_constant<int, 32>(), std::integral_constant<int, MOST>());
     case 64: return f(std::integral_constant<int, 64>(), std::integral_constant<int, MOST>());
@@ -577,10 +566,10 @@ static int ln_forward_t(const LnForwardArgs& a, int sms, cudaStream_t stream) {
   }
   const bool vec = vector_rows(a.x, a.x_pitch, a.cols, a.dtype) && vector_rows(a.y, a.y_pitch, a.cols, a.dtype);
   if (vec)
-    return ln_by_team<64 / (int)sizeof(T)>(a.cols, [&](auto team, auto elems) {
+    return ln_by_team<64 / (int)sizeof(T), 16 / (int)sizeof(T)>(a.cols, [&](auto team, auto elems) {
       return ln_forward_launch<T, 16 / (int)sizeof(T), team.value, elems.value>(a, sms, stream);
     });
-  return ln_by_team<16>(a.cols, [&](auto team, auto elems) { return ln_forward_launch<T, 1, team.value, elems.value>(a, sms, stream); });
+  return ln_by_team<16, 1>(a.cols, [&](auto team, auto elems) { return ln_forward_launch<T, 1, team.value, elems.value>(a, sms, stream); });
 }
 
 template <typename T>
@@ -600,11 +589,11 @@ static int ln_backward_t(const LnBackwardArgs& a, int partitions, int sms, cudaS
     const bool vec = vector_rows(a.x, a.x_pitch, a.cols, a.dtype) && vector_rows(a.dy, a.dy_pitch, a.cols, a.dtype) &&
                      (!a.dx || vector_rows(a.dx, a.dx_pitch, a.cols, a.dtype));
     if (vec)
-      rc = ln_by_team<64 / (int)sizeof(T)>(a.cols, [&](auto team, auto elems) {
+      rc = ln_by_team<16, 16 / (int)sizeof(T)>(a.cols, [&](auto team, auto elems) {
         return ln_backward_launch<T, 16 / (int)sizeof(T), team.value, elems.value>(a, partitions, stream);
       });
     else
-      rc = ln_by_team<16>(a.cols, [&](auto team, auto elems) { return ln_backward_launch<T, 1, team.value, elems.value>(a, partitions, stream); });
+      rc = ln_by_team<16, 1>(a.cols, [&](auto team, auto elems) { return ln_backward_launch<T, 1, team.value, elems.value>(a, partitions, stream); });
   }
   if (rc || a.splits == 1 || (!a.dweight && !a.dbias)) return rc;
   return launch_dependent(ln_param_grad_kernel, dim3((unsigned)((2 * a.cols + 31) / 32), (unsigned)partitions), dim3(256), 0, stream, a);
@@ -625,8 +614,7 @@ int solon_layernorm_forward(const void* x, int64_t x_pitch, int dtype, const voi
   if (!param_ok(weight, param_dtype) || !param_ok(bias, param_dtype) || ((uintptr_t)mean | (uintptr_t)rstd) & 3) return SOLON_ERR_INVALID_ARG;
   int sms = 0, rc;
   if ((rc = current_sms(&sms))) return rc;
-  LnForwardArgs a = {x, weight, bias, y, mean, rstd, rows, cols, x_pitch, y_pitch, (float)eps, param_dtype == SOLON_F32, dtype,
-                     ((uintptr_t)weight & 15) == 0, ((uintptr_t)bias & 15) == 0};
+  LnForwardArgs a = {x, weight, bias, y, mean, rstd, rows, cols, x_pitch, y_pitch, (float)eps, param_dtype == SOLON_F32, dtype};
   cudaStream_t stream = (cudaStream_t)cuda_stream;
   if (dtype == SOLON_F32) return ln_forward_t<float>(a, sms, stream);
   if (dtype == SOLON_BF16) return ln_forward_t<__nv_bfloat16>(a, sms, stream);
@@ -679,7 +667,6 @@ int solon_layernorm_backward(const void* dy, int64_t dy_pitch, const void* x, in
   a.param_f32 = param_dtype == SOLON_F32;
   a.dtype = dtype;
   a.grad_f64 = grad_dtype == SOLON_F64;
-  a.weight_aligned = ((uintptr_t)weight & 15) == 0;
   cudaStream_t stream = (cudaStream_t)cuda_stream;
   if (dtype == SOLON_F32) return ln_backward_t<float>(a, partitions, sms, stream);
   if (dtype == SOLON_BF16) return ln_backward_t<__nv_bfloat16>(a, partitions, sms, stream);
