@@ -399,7 +399,7 @@ int solon_adamw_bind_grads(solon_adamw* opt, const void* const* grads, int grad_
  *   grad_norm   device, one float32 (output; NULL: not wanted; needs max_norm > 0): the norm before clipping
  *   guard       a plan whose last decode the step depends on (NULL: none): if that decode was undecodable, or a wait in it
  *               ran out, the step changes nothing.  Enqueue the step after the decode, on its stream or ordered behind it.
- * A norm that is not finite also makes the step change nothing; without clipping a gradient that is not finite goes into its
+ * A norm that is not finite (float64 squares: a gradient that is not) also makes the step change nothing; without clipping a gradient that is not finite goes into its
  * weight as the formulas have it.  Steps are counted on the device, only those that were applied count: a captured step may be replayed. */
 int solon_adamw_step(solon_adamw* opt, const void* grad, int grad_dtype, double grad_scale, double lr, double max_norm, float* grad_norm,
                      const solon_plan* guard, void* cuda_stream);

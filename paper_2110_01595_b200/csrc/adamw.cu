@@ -21,21 +21,17 @@ namespace solon {
 constexpr int kAdamBlock = 256;                        // elements of a state block (one warp, eight per lane)
 constexpr int kAdamChunkBlocks = 8;                    // blocks of a chunk (one CTA of eight warps)
 constexpr int kAdamThreads = 32 * kAdamChunkBlocks;
+constexpr int kAdamChunk = kAdamBlock * kAdamChunkBlocks;
 
-struct AdamTensor {
-  float* p;
+// All that a CTA needs to know of its chunk, in one 64-byte record: one trip to memory before the data, not two.
+struct alignas(64) AdamChunk {
+  float* p;                  // the chunk's first element
   __nv_bfloat16* copy;       // nullptr: none
-  const void* grad;          // bound gradient (nullptr: the gradient is the flat vector of the call)
+  const void* grad;          // bound gradient of the chunk's first element
   int64_t offset;            // first element in the concatenated order
-  int64_t numel;
-  int64_t first_block;
+  int64_t slot;              // first element in the state
+  int count;                 // elements
   float weight_decay;
-  int pad;
-};
-
-struct AdamChunk {
-  int tensor;
-  int index;                 // chunk inside the tensor
 };
 
 // What the update reads, written by the control kernel of the same step.
@@ -57,8 +53,8 @@ struct solon_adamw {
   int grads_bound, grad_dtype;             // bound gradients and their type
   void *exp_avg, *exp_avg_sq;
   int16_t* base;
-  std::vector<solon::AdamTensor> tensors;
-  solon::AdamTensor* d_tensors;
+  std::vector<int64_t> numel;
+  std::vector<solon::AdamChunk> chunks;
   solon::AdamChunk* d_chunks;
   solon::AdamScalars* d_scalars;
   double* d_partials;                      // norm kernel: one sum per CTA
@@ -76,9 +72,11 @@ __host__ __device__ __forceinline__ uint32_t mix32(uint32_t h) {
   return h ^ (h >> 16);
 }
 
-// The 32 random bits of a state slot in a step (key: step and seed): the low half rounds m, the high half v.
-__device__ __forceinline__ uint32_t slot_random(uint32_t key, int64_t slot) {
-  return mix32(((uint32_t)slot * 0x9E3779B1u + (uint32_t)((uint64_t)slot >> 32) * 0x85EBCA77u) ^ key);
+// The 32 random bits of a state slot in a step are mix32((hash start of the slot) ^ key), key: step and seed; the low half
+// rounds m, the high half v.  Slots 0 .. n behind one add n kSlotFactor to its start (a block of 256 does not cross 2^32).
+constexpr uint32_t kSlotFactor = 0x9E3779B1u;
+__device__ __forceinline__ uint32_t slot_hash_start(int64_t slot) {
+  return (uint32_t)slot * kSlotFactor + (uint32_t)((uint64_t)slot >> 32) * 0x85EBCA77u;
 }
 
 // ---- the 8-bit state -------------------------------------------------------------------------------------------
@@ -171,49 +169,12 @@ __global__ void __launch_bounds__(256) adam_control_kernel(AdamControlArgs a) {
 }
 
 // ---- squared norm of the gradient ----------------------------------------------------------------------------------
-// Squares and sums of at most eight of them in float32, everything further in float64, in an order that depends on the
-// sizes alone.  A square that overflows float32 counts as infinite.
+// Squares and sums in float64 (of the values rounded to float32, as the update takes them), so that neither a square overflows
+// nor the order of the sums shows in the result.  A conversion and a multiply-add per element stay below the time that the
+// gradient takes to arrive.
 
-template <typename G>
-__global__ void __launch_bounds__(kAdamThreads) adam_norm_kernel(const AdamTensor* __restrict__ tensors, const AdamChunk* __restrict__ chunks,
-                                                                 int64_t n_chunks, const G* __restrict__ flat, double* __restrict__ partials) {
+__device__ __forceinline__ void norm_finish(double acc, double* partials) {
   __shared__ double part_s[kAdamChunkBlocks];
-  pdl_trigger();
-  pdl_wait();
-  double acc = 0.0;
-  for (int64_t c = blockIdx.x; c < n_chunks; c += gridDim.x) {
-    const AdamChunk ch = chunks[c];
-    const AdamTensor* t = tensors + ch.tensor;
-    const G* g = flat ? flat + t->offset : static_cast<const G*>(t->grad);
-    const int64_t first = (int64_t)ch.index * (kAdamBlock * kAdamChunkBlocks);
-    const int64_t left = t->numel - first;
-    g += first;
-    float sum = 0.0f;
-    if (left >= kAdamBlock * kAdamChunkBlocks && ((uintptr_t)g & 15) == 0) {
-      constexpr int kVec = 16 / sizeof(G);
-      constexpr int kLoads = 8 / kVec;
-      Pack<G, kVec> v[kLoads];
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) v[i] = load_pack<G, kVec>(g + ((int64_t)i * kAdamThreads + threadIdx.x) * kVec);
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i)
-#pragma unroll
-        for (int k = 0; k < kVec; ++k) {
-          const float x = to_float(v[i].e[k]);
-          sum = fmaf(x, x, sum);
-        }
-    } else {
-      float x[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int e = i * kAdamThreads + threadIdx.x;
-        x[i] = e < left ? to_float(g[e]) : 0.0f;
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], sum);
-    }
-    acc += (double)sum;
-  }
 #pragma unroll
   for (int off = 16; off > 0; off >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, off);
   if ((threadIdx.x & 31) == 0) part_s[threadIdx.x >> 5] = acc;
@@ -225,12 +186,74 @@ __global__ void __launch_bounds__(kAdamThreads) adam_norm_kernel(const AdamTenso
   }
 }
 
+// A flat gradient: four 16-byte words a thread at a time, a contiguous stretch per CTA and turn.
+template <typename G>
+__global__ void __launch_bounds__(kAdamThreads) adam_norm_flat_kernel(const G* __restrict__ grad, int64_t n, double* __restrict__ partials) {
+  constexpr int kVec = 16 / sizeof(G);
+  constexpr int kUnroll = 4;
+  pdl_trigger();
+  pdl_wait();
+  const int64_t to_boundary = (int64_t)((16 - ((uintptr_t)grad & 15)) & 15) / (int64_t)sizeof(G);
+  const int64_t head = to_boundary < n ? to_boundary : n;
+  const int64_t words = (n - head) / kVec, tail = head + words * kVec;
+  const G* body = grad + head;
+  double acc = 0.0;
+  if (blockIdx.x == 0) {
+    double x = (int64_t)threadIdx.x < head ? (double)to_float(grad[threadIdx.x]) : 0.0;
+    acc = x * x;
+    x = (int64_t)threadIdx.x < n - tail ? (double)to_float(grad[tail + threadIdx.x]) : 0.0;
+    acc = fma(x, x, acc);
+  }
+  double part[kVec];
+#pragma unroll
+  for (int k = 0; k < kVec; ++k) part[k] = 0.0;
+  for (int64_t base = (int64_t)blockIdx.x * kAdamThreads * kUnroll; base < words; base += (int64_t)gridDim.x * kAdamThreads * kUnroll) {
+    Pack<G, kVec> v[kUnroll];
+    const int64_t first = base + threadIdx.x;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+      if (first + u * kAdamThreads < words) v[u] = load_pack<G, kVec>(body + (first + u * kAdamThreads) * kVec);
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+      if (first + u * kAdamThreads < words) {
+#pragma unroll
+        for (int k = 0; k < kVec; ++k) {
+          const double x = (double)to_float(v[u].e[k]);
+          part[k] = fma(x, x, part[k]);
+        }
+      }
+  }
+#pragma unroll
+  for (int k = 0; k < kVec; ++k) acc += part[k];
+  norm_finish(acc, partials);
+}
+
+// Gradients in tensors of their own: chunk by chunk.
+template <typename G>
+__global__ void __launch_bounds__(kAdamThreads) adam_norm_bound_kernel(const AdamChunk* __restrict__ chunks, int64_t n_chunks, double* __restrict__ partials) {
+  pdl_trigger();
+  pdl_wait();
+  double acc = 0.0;
+  for (int64_t c = blockIdx.x; c < n_chunks; c += gridDim.x) {
+    const G* g = static_cast<const G*>(chunks[c].grad);
+    const int left = chunks[c].count;
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int e = i * kAdamThreads + threadIdx.x;
+      x[i] = e < left ? to_float(g[e]) : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc = fma((double)x[i], (double)x[i], acc);
+  }
+  norm_finish(acc, partials);
+}
+
 // ---- the update ------------------------------------------------------------------------------------------------------
 
 struct AdamStepArgs {
-  const AdamTensor* tensors;
   const AdamChunk* chunks;
-  const void* flat;            // nullptr: the tensors' bound gradients
+  const void* flat;            // nullptr: the chunks' bound gradients
   void* exp_avg;
   void* exp_avg_sq;
   int16_t* base;               // two per block: m's, v's (8-bit states)
@@ -285,44 +308,85 @@ __device__ __forceinline__ void store8(T* p, const T (&x)[8], int lane, int n) {
   }
 }
 
+// A lane's eight codes: two 32-bit words of four neighbours (VEC), or eight single bytes.
+template <bool VEC>
+__device__ __forceinline__ void load_codes(uint32_t (&c)[8], const uint8_t* p, int lane) {
+  if constexpr (VEC) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t w = reinterpret_cast<const uint32_t*>(p)[h * 32 + lane];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) c[h * 4 + k] = (w >> (8 * k)) & 0xFFu;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = p[i * 32 + lane];
+  }
+}
+template <bool VEC>
+__device__ __forceinline__ void store_codes(uint8_t* p, const uint32_t (&c)[8], int lane) {
+  if constexpr (VEC) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      reinterpret_cast<uint32_t*>(p)[h * 32 + lane] =
+          __byte_perm(__byte_perm(c[h * 4], c[h * 4 + 1], 0x0040), __byte_perm(c[h * 4 + 2], c[h * 4 + 3], 0x0040), 0x5410);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i * 32 + lane] = (uint8_t)c[i];
+  }
+}
+
+// The hardware's square root and quotient (one and two units in the last place): the update is rounded by far less than
+// the state's own width, and the exact forms cost a quarter of the 8-bit step's instructions.
+__device__ __forceinline__ float sqrt_fast(float x) {
+  float r;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
 template <int BITS, typename G, bool VEC>
-__device__ __forceinline__ void adam_block(const AdamStepArgs& a, const AdamTensor& t, const AdamScalars& s, const G* grad, int64_t first, int64_t block,
-                                           int lane, int n) {
+__device__ __forceinline__ void adam_block(const AdamStepArgs& a, const AdamChunk& ch, const G* grad, int first, int lane, int n) {
   float p[8], m[8], v[8];
   G g[8];
-  load8<VEC>(p, (const float*)t.p + first, lane, n);
+  const int64_t slot = ch.slot + first;
+  const int64_t block = slot / kAdamBlock;
+  load8<VEC>(p, (const float*)ch.p + first, lane, n);
   load8<VEC>(g, grad + first, lane, n);
-  const int64_t slot = block * kAdamBlock;
+  uint32_t mc[8], vc[8];
+  Pack<int16_t, 2> base;
   if constexpr (BITS == 32) {
     load8<VEC>(m, (const float*)a.exp_avg + slot, lane, kAdamBlock);
     load8<VEC>(v, (const float*)a.exp_avg_sq + slot, lane, kAdamBlock);
   } else {
-    uint8_t mc[8], vc[8];
-    load8<VEC>(mc, (const uint8_t*)a.exp_avg + slot, lane, kAdamBlock);
-    load8<VEC>(vc, (const uint8_t*)a.exp_avg_sq + slot, lane, kAdamBlock);
-    const Pack<int16_t, 2> base = load_pack<int16_t, 2>(a.base + 2 * block);
+    load_codes<VEC>(mc, (const uint8_t*)a.exp_avg + slot, lane);
+    load_codes<VEC>(vc, (const uint8_t*)a.exp_avg_sq + slot, lane);
+    base = load_pack<int16_t, 2>(a.base + 2 * block);
+  }
+  const float grad_scale = a.scalars->grad_scale, inv_sqrt_bc2 = a.scalars->inv_sqrt_bc2;
+  const float minus_step = -a.lr * a.scalars->inv_bc1;
+  const float decay = 1.0f - a.lr * ch.weight_decay;
+  if constexpr (BITS == 8) {
+    const uint32_t mb = (uint32_t)(int)base.e[0] << 20, vb = (uint32_t)(int)base.e[1] << 20;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float mag = state_value(mc[i] & 127u, base.e[0]);
-      m[i] = (mc[i] & 128u) ? -mag : mag;
-      v[i] = state_value(vc[i], base.e[1]);
+      const uint32_t mag = mc[i] & 127u;
+      m[i] = __uint_as_float((mag ? (mag << 20) + mb : 0u) | ((mc[i] & 128u) << 24));
+      v[i] = __uint_as_float(vc[i] ? (vc[i] << 20) + vb : 0u);
     }
   }
-  const float decay = 1.0f - a.lr * t.weight_decay;
-  const float step = a.lr * s.inv_bc1;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float gi = to_float(g[i]) * s.grad_scale;
-    m[i] = a.beta1 * m[i] + a.one_minus_beta1 * gi;
-    v[i] = a.beta2 * v[i] + a.one_minus_beta2 * gi * gi;
-    p[i] = p[i] * decay - step * m[i] / (sqrtf(v[i]) * s.inv_sqrt_bc2 + a.eps);
+    const float gi = to_float(g[i]) * grad_scale;
+    m[i] = fmaf(a.beta1, m[i], a.one_minus_beta1 * gi);
+    v[i] = fmaf(a.beta2, v[i], a.one_minus_beta2 * gi * gi);
+    p[i] = fmaf(p[i], decay, __fdividef(minus_step * m[i], fmaf(sqrt_fast(v[i]), inv_sqrt_bc2, a.eps)));
   }
-  store8<VEC>(t.p + first, p, lane, n);
-  if (t.copy) {
+  store8<VEC>(ch.p + first, p, lane, n);
+  if (ch.copy) {
     __nv_bfloat16 c[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) c[i] = from_float<__nv_bfloat16>(p[i]);
-    store8<VEC>(t.copy + first, c, lane, n);
+    store8<VEC>(ch.copy + first, c, lane, n);
   }
   if constexpr (BITS == 32) {
     store8<VEC>((float*)a.exp_avg + slot, m, lane, kAdamBlock);
@@ -331,25 +395,35 @@ __device__ __forceinline__ void adam_block(const AdamStepArgs& a, const AdamTens
     uint32_t mbits = 0, vbits = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      mbits = max(mbits, finite_bits(__float_as_uint(m[i]) & 0x7FFFFFFFu));
-      vbits = max(vbits, finite_bits(__float_as_uint(v[i]) & 0x7FFFFFFFu));
+      mbits = max(mbits, __float_as_uint(m[i]) & 0x7FFFFFFFu);
+      vbits = max(vbits, __float_as_uint(v[i]) & 0x7FFFFFFFu);
     }
-    const int mbase = window_base(__reduce_max_sync(0xffffffffu, mbits), 127u);
-    const int vbase = window_base(__reduce_max_sync(0xffffffffu, vbits), 255u);
-    uint8_t mc[8], vc[8];
+    mbits = __reduce_max_sync(0xffffffffu, mbits);
+    vbits = __reduce_max_sync(0xffffffffu, vbits);
+    if (max(mbits, vbits) >= 0x7F800000u) {          // something is not finite: the largest of the others
+      mbits = vbits = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        mbits = max(mbits, finite_bits(__float_as_uint(m[i]) & 0x7FFFFFFFu));
+        vbits = max(vbits, finite_bits(__float_as_uint(v[i]) & 0x7FFFFFFFu));
+      }
+      mbits = __reduce_max_sync(0xffffffffu, mbits);
+      vbits = __reduce_max_sync(0xffffffffu, vbits);
+    }
+    const int mbase = window_base(mbits, 127u), vbase = window_base(vbits, 255u);
+    const uint32_t hash0 = slot_hash_start(slot), key = a.scalars->key;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const uint32_t r = slot_random(s.key, slot + lane_element<VEC>(lane, i));
-      const uint32_t sign = __float_as_uint(m[i]) >> 31;
-      const int cm = max(state_code(__float_as_uint(m[i]) & 0x7FFFFFFFu, (r & 0xFFFFu) << 4, mbase, 127), 0);
+      const uint32_t r = mix32((hash0 + (uint32_t)lane_element<VEC>(lane, i) * kSlotFactor) ^ key);
+      const uint32_t bits = __float_as_uint(m[i]);
+      const int cm = max(state_code(bits & 0x7FFFFFFFu, (r & 0xFFFFu) << 4, mbase, 127), 0);
       const int cv = max(state_code(__float_as_uint(v[i]) & 0x7FFFFFFFu, (r >> 16) << 4, vbase, 255), v[i] != 0.0f ? 1 : 0);
-      mc[i] = (uint8_t)(cm | (cm ? sign << 7 : 0u));
-      vc[i] = (uint8_t)cv;
+      mc[i] = (uint32_t)cm | (cm ? (bits >> 24) & 128u : 0u);
+      vc[i] = (uint32_t)cv;
     }
-    store8<VEC>((uint8_t*)a.exp_avg + slot, mc, lane, kAdamBlock);
-    store8<VEC>((uint8_t*)a.exp_avg_sq + slot, vc, lane, kAdamBlock);
+    store_codes<VEC>((uint8_t*)a.exp_avg + slot, mc, lane);
+    store_codes<VEC>((uint8_t*)a.exp_avg_sq + slot, vc, lane);
     if (lane == 0) {
-      Pack<int16_t, 2> base;
       base.e[0] = (int16_t)mbase;
       base.e[1] = (int16_t)vbase;
       store_pack<int16_t, 2>(a.base + 2 * block, base);
@@ -357,22 +431,19 @@ __device__ __forceinline__ void adam_block(const AdamStepArgs& a, const AdamTens
   }
 }
 
+// Chunks go from the last to the first: what the norm kernel read last is still in L2.
 template <int BITS, typename G>
-__global__ void __launch_bounds__(kAdamThreads) adam_step_kernel(AdamStepArgs a) {
-  const AdamChunk ch = a.chunks[blockIdx.x];
-  const AdamTensor t = a.tensors[ch.tensor];
-  const int lane = threadIdx.x & 31;
-  const int64_t local = (int64_t)ch.index * kAdamChunkBlocks + (threadIdx.x >> 5);     // block inside the tensor
-  const int64_t first = local * kAdamBlock;
-  const int64_t left = t.numel - first;
+__global__ void __launch_bounds__(kAdamThreads, 4) adam_step_kernel(AdamStepArgs a) {
+  const AdamChunk ch = a.chunks[gridDim.x - 1 - blockIdx.x];
+  const int lane = threadIdx.x & 31, first = (threadIdx.x >> 5) * kAdamBlock;
+  const int left = ch.count - first;
+  const G* grad = a.flat ? static_cast<const G*>(a.flat) + ch.offset : static_cast<const G*>(ch.grad);
+  const bool vec = left >= kAdamBlock && ((uintptr_t)ch.p & 15) == 0 && ((uintptr_t)ch.copy & 7) == 0 &&
+                   ((uintptr_t)grad & (sizeof(G) < 4 ? 7 : 15)) == 0;
   pdl_wait();
   if (left <= 0 || a.scalars->skip) return;
-  const AdamScalars s = *a.scalars;
-  const G* grad = a.flat ? static_cast<const G*>(a.flat) + t.offset : static_cast<const G*>(t.grad);
-  const bool vec = left >= kAdamBlock && ((uintptr_t)t.p & 15) == 0 && ((uintptr_t)t.copy & 7) == 0 &&
-                   ((uintptr_t)grad & (sizeof(G) < 4 ? 7 : 15)) == 0;
-  if (vec) adam_block<BITS, G, true>(a, t, s, grad, first, t.first_block + local, lane, kAdamBlock);
-  else adam_block<BITS, G, false>(a, t, s, grad, first, t.first_block + local, lane, left < kAdamBlock ? (int)left : kAdamBlock);
+  if (vec) adam_block<BITS, G, true>(a, ch, grad, first, lane, kAdamBlock);
+  else adam_block<BITS, G, false>(a, ch, grad, first, lane, left < kAdamBlock ? left : kAdamBlock);
 }
 
 // What the 8-bit state stands for, as bfloat16 (every value of the grid is one): blocks x 256.
@@ -405,7 +476,6 @@ static int adam_upload_scalars(solon_adamw* o, int64_t step) {
 }
 
 static void adam_free(solon_adamw* o) {
-  cudaFree(o->d_tensors);
   cudaFree(o->d_chunks);
   cudaFree(o->d_scalars);
   cudaFree(o->d_partials);
@@ -423,41 +493,44 @@ static int adam_alloc(T** ptr, size_t count) {
 
 static int64_t adam_blocks(int64_t numel) { return (numel + kAdamBlock - 1) / kAdamBlock; }
 
+static int adam_upload_chunks(solon_adamw* o) {
+  if (!o->chunks.empty()) SOLON_CUDA_TRY(cudaMemcpy(o->d_chunks, o->chunks.data(), o->chunks.size() * sizeof(AdamChunk), cudaMemcpyHostToDevice));
+  return SOLON_OK;
+}
+
 static int adam_create(solon_adamw* o, const int64_t* numel, float* const* params, void* const* copies, const float* weight_decay) {
-  std::vector<AdamChunk> chunks;
-  o->tensors.resize((size_t)o->n_tensors);
+  o->numel.assign(numel, numel + o->n_tensors);
   for (int i = 0; i < o->n_tensors; ++i) {
-    AdamTensor& t = o->tensors[(size_t)i];
-    t = AdamTensor();
-    t.p = params[i];
-    t.copy = copies ? static_cast<__nv_bfloat16*>(copies[i]) : nullptr;
-    t.offset = o->total;
-    t.numel = numel[i];
-    t.first_block = o->n_blocks;
-    t.weight_decay = weight_decay ? weight_decay[i] : 0.0f;
+    for (int64_t first = 0; first < numel[i]; first += kAdamChunk) {
+      AdamChunk c = {};
+      c.p = params[i] + first;
+      c.copy = copies && copies[i] ? static_cast<__nv_bfloat16*>(copies[i]) + first : nullptr;
+      c.offset = o->total + first;
+      c.slot = o->n_blocks * kAdamBlock + first;
+      c.count = (int)(numel[i] - first < kAdamChunk ? numel[i] - first : kAdamChunk);
+      c.weight_decay = weight_decay ? weight_decay[i] : 0.0f;
+      o->chunks.push_back(c);
+    }
     o->total += numel[i];
     o->n_blocks += adam_blocks(numel[i]);
-    const int64_t n = (adam_blocks(numel[i]) + kAdamChunkBlocks - 1) / kAdamChunkBlocks;
-    for (int64_t c = 0; c < n; ++c) chunks.push_back({i, (int)c});
   }
-  o->n_chunks = (int64_t)chunks.size();
+  o->n_chunks = (int64_t)o->chunks.size();
   if (o->n_chunks > 0x7fffffffLL) return SOLON_ERR_INVALID_ARG;
   o->norm_grid = o->num_sms * 4;
   if (o->norm_grid > o->n_chunks) o->norm_grid = o->n_chunks ? (int)o->n_chunks : 1;
   int rc;
-  if ((rc = adam_alloc(&o->d_tensors, o->tensors.size()))) return rc;
-  if ((rc = adam_alloc(&o->d_chunks, chunks.size()))) return rc;
+  if ((rc = adam_alloc(&o->d_chunks, o->chunks.size()))) return rc;
   if ((rc = adam_alloc(&o->d_scalars, 1))) return rc;
   if ((rc = adam_alloc(&o->d_partials, (size_t)o->norm_grid))) return rc;
-  SOLON_CUDA_TRY(cudaMemcpy(o->d_tensors, o->tensors.data(), o->tensors.size() * sizeof(AdamTensor), cudaMemcpyHostToDevice));
-  if (!chunks.empty()) SOLON_CUDA_TRY(cudaMemcpy(o->d_chunks, chunks.data(), chunks.size() * sizeof(AdamChunk), cudaMemcpyHostToDevice));
+  if ((rc = adam_upload_chunks(o))) return rc;
   return adam_upload_scalars(o, 0);
 }
 
 template <typename G>
 static int adam_norm(solon_adamw* o, const void* flat, cudaStream_t stream) {
-  return launch_dependent(adam_norm_kernel<G>, dim3((unsigned)o->norm_grid), dim3(kAdamThreads), 0, stream, (const AdamTensor*)o->d_tensors,
-                          (const AdamChunk*)o->d_chunks, o->n_chunks, static_cast<const G*>(flat), o->d_partials);
+  const dim3 grid((unsigned)o->norm_grid), block(kAdamThreads);
+  if (flat) return launch_dependent(adam_norm_flat_kernel<G>, grid, block, 0, stream, static_cast<const G*>(flat), o->total, o->d_partials);
+  return launch_dependent(adam_norm_bound_kernel<G>, grid, block, 0, stream, (const AdamChunk*)o->d_chunks, o->n_chunks, o->d_partials);
 }
 
 template <typename G>
@@ -538,10 +611,13 @@ int solon_adamw_bind_grads(solon_adamw* opt, const void* const* grads, int grad_
   if (!opt || !grads || (grad_dtype != SOLON_F32 && grad_dtype != SOLON_F64 && grad_dtype != SOLON_BF16)) return SOLON_ERR_INVALID_ARG;
   const uintptr_t size = grad_dtype == SOLON_F64 ? 8 : grad_dtype == SOLON_F32 ? 4 : 2;
   for (int i = 0; i < opt->n_tensors; ++i)
-    if (opt->tensors[(size_t)i].numel > 0 && (!grads[i] || ((uintptr_t)grads[i] & (size - 1)))) return SOLON_ERR_INVALID_ARG;
-  for (int i = 0; i < opt->n_tensors; ++i) opt->tensors[(size_t)i].grad = grads[i];
+    if (opt->numel[(size_t)i] > 0 && (!grads[i] || ((uintptr_t)grads[i] & (size - 1)))) return SOLON_ERR_INVALID_ARG;
   SOLON_CUDA_TRY(cudaDeviceSynchronize());     // steps in flight read the table
-  SOLON_CUDA_TRY(cudaMemcpy(opt->d_tensors, opt->tensors.data(), opt->tensors.size() * sizeof(AdamTensor), cudaMemcpyHostToDevice));
+  size_t chunk = 0;
+  for (int i = 0; i < opt->n_tensors; ++i)
+    for (int64_t first = 0; first < opt->numel[(size_t)i]; first += kAdamChunk) opt->chunks[chunk++].grad = static_cast<const char*>(grads[i]) + first * (int64_t)size;
+  int rc;
+  if ((rc = adam_upload_chunks(opt))) return rc;
   opt->grads_bound = 1;
   opt->grad_dtype = grad_dtype;
   return SOLON_OK;
@@ -601,7 +677,6 @@ int solon_adamw_step(solon_adamw* opt, const void* grad, int grad_dtype, double 
   if ((rc = launch_dependent(adam_control_kernel, dim3(1), dim3(256), 0, stream, c))) return rc;
   if (opt->n_chunks == 0) return SOLON_OK;
   AdamStepArgs a = {};
-  a.tensors = opt->d_tensors;
   a.chunks = opt->d_chunks;
   a.flat = grad;
   a.exp_avg = opt->exp_avg;
