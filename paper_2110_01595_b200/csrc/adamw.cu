@@ -308,34 +308,6 @@ __device__ __forceinline__ void store8(T* p, const T (&x)[8], int lane, int n) {
   }
 }
 
-// A lane's eight codes: two 32-bit words of four neighbours (VEC), or eight single bytes.
-template <bool VEC>
-__device__ __forceinline__ void load_codes(uint32_t (&c)[8], const uint8_t* p, int lane) {
-  if constexpr (VEC) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint32_t w = reinterpret_cast<const uint32_t*>(p)[h * 32 + lane];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) c[h * 4 + k] = (w >> (8 * k)) & 0xFFu;
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) c[i] = p[i * 32 + lane];
-  }
-}
-template <bool VEC>
-__device__ __forceinline__ void store_codes(uint8_t* p, const uint32_t (&c)[8], int lane) {
-  if constexpr (VEC) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      reinterpret_cast<uint32_t*>(p)[h * 32 + lane] =
-          __byte_perm(__byte_perm(c[h * 4], c[h * 4 + 1], 0x0040), __byte_perm(c[h * 4 + 2], c[h * 4 + 3], 0x0040), 0x5410);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) p[i * 32 + lane] = (uint8_t)c[i];
-  }
-}
-
 // The hardware's square root and quotient (one and two units in the last place): the update is rounded by far less than
 // the state's own width, and the exact forms cost a quarter of the 8-bit step's instructions.
 __device__ __forceinline__ float sqrt_fast(float x) {
@@ -343,6 +315,108 @@ __device__ __forceinline__ float sqrt_fast(float x) {
   asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
+
+// A lane's eight codes of m and of v: two 32-bit words of four neighbours each (VEC), or eight single bytes.
+template <bool VEC>
+struct LaneCodes {
+  uint32_t m[VEC ? 2 : 8], v[VEC ? 2 : 8];
+
+  __device__ __forceinline__ void load(const uint8_t* mp, const uint8_t* vp, int lane) {
+#pragma unroll
+    for (int i = 0; i < (VEC ? 2 : 8); ++i) {
+      m[i] = VEC ? reinterpret_cast<const uint32_t*>(mp)[i * 32 + lane] : mp[i * 32 + lane];
+      v[i] = VEC ? reinterpret_cast<const uint32_t*>(vp)[i * 32 + lane] : vp[i * 32 + lane];
+    }
+  }
+  __device__ __forceinline__ void store(uint8_t* mp, uint8_t* vp, int lane) const {
+#pragma unroll
+    for (int i = 0; i < (VEC ? 2 : 8); ++i) {
+      if constexpr (VEC) {
+        reinterpret_cast<uint32_t*>(mp)[i * 32 + lane] = m[i];
+        reinterpret_cast<uint32_t*>(vp)[i * 32 + lane] = v[i];
+      } else {
+        mp[i * 32 + lane] = (uint8_t)m[i];
+        vp[i * 32 + lane] = (uint8_t)v[i];
+      }
+    }
+  }
+  // Whether no code in the warp stands for zero (nearly always so: every weight that has had a gradient).
+  __device__ __forceinline__ bool none_zero() const {
+    uint32_t all = 0x80808080u;
+#pragma unroll
+    for (int i = 0; i < (VEC ? 2 : 8); ++i) {      // the top bit of a byte of the sums says that the byte is not 0
+      const uint32_t mm = (m[i] & 0x7F7F7F7Fu) + 0x7F7F7F7Fu, vv = ((v[i] & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | v[i];
+      all &= mm & vv;
+    }
+    return __all_sync(0xffffffffu, VEC ? all == 0x80808080u : (all & 0x80u) != 0);
+  }
+  __device__ __forceinline__ uint32_t m_at(int i) const { return VEC ? (m[i / 4 % 2] >> (8 * (i % 4))) & 0xFFu : m[i % (VEC ? 2 : 8)]; }
+  __device__ __forceinline__ uint32_t v_at(int i) const { return VEC ? (v[i / 4 % 2] >> (8 * (i % 4))) & 0xFFu : v[i % (VEC ? 2 : 8)]; }
+
+  __device__ __forceinline__ void decode(float (&mf)[8], float (&vf)[8], uint32_t mb, uint32_t vb, bool no_zeros) const {
+    if (no_zeros) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (VEC) {                       // the byte to bits 16 .. 23, four up, plus the base; the sign byte on top
+          const uint32_t mag = __byte_perm(m[i / 4] & 0x7F7F7F7Fu, 0u, 0x4044 | (i % 4) << 8), sign = __byte_perm(m[i / 4], 0u, 0x0444 | (i % 4) << 12);
+          mf[i] = __uint_as_float(((mag << 4) + mb) | (sign & 0x80000000u));
+          vf[i] = __uint_as_float((__byte_perm(v[i / 4], 0u, 0x4044 | (i % 4) << 8) << 4) + vb);
+        } else {
+          mf[i] = __uint_as_float((((m[i] & 127u) << 20) + mb) | ((m[i] & 128u) << 24));
+          vf[i] = __uint_as_float((v[i] << 20) + vb);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t c = m_at(i), mag = c & 127u, q = v_at(i);
+        mf[i] = __uint_as_float((mag ? (mag << 20) + mb : 0u) | ((c & 128u) << 24));
+        vf[i] = __uint_as_float(q ? (q << 20) + vb : 0u);
+      }
+    }
+  }
+
+  // `simple`: every value is finite and no v is 0, which allows the shorter forms of the same codes.
+  __device__ __forceinline__ void encode(const float (&mf)[8], const float (&vf)[8], int mbase, int vbase, int64_t slot, uint32_t key, int lane, bool simple) {
+    const uint32_t hash0 = slot_hash_start(slot);
+    uint32_t cm[8], cv[8];
+    if (simple) {
+      const uint32_t mshift = (uint32_t)mbase << 20, vshift = ((uint32_t)vbase + 1u) << 20;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t r = mix32((hash0 + (uint32_t)lane_element<VEC>(lane, i) * kSlotFactor) ^ key);
+        const uint32_t mbits = __float_as_uint(mf[i]) & 0x7FFFFFFFu;
+        cm[i] = (uint32_t)__vimin_s32_relu((int)(mbits + ((r & 0xFFFFu) << 4) - mshift) >> 20, 127);
+        cv[i] = (uint32_t)__vimin_s32_relu((int)(__float_as_uint(vf[i]) + ((r >> 16) << 4) - vshift) >> 20, 254);     // one less
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t r = mix32((hash0 + (uint32_t)lane_element<VEC>(lane, i) * kSlotFactor) ^ key);
+        cm[i] = (uint32_t)max(state_code(__float_as_uint(mf[i]) & 0x7FFFFFFFu, (r & 0xFFFFu) << 4, mbase, 127), 0);
+        cv[i] = (uint32_t)max(state_code(__float_as_uint(vf[i]) & 0x7FFFFFFFu, (r >> 16) << 4, vbase, 255), vf[i] != 0.0f ? 1 : 0);
+      }
+    }
+    if constexpr (VEC) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        auto four = [](uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t pick) {      // one byte of each
+          return __byte_perm(__byte_perm(a, b, pick), __byte_perm(c, d, pick), 0x5410);
+        };
+        const uint32_t mag = four(cm[4 * h], cm[4 * h + 1], cm[4 * h + 2], cm[4 * h + 3], 0x0040);
+        const uint32_t sign = four(__float_as_uint(mf[4 * h]), __float_as_uint(mf[4 * h + 1]), __float_as_uint(mf[4 * h + 2]), __float_as_uint(mf[4 * h + 3]), 0x0073);
+        m[h] = mag | (sign & (mag + 0x7F7F7F7Fu) & 0x80808080u);                             // no sign on a zero
+        v[h] = four(cv[4 * h], cv[4 * h + 1], cv[4 * h + 2], cv[4 * h + 3], 0x0040) + (simple ? 0x01010101u : 0u);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        m[i] = cm[i] | (cm[i] ? (__float_as_uint(mf[i]) >> 24) & 128u : 0u);
+        v[i] = cv[i] + (simple ? 1u : 0u);
+      }
+    }
+  }
+};
 
 template <int BITS, typename G, bool VEC>
 __device__ __forceinline__ void adam_block(const AdamStepArgs& a, const AdamChunk& ch, const G* grad, int first, int lane, int n) {
@@ -352,27 +426,22 @@ __device__ __forceinline__ void adam_block(const AdamStepArgs& a, const AdamChun
   const int64_t block = slot / kAdamBlock;
   load8<VEC>(p, (const float*)ch.p + first, lane, n);
   load8<VEC>(g, grad + first, lane, n);
-  uint32_t mc[8], vc[8];
+  LaneCodes<VEC> codes;
   Pack<int16_t, 2> base;
   if constexpr (BITS == 32) {
     load8<VEC>(m, (const float*)a.exp_avg + slot, lane, kAdamBlock);
     load8<VEC>(v, (const float*)a.exp_avg_sq + slot, lane, kAdamBlock);
   } else {
-    load_codes<VEC>(mc, (const uint8_t*)a.exp_avg + slot, lane);
-    load_codes<VEC>(vc, (const uint8_t*)a.exp_avg_sq + slot, lane);
+    codes.load((const uint8_t*)a.exp_avg + slot, (const uint8_t*)a.exp_avg_sq + slot, lane);
     base = load_pack<int16_t, 2>(a.base + 2 * block);
   }
   const float grad_scale = a.scalars->grad_scale, inv_sqrt_bc2 = a.scalars->inv_sqrt_bc2;
   const float minus_step = -a.lr * a.scalars->inv_bc1;
   const float decay = 1.0f - a.lr * ch.weight_decay;
+  bool simple = false;
   if constexpr (BITS == 8) {
-    const uint32_t mb = (uint32_t)(int)base.e[0] << 20, vb = (uint32_t)(int)base.e[1] << 20;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t mag = mc[i] & 127u;
-      m[i] = __uint_as_float((mag ? (mag << 20) + mb : 0u) | ((mc[i] & 128u) << 24));
-      v[i] = __uint_as_float(vc[i] ? (vc[i] << 20) + vb : 0u);
-    }
+    simple = codes.none_zero();
+    codes.decode(m, v, (uint32_t)(int)base.e[0] << 20, (uint32_t)(int)base.e[1] << 20, simple);
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -396,11 +465,12 @@ __device__ __forceinline__ void adam_block(const AdamStepArgs& a, const AdamChun
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       mbits = max(mbits, __float_as_uint(m[i]) & 0x7FFFFFFFu);
-      vbits = max(vbits, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+      vbits = max(vbits, __float_as_uint(v[i]));
     }
     mbits = __reduce_max_sync(0xffffffffu, mbits);
     vbits = __reduce_max_sync(0xffffffffu, vbits);
     if (max(mbits, vbits) >= 0x7F800000u) {          // something is not finite: the largest of the others
+      simple = false;
       mbits = vbits = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -410,24 +480,13 @@ __device__ __forceinline__ void adam_block(const AdamStepArgs& a, const AdamChun
       mbits = __reduce_max_sync(0xffffffffu, mbits);
       vbits = __reduce_max_sync(0xffffffffu, vbits);
     }
-    const int mbase = window_base(mbits, 127u), vbase = window_base(vbits, 255u);
-    const uint32_t hash0 = slot_hash_start(slot), key = a.scalars->key;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t r = mix32((hash0 + (uint32_t)lane_element<VEC>(lane, i) * kSlotFactor) ^ key);
-      const uint32_t bits = __float_as_uint(m[i]);
-      const int cm = max(state_code(bits & 0x7FFFFFFFu, (r & 0xFFFFu) << 4, mbase, 127), 0);
-      const int cv = max(state_code(__float_as_uint(v[i]) & 0x7FFFFFFFu, (r >> 16) << 4, vbase, 255), v[i] != 0.0f ? 1 : 0);
-      mc[i] = (uint32_t)cm | (cm ? (bits >> 24) & 128u : 0u);
-      vc[i] = (uint32_t)cv;
-    }
-    store_codes<VEC>((uint8_t*)a.exp_avg + slot, mc, lane);
-    store_codes<VEC>((uint8_t*)a.exp_avg_sq + slot, vc, lane);
-    if (lane == 0) {
-      base.e[0] = (int16_t)mbase;
-      base.e[1] = (int16_t)vbase;
-      store_pack<int16_t, 2>(a.base + 2 * block, base);
-    }
+    // (v was not 0 and beta2 leaves it so: a quarter of the smallest value of the grid is still a float32)
+    simple = simple && a.beta2 >= 0.25f;
+    base.e[0] = (int16_t)window_base(mbits, 127u);
+    base.e[1] = (int16_t)window_base(vbits, 255u);
+    codes.encode(m, v, base.e[0], base.e[1], slot, a.scalars->key, lane, simple);
+    codes.store((uint8_t*)a.exp_avg + slot, (uint8_t*)a.exp_avg_sq + slot, lane);
+    if (lane == 0) store_pack<int16_t, 2>(a.base + 2 * block, base);
   }
 }
 
