@@ -408,7 +408,7 @@ int solon_adamw_step(solon_adamw* opt, const void* grad, int grad_dtype, double 
 int solon_adamw_set_step(solon_adamw* opt, int64_t step);
 int solon_adamw_get_steps(solon_adamw* opt, int64_t* applied, int64_t* skipped);
 
-/* What an 8-bit state stands for: blocks x 256 bfloat16 each (exact), 8-byte aligned.  Enqueued on cuda_stream. */
+/* What an 8-bit state stands for: blocks x 256 bfloat16 each (exact), 16-byte aligned.  Enqueued on cuda_stream. */
 int solon_adamw_moments(solon_adamw* opt, void* exp_avg_out, void* exp_avg_sq_out, void* cuda_stream);
 
 /* ------------------------------------------------------------------------------------------

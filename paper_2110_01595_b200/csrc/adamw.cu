@@ -32,6 +32,7 @@ struct alignas(64) AdamChunk {
   int64_t slot;              // first element in the state
   int count;                 // elements
   float weight_decay;
+  int ends;                  // 1: the tensor's first chunk, 2: its last
 };
 
 // What the update reads, written by the control kernel of the same step.
@@ -92,10 +93,6 @@ __device__ __forceinline__ uint32_t slot_hash_start(int64_t slot) {
 // v, which is never 0 unless v is - a zero v under a moving m would divide by eps.  Non-finite values take the top code
 // and have no part in the choice of the window, so they spoil no other element of their block.
 constexpr uint32_t kTopFinite = 0x7F7u;                // rank of the largest finite value of the grid
-
-__device__ __forceinline__ float state_value(uint32_t code, int base) {
-  return code ? __uint_as_float((code + (uint32_t)base) << 20) : 0.0f;
-}
 
 // Largest finite magnitude of the block as bits (float order = integer order for non-negative floats).
 __device__ __forceinline__ uint32_t finite_bits(uint32_t bits) { return bits < 0x7F800000u ? bits : 0u; }
@@ -261,11 +258,84 @@ struct AdamStepArgs {
   float beta1, one_minus_beta1, beta2, one_minus_beta2, eps, lr;
 };
 
-// A lane's eight elements of its warp's block: two groups of four consecutive ones (VEC), or every 32nd (any alignment,
-// and blocks that the tensor does not fill).
+// How a warp goes through its block.  A lane has two groups of four consecutive elements; where parameters or gradients do not
+// start on the groups' boundaries (tensors that are pieces of one vector, at any offset: what the aggregate's users have), a
+// group is put together from the two aligned words that hold it, and parameters go back as aligned words too.  Single
+// accesses of four bytes move the same bytes in four times as many requests, which caps what is on the way: 11.2 M weights of
+// an odd offset take 63 us that way against 49 us aligned.  The aligned words reach up to three elements beyond the block,
+// so a tensor's first and last block, and blocks that are not full, go element by element (every 32nd a lane's).
+enum BlockMode { kSingle, kAligned, kShifted };
+
 template <bool VEC>
 __device__ __forceinline__ int lane_element(int lane, int i) {
   return VEC ? ((i >> 2) * 32 + lane) * 4 + (i & 3) : i * 32 + lane;
+}
+
+// Four consecutive elements at p from 16-byte words; delta: elements from the word that holds the first to p.
+__device__ __forceinline__ void select4(float (&x)[4], const float4& a, const float4& b, int delta) {
+  const float e[7] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) x[k] = delta < 2 ? (delta == 0 ? e[k] : e[k + 1 < 7 ? k + 1 : 6]) : (delta == 2 ? e[k + 2 < 7 ? k + 2 : 6] : e[k + 3]);
+}
+template <typename T>
+__device__ __forceinline__ void load8_shifted(T (&x)[8], const T* p, int lane) {
+  if constexpr (sizeof(T) == 4) {
+    const int delta = (int)(((uintptr_t)p >> 2) & 3);
+    const float4* w = reinterpret_cast<const float4*>(p - delta);
+    float4 a[2], b[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      a[h] = w[h * 32 + lane];
+      b[h] = w[h * 32 + lane + (delta ? 1 : 0)];
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float q[4];
+      select4(q, a[h], b[h], delta);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[h * 4 + k] = q[k];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = p[lane_element<true>(lane, i)];
+  }
+}
+// Word j of the shifted block holds the last delta elements of group j - 1 and the first 4 - delta of group j; the block's first
+// and last word are shared with its neighbours, so their elements go one by one.
+__device__ __forceinline__ void store8_shifted(float* p, const float (&x)[8], int lane) {
+  const int delta = (int)(((uintptr_t)p >> 2) & 3);
+  float4* w = reinterpret_cast<float4*>(p - delta);
+  if (delta == 0) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) w[h * 32 + lane] = make_float4(x[h * 4], x[h * 4 + 1], x[h * 4 + 2], x[h * 4 + 3]);
+    return;
+  }
+  float before[2][3];                          // elements 1 .. 3 of the group before
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    const float last = __shfl_sync(0xffffffffu, x[k + 1], 31);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) before[h][k] = __shfl_up_sync(0xffffffffu, x[h * 4 + k + 1], 1);
+    if (lane == 0) before[1][k] = last;
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const float e[7] = {before[h][0], before[h][1], before[h][2], x[h * 4], x[h * 4 + 1], x[h * 4 + 2], x[h * 4 + 3]};
+    float q[4];                                // elements -delta .. 3 - delta of the group
+#pragma unroll
+    for (int k = 0; k < 4; ++k) q[k] = delta == 1 ? e[k + 2 < 7 ? k + 2 : 6] : delta == 2 ? e[k + 1] : e[k];
+    if (h > 0 || lane > 0) w[h * 32 + lane] = make_float4(q[0], q[1], q[2], q[3]);
+  }
+  if (lane == 0) {
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (k < 4 - delta) p[k] = x[k];
+  }
+  if (lane == 31) {
+#pragma unroll
+    for (int k = 1; k < 4; ++k)
+      if (k >= 4 - delta) p[252 + k] = x[4 + k];
+  }
 }
 
 template <bool VEC, typename T>
@@ -418,14 +488,20 @@ struct LaneCodes {
   }
 };
 
-template <int BITS, typename G, bool VEC>
+template <int BITS, typename G, BlockMode MODE>
 __device__ __forceinline__ void adam_block(const AdamStepArgs& a, const AdamChunk& ch, const G* grad, int first, int lane, int n) {
+  constexpr bool VEC = MODE != kSingle;
   float p[8], m[8], v[8];
   G g[8];
   const int64_t slot = ch.slot + first;
   const int64_t block = slot / kAdamBlock;
-  load8<VEC>(p, (const float*)ch.p + first, lane, n);
-  load8<VEC>(g, grad + first, lane, n);
+  if constexpr (MODE == kShifted) {
+    load8_shifted(p, (const float*)ch.p + first, lane);
+    load8_shifted(g, grad + first, lane);
+  } else {
+    load8<VEC>(p, (const float*)ch.p + first, lane, n);
+    load8<VEC>(g, grad + first, lane, n);
+  }
   LaneCodes<VEC> codes;
   Pack<int16_t, 2> base;
   if constexpr (BITS == 32) {
@@ -450,12 +526,19 @@ __device__ __forceinline__ void adam_block(const AdamStepArgs& a, const AdamChun
     v[i] = fmaf(a.beta2, v[i], a.one_minus_beta2 * gi * gi);
     p[i] = fmaf(p[i], decay, __fdividef(minus_step * m[i], fmaf(sqrt_fast(v[i]), inv_sqrt_bc2, a.eps)));
   }
-  store8<VEC>(ch.p + first, p, lane, n);
+  if constexpr (MODE == kShifted) store8_shifted(ch.p + first, p, lane);
+  else store8<VEC>(ch.p + first, p, lane, n);
   if (ch.copy) {
     __nv_bfloat16 c[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) c[i] = from_float<__nv_bfloat16>(p[i]);
-    store8<VEC>(ch.copy + first, c, lane, n);
+    __nv_bfloat16* copy = ch.copy + first;
+    if (MODE == kShifted && ((uintptr_t)copy & 7) != 0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) copy[lane_element<true>(lane, i)] = c[i];
+    } else {
+      store8<VEC>(copy, c, lane, n);
+    }
   }
   if constexpr (BITS == 32) {
     store8<VEC>((float*)a.exp_avg + slot, m, lane, kAdamBlock);
@@ -497,30 +580,38 @@ __global__ void __launch_bounds__(kAdamThreads, 4) adam_step_kernel(AdamStepArgs
   const int lane = threadIdx.x & 31, first = (threadIdx.x >> 5) * kAdamBlock;
   const int left = ch.count - first;
   const G* grad = a.flat ? static_cast<const G*>(a.flat) + ch.offset : static_cast<const G*>(ch.grad);
-  const bool vec = left >= kAdamBlock && ((uintptr_t)ch.p & 15) == 0 && ((uintptr_t)ch.copy & 7) == 0 &&
-                   ((uintptr_t)grad & (sizeof(G) < 4 ? 7 : 15)) == 0;
+  const bool aligned = ((uintptr_t)ch.p & 15) == 0 && ((uintptr_t)ch.copy & 7) == 0 && ((uintptr_t)grad & (sizeof(G) < 4 ? 7 : 15)) == 0;
+  const bool full = left >= kAdamBlock;
+  const bool inside = full && !(first == 0 && (ch.ends & 1)) && !(left == kAdamBlock && (ch.ends & 2));
   pdl_wait();
   if (left <= 0 || a.scalars->skip) return;
-  if (vec) adam_block<BITS, G, true>(a, ch, grad, first, lane, kAdamBlock);
-  else adam_block<BITS, G, false>(a, ch, grad, first, lane, left < kAdamBlock ? left : kAdamBlock);
+  if (aligned && full) adam_block<BITS, G, kAligned>(a, ch, grad, first, lane, kAdamBlock);
+  else if (inside) adam_block<BITS, G, kShifted>(a, ch, grad, first, lane, kAdamBlock);
+  else adam_block<BITS, G, kSingle>(a, ch, grad, first, lane, full ? kAdamBlock : left);
 }
 
-// What the 8-bit state stands for, as bfloat16 (every value of the grid is one): blocks x 256.
-__global__ void __launch_bounds__(256) adam_moments_kernel(const uint8_t* __restrict__ m, const uint8_t* __restrict__ v, const int16_t* __restrict__ base,
-                                                           int64_t n_quads, __nv_bfloat16* __restrict__ m_out, __nv_bfloat16* __restrict__ v_out) {
-  for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < n_quads; q += (int64_t)gridDim.x * 256) {
-    const Pack<int16_t, 2> b = load_pack<int16_t, 2>(base + 2 * (q / (kAdamBlock / 4)));
-    const Pack<uint8_t, 4> mc = load_pack<uint8_t, 4>(m + 4 * q), vc = load_pack<uint8_t, 4>(v + 4 * q);
-    Pack<__nv_bfloat16, 4> mo, vo;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float mag = state_value(mc.e[k] & 127u, b.e[0]);
-      mo.e[k] = from_float<__nv_bfloat16>((mc.e[k] & 128u) ? -mag : mag);
-      vo.e[k] = from_float<__nv_bfloat16>(state_value(vc.e[k], b.e[1]));
-    }
-    store_pack<__nv_bfloat16, 4>(m_out + 4 * q, mo);
-    store_pack<__nv_bfloat16, 4>(v_out + 4 * q, vo);
-  }
+// What the 8-bit state stands for, as bfloat16: blocks x 256.  A value of the grid has zeros in the low 20 of its float32's
+// bits, so the upper 16 are its bfloat16: (code + base) << 4, two to a word.  16 codes a thread.
+__device__ __forceinline__ uint32_t two_moments(uint32_t c, uint32_t base2, uint32_t mask) {      // codes in bytes 0 and 2
+  const uint32_t mag = c & mask;
+  const uint32_t nonzero = ((mag + 0x00FF00FFu) >> 8) & 0x00010001u;
+  return (((mag + base2) << 4) & (nonzero * 0xFFFFu)) | ((c & ~mask & 0x00800080u) << 8);
+}
+__device__ __forceinline__ uint4 eight_moments(uint32_t lo, uint32_t hi, uint32_t base2, uint32_t mask) {
+  return make_uint4(two_moments(__byte_perm(lo, 0u, 0x4140), base2, mask), two_moments(__byte_perm(lo, 0u, 0x4342), base2, mask),
+                    two_moments(__byte_perm(hi, 0u, 0x4140), base2, mask), two_moments(__byte_perm(hi, 0u, 0x4342), base2, mask));
+}
+__global__ void __launch_bounds__(256) adam_moments_kernel(const uint4* __restrict__ m, const uint4* __restrict__ v, const uint32_t* __restrict__ base,
+                                                           int64_t n_words, uint4* __restrict__ m_out, uint4* __restrict__ v_out) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n_words) return;
+  const uint4 mc = m[i], vc = v[i];
+  const uint32_t b = base[i / (kAdamBlock / 16)];
+  const uint32_t mb = __byte_perm(b, 0u, 0x1010), vb = __byte_perm(b, 0u, 0x3232);
+  m_out[2 * i] = eight_moments(mc.x, mc.y, mb, 0x007F007Fu);
+  m_out[2 * i + 1] = eight_moments(mc.z, mc.w, mb, 0x007F007Fu);
+  v_out[2 * i] = eight_moments(vc.x, vc.y, vb, 0x00FF00FFu);
+  v_out[2 * i + 1] = eight_moments(vc.z, vc.w, vb, 0x00FF00FFu);
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
@@ -568,6 +659,7 @@ static int adam_create(solon_adamw* o, const int64_t* numel, float* const* param
       c.slot = o->n_blocks * kAdamBlock + first;
       c.count = (int)(numel[i] - first < kAdamChunk ? numel[i] - first : kAdamChunk);
       c.weight_decay = weight_decay ? weight_decay[i] : 0.0f;
+      c.ends = (first == 0 ? 1 : 0) | (first + kAdamChunk >= numel[i] ? 2 : 0);
       o->chunks.push_back(c);
     }
     o->total += numel[i];
@@ -754,12 +846,12 @@ int solon_adamw_step(solon_adamw* opt, const void* grad, int grad_dtype, double 
 
 int solon_adamw_moments(solon_adamw* opt, void* exp_avg_out, void* exp_avg_sq_out, void* cuda_stream) {
   if (!opt || opt->bits != 8 || !exp_avg_out || !exp_avg_sq_out) return SOLON_ERR_INVALID_ARG;
-  if (((uintptr_t)exp_avg_out | (uintptr_t)exp_avg_sq_out) & 7) return SOLON_ERR_INVALID_ARG;
-  const int64_t quads = opt->n_blocks * (kAdamBlock / 4);
-  if (quads == 0) return SOLON_OK;
-  const int64_t want = (quads + 255) / 256, cap = (int64_t)opt->num_sms * 16;
-  adam_moments_kernel<<<(unsigned)(want < cap ? want : cap), 256, 0, (cudaStream_t)cuda_stream>>>(
-      (const uint8_t*)opt->exp_avg, (const uint8_t*)opt->exp_avg_sq, opt->base, quads, (__nv_bfloat16*)exp_avg_out, (__nv_bfloat16*)exp_avg_sq_out);
+  if (((uintptr_t)exp_avg_out | (uintptr_t)exp_avg_sq_out) & 15) return SOLON_ERR_INVALID_ARG;
+  const int64_t words = opt->n_blocks * (kAdamBlock / 16);
+  if (words == 0) return SOLON_OK;
+  if ((words + 255) / 256 > 0x7fffffffLL) return SOLON_ERR_INVALID_ARG;
+  adam_moments_kernel<<<(unsigned)((words + 255) / 256), 256, 0, (cudaStream_t)cuda_stream>>>(
+      (const uint4*)opt->exp_avg, (const uint4*)opt->exp_avg_sq, (const uint32_t*)opt->base, words, (uint4*)exp_avg_out, (uint4*)exp_avg_sq_out);
   SOLON_CUDA_TRY(cudaGetLastError());
   return SOLON_OK;
 }
