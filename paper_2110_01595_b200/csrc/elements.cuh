@@ -47,6 +47,15 @@ __device__ __forceinline__ uint4 load16_once(const void* p) {
   return v;
 }
 
+// 16 bytes to shared memory without passing registers, in groups that a thread waits for by their number (its own copies only).
+__device__ __forceinline__ void copy16_async(void* dst_smem, const void* src, bool inside) {
+  const int bytes = inside ? 16 : 0;           // 0: the 16 bytes are filled with zeros, nothing is read
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst_smem)), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 // The elements of 16 bytes as float32, and their largest value (NaN if there is one).
 template <typename T>
 struct Word16;
@@ -60,6 +69,15 @@ struct Word16<float> {
     x[2] = __uint_as_float(v.z);
     x[3] = __uint_as_float(v.w);
   }
+  static constexpr uint32_t kMinusInf = 0xFF800000u;                  // two or one elements of -infinity
+  static __device__ __forceinline__ uint32_t first(float v) { return *reinterpret_cast<const uint32_t*>(&v); }
+  static __device__ __forceinline__ uint32_t twice(float v) { return __float_as_uint(v); }
+  static __device__ __forceinline__ uint32_t at_least(uint32_t w, uint32_t low) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(__uint_as_float(w)), "f"(__uint_as_float(low)));
+    return __float_as_uint(r);
+  }
+  static __device__ __forceinline__ float widest(uint32_t w) { return __uint_as_float(w); }
   static __device__ __forceinline__ uint4 pack(const float (&x)[4]) {
     return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
   }
@@ -96,12 +114,18 @@ struct Word16<__nv_bfloat16> {
     asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
     return m;
   }
-  static __device__ __forceinline__ float largest(const uint4& v) {
-    const uint32_t m = max2(max2(v.x, v.y), max2(v.z, v.w));
+  static constexpr uint32_t kMinusInf = 0xFF80FF80u;
+  static __device__ __forceinline__ uint32_t first(__nv_bfloat16 v) { return (kMinusInf & 0xFFFF0000u) | *reinterpret_cast<const uint16_t*>(&v); }
+  static __device__ __forceinline__ uint32_t twice(float v) { return join(v, v); }
+  static __device__ __forceinline__ uint32_t at_least(uint32_t w, uint32_t low) { return max2(w, low); }
+  static __device__ __forceinline__ float widest(uint32_t w) {
     float a, b, r;
-    pair(m, a, b);
+    pair(w, a, b);
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
+  }
+  static __device__ __forceinline__ float largest(const uint4& v) {
+    return widest(max2(max2(v.x, v.y), max2(v.z, v.w)));
   }
 };
 
@@ -130,12 +154,18 @@ struct Word16<__half> {
     asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
     return m;
   }
-  static __device__ __forceinline__ float largest(const uint4& v) {
-    const uint32_t m = max2(max2(v.x, v.y), max2(v.z, v.w));
+  static constexpr uint32_t kMinusInf = 0xFC00FC00u;
+  static __device__ __forceinline__ uint32_t first(__half v) { return (kMinusInf & 0xFFFF0000u) | *reinterpret_cast<const uint16_t*>(&v); }
+  static __device__ __forceinline__ uint32_t twice(float v) { return join(v, v); }
+  static __device__ __forceinline__ uint32_t at_least(uint32_t w, uint32_t low) { return max2(w, low); }
+  static __device__ __forceinline__ float widest(uint32_t w) {
     float a, b, r;
-    pair(m, a, b);
+    pair(w, a, b);
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
+  }
+  static __device__ __forceinline__ float largest(const uint4& v) {
+    return widest(max2(max2(v.x, v.y), max2(v.z, v.w)));
   }
 };
 

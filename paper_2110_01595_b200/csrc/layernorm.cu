@@ -67,14 +67,6 @@ __device__ __forceinline__ void team_sum(float (&v)[N], float* slots, int& turn,
   }
 }
 
-__device__ __forceinline__ void copy16_async(void* dst_smem, const void* src, bool inside) {
-  const int bytes = inside ? 16 : 0;           // 0: the 16 bytes are filled with zeros, nothing is read
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst_smem)), "l"(src), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 __device__ __forceinline__ float param_at(const void* p, int is_f32, int dtype, int64_t c) {
   if (is_f32) return static_cast<const float*>(p)[c];
   if (dtype == SOLON_BF16) return to_float(static_cast<const __nv_bfloat16*>(p)[c]);

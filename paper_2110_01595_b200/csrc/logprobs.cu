@@ -17,30 +17,36 @@
 
 namespace solon {
 
-// Bound by memory, with the exponentials close behind (one a logit: at 16 a clock and SM 60 % of the time that bfloat16 logits
-// take to arrive), so the arithmetic beside them is kept short: two values an instruction where there is one for it, sums
-// against a reference value that need not be the maximum, and one comparison per 16 bytes for everything that is rare.
+// Bound by memory, with the exponentials (one a logit: at 16 a clock and SM 60 % of the time that bfloat16 logits take to
+// arrive) and the instructions beside them close behind, so those are kept few: two values an instruction, one multiply-add
+// from a logit to its exponent, and one comparison per 64 bytes for everything that is rare.
 constexpr int kLpThreads = 256;
 constexpr int kLpWarps = kLpThreads / 32;
-constexpr int kLpUnroll = 4;                   // 16-byte words a thread has in flight
+constexpr int kLpWords = 4;                    // 16-byte words of a thread in an iteration
+constexpr int kLpChunk = kLpThreads * kLpWords;
+constexpr int kLpCtasPerSm = 4;
 constexpr int kLpMaxCluster = 8;
-constexpr int kLpCandidates = 2048;
+constexpr int kLpCandidates = 1024;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
+
+// Iterations' words in shared memory: three beside the 16 KB of candidates would leave room for three CTAs on an SM only.
+template <bool TOP>
+constexpr int lp_stages = TOP ? 2 : 3;
 
 // Order of the likeliest tokens as one integer: value first (NaN above all, -0 = +0), of equal values the lower index.
 __device__ __forceinline__ uint32_t order_bits(float z) {
   const uint32_t b = __float_as_uint(z + 0.0f);
   return z != z ? 0xFFFFFFFFu : (b & 0x80000000u) ? ~b : (b | 0x80000000u);      // > 0 for every value
 }
+__device__ __forceinline__ float order_value(uint32_t o) {
+  return o == 0xFFFFFFFFu ? NAN : __uint_as_float((o & 0x80000000u) ? (o & 0x7FFFFFFFu) : ~o);
+}
 __device__ __forceinline__ unsigned long long rank_key(float z, uint32_t index) {
   return ((unsigned long long)order_bits(z) << 32) | (0xFFFFFFFFu - index);
 }
 __device__ __forceinline__ uint32_t key_index(unsigned long long key) { return 0xFFFFFFFFu - (uint32_t)key; }
-__device__ __forceinline__ float key_value(unsigned long long key) {
-  const uint32_t o = (uint32_t)(key >> 32);
-  return o == 0xFFFFFFFFu ? NAN : __uint_as_float((o & 0x80000000u) ? (o & 0x7FFFFFFFu) : ~o);
-}
+__device__ __forceinline__ float key_value(unsigned long long key) { return order_value((uint32_t)(key >> 32)); }
 
 struct LogprobArgs {
   const void* logits;
@@ -55,69 +61,127 @@ struct LogprobArgs {
   int top_k;
 };
 
-// Softmax sums of a part of a row: largest logit, and against a reference r (in base 2, t = (z - r) log2 e)
-// s = sum 2^t, a = sum 2^t t.
+// Softmax sums of a part of a row against its largest logit: s = sum 2^t, a = sum 2^t t, t = (z - peak) log2 e.
+// Without a finite logit s = a = 0; s is NaN where the row has no softmax.
 struct SoftmaxPart {
-  float peak, ref, s, a;
+  float peak, s, a;
 };
 
-// The same sums against another reference: t' = t + d, d = (r - r') log2 e.  A part whose terms all vanish adds nothing; one
-// without terms has no reference to move from.
-__device__ __forceinline__ void shift_part(SoftmaxPart& p, float ref) {
-  if (p.s == 0.0f) {
-    p.ref = ref;
-    return;
+__device__ __forceinline__ SoftmaxPart join_parts(const SoftmaxPart& x, const SoftmaxPart& y) {
+  SoftmaxPart r;
+  r.peak = fmaxf(x.peak, y.peak);
+  // (a part that holds nothing, or nothing that counts beside the other, adds nothing; its distance may be infinite)
+  const float dx = (x.peak - r.peak) * kLog2e, fx = exp2_fast(dx), dy = (y.peak - r.peak) * kLog2e, fy = exp2_fast(dy);
+  const bool has_x = x.s != 0.0f && !(fx == 0.0f && x.s == x.s), has_y = y.s != 0.0f && !(fy == 0.0f && y.s == y.s);
+  r.s = (has_x ? x.s * fx : 0.0f) + (has_y ? y.s * fy : 0.0f);
+  r.a = (has_x ? fx * fmaf(dx, x.s, x.a) : 0.0f) + (has_y ? fy * fmaf(dy, y.s, y.a) : 0.0f);
+  return r;
+}
+template <int LANES>
+__device__ __forceinline__ SoftmaxPart join_lanes(SoftmaxPart p) {
+#pragma unroll
+  for (int off = LANES / 2; off > 0; off >>= 1) {
+    SoftmaxPart o;
+    o.peak = __shfl_xor_sync(0xffffffffu, p.peak, off);
+    o.s = __shfl_xor_sync(0xffffffffu, p.s, off);
+    o.a = __shfl_xor_sync(0xffffffffu, p.a, off);
+    p = join_parts(p, o);
   }
-  const float d = (p.ref - ref) * kLog2e, f = exp2_fast(d);
-  p.a = f > 0.0f ? f * (p.a + d * p.s) : (p.s != p.s ? p.s : 0.0f);
-  p.s *= f;
-  p.ref = ref;
+  return p;
 }
 
-// What a thread carries through its share of a row.  Sums run against `ref`, one of the values seen; it is replaced (and the
-// sums rescaled) only when a value exceeds it by 8 in base 2, which spares the rescaling in almost every word and costs the
-// sums nothing but a factor of at most 256.  `peak` is the largest value itself.
+// The sums of a thread while its warp goes through a row.  The exponent of a logit is one multiply-add, t = z log2 e - ref, the
+// product exact, so the reference costs no rounding; it is a value of the row's scale, the same in the whole warp, and moves
+// (rescaling the sums) only when a logit lies more than 8 above it in base 2: hardly ever after the first words.
+// Logits below `floor`, 140 or more under the reference, are raised to it: their 2^t is 0 either way, but t 2^t is defined.
+// Beyond 2e38 the product overflows, and next to the type's lowest value there is no such floor.  A logit that far down is no
+// reference (beside any ordinary one its 2^t is 0); `far` says that one was seen: if nothing larger turns up - a row masked with
+// its type's lowest value - or a logit was that far up, the row is gone through once more with differences.
+constexpr int kFarDown = 1, kFarUp = 2;
+template <typename T>
 struct LogprobThread {
-  float peak, ref, limit;      // limit: values above it need the reference moved (-infinity until there is a reference)
+  static constexpr float kLowest = Word16<T>::kMinusInf == 0xFC00FC00u ? -64000.0f : -2e38f;      // (float16 ends at 65504)
+  float peak, ref, limit;
+  uint32_t floor;
   Float2 s, a;
+  int far;
 
   __device__ __forceinline__ void init() {
-    peak = -INFINITY;
+    peak = limit = -INFINITY;          // (no reference yet: every finite logit is above the limit)
     ref = 0.0f;
-    limit = -INFINITY;
+    floor = Word16<T>::twice(-140.0f);
     s = a = pack2(0.0f, 0.0f);
+    far = 0;
   }
-  __device__ __forceinline__ SoftmaxPart part() const {
+  // `big`: the thread's largest value of what comes next (NaN if there is one).  The whole warp calls it.
+  __device__ __forceinline__ void move_reference(float big) {
+    if (!(big < INFINITY)) {           // +infinity or NaN: the row has no softmax
+      s = pack2(NAN, NAN);
+      big = -INFINITY;
+    }
+    const float to = order_value(__reduce_max_sync(0xffffffffu, order_bits(big)));
+    if (!(to > limit)) return;
+    if (to < kLowest) {
+      far |= kFarDown;
+      return;
+    }
+    if (to > 2e38f) far |= kFarUp;
+    const float r = rintf(to * kLog2e);
+    if (limit > -INFINITY) {
+      const float d = ref - r, f = exp2_fast(d);
+      s = mul2(s, pack2(f, f));
+      a = fma2(s, pack2(d, d), mul2(a, pack2(f, f)));      // (d is -infinity at most where `far` is set)
+    }
+    ref = r;
+    limit = to + 8.0f / kLog2e;
+    floor = Word16<T>::twice(to - fmaxf(140.0f, fabsf(to) * 0.015625f));
+  }
+  // Two elements: t = z log2 e - ref, none above the limit.
+  __device__ __forceinline__ void add_pair(Float2 z) {
+    const Float2 t = fma2(z, pack2(kLog2e, kLog2e), pack2(-ref, -ref));
+    float t0, t1;
+    unpack2(t, t0, t1);
+    const Float2 e = pack2(exp2_fast(t0), exp2_fast(t1));
+    s = add2(s, e);
+    a = fma2(e, t, a);
+  }
+  __device__ __forceinline__ void add_word(const uint4& w) {
+    uint4 q;
+    q.x = Word16<T>::at_least(w.x, floor);
+    q.y = Word16<T>::at_least(w.y, floor);
+    q.z = Word16<T>::at_least(w.z, floor);
+    q.w = Word16<T>::at_least(w.w, floor);
+    float x[Word16<T>::kCount];
+    Word16<T>::unpack(q, x);
+#pragma unroll
+    for (int j = 0; j < Word16<T>::kCount; j += 2) add_pair(pack2(x[j], x[j + 1]));
+  }
+  // The warp's sums, against its largest logit.
+  __device__ __forceinline__ SoftmaxPart warp_part() const {
     float s0, s1, a0, a1;
     unpack2(s, s0, s1);
     unpack2(a, a0, a1);
-    return {peak, ref, s0 + s1, a0 + a1};
-  }
-  __device__ __forceinline__ void move_reference(float to) {
-    SoftmaxPart p = part();
-    shift_part(p, to);
-    if (!(to < INFINITY)) p.s = NAN;             // +infinity or NaN: the row has no softmax
-    s = pack2(p.s, 0.0f);
-    a = pack2(p.a, 0.0f);
-    ref = to;
-    limit = to + 8.0f / kLog2e;
-  }
-  // N values of which none is above `limit`.  t is held at -200 or more, where 2^t is 0 and t 2^t defined.
-  template <int N>
-  __device__ __forceinline__ void add(const float (&z)[N]) {
-    const Float2 minus_ref = pack2(-ref, -ref), scale = pack2(kLog2e, kLog2e);
+    SoftmaxPart p = {order_value(__reduce_max_sync(0xffffffffu, order_bits(peak))), s0 + s1, a0 + a1};
 #pragma unroll
-    for (int i = 0; i < N; i += 2) {
-      float t0, t1;
-      unpack2(mul2(add2(pack2(z[i], z[i + 1]), minus_ref), scale), t0, t1);
-      t0 = max_nan(t0, -200.0f);
-      t1 = max_nan(t1, -200.0f);
-      const Float2 e = pack2(exp2_fast(t0), exp2_fast(t1));
-      s = add2(s, e);
-      a = fma2(e, pack2(t0, t1), a);
+    for (int off = 16; off > 0; off >>= 1) {
+      p.s += __shfl_xor_sync(0xffffffffu, p.s, off);
+      p.a += __shfl_xor_sync(0xffffffffu, p.a, off);
     }
+    if (p.peak > -INFINITY && p.s != 0.0f) {
+      const float d = fmaf(-p.peak, kLog2e, ref), f = exp2_fast(d);
+      p.a = f * fmaf(d, p.s, p.a);
+      p.s *= f;
+    }
+    return p;
   }
 };
+
+// One element by differences from the largest so far (rows that are `far`, see above).
+__device__ __forceinline__ void add_far(SoftmaxPart& p, float z) {
+  if (z == -INFINITY) return;
+  const SoftmaxPart one = {z, z < INFINITY ? 1.0f : NAN, 0.0f};
+  p = join_parts(p, one);
+}
 
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -151,274 +215,365 @@ __device__ __forceinline__ unsigned long long peer_key(uint32_t addr) {
 // Candidates for the likeliest tokens.  A value enters unless k values at least as large, of lower index, are known: the
 // threshold is the k-th largest of the maxima of 32 groups of eight threads, taken anew whenever the part of the row that
 // has been seen has doubled, with all threads at the same place of the row.  The k largest are picked from the candidates at
-// the end.  Should they overflow (a row that rises throughout), the k largest are found by going through the row k times.
+// the end.  Should they overflow - ties by the thousand, as in a masked row, or a row that rises throughout -, they are
+// collected once more with the final threshold, of the values equal to it only the row's first; failing that too, the k
+// largest are found one by one.
 struct LogprobTop {
-  unsigned long long key[kLpCandidates];
-  unsigned long long best[SOLON_MAX_TOP];      // this CTA's k largest, in falling order (0: fewer)
+  unsigned long long key[2][kLpCandidates];      // by the parity of the row: one warp picks while the others go on
+  unsigned long long best[SOLON_MAX_TOP];        // this CTA's k largest, in falling order (0: fewer)
   unsigned long long scratch[kLpWarps];
-  uint32_t group_max[32];
-  float threshold;
-  uint32_t threshold_order;
-  int count;
+  uint32_t group_max[2][32];                     // by the parity of the refresh
+  uint32_t threshold;                            // order bits; 0: none yet
+  int count[3];                                  // by the row modulo 3, see below
 };
 
-__device__ __forceinline__ void push_candidate(LogprobTop& top, float z, uint32_t index) {
-  const int at = atomicAdd(&top.count, 1);
-  if (at < kLpCandidates) top.key[at] = rank_key(z, index);
+__device__ __forceinline__ void push_candidate(int* count, unsigned long long* keys, float z, uint32_t index) {
+  const int at = atomicAdd(count, 1);
+  if (at < kLpCandidates) keys[at] = rank_key(z, index);
 }
 
-// New threshold from the threads' maxima (order bits, 0: has seen nothing).  All threads call it, at the same place of the row.
-__device__ __forceinline__ void refresh_threshold(LogprobTop& top, uint32_t seen, int k) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+// A thread's largest value so far (order bits, 0: it has seen nothing) to its group's.
+__device__ __forceinline__ void write_group_max(LogprobTop& top, int buffer, uint32_t seen) {
+  const int lane = threadIdx.x & 31;
 #pragma unroll
   for (int off = 1; off < 8; off <<= 1) seen = max(seen, __shfl_xor_sync(0xffffffffu, seen, off));
-  if ((lane & 7) == 0) top.group_max[warp * 4 + (lane >> 3)] = seen;
-  __syncthreads();
-  if (warp == 0) {
-    const uint32_t mine = top.group_max[lane];
-    int rank = 0;
+  if ((lane & 7) == 0) top.group_max[buffer][(threadIdx.x >> 5) * 4 + (lane >> 3)] = seen;
+}
+// The k-th largest of 32 values, one a lane, equal ones counted apart.
+__device__ __forceinline__ uint32_t kth_largest(uint32_t mine, int k) {
+  const int lane = threadIdx.x & 31;
+  int rank = 0;
 #pragma unroll
-    for (int j = 0; j < 32; ++j) {
-      const uint32_t other = __shfl_sync(0xffffffffu, mine, j);
-      rank += other > mine || (other == mine && j < lane);
-    }
-    if (rank == k - 1) {
-      top.threshold_order = mine;
-      top.threshold = key_value((unsigned long long)mine << 32);
+  for (int j = 0; j < 32; ++j) {
+    const uint32_t other = __shfl_sync(0xffffffffu, mine, j);
+    rank += other > mine || (other == mine && j < lane);
+  }
+  return __shfl_sync(0xffffffffu, mine, __ffs(__ballot_sync(0xffffffffu, rank == k - 1)) - 1);
+}
+
+// The k largest of n keys (all different, beside zeros) into best, zeros behind them.  One warp.
+__device__ __forceinline__ void select_largest(const unsigned long long* keys, int n, unsigned long long* best, int k) {
+  const int lane = threadIdx.x & 31;
+  unsigned long long mine = 0;
+  for (int i = lane; i < n; i += 32) mine = max(mine, keys[i]);
+  for (int j = 0; j < k; ++j) {
+    const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(mine >> 32));
+    const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(mine >> 32) == hi ? (uint32_t)mine : 0u);
+    const unsigned long long key = ((unsigned long long)hi << 32) | lo;
+    if (lane == 0) best[j] = key;
+    if (mine == key && key != 0) {               // the lane that held it: its next
+      mine = 0;
+      for (int i = lane; i < n; i += 32) {
+        const unsigned long long q = keys[i];
+        if (q < key && q > mine) mine = q;
+      }
     }
   }
+  __syncwarp();
+}
+
+// The share of a row that a CTA reads: words [begin, end) of 16 bytes from the row's first 16-byte boundary on.  Elements before
+// it (`head`) and behind the last whole word go one by one to the cluster's first and last CTA.
+template <typename T>
+struct RowShare {
+  const T* z;
+  int head, words, begin, end;
+
+  __device__ __forceinline__ RowShare(const LogprobArgs& a, int64_t row, uint32_t rank, uint32_t size) {
+    z = static_cast<const T*>(a.logits) + row * a.pitch;
+    const int cols = (int)a.cols;
+    const int to_boundary = (int)((16 - ((uintptr_t)z & 15)) & 15) / (int)sizeof(T);
+    head = to_boundary < cols ? to_boundary : cols;
+    words = (cols - head) / Word16<T>::kCount;
+    const int shift = __ffs(size) - 1;           // (a power of two)
+    begin = (int)((uint32_t)words * rank >> shift);
+    end = (int)((uint32_t)words * (rank + 1) >> shift);
+  }
+  __device__ __forceinline__ const uint4* body() const { return reinterpret_cast<const uint4*>(z + head); }
+  // all its elements, those outside the words included
+  __device__ __forceinline__ int first(uint32_t rank) const { return rank == 0 ? 0 : head + begin * Word16<T>::kCount; }
+  __device__ __forceinline__ int behind(uint32_t rank, uint32_t size, int cols) const { return rank == size - 1 ? cols : head + end * Word16<T>::kCount; }
+};
+
+// The sums of a CTA's share by differences.  All threads; the result is in warp_part.
+template <typename T>
+__device__ __noinline__ void far_sums(const T* z, int first, int behind, SoftmaxPart* warp_part) {
+  __syncthreads();                               // (everybody has looked at warp_part)
+  SoftmaxPart p = {-INFINITY, 0.0f, 0.0f};
+  for (int c = first + threadIdx.x; c < behind; c += kLpThreads) add_far(p, to_float(z[c]));
+  p = join_lanes<32>(p);
+  if ((threadIdx.x & 31) == 0) warp_part[threadIdx.x >> 5] = p;
   __syncthreads();
 }
 
-// Sorts the largest k of n keys (all different, beside zeros) into out, zeros behind them.
-__device__ __forceinline__ void select_largest(const unsigned long long* keys, int n, unsigned long long* out, int k) {
-  for (int i = threadIdx.x; i < k; i += kLpThreads) out[i] = 0;
+// The candidates of a CTA's share when they have overflowed.  All threads; true: they are in the list, false: top.best is done.
+template <typename T>
+__device__ __noinline__ bool collect_again(const T* z, int first, int behind, LogprobTop& top, int* count, unsigned long long* keys, int k) {
+  const uint32_t threshold = top.threshold;
+  __syncthreads();                               // (everybody has looked at the count)
+  if (threadIdx.x == 0) *count = 0;
   __syncthreads();
-  for (int i = threadIdx.x; i < n; i += kLpThreads) {
-    const unsigned long long mine = keys[i];
-    if (mine == 0) continue;
-    int rank = 0;
-    for (int j = 0; j < n && rank < k; ++j) rank += keys[j] > mine;
-    if (rank < k) out[rank] = mine;
+  for (int c = first + threadIdx.x; c < behind; c += kLpThreads) {
+    const float v = to_float(z[c]);
+    const uint32_t o = order_bits(v);
+    if (o > threshold || (o == threshold && c < first + kLpCandidates / 2)) push_candidate(count, keys, v, (uint32_t)c);
   }
   __syncthreads();
+  const int found = *count;
+  if (found >= k && found <= kLpCandidates) return true;
+  unsigned long long last = ~0ull;
+  for (int j = 0; j < k; ++j) {                  // the largest key below the one before
+    unsigned long long best = 0;
+    for (int c = first + threadIdx.x; c < behind; c += kLpThreads) {
+      const unsigned long long key = rank_key(to_float(z[c]), (uint32_t)c);
+      if (key < last && key > best) best = key;
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, off));
+    if ((threadIdx.x & 31) == 0) top.scratch[threadIdx.x >> 5] = best;
+    __syncthreads();
+    for (int i = 0; i < kLpWarps; ++i) best = max(best, top.scratch[i]);
+    if (threadIdx.x == 0) top.best[j] = best;
+    last = best;
+    __syncthreads();
+  }
+  return false;
 }
 
-// A row is read by a cluster of 1 to 8 CTAs, each taking a stretch of it.  Elements before the row's first and behind its last
-// 16-byte boundary go one by one to the first and the last CTA.
+// A row is read by a cluster of 1 to 8 CTAs, each taking a stretch of it; clusters stay for many rows.  Every thread copies its
+// words of the next iterations into shared memory ahead of time, across the rows' ends (cp.async: a thread waits for its own
+// copies only), and one warp finishes a row - another one each row - while the others are at the next.
 template <typename T, bool TOP>
-__global__ void __launch_bounds__(kLpThreads, 4) logprob_kernel(LogprobArgs a) {
+__global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprob_kernel(LogprobArgs a) {
   constexpr int kVec = Word16<T>::kCount;
-  constexpr int kChunk = kLpThreads * kLpUnroll;          // words of an iteration
-  __shared__ SoftmaxPart warp_part[kLpWarps];
+  constexpr int kStages = lp_stages<TOP>;
+  extern __shared__ __align__(16) uint4 ring[];           // stages x kLpWords x threads
+  __shared__ SoftmaxPart warp_part[2][kLpWarps];          // by the parity of the row
   __shared__ SoftmaxPart cta_part;
-  __shared__ float row_stats[2];                          // peak, log sum
+  __shared__ int far_rows[3];
   __shared__ __align__(16) unsigned char top_bytes[TOP ? sizeof(LogprobTop) : 16];
   LogprobTop& top = *reinterpret_cast<LogprobTop*>(top_bytes);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t rank = cluster_rank(), size = cluster_size();
-  const int64_t row = blockIdx.x / size;
-  const T* z = static_cast<const T*>(a.logits) + row * a.pitch;
   const int cols = (int)a.cols;
-  const int to_boundary = (int)((16 - ((uintptr_t)z & 15)) & 15) / (int)sizeof(T);
-  const int head = to_boundary < cols ? to_boundary : cols;
-  const int words = (cols - head) / kVec;
-  const int begin = (int)((int64_t)words * rank / size), end = (int)((int64_t)words * (rank + 1) / size);
-  const uint4* body = reinterpret_cast<const uint4*>(z + head);
+  const int64_t stride = gridDim.x / size;
 
-  LogprobThread t;
-  t.init();
-  auto add_one = [&](int c) {                             // an element outside the words
-    const float v = to_float(z[c]);
-    t.peak = fmaxf(t.peak, v);
-    if (!(v <= t.limit)) t.move_reference(v);
-    const float pair[2] = {v, -INFINITY};
-    t.add(pair);
-    if (TOP) push_candidate(top, v, (uint32_t)c);
+  int64_t ahead_row = blockIdx.x / size;                  // what is copied next
+  RowShare<T> ahead(a, ahead_row < a.rows ? ahead_row : 0, rank, size);
+  int ahead_base = ahead.begin;
+  auto issue = [&](int stage) {
+    while (ahead_row < a.rows && ahead_base >= ahead.end) {
+      ahead_row += stride;
+      if (ahead_row < a.rows) {
+        ahead = RowShare<T>(a, ahead_row, rank, size);
+        ahead_base = ahead.begin;
+      }
+    }
+    if (ahead_row < a.rows) {
+      const uint4* from = ahead.body() + ahead_base + threadIdx.x;
+      uint4* to = ring + stage * kLpChunk + threadIdx.x;
+      const int left = ahead.end - ahead_base - (int)threadIdx.x;
+#pragma unroll
+      for (int u = 0; u < kLpWords; ++u)
+        if (u * kLpThreads < left) copy16_async(to + u * kLpThreads, from + u * kLpThreads, true);
+      ahead_base += kLpChunk;
+    }
+    copies_commit();
   };
-  if (TOP) {
-    if (threadIdx.x == 0) top.count = 0;
-    __syncthreads();
+  if (threadIdx.x < 3) {
+    far_rows[threadIdx.x] = 0;
+    if (TOP) top.count[threadIdx.x] = 0;
   }
-  if (rank == 0 && (int)threadIdx.x < head) add_one(threadIdx.x);
+#pragma unroll
+  for (int s = 0; s < kStages; ++s) issue(s);
+  __syncthreads();
+  int stage = 0, parity = 0, third = 0, finisher = 0, refresh = 0;
 
-  float threshold = -INFINITY;                            // candidates are above it; +infinity in a sweep without candidates
-  auto add_word = [&](const uint4& w, int index, bool candidates) {
-    const float big = Word16<T>::largest(w);
-    float x[kVec];
-    Word16<T>::unpack(w, x);
-    t.peak = fmaxf(t.peak, big);
-    if (!(big <= t.limit)) t.move_reference(big);
-    t.add(x);
-    if (TOP && candidates && !(big <= threshold)) {
-#pragma unroll
-      for (int j = 0; j < kVec; ++j)
-        if (!(x[j] <= threshold)) push_candidate(top, x[j], (uint32_t)(head + index * kVec + j));
-    }
-  };
-
-  int next_refresh = 1, iteration = 0;
-  for (int base = begin; base < end; base += kChunk, ++iteration) {
-    uint4 w[kLpUnroll];
-    if (base + kChunk <= end) {
-#pragma unroll
-      for (int u = 0; u < kLpUnroll; ++u) w[u] = load16_once(body + base + u * kLpThreads + threadIdx.x);
-#pragma unroll
-      for (int u = 0; u < kLpUnroll; ++u) add_word(w[u], base + u * kLpThreads + threadIdx.x, iteration > 0);
-    } else {
-#pragma unroll
-      for (int u = 0; u < kLpUnroll; ++u) {
-        const int i = base + u * kLpThreads + threadIdx.x;
-        if (i < end) w[u] = load16_once(body + i);
-      }
-#pragma unroll
-      for (int u = 0; u < kLpUnroll; ++u) {
-        const int i = base + u * kLpThreads + threadIdx.x;
-        if (i < end) add_word(w[u], i, iteration > 0);
+  for (int64_t row = blockIdx.x / size; row < a.rows; row += stride) {
+    const RowShare<T> share(a, row, rank, size);
+    const T* z = share.z;
+    int* const count = &top.count[TOP ? third : 0];
+    unsigned long long* const keys = top.key[TOP ? parity : 0];
+    // what the finishing warp will need from memory
+    T edge = from_float<T>(-INFINITY);                    // the elements outside the words: head in lanes 0 .., tail in lanes 16 ..
+    int edge_index = -1;
+    int64_t target = -1;
+    float target_logit = 0.0f;
+    if (warp == finisher) {
+      const int tail = share.head + share.words * kVec;
+      if (rank == 0 && lane < share.head) edge_index = lane;
+      if (rank == size - 1 && lane >= 16 && lane - 16 < cols - tail) edge_index = tail + lane - 16;
+      if (edge_index >= 0) edge = z[edge_index];
+      if (a.targets && a.logp && rank == 0) {
+        target = a.targets[row];
+        if (target >= 0 && target < a.cols) target_logit = to_float(z[target]);
       }
     }
-    if constexpr (TOP) {
-      if (iteration == 0) {
-        // the first stretch is compared with its own threshold, so values equal to it count too; where they are many (a
-        // masked row), only those of the first 1024 elements, if that leaves k
-        refresh_threshold(top, begin + (int)threadIdx.x < end ? order_bits(t.peak) : 0u, a.top_k);
-        const uint32_t at_least = top.threshold_order;
-        const int before = top.count;
-        __syncthreads();
-        for (int pass = 0; pass < 2; ++pass) {
-          const int ties_until = pass == 0 ? 0x7FFFFFFF : begin * kVec + 1024;
+
+    LogprobThread<T> t;
+    t.init();
+    float threshold = -INFINITY;                          // candidates are above it
+    int next_refresh = 2, iteration = 0;
+    for (int base = share.begin; base < share.end; base += kLpChunk, ++iteration) {
+      const uint4* words = ring + stage * kLpChunk + threadIdx.x;
+      copies_wait<kStages - 1>();
+      uint4 w[kLpWords];
 #pragma unroll
-          for (int u = 0; u < kLpUnroll; ++u) {
-            const int i = base + u * kLpThreads + threadIdx.x;
-            if (i < end) {
-              float x[kVec];
-              Word16<T>::unpack(w[u], x);
+      for (int u = 0; u < kLpWords; ++u) w[u] = words[u * kLpThreads];
+      if (base + kLpChunk > share.end) {
+        constexpr uint32_t kNone = Word16<T>::kMinusInf;
 #pragma unroll
-              for (int j = 0; j < kVec; ++j) {
-                const uint32_t o = order_bits(x[j]);
-                if (o > at_least || (o == at_least && i * kVec + j < ties_until)) push_candidate(top, x[j], (uint32_t)(head + i * kVec + j));
+        for (int u = 0; u < kLpWords; ++u)
+          if (base + u * kLpThreads + (int)threadIdx.x >= share.end) w[u] = make_uint4(kNone, kNone, kNone, kNone);
+      }
+      float big[kLpWords];
+      float biggest;
+      if constexpr (TOP || sizeof(T) == 4) {
+#pragma unroll
+        for (int u = 0; u < kLpWords; ++u) big[u] = Word16<T>::largest(w[u]);
+        biggest = max_nan(max_nan(big[0], big[1]), max_nan(big[2], big[3]));
+      } else {
+        uint32_t m[kLpWords];
+#pragma unroll
+        for (int u = 0; u < kLpWords; ++u) m[u] = Word16<T>::at_least(Word16<T>::at_least(w[u].x, w[u].y), Word16<T>::at_least(w[u].z, w[u].w));
+        biggest = Word16<T>::widest(Word16<T>::at_least(Word16<T>::at_least(m[0], m[1]), Word16<T>::at_least(m[2], m[3])));
+      }
+      t.peak = fmaxf(t.peak, biggest);
+      if (__any_sync(0xffffffffu, !(biggest <= t.limit))) t.move_reference(biggest);
+#pragma unroll
+      for (int u = 0; u < kLpWords; ++u) t.add_word(w[u]);
+
+      if constexpr (TOP) {
+        if (iteration > 0) {
+          threshold = order_value(*(volatile uint32_t*)&top.threshold);
+          if (!(biggest <= threshold)) {
+#pragma unroll
+            for (int u = 0; u < kLpWords; ++u) {
+              if (!(big[u] <= threshold)) {
+                float x[kVec];
+                Word16<T>::unpack(w[u], x);
+#pragma unroll
+                for (int j = 0; j < kVec; ++j)
+                  if (!(x[j] <= threshold)) push_candidate(count, keys, x[j], (uint32_t)(share.head + (base + u * kLpThreads + (int)threadIdx.x) * kVec + j));
               }
             }
           }
+        }
+        if (iteration == 0 || (iteration + 1 == next_refresh && base + kLpChunk < share.end)) {
+          // one warp works the threshold out; the others need not wait for it but in the first stretch, which is compared
+          // with its own (so values equal to it count there)
+          write_group_max(top, refresh, share.begin + (int)threadIdx.x < share.end ? order_bits(t.peak) : 0u);
           __syncthreads();
-          const int found = top.count;
-          __syncthreads();
-          if (found <= kLpCandidates || pass == 1) {
-            // (too few after the second pass cannot pass for a result: the count says overflow)
-            if (pass == 1 && found - before < a.top_k && threadIdx.x == 0) top.count = kLpCandidates + 1;
-            break;
+          if (warp == kLpWarps - 1) {
+            const uint32_t found = kth_largest(top.group_max[refresh][lane], a.top_k);
+            if (lane == 0) *(volatile uint32_t*)&top.threshold = found;
           }
-          if (threadIdx.x == 0) top.count = before;
-          __syncthreads();
+          refresh ^= 1;
+          if (iteration > 0) next_refresh *= 2;
+          if (iteration == 0) {
+            __syncthreads();
+            const uint32_t at_least = top.threshold;
+            const float low = at_least ? order_value(at_least) : -INFINITY;
+#pragma unroll
+            for (int u = 0; u < kLpWords; ++u) {
+              const int i = base + u * kLpThreads + (int)threadIdx.x;
+              if (i < share.end && !(big[u] < low)) {
+                float x[kVec];
+                Word16<T>::unpack(w[u], x);
+#pragma unroll
+                for (int j = 0; j < kVec; ++j)
+                  if (!(x[j] < low)) push_candidate(count, keys, x[j], (uint32_t)(share.head + i * kVec + j));
+              }
+            }
+          }
         }
-        __syncthreads();
-        threshold = top.threshold;
-        next_refresh = 2;
-      } else if (iteration + 1 == next_refresh && base + kChunk < end) {
-        refresh_threshold(top, order_bits(t.peak), a.top_k);
-        threshold = top.threshold;
-        next_refresh *= 2;
       }
+      issue(stage);                                       // into the words just read
+      stage = stage + 1 == kStages ? 0 : stage + 1;
     }
-  }
 
-  // behind everything else: the threshold takes what it has seen to be of lower index than what it is compared with
-  if (rank == size - 1 && (int)threadIdx.x < cols - head - words * kVec) add_one(head + words * kVec + threadIdx.x);
-
-  // the CTA's sums: everything against the warp's, then the CTA's largest value
-  SoftmaxPart p = t.part();
-  float peak = p.peak;
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) peak = fmaxf(peak, __shfl_xor_sync(0xffffffffu, peak, off));
-  p.peak = peak;
-  if (peak > -INFINITY) shift_part(p, peak);
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) {
-    p.s += __shfl_xor_sync(0xffffffffu, p.s, off);
-    p.a += __shfl_xor_sync(0xffffffffu, p.a, off);
-  }
-  if (lane == 0) warp_part[warp] = p;
-  __syncthreads();
-  auto join = [](SoftmaxPart& sum, SoftmaxPart q, float to) {
-    if (to > -INFINITY) shift_part(q, to);
-    sum.s += q.s;
-    sum.a += q.a;
-  };
-  SoftmaxPart cta = {-INFINITY, 0.0f, 0.0f, 0.0f};
-  if (threadIdx.x == 0) {
-    for (int i = 0; i < kLpWarps; ++i) cta.peak = fmaxf(cta.peak, warp_part[i].peak);
-    cta.ref = cta.peak;
-    for (int i = 0; i < kLpWarps; ++i) join(cta, warp_part[i], cta.peak);
-    cta_part = cta;
-  }
-
-  if constexpr (TOP) {
+    // the elements outside the words come last: the threshold takes what it has seen to be of lower index than what it is
+    // compared with, so these have no part in it
+    if (warp == finisher && __any_sync(0xffffffffu, edge_index >= 0)) {
+      const float v = to_float(edge);
+      t.peak = fmaxf(t.peak, v);
+      if (__any_sync(0xffffffffu, !(v <= t.limit))) t.move_reference(v);
+      constexpr uint32_t kNone = Word16<T>::kMinusInf;
+      t.add_word(make_uint4(Word16<T>::first(edge), kNone, kNone, kNone));
+      if (TOP && edge_index >= 0) push_candidate(count, keys, v, (uint32_t)edge_index);
+    }
+    const SoftmaxPart mine = t.warp_part();
+    if (lane == 0) warp_part[parity][warp] = mine;
+    if (t.far) atomicOr(&far_rows[third], t.far);
     __syncthreads();
-    const int count = top.count;
-    if (count <= kLpCandidates) {
-      select_largest(top.key, count, top.best, a.top_k);
-    } else {
-      unsigned long long last = ~0ull;
-      for (int k = 0; k < a.top_k; ++k) {                 // the largest key below the one before
-        unsigned long long best = 0;
-        const int first = rank == 0 ? 0 : head + begin * kVec, behind = rank == size - 1 ? cols : head + end * kVec;
-        for (int c = first + threadIdx.x; c < behind; c += kLpThreads) {
-          const unsigned long long key = rank_key(to_float(z[c]), (uint32_t)c);
-          if (key < last && key > best) best = key;
-        }
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, off));
-        if (lane == 0) top.scratch[warp] = best;
-        __syncthreads();
-        for (int i = 0; i < kLpWarps; ++i) best = max(best, top.scratch[i]);
-        if (threadIdx.x == 0) top.best[k] = best;
-        last = best;
-        __syncthreads();
-      }
-    }
-  }
 
-  if (size > 1) cluster_barrier();
-  if (rank == 0) {
+    // Everybody has read the row before's marks and counts on the way here; their place is used again by the row after the
+    // next, which begins behind the next one's barrier.
     if (threadIdx.x == 0) {
-      for (uint32_t r = 1; r < size; ++r) {
-        const uint32_t at = peer_address(&cta_part, r);
-        const SoftmaxPart q = {peer_float(at), peer_float(at + 4), peer_float(at + 8), peer_float(at + 12)};
-        const float big = fmaxf(cta.peak, q.peak);
-        if (big > -INFINITY) shift_part(cta, big);
-        cta.peak = big;
-        join(cta, q, big);
-      }
-      const bool empty = cta.peak == -INFINITY && cta.s == 0.0f;
-      const float log_s = empty ? 0.0f : logf(cta.s);
-      row_stats[0] = cta.peak;
-      row_stats[1] = log_s;
-      if (a.peak) a.peak[row] = cta.peak;
-      if (a.log_sum) a.log_sum[row] = log_s;
-      if (a.entropy) a.entropy[row] = empty ? 0.0f : log_s - kLn2 * (cta.a / cta.s);
-      if (a.targets && a.logp) {
-        const int64_t target = a.targets[row];
-        float lp = 0.0f;
-        if (target >= a.cols) lp = NAN;
-        else if (target >= 0) lp = empty ? -INFINITY : (to_float(z[target]) - cta.peak) - log_s;
-        a.logp[row] = lp;
-      }
+      const int before = third == 0 ? 2 : third - 1;
+      far_rows[before] = 0;
+      if (TOP) top.count[before] = 0;
     }
-    if constexpr (TOP) {
-      __syncthreads();
+    int far = far_rows[third];
+    if (far == kFarDown) {
+      float largest = -INFINITY;
+      for (int i = 0; i < kLpWarps; ++i) largest = fmaxf(largest, warp_part[parity][i].peak);
+      if (largest >= LogprobThread<T>::kLowest) far = 0;
+    }
+    if (far) far_sums<T>(z, share.first(rank), share.behind(rank, size, cols), warp_part[parity]);
+    bool listed = true;                                   // the candidates are in the list
+    if (TOP && *count > kLpCandidates) listed = collect_again<T>(z, share.first(rank), share.behind(rank, size, cols), top, count, keys, a.top_k);
+
+    SoftmaxPart part = {-INFINITY, 0.0f, 0.0f};
+    if (warp == finisher) {
+      if (lane < kLpWarps) part = warp_part[parity][lane];
+      part = join_lanes<kLpWarps>(part);
+      if (TOP && listed) select_largest(keys, *count, top.best, a.top_k);
+      if (size > 1 && lane == 0) cta_part = part;
+    }
+    if (size > 1) cluster_barrier();
+    if (warp == finisher && rank == 0) {
       if (size > 1) {
-        for (int i = threadIdx.x; i < (int)size * a.top_k; i += kLpThreads) top.key[i] = peer_key(peer_address(&top.best[i % a.top_k], i / a.top_k));
-        __syncthreads();
-        select_largest(top.key, (int)size * a.top_k, top.best, a.top_k);
+        part = {-INFINITY, 0.0f, 0.0f};
+        if (lane < (int)size) {
+          const uint32_t at = peer_address(&cta_part, lane);
+          part = {peer_float(at), peer_float(at + 4), peer_float(at + 8)};
+        }
+        part = join_lanes<kLpMaxCluster>(part);
+        if (TOP) {
+          __syncwarp();
+          for (int i = lane; i < (int)size * a.top_k; i += 32) keys[i] = peer_key(peer_address(&top.best[i % a.top_k], i / a.top_k));
+          __syncwarp();
+          select_largest(keys, (int)size * a.top_k, top.best, a.top_k);
+        }
       }
-      for (int i = threadIdx.x; i < a.top_k; i += kLpThreads) {
-        const unsigned long long key = top.best[i];
-        a.top_ids[row * a.top_k + i] = key_index(key);
-        a.top_logp[row * a.top_k + i] = row_stats[0] == -INFINITY && row_stats[1] == 0.0f ? -INFINITY : (key_value(key) - row_stats[0]) - row_stats[1];
+      part.peak = __shfl_sync(0xffffffffu, part.peak, 0);
+      part.s = __shfl_sync(0xffffffffu, part.s, 0);
+      part.a = __shfl_sync(0xffffffffu, part.a, 0);
+      const bool empty = part.peak == -INFINITY && part.s == 0.0f;
+      const float log_s = empty ? 0.0f : logf(part.s);
+      if (lane == 0) {
+        if (a.peak) a.peak[row] = part.peak;
+        if (a.log_sum) a.log_sum[row] = log_s;
+        if (a.entropy) a.entropy[row] = empty ? 0.0f : log_s - kLn2 * (part.a / part.s);
+        if (a.targets && a.logp) {
+          float lp = 0.0f;
+          if (target >= a.cols) lp = NAN;
+          else if (target >= 0) lp = empty ? -INFINITY : (target_logit - part.peak) - log_s;
+          a.logp[row] = lp;
+        }
+      }
+      if (TOP && lane < a.top_k) {
+        const unsigned long long key = top.best[lane];
+        a.top_ids[row * a.top_k + lane] = key_index(key);
+        a.top_logp[row * a.top_k + lane] = empty ? -INFINITY : (key_value(key) - part.peak) - log_s;
       }
     }
+    if (size > 1) cluster_barrier();                      // the first CTA has read the others' shared memory
+    parity ^= 1;
+    third = third == 2 ? 0 : third + 1;
+    finisher = finisher + 1 == kLpWarps ? 0 : finisher + 1;
   }
-  if (size > 1) cluster_barrier();        // the first CTA has read the others' shared memory
 }
 
 struct LogprobGradArgs {
@@ -462,7 +617,7 @@ __device__ __forceinline__ float logit_grad(const RowGrad& r, float z) {
   return -exp2_fast(lp * kLog2e) * fmaf(r.gh, lp + r.h, r.g);
 }
 
-// A CTA per stretch of kLpThreads * kLpUnroll words of a row.
+// A CTA per stretch of kLpThreads * kLpWords words of a row.
 template <typename T>
 __global__ void __launch_bounds__(kLpThreads) logprob_grad_kernel(LogprobGradArgs a) {
   constexpr int kVec = Word16<T>::kCount;
@@ -473,9 +628,9 @@ __global__ void __launch_bounds__(kLpThreads) logprob_grad_kernel(LogprobGradArg
     const RowGrad r = row_grad(a, row);
     auto one = [&](int c) { dz[c] = r.zero ? from_float<T>(0.0f) : from_float<T>(logit_grad(r, to_float(z[c])) + (c == r.target ? r.g : 0.0f)); };
     if (((uintptr_t)z ^ (uintptr_t)dz) & 15) {            // the two rows lie differently between 16-byte boundaries
-      const int begin = blockIdx.x * (kLpThreads * kLpUnroll * kVec);
+      const int begin = blockIdx.x * (kLpThreads * kLpWords * kVec);
 #pragma unroll 4
-      for (int i = 0; i < kLpUnroll * kVec; ++i) {
+      for (int i = 0; i < kLpWords * kVec; ++i) {
         const int c = begin + i * kLpThreads + threadIdx.x;
         if (c < cols) one(c);
       }
@@ -490,15 +645,15 @@ __global__ void __launch_bounds__(kLpThreads) logprob_grad_kernel(LogprobGradArg
     }
     const uint4* from = reinterpret_cast<const uint4*>(z + head);
     uint4* to = reinterpret_cast<uint4*>(dz + head);
-    const int first = blockIdx.x * (kLpThreads * kLpUnroll) + threadIdx.x;
-    uint4 w[kLpUnroll];
+    const int first = blockIdx.x * (kLpThreads * kLpWords) + threadIdx.x;
+    uint4 w[kLpWords];
     if (!r.zero) {
 #pragma unroll
-      for (int u = 0; u < kLpUnroll; ++u)
+      for (int u = 0; u < kLpWords; ++u)
         if (first + u * kLpThreads < words) w[u] = load16_once(from + first + u * kLpThreads);
     }
 #pragma unroll
-    for (int u = 0; u < kLpUnroll; ++u) {
+    for (int u = 0; u < kLpWords; ++u) {
       const int i = first + u * kLpThreads;
       if (i >= words) break;
       if (r.zero) {
@@ -523,15 +678,19 @@ __global__ void __launch_bounds__(kLpThreads) logprob_grad_kernel(LogprobGradArg
 // CTAs per row: as many as bring the grid to four per SM, as long as each has an iteration's words to read.
 static int logprob_cluster(int64_t rows, int64_t cols, size_t size, int sms) {
   int cluster = 1;
-  while (cluster < kLpMaxCluster && rows * cluster * 2 <= (int64_t)sms * 4 && cols * (int64_t)size >= (int64_t)cluster * 2 * kLpThreads * kLpUnroll * 16) cluster *= 2;
+  while (cluster < kLpMaxCluster && rows * cluster * 2 <= (int64_t)sms * 4 && cols * (int64_t)size >= (int64_t)cluster * 2 * kLpChunk * 16) cluster *= 2;
   return cluster;
 }
 
 template <typename T, bool TOP>
-static int logprob_launch_top(const LogprobArgs& a, int cluster, cudaStream_t stream) {
+static int logprob_launch_top(const LogprobArgs& a, int cluster, int sms, cudaStream_t stream) {
+  constexpr size_t kSmem = (size_t)lp_stages<TOP> * kLpChunk * 16;
+  SOLON_CUDA_TRY(cudaFuncSetAttribute(logprob_kernel<T, TOP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem));
+  const int64_t resident = (int64_t)sms * kLpCtasPerSm / cluster;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(a.rows * cluster));
+  cfg.gridDim = dim3((unsigned)((a.rows < resident ? a.rows : resident) * cluster));
   cfg.blockDim = dim3(kLpThreads);
+  cfg.dynamicSmemBytes = kSmem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -546,12 +705,12 @@ static int logprob_launch_top(const LogprobArgs& a, int cluster, cudaStream_t st
 template <typename T>
 static int logprob_launch(const LogprobArgs& a, int sms, cudaStream_t stream) {
   const int cluster = logprob_cluster(a.rows, a.cols, sizeof(T), sms);
-  return a.top_k > 0 ? logprob_launch_top<T, true>(a, cluster, stream) : logprob_launch_top<T, false>(a, cluster, stream);
+  return a.top_k > 0 ? logprob_launch_top<T, true>(a, cluster, sms, stream) : logprob_launch_top<T, false>(a, cluster, sms, stream);
 }
 
 template <typename T>
 static int logprob_grad_launch(const LogprobGradArgs& a, cudaStream_t stream) {
-  const int64_t stretch = (int64_t)kLpThreads * kLpUnroll * Word16<T>::kCount;
+  const int64_t stretch = (int64_t)kLpThreads * kLpWords * Word16<T>::kCount;
   const int64_t x = (a.cols + stretch - 1) / stretch;
   logprob_grad_kernel<T><<<dim3((unsigned)x, (unsigned)(a.rows < 65535 ? a.rows : 65535)), kLpThreads, 0, stream>>>(a);
   SOLON_CUDA_TRY(cudaGetLastError());

@@ -108,7 +108,7 @@ def test_forward_strides_and_alignment(rows, cols, pitch, offset, dtype):
 
 @pytest.mark.parametrize("rows", [1, 12, 600])
 @pytest.mark.parametrize("cols", [50, 3000, 70001])
-@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 def test_masks(rows, cols, dtype):
     """Rows with few tokens left, with one, with none, and masks of the type's lowest value instead of -infinity."""
     z, targets = _logits(rows, cols, dtype, 6, masked=0.9)
