@@ -508,7 +508,7 @@ static int ln_forward_launch(const LnForwardArgs& a, int sms, cudaStream_t strea
   constexpr int kBlock = TPR < kLnThreads ? kLnThreads : TPR;
   constexpr int kTeams = kBlock / TPR;
   constexpr size_t kSmem = VEC > 1 ? (size_t)ln_stages<T, TPR, ELEMS, 1> * (ELEMS / VEC) * 16 * kBlock : 0;
-  if constexpr (kSmem > 40 * 1024) SOLON_CUDA_TRY(cudaFuncSetAttribute(ln_forward_kernel<T, VEC, TPR, ELEMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem));
+  if constexpr (kSmem > 40 * 1024) SOLON_SHARED_MEMORY_ONCE((ln_forward_kernel<T, VEC, TPR, ELEMS>), kSmem);
   const int64_t want = (a.rows + kTeams - 1) / kTeams, cap = (int64_t)sms * (TPR < 512 ? 2 : 1);
   ln_forward_kernel<T, VEC, TPR, ELEMS><<<(unsigned)ln_min(want, cap), kBlock, kSmem, stream>>>(a);
   SOLON_CUDA_TRY(cudaGetLastError());
@@ -521,7 +521,7 @@ static int ln_backward_launch(const LnBackwardArgs& a, int partitions, cudaStrea
   constexpr size_t kRing = VEC > 1 ? (size_t)ln_stages<T, TPR, ELEMS, 2> * 2 * (ELEMS / VEC) * 16 * kBlock : 0;
   constexpr size_t kCombine = TPR < kBlock ? (size_t)kBlock * ELEMS * sizeof(float) : 0;
   constexpr size_t kSmem = kRing > kCombine ? kRing : kCombine;
-  if constexpr (kSmem > 40 * 1024) SOLON_CUDA_TRY(cudaFuncSetAttribute(ln_backward_kernel<T, VEC, TPR, ELEMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem));
+  if constexpr (kSmem > 40 * 1024) SOLON_SHARED_MEMORY_ONCE((ln_backward_kernel<T, VEC, TPR, ELEMS>), kSmem);
   ln_backward_kernel<T, VEC, TPR, ELEMS><<<dim3((unsigned)a.splits, (unsigned)partitions), kBlock, kSmem, stream>>>(a);
   SOLON_CUDA_TRY(cudaGetLastError());
   return SOLON_OK;

@@ -176,6 +176,19 @@ struct LogprobThread {
   }
 };
 
+// Largest element of a thread's words (NaN if there is one).
+template <typename T>
+__device__ __forceinline__ float largest_of(const uint4 (&w)[kLpWords]) {
+  uint32_t m[kLpWords];
+#pragma unroll
+  for (int u = 0; u < kLpWords; ++u) m[u] = Word16<T>::at_least(Word16<T>::at_least(w[u].x, w[u].y), Word16<T>::at_least(w[u].z, w[u].w));
+#pragma unroll
+  for (int n = kLpWords / 2; n > 0; n /= 2)
+#pragma unroll
+    for (int u = 0; u < n; ++u) m[u] = Word16<T>::at_least(m[u], m[u + n]);
+  return Word16<T>::widest(m[0]);
+}
+
 // One element by differences from the largest so far (rows that are `far`, see above).
 __device__ __forceinline__ void add_far(SoftmaxPart& p, float z) {
   if (z == -INFINITY) return;
@@ -230,6 +243,25 @@ struct LogprobTop {
 __device__ __forceinline__ void push_candidate(int* count, unsigned long long* keys, float z, uint32_t index) {
   const int at = atomicAdd(count, 1);
   if (at < kLpCandidates) keys[at] = rank_key(z, index);
+}
+
+// Which of a thread's elements are above the threshold (`ties`: not below it), as bits; words whose largest value is not are
+// passed over.  Elements are fetched from the ring again by their bits: few are, and the code for them stays short.
+template <typename T>
+__device__ __forceinline__ uint32_t candidate_bits(const uint4 (&w)[kLpWords], float threshold, bool ties) {
+  uint32_t bits = 0;
+#pragma unroll
+  for (int u = 0; u < kLpWords; ++u) {
+    const float big = Word16<T>::largest(w[u]);
+    if (ties ? !(big < threshold) : !(big <= threshold)) {
+      float x[Word16<T>::kCount];
+      Word16<T>::unpack(w[u], x);
+#pragma unroll
+      for (int j = 0; j < Word16<T>::kCount; ++j)
+        if (ties ? !(x[j] < threshold) : !(x[j] <= threshold)) bits |= 1u << (u * Word16<T>::kCount + j);
+    }
+  }
+  return bits;
 }
 
 // A thread's largest value so far (order bits, 0: it has seen nothing) to its group's.
@@ -410,6 +442,15 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprob_kernel(Logpr
       }
     }
 
+    auto push_bits = [&](uint32_t bits, const uint4* words, int base) {
+      while (bits) {
+        const int e = __ffs(bits) - 1, u = e / kVec, j = e % kVec;
+        bits &= bits - 1;
+        const float v = to_float(reinterpret_cast<const T*>(words + u * kLpThreads)[j]);
+        push_candidate(count, keys, v, (uint32_t)(share.head + (base + u * kLpThreads + (int)threadIdx.x) * kVec + j));
+      }
+    };
+
     LogprobThread<T> t;
     t.init();
     float threshold = -INFINITY;                          // candidates are above it
@@ -426,18 +467,7 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprob_kernel(Logpr
         for (int u = 0; u < kLpWords; ++u)
           if (base + u * kLpThreads + (int)threadIdx.x >= share.end) w[u] = make_uint4(kNone, kNone, kNone, kNone);
       }
-      float big[kLpWords];
-      float biggest;
-      if constexpr (TOP || sizeof(T) == 4) {
-#pragma unroll
-        for (int u = 0; u < kLpWords; ++u) big[u] = Word16<T>::largest(w[u]);
-        biggest = max_nan(max_nan(big[0], big[1]), max_nan(big[2], big[3]));
-      } else {
-        uint32_t m[kLpWords];
-#pragma unroll
-        for (int u = 0; u < kLpWords; ++u) m[u] = Word16<T>::at_least(Word16<T>::at_least(w[u].x, w[u].y), Word16<T>::at_least(w[u].z, w[u].w));
-        biggest = Word16<T>::widest(Word16<T>::at_least(Word16<T>::at_least(m[0], m[1]), Word16<T>::at_least(m[2], m[3])));
-      }
+      const float biggest = largest_of<T>(w);
       t.peak = fmaxf(t.peak, biggest);
       if (__any_sync(0xffffffffu, !(biggest <= t.limit))) t.move_reference(biggest);
 #pragma unroll
@@ -446,18 +476,7 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprob_kernel(Logpr
       if constexpr (TOP) {
         if (iteration > 0) {
           threshold = order_value(*(volatile uint32_t*)&top.threshold);
-          if (!(biggest <= threshold)) {
-#pragma unroll
-            for (int u = 0; u < kLpWords; ++u) {
-              if (!(big[u] <= threshold)) {
-                float x[kVec];
-                Word16<T>::unpack(w[u], x);
-#pragma unroll
-                for (int j = 0; j < kVec; ++j)
-                  if (!(x[j] <= threshold)) push_candidate(count, keys, x[j], (uint32_t)(share.head + (base + u * kLpThreads + (int)threadIdx.x) * kVec + j));
-              }
-            }
-          }
+          if (!(biggest <= threshold)) push_bits(candidate_bits<T>(w, threshold, false), words, base);
         }
         if (iteration == 0 || (iteration + 1 == next_refresh && base + kLpChunk < share.end)) {
           // one warp works the threshold out; the others need not wait for it but in the first stretch, which is compared
@@ -473,18 +492,11 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprob_kernel(Logpr
           if (iteration == 0) {
             __syncthreads();
             const uint32_t at_least = top.threshold;
-            const float low = at_least ? order_value(at_least) : -INFINITY;
+            uint32_t bits = candidate_bits<T>(w, at_least ? order_value(at_least) : -INFINITY, true);
 #pragma unroll
-            for (int u = 0; u < kLpWords; ++u) {
-              const int i = base + u * kLpThreads + (int)threadIdx.x;
-              if (i < share.end && !(big[u] < low)) {
-                float x[kVec];
-                Word16<T>::unpack(w[u], x);
-#pragma unroll
-                for (int j = 0; j < kVec; ++j)
-                  if (!(x[j] < low)) push_candidate(count, keys, x[j], (uint32_t)(share.head + i * kVec + j));
-              }
-            }
+            for (int u = 0; u < kLpWords; ++u)            // (not the -infinities behind the row's end)
+              if (base + u * kLpThreads + (int)threadIdx.x >= share.end) bits &= ~(((1u << kVec) - 1u) << (u * kVec));
+            push_bits(bits, words, base);
           }
         }
       }
@@ -573,6 +585,182 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprob_kernel(Logpr
     parity ^= 1;
     third = third == 2 ? 0 : third + 1;
     finisher = finisher + 1 == kLpWarps ? 0 : finisher + 1;
+  }
+}
+
+// ---- many rows: a warp a row -----------------------------------------------------------------------------------------
+// Nothing in a row then waits for another warp, and the serial work at a row's end (and for its likeliest tokens) of one warp
+// hides behind the others' streams.  Measured, CTA a row against warp a row: 8192 x 32768 bfloat16 107 / 100 us, with 8
+// alternatives 285 / 166; 2500 x 2000 with 8 36 / 18; the two meet at 12 rows per SM (1776 x 50000: 42 / 39, with 8 68 / 68),
+// below that the warps are too few.
+// The candidates are a warp's own: filtered as above with the lanes' maxima for groups, appended by ballots, and pruned to the k
+// largest when the list is full.
+constexpr int kLpWarpCtas = 3;                 // CTAs per SM: 24 warps with 8 KB of shared memory each
+constexpr int kLpWarpList = 256;
+constexpr int kLpWarpRows = 12;                // rows per SM from which on rows go to warps
+template <bool TOP>
+constexpr int lp_warp_stages = TOP ? 3 : 4;
+
+// A lower bound of the k-th largest of the lanes' values (order bits): exact in the upper 16 bits.
+__device__ __forceinline__ uint32_t kth_largest_bound(uint32_t mine, int k) {
+  uint32_t bound = 0;
+#pragma unroll
+  for (int bit = 31; bit >= 16; --bit) {
+    const uint32_t trial = bound | (1u << bit);
+    if (__popc(__ballot_sync(0xffffffffu, mine >= trial)) >= k) bound = trial;
+  }
+  return bound;
+}
+
+template <typename T, bool TOP>
+__global__ void __launch_bounds__(kLpThreads, kLpWarpCtas) logprob_warp_kernel(LogprobArgs a) {
+  constexpr int kVec = Word16<T>::kCount;
+  constexpr int kStages = lp_warp_stages<TOP>;
+  constexpr int kChunk = 32 * kLpWords;                   // words of an iteration
+  constexpr uint32_t kNone = Word16<T>::kMinusInf;
+  extern __shared__ __align__(16) uint4 shared[];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint4* ring = shared + warp * kStages * kChunk + lane;
+  unsigned long long* list = reinterpret_cast<unsigned long long*>(shared + kLpWarps * kStages * kChunk) + warp * (kLpWarpList + SOLON_MAX_TOP);
+  unsigned long long* best = list + kLpWarpList;
+  const int cols = (int)a.cols, k = a.top_k;
+  const int64_t stride = (int64_t)gridDim.x * kLpWarps;
+
+  int64_t row = (int64_t)warp * gridDim.x + blockIdx.x;   // (neighbouring rows to different SMs)
+  int64_t ahead_row = row;                                // what is copied next
+  RowShare<T> ahead(a, ahead_row < a.rows ? ahead_row : 0, 0, 1);
+  int ahead_base = 0;
+  auto issue = [&](int stage) {
+    while (ahead_row < a.rows && ahead_base >= ahead.words) {
+      ahead_row += stride;
+      if (ahead_row < a.rows) ahead = RowShare<T>(a, ahead_row, 0, 1);
+      ahead_base = 0;
+    }
+    if (ahead_row < a.rows) {
+      const uint4* from = ahead.body() + ahead_base + lane;
+      const int left = ahead.words - ahead_base - lane;
+#pragma unroll
+      for (int u = 0; u < kLpWords; ++u)
+        if (u * 32 < left) copy16_async(ring + stage * kChunk + u * 32, from + u * 32, true);
+      ahead_base += kChunk;
+    }
+    copies_commit();
+  };
+#pragma unroll
+  for (int s = 0; s < kStages; ++s) issue(s);
+  const bool with_target = a.targets && a.logp;
+  int64_t next_target = with_target && row < a.rows ? a.targets[row] : -1;
+  int stage = 0;
+
+  for (; row < a.rows; row += stride) {
+    const RowShare<T> share(a, row, 0, 1);
+    const T* z = share.z;
+    const int tail = share.head + share.words * kVec;
+    // from memory, for the row's end: the elements outside the words (head in lanes 0 .., tail in lanes 16 ..) and the target
+    const int edge_index = lane < share.head ? lane : lane >= 16 && lane - 16 < cols - tail ? tail + lane - 16 : -1;
+    T edge = from_float<T>(-INFINITY), target_logit = from_float<T>(0.0f);
+    if (edge_index >= 0) edge = z[edge_index];
+    const int64_t target = next_target;
+    if (target >= 0 && target < a.cols) target_logit = z[target];
+    if (with_target && row + stride < a.rows) next_target = a.targets[row + stride];
+
+    LogprobThread<T> t;
+    t.init();
+    int listed = 0, next_refresh = 1, iteration = 0;
+    float threshold = -INFINITY;                          // candidates are above it, or (see above) not below it
+    auto append = [&](bool wanted, float v, int index) {
+      const uint32_t mask = __ballot_sync(0xffffffffu, wanted);
+      if (listed + __popc(mask) > kLpWarpList) {
+        select_largest(list, listed, best, k);
+        if (lane < k) list[lane] = best[lane];
+        listed = k;                                       // (of a full list: k of them)
+        threshold = fmaxf(threshold, key_value(best[k - 1]));
+        __syncwarp();
+      }
+      if (wanted) list[listed + __popc(mask & ((1u << lane) - 1u))] = rank_key(v, (uint32_t)index);
+      listed += __popc(mask);
+      __syncwarp();
+    };
+    for (int base = 0; base < share.words; base += kChunk, ++iteration) {
+      copies_wait<kStages - 1>();
+      uint4 w[kLpWords];
+#pragma unroll
+      for (int u = 0; u < kLpWords; ++u) w[u] = ring[stage * kChunk + u * 32];
+      if (base + kChunk > share.words) {
+#pragma unroll
+        for (int u = 0; u < kLpWords; ++u)
+          if (base + u * 32 + lane >= share.words) w[u] = make_uint4(kNone, kNone, kNone, kNone);
+      }
+      const float biggest = largest_of<T>(w);
+      t.peak = fmaxf(t.peak, biggest);
+      if (__any_sync(0xffffffffu, !(biggest <= t.limit))) t.move_reference(biggest);
+#pragma unroll
+      for (int u = 0; u < kLpWords; ++u) t.add_word(w[u]);
+      if constexpr (TOP) {
+        const bool first = iteration == 0;
+        if (first) {                                      // compared with its own threshold: equal values enter
+          const uint32_t bound = kth_largest_bound(lane < share.words ? order_bits(t.peak) : 0u, k);
+          if (bound >= 0x00800000u) threshold = order_value(bound);      // (below: fewer than k lanes have a finite value; all enter)
+        }
+        if (__any_sync(0xffffffffu, first ? !(biggest < threshold) : !(biggest <= threshold))) {
+          uint32_t bits = candidate_bits<T>(w, threshold, first);
+#pragma unroll
+          for (int u = 0; u < kLpWords; ++u)              // (not the -infinities behind the row's end)
+            if (base + u * 32 + lane >= share.words) bits &= ~(((1u << kVec) - 1u) << (u * kVec));
+          // (all picked with one threshold: one that is raised on the way, by pruning, counts from the next stretch on)
+          while (__any_sync(0xffffffffu, bits != 0)) {
+            const int e = bits ? __ffs(bits) - 1 : 0, u = e / kVec, j = e % kVec;
+            const float v = to_float(reinterpret_cast<const T*>(ring + stage * kChunk + u * 32)[j]);
+            append(bits != 0, v, share.head + (base + u * 32 + lane) * kVec + j);
+            bits &= bits - 1;
+          }
+        }
+        if (iteration + 1 == next_refresh) {
+          if (!first) threshold = fmaxf(threshold, order_value(kth_largest_bound(order_bits(t.peak), k)));      // (NaN: below -infinity)
+          next_refresh *= 2;
+        }
+      }
+      __syncwarp();
+      issue(stage);                                       // into the words just read
+      stage = stage + 1 == kStages ? 0 : stage + 1;
+    }
+    if (__any_sync(0xffffffffu, edge_index >= 0)) {
+      const float v = to_float(edge);
+      t.peak = fmaxf(t.peak, v);
+      if (__any_sync(0xffffffffu, !(v <= t.limit))) t.move_reference(v);
+      t.add_word(make_uint4(Word16<T>::first(edge), kNone, kNone, kNone));
+      if (TOP) append(edge_index >= 0, v, edge_index);
+    }
+    SoftmaxPart part = t.warp_part();
+    const int far = (int)__reduce_or_sync(0xffffffffu, (uint32_t)t.far);
+    if (far && !(far == kFarDown && part.peak >= LogprobThread<T>::kLowest)) {       // (see LogprobThread)
+      part = {-INFINITY, 0.0f, 0.0f};
+      for (int c = lane; c < cols; c += 32) add_far(part, to_float(z[c]));
+      part = join_lanes<32>(part);
+    }
+    const bool empty = part.peak == -INFINITY && part.s == 0.0f;
+    const float log_s = empty ? 0.0f : logf(part.s);
+    if (lane == 0) {
+      if (a.peak) a.peak[row] = part.peak;
+      if (a.log_sum) a.log_sum[row] = log_s;
+      if (a.entropy) a.entropy[row] = empty ? 0.0f : log_s - kLn2 * (part.a / part.s);
+      if (with_target) {
+        float lp = 0.0f;
+        if (target >= a.cols) lp = NAN;
+        else if (target >= 0) lp = empty ? -INFINITY : (to_float(target_logit) - part.peak) - log_s;
+        a.logp[row] = lp;
+      }
+    }
+    if constexpr (TOP) {
+      __syncwarp();
+      select_largest(list, listed, best, k);
+      if (lane < k) {
+        const unsigned long long key = best[lane];
+        a.top_ids[row * k + lane] = key_index(key);
+        a.top_logp[row * k + lane] = empty ? -INFINITY : (key_value(key) - part.peak) - log_s;
+      }
+      __syncwarp();
+    }
   }
 }
 
@@ -685,7 +873,7 @@ static int logprob_cluster(int64_t rows, int64_t cols, size_t size, int sms) {
 template <typename T, bool TOP>
 static int logprob_launch_top(const LogprobArgs& a, int cluster, int sms, cudaStream_t stream) {
   constexpr size_t kSmem = (size_t)lp_stages<TOP> * kLpChunk * 16;
-  SOLON_CUDA_TRY(cudaFuncSetAttribute(logprob_kernel<T, TOP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem));
+  SOLON_SHARED_MEMORY_ONCE((logprob_kernel<T, TOP>), kSmem);
   const int64_t resident = (int64_t)sms * kLpCtasPerSm / cluster;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((a.rows < resident ? a.rows : resident) * cluster));
@@ -702,8 +890,20 @@ static int logprob_launch_top(const LogprobArgs& a, int cluster, int sms, cudaSt
   return SOLON_OK;
 }
 
+template <typename T, bool TOP>
+static int logprob_launch_warps(const LogprobArgs& a, int sms, cudaStream_t stream) {
+  constexpr size_t kSmem = (size_t)kLpWarps * (lp_warp_stages<TOP> * 32 * kLpWords * 16 + (TOP ? (kLpWarpList + SOLON_MAX_TOP) * 8 : 0));
+  SOLON_SHARED_MEMORY_ONCE((logprob_warp_kernel<T, TOP>), kSmem);
+  const int64_t want = (a.rows + kLpWarps - 1) / kLpWarps, resident = (int64_t)sms * kLpWarpCtas;
+  logprob_warp_kernel<T, TOP><<<(unsigned)(want < resident ? want : resident), kLpThreads, kSmem, stream>>>(a);
+  SOLON_CUDA_TRY(cudaGetLastError());
+  return SOLON_OK;
+}
+
 template <typename T>
 static int logprob_launch(const LogprobArgs& a, int sms, cudaStream_t stream) {
+  if (a.rows >= (int64_t)sms * kLpWarpRows)
+    return a.top_k > 0 ? logprob_launch_warps<T, true>(a, sms, stream) : logprob_launch_warps<T, false>(a, sms, stream);
   const int cluster = logprob_cluster(a.rows, a.cols, sizeof(T), sms);
   return a.top_k > 0 ? logprob_launch_top<T, true>(a, cluster, sms, stream) : logprob_launch_top<T, false>(a, cluster, sms, stream);
 }

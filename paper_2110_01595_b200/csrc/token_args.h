@@ -1,7 +1,23 @@
 // Checks of arguments that the row operators (layer norm, token log probabilities) share.
 #pragma once
 
+#include <atomic>
+
 #include "solon_internal.h"
+
+// Raises a kernel's limit of dynamic shared memory, the first time the calling function launches it on a device (the call costs
+// about as much as a small launch).  Devices from 64 on are asked every time.
+#define SOLON_SHARED_MEMORY_ONCE(kernel, bytes)                                                                              \
+  do {                                                                                                                       \
+    static std::atomic<uint64_t> solon_done__{0};                                                                            \
+    int solon_dev__ = 0;                                                                                                     \
+    SOLON_CUDA_TRY(cudaGetDevice(&solon_dev__));                                                                             \
+    const uint64_t solon_bit__ = solon_dev__ < 64 ? 1ull << solon_dev__ : 0ull;                                              \
+    if (!(solon_done__.load(std::memory_order_relaxed) & solon_bit__)) {                                                     \
+      SOLON_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(bytes)));               \
+      solon_done__.fetch_or(solon_bit__, std::memory_order_relaxed);                                                         \
+    }                                                                                                                        \
+  } while (0)
 
 namespace solon {
 

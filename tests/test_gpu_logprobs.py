@@ -85,7 +85,7 @@ def _check(z, targets, top_k, got):
 
 
 SHAPES = [(1, 1), (1, 2), (5, 7), (3, 33), (2, 255), (4, 256), (9, 1000), (1, 4096), (200, 1031), (2, 8193), (700, 2048), (1, 32768), (3, 50001), (1, 131072), (17, 65536),
-          (150, 30001), (1, 200003), (400, 16384)]
+          (150, 30001), (1, 200003), (400, 16384), (2000, 1), (1800, 37), (1999, 1031), (2400, 4096), (1777, 9001), (5000, 2000)]
 
 
 @pytest.mark.parametrize("rows,cols", SHAPES)
@@ -100,14 +100,13 @@ def test_forward(rows, cols, dtype):
 
 @pytest.mark.parametrize("cols,pitch,offset", [(64, 64, 1), (1000, 1003, 0), (1000, 1008, 8), (5000, 5004, 4), (129, 140, 3), (40001, 40008, 8), (40000, 40001, 5)])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("rows", [3, 400])
+@pytest.mark.parametrize("rows", [3, 400, 1800])
 def test_forward_strides_and_alignment(rows, cols, pitch, offset, dtype):
     z, targets = _logits(rows, cols, dtype, 5, pitch=pitch, offset=offset)
     _check(z, targets, 5, binding.solon_token_logprobs(z, targets, top_k=5))       # the 99s beside the rows are not read
 
 
-@pytest.mark.parametrize("rows", [1, 12, 600])
-@pytest.mark.parametrize("cols", [50, 3000, 70001])
+@pytest.mark.parametrize("rows,cols", [(1, 50), (1, 3000), (1, 70001), (12, 50), (12, 3000), (12, 70001), (600, 50), (600, 3000), (600, 70001), (1800, 50), (1900, 9000)])
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 def test_masks(rows, cols, dtype):
     """Rows with few tokens left, with one, with none, and masks of the type's lowest value instead of -infinity."""
@@ -128,8 +127,7 @@ def test_masks(rows, cols, dtype):
         _check(z, targets, k, binding.solon_token_logprobs(z, targets, top_k=k))
 
 
-@pytest.mark.parametrize("cols", [40, 5000, 100_000])
-@pytest.mark.parametrize("rows", [1, 300])
+@pytest.mark.parametrize("rows,cols", [(1, 40), (1, 5000), (1, 100_000), (300, 40), (300, 5000), (300, 100_000), (1800, 40), (1800, 5000)])
 def test_ties_orders_and_extremes_among_the_likeliest(rows, cols):
     """Constant rows, few distinct values, rising and falling rows, +0 and -0, the largest values packed into one stretch."""
     g = torch.Generator(device="cuda").manual_seed(3)
@@ -148,7 +146,7 @@ def test_ties_orders_and_extremes_among_the_likeliest(rows, cols):
 
 def test_wide_spread_of_values():
     """Logits over hundreds of units, each thread's and each CTA's maximum far from the row's."""
-    for rows in (1, 3, 400):
+    for rows in (1, 3, 400, 1800):
         z = torch.linspace(-300, 300, 30_000, device="cuda").repeat(rows, 1)
         z = z[:, torch.randperm(30_000, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))].contiguous()
         targets = torch.zeros(rows, dtype=torch.long, device="cuda")
@@ -156,13 +154,14 @@ def test_wide_spread_of_values():
             _check(order, targets, 9, binding.solon_token_logprobs(order, targets, top_k=9))
 
 
-@pytest.mark.parametrize("cols", [300, 40_000])
-def test_targets_and_values_that_are_not_numbers(cols):
+@pytest.mark.parametrize("cols,copies", [(300, 1), (40_000, 1), (300, 400), (4000, 400)])
+def test_targets_and_values_that_are_not_numbers(cols, copies):
     z, _ = _logits(6, cols, "f32", 8)
     targets = torch.tensor([0, -1, cols, cols - 1, 5, -100], device="cuda")
     z[4, 7] = float("nan")
     z[5, 9] = INF
-    got = binding.solon_token_logprobs(z, targets, top_k=3)
+    got = binding.solon_token_logprobs(z.repeat(copies, 1), targets.repeat(copies), top_k=3)
+    got = binding.TokenLogprobs(*[x[-6:] for x in got])
     ok = [0, 1, 3]
     _check(z[ok], targets[ok], 3, binding.TokenLogprobs(*[t[ok] for t in got]))
     assert got.logp[2].isnan() and got.log_sum[2].isfinite()
@@ -277,7 +276,7 @@ def test_empty_other_streams_and_repeats():
     r = binding.solon_token_logprobs(z, torch.empty(0, dtype=torch.long, device="cuda"), top_k=3)
     assert r.logp.shape == (0,) and r.top_ids.shape == (0, 3)
     assert binding.solon_token_logprobs_backward(z, None, r.peak, r.log_sum).shape == (0, 40)
-    for rows in (2, 500):
+    for rows in (2, 500, 2000):
         z, targets = _logits(rows, 20_000, "bf16", 12)
         want = binding.solon_token_logprobs(z, targets, top_k=6)
         side = torch.cuda.Stream()
