@@ -265,14 +265,18 @@ def solon_layernorm_forward(x, weight=None, bias=None, eps: float = 1e-5, y=None
     stream = _current_stream(device)
     if y is None:
         y = x.new_empty((rows, cols))
-    if mean is None:
-        mean = x.new_empty((rows,), dtype=f32)
-    if rstd is None:
-        rstd = x.new_empty((rows,), dtype=f32)
-    py, y_pitch = _matrix(y, "y", x)
+        py, y_pitch = y.data_ptr(), cols
+    else:
+        py, y_pitch = _matrix(y, "y", x)
+    if mean is None and rstd is None:
+        mean, rstd = x.new_empty((2, rows), dtype=f32).unbind(0)
+        pm, pr = mean.data_ptr(), rstd.data_ptr()
+    else:
+        mean = x.new_empty((rows,), dtype=f32) if mean is None else mean
+        rstd = x.new_empty((rows,), dtype=f32) if rstd is None else rstd
+        pm, pr = _vector(mean, "mean", rows, f32, device), _vector(rstd, "rstd", rows, f32, device)
     pw, pb, code = _params(weight, bias, cols, x)
-    _check(lib().solon_layernorm_forward(px, x_pitch, _dtype_code(x.dtype), pw, pb, code, rows, cols, eps, py, y_pitch,
-                                         _vector(mean, "mean", rows, f32, device), _vector(rstd, "rstd", rows, f32, device), stream),
+    _check(lib().solon_layernorm_forward(px, x_pitch, _dtype_code(x.dtype), pw, pb, code, rows, cols, eps, py, y_pitch, pm, pr, stream),
            "solon_layernorm_forward")
     return y, mean, rstd
 
@@ -290,7 +294,9 @@ def solon_layernorm_backward(dy, x, mean, rstd, weight=None, partitions: int = 1
     stream = _current_stream(device)
     if dx is None:
         dx = x.new_empty((rows, cols))
-    pdx, dx_pitch = _matrix(dx, "dx", x)
+        pdx, dx_pitch = dx.data_ptr(), cols
+    else:
+        pdx, dx_pitch = _matrix(dx, "dx", x)
     pw, _, code = _params(weight, None, cols, x)
     pdw = pdb = workspace = None
     grad_pitch, grad_code, n_bytes = cols, F32, 0
@@ -363,7 +369,9 @@ def solon_token_logprobs_backward(logits, targets, peak, log_sum, grad_logp=None
     stream = _current_stream(device)
     if out is None:
         out = logits.new_empty((rows, vocab))
-    po, out_pitch = _matrix(out, "out", logits)
+        po, out_pitch = out.data_ptr(), vocab
+    else:
+        po, out_pitch = _matrix(out, "out", logits)
 
     def row_vector(t, name):
         return None if t is None else _vector(t, name, rows, torch.float32, device)
