@@ -138,6 +138,18 @@ struct LnRow {
   // weight or bias of the thread's columns (once per CTA)
   static __device__ __forceinline__ void params(Float2 (&w)[ELEMS / 2], const void* p, int is_f32, int dtype, float absent, int cols, int tid) {
     float e[ELEMS];
+    if constexpr (VEC > 1) {
+      if (p && is_f32 && ((uintptr_t)p & 15) == 0) {
+#pragma unroll
+        for (int i = 0; i < ELEMS; i += 4) {
+          const int c = column(i / VEC, tid) + i % VEC;
+          const float4 v = c < cols ? *reinterpret_cast<const float4*>(static_cast<const float*>(p) + c) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          w[i / 2] = pack2(v.x, v.y);
+          w[i / 2 + 1] = pack2(v.z, v.w);
+        }
+        return;
+      }
+    }
 #pragma unroll
     for (int i = 0; i < ELEMS; ++i) {
       const int c = column(i / VEC, tid) + i % VEC;
