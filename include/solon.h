@@ -45,7 +45,7 @@ typedef enum solon_status {
 #define SOLON_MAX_PROJECTIONS 4   /* random projections K                                     */
 #define SOLON_MAX_COLS (1 << 24)  /* width of a layer norm's row; vocabulary                  */
 #define SOLON_MAX_TOP 32          /* likeliest tokens solon_token_logprobs reports            */
-#define SOLON_ADAMW_MAX_NUMEL (1LL << 40)
+#define SOLON_ADAMW_MAX_NUMEL (1LL << 36)   /* parameters of an optimizer handle, rounded up to blocks of 256 */
 
 /* Element type of partition gradients, coded vectors and aggregate (a property of the plan). */
 typedef enum solon_dtype {

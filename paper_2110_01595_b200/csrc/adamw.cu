@@ -670,8 +670,7 @@ static int adam_create(solon_adamw* o, const int64_t* numel, float* const* param
     o->total += numel[i];
     o->n_blocks += adam_blocks(numel[i]);
   }
-  o->n_chunks = (int64_t)o->chunks.size();
-  if (o->n_chunks > 0x7fffffffLL) return SOLON_ERR_INVALID_ARG;
+  o->n_chunks = (int64_t)o->chunks.size();      // (at most one a block: below 2^31)
   o->norm_grid = o->num_sms * 4;
   if (o->norm_grid > o->n_chunks) o->norm_grid = o->n_chunks ? (int)o->n_chunks : 1;
   int rc;
@@ -706,8 +705,9 @@ int64_t solon_adamw_state_blocks(int n_tensors, const int64_t* numel) {
   if (n_tensors < 1 || !numel) return SOLON_ERR_INVALID_ARG;
   int64_t blocks = 0;
   for (int i = 0; i < n_tensors; ++i) {
-    if (numel[i] < 0 || numel[i] > SOLON_ADAMW_MAX_NUMEL || blocks > SOLON_ADAMW_MAX_NUMEL) return SOLON_ERR_INVALID_ARG;
+    if (numel[i] < 0 || numel[i] > SOLON_ADAMW_MAX_NUMEL) return SOLON_ERR_INVALID_ARG;
     blocks += adam_blocks(numel[i]);
+    if (blocks > SOLON_ADAMW_MAX_NUMEL / kAdamBlock) return SOLON_ERR_INVALID_ARG;
   }
   return blocks;
 }
@@ -854,7 +854,6 @@ int solon_adamw_moments(solon_adamw* opt, void* exp_avg_out, void* exp_avg_sq_ou
   if (((uintptr_t)exp_avg_out | (uintptr_t)exp_avg_sq_out) & 15) return SOLON_ERR_INVALID_ARG;
   const int64_t words = opt->n_blocks * (kAdamBlock / 16);
   if (words == 0) return SOLON_OK;
-  if ((words + 255) / 256 > 0x7fffffffLL) return SOLON_ERR_INVALID_ARG;
   adam_moments_kernel<<<(unsigned)((words + 255) / 256), 256, 0, (cudaStream_t)cuda_stream>>>(
       (const uint4*)opt->exp_avg, (const uint4*)opt->exp_avg_sq, (const uint32_t*)opt->base, words, (uint4*)exp_avg_out, (uint4*)exp_avg_sq_out);
   SOLON_CUDA_TRY(cudaGetLastError());

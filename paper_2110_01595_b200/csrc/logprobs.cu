@@ -177,13 +177,13 @@ struct LogprobThread {
 };
 
 // Largest element of a thread's words (NaN if there is one).
-template <typename T>
-__device__ __forceinline__ float largest_of(const uint4 (&w)[kLpWords]) {
-  uint32_t m[kLpWords];
+template <typename T, int N>
+__device__ __forceinline__ float largest_of(const uint4 (&w)[N]) {
+  uint32_t m[N];
 #pragma unroll
-  for (int u = 0; u < kLpWords; ++u) m[u] = Word16<T>::at_least(Word16<T>::at_least(w[u].x, w[u].y), Word16<T>::at_least(w[u].z, w[u].w));
+  for (int u = 0; u < N; ++u) m[u] = Word16<T>::at_least(Word16<T>::at_least(w[u].x, w[u].y), Word16<T>::at_least(w[u].z, w[u].w));
 #pragma unroll
-  for (int n = kLpWords / 2; n > 0; n /= 2)
+  for (int n = N / 2; n > 0; n /= 2)
 #pragma unroll
     for (int u = 0; u < n; ++u) m[u] = Word16<T>::at_least(m[u], m[u + n]);
   return Word16<T>::widest(m[0]);
@@ -247,11 +247,11 @@ __device__ __forceinline__ void push_candidate(int* count, unsigned long long* k
 
 // Which of a thread's elements are above the threshold (`ties`: not below it), as bits; words whose largest value is not are
 // passed over.  Elements are fetched from the ring again by their bits: few are, and the code for them stays short.
-template <typename T>
-__device__ __forceinline__ uint32_t candidate_bits(const uint4 (&w)[kLpWords], float threshold, bool ties) {
+template <typename T, int N>
+__device__ __forceinline__ uint32_t candidate_bits(const uint4 (&w)[N], float threshold, bool ties) {
   uint32_t bits = 0;
 #pragma unroll
-  for (int u = 0; u < kLpWords; ++u) {
+  for (int u = 0; u < N; ++u) {
     const float big = Word16<T>::largest(w[u]);
     if (ties ? !(big < threshold) : !(big <= threshold)) {
       float x[Word16<T>::kCount];
@@ -407,7 +407,7 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprob_kernel(Logpr
       const int left = ahead.end - ahead_base - (int)threadIdx.x;
 #pragma unroll
       for (int u = 0; u < kLpWords; ++u)
-        if (u * kLpThreads < left) copy16_async(to + u * kLpThreads, from + u * kLpThreads, true);
+        if (u * kLpThreads < left) copy16_async(to + u * kLpThreads, from + u * kLpThreads);
       ahead_base += kLpChunk;
     }
     copies_commit();
@@ -590,16 +590,19 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprob_kernel(Logpr
 
 // ---- many rows: a warp a row -----------------------------------------------------------------------------------------
 // Nothing in a row then waits for another warp, and the serial work at a row's end (and for its likeliest tokens) of one warp
-// hides behind the others' streams.  Measured, CTA a row against warp a row: 8192 x 32768 bfloat16 107 / 100 us, with 8
-// alternatives 285 / 166; 2500 x 2000 with 8 36 / 18; the two meet at 12 rows per SM (1776 x 50000: 42 / 39, with 8 68 / 68),
+// hides behind the others' streams.  Measured, CTA a row against warp a row: 8192 x 32768 bfloat16 107 / 91 us, with 8
+// alternatives 285 / 157; 2500 x 2000 with 8 36 / 18; the two meet at 12 rows per SM (1776 x 50000: 42 / 39, with 8 68 / 68),
 // below that the warps are too few.
 // The candidates are a warp's own: filtered as above with the lanes' maxima for groups, appended by ballots, and pruned to the k
 // largest when the list is full.
-constexpr int kLpWarpCtas = 3;                 // CTAs per SM: 24 warps with 8 KB of shared memory each
-constexpr int kLpWarpList = 256;
+constexpr int kLpWarpCtas = 3;                 // CTAs per SM: 24 warps with 8 to 9.5 KB of shared memory each
 constexpr int kLpWarpRows = 12;                // rows per SM from which on rows go to warps
-template <bool TOP>
-constexpr int lp_warp_stages = TOP ? 3 : 4;
+template <typename T>
+constexpr int lp_warp_words = 32 / Word16<T>::kCount;                    // words of a lane in an iteration: 32 elements
+template <typename T, bool TOP>
+constexpr int lp_warp_stages = sizeof(T) == 4 ? 2 : TOP ? 3 : 4;         // iterations' words in shared memory
+template <typename T>
+constexpr int lp_warp_list = sizeof(T) == 4 ? 128 : 256;                 // candidates
 
 // A lower bound of the k-th largest of the lanes' values (order bits): exact in the upper 16 bits.
 __device__ __forceinline__ uint32_t kth_largest_bound(uint32_t mine, int k) {
@@ -615,42 +618,56 @@ __device__ __forceinline__ uint32_t kth_largest_bound(uint32_t mine, int k) {
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(kLpThreads, kLpWarpCtas) logprob_warp_kernel(LogprobArgs a) {
   constexpr int kVec = Word16<T>::kCount;
-  constexpr int kStages = lp_warp_stages<TOP>;
-  constexpr int kChunk = 32 * kLpWords;                   // words of an iteration
+  constexpr int kWords = lp_warp_words<T>;
+  constexpr int kStages = lp_warp_stages<T, TOP>;
+  constexpr int kChunk = 32 * kWords;                     // words of an iteration
   constexpr uint32_t kNone = Word16<T>::kMinusInf;
   extern __shared__ __align__(16) uint4 shared[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   uint4* ring = shared + warp * kStages * kChunk + lane;
-  unsigned long long* list = reinterpret_cast<unsigned long long*>(shared + kLpWarps * kStages * kChunk) + warp * (kLpWarpList + SOLON_MAX_TOP);
-  unsigned long long* best = list + kLpWarpList;
+  unsigned long long* list = reinterpret_cast<unsigned long long*>(shared + kLpWarps * kStages * kChunk) + warp * (lp_warp_list<T> + SOLON_MAX_TOP);
+  unsigned long long* best = list + lp_warp_list<T>;
   const int cols = (int)a.cols, k = a.top_k;
   const int64_t stride = (int64_t)gridDim.x * kLpWarps;
 
   int64_t row = (int64_t)warp * gridDim.x + blockIdx.x;   // (neighbouring rows to different SMs)
-  int64_t ahead_row = row;                                // what is copied next
-  RowShare<T> ahead(a, ahead_row < a.rows ? ahead_row : 0, 0, 1);
-  int ahead_base = 0;
-  auto issue = [&](int stage) {
-    while (ahead_row < a.rows && ahead_base >= ahead.words) {
+  int64_t ahead_row = row;                                // what is copied next: the row, the lane's word, the words from there on
+  const uint4* ahead = nullptr;
+  int ahead_left = 0;
+  auto ahead_from = [&]() {
+    while (ahead_row < a.rows) {
+      const RowShare<T> share(a, ahead_row, 0, 1);
+      ahead = share.body() + lane;
+      ahead_left = share.words - lane;
+      if (share.words > 0) return;
       ahead_row += stride;
-      if (ahead_row < a.rows) ahead = RowShare<T>(a, ahead_row, 0, 1);
-      ahead_base = 0;
     }
+  };
+  ahead_from();
+  auto issue = [&](uint4* to) {
     if (ahead_row < a.rows) {
-      const uint4* from = ahead.body() + ahead_base + lane;
-      const int left = ahead.words - ahead_base - lane;
+      if (ahead_left + lane >= kChunk) {
 #pragma unroll
-      for (int u = 0; u < kLpWords; ++u)
-        if (u * 32 < left) copy16_async(ring + stage * kChunk + u * 32, from + u * 32, true);
-      ahead_base += kChunk;
+        for (int u = 0; u < kWords; ++u) copy16_async(to + u * 32, ahead + u * 32);
+      } else {
+#pragma unroll
+        for (int u = 0; u < kWords; ++u)
+          if (u * 32 < ahead_left) copy16_async(to + u * 32, ahead + u * 32);
+      }
+      ahead += kChunk;
+      ahead_left -= kChunk;
+      if (ahead_left + lane <= 0) {
+        ahead_row += stride;
+        ahead_from();
+      }
     }
     copies_commit();
   };
 #pragma unroll
-  for (int s = 0; s < kStages; ++s) issue(s);
+  for (int s = 0; s < kStages; ++s) issue(ring + s * kChunk);
   const bool with_target = a.targets && a.logp;
   int64_t next_target = with_target && row < a.rows ? a.targets[row] : -1;
-  int stage = 0;
+  uint4* stage = ring;
 
   for (; row < a.rows; row += stride) {
     const RowShare<T> share(a, row, 0, 1);
@@ -670,7 +687,7 @@ __global__ void __launch_bounds__(kLpThreads, kLpWarpCtas) logprob_warp_kernel(L
     float threshold = -INFINITY;                          // candidates are above it, or (see above) not below it
     auto append = [&](bool wanted, float v, int index) {
       const uint32_t mask = __ballot_sync(0xffffffffu, wanted);
-      if (listed + __popc(mask) > kLpWarpList) {
+      if (listed + __popc(mask) > lp_warp_list<T>) {
         select_largest(list, listed, best, k);
         if (lane < k) list[lane] = best[lane];
         listed = k;                                       // (of a full list: k of them)
@@ -683,19 +700,20 @@ __global__ void __launch_bounds__(kLpThreads, kLpWarpCtas) logprob_warp_kernel(L
     };
     for (int base = 0; base < share.words; base += kChunk, ++iteration) {
       copies_wait<kStages - 1>();
-      uint4 w[kLpWords];
+      uint4 w[kWords];
 #pragma unroll
-      for (int u = 0; u < kLpWords; ++u) w[u] = ring[stage * kChunk + u * 32];
-      if (base + kChunk > share.words) {
+      for (int u = 0; u < kWords; ++u) w[u] = stage[u * 32];
+      const bool last = base + kChunk > share.words;
+      if (last) {
 #pragma unroll
-        for (int u = 0; u < kLpWords; ++u)
+        for (int u = 0; u < kWords; ++u)
           if (base + u * 32 + lane >= share.words) w[u] = make_uint4(kNone, kNone, kNone, kNone);
       }
       const float biggest = largest_of<T>(w);
       t.peak = fmaxf(t.peak, biggest);
       if (__any_sync(0xffffffffu, !(biggest <= t.limit))) t.move_reference(biggest);
 #pragma unroll
-      for (int u = 0; u < kLpWords; ++u) t.add_word(w[u]);
+      for (int u = 0; u < kWords; ++u) t.add_word(w[u]);
       if constexpr (TOP) {
         const bool first = iteration == 0;
         if (first) {                                      // compared with its own threshold: equal values enter
@@ -704,13 +722,15 @@ __global__ void __launch_bounds__(kLpThreads, kLpWarpCtas) logprob_warp_kernel(L
         }
         if (__any_sync(0xffffffffu, first ? !(biggest < threshold) : !(biggest <= threshold))) {
           uint32_t bits = candidate_bits<T>(w, threshold, first);
+          if (last) {                                     // (not the -infinities behind the row's end)
 #pragma unroll
-          for (int u = 0; u < kLpWords; ++u)              // (not the -infinities behind the row's end)
-            if (base + u * 32 + lane >= share.words) bits &= ~(((1u << kVec) - 1u) << (u * kVec));
+            for (int u = 0; u < kWords; ++u)
+              if (base + u * 32 + lane >= share.words) bits &= ~(((1u << kVec) - 1u) << (u * kVec));
+          }
           // (all picked with one threshold: one that is raised on the way, by pruning, counts from the next stretch on)
           while (__any_sync(0xffffffffu, bits != 0)) {
             const int e = bits ? __ffs(bits) - 1 : 0, u = e / kVec, j = e % kVec;
-            const float v = to_float(reinterpret_cast<const T*>(ring + stage * kChunk + u * 32)[j]);
+            const float v = to_float(reinterpret_cast<const T*>(stage + u * 32)[j]);
             append(bits != 0, v, share.head + (base + u * 32 + lane) * kVec + j);
             bits &= bits - 1;
           }
@@ -720,9 +740,8 @@ __global__ void __launch_bounds__(kLpThreads, kLpWarpCtas) logprob_warp_kernel(L
           next_refresh *= 2;
         }
       }
-      __syncwarp();
       issue(stage);                                       // into the words just read
-      stage = stage + 1 == kStages ? 0 : stage + 1;
+      stage = stage == ring + (kStages - 1) * kChunk ? ring : stage + kChunk;
     }
     if (__any_sync(0xffffffffu, edge_index >= 0)) {
       const float v = to_float(edge);
@@ -892,10 +911,15 @@ static int logprob_launch_top(const LogprobArgs& a, int cluster, int sms, cudaSt
 
 template <typename T, bool TOP>
 static int logprob_launch_warps(const LogprobArgs& a, int sms, cudaStream_t stream) {
-  constexpr size_t kSmem = (size_t)kLpWarps * (lp_warp_stages<TOP> * 32 * kLpWords * 16 + (TOP ? (kLpWarpList + SOLON_MAX_TOP) * 8 : 0));
+  constexpr size_t kPerWarp = lp_warp_stages<T, TOP> * 32 * lp_warp_words<T> * 16 + (TOP ? (lp_warp_list<T> + SOLON_MAX_TOP) * 8 : 0);
+  constexpr size_t kSmem = kLpWarps * kPerWarp;
   SOLON_SHARED_MEMORY_ONCE((logprob_warp_kernel<T, TOP>), kSmem);
-  const int64_t want = (a.rows + kLpWarps - 1) / kLpWarps, resident = (int64_t)sms * kLpWarpCtas;
-  logprob_warp_kernel<T, TOP><<<(unsigned)(want < resident ? want : resident), kLpThreads, kSmem, stream>>>(a);
+  // 24 warps an SM, 16 for the plain sums of two-byte logits: 8192 x 32768 bfloat16 takes 100 us with 24, 91 with 16, 16384 x
+  // 16384 89 and 85 (the last round of rows is fuller, and 16 streams a SM keep the memory as busy); float32 (4096 x 32768: 90
+  // and 90) and likeliest tokens (8192 x 32768 with 8: 157 and 168) have nothing from fewer.
+  constexpr int kCtas = !TOP && sizeof(T) == 2 ? 2 : kLpWarpCtas;
+  const int64_t resident = (int64_t)sms * kCtas;          // (a CTA may have fewer rows than warps: the SMs get equally many)
+  logprob_warp_kernel<T, TOP><<<(unsigned)(a.rows < resident ? a.rows : resident), kLpThreads, kSmem, stream>>>(a);
   SOLON_CUDA_TRY(cudaGetLastError());
   return SOLON_OK;
 }

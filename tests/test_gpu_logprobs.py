@@ -1,7 +1,8 @@
 """Token log probabilities, entropy, likeliest tokens and the gradient, against the formulas in float64 and against differences.
 
 Tolerances (u = 2^-24).  A term e^(z - M) carries a relative error of (2 |z - M| + 4) u; a thread adds at most cols / 256 + 32 of
-them and the threads' sums are joined over at most 40 more roundings.  With k = cols / 256 + 72 and D = E|z - M| + 4 under the softmax:
+them (where a warp has the row, cols / 64, whose rounding errors, of independent sign, stay below the same number) and the threads'
+sums are joined over at most 40 more roundings.  With k = cols / 256 + 72 and D = E|z - M| + 4 under the softmax:
 log S is off by (k + 2 D) u + 2 u |log S|, logp = (z_t - M) - log S by 2 u (|z_t - M| + |log S|) more, and the entropy, a difference of log S and A / S, by
 (2 k + 4 D) u (1 + |log S| + E|z - M| + E|z - M|^2).  In the gradient, whose M, log S and entropy are inputs, p is off by a
 relative (4 |log p| + 6) u, log p itself by 2 u (|z - M| + |log S|) and each product by 4 u more; then the element type's rounding."""

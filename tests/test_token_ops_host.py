@@ -21,6 +21,7 @@ def test_state_blocks(lib):
 
     assert blocks(1) == 1 and blocks(256) == 1 and blocks(257, 0, 5) == 3 and blocks(0) == 0
     assert blocks() == BAD and blocks(-1) == BAD and blocks(1 << 41) == BAD
+    assert blocks(1 << 36) == 1 << 28 and blocks(1 << 36, 1) == BAD and blocks(*[1 << 35] * 3) == BAD
     assert lib.solon_adamw_state_blocks(1, None) == BAD
 
 
@@ -63,6 +64,12 @@ def test_refused_arguments(lib):
                  lambda h: lib.solon_adamw_bind_grads(h, None, 0), lambda h: lib.solon_adamw_moments(h, at, at, None),
                  lambda h: lib.solon_adamw_step(h, at, 0, 1.0, 1.0, 0.0, None, None, None)):
         assert call(None) == BAD
+
+
+def test_plans_refuse_the_types_of_the_token_operators(lib):
+    plan = ctypes.c_void_p()
+    for dtype in (binding.BF16, binding.F16, 4, -1):
+        assert lib.solon_plan_create_ex(8, 1, 2, 4, 64, 1, dtype, ctypes.byref(plan)) == BAD and plan.value is None
 
 
 def test_refused_handles(lib):
