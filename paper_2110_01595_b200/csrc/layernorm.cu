@@ -167,8 +167,12 @@ __device__ __forceinline__ float sum_of(Float2 x) {
   return a + b;
 }
 
+// CTAs of the forward pass on an SM: with single elements a third one pays (30000 x 2001 bfloat16 81 -> 71 us, float32 98 -> 91).
+template <int VEC, int TPR, int ELEMS>
+constexpr int ln_forward_ctas = TPR >= 512 ? 1 : VEC > 1 || ELEMS > 16 ? 2 : 3;
+
 template <typename T, int VEC, int TPR, int ELEMS>
-__global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, TPR < 512 ? 2 : 1) ln_forward_kernel(LnForwardArgs a) {
+__global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, ln_forward_ctas<VEC, TPR, ELEMS>) ln_forward_kernel(LnForwardArgs a) {
   using Row = LnRow<T, VEC, TPR, ELEMS>;
   constexpr int kStages = ln_stages<T, TPR, ELEMS, 1>;
   constexpr int kStageWords = Row::kGroups * Row::kBlock;
@@ -521,7 +525,7 @@ static int ln_forward_launch(const LnForwardArgs& a, int sms, cudaStream_t strea
   constexpr int kTeams = kBlock / TPR;
   constexpr size_t kSmem = VEC > 1 ? (size_t)ln_stages<T, TPR, ELEMS, 1> * (ELEMS / VEC) * 16 * kBlock : 0;
   if constexpr (kSmem > 40 * 1024) SOLON_SHARED_MEMORY_ONCE((ln_forward_kernel<T, VEC, TPR, ELEMS>), kSmem);
-  const int64_t want = (a.rows + kTeams - 1) / kTeams, cap = (int64_t)sms * (TPR < 512 ? 2 : 1);
+  const int64_t want = (a.rows + kTeams - 1) / kTeams, cap = (int64_t)sms * ln_forward_ctas<VEC, TPR, ELEMS>;
   ln_forward_kernel<T, VEC, TPR, ELEMS><<<(unsigned)ln_min(want, cap), kBlock, kSmem, stream>>>(a);
   SOLON_CUDA_TRY(cudaGetLastError());
   return SOLON_OK;
@@ -538,6 +542,10 @@ static int ln_backward_launch(const LnBackwardArgs& a, int partitions, cudaStrea
   SOLON_CUDA_TRY(cudaGetLastError());
   return SOLON_OK;
 }
+
+// Rows of single elements wider than this take 32 a thread, so that two CTAs fit on an SM (8000 x 7001 bfloat16 115 -> 87 us;
+// narrower ones lose by it: 30000 x 2001 70 -> 75).
+constexpr int kLnWideSingle = 4096;
 
 // f(team size, elements of a thread), both as compile-time constants.  A thread takes up to 16 elements; 32 in the forward
 // pass over 16-byte words of two-byte types.
@@ -573,6 +581,8 @@ static int ln_forward_t(const LnForwardArgs& a, int sms, cudaStream_t stream) {
     return ln_by_team<64 / (int)sizeof(T), 16 / (int)sizeof(T)>(a.cols, [&](auto team, auto elems) {
       return ln_forward_launch<T, 16 / (int)sizeof(T), team.value, elems.value>(a, sms, stream);
     });
+  if (a.cols > kLnWideSingle)
+    return ln_by_team<32, 1>(a.cols, [&](auto team, auto elems) { return ln_forward_launch<T, 1, team.value, elems.value>(a, sms, stream); });
   return ln_by_team<16, 1>(a.cols, [&](auto team, auto elems) { return ln_forward_launch<T, 1, team.value, elems.value>(a, sms, stream); });
 }
 
