@@ -339,6 +339,7 @@ __global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, TPR < 512
       Row::store(dx + row * a.dx_pitch, g, cols, tid);
     }
   }
+  pdl_trigger();                               // the kernel that adds up the partial sums may take its place (it waits for this one)
   if (!a.dweight && !a.dbias) return;
   float sums[2][ELEMS];                        // weight, bias
 #pragma unroll

@@ -338,6 +338,21 @@ def test_nothing_beside_the_tensors_is_written():
             assert torch.equal(g, keep)
 
 
+def test_offsets_beyond_32_bits():
+    """More than 2^31 weights with 8-bit states: the last tensor's step as that of a handle of its own would be, but for the
+    rounding's random bits (which go by the place in the state): parameters, whose step comes before the rounding, are equal."""
+    n = 2_200_000_001
+    p, g = torch.zeros(n, device="cuda"), torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    p[-5000:], g[-5000:] = _randn(5000, 1), _randn(5000, 2).bfloat16()
+    own, grad = p[-5000:].clone(), g[-5000:].clone()
+    big, small = binding.AdamW([p[:-5000], p[-5000:]], bits=8), binding.AdamW([own], bits=8)
+    a, b = big.step(g, lr=1e-2, max_norm=0.5), small.step(grad, lr=1e-2, max_norm=0.5)
+    assert abs(float(a) - float(b)) <= 1e-6 * float(b) and float((p[-5000:] - own).abs().max()) <= 1e-6
+    m, v = (big.of_tensor(t, 1).float() for t in big.moments())
+    assert float((m - 0.1 * grad.float() * (0.5 / float(b))).abs().max()) <= 0.13 * 0.1 * float(grad.float().abs().max()) * 0.5 / float(b)
+    assert (v > 0).all() and not big.state[0][:-20].any() and (p[:-5000] == 0).all()
+
+
 def test_refusals():
     p = torch.zeros(100, device="cuda")
     g = torch.zeros(100, device="cuda")

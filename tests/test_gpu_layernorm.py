@@ -215,6 +215,23 @@ def test_empty_and_other_streams():
     assert all(torch.equal(p, q) for p, q in zip(want + want_b, got + got_b))
 
 
+def test_offsets_beyond_32_bits():
+    """A matrix of more than 2^32 bytes and 2^31 elements: its last rows, and the last partition's sums, as those of a copy."""
+    rows, cols, tail = 540_000, 4000, 1000
+    x = torch.empty((rows, cols), dtype=torch.bfloat16, device="cuda")
+    x[:-tail] = 1.0
+    x[-tail:] = _randn((tail, cols), torch.bfloat16, 1)
+    w = _randn(cols, torch.float32, 2)
+    y, mean, rstd = binding.solon_layernorm_forward(x, w, w)
+    part = binding.solon_layernorm_forward(x[-tail:].clone(), w, w)
+    assert torch.equal(y[-tail:], part[0]) and torch.equal(mean[-tail:], part[1]) and torch.equal(rstd[-tail:], part[2])
+    parts = rows // tail
+    dx, dw, db = binding.solon_layernorm_backward(x, x, mean, rstd, w, partitions=parts, dx=y)
+    got = binding.solon_layernorm_backward(x[-tail:].clone(), x[-tail:].clone(), part[1], part[2], w)
+    assert torch.equal(dx[-tail:], got[0])
+    assert float((dw[-1] - got[1][0]).abs().max()) <= 1e-4 * float(got[1].abs().max()) and float((db[-1] - got[2][0]).abs().max()) <= 1e-4 * float(got[2].abs().max())
+
+
 def test_refusals():
     x = torch.zeros((6, 8), device="cuda")
     m = torch.zeros(6, device="cuda")

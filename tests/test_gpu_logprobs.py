@@ -288,6 +288,22 @@ def test_empty_other_streams_and_repeats():
         assert all(torch.equal(p, q) for p, q in zip(want, got))
 
 
+def test_offsets_beyond_32_bits():
+    """A matrix of more than 2^32 bytes and 2^31 elements: its last rows as those of a copy, forward and backward in place."""
+    rows, cols, tail = 70_000, 32_000, 2000
+    z = torch.zeros((rows, cols), dtype=torch.bfloat16, device="cuda")
+    z[-tail:], last = _logits(tail, cols, "bf16", 3)
+    targets = torch.zeros(rows, dtype=torch.long, device="cuda")
+    targets[-tail:] = last
+    got = binding.solon_token_logprobs(z, targets, top_k=3)
+    want = binding.solon_token_logprobs(z[-tail:].clone(), last, top_k=3)
+    assert all(torch.equal(x[-tail:], y) for x, y in zip(got, want))
+    g = torch.full((rows,), 0.5, device="cuda")
+    want = binding.solon_token_logprobs_backward(z[-tail:].clone(), last, want.peak, want.log_sum, g[-tail:].clone())
+    binding.solon_token_logprobs_backward(z, targets, got.peak, got.log_sum, g, out=z)
+    assert torch.equal(z[-tail:], want)
+
+
 def test_refusals():
     z = torch.zeros((6, 8), device="cuda")
     t = torch.zeros(6, dtype=torch.long, device="cuda")
