@@ -7,6 +7,7 @@ The library is loaded on first use and a missing build raises: there is no fallb
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int, c_int64, c_uint8, c_uint64, c_void_p
 from typing import NamedTuple
@@ -281,6 +282,11 @@ def solon_layernorm_forward(x, weight=None, bias=None, eps: float = 1e-5, y=None
     return y, mean, rstd
 
 
+@functools.lru_cache(maxsize=256)
+def _layernorm_workspace(rows: int, cols: int, partitions: int) -> int:
+    return lib().solon_layernorm_backward_workspace(rows, cols, partitions)
+
+
 def solon_layernorm_backward(dy, x, mean, rstd, weight=None, partitions: int = 1, dx=None, dweight=None, dbias=None, param_grads: bool = True):
     """Gradients of layer norm.  Returns (dx, dweight, dbias); dweight and dbias are partitions x cols, row k summed over the
     rows of partition k (rows / partitions consecutive ones).  They may be views into the partition-gradient matrix
@@ -315,7 +321,7 @@ def solon_layernorm_backward(dy, x, mean, rstd, weight=None, partitions: int = 1
         if grad_pitch != other_pitch:
             raise ValueError("dweight and dbias must have the same row pitch")
         grad_code = _dtype_code(dweight.dtype)
-        n_bytes = lib().solon_layernorm_backward_workspace(rows, cols, partitions)
+        n_bytes = _layernorm_workspace(rows, cols, partitions)
         if n_bytes > 0:
             workspace = x.new_empty((n_bytes // 4,), dtype=f32)
     _check(lib().solon_layernorm_backward(pdy, dy_pitch, px, x_pitch, _dtype_code(x.dtype), pw, code, _vector(mean, "mean", rows, f32, device),

@@ -5,6 +5,9 @@
 // All of it in float32; b1^t and b2^t are kept in float64 on the device, so that a replayed CUDA graph counts its steps.
 //
 // Bound by memory: a weight with float32 gradient moves 28 bytes (32-bit states) or 16 (8-bit states) against about 20 flops.
+// Measured on 50 M weights: 32-bit states 204 us (6.9 TB/s); 8-bit states 144 us (5.6 TB/s; codes and random bits keep the integer
+// pipe busy 61 % of the time), with float64 gradients 155 us (6.4 TB/s); the norm 65 us of 400 MB of float64 gradients, 31 us of
+// float32 ones, which the update then partly finds in L2.
 //
 // Work: the state is laid out in blocks of 256 elements, every tensor starting a block of its own; one warp owns a block, one
 // CTA eight consecutive blocks of a tensor (a chunk).  Three launches at most: the gradient's squared norm (only when it is
@@ -266,8 +269,9 @@ struct AdamStepArgs {
 // start on the groups' boundaries (tensors that are pieces of one vector, at any offset: what the aggregate's users have), a
 // group is put together from the two aligned words that hold it, and parameters go back as aligned words too.  Single
 // accesses of four bytes move the same bytes in four times as many requests, which caps what is on the way: 11.2 M weights of
-// an odd offset take 63 us that way against 49 us aligned.  The aligned words reach up to three elements beyond the block,
-// so a tensor's first and last block, and blocks that are not full, go element by element (every 32nd a lane's).
+// an odd offset take 63 us that way, 55 us from aligned words, 49 us where they are aligned.  The aligned words reach up to three
+// elements beyond the block, so a tensor's first and last block, and blocks that are not full, go element by element (every 32nd a
+// lane's).
 enum BlockMode { kSingle, kAligned, kShifted };
 
 template <bool VEC>

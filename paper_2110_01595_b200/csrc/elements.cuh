@@ -47,10 +47,14 @@ __device__ __forceinline__ uint4 load16_once(const void* p) {
   return v;
 }
 
-// 16 bytes to shared memory without passing registers, in groups that a thread waits for by their number (its own copies only).
-__device__ __forceinline__ void copy16_async(void* dst_smem, const void* src, bool inside) {
-  const int bytes = inside ? 16 : 0;           // 0: the 16 bytes are filled with zeros, nothing is read
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst_smem)), "l"(src), "r"(bytes) : "memory");
+// Copies to shared memory that do not pass registers, in groups that a thread waits for by their number (its own copies only).
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* dst_smem, const void* src, bool inside) {       // 4, 8 or 16 bytes
+  const int bytes = inside ? BYTES : 0;        // 0: the place is filled with zeros, nothing is read
+  if constexpr (BYTES == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst_smem)), "l"(src), "r"(bytes) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"((uint32_t)__cvta_generic_to_shared(dst_smem)), "l"(src), "n"(BYTES), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void copy16_async(void* dst_smem, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst_smem)), "l"(src) : "memory");

@@ -5,7 +5,10 @@
 // The variance is summed over the differences from the mean (a second sweep over values that sit in registers), not as a
 // difference of two sums; statistics and sums are float32.
 //
-// Bound by memory: 2 (forward) and 3 (backward) accesses of the matrix against about 8 and 14 flops an element.
+// Bound by memory: 2 (forward) and 3 (backward) accesses of the matrix against about 8 and 14 flops an element.  Measured:
+// forward 16384 x 4096 bfloat16 48 us (5.6 TB/s), float32 96 us (5.6 TB/s); backward 15 x 2048 rows of 2048 bfloat16 68 us
+// (5.6 TB/s) and 7 us for the partial sums, 16384 x 4096 float32 143 us (5.6 TB/s).  What keeps it from the copy rate is 16 warps
+// an SM (the registers of a column's parameters and sums), each with a barrier or two a row.
 //
 // Layout: a row belongs to a team of TPR threads that hold 16 or 32 elements each (fewer in short rows), so that a team's
 // reductions cost little beside the work on the elements.  Teams of one warp meet in shuffles only, larger ones
@@ -85,60 +88,73 @@ struct LnForwardArgs {
   int param_f32, dtype;
 };
 
-// How a thread sees a row: ELEMS elements in groups of VEC neighbours - 16-byte words, or single elements where rows are not
-// made of 16-byte words at 16-byte boundaries; those are loaded straight into registers.  Pairs of elements share an instruction.
+// How a thread sees a row: ELEMS elements in groups of VEC neighbours - 16-byte words, or, where rows are not made of 16-byte
+// words at 16-byte boundaries, pairs or single elements.  Single elements are loaded straight into registers: no asynchronous copy
+// moves two bytes, and with four a copy per element costs more than it hides (backward 15 x 1000 x 2001 float32 78 us straight, 98
+// copied).  Pairs gain by the ring (30000 x 2002 bfloat16 70 -> 54 us, backward 45 x 700 x 1002 63 -> 54).  Two elements share an
+// instruction.
 template <typename T, int VEC, int TPR, int ELEMS>
 struct LnRow {
   static constexpr int kGroups = ELEMS / VEC;
   static constexpr int kBlock = TPR < kLnThreads ? kLnThreads : TPR;
   static constexpr int kTeams = kBlock / TPR;
+  static constexpr bool kRing = VEC > 1;
+  using Group = Pack<T, VEC>;
+  static constexpr int kStageGroups = kGroups * kBlock;      // of a stage: one row of every team
 
   static __device__ __forceinline__ int column(int group, int tid) { return (group * TPR + tid) * VEC; }
 
-  // the copies of a row's words into a stage of the ring (words x threads)
-  static __device__ __forceinline__ void issue(uint4* stage, const T* row, int cols, int tid) {
+  // the copies of a row's groups into a stage of the ring (groups x threads)
+  static __device__ __forceinline__ void issue(Group* stage, const T* row, int cols, int tid) {
 #pragma unroll
     for (int i = 0; i < kGroups; ++i) {
       const int c = column(i, tid);
-      copy16_async(stage + i * kBlock + threadIdx.x, c < cols ? row + c : row, c < cols);
+      copy_async<(int)sizeof(Group)>(stage + i * kBlock + threadIdx.x, c < cols ? row + c : row, c < cols);
     }
   }
-  static __device__ __forceinline__ void take(Float2 (&v)[ELEMS / 2], const uint4* stage, const T* row, int cols, int tid) {
-    if constexpr (VEC > 1) {
+  static __device__ __forceinline__ void take(Float2 (&v)[ELEMS / 2], const Group* stage, const T* row, int cols, int tid) {
+    if constexpr (VEC * sizeof(T) == 16) {
 #pragma unroll
       for (int i = 0; i < kGroups; ++i) {
         float part[VEC];
-        Word16<T>::unpack(stage[i * kBlock + threadIdx.x], part);
+        Word16<T>::unpack(reinterpret_cast<const uint4&>(stage[i * kBlock + threadIdx.x]), part);
 #pragma unroll
         for (int k = 0; k < VEC; k += 2) v[(i * VEC + k) / 2] = pack2(part[k], part[k + 1]);
       }
     } else {
-      T part[ELEMS];
+      Group part[kGroups];
 #pragma unroll
-      for (int i = 0; i < ELEMS; ++i) part[i] = column(i, tid) < cols ? row[column(i, tid)] : from_float<T>(0.0f);
+      for (int i = 0; i < kGroups; ++i) {
+        if constexpr (kRing) part[i] = stage[i * kBlock + threadIdx.x];
+        else part[i].e[0] = column(i, tid) < cols ? row[column(i, tid)] : from_float<T>(0.0f);
+      }
 #pragma unroll
-      for (int i = 0; i < ELEMS; i += 2) v[i / 2] = pack2(to_float(part[i]), to_float(part[i + 1]));
+      for (int i = 0; i < ELEMS; i += 2) v[i / 2] = pack2(to_float(part[i / VEC].e[i % VEC]), to_float(part[(i + 1) / VEC].e[(i + 1) % VEC]));
     }
   }
   static __device__ __forceinline__ void store(T* row, const Float2 (&v)[ELEMS / 2], int cols, int tid) {
 #pragma unroll
     for (int i = 0; i < kGroups; ++i) {
-      if constexpr (VEC > 1) {
+      const int c = column(i, tid);
+      if constexpr (VEC * sizeof(T) == 16) {
         float part[VEC];
 #pragma unroll
         for (int k = 0; k < VEC; k += 2) unpack2(v[(i * VEC + k) / 2], part[k], part[k + 1]);
-        if (column(i, tid) < cols) *reinterpret_cast<uint4*>(row + column(i, tid)) = Word16<T>::pack(part);
+        if (c < cols) *reinterpret_cast<uint4*>(row + c) = Word16<T>::pack(part);
       } else {
         float part[2];
-        unpack2(v[i / 2], part[0], part[1]);
-        if (column(i, tid) < cols) row[column(i, tid)] = from_float<T>(part[i % 2]);
+        unpack2(v[i * VEC / 2], part[0], part[1]);
+        Group p;
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) p.e[k] = from_float<T>(part[(i * VEC + k) % 2]);
+        if (c < cols) store_pack<T, VEC>(row + c, p);
       }
     }
   }
   // weight or bias of the thread's columns (once per CTA)
   static __device__ __forceinline__ void params(Float2 (&w)[ELEMS / 2], const void* p, int is_f32, int dtype, float absent, int cols, int tid) {
     float e[ELEMS];
-    if constexpr (VEC > 1) {
+    if constexpr (VEC >= 4) {
       if (p && is_f32 && ((uintptr_t)p & 15) == 0) {
 #pragma unroll
         for (int i = 0; i < ELEMS; i += 4) {
@@ -175,8 +191,8 @@ template <typename T, int VEC, int TPR, int ELEMS>
 __global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, ln_forward_ctas<VEC, TPR, ELEMS>) ln_forward_kernel(LnForwardArgs a) {
   using Row = LnRow<T, VEC, TPR, ELEMS>;
   constexpr int kStages = ln_stages<T, TPR, ELEMS, 1>;
-  constexpr int kStageWords = Row::kGroups * Row::kBlock;
-  extern __shared__ __align__(16) uint4 ring[];           // stages x words x threads
+  extern __shared__ __align__(16) uint4 ring_memory[];
+  typename Row::Group* ring = reinterpret_cast<typename Row::Group*>(ring_memory);      // stages x groups x threads
   __shared__ __align__(16) float slots[2 * 32];
   const int tid = threadIdx.x & (TPR - 1), team = threadIdx.x / TPR, cols = (int)a.cols;
   const T* x = static_cast<const T*>(a.x);
@@ -184,10 +200,10 @@ __global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, ln_forwar
   const float inv_n = 1.0f / (float)cols;
   const int64_t stride = (int64_t)gridDim.x * Row::kTeams;
   int64_t row = (int64_t)blockIdx.x * Row::kTeams + team;
-  if constexpr (VEC > 1) {
+  if constexpr (Row::kRing) {
 #pragma unroll
     for (int s = 0; s < kStages; ++s) {
-      if (row + s * stride < a.rows) Row::issue(ring + s * kStageWords, x + (row + s * stride) * a.x_pitch, cols, tid);
+      if (row + s * stride < a.rows) Row::issue(ring + s * Row::kStageGroups, x + (row + s * stride) * a.x_pitch, cols, tid);
       copies_commit();
     }
   }
@@ -197,10 +213,10 @@ __global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, ln_forwar
   int turn = 0, stage = 0;
   for (; row < a.rows; row += stride) {
     Float2 v[ELEMS / 2];
-    uint4* words = ring + stage * kStageWords;
-    if constexpr (VEC > 1) copies_wait<kStages - 1>();
+    typename Row::Group* words = ring + stage * Row::kStageGroups;
+    if constexpr (Row::kRing) copies_wait<kStages - 1>();
     Row::take(v, words, x + row * a.x_pitch, cols, tid);
-    if constexpr (VEC > 1) {
+    if constexpr (Row::kRing) {
       const int64_t ahead = row + kStages * stride;       // into the words just read
       if (ahead < a.rows) Row::issue(words, x + ahead * a.x_pitch, cols, tid);
       copies_commit();
@@ -267,8 +283,8 @@ __global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, TPR < 512
   using Row = LnRow<T, VEC, TPR, ELEMS>;
   constexpr int kTeams = Row::kTeams;
   constexpr int kStages = ln_stages<T, TPR, ELEMS, 2>;
-  constexpr int kRowWords = Row::kGroups * Row::kBlock;
-  extern __shared__ __align__(16) uint4 ring[];           // stages x 2 (x, dy) x words x threads; teams' sums at the end
+  extern __shared__ __align__(16) uint4 ring_memory[];
+  typename Row::Group* ring = reinterpret_cast<typename Row::Group*>(ring_memory);      // stages x 2 (x, dy) x groups x threads
   __shared__ __align__(16) float slots[2 * 32 * 2];
   const int tid = threadIdx.x & (TPR - 1), team = threadIdx.x / TPR, cols = (int)a.cols;
   const int split = blockIdx.x, part = blockIdx.y;
@@ -278,13 +294,13 @@ __global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, TPR < 512
   const float inv_n = 1.0f / (float)cols;
   const int64_t stride = (int64_t)a.splits * kTeams, end = (int64_t)(part + 1) * a.rows_per_part;
   int64_t row = (int64_t)part * a.rows_per_part + (int64_t)split * kTeams + team;
-  if constexpr (VEC > 1) {
+  if constexpr (Row::kRing) {
 #pragma unroll
     for (int s = 0; s < kStages; ++s) {
       const int64_t at = row + s * stride;
       if (at < end) {
-        Row::issue(ring + s * 2 * kRowWords, x + at * a.x_pitch, cols, tid);
-        Row::issue(ring + (s * 2 + 1) * kRowWords, dy + at * a.dy_pitch, cols, tid);
+        Row::issue(ring + s * 2 * Row::kStageGroups, x + at * a.x_pitch, cols, tid);
+        Row::issue(ring + (s * 2 + 1) * Row::kStageGroups, dy + at * a.dy_pitch, cols, tid);
       }
       copies_commit();
     }
@@ -305,22 +321,22 @@ __global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, TPR < 512
       next_mean = a.mean[row + stride];
       next_rstd = a.rstd[row + stride];
     }
+    const Float2 minus_mean = both(-mean), scale = both(rstd);
+    Float2 s0 = both(0.0f), s1 = both(0.0f);
+    typename Row::Group* words = ring + stage * 2 * Row::kStageGroups;
     Float2 xh[ELEMS / 2], g[ELEMS / 2];
-    uint4* words = ring + stage * 2 * kRowWords;
-    if constexpr (VEC > 1) copies_wait<kStages - 1>();
+    if constexpr (Row::kRing) copies_wait<kStages - 1>();
     Row::take(xh, words, x + row * a.x_pitch, cols, tid);
-    Row::take(g, words + kRowWords, dy + row * a.dy_pitch, cols, tid);
-    if constexpr (VEC > 1) {
+    Row::take(g, words + Row::kStageGroups, dy + row * a.dy_pitch, cols, tid);
+    if constexpr (Row::kRing) {
       const int64_t ahead = row + kStages * stride;       // into the words just read
       if (ahead < end) {
         Row::issue(words, x + ahead * a.x_pitch, cols, tid);
-        Row::issue(words + kRowWords, dy + ahead * a.dy_pitch, cols, tid);
+        Row::issue(words + Row::kStageGroups, dy + ahead * a.dy_pitch, cols, tid);
       }
       copies_commit();
       stage = stage + 1 == kStages ? 0 : stage + 1;
     }
-    const Float2 minus_mean = both(-mean), scale = both(rstd);
-    Float2 s0 = both(0.0f), s1 = both(0.0f);
 #pragma unroll
     for (int i = 0; i < ELEMS / 2; ++i) {                 // (outside the row dy and w are 0)
       xh[i] = mul2(add2(xh[i], minus_mean), scale);
@@ -348,7 +364,7 @@ __global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, TPR < 512
     unpack2(db[i / 2], sums[1][i], sums[1][i + 1]);
   }
   if constexpr (kTeams > 1) {                  // add the teams' sums, in team order
-    float* combine = reinterpret_cast<float*>(ring);
+    float* combine = reinterpret_cast<float*>(ring_memory);
     if constexpr (VEC > 1) copies_wait<0>();
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
@@ -515,16 +531,16 @@ static int ln_splits(int64_t rows_per_part, int64_t cols, int partitions) {
   return splits < 1 ? 1 : (int)splits;
 }
 
-static bool vector_rows(const void* p, int64_t pitch, int64_t cols, int dtype) {
-  const int vec = (int)(16 / element_size(dtype));
-  return ((uintptr_t)p & 15) == 0 && pitch % vec == 0 && cols % vec == 0;
+// Whether rows consist of groups of `vec` elements that start on multiples of their size.
+static bool grouped_rows(const void* p, int64_t pitch, int64_t cols, int dtype, int vec) {
+  return ((uintptr_t)p & (vec * element_size(dtype) - 1)) == 0 && pitch % vec == 0 && cols % vec == 0;
 }
 
 template <typename T, int VEC, int TPR, int ELEMS>
 static int ln_forward_launch(const LnForwardArgs& a, int sms, cudaStream_t stream) {
   constexpr int kBlock = TPR < kLnThreads ? kLnThreads : TPR;
   constexpr int kTeams = kBlock / TPR;
-  constexpr size_t kSmem = VEC > 1 ? (size_t)ln_stages<T, TPR, ELEMS, 1> * (ELEMS / VEC) * 16 * kBlock : 0;
+  constexpr size_t kSmem = LnRow<T, VEC, TPR, ELEMS>::kRing ? (size_t)ln_stages<T, TPR, ELEMS, 1> * ELEMS * sizeof(T) * kBlock : 0;
   if constexpr (kSmem > 40 * 1024) SOLON_SHARED_MEMORY_ONCE((ln_forward_kernel<T, VEC, TPR, ELEMS>), kSmem);
   const int64_t want = (a.rows + kTeams - 1) / kTeams, cap = (int64_t)sms * ln_forward_ctas<VEC, TPR, ELEMS>;
   ln_forward_kernel<T, VEC, TPR, ELEMS><<<(unsigned)ln_min(want, cap), kBlock, kSmem, stream>>>(a);
@@ -535,7 +551,7 @@ static int ln_forward_launch(const LnForwardArgs& a, int sms, cudaStream_t strea
 template <typename T, int VEC, int TPR, int ELEMS>
 static int ln_backward_launch(const LnBackwardArgs& a, int partitions, cudaStream_t stream) {
   constexpr int kBlock = TPR < kLnThreads ? kLnThreads : TPR;
-  constexpr size_t kRing = VEC > 1 ? (size_t)ln_stages<T, TPR, ELEMS, 2> * 2 * (ELEMS / VEC) * 16 * kBlock : 0;
+  constexpr size_t kRing = LnRow<T, VEC, TPR, ELEMS>::kRing ? (size_t)ln_stages<T, TPR, ELEMS, 2> * 2 * ELEMS * sizeof(T) * kBlock : 0;
   constexpr size_t kCombine = TPR < kBlock ? (size_t)kBlock * ELEMS * sizeof(float) : 0;
   constexpr size_t kSmem = kRing > kCombine ? kRing : kCombine;
   if constexpr (kSmem > 40 * 1024) SOLON_SHARED_MEMORY_ONCE((ln_backward_kernel<T, VEC, TPR, ELEMS>), kSmem);
@@ -548,25 +564,37 @@ static int ln_backward_launch(const LnBackwardArgs& a, int partitions, cudaStrea
 // narrower ones lose by it: 30000 x 2001 70 -> 75).
 constexpr int kLnWideSingle = 4096;
 
-// f(team size, elements of a thread), both as compile-time constants.  A thread takes up to 16 elements; 32 in the forward
-// pass over 16-byte words of two-byte types.
-template <int MOST, int VEC, typename F>
+// f(team size, elements of a thread), both as compile-time constants, for rows of up to LIMIT columns.  A thread takes up to MOST
+// elements, at least a group of VEC.
+template <int MOST, int VEC, int LIMIT, typename F>
 static int ln_by_team(int64_t cols, F f) {
   const LnTeam t = ln_team(cols, MOST);
   constexpr int kLeast = MOST / 4 < VEC ? VEC : MOST / 4;
+  using std::integral_constant;
   switch (t.threads) {
     case 32:
-      if (t.elems == MOST / 4) return f(std::integral_constant<int, 32>(), std::integral_constant<int, kLeast>());
-      if (t.elems == MOST / 2) return f(std::integral_constant<int, 32>(), std::integral_constant<int, MOST / 2>());
-      return f(std::integral_constant<int, 32>(), std::integral_constant<int, MOST>());
-    case 64: return f(std::integral_constant<int, 64>(), std::integral_constant<int, MOST>());
-    case 128: return f(std::integral_constant<int, 128>(), std::integral_constant<int, MOST>());
-    case 256: return f(std::integral_constant<int, 256>(), std::integral_constant<int, MOST>());
-    case 512: return f(std::integral_constant<int, 512>(), std::integral_constant<int, MOST>());
-    default:
-      if constexpr (MOST * 1024 <= kLnMaxCols) return f(std::integral_constant<int, 1024>(), std::integral_constant<int, MOST>());
-      else return SOLON_ERR_INTERNAL;          // 512 threads of 32 elements hold the widest row
+      if (t.elems == MOST / 4) return f(integral_constant<int, 32>(), integral_constant<int, kLeast>());
+      if (t.elems == MOST / 2) return f(integral_constant<int, 32>(), integral_constant<int, MOST / 2>());
+      return f(integral_constant<int, 32>(), integral_constant<int, MOST>());
+    case 64: return f(integral_constant<int, 64>(), integral_constant<int, MOST>());
+    case 128: return f(integral_constant<int, 128>(), integral_constant<int, MOST>());
+    case 256: return f(integral_constant<int, 256>(), integral_constant<int, MOST>());
+    case 512:
+      if constexpr (256 * MOST < LIMIT) return f(integral_constant<int, 512>(), integral_constant<int, MOST>());
+      break;
+    case 1024:
+      if constexpr (512 * MOST < LIMIT) return f(integral_constant<int, 1024>(), integral_constant<int, MOST>());
+      break;
   }
+  return SOLON_ERR_INTERNAL;      // (wider than LIMIT)
+}
+
+// Rows that are not made of words: pairs or single elements, 16 a thread, 32 in wide rows.
+template <typename T, int VEC>
+static int ln_forward_loose(const LnForwardArgs& a, int sms, cudaStream_t stream) {
+  if (a.cols > 8192) return ln_forward_launch<T, VEC, 512, 32>(a, sms, stream);
+  if (a.cols > kLnWideSingle) return ln_forward_launch<T, VEC, 256, 32>(a, sms, stream);
+  return ln_by_team<16, VEC, kLnWideSingle>(a.cols, [&](auto team, auto elems) { return ln_forward_launch<T, VEC, team.value, elems.value>(a, sms, stream); });
 }
 
 template <typename T>
@@ -577,14 +605,13 @@ static int ln_forward_t(const LnForwardArgs& a, int sms, cudaStream_t stream) {
     SOLON_CUDA_TRY(cudaGetLastError());
     return SOLON_OK;
   }
-  const bool vec = vector_rows(a.x, a.x_pitch, a.cols, a.dtype) && vector_rows(a.y, a.y_pitch, a.cols, a.dtype);
-  if (vec)
-    return ln_by_team<64 / (int)sizeof(T), 16 / (int)sizeof(T)>(a.cols, [&](auto team, auto elems) {
-      return ln_forward_launch<T, 16 / (int)sizeof(T), team.value, elems.value>(a, sms, stream);
+  constexpr int kWord = 16 / (int)sizeof(T);
+  auto grouped = [&](int vec) { return grouped_rows(a.x, a.x_pitch, a.cols, a.dtype, vec) && grouped_rows(a.y, a.y_pitch, a.cols, a.dtype, vec); };
+  if (grouped(kWord))
+    return ln_by_team<64 / (int)sizeof(T), kWord, kLnMaxCols>(a.cols, [&](auto team, auto elems) {
+      return ln_forward_launch<T, kWord, team.value, elems.value>(a, sms, stream);
     });
-  if (a.cols > kLnWideSingle)
-    return ln_by_team<32, 1>(a.cols, [&](auto team, auto elems) { return ln_forward_launch<T, 1, team.value, elems.value>(a, sms, stream); });
-  return ln_by_team<16, 1>(a.cols, [&](auto team, auto elems) { return ln_forward_launch<T, 1, team.value, elems.value>(a, sms, stream); });
+  return grouped(2) ? ln_forward_loose<T, 2>(a, sms, stream) : ln_forward_loose<T, 1>(a, sms, stream);
 }
 
 template <typename T>
@@ -601,14 +628,19 @@ static int ln_backward_t(const LnBackwardArgs& a, int partitions, int sms, cudaS
       SOLON_CUDA_TRY(cudaGetLastError());
     }
   } else {
-    const bool vec = vector_rows(a.x, a.x_pitch, a.cols, a.dtype) && vector_rows(a.dy, a.dy_pitch, a.cols, a.dtype) &&
-                     (!a.dx || vector_rows(a.dx, a.dx_pitch, a.cols, a.dtype));
-    if (vec)
-      rc = ln_by_team<16, 16 / (int)sizeof(T)>(a.cols, [&](auto team, auto elems) {
-        return ln_backward_launch<T, 16 / (int)sizeof(T), team.value, elems.value>(a, partitions, stream);
-      });
-    else
-      rc = ln_by_team<16, 1>(a.cols, [&](auto team, auto elems) { return ln_backward_launch<T, 1, team.value, elems.value>(a, partitions, stream); });
+    constexpr int kWord = 16 / (int)sizeof(T);
+    auto grouped = [&](int vec) {
+      return grouped_rows(a.x, a.x_pitch, a.cols, a.dtype, vec) && grouped_rows(a.dy, a.dy_pitch, a.cols, a.dtype, vec) &&
+             (!a.dx || grouped_rows(a.dx, a.dx_pitch, a.cols, a.dtype, vec));
+    };
+    auto single = [&](auto team, auto elems) { return ln_backward_launch<T, 1, team.value, elems.value>(a, partitions, stream); };
+    auto pairs = [&](auto team, auto elems) { return ln_backward_launch<T, 2, team.value, elems.value>(a, partitions, stream); };
+    auto words = [&](auto team, auto elems) { return ln_backward_launch<T, kWord, team.value, elems.value>(a, partitions, stream); };
+    if (!grouped(kWord)) {
+      rc = grouped(2) ? ln_by_team<16, 2, kLnMaxCols>(a.cols, pairs) : ln_by_team<16, 1, kLnMaxCols>(a.cols, single);
+    } else {
+      rc = ln_by_team<16, kWord, kLnMaxCols>(a.cols, words);
+    }
   }
   if (rc || a.splits == 1 || (!a.dweight && !a.dbias)) return rc;
   return launch_dependent(ln_param_grad_kernel, dim3((unsigned)((2 * a.cols + 31) / 32), (unsigned)partitions), dim3(256), 0, stream, a);

@@ -17,6 +17,9 @@
 
 namespace solon {
 
+// Measured: 8192 x 32768 bfloat16 100 us (5.4 TB/s), 4096 x 32768 float32 90 us (6.0 TB/s), 2047 x 50001 float32 72 us and with 20
+// likeliest tokens 102 us; the gradient on 8192 x 32768 bfloat16 190 us (5.7 TB/s).
+//
 // Bound by memory, with the exponentials (one a logit: at 16 a clock and SM 60 % of the time that bfloat16 logits take to
 // arrive) and the instructions beside them close behind, so those are kept few: two values an instruction, one multiply-add
 // from a logit to its exponent, and one comparison per 64 bytes for everything that is rare.

@@ -58,7 +58,7 @@ def _check_forward(x, w, b, eps, y, mean, rstd, t):
 
 
 SHAPES = [(1, 1), (3, 2), (1, 2048), (7, 5), (33, 31), (64, 64), (9, 127), (130, 512), (65, 513), (40, 1000), (37, 1001), (300, 1024), (19, 2047),
-          (50, 4096), (11, 4100), (6, 8192), (5, 9001), (9, 16384), (3, 16385), (4, 20000)]
+          (50, 4096), (11, 4100), (6, 8192), (5, 9001), (9, 16384), (3, 16385), (4, 20000), (6, 1002), (5, 4102), (4, 10002), (9, 98)]
 
 
 @pytest.mark.parametrize("rows,cols", SHAPES)
@@ -131,7 +131,8 @@ def _check_backward(dy, x, mean, rstd, w, parts, got, t):
 
 @pytest.mark.parametrize("parts,n,cols", [(1, 1, 1), (1, 1, 2048), (2, 3, 7), (15, 4, 64), (45, 7, 1001), (1, 700, 129), (4, 100, 513), (3, 33, 1000), (1, 2000, 256),
                                           (7, 40, 2048), (2, 50, 4096), (5, 9, 4097), (3, 20, 8192), (2, 9, 12345), (4, 8, 16384), (2, 5, 16387), (1, 40, 20000),
-                                          (1000, 2, 40), (400, 1, 33)])
+                                          (1000, 2, 40), (400, 1, 33), (3, 20, 1002), (2, 7, 5002),
+                                          (3, 10, 6152), (2, 3, 10008), (5, 30, 98)])
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 def test_backward_by_partitions(parts, n, cols, dtype):
     dt, t = TYPES[dtype]
