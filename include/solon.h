@@ -354,7 +354,8 @@ int solon_token_logprobs(const void* logits, int64_t pitch, int dtype, const int
  *   peak, log_sum, entropy   device, rows float32: the forward's (entropy may be NULL without grad_entropy)
  *   grad_logp, grad_entropy  device, rows float32 (NULL: 0; grad_logp needs targets)
  *   dlogits                  device, rows x vocab of `dtype` (output); may be the logits, with their pitch
- * Rows with peak = -infinity, and rows whose two factors are 0 (a row without target has grad_logp 0), get gradients of 0. */
+ * Probabilities below 2^-126 count as 0.  Rows with peak = -infinity, and rows whose two factors are 0 (a row without target has
+ * grad_logp 0), get gradients of 0. */
 int solon_token_logprobs_backward(const void* logits, int64_t pitch, int dtype, const int64_t* targets, int64_t rows, int64_t vocab, const float* peak,
                                   const float* log_sum, const float* entropy, const float* grad_logp, const float* grad_entropy, void* dlogits, int64_t dlogits_pitch,
                                   void* cuda_stream);

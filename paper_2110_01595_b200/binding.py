@@ -239,8 +239,14 @@ def _matrix(t, name: str, like=None):
     return t.data_ptr(), pitch if rows > 1 else cols
 
 
+def _empty_matrix(like):
+    import torch
+
+    return torch.empty_like(like) if like.is_contiguous() else like.new_empty(like.shape)
+
+
 def _vector(t, name: str, n: int, dtype, device) -> int:
-    if t.dim() != 1 or t.shape[0] != n or t.dtype != dtype or t.device != device or not t.is_contiguous():
+    if t.dim() != 1 or t.numel() != n or t.dtype != dtype or t.device != device or not t.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous vector of {n} {dtype} on {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
     return t.data_ptr()
 
@@ -265,16 +271,16 @@ def solon_layernorm_forward(x, weight=None, bias=None, eps: float = 1e-5, y=None
     device, f32 = x.device, torch.float32
     stream = _current_stream(device)
     if y is None:
-        y = x.new_empty((rows, cols))
+        y = _empty_matrix(x)
         py, y_pitch = y.data_ptr(), cols
     else:
         py, y_pitch = _matrix(y, "y", x)
     if mean is None and rstd is None:
-        mean, rstd = x.new_empty((2, rows), dtype=f32).unbind(0)
+        mean, rstd = x.new_empty(rows, dtype=f32), x.new_empty(rows, dtype=f32)
         pm, pr = mean.data_ptr(), rstd.data_ptr()
     else:
-        mean = x.new_empty((rows,), dtype=f32) if mean is None else mean
-        rstd = x.new_empty((rows,), dtype=f32) if rstd is None else rstd
+        mean = x.new_empty(rows, dtype=f32) if mean is None else mean
+        rstd = x.new_empty(rows, dtype=f32) if rstd is None else rstd
         pm, pr = _vector(mean, "mean", rows, f32, device), _vector(rstd, "rstd", rows, f32, device)
     pw, pb, code = _params(weight, bias, cols, x)
     _check(lib().solon_layernorm_forward(px, x_pitch, _dtype_code(x.dtype), pw, pb, code, rows, cols, eps, py, y_pitch, pm, pr, stream),
@@ -299,7 +305,7 @@ def solon_layernorm_backward(dy, x, mean, rstd, weight=None, partitions: int = 1
     pdy, dy_pitch = _matrix(dy, "dy", x)
     stream = _current_stream(device)
     if dx is None:
-        dx = x.new_empty((rows, cols))
+        dx = _empty_matrix(x)
         pdx, dx_pitch = dx.data_ptr(), cols
     else:
         pdx, dx_pitch = _matrix(dx, "dx", x)
@@ -323,7 +329,7 @@ def solon_layernorm_backward(dy, x, mean, rstd, weight=None, partitions: int = 1
         grad_code = _dtype_code(dweight.dtype)
         n_bytes = _layernorm_workspace(rows, cols, partitions)
         if n_bytes > 0:
-            workspace = x.new_empty((n_bytes // 4,), dtype=f32)
+            workspace = x.new_empty(n_bytes // 4, dtype=f32)
     _check(lib().solon_layernorm_backward(pdy, dy_pitch, px, x_pitch, _dtype_code(x.dtype), pw, code, _vector(mean, "mean", rows, f32, device),
                                           _vector(rstd, "rstd", rows, f32, device), rows, cols, partitions, pdx, dx_pitch, pdw, pdb, grad_pitch,
                                           grad_code, None if workspace is None else workspace.data_ptr(), n_bytes, stream),
@@ -351,10 +357,11 @@ def solon_token_logprobs(logits, targets=None, top_k: int = 0) -> TokenLogprobs:
     rows, vocab = logits.shape
     device = logits.device
     stream = _current_stream(device)
-    stats = logits.new_empty((4, rows), dtype=torch.float32)
+    f32 = torch.float32
+    stats = logits.new_empty((4, rows), dtype=f32)
     base, row_bytes = stats.data_ptr(), 4 * rows
     top_ids = logits.new_empty((rows, top_k), dtype=torch.int64) if top_k > 0 else None
-    top_logp = logits.new_empty((rows, top_k), dtype=torch.float32) if top_k > 0 else None
+    top_logp = logits.new_empty((rows, top_k), dtype=f32) if top_k > 0 else None
     _check(lib().solon_token_logprobs(pz, pitch, _dtype_code(logits.dtype),
                                       None if targets is None else _vector(targets, "targets", rows, torch.int64, device), rows, vocab, top_k,
                                       None if targets is None else base, base + row_bytes, base + 2 * row_bytes, base + 3 * row_bytes,
@@ -374,7 +381,7 @@ def solon_token_logprobs_backward(logits, targets, peak, log_sum, grad_logp=None
     device = logits.device
     stream = _current_stream(device)
     if out is None:
-        out = logits.new_empty((rows, vocab))
+        out = _empty_matrix(logits)
         po, out_pitch = out.data_ptr(), vocab
     else:
         po, out_pitch = _matrix(out, "out", logits)

@@ -8,7 +8,8 @@
 //
 // Edge cases, the same in both directions: a logit of -infinity has p = 0 and adds nothing (0 log 0 = 0); a row of nothing
 // but -infinity has M = logp = -infinity, log S = H = 0 and gradient 0; a negative target has logp 0 and passes no
-// gradient; a target beyond the vocabulary is not read and has logp NaN; NaN and +infinity make the row's results NaN.
+// gradient; a target beyond the vocabulary is not read and has logp NaN; NaN and +infinity make the row's results NaN.  A
+// probability below 2^-126 counts as 0.
 #include <math.h>
 
 #include "elements.cuh"
