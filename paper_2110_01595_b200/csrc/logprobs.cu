@@ -19,7 +19,7 @@
 namespace solon {
 
 // Measured: 8192 x 32768 bfloat16 100 us (5.4 TB/s), 4096 x 32768 float32 90 us (6.0 TB/s), 2047 x 50001 float32 72 us and with 20
-// likeliest tokens 102 us; the gradient on 8192 x 32768 bfloat16 190 us (5.7 TB/s).
+// likeliest tokens 89 us; the gradient on 8192 x 32768 bfloat16 190 us (5.7 TB/s).
 //
 // Bound by memory, with the exponentials (one a logit: at 16 a clock and SM 60 % of the time that bfloat16 logits take to
 // arrive) and the instructions beside them close behind, so those are kept few: two values an instruction, one multiply-add
@@ -599,14 +599,18 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprob_kernel(Logpr
 // below that the warps are too few.
 // The candidates are a warp's own: filtered as above with the lanes' maxima for groups, appended by ballots, and pruned to the k
 // largest when the list is full.
-constexpr int kLpWarpCtas = 3;                 // CTAs per SM: 24 warps with 8 to 9.5 KB of shared memory each
 constexpr int kLpWarpRows = 12;                // rows per SM from which on rows go to warps
+constexpr int kLpWarpList = 256;               // candidates
 template <typename T>
 constexpr int lp_warp_words = 32 / Word16<T>::kCount;                    // words of a lane in an iteration: 32 elements
+// CTAs of eight warps on an SM.  Two suffice the plain sums of two-byte logits (8192 x 32768 bfloat16 takes 100 us with three, 91 with
+// two, 16384 x 16384 89 and 85: the last round of rows is fuller), and for likeliest tokens of float32 ones three would have to
+// share the memory of the lists (2047 x 50001 with 20: 102 us, 89 with two); float32 sums (2047 x 50001: 72 us, 77 with two) and
+// likeliest tokens of two-byte logits (8192 x 32768 with 8: 157 us, 168 with two) take three.
 template <typename T, bool TOP>
-constexpr int lp_warp_stages = sizeof(T) == 4 ? 2 : TOP ? 3 : 4;         // iterations' words in shared memory
-template <typename T>
-constexpr int lp_warp_list = sizeof(T) == 4 ? 128 : 256;                 // candidates
+constexpr int lp_warp_ctas = (sizeof(T) == 4) == TOP ? 2 : 3;
+template <typename T, bool TOP>
+constexpr int lp_warp_stages = sizeof(T) == 4 ? 2 : TOP ? 3 : 4;      // iterations' words in shared memory
 
 // A lower bound of the k-th largest of the lanes' values (order bits): exact in the upper 16 bits.
 __device__ __forceinline__ uint32_t kth_largest_bound(uint32_t mine, int k) {
@@ -620,7 +624,7 @@ __device__ __forceinline__ uint32_t kth_largest_bound(uint32_t mine, int k) {
 }
 
 template <typename T, bool TOP>
-__global__ void __launch_bounds__(kLpThreads, kLpWarpCtas) logprob_warp_kernel(LogprobArgs a) {
+__global__ void __launch_bounds__(kLpThreads, (lp_warp_ctas<T, TOP>)) logprob_warp_kernel(LogprobArgs a) {
   constexpr int kVec = Word16<T>::kCount;
   constexpr int kWords = lp_warp_words<T>;
   constexpr int kStages = lp_warp_stages<T, TOP>;
@@ -629,8 +633,8 @@ __global__ void __launch_bounds__(kLpThreads, kLpWarpCtas) logprob_warp_kernel(L
   extern __shared__ __align__(16) uint4 shared[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   uint4* ring = shared + warp * kStages * kChunk + lane;
-  unsigned long long* list = reinterpret_cast<unsigned long long*>(shared + kLpWarps * kStages * kChunk) + warp * (lp_warp_list<T> + SOLON_MAX_TOP);
-  unsigned long long* best = list + lp_warp_list<T>;
+  unsigned long long* list = reinterpret_cast<unsigned long long*>(shared + kLpWarps * kStages * kChunk) + warp * (kLpWarpList + SOLON_MAX_TOP);
+  unsigned long long* best = list + kLpWarpList;
   const int cols = (int)a.cols, k = a.top_k;
   const int64_t stride = (int64_t)gridDim.x * kLpWarps;
 
@@ -691,7 +695,7 @@ __global__ void __launch_bounds__(kLpThreads, kLpWarpCtas) logprob_warp_kernel(L
     float threshold = -INFINITY;                          // candidates are above it, or (see above) not below it
     auto append = [&](bool wanted, float v, int index) {
       const uint32_t mask = __ballot_sync(0xffffffffu, wanted);
-      if (listed + __popc(mask) > lp_warp_list<T>) {
+      if (listed + __popc(mask) > kLpWarpList) {
         select_largest(list, listed, best, k);
         if (lane < k) list[lane] = best[lane];
         listed = k;                                       // (of a full list: k of them)
@@ -915,14 +919,10 @@ static int logprob_launch_top(const LogprobArgs& a, int cluster, int sms, cudaSt
 
 template <typename T, bool TOP>
 static int logprob_launch_warps(const LogprobArgs& a, int sms, cudaStream_t stream) {
-  constexpr size_t kPerWarp = lp_warp_stages<T, TOP> * 32 * lp_warp_words<T> * 16 + (TOP ? (lp_warp_list<T> + SOLON_MAX_TOP) * 8 : 0);
+  constexpr size_t kPerWarp = lp_warp_stages<T, TOP> * 32 * lp_warp_words<T> * 16 + (TOP ? (kLpWarpList + SOLON_MAX_TOP) * 8 : 0);
   constexpr size_t kSmem = kLpWarps * kPerWarp;
   SOLON_SHARED_MEMORY_ONCE((logprob_warp_kernel<T, TOP>), kSmem);
-  // 24 warps an SM, 16 for the plain sums of two-byte logits: 8192 x 32768 bfloat16 takes 100 us with 24, 91 with 16, 16384 x
-  // 16384 89 and 85 (the last round of rows is fuller, and 16 streams a SM keep the memory as busy); float32 (4096 x 32768: 90
-  // and 90) and likeliest tokens (8192 x 32768 with 8: 157 and 168) have nothing from fewer.
-  constexpr int kCtas = !TOP && sizeof(T) == 2 ? 2 : kLpWarpCtas;
-  const int64_t resident = (int64_t)sms * kCtas;          // (a CTA may have fewer rows than warps: the SMs get equally many)
+  const int64_t resident = (int64_t)sms * lp_warp_ctas<T, TOP>;      // (a CTA may have fewer rows than warps: the SMs get equally many)
   logprob_warp_kernel<T, TOP><<<(unsigned)(a.rows < resident ? a.rows : resident), kLpThreads, kSmem, stream>>>(a);
   SOLON_CUDA_TRY(cudaGetLastError());
   return SOLON_OK;
