@@ -18,7 +18,7 @@
 
 namespace solon {
 
-// Measured: 8192 x 32768 bfloat16 100 us (5.4 TB/s), 4096 x 32768 float32 90 us (6.0 TB/s), 2047 x 50001 float32 72 us and with 20
+// Measured: 8192 x 32768 bfloat16 94 us (5.7 TB/s), 4096 x 32768 float32 90 us (6.0 TB/s), 2047 x 50001 float32 72 us and with 20
 // likeliest tokens 89 us; the gradient on 8192 x 32768 bfloat16 190 us (5.7 TB/s).
 //
 // Bound by memory, with the exponentials (one a logit: at 16 a clock and SM 60 % of the time that bfloat16 logits take to
