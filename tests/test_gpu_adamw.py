@@ -287,6 +287,21 @@ def test_guard_of_a_failed_decode():
                 opt.step(agg, plan=plan)
 
 
+def test_step_from_the_aggregate_of_a_float64_plan():
+    """The 8-byte wire format's aggregate goes into the step as it is; the same step from its float32 rounding is equal."""
+    P, d = 8, 6001
+    G = torch.randn((P, d), dtype=torch.float64, device="cuda", generator=_gen(3))
+    with binding.Plan(P, 1, 2, 4, d, seed=1, dtype="f64") as plan:
+        agg, mask = plan.decode(plan.encode(G))
+        p, q = torch.zeros(d, device="cuda"), torch.zeros(d, device="cuda")
+        a, b = binding.AdamW([p[:5], p[5:]], bits=8), binding.AdamW([q[:5], q[5:]], bits=8)
+        a.step(agg, lr=1e-2, grad_scale=1 / P, plan=plan)
+        b.step(agg.float(), lr=1e-2, grad_scale=1 / P, plan=plan)
+        assert plan.decode_status() == 0 and not mask.any()
+        assert torch.equal(p, q) and all(torch.equal(x, y) for x, y in zip(a.state, b.state))
+        assert float((a.of_tensor(a.moments()[0], 1).float() - 0.1 * G.mean(0)[5:].float()).abs().max()) <= 0.13 * 0.1 * float(G.mean(0).abs().max())
+
+
 def test_replayed_graph_counts_its_steps():
     for bits in (32, 8):
         flat, views, grad = _setup(SIZES, 7)
