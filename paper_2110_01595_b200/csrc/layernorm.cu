@@ -7,7 +7,7 @@
 //
 // Bound by memory: 2 (forward) and 3 (backward) accesses of the matrix against about 8 and 14 flops an element.  Measured:
 // forward 16384 x 4096 bfloat16 48 us (5.6 TB/s), float32 96 us (5.6 TB/s); backward 15 x 2048 rows of 2048 bfloat16 68 us
-// (5.6 TB/s) and 7 us for the partial sums, 16384 x 4096 float32 143 us (5.6 TB/s).  What keeps it from the copy rate is 16 warps
+// (5.6 TB/s) with 3.5 us for the partial sums, 16384 x 4096 float32 143 us (5.6 TB/s).  What keeps it from the copy rate is 16 warps
 // an SM (the registers of a column's parameters and sums), each with a barrier or two a row.
 //
 // Layout: a row belongs to a team of TPR threads that hold 16 or 32 elements each (fewer in short rows), so that a team's
@@ -55,6 +55,15 @@ __device__ __forceinline__ void team_sum(float (&v)[N], float* slots, int& turn,
       for (int k = 0; k < N; ++k) s[k * kWarps + warp] = v[k];
     }
     asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "n"(TPR) : "memory");
+    if constexpr (kWarps == 32) {              // a lane a warp's sum: 32 warps that each read 32 sums would queue for shared memory
+#pragma unroll
+      for (int k = 0; k < N; ++k) v[k] = s[k * kWarps + (threadIdx.x & 31)];
+#pragma unroll
+      for (int off = 16; off > 0; off >>= 1)
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], off);
+      return;
+    }
     constexpr int kRead = kWarps < 4 ? kWarps : 4;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
@@ -277,6 +286,37 @@ __device__ __forceinline__ void store_grad(void* p, int f64, int64_t i, float v)
   else static_cast<float*>(p)[i] = v;
 }
 
+// A team's sums for weight and bias: the partition's gradient, or a partial sum where several CTAs share the partition.
+template <typename Row, int VEC, int ELEMS>
+__device__ __forceinline__ void put_param_sums(const LnBackwardArgs& a, const float (&sums)[2][ELEMS], int part, int split, int tid) {
+  const int cols = (int)a.cols;
+  if (a.splits > 1) {
+    constexpr int kStore = VEC < 4 ? VEC : 4;  // a row of groups of VEC elements is a row of groups of kStore
+    float* out = a.partials + ((int64_t)part * a.splits + split) * 2 * a.cols;
+#pragma unroll
+    for (int i = 0; i < ELEMS; i += kStore) {
+      const int c = Row::column(i / VEC, tid) + i % VEC;
+      if (c >= cols) continue;
+#pragma unroll
+      for (int which = 0; which < 2; ++which) {
+        float* to = out + which * cols + c;
+        const float* v = &sums[which][i];
+        if constexpr (kStore == 4) *reinterpret_cast<float4*>(to) = make_float4(v[0], v[1], v[2], v[3]);
+        else if constexpr (kStore == 2) *reinterpret_cast<float2*>(to) = make_float2(v[0], v[1]);
+        else *to = *v;
+      }
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < ELEMS; ++i) {
+    const int c = Row::column(i / VEC, tid) + i % VEC;
+    if (c >= cols) continue;
+    if (a.dweight) store_grad(a.dweight, a.grad_f64, part * a.grad_pitch + c, sums[0][i]);
+    if (a.dbias) store_grad(a.dbias, a.grad_f64, part * a.grad_pitch + c, sums[1][i]);
+  }
+}
+
 // CTA (split, partition): rows split * teams + team, stepping by splits * teams, of its partition.
 template <typename T, int VEC, int TPR, int ELEMS>
 __global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, TPR < 512 ? 2 : 1) ln_backward_kernel(LnBackwardArgs a) {
@@ -380,42 +420,157 @@ __global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, TPR < 512
     }
     if (team != 0) return;
   }
-  float* out = a.splits > 1 ? a.partials + ((int64_t)part * a.splits + split) * 2 * a.cols : nullptr;
-#pragma unroll
-  for (int i = 0; i < ELEMS; ++i) {
-    const int c = Row::column(i / VEC, tid) + i % VEC;
-    if (c >= cols) continue;
-    if (out) {
-      out[c] = sums[0][i];
-      out[cols + c] = sums[1][i];
-    } else {
-      if (a.dweight) store_grad(a.dweight, a.grad_f64, part * a.grad_pitch + c, sums[0][i]);
-      if (a.dbias) store_grad(a.dbias, a.grad_f64, part * a.grad_pitch + c, sums[1][i]);
-    }
-  }
+  put_param_sums<Row, VEC, ELEMS>(a, sums, part, split, tid);
 }
 
-// Sums of the CTAs' partial sums: 32 columns a CTA (lanes), the splits dealt to 8 warps and added up in order.
-__global__ void __launch_bounds__(256) ln_param_grad_kernel(LnBackwardArgs a) {
-  __shared__ float part_s[8][33];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = blockIdx.y;
-  const int64_t c2 = (int64_t)blockIdx.x * 32 + lane;                 // 0 .. cols - 1: weight, then bias
-  pdl_wait();
-  const float* src = a.partials + (int64_t)part * a.splits * 2 * a.cols + c2;
-  float sum = 0.0f;
-  if (c2 < 2 * a.cols) {
-#pragma unroll 4
-    for (int s = warp; s < a.splits; s += 8) sum += src[(int64_t)s * 2 * a.cols];
-  }
-  part_s[warp][lane] = sum;
-  __syncthreads();
-  if (warp != 0 || c2 >= 2 * a.cols) return;
-  sum = 0.0f;
+// Rows of 8193 .. 16384 elements: a row a CTA of 1024 threads, whose 64 registers hold the sums of 16 columns but not the row and
+// the weight beside them.  So the weight sits in shared memory, and the row is taken from the ring twice: for the sums, and
+// again, piece by piece, for dx; each piece of the ring is refilled as soon as it has been taken for the second time.
+// (15 x 64 rows of 12000 bfloat16 with all of it in registers, which spilled 312 bytes a thread: 49 us; so: 30 to 32.)
+template <typename T>
+constexpr int ln_broad_stages = sizeof(T) == 2 ? 2 : 1;      // 64 KB of weights and 64 or 128 KB a stage
+template <typename T, int VEC>
+__global__ void __launch_bounds__(1024) ln_backward_broad_kernel(LnBackwardArgs a) {
+  constexpr int kTeam = 1024, kElems = 16, kPiece = VEC == 1 ? 2 : VEC, kPieces = kElems / kPiece, kSpan = kPiece * kTeam;
+  constexpr int kStages = ln_broad_stages<T>;
+  using Row = LnRow<T, VEC, kTeam, kElems>;
+  using Piece = LnRow<T, VEC, kTeam, kPiece>;                // piece k: the row's columns from k * kSpan on
+  extern __shared__ __align__(16) uint4 ring_memory[];
+  Float2* weights = reinterpret_cast<Float2*>(ring_memory);                             // [kElems / 2][threads]
+  typename Row::Group* ring = reinterpret_cast<typename Row::Group*>(weights + kElems / 2 * kTeam);
+  __shared__ __align__(16) float slots[2 * 32 * 2];
+  const int tid = threadIdx.x, cols = (int)a.cols, split = blockIdx.x, part = blockIdx.y;
+  const T* x = static_cast<const T*>(a.x);
+  const T* dy = static_cast<const T*>(a.dy);
+  T* dx = static_cast<T*>(a.dx);
+  const float inv_n = 1.0f / (float)cols;
+  const int64_t end = (int64_t)(part + 1) * a.rows_per_part;
+  int64_t row = (int64_t)part * a.rows_per_part + split;
+  auto issue = [&](int stage, int k, int64_t at) {
+    typename Row::Group* words = ring + stage * 2 * Row::kStageGroups + k * Piece::kStageGroups;
+    const int from = k * kSpan < cols ? k * kSpan : 0, left = cols - k * kSpan;
+    Piece::issue(words, x + at * a.x_pitch + from, left, tid);
+    Piece::issue(words + Row::kStageGroups, dy + at * a.dy_pitch + from, left, tid);
+  };
+  if constexpr (Row::kRing) {
 #pragma unroll
-  for (int w = 0; w < 8; ++w) sum += part_s[w][lane];
-  const int64_t c = c2 < a.cols ? c2 : c2 - a.cols;
-  void* dst = c2 < a.cols ? a.dweight : a.dbias;
-  if (dst) store_grad(dst, a.grad_f64, part * a.grad_pitch + c, sum);
+    for (int s = 0; s < kStages; ++s) {
+      const int64_t at = row + (int64_t)s * a.splits;
+      if (at < end) {
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) issue(s, k, at);
+      }
+      copies_commit();
+    }
+  }
+  {
+    Float2 w[kElems / 2];
+    Row::params(w, a.weight, a.param_f32, a.dtype, 1.0f, cols, tid);
+#pragma unroll
+    for (int i = 0; i < kElems / 2; ++i) weights[i * kTeam + tid] = w[i];               // read by this thread only
+  }
+  Float2 dw[kElems / 2], db[kElems / 2];
+#pragma unroll
+  for (int i = 0; i < kElems / 2; ++i) dw[i] = db[i] = both(0.0f);
+  int turn = 0, stage = 0;
+  for (; row < end; row += a.splits) {
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    const Float2 minus_mean = both(-mean), scale = both(rstd);
+    Float2 s0 = both(0.0f), s1 = both(0.0f);
+    const typename Row::Group* words = ring + stage * 2 * Row::kStageGroups;
+    const T* x_row = x + row * a.x_pitch;
+    const T* dy_row = dy + row * a.dy_pitch;
+    if constexpr (Row::kRing) copies_wait<kStages - 1>();
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k) {
+      Float2 xh[kPiece / 2], g[kPiece / 2];
+      Piece::take(xh, words + k * Piece::kStageGroups, x_row + k * kSpan, cols - k * kSpan, tid);
+      Piece::take(g, words + Row::kStageGroups + k * Piece::kStageGroups, dy_row + k * kSpan, cols - k * kSpan, tid);
+#pragma unroll
+      for (int i = 0; i < kPiece / 2; ++i) {
+        const int e = k * kPiece / 2 + i;
+        xh[i] = mul2(add2(xh[i], minus_mean), scale);
+        dw[e] = fma2(g[i], xh[i], dw[e]);
+        db[e] = add2(db[e], g[i]);
+        g[i] = mul2(g[i], weights[e * kTeam + tid]);
+        s0 = add2(s0, g[i]);
+        s1 = fma2(g[i], xh[i], s1);
+      }
+    }
+    float s[2] = {sum_of(s0), sum_of(s1)};
+    if (dx) team_sum<kTeam>(s, slots, turn, 0);
+    const Float2 minus_m0 = both(-s[0] * inv_n), minus_m1 = both(-s[1] * inv_n);
+    const int64_t ahead = row + (int64_t)kStages * a.splits;
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k) {
+      if (dx) {
+        Float2 xh[kPiece / 2], g[kPiece / 2];
+        Piece::take(xh, words + k * Piece::kStageGroups, x_row + k * kSpan, cols - k * kSpan, tid);
+        Piece::take(g, words + Row::kStageGroups + k * Piece::kStageGroups, dy_row + k * kSpan, cols - k * kSpan, tid);
+#pragma unroll
+        for (int i = 0; i < kPiece / 2; ++i) {
+          xh[i] = mul2(add2(xh[i], minus_mean), scale);
+          g[i] = mul2(g[i], weights[(k * kPiece / 2 + i) * kTeam + tid]);
+          g[i] = mul2(fma2(xh[i], minus_m1, add2(g[i], minus_m0)), scale);
+        }
+        Piece::store(dx + row * a.dx_pitch + k * kSpan, g, cols - k * kSpan, tid);
+      }
+      if constexpr (Row::kRing) {
+        if (ahead < end) issue(stage, k, ahead);
+      }
+    }
+    if constexpr (Row::kRing) {
+      copies_commit();
+      stage = stage + 1 == kStages ? 0 : stage + 1;
+    }
+  }
+  pdl_trigger();
+  if (!a.dweight && !a.dbias) return;
+  float sums[2][kElems];
+#pragma unroll
+  for (int i = 0; i < kElems; i += 2) {
+    unpack2(dw[i / 2], sums[0][i], sums[0][i + 1]);
+    unpack2(db[i / 2], sums[1][i], sums[1][i + 1]);
+  }
+  put_param_sums<Row, VEC, kElems>(a, sums, part, split, tid);
+}
+
+// Sums of the CTAs' partial sums, in a fixed order: a lane takes two columns, the splits are dealt to WARPS warps.
+template <int WARPS>
+__global__ void __launch_bounds__(WARPS < 8 ? 256 : WARPS * 32) ln_param_grad_kernel(LnBackwardArgs a) {
+  const int part = blockIdx.y, warp = WARPS == 1 ? 0 : threadIdx.x >> 5;
+  const int64_t all = 2 * a.cols;                                      // 0 .. cols - 1: weight, then bias
+  const int64_t first = WARPS == 1 ? ((int64_t)blockIdx.x * 256 + threadIdx.x) * 2 : (int64_t)blockIdx.x * 64 + (threadIdx.x & 31) * 2;
+  pdl_wait();
+  float2 sum = make_float2(0.0f, 0.0f);
+  if (first < all) {
+    const float* src = a.partials + (int64_t)part * a.splits * all + first;
+#pragma unroll 4
+    for (int s = warp; s < a.splits; s += WARPS) {
+      const float2 v = *reinterpret_cast<const float2*>(src + s * all);
+      sum.x += v.x;
+      sum.y += v.y;
+    }
+  }
+  auto put = [&](int64_t c, float v) {
+    if (c >= all) return;
+    void* dst = c < a.cols ? a.dweight : a.dbias;
+    if (dst) store_grad(dst, a.grad_f64, part * a.grad_pitch + (c < a.cols ? c : c - a.cols), v);
+  };
+  if constexpr (WARPS == 1) {
+    put(first, sum.x);
+    put(first + 1, sum.y);
+  } else {
+    __shared__ float2 part_s[WARPS][32];
+    part_s[warp][threadIdx.x & 31] = sum;
+    __syncthreads();
+    if (threadIdx.x >= 64) return;
+    const float* column = reinterpret_cast<const float*>(part_s) + threadIdx.x;
+    float total = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) total += column[w * 64];
+    put((int64_t)blockIdx.x * 64 + threadIdx.x, total);
+  }
 }
 
 // ---- rows too wide for registers: one CTA a row, the row read again for every sweep (it stays in L2) ----------------------
@@ -519,13 +674,21 @@ static LnTeam ln_team(int64_t cols, int most) {
 
 static int64_t ln_min(int64_t a, int64_t b) { return a < b ? a : b; }
 
-// CTAs that share a partition's rows: as many as run at once (two per SM of 256 threads, one of more), shared by the
-// partitions - one more and the last would run alone after all others -, as long as every CTA has a row for each of its teams.
+// CTAs that share a partition's rows.  One a SM in all, as long as every team has a row; the partitions share them evenly
+// (rounded down: one more and the last CTAs would run after all others).  Two a SM where two fit (CTAs of 256 threads), if
+// that leaves 8 rows to a CTA: below, writing and adding up twice the partial sums costs more than the second CTA brings
+// (us with one and two, bfloat16: 45 x 16 rows of 4096 10.0, 11.1; 45 x 64 19.1, 18.0; 1 x 1024 10.3, 12.1).
+// Wider rows, of which a CTA takes 256 columns: sixteen a SM, with 24 rows or more (45 x 8 rows of 20000 33 us with one, 42 with two).
 constexpr int kLnSms = 148;
 static int ln_splits(int64_t rows_per_part, int64_t cols, int partitions) {
-  const int team = cols > kLnMaxCols ? 1024 : ln_team(cols, 16).threads;
+  if (cols > kLnMaxCols) {
+    const int64_t splits = ln_min(16 * kLnSms / (partitions * ((cols + 255) / 256)), rows_per_part / 24);
+    return splits < 1 ? 1 : (int)splits;
+  }
+  const int team = ln_team(cols, 16).threads;
   const int teams = team < kLnThreads ? kLnThreads / team : 1;
-  const int64_t want = 2 * kLnSms / partitions;
+  const int64_t two = 2 * kLnSms / partitions;
+  const int64_t want = team <= kLnThreads && two * 8 <= rows_per_part ? two : kLnSms / partitions;
   const int64_t most = (rows_per_part + teams - 1) / teams;
   const int64_t splits = ln_min(want, most);
   return splits < 1 ? 1 : (int)splits;
@@ -550,12 +713,18 @@ static int ln_forward_launch(const LnForwardArgs& a, int sms, cudaStream_t strea
 
 template <typename T, int VEC, int TPR, int ELEMS>
 static int ln_backward_launch(const LnBackwardArgs& a, int partitions, cudaStream_t stream) {
-  constexpr int kBlock = TPR < kLnThreads ? kLnThreads : TPR;
-  constexpr size_t kRing = LnRow<T, VEC, TPR, ELEMS>::kRing ? (size_t)ln_stages<T, TPR, ELEMS, 2> * 2 * ELEMS * sizeof(T) * kBlock : 0;
-  constexpr size_t kCombine = TPR < kBlock ? (size_t)kBlock * ELEMS * sizeof(float) : 0;
-  constexpr size_t kSmem = kRing > kCombine ? kRing : kCombine;
-  if constexpr (kSmem > 40 * 1024) SOLON_SHARED_MEMORY_ONCE((ln_backward_kernel<T, VEC, TPR, ELEMS>), kSmem);
-  ln_backward_kernel<T, VEC, TPR, ELEMS><<<dim3((unsigned)a.splits, (unsigned)partitions), kBlock, kSmem, stream>>>(a);
+  if constexpr (TPR == 1024) {
+    constexpr size_t kBytes = 1024 * ELEMS * (sizeof(float) + (VEC > 1 ? ln_broad_stages<T> * 2 * sizeof(T) : 0));
+    SOLON_SHARED_MEMORY_ONCE((ln_backward_broad_kernel<T, VEC>), kBytes);
+    ln_backward_broad_kernel<T, VEC><<<dim3((unsigned)a.splits, (unsigned)partitions), 1024, kBytes, stream>>>(a);
+  } else {
+    constexpr int kBlock = TPR < kLnThreads ? kLnThreads : TPR;
+    constexpr size_t kRing = LnRow<T, VEC, TPR, ELEMS>::kRing ? (size_t)ln_stages<T, TPR, ELEMS, 2> * 2 * ELEMS * sizeof(T) * kBlock : 0;
+    constexpr size_t kCombine = TPR < kBlock ? (size_t)kBlock * ELEMS * sizeof(float) : 0;
+    constexpr size_t kSmem = kRing > kCombine ? kRing : kCombine;
+    if constexpr (kSmem > 40 * 1024) SOLON_SHARED_MEMORY_ONCE((ln_backward_kernel<T, VEC, TPR, ELEMS>), kSmem);
+    ln_backward_kernel<T, VEC, TPR, ELEMS><<<dim3((unsigned)a.splits, (unsigned)partitions), kBlock, kSmem, stream>>>(a);
+  }
   SOLON_CUDA_TRY(cudaGetLastError());
   return SOLON_OK;
 }
@@ -643,7 +812,11 @@ static int ln_backward_t(const LnBackwardArgs& a, int partitions, int sms, cudaS
     }
   }
   if (rc || a.splits == 1 || (!a.dweight && !a.dbias)) return rc;
-  return launch_dependent(ln_param_grad_kernel, dim3((unsigned)((2 * a.cols + 31) / 32), (unsigned)partitions), dim3(256), 0, stream, a);
+  const int64_t columns = 2 * a.cols;
+  if (a.splits < 8) return launch_dependent(ln_param_grad_kernel<1>, dim3((unsigned)((columns + 511) / 512), (unsigned)partitions), dim3(256), 0, stream, a);
+  const dim3 grid((unsigned)((columns + 63) / 64), (unsigned)partitions);
+  if (a.splits < 64) return launch_dependent(ln_param_grad_kernel<8>, grid, dim3(256), 0, stream, a);
+  return launch_dependent(ln_param_grad_kernel<32>, grid, dim3(1024), 0, stream, a);
 }
 
 }  // namespace solon

@@ -173,6 +173,31 @@ def test_backward_writes_into_the_gradient_matrix(cols, grad):
         _check_backward(dy, x, mean, rstd, w, parts, got2, 2.0 ** -23)
 
 
+@pytest.mark.parametrize("parts,n,cols", [(1, 900, 8200), (1, 700, 16384), (45, 12, 8194), (2, 300, 8201), (149, 3, 9000), (1, 1, 16000), (20, 40, 8192), (50, 30, 5001),
+                                          (1, 1300, 2048), (37, 9, 770)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_backward_of_rows_that_take_turns(parts, n, cols, dtype):
+    """CTAs of one to many rows, shares of a partition that are not alike, on both sides of the widths where the kernel changes;
+    dx over dy, over x, or not wanted; no weight."""
+    dt, t = TYPES[dtype]
+    rows = parts * n
+    x, dy = _strided(_randn((rows, cols), dt, rows + cols, 1.5, -0.4), cols + 8, 0), _strided(_randn((rows, cols), dt, cols), cols + 16, 8)
+    _, mean, rstd = binding.solon_layernorm_forward(x, None)
+    got = binding.solon_layernorm_backward(dy, x, mean, rstd, None, partitions=parts)
+    _check_backward(dy, x, mean, rstd, None, parts, got, t)
+    w = _randn(cols, torch.float32, 5)
+    want = binding.solon_layernorm_backward(dy, x, mean, rstd, w, partitions=parts)
+    _check_backward(dy, x, mean, rstd, w, parts, want, t)
+    over = dy.clone()                                                                  # (dense: the same elements, other pitches)
+    dw = torch.empty((parts, cols), device="cuda")
+    got = binding.solon_layernorm_backward(over, x, mean, rstd, w, partitions=parts, dx=over, dweight=dw, dbias=torch.empty_like(dw))
+    assert got[0].data_ptr() == over.data_ptr()
+    _check_backward(dy, x, mean, rstd, w, parts, got, t)
+    over = x.clone()
+    got = binding.solon_layernorm_backward(dy, over, mean, rstd, w, partitions=parts, dx=over, param_grads=False)
+    _check_backward(dy, x, mean, rstd, w, parts, (got[0], *want[1:]), t)
+
+
 def test_backward_agrees_with_differences():
     """Directional derivatives of sum c y by central differences of the forward kernel.  h = 2^-6 along a direction of unit
     entries: the second-order error is below h^2 relative, rounding (u |y| per output, independent) below sqrt(N) u / h of the
