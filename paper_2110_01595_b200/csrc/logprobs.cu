@@ -230,7 +230,8 @@ __device__ __forceinline__ unsigned long long peer_key(uint32_t addr) {
 }
 
 // Candidates for the likeliest tokens.  A value enters unless k values at least as large, of lower index, are known: the
-// threshold is the k-th largest of the maxima of 32 groups of eight threads, taken anew whenever the part of the row that
+// threshold is the k-th largest of the maxima of groups of eight threads, or of two from k = 9 on (of the eights' 32 maxima the
+// 32nd is the smallest, with some 130 values above it, of the pairs' 128 it has 37), taken anew whenever the part of the row that
 // has been seen has doubled, with all threads at the same place of the row.  The k largest are picked from the candidates at
 // the end.  Should they overflow - ties by the thousand, as in a masked row, or a row that rises throughout -, they are
 // collected once more with the final threshold, of the values equal to it only the row's first; failing that too, the k
@@ -239,7 +240,7 @@ struct LogprobTop {
   unsigned long long key[2][kLpCandidates];      // by the parity of the row: one warp picks while the others go on
   unsigned long long best[SOLON_MAX_TOP];        // this CTA's k largest, in falling order (0: fewer)
   unsigned long long scratch[kLpWarps];
-  uint32_t group_max[2][32];                     // by the parity of the refresh
+  __align__(16) uint32_t pair_max[2][kLpThreads / 2];      // by the parity of the refresh
   uint32_t threshold;                            // order bits; 0: none yet
   int count[3];                                  // by the row modulo 3, see below
 };
@@ -268,12 +269,10 @@ __device__ __forceinline__ uint32_t candidate_bits(const uint4 (&w)[N], float th
   return bits;
 }
 
-// A thread's largest value so far (order bits, 0: it has seen nothing) to its group's.
-__device__ __forceinline__ void write_group_max(LogprobTop& top, int buffer, uint32_t seen) {
-  const int lane = threadIdx.x & 31;
-#pragma unroll
-  for (int off = 1; off < 8; off <<= 1) seen = max(seen, __shfl_xor_sync(0xffffffffu, seen, off));
-  if ((lane & 7) == 0) top.group_max[buffer][(threadIdx.x >> 5) * 4 + (lane >> 3)] = seen;
+// A thread's largest value so far (order bits, 0: it has seen nothing) to its pair's.
+__device__ __forceinline__ void write_pair_max(LogprobTop& top, int buffer, uint32_t seen) {
+  seen = max(seen, __shfl_xor_sync(0xffffffffu, seen, 1));
+  if ((threadIdx.x & 1) == 0) top.pair_max[buffer][threadIdx.x >> 1] = seen;
 }
 // The k-th largest of 32 values, one a lane, equal ones counted apart.
 __device__ __forceinline__ uint32_t kth_largest(uint32_t mine, int k) {
@@ -286,25 +285,91 @@ __device__ __forceinline__ uint32_t kth_largest(uint32_t mine, int k) {
   }
   return __shfl_sync(0xffffffffu, mine, __ffs(__ballot_sync(0xffffffffu, rank == k - 1)) - 1);
 }
-
-// The k largest of n keys (all different, beside zeros) into best, zeros behind them.  One warp.
-__device__ __forceinline__ void select_largest(const unsigned long long* keys, int n, unsigned long long* best, int k) {
-  const int lane = threadIdx.x & 31;
-  unsigned long long mine = 0;
-  for (int i = lane; i < n; i += 32) mine = max(mine, keys[i]);
-  for (int j = 0; j < k; ++j) {
-    const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(mine >> 32));
-    const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(mine >> 32) == hi ? (uint32_t)mine : 0u);
-    const unsigned long long key = ((unsigned long long)hi << 32) | lo;
-    if (lane == 0) best[j] = key;
-    if (mine == key && key != 0) {               // the lane that held it: its next
-      mine = 0;
-      for (int i = lane; i < n; i += 32) {
-        const unsigned long long q = keys[i];
-        if (q < key && q > mine) mine = q;
-      }
+// The k-th largest of 128 values, four a lane, from the bits on in which they differ: until k lie above, or all bits are known.
+__device__ __forceinline__ uint32_t kth_largest(const uint4& q, int k) {
+  const uint32_t high = __reduce_max_sync(0xffffffffu, max(max(q.x, q.y), max(q.z, q.w)));
+  const uint32_t low = __reduce_min_sync(0xffffffffu, min(min(q.x, q.y), min(q.z, q.w)));
+  if (high == low) return high;
+  const int top = 31 - __clz(high ^ low);
+  uint32_t bound = high & ~((2u << top) - 1u);
+  for (int bit = top; bit >= 0; --bit) {
+    const uint32_t trial = bound | (1u << bit);
+    const int above = (int)__reduce_add_sync(0xffffffffu, (uint32_t)((q.x >= trial) + (q.y >= trial) + (q.z >= trial) + (q.w >= trial)));
+    if (above >= k) bound = trial;
+    if (above == k) {
+      const uint32_t least = min(min(q.x >= bound ? q.x : ~0u, q.y >= bound ? q.y : ~0u), min(q.z >= bound ? q.z : ~0u, q.w >= bound ? q.w : ~0u));
+      return __reduce_min_sync(0xffffffffu, least);
     }
   }
+  return bound;
+}
+
+// Of n keys (all different, beside zeros) the k largest and some more, `most` at most, in their order; how many there are, and
+// the order bits of the smallest.  One warp.
+__device__ __noinline__ int trim_keys(unsigned long long* keys, int n, int k, int most, uint32_t* smallest) {
+  const int lane = threadIdx.x & 31;
+  uint32_t high = 0, low = ~0u;
+  for (int i = lane; i < n; i += 32) {
+    const uint32_t o = (uint32_t)(keys[i] >> 32);
+    high = max(high, o);
+    low = min(low, o);
+  }
+  high = __reduce_max_sync(0xffffffffu, high);
+  low = __reduce_min_sync(0xffffffffu, low);
+  const int top = high == low ? -1 : 31 - __clz(high ^ low);           // the highest bit in which they differ
+  unsigned long long bound = (unsigned long long)(top < 0 ? high : high & ~((2u << top) - 1u)) << 32;
+  for (int bit = top + 32; bit >= 0; --bit) {
+    const unsigned long long trial = bound | (1ull << bit);
+    uint32_t above = 0;
+#pragma unroll 4
+    for (int i = lane; i < n; i += 32) above += keys[i] >= trial;
+    above = __reduce_add_sync(0xffffffffu, above);
+    if ((int)above >= k) {
+      bound = trial;
+      if ((int)above <= most) break;
+    }
+  }
+  int kept = 0;
+  low = ~0u;
+  for (int base = 0; base < n; base += 32) {
+    const unsigned long long key = base + lane < n ? keys[base + lane] : 0;
+    const bool keep = key >= bound && key != 0;
+    const uint32_t mask = __ballot_sync(0xffffffffu, keep);
+    __syncwarp();
+    if (keep) {
+      keys[kept + __popc(mask & ((1u << lane) - 1u))] = key;
+      low = min(low, (uint32_t)(key >> 32));
+    }
+    kept += __popc(mask);
+    __syncwarp();
+  }
+  *smallest = __reduce_min_sync(0xffffffffu, low);
+  return kept;
+}
+
+// The k largest of n keys (all different, beside zeros) into best, in falling order, zeros behind them; the keys are lost.  One
+// warp: of more than 64 keys those that cannot be among them go first, then each counts the larger ones.
+__device__ __forceinline__ void select_largest(unsigned long long* keys, int n, unsigned long long* best, int k) {
+  const int lane = threadIdx.x & 31;
+  uint32_t smallest;
+  if (n > 64) n = trim_keys(keys, n, k, 64, &smallest);
+  const unsigned long long mine = lane < n ? keys[lane] : 0, second = lane + 32 < n ? keys[lane + 32] : 0;
+  int rank = 0, second_rank = 0;
+  if (n <= 32) {
+#pragma unroll 4
+    for (int j = 0; j < n; ++j) rank += keys[j] > mine;
+  } else {
+#pragma unroll 4
+    for (int j = 0; j < n; ++j) {
+      const unsigned long long other = keys[j];
+      rank += other > mine;
+      second_rank += other > second;
+    }
+  }
+  if (lane < k) best[lane] = 0;
+  __syncwarp();
+  if (mine != 0 && rank < k) best[rank] = mine;
+  if (second != 0 && second_rank < k) best[second_rank] = second;
   __syncwarp();
 }
 
@@ -485,10 +550,11 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprob_kernel(Logpr
         if (iteration == 0 || (iteration + 1 == next_refresh && base + kLpChunk < share.end)) {
           // one warp works the threshold out; the others need not wait for it but in the first stretch, which is compared
           // with its own (so values equal to it count there)
-          write_group_max(top, refresh, share.begin + (int)threadIdx.x < share.end ? order_bits(t.peak) : 0u);
+          write_pair_max(top, refresh, share.begin + (int)threadIdx.x < share.end ? order_bits(t.peak) : 0u);
           __syncthreads();
           if (warp == kLpWarps - 1) {
-            const uint32_t found = kth_largest(top.group_max[refresh][lane], a.top_k);
+            const uint4 q = reinterpret_cast<const uint4*>(top.pair_max[refresh])[lane];
+            const uint32_t found = a.top_k <= 8 ? kth_largest(max(max(q.x, q.y), max(q.z, q.w)), a.top_k) : kth_largest(q, a.top_k);
             if (lane == 0) *(volatile uint32_t*)&top.threshold = found;
           }
           refresh ^= 1;
@@ -594,12 +660,18 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprob_kernel(Logpr
 
 // ---- many rows: a warp a row -----------------------------------------------------------------------------------------
 // Nothing in a row then waits for another warp, and the serial work at a row's end (and for its likeliest tokens) of one warp
-// hides behind the others' streams.  Measured, CTA a row against warp a row: 8192 x 32768 bfloat16 107 / 91 us, with 8
-// alternatives 285 / 157; 2500 x 2000 with 8 36 / 18; the two meet at 12 rows per SM (1776 x 50000: 42 / 39, with 8 68 / 68),
-// below that the warps are too few.
-// The candidates are a warp's own: filtered as above with the lanes' maxima for groups, appended by ballots, and pruned to the k
-// largest when the list is full.
-constexpr int kLpWarpRows = 12;                // rows per SM from which on rows go to warps
+// hides behind the others' streams; but a warp alone takes its time over a row, so there have to be the more rows the longer they
+// are, up to 12 per SM.  Measured, bfloat16, CTA a row against warp a row in us: 8192 x 32768 107 / 91; 1200 x 16000 13.0 / 11.9;
+// 600 x 8000 6.4 / 6.3; 300 x 4000 4.9 / 4.5; 75 x 4000 4.0 / 4.1; 16 x 2000 3.9 / 3.5; with 8 likeliest tokens 1776 x 50000 68 / 68;
+// 1200 x 8000 17.5 / 17.1; 600 x 4000 11.3 / 10.1; 300 x 4000 7.3 / 9.4; 300 x 2000 7.2 / 6.5; 16 x 1000 6.2 / 5.1.
+// The candidates are a warp's own: filtered as above with the lanes' maxima for groups - with many to find, of the first stretch
+// the maxima of quarters, and then what is left of the list: of the 32 lanes' maxima the 32nd is the smallest -, appended by
+// ballots, and pruned to little more than k when the list is full.
+constexpr int kLpWarpRows = 12;
+static bool logprob_by_warps(int64_t rows, int64_t cols, bool top, int sms) {
+  const int64_t span = top ? 1024 : 2048;      // columns that a row may have for every row per SM; up to it any number of rows will do
+  return cols <= span || rows >= (int64_t)sms * kLpWarpRows || rows * span >= cols * sms;
+}
 constexpr int kLpWarpList = 256;               // candidates
 template <typename T>
 constexpr int lp_warp_words = 32 / Word16<T>::kCount;                    // words of a lane in an iteration: 32 elements
@@ -693,14 +765,15 @@ __global__ void __launch_bounds__(kLpThreads, (lp_warp_ctas<T, TOP>)) logprob_wa
     t.init();
     int listed = 0, next_refresh = 1, iteration = 0;
     float threshold = -INFINITY;                          // candidates are above it, or (see above) not below it
+    auto prune = [&]() {                                  // to the k largest and a half as many again
+      uint32_t smallest;
+      listed = trim_keys(list, listed, k, k + (k >> 1), &smallest);
+      threshold = fmaxf(threshold, order_value(smallest));
+    };
     auto append = [&](bool wanted, float v, int index) {
       const uint32_t mask = __ballot_sync(0xffffffffu, wanted);
       if (listed + __popc(mask) > kLpWarpList) {
-        select_largest(list, listed, best, k);
-        if (lane < k) list[lane] = best[lane];
-        listed = k;                                       // (of a full list: k of them)
-        threshold = fmaxf(threshold, key_value(best[k - 1]));
-        __syncwarp();
+        prune();
       }
       if (wanted) list[listed + __popc(mask & ((1u << lane) - 1u))] = rank_key(v, (uint32_t)index);
       listed += __popc(mask);
@@ -725,7 +798,18 @@ __global__ void __launch_bounds__(kLpThreads, (lp_warp_ctas<T, TOP>)) logprob_wa
       if constexpr (TOP) {
         const bool first = iteration == 0;
         if (first) {                                      // compared with its own threshold: equal values enter
-          const uint32_t bound = kth_largest_bound(lane < share.words ? order_bits(t.peak) : 0u, k);
+          uint32_t bound;
+          if (k <= 16) {
+            bound = kth_largest_bound(lane < share.words ? order_bits(t.peak) : 0u, k);
+          } else {                                        // of the maxima of a quarter of a lane's elements each
+            uint32_t quarter[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              quarter[u] = order_bits(Word16<T>::largest(w[u]));
+              if constexpr (kWords == 8) quarter[u] = max(quarter[u], order_bits(Word16<T>::largest(w[u + 4])));
+            }
+            bound = kth_largest(make_uint4(quarter[0], quarter[1], quarter[2], quarter[3]), k);
+          }
           if (bound >= 0x00800000u) threshold = order_value(bound);      // (below: fewer than k lanes have a finite value; all enter)
         }
         if (__any_sync(0xffffffffu, first ? !(biggest < threshold) : !(biggest <= threshold))) {
@@ -743,8 +827,10 @@ __global__ void __launch_bounds__(kLpThreads, (lp_warp_ctas<T, TOP>)) logprob_wa
             bits &= bits - 1;
           }
         }
-        if (iteration + 1 == next_refresh) {
-          if (!first) threshold = fmaxf(threshold, order_value(kth_largest_bound(order_bits(t.peak), k)));      // (NaN: below -infinity)
+        if (iteration + 1 == next_refresh && base + kChunk < share.words) {
+          if (k > 24) {
+            if (listed > k + (k >> 1)) prune();
+          } else if (!first) threshold = fmaxf(threshold, order_value(kth_largest_bound(order_bits(t.peak), k)));      // (NaN: below -infinity)
           next_refresh *= 2;
         }
       }
@@ -930,7 +1016,7 @@ static int logprob_launch_warps(const LogprobArgs& a, int sms, cudaStream_t stre
 
 template <typename T>
 static int logprob_launch(const LogprobArgs& a, int sms, cudaStream_t stream) {
-  if (a.rows >= (int64_t)sms * kLpWarpRows)
+  if (logprob_by_warps(a.rows, a.cols, a.top_k > 0, sms))
     return a.top_k > 0 ? logprob_launch_warps<T, true>(a, sms, stream) : logprob_launch_warps<T, false>(a, sms, stream);
   const int cluster = logprob_cluster(a.rows, a.cols, sizeof(T), sms);
   return a.top_k > 0 ? logprob_launch_top<T, true>(a, cluster, sms, stream) : logprob_launch_top<T, false>(a, cluster, sms, stream);

@@ -145,6 +145,22 @@ def test_ties_orders_and_extremes_among_the_likeliest(rows, cols):
                 _check(z, targets, k, binding.solon_token_logprobs(z, targets, top_k=k))
 
 
+@pytest.mark.parametrize("rows,cols", [(2, 700), (2, 1500), (150, 1025), (3, 30_001), (900, 6000), (1790, 3001), (2000, 20_000)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_likeliest(rows, cols, dtype):
+    """Numbers of tokens on both sides of where the search for them changes; their values spread, in few columns, rising, tied."""
+    z, targets = _logits(rows, cols, dtype, 9)
+    spiked = z.clone()
+    spiked[:, ::29] += 8.0
+    near = z.clone()
+    near[:, cols // 3:cols // 3 + 40] = 30.0                  # more equal ones than are wanted, in neighbouring columns
+    few = torch.full_like(z, -1e4)                            # masked by a finite value, with fewer left than are wanted
+    few[:, 11::cols // 9] = z[:, 11::cols // 9]
+    for k in (8, 9, 16, 17, 24, 25, 31):
+        for q in (z, spiked, near, few, z.sort(dim=1).values):
+            _check(q, targets, k, binding.solon_token_logprobs(q, targets, top_k=k))
+
+
 def test_wide_spread_of_values():
     """Logits over hundreds of units, each thread's and each CTA's maximum far from the row's."""
     for rows in (1, 3, 400, 1800):
