@@ -2,7 +2,10 @@
 // solon_decode returns.  Per weight, with g' = grad_scale * clip * g:
 //     m <- b1 m + (1 - b1) g'          v <- b2 v + (1 - b2) g'^2
 //     p <- p (1 - lr wd) - lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)
-// All of it in float32; b1^t and b2^t are kept in float64 on the device, so that a replayed CUDA graph counts its steps.
+// All of it in float32; b1^t and b2^t are kept in float64 on the device, so that a replayed CUDA graph counts its steps.  The
+// moments are formed as written, every product and sum rounded by itself (g' = (grad_scale g) clip, ((1 - b2) g') g', no
+// multiply-adds): the 8-bit state's codes can hang on a moment's last bit, and so they are those of one elementary operation
+// after the other.  (With multiply-adds 9 to 19 codes of 50 M came out otherwise per step, and a quarter of the moments in their last bit.)
 //
 // Bound by memory: a weight with float32 gradient moves 28 bytes (32-bit states) or 16 (8-bit states) against about 20 flops.
 // Measured on 50 M weights: 32-bit states 204 us (6.9 TB/s); 8-bit states 144 us (5.6 TB/s; codes and random bits keep the integer
@@ -42,7 +45,7 @@ struct alignas(64) AdamChunk {
 struct AdamScalars {
   double b1t, b2t;           // b1^t, b2^t of the last step that was applied
   long long applied, skipped;
-  float inv_bc1, inv_sqrt_bc2, grad_scale;
+  float inv_bc1, inv_sqrt_bc2, grad_scale, clip;
   int skip;
   unsigned key;              // of the step's random words
 };
@@ -145,14 +148,22 @@ __global__ void __launch_bounds__(256) adam_control_kernel(AdamControlArgs a) {
   bad = __syncthreads_or(bad);
   if (threadIdx.x != 0) return;
   double scale = a.grad_scale;
+  float clip = 1.0f;
   if (a.n_partials > 0) {
     sum = 0.0;
     for (int w = 0; w < 8; ++w) sum += part_s[w];
     const double norm = sqrt(sum) * fabs(a.grad_scale);
     if (a.norm_out) *a.norm_out = (float)norm;
     if (!(norm < INFINITY)) bad = 1;               // NaN or infinite: there is nothing to clip to
-    const double clip = a.max_norm / (norm + 1e-6);
-    if (clip < 1.0) scale *= clip;
+    // From the norm that is handed back, in float32 like everything that the moments are made of.  Beyond its range in float64,
+    // with a power of two moved from one factor to the other: the clip factor alone could be subnormal.
+    const float narrow = (float)norm;
+    if (narrow < INFINITY) {
+      clip = fminf(__fmul_rn((float)a.max_norm, __frcp_rn(__fadd_rn(narrow, 1e-6f))), 1.0f);
+    } else {
+      clip = (float)(fmin(a.max_norm / norm, 1.0) * 0x1p64);
+      scale *= 0x1p-64;
+    }
   }
   AdamScalars* s = a.s;
   s->skip = bad;
@@ -168,6 +179,7 @@ __global__ void __launch_bounds__(256) adam_control_kernel(AdamControlArgs a) {
   s->inv_bc1 = (float)(1.0 / (1.0 - b1t));
   s->inv_sqrt_bc2 = (float)(1.0 / sqrt(1.0 - b2t));
   s->grad_scale = (float)scale;
+  s->clip = clip;
   s->key = mix32((uint32_t)t * 0x9E3779B1u + (uint32_t)a.seed) ^ (uint32_t)(a.seed >> 32);
 }
 
@@ -520,7 +532,10 @@ __device__ __forceinline__ void adam_block(const AdamStepArgs& a, const AdamChun
     codes.load((const uint8_t*)a.exp_avg + slot, (const uint8_t*)a.exp_avg_sq + slot, lane);
     base = load_pack<int16_t, 2>(a.base + 2 * block);
   }
-  const float grad_scale = a.scalars->grad_scale, inv_sqrt_bc2 = a.scalars->inv_sqrt_bc2;
+  const float inv_sqrt_bc2 = a.scalars->inv_sqrt_bc2;
+  const Float2 grad_scale = pack2(a.scalars->grad_scale, a.scalars->grad_scale), clip = pack2(a.scalars->clip, a.scalars->clip);
+  const Float2 b1 = pack2(a.beta1, a.beta1), c1 = pack2(a.one_minus_beta1, a.one_minus_beta1);
+  const Float2 b2 = pack2(a.beta2, a.beta2), c2 = pack2(a.one_minus_beta2, a.one_minus_beta2);
   const float minus_step = -a.lr * a.scalars->inv_bc1;
   const float decay = 1.0f - a.lr * ch.weight_decay;
   bool simple = false;
@@ -529,10 +544,20 @@ __device__ __forceinline__ void adam_block(const AdamStepArgs& a, const AdamChun
     codes.decode(m, v, (uint32_t)(int)base.e[0] << 20, (uint32_t)(int)base.e[1] << 20, simple);
   }
 #pragma unroll
+  for (int i = 0; i < 8; i += 2) {
+    const Float2 gi = mul2(mul2(pack2(to_float(g[i]), to_float(g[i + 1])), grad_scale), clip);
+    float kept[2], added[2];                   // (added one by one: a packed sum of packed products becomes a multiply-add)
+    unpack2(mul2(b1, pack2(m[i], m[i + 1])), kept[0], kept[1]);
+    unpack2(mul2(c1, gi), added[0], added[1]);
+    m[i] = __fadd_rn(kept[0], added[0]);
+    m[i + 1] = __fadd_rn(kept[1], added[1]);
+    unpack2(mul2(b2, pack2(v[i], v[i + 1])), kept[0], kept[1]);
+    unpack2(mul2(mul2(c2, gi), gi), added[0], added[1]);
+    v[i] = __fadd_rn(kept[0], added[0]);
+    v[i + 1] = __fadd_rn(kept[1], added[1]);
+  }
+#pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float gi = to_float(g[i]) * grad_scale;
-    m[i] = fmaf(a.beta1, m[i], a.one_minus_beta1 * gi);
-    v[i] = fmaf(a.beta2, v[i], a.one_minus_beta2 * gi * gi);
     p[i] = fmaf(p[i], decay, __fdividef(minus_step * m[i], fmaf(sqrt_fast(v[i]), inv_sqrt_bc2, a.eps)));
   }
   if constexpr (MODE == kShifted) store8_shifted(ch.p + first, p, lane);

@@ -133,6 +133,34 @@ def test_32_bit_states_over_several_steps(grad_type, offset, max_norm):
         assert opt.steps() == (4, 0)
 
 
+@pytest.mark.parametrize("grad_type", [torch.float32, torch.float64, torch.bfloat16])
+@pytest.mark.parametrize("offset", [0, 1])
+@pytest.mark.parametrize("max_norm", [0.0, 0.7, 1e9])
+def test_moments_are_those_of_elementary_operations(grad_type, offset, max_norm):
+    """Bit for bit those of float32 products and sums, one after the other, with the clip factor from the norm that is handed back."""
+    flat, views, grad = _setup(SIZES, 21, offset)
+    with binding.AdamW(views, betas=(B1, B2), eps=EPS) as opt:
+        for t in range(1, 4):
+            g = torch.roll(grad, t).to(grad_type)
+            m, v = (_flat(x, SIZES).clone() for x in opt.moments())
+            norm = opt.step(g, lr=1e-2, grad_scale=1 / 15, max_norm=max_norm)
+            h = g.float() * (1 / 15)
+            if max_norm:
+                h = h * (max_norm * (norm + 1e-6).reciprocal()).clamp(max=1.0)
+            got_m, got_v = (_flat(x, SIZES) for x in opt.moments())
+            assert torch.equal(got_m, B1 * m + (1 - B1) * h) and torch.equal(got_v, B2 * v + (1 - B2) * h * h)
+
+
+def test_clipping_by_a_norm_beyond_float32():
+    flat, views, _ = _setup([4096], 22)
+    grad = torch.full((4096,), 3e38, device="cuda")          # norm 1.92e40
+    with binding.AdamW(views, betas=(B1, B2), eps=EPS) as opt:
+        norm = opt.step(grad, lr=1e-2, max_norm=1.0)
+        m, _ = (_flat(x, [4096]) for x in opt.moments())
+        assert float(norm) == float("inf") and opt.steps() == (1, 0)
+        assert ((m.double() * 10 * 64 - 1).abs() < 2.0 ** -20).all()     # g' = 1 / 64
+
+
 def _codes(low, high, rand, base, levels):
     """The two ends' codes of magnitudes known to lie in [low, high] (float64), for given random bits and window bases."""
     out = []
