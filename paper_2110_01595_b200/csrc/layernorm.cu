@@ -37,6 +37,11 @@ constexpr int ln_stages_for(int threads, int row_bytes_per_thread) {
 }
 template <typename T, int TPR, int ELEMS, int ROWS>
 constexpr int ln_stages = ln_stages_for(TPR < kLnThreads ? kLnThreads : TPR, ROWS * ELEMS * (int)sizeof(T));
+template <int TPR>
+__device__ __forceinline__ void team_barrier(int team = 0) {
+  if constexpr (TPR == 32) __syncwarp();
+  else asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "n"(TPR) : "memory");
+}
 // Sum over the team, the result in every thread.  Teams of several warps alternate between two slots, so one barrier a
 // sum is enough: a slot is written again only after everybody has passed the barrier of the sum in between.
 template <int TPR, int N>
@@ -54,7 +59,7 @@ __device__ __forceinline__ void team_sum(float (&v)[N], float* slots, int& turn,
 #pragma unroll
       for (int k = 0; k < N; ++k) s[k * kWarps + warp] = v[k];
     }
-    asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "n"(TPR) : "memory");
+    team_barrier<TPR>(team);
     if constexpr (kWarps == 32) {              // a lane a warp's sum: 32 warps that each read 32 sums would queue for shared memory
 #pragma unroll
       for (int k = 0; k < N; ++k) v[k] = s[k * kWarps + (threadIdx.x & 31)];
@@ -106,39 +111,54 @@ template <typename T, int VEC, int TPR, int ELEMS>
 struct LnRow {
   static constexpr int kGroups = ELEMS / VEC;
   static constexpr int kBlock = TPR < kLnThreads ? kLnThreads : TPR;
-  static constexpr int kTeams = kBlock / TPR;
+  static constexpr int kTeam = TPR, kTeams = kBlock / TPR;
   static constexpr bool kRing = VEC > 1;
   using Group = Pack<T, VEC>;
   static constexpr int kStageGroups = kGroups * kBlock;      // of a stage: one row of every team
+  // Elements can be gone through in steps of a few, and those left out in which a warp has no column of the row.  What that
+  // saves, and the order of loads and sums that comes with it, pays where the functions below say so.
+  static constexpr int kStep = VEC > 4 ? VEC : ELEMS < 4 ? ELEMS : 4, kSteps = ELEMS / kStep, kStepGroups = kStep / VEC;
 
   static __device__ __forceinline__ int column(int group, int tid) { return (group * TPR + tid) * VEC; }
+  static __device__ __forceinline__ int steps(int cols, int tid) {
+    int n = 1;
+#pragma unroll
+    for (int s = 1; s < kSteps; ++s) n += column(s * kStepGroups, tid & ~31) < cols;
+    return n;
+  }
 
   // the copies of a row's groups into a stage of the ring (groups x threads)
-  static __device__ __forceinline__ void issue(Group* stage, const T* row, int cols, int tid) {
+  static __device__ __forceinline__ void issue(Group* stage, const T* row, int cols, int tid, int steps) {
 #pragma unroll
     for (int i = 0; i < kGroups; ++i) {
+      if (i >= kStepGroups && i / kStepGroups >= steps) break;
       const int c = column(i, tid);
       copy_async<(int)sizeof(Group)>(stage + i * kBlock + threadIdx.x, c < cols ? row + c : row, c < cols);
     }
   }
-  static __device__ __forceinline__ void take(Float2 (&v)[ELEMS / 2], const Group* stage, const T* row, int cols, int tid) {
-    if constexpr (VEC * sizeof(T) == 16) {
+  static __device__ __forceinline__ void take(Float2 (&v)[ELEMS / 2], const Group* stage, const T* row, int cols, int tid, int steps) {
 #pragma unroll
-      for (int i = 0; i < kGroups; ++i) {
-        float part[VEC];
-        Word16<T>::unpack(reinterpret_cast<const uint4&>(stage[i * kBlock + threadIdx.x]), part);
+    for (int s = 0; s < kSteps; ++s) {
+      if (s > 0 && s >= steps) break;
+      if constexpr (VEC * sizeof(T) == 16) {
 #pragma unroll
-        for (int k = 0; k < VEC; k += 2) v[(i * VEC + k) / 2] = pack2(part[k], part[k + 1]);
+        for (int i = s * kStepGroups; i < (s + 1) * kStepGroups; ++i) {
+          float part[VEC];
+          Word16<T>::unpack(reinterpret_cast<const uint4&>(stage[i * kBlock + threadIdx.x]), part);
+#pragma unroll
+          for (int k = 0; k < VEC; k += 2) v[(i * VEC + k) / 2] = pack2(part[k], part[k + 1]);
+        }
+      } else {
+        Group part[kStepGroups];
+#pragma unroll
+        for (int i = 0; i < kStepGroups; ++i) {
+          const int group = s * kStepGroups + i;
+          if constexpr (kRing) part[i] = stage[group * kBlock + threadIdx.x];
+          else part[i].e[0] = column(group, tid) < cols ? row[column(group, tid)] : from_float<T>(0.0f);
+        }
+#pragma unroll
+        for (int i = 0; i < kStep; i += 2) v[(s * kStep + i) / 2] = pack2(to_float(part[i / VEC].e[i % VEC]), to_float(part[(i + 1) / VEC].e[(i + 1) % VEC]));
       }
-    } else {
-      Group part[kGroups];
-#pragma unroll
-      for (int i = 0; i < kGroups; ++i) {
-        if constexpr (kRing) part[i] = stage[i * kBlock + threadIdx.x];
-        else part[i].e[0] = column(i, tid) < cols ? row[column(i, tid)] : from_float<T>(0.0f);
-      }
-#pragma unroll
-      for (int i = 0; i < ELEMS; i += 2) v[i / 2] = pack2(to_float(part[i / VEC].e[i % VEC]), to_float(part[(i + 1) / VEC].e[(i + 1) % VEC]));
     }
   }
   static __device__ __forceinline__ void store(T* row, const Float2 (&v)[ELEMS / 2], int cols, int tid) {
@@ -192,6 +212,21 @@ __device__ __forceinline__ float sum_of(Float2 x) {
   return a + b;
 }
 
+// Which steps without columns are left out - of the copies, of the loads, of the work.  Measured with and without, us, caches
+// cold.  Forward: words of float32 8192 x 8192 88, 97 (of two-byte elements the same, or 55, 53 with 4000 x 16384); single float32
+// elements 4000 x 15001 130, 155.  Backward: teams up to 128 15 x 2048 x 2048 bfloat16 73, 78; of 256, the work alone, 16384 x 2560
+// 68, 70; of 512, loads and work, 8192 x 5120 bfloat16 70, 74, but 8192 x 8192 85, 82, float32 131, 136; single float32 elements
+// 30000 x 2001 134, 145 (two-byte ones 270, 109: their loads then wait for one another).
+struct LnSkip {
+  bool copies, loads, work;
+};
+template <typename T, int VEC>
+constexpr LnSkip ln_forward_skip = {VEC == 4 && sizeof(T) == 4, VEC == 1 && sizeof(T) == 4, VEC != 2 && sizeof(T) == 4};
+template <typename T, int VEC, int TPR>
+constexpr LnSkip ln_backward_skip = VEC == 1   ? LnSkip{false, sizeof(T) == 4, sizeof(T) == 4}
+                                    : VEC == 2 ? LnSkip{false, false, false}
+                                               : LnSkip{TPR <= 128, TPR > 256, true};
+
 // CTAs of the forward pass on an SM: with single elements a third one pays (30000 x 2001 bfloat16 81 -> 71 us, float32 98 -> 91).
 template <int VEC, int TPR, int ELEMS>
 constexpr int ln_forward_ctas = TPR >= 512 ? 1 : VEC > 1 || ELEMS > 16 ? 2 : 3;
@@ -206,13 +241,17 @@ __global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, ln_forwar
   const int tid = threadIdx.x & (TPR - 1), team = threadIdx.x / TPR, cols = (int)a.cols;
   const T* x = static_cast<const T*>(a.x);
   T* y = static_cast<T*>(a.y);
+  constexpr LnSkip kSkip = ln_forward_skip<T, VEC>;
+  const int with_columns = Row::steps(cols, tid);
+  const int copy_steps = kSkip.copies ? with_columns : Row::kSteps, load_steps = kSkip.loads ? with_columns : Row::kSteps;
+  const int steps = kSkip.work ? with_columns : Row::kSteps;
   const float inv_n = 1.0f / (float)cols;
   const int64_t stride = (int64_t)gridDim.x * Row::kTeams;
   int64_t row = (int64_t)blockIdx.x * Row::kTeams + team;
   if constexpr (Row::kRing) {
 #pragma unroll
     for (int s = 0; s < kStages; ++s) {
-      if (row + s * stride < a.rows) Row::issue(ring + s * Row::kStageGroups, x + (row + s * stride) * a.x_pitch, cols, tid);
+      if (row + s * stride < a.rows) Row::issue(ring + s * Row::kStageGroups, x + (row + s * stride) * a.x_pitch, cols, tid, copy_steps);
       copies_commit();
     }
   }
@@ -224,33 +263,41 @@ __global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, ln_forwar
     Float2 v[ELEMS / 2];
     typename Row::Group* words = ring + stage * Row::kStageGroups;
     if constexpr (Row::kRing) copies_wait<kStages - 1>();
-    Row::take(v, words, x + row * a.x_pitch, cols, tid);
+    Row::take(v, words, x + row * a.x_pitch, cols, tid, load_steps);
     if constexpr (Row::kRing) {
       const int64_t ahead = row + kStages * stride;       // into the words just read
-      if (ahead < a.rows) Row::issue(words, x + ahead * a.x_pitch, cols, tid);
+      if (ahead < a.rows) Row::issue(words, x + ahead * a.x_pitch, cols, tid, copy_steps);
       copies_commit();
       stage = stage + 1 == kStages ? 0 : stage + 1;
     }
     Float2 acc = both(0.0f);
 #pragma unroll
-    for (int i = 0; i < ELEMS / 2; ++i) acc = add2(acc, v[i]);
+    for (int s = 0; s < Row::kSteps; ++s) {
+      if (s > 0 && s >= steps) break;
+#pragma unroll
+      for (int i = s * Row::kStep / 2; i < (s + 1) * Row::kStep / 2; ++i) acc = add2(acc, v[i]);
+    }
     float sum[1] = {sum_of(acc)};
     team_sum<TPR>(sum, slots, turn, team);
     const float mean = sum[0] * inv_n;
     const Float2 minus_mean = both(-mean);
     acc = both(0.0f);
 #pragma unroll
-    for (int i = 0; i < ELEMS / 2; ++i) {
-      v[i] = add2(v[i], minus_mean);
-      if constexpr (VEC > 1) {                            // a group lies inside the row or outside
-        if (Row::column(2 * i / VEC, tid) < cols) acc = fma2(v[i], v[i], acc);
-      } else {
-        float e0, e1;
-        unpack2(v[i], e0, e1);
-        e0 = Row::column(2 * i, tid) < cols ? e0 : 0.0f;
-        e1 = Row::column(2 * i + 1, tid) < cols ? e1 : 0.0f;
-        const Float2 e = pack2(e0, e1);
-        acc = fma2(e, e, acc);
+    for (int s = 0; s < Row::kSteps; ++s) {
+      if (s > 0 && s >= steps) break;
+#pragma unroll
+      for (int i = s * Row::kStep / 2; i < (s + 1) * Row::kStep / 2; ++i) {
+        v[i] = add2(v[i], minus_mean);
+        if constexpr (VEC > 1) {                            // a group lies inside the row or outside
+          if (Row::column(2 * i / VEC, tid) < cols) acc = fma2(v[i], v[i], acc);
+        } else {
+          float e0, e1;
+          unpack2(v[i], e0, e1);
+          e0 = Row::column(2 * i, tid) < cols ? e0 : 0.0f;
+          e1 = Row::column(2 * i + 1, tid) < cols ? e1 : 0.0f;
+          const Float2 e = pack2(e0, e1);
+          acc = fma2(e, e, acc);
+        }
       }
     }
     float sq[1] = {sum_of(acc)};
@@ -258,7 +305,11 @@ __global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, ln_forwar
     const float rstd = rsqrtf(sq[0] * inv_n + a.eps);
     const Float2 scale = both(rstd);
 #pragma unroll
-    for (int i = 0; i < ELEMS / 2; ++i) v[i] = fma2(mul2(v[i], scale), w[i], b[i]);
+    for (int s = 0; s < Row::kSteps; ++s) {
+      if (s > 0 && s >= steps) break;
+#pragma unroll
+      for (int i = s * Row::kStep / 2; i < (s + 1) * Row::kStep / 2; ++i) v[i] = fma2(mul2(v[i], scale), w[i], b[i]);
+    }
     Row::store(y + row * a.y_pitch, v, cols, tid);
     if (tid == 0) {
       if (a.mean) a.mean[row] = mean;
@@ -286,9 +337,10 @@ __device__ __forceinline__ void store_grad(void* p, int f64, int64_t i, float v)
   else static_cast<float*>(p)[i] = v;
 }
 
-// A team's sums for weight and bias: the partition's gradient, or a partial sum where several CTAs share the partition.
+// A team's sums for weight and bias: the partition's gradient, or a partial sum where several CTAs share the partition.  `line`:
+// shared memory for a float of each of the team's columns.
 template <typename Row, int VEC, int ELEMS>
-__device__ __forceinline__ void put_param_sums(const LnBackwardArgs& a, const float (&sums)[2][ELEMS], int part, int split, int tid) {
+__device__ __forceinline__ void put_param_sums(const LnBackwardArgs& a, const float (&sums)[2][ELEMS], float* line, int part, int split, int tid) {
   const int cols = (int)a.cols;
   if (a.splits > 1) {
     constexpr int kStore = VEC < 4 ? VEC : 4;  // a row of groups of VEC elements is a row of groups of kStore
@@ -308,12 +360,28 @@ __device__ __forceinline__ void put_param_sums(const LnBackwardArgs& a, const fl
     }
     return;
   }
+  if constexpr (VEC >= 4) {                    // by way of shared memory, so that neighbouring threads store neighbouring elements
 #pragma unroll
-  for (int i = 0; i < ELEMS; ++i) {
-    const int c = Row::column(i / VEC, tid) + i % VEC;
-    if (c >= cols) continue;
-    if (a.dweight) store_grad(a.dweight, a.grad_f64, part * a.grad_pitch + c, sums[0][i]);
-    if (a.dbias) store_grad(a.dbias, a.grad_f64, part * a.grad_pitch + c, sums[1][i]);
+    for (int which = 0; which < 2; ++which) {
+      void* dst = which ? a.dbias : a.dweight;
+      if (!dst) continue;
+      team_barrier<Row::kTeam>();              // (only the first team is here)
+#pragma unroll
+      for (int i = 0; i < ELEMS; i += 4) {
+        const float* v = &sums[which][i];
+        *reinterpret_cast<float4*>(line + Row::column(i / VEC, tid) + i % VEC) = make_float4(v[0], v[1], v[2], v[3]);
+      }
+      team_barrier<Row::kTeam>();
+      for (int c = tid; c < cols; c += Row::kTeam) store_grad(dst, a.grad_f64, part * a.grad_pitch + c, line[c]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < ELEMS; ++i) {
+      const int c = Row::column(i / VEC, tid) + i % VEC;
+      if (c >= cols) continue;
+      if (a.dweight) store_grad(a.dweight, a.grad_f64, part * a.grad_pitch + c, sums[0][i]);
+      if (a.dbias) store_grad(a.dbias, a.grad_f64, part * a.grad_pitch + c, sums[1][i]);
+    }
   }
 }
 
@@ -331,6 +399,10 @@ __global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, TPR < 512
   const T* x = static_cast<const T*>(a.x);
   const T* dy = static_cast<const T*>(a.dy);
   T* dx = static_cast<T*>(a.dx);
+  constexpr LnSkip kSkip = ln_backward_skip<T, VEC, TPR>;
+  const int with_columns = Row::steps(cols, tid);
+  const int copy_steps = kSkip.copies ? with_columns : Row::kSteps, load_steps = kSkip.loads ? with_columns : Row::kSteps;
+  const int steps = kSkip.work ? with_columns : Row::kSteps;
   const float inv_n = 1.0f / (float)cols;
   const int64_t stride = (int64_t)a.splits * kTeams, end = (int64_t)(part + 1) * a.rows_per_part;
   int64_t row = (int64_t)part * a.rows_per_part + (int64_t)split * kTeams + team;
@@ -339,8 +411,8 @@ __global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, TPR < 512
     for (int s = 0; s < kStages; ++s) {
       const int64_t at = row + s * stride;
       if (at < end) {
-        Row::issue(ring + s * 2 * Row::kStageGroups, x + at * a.x_pitch, cols, tid);
-        Row::issue(ring + (s * 2 + 1) * Row::kStageGroups, dy + at * a.dy_pitch, cols, tid);
+        Row::issue(ring + s * 2 * Row::kStageGroups, x + at * a.x_pitch, cols, tid, copy_steps);
+        Row::issue(ring + (s * 2 + 1) * Row::kStageGroups, dy + at * a.dy_pitch, cols, tid, copy_steps);
       }
       copies_commit();
     }
@@ -366,32 +438,40 @@ __global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, TPR < 512
     typename Row::Group* words = ring + stage * 2 * Row::kStageGroups;
     Float2 xh[ELEMS / 2], g[ELEMS / 2];
     if constexpr (Row::kRing) copies_wait<kStages - 1>();
-    Row::take(xh, words, x + row * a.x_pitch, cols, tid);
-    Row::take(g, words + Row::kStageGroups, dy + row * a.dy_pitch, cols, tid);
+    Row::take(xh, words, x + row * a.x_pitch, cols, tid, load_steps);
+    Row::take(g, words + Row::kStageGroups, dy + row * a.dy_pitch, cols, tid, load_steps);
     if constexpr (Row::kRing) {
       const int64_t ahead = row + kStages * stride;       // into the words just read
       if (ahead < end) {
-        Row::issue(words, x + ahead * a.x_pitch, cols, tid);
-        Row::issue(words + Row::kStageGroups, dy + ahead * a.dy_pitch, cols, tid);
+        Row::issue(words, x + ahead * a.x_pitch, cols, tid, copy_steps);
+        Row::issue(words + Row::kStageGroups, dy + ahead * a.dy_pitch, cols, tid, copy_steps);
       }
       copies_commit();
       stage = stage + 1 == kStages ? 0 : stage + 1;
     }
 #pragma unroll
-    for (int i = 0; i < ELEMS / 2; ++i) {                 // (outside the row dy and w are 0)
-      xh[i] = mul2(add2(xh[i], minus_mean), scale);
-      dw[i] = fma2(g[i], xh[i], dw[i]);
-      db[i] = add2(db[i], g[i]);
-      g[i] = mul2(g[i], w[i]);
-      s0 = add2(s0, g[i]);
-      s1 = fma2(g[i], xh[i], s1);
+    for (int s = 0; s < Row::kSteps; ++s) {
+      if (s > 0 && s >= steps) break;
+#pragma unroll
+      for (int i = s * Row::kStep / 2; i < (s + 1) * Row::kStep / 2; ++i) {               // (outside the row dy and w are 0)
+        xh[i] = mul2(add2(xh[i], minus_mean), scale);
+        dw[i] = fma2(g[i], xh[i], dw[i]);
+        db[i] = add2(db[i], g[i]);
+        g[i] = mul2(g[i], w[i]);
+        s0 = add2(s0, g[i]);
+        s1 = fma2(g[i], xh[i], s1);
+      }
     }
     if (dx) {
-      float s[2] = {sum_of(s0), sum_of(s1)};
-      team_sum<TPR>(s, slots, turn, team);
-      const Float2 minus_m0 = both(-s[0] * inv_n), minus_m1 = both(-s[1] * inv_n);
+      float sums[2] = {sum_of(s0), sum_of(s1)};
+      team_sum<TPR>(sums, slots, turn, team);
+      const Float2 minus_m0 = both(-sums[0] * inv_n), minus_m1 = both(-sums[1] * inv_n);
 #pragma unroll
-      for (int i = 0; i < ELEMS / 2; ++i) g[i] = mul2(fma2(xh[i], minus_m1, add2(g[i], minus_m0)), scale);
+      for (int s = 0; s < Row::kSteps; ++s) {
+        if (s > 0 && s >= steps) break;
+#pragma unroll
+        for (int i = s * Row::kStep / 2; i < (s + 1) * Row::kStep / 2; ++i) g[i] = mul2(fma2(xh[i], minus_m1, add2(g[i], minus_m0)), scale);
+      }
       Row::store(dx + row * a.dx_pitch, g, cols, tid);
     }
   }
@@ -420,18 +500,19 @@ __global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, TPR < 512
     }
     if (team != 0) return;
   }
-  put_param_sums<Row, VEC, ELEMS>(a, sums, part, split, tid);
+  put_param_sums<Row, VEC, ELEMS>(a, sums, reinterpret_cast<float*>(ring_memory), part, split, tid);
 }
 
 // Rows of 8193 .. 16384 elements: a row a CTA of 1024 threads, whose 64 registers hold the sums of 16 columns but not the row and
 // the weight beside them.  So the weight sits in shared memory, and the row is taken from the ring twice: for the sums, and
 // again, piece by piece, for dx; each piece of the ring is refilled as soon as it has been taken for the second time.
-// (15 x 64 rows of 12000 bfloat16 with all of it in registers, which spilled 312 bytes a thread: 49 us; so: 30 to 32.)
+// (15 x 64 rows of 12000 bfloat16 with all of it in registers, which spilled 312 bytes a thread: 49 us; so: 30 to 32.  Pieces of a
+// word or four elements: 4000 x 15001 float32 190 us, of two 240; 4000 x 15002 bfloat16 131, of two 136; of eight 211, 130.)
 template <typename T>
 constexpr int ln_broad_stages = sizeof(T) == 2 ? 2 : 1;      // 64 KB of weights and 64 or 128 KB a stage
 template <typename T, int VEC>
 __global__ void __launch_bounds__(1024) ln_backward_broad_kernel(LnBackwardArgs a) {
-  constexpr int kTeam = 1024, kElems = 16, kPiece = VEC == 1 ? 2 : VEC, kPieces = kElems / kPiece, kSpan = kPiece * kTeam;
+  constexpr int kTeam = 1024, kElems = 16, kPiece = VEC < 4 ? 4 : VEC, kPieces = kElems / kPiece, kSpan = kPiece * kTeam;
   constexpr int kStages = ln_broad_stages<T>;
   using Row = LnRow<T, VEC, kTeam, kElems>;
   using Piece = LnRow<T, VEC, kTeam, kPiece>;                // piece k: the row's columns from k * kSpan on
@@ -449,8 +530,8 @@ __global__ void __launch_bounds__(1024) ln_backward_broad_kernel(LnBackwardArgs 
   auto issue = [&](int stage, int k, int64_t at) {
     typename Row::Group* words = ring + stage * 2 * Row::kStageGroups + k * Piece::kStageGroups;
     const int from = k * kSpan < cols ? k * kSpan : 0, left = cols - k * kSpan;
-    Piece::issue(words, x + at * a.x_pitch + from, left, tid);
-    Piece::issue(words + Row::kStageGroups, dy + at * a.dy_pitch + from, left, tid);
+    Piece::issue(words, x + at * a.x_pitch + from, left, tid, Piece::kSteps);
+    Piece::issue(words + Row::kStageGroups, dy + at * a.dy_pitch + from, left, tid, Piece::kSteps);
   };
   if constexpr (Row::kRing) {
 #pragma unroll
@@ -484,8 +565,8 @@ __global__ void __launch_bounds__(1024) ln_backward_broad_kernel(LnBackwardArgs 
 #pragma unroll
     for (int k = 0; k < kPieces; ++k) {
       Float2 xh[kPiece / 2], g[kPiece / 2];
-      Piece::take(xh, words + k * Piece::kStageGroups, x_row + k * kSpan, cols - k * kSpan, tid);
-      Piece::take(g, words + Row::kStageGroups + k * Piece::kStageGroups, dy_row + k * kSpan, cols - k * kSpan, tid);
+      Piece::take(xh, words + k * Piece::kStageGroups, x_row + k * kSpan, cols - k * kSpan, tid, Piece::kSteps);
+      Piece::take(g, words + Row::kStageGroups + k * Piece::kStageGroups, dy_row + k * kSpan, cols - k * kSpan, tid, Piece::kSteps);
 #pragma unroll
       for (int i = 0; i < kPiece / 2; ++i) {
         const int e = k * kPiece / 2 + i;
@@ -505,8 +586,8 @@ __global__ void __launch_bounds__(1024) ln_backward_broad_kernel(LnBackwardArgs 
     for (int k = 0; k < kPieces; ++k) {
       if (dx) {
         Float2 xh[kPiece / 2], g[kPiece / 2];
-        Piece::take(xh, words + k * Piece::kStageGroups, x_row + k * kSpan, cols - k * kSpan, tid);
-        Piece::take(g, words + Row::kStageGroups + k * Piece::kStageGroups, dy_row + k * kSpan, cols - k * kSpan, tid);
+        Piece::take(xh, words + k * Piece::kStageGroups, x_row + k * kSpan, cols - k * kSpan, tid, Piece::kSteps);
+        Piece::take(g, words + Row::kStageGroups + k * Piece::kStageGroups, dy_row + k * kSpan, cols - k * kSpan, tid, Piece::kSteps);
 #pragma unroll
         for (int i = 0; i < kPiece / 2; ++i) {
           xh[i] = mul2(add2(xh[i], minus_mean), scale);
@@ -532,7 +613,7 @@ __global__ void __launch_bounds__(1024) ln_backward_broad_kernel(LnBackwardArgs 
     unpack2(dw[i / 2], sums[0][i], sums[0][i + 1]);
     unpack2(db[i / 2], sums[1][i], sums[1][i + 1]);
   }
-  put_param_sums<Row, VEC, kElems>(a, sums, part, split, tid);
+  put_param_sums<Row, VEC, kElems>(a, sums, reinterpret_cast<float*>(ring_memory), part, split, tid);
 }
 
 // Sums of the CTAs' partial sums, in a fixed order: a lane takes two columns, the splits are dealt to WARPS warps.
