@@ -201,12 +201,12 @@ __device__ __forceinline__ void norm_finish(double acc, double* partials) {
   }
 }
 
-// A flat gradient: eight 16-byte words a thread at a time (50 M float64: 64 us, with four 93), a contiguous stretch per CTA
-// and turn.
+// A flat gradient: eight 16-byte words a thread at a time (50 M float64: 64 us, with four 93), of two-byte elements four (50 M: 23
+// us, with eight, which spill, 49), a contiguous stretch per CTA and turn.
 template <typename G>
 __global__ void __launch_bounds__(kAdamThreads, 4) adam_norm_flat_kernel(const G* __restrict__ grad, int64_t n, double* __restrict__ partials) {
   constexpr int kVec = 16 / sizeof(G);
-  constexpr int kUnroll = 8;
+  constexpr int kUnroll = sizeof(G) == 2 ? 4 : 8;
   pdl_trigger();
   pdl_wait();
   const int64_t to_boundary = (int64_t)((16 - ((uintptr_t)grad & 15)) & 15) / (int64_t)sizeof(G);
