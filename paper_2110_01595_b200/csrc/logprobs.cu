@@ -304,36 +304,60 @@ __device__ __forceinline__ uint32_t kth_largest(const uint4& q, int k) {
   return bound;
 }
 
-// Of n keys (all different, beside zeros) the k largest and some more, `most` at most, in their order; how many there are, and
-// the order bits of the smallest.  One warp.
+// Of n > most keys in shared memory (all different, beside zeros) the k largest and some more, `most` at most, in their order; how
+// many there are, and the order bits of the smallest.  One warp: bit by bit, from the first on in which the keys differ, the
+// largest bound that k keys reach; up to 128 keys stay in registers, and hardly ever do values tie so that their indices count.
 __device__ __noinline__ int trim_keys(unsigned long long* keys, int n, int k, int most, uint32_t* smallest) {
+  constexpr int kHeld = 4;
   const int lane = threadIdx.x & 31;
-  uint32_t high = 0, low = ~0u;
-  for (int i = lane; i < n; i += 32) {
+  uint32_t order[kHeld], high = 0, low = ~0u;
+#pragma unroll
+  for (int u = 0; u < kHeld; ++u) {
+    order[u] = u * 32 + lane < n ? (uint32_t)(keys[u * 32 + lane] >> 32) : 0u;
+    if (u * 32 + lane < n) {
+      high = max(high, order[u]);
+      low = min(low, order[u]);
+    }
+  }
+  for (int i = kHeld * 32 + lane; i < n; i += 32) {
     const uint32_t o = (uint32_t)(keys[i] >> 32);
     high = max(high, o);
     low = min(low, o);
   }
   high = __reduce_max_sync(0xffffffffu, high);
   low = __reduce_min_sync(0xffffffffu, low);
-  const int top = high == low ? -1 : 31 - __clz(high ^ low);           // the highest bit in which they differ
-  unsigned long long bound = (unsigned long long)(top < 0 ? high : high & ~((2u << top) - 1u)) << 32;
-  for (int bit = top + 32; bit >= 0; --bit) {
-    const unsigned long long trial = bound | (1ull << bit);
+  const int top = high == low ? -1 : 31 - __clz(high ^ low);
+  uint32_t bound = top < 0 ? high : high & ~((2u << top) - 1u);
+  unsigned long long least = 0;                  // the smallest key that stays
+  int left = n;
+  for (int bit = top; bit >= 0 && left > most; --bit) {
+    const uint32_t trial = bound | (1u << bit);
     uint32_t above = 0;
-#pragma unroll 4
-    for (int i = lane; i < n; i += 32) above += keys[i] >= trial;
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u) above += order[u] >= trial;
+    for (int i = kHeld * 32 + lane; i < n; i += 32) above += (uint32_t)(keys[i] >> 32) >= trial;
     above = __reduce_add_sync(0xffffffffu, above);
     if ((int)above >= k) {
       bound = trial;
-      if ((int)above <= most) break;
+      left = (int)above;
+    }
+  }
+  least = (unsigned long long)bound << 32;
+  for (int bit = 31; bit >= 0 && left > most; --bit) {       // among equal values by the index
+    const unsigned long long trial = least | (1ull << bit);
+    uint32_t above = 0;
+    for (int i = lane; i < n; i += 32) above += keys[i] >= trial;
+    above = __reduce_add_sync(0xffffffffu, above);
+    if ((int)above >= k) {
+      least = trial;
+      left = (int)above;
     }
   }
   int kept = 0;
   low = ~0u;
   for (int base = 0; base < n; base += 32) {
     const unsigned long long key = base + lane < n ? keys[base + lane] : 0;
-    const bool keep = key >= bound && key != 0;
+    const bool keep = key >= least && key != 0;
     const uint32_t mask = __ballot_sync(0xffffffffu, keep);
     __syncwarp();
     if (keep) {
