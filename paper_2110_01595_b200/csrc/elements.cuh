@@ -82,16 +82,17 @@ struct Word16<float> {
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(__uint_as_float(w)), "f"(__uint_as_float(low)));
     return __float_as_uint(r);
   }
+  static __device__ __forceinline__ uint32_t max3(uint32_t a, uint32_t b, uint32_t c) {      // (one instruction)
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(__uint_as_float(a)), "f"(__uint_as_float(b)), "f"(__uint_as_float(c)));
+    return __float_as_uint(r);
+  }
   static __device__ __forceinline__ float widest(uint32_t w) { return __uint_as_float(w); }
   static __device__ __forceinline__ uint4 pack(const float (&x)[4]) {
     return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
   }
   static __device__ __forceinline__ float largest(const uint4& v) {
-    float m;
-    asm("{\n\t.reg .f32 a, b;\n\tmax.NaN.f32 a, %1, %2;\n\tmax.NaN.f32 b, %3, %4;\n\tmax.NaN.f32 %0, a, b;\n\t}"
-        : "=f"(m)
-        : "f"(__uint_as_float(v.x)), "f"(__uint_as_float(v.y)), "f"(__uint_as_float(v.z)), "f"(__uint_as_float(v.w)));
-    return m;
+    return widest(at_least(max3(v.x, v.y, v.z), v.w));
   }
 };
 

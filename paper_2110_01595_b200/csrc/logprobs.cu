@@ -183,14 +183,29 @@ struct LogprobThread {
 // Largest element of a thread's words (NaN if there is one).
 template <typename T, int N>
 __device__ __forceinline__ float largest_of(const uint4 (&w)[N]) {
-  uint32_t m[N];
+  using Word = Word16<T>;
+  static_assert(N % 2 == 0 && N >= 4);
+  if constexpr (sizeof(T) == 4) {                // three at a time: half as many instructions
+    uint4 m = w[0];
 #pragma unroll
-  for (int u = 0; u < N; ++u) m[u] = Word16<T>::at_least(Word16<T>::at_least(w[u].x, w[u].y), Word16<T>::at_least(w[u].z, w[u].w));
+    for (int u = 1; u < N - 1; u += 2) {
+      m.x = Word::max3(m.x, w[u].x, w[u + 1].x);
+      m.y = Word::max3(m.y, w[u].y, w[u + 1].y);
+      m.z = Word::max3(m.z, w[u].z, w[u + 1].z);
+      m.w = Word::max3(m.w, w[u].w, w[u + 1].w);
+    }
+    const uint4& last = w[N - 1];
+    return Word::widest(Word::at_least(Word::max3(m.x, m.y, m.z), Word::max3(Word::max3(m.w, last.x, last.y), last.z, last.w)));
+  } else {
+    uint32_t m[N];
 #pragma unroll
-  for (int n = N / 2; n > 0; n /= 2)
+    for (int u = 0; u < N; ++u) m[u] = Word::at_least(Word::at_least(w[u].x, w[u].y), Word::at_least(w[u].z, w[u].w));
 #pragma unroll
-    for (int u = 0; u < n; ++u) m[u] = Word16<T>::at_least(m[u], m[u + n]);
-  return Word16<T>::widest(m[0]);
+    for (int n = N / 2; n > 0; n /= 2)
+#pragma unroll
+      for (int u = 0; u < n; ++u) m[u] = Word::at_least(m[u], m[u + n]);
+    return Word::widest(m[0]);
+  }
 }
 
 // One element by differences from the largest so far (rows that are `far`, see above).
