@@ -6,8 +6,8 @@
 // difference of two sums; statistics and sums are float32.
 //
 // Bound by memory: 2 (forward) and 3 (backward) accesses of the matrix against about 8 and 14 flops an element.  Measured:
-// forward 16384 x 4096 bfloat16 48 us (5.6 TB/s), float32 96 us (5.6 TB/s); backward 15 x 2048 rows of 2048 bfloat16 68 us
-// (5.6 TB/s) with 3.5 us for the partial sums, 16384 x 4096 float32 143 us (5.6 TB/s).  What keeps it from the copy rate is 16 warps
+// forward 16384 x 4096 bfloat16 48 us (5.6 TB/s), 8192 x 8192 float32 82 us (6.5 TB/s); backward 15 x 2048 rows of 2048 bfloat16 65 us
+// (5.8 TB/s) with 3.5 us for the partial sums, 8192 x 8192 float32 136 us (5.9 TB/s).  What keeps it from the copy rate is 16 warps
 // an SM (the registers of a column's parameters and sums), each with a barrier or two a row.
 //
 // Layout: a row belongs to a team of TPR threads that hold 16 or 32 elements each (fewer in short rows), so that a team's

@@ -19,7 +19,7 @@
 namespace solon {
 
 // Measured: 8192 x 32768 bfloat16 94 us (5.7 TB/s), 4096 x 32768 float32 90 us (6.0 TB/s), 2047 x 50001 float32 72 us and with 20
-// likeliest tokens 89 us; the gradient on 8192 x 32768 bfloat16 190 us (5.7 TB/s).
+// likeliest tokens 85 us; the gradient on 8192 x 32768 bfloat16 190 us (5.7 TB/s).
 //
 // Bound by memory, with the exponentials (one a logit: at 16 a clock and SM 60 % of the time that bfloat16 logits take to
 // arrive) and the instructions beside them close behind, so those are kept few: two values an instruction, one multiply-add
@@ -697,7 +697,7 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprob_kernel(Logpr
   }
 }
 
-// ---- many rows: a warp a row -----------------------------------------------------------------------------------------
+// ---- many or short rows: a warp a row --------------------------------------------------------------------------------------
 // Nothing in a row then waits for another warp, and the serial work at a row's end (and for its likeliest tokens) of one warp
 // hides behind the others' streams; but a warp alone takes its time over a row, so there have to be the more rows the longer they
 // are, up to 12 per SM.  Measured, bfloat16, CTA a row against warp a row in us: 8192 x 32768 107 / 91; 1200 x 16000 13.0 / 11.9;
@@ -716,8 +716,8 @@ template <typename T>
 constexpr int lp_warp_words = 32 / Word16<T>::kCount;                    // words of a lane in an iteration: 32 elements
 // CTAs of eight warps on an SM.  Two suffice the plain sums of two-byte logits (8192 x 32768 bfloat16 takes 100 us with three, 91 with
 // two, 16384 x 16384 89 and 85: the last round of rows is fuller), and for likeliest tokens of float32 ones three would have to
-// share the memory of the lists (2047 x 50001 with 20: 102 us, 89 with two); float32 sums (2047 x 50001: 72 us, 77 with two) and
-// likeliest tokens of two-byte logits (8192 x 32768 with 8: 157 us, 168 with two) take three.
+// share the memory of the lists (2047 x 50001 with 20: 91 us, 85 with two); float32 sums (2047 x 50001: 72 us, 77 with two) and
+// likeliest tokens of two-byte logits (8192 x 32768 with 8: 155 us, 168 with two) take three.
 template <typename T, bool TOP>
 constexpr int lp_warp_ctas = (sizeof(T) == 4) == TOP ? 2 : 3;
 template <typename T, bool TOP>
