@@ -95,27 +95,28 @@ __device__ __forceinline__ SoftmaxPart join_lanes(SoftmaxPart p) {
 }
 
 // The sums of a thread while its warp goes through a row.  The exponent of a logit is one multiply-add, t = z log2 e - ref, the
-// product exact, so the reference costs no rounding; it is a value of the row's scale, the same in the whole warp, and moves
-// (rescaling the sums) only when a logit lies more than 8 above it in base 2: hardly ever after the first words.
+// product exact; the reference is the integer next to a logit's product, the same in the whole warp, and moves (rescaling the
+// sums) only when a logit lies more than 8 above it in base 2: hardly ever after the first words.
 // Logits below `floor`, 140 or more under the reference, are raised to it: their 2^t is 0 either way, but t 2^t is defined.
-// Beyond 2e38 the product overflows, and next to the type's lowest value there is no such floor.  A logit that far down is no
-// reference (beside any ordinary one its 2^t is 0); `far` says that one was seen: if nothing larger turns up - a row masked with
-// its type's lowest value - or a logit was that far up, the row is gone through once more with differences.
-constexpr int kFarDown = 1, kFarUp = 2;
+// That holds for references of logits up to 1e7.  From 2^24 / log2 e = 1.16e7 on the integers of float32 lie 2 and more apart (at 1e10
+// 1024), so the largest logit's own t can be that far from 0, which costs digits and then overflows or leaves nothing; next to
+// float16's lowest value there is no floor.  Such a row - masked with a large finite value, until something else turns up -
+// takes differences from a logit, which are exact or their 2^t is 0 (2047 x 50001 float32 71 us with every 50th row
+// all -1e9 and without).
 template <typename T>
 struct LogprobThread {
-  static constexpr float kLowest = Word16<T>::kMinusInf == 0xFC00FC00u ? -64000.0f : -2e38f;      // (float16 ends at 65504)
+  static constexpr float kLowest = Word16<T>::kMinusInf == 0xFC00FC00u ? -64000.0f : -1e7f, kHighest = 1e7f;      // (float16 ends at 65504)
   float peak, ref, limit;
   uint32_t floor;
   Float2 s, a;
-  int far;
+  bool differences;                    // t = (z - ref) log2 e
 
   __device__ __forceinline__ void init() {
     peak = limit = -INFINITY;          // (no reference yet: every finite logit is above the limit)
     ref = 0.0f;
     floor = Word16<T>::twice(-140.0f);
     s = a = pack2(0.0f, 0.0f);
-    far = 0;
+    differences = false;
   }
   // `big`: the thread's largest value of what comes next (NaN if there is one).  The whole warp calls it.
   __device__ __forceinline__ void move_reference(float big) {
@@ -125,17 +126,16 @@ struct LogprobThread {
     }
     const float to = order_value(__reduce_max_sync(0xffffffffu, order_bits(big)));
     if (!(to > limit)) return;
-    if (to < kLowest) {
-      far |= kFarDown;
-      return;
-    }
-    if (to > 2e38f) far |= kFarUp;
-    const float r = rintf(to * kLog2e);
+    const bool far = to < kLowest || to > kHighest;
+    const float r = far ? to : rintf(to * kLog2e);
     if (limit > -INFINITY) {
-      const float d = ref - r, f = exp2_fast(d);
+      float d = differences ? (far ? (ref - r) * kLog2e : fmaf(ref, kLog2e, -r)) : (far ? -fmaf(r, kLog2e, -ref) : ref - r);
+      d = fmaxf(d, -1e4f);             // (finite)
+      const float f = exp2_fast(d);
       s = mul2(s, pack2(f, f));
-      a = fma2(s, pack2(d, d), mul2(a, pack2(f, f)));      // (d is -infinity at most where `far` is set)
+      a = fma2(s, pack2(d, d), mul2(a, pack2(f, f)));
     }
+    differences = far;
     ref = r;
     limit = to + 8.0f / kLog2e;
     floor = Word16<T>::twice(to - fmaxf(140.0f, fabsf(to) * 0.015625f));
@@ -160,6 +160,19 @@ struct LogprobThread {
 #pragma unroll
     for (int j = 0; j < Word16<T>::kCount; j += 2) add_pair(pack2(x[j], x[j + 1]));
   }
+  // The same by differences.
+  __device__ __forceinline__ void add_pair_far(float z0, float z1) {
+    const float t0 = max_nan((z0 - ref) * kLog2e, -200.0f), t1 = max_nan((z1 - ref) * kLog2e, -200.0f);
+    const Float2 e = pack2(exp2_fast(t0), exp2_fast(t1));
+    s = add2(s, e);
+    a = fma2(e, pack2(t0, t1), a);
+  }
+  __device__ __forceinline__ void add_word_far(const uint4& w) {
+    float x[Word16<T>::kCount];
+    Word16<T>::unpack(w, x);
+#pragma unroll
+    for (int j = 0; j < Word16<T>::kCount; j += 2) add_pair_far(x[j], x[j + 1]);
+  }
   // The warp's sums, against its largest logit.
   __device__ __forceinline__ SoftmaxPart warp_part() const {
     float s0, s1, a0, a1;
@@ -172,7 +185,7 @@ struct LogprobThread {
       p.a += __shfl_xor_sync(0xffffffffu, p.a, off);
     }
     if (p.peak > -INFINITY && p.s != 0.0f) {
-      const float d = fmaf(-p.peak, kLog2e, ref), f = exp2_fast(d);
+      const float d = differences ? (ref - p.peak) * kLog2e : fmaf(-p.peak, kLog2e, ref), f = exp2_fast(d);
       p.a = f * fmaf(d, p.s, p.a);
       p.s *= f;
     }
@@ -206,13 +219,6 @@ __device__ __forceinline__ float largest_of(const uint4 (&w)[N]) {
       for (int u = 0; u < n; ++u) m[u] = Word::at_least(m[u], m[u + n]);
     return Word::widest(m[0]);
   }
-}
-
-// One element by differences from the largest so far (rows that are `far`, see above).
-__device__ __forceinline__ void add_far(SoftmaxPart& p, float z) {
-  if (z == -INFINITY) return;
-  const SoftmaxPart one = {z, z < INFINITY ? 1.0f : NAN, 0.0f};
-  p = join_parts(p, one);
 }
 
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -435,17 +441,6 @@ struct RowShare {
   __device__ __forceinline__ int behind(uint32_t rank, uint32_t size, int cols) const { return rank == size - 1 ? cols : head + end * Word16<T>::kCount; }
 };
 
-// The sums of a CTA's share by differences.  All threads; the result is in warp_part.
-template <typename T>
-__device__ __noinline__ void far_sums(const T* z, int first, int behind, SoftmaxPart* warp_part) {
-  __syncthreads();                               // (everybody has looked at warp_part)
-  SoftmaxPart p = {-INFINITY, 0.0f, 0.0f};
-  for (int c = first + threadIdx.x; c < behind; c += kLpThreads) add_far(p, to_float(z[c]));
-  p = join_lanes<32>(p);
-  if ((threadIdx.x & 31) == 0) warp_part[threadIdx.x >> 5] = p;
-  __syncthreads();
-}
-
 // The candidates of a CTA's share when they have overflowed.  All threads; true: they are in the list, false: top.best is done.
 template <typename T>
 __device__ __noinline__ bool collect_again(const T* z, int first, int behind, LogprobTop& top, int* count, unsigned long long* keys, int k) {
@@ -490,7 +485,6 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprob_kernel(Logpr
   extern __shared__ __align__(16) uint4 ring[];           // stages x kLpWords x threads
   __shared__ SoftmaxPart warp_part[2][kLpWarps];          // by the parity of the row
   __shared__ SoftmaxPart cta_part;
-  __shared__ int far_rows[3];
   __shared__ __align__(16) unsigned char top_bytes[TOP ? sizeof(LogprobTop) : 16];
   LogprobTop& top = *reinterpret_cast<LogprobTop*>(top_bytes);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -520,10 +514,7 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprob_kernel(Logpr
     }
     copies_commit();
   };
-  if (threadIdx.x < 3) {
-    far_rows[threadIdx.x] = 0;
-    if (TOP) top.count[threadIdx.x] = 0;
-  }
+  if (TOP && threadIdx.x < 3) top.count[threadIdx.x] = 0;
 #pragma unroll
   for (int s = 0; s < kStages; ++s) issue(s);
   __syncthreads();
@@ -578,8 +569,13 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprob_kernel(Logpr
       const float biggest = largest_of<T>(w);
       t.peak = fmaxf(t.peak, biggest);
       if (__any_sync(0xffffffffu, !(biggest <= t.limit))) t.move_reference(biggest);
+      if (t.differences) {
 #pragma unroll
-      for (int u = 0; u < kLpWords; ++u) t.add_word(w[u]);
+        for (int u = 0; u < kLpWords; ++u) t.add_word_far(w[u]);
+      } else {
+#pragma unroll
+        for (int u = 0; u < kLpWords; ++u) t.add_word(w[u]);
+      }
 
       if constexpr (TOP) {
         if (iteration > 0) {
@@ -620,28 +616,17 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprob_kernel(Logpr
       t.peak = fmaxf(t.peak, v);
       if (__any_sync(0xffffffffu, !(v <= t.limit))) t.move_reference(v);
       constexpr uint32_t kNone = Word16<T>::kMinusInf;
-      t.add_word(make_uint4(Word16<T>::first(edge), kNone, kNone, kNone));
+      if (t.differences) t.add_pair_far(v, -INFINITY);
+      else t.add_word(make_uint4(Word16<T>::first(edge), kNone, kNone, kNone));
       if (TOP && edge_index >= 0) push_candidate(count, keys, v, (uint32_t)edge_index);
     }
     const SoftmaxPart mine = t.warp_part();
     if (lane == 0) warp_part[parity][warp] = mine;
-    if (t.far) atomicOr(&far_rows[third], t.far);
     __syncthreads();
 
-    // Everybody has read the row before's marks and counts on the way here; their place is used again by the row after the
-    // next, which begins behind the next one's barrier.
-    if (threadIdx.x == 0) {
-      const int before = third == 0 ? 2 : third - 1;
-      far_rows[before] = 0;
-      if (TOP) top.count[before] = 0;
-    }
-    int far = far_rows[third];
-    if (far == kFarDown) {
-      float largest = -INFINITY;
-      for (int i = 0; i < kLpWarps; ++i) largest = fmaxf(largest, warp_part[parity][i].peak);
-      if (largest >= LogprobThread<T>::kLowest) far = 0;
-    }
-    if (far) far_sums<T>(z, share.first(rank), share.behind(rank, size, cols), warp_part[parity]);
+    // Everybody has read the row before's count on the way here; its place is used again by the row after the next, which begins
+    // behind the next one's barrier.
+    if (TOP && threadIdx.x == 0) top.count[third == 0 ? 2 : third - 1] = 0;
     bool listed = true;                                   // the candidates are in the list
     if (TOP && *count > kLpCandidates) listed = collect_again<T>(z, share.first(rank), share.behind(rank, size, cols), top, count, keys, a.top_k);
 
@@ -832,8 +817,13 @@ __global__ void __launch_bounds__(kLpThreads, (lp_warp_ctas<T, TOP>)) logprob_wa
       const float biggest = largest_of<T>(w);
       t.peak = fmaxf(t.peak, biggest);
       if (__any_sync(0xffffffffu, !(biggest <= t.limit))) t.move_reference(biggest);
+      if (t.differences) {
 #pragma unroll
-      for (int u = 0; u < kWords; ++u) t.add_word(w[u]);
+        for (int u = 0; u < kWords; ++u) t.add_word_far(w[u]);
+      } else {
+#pragma unroll
+        for (int u = 0; u < kWords; ++u) t.add_word(w[u]);
+      }
       if constexpr (TOP) {
         const bool first = iteration == 0;
         if (first) {                                      // compared with its own threshold: equal values enter
@@ -880,16 +870,11 @@ __global__ void __launch_bounds__(kLpThreads, (lp_warp_ctas<T, TOP>)) logprob_wa
       const float v = to_float(edge);
       t.peak = fmaxf(t.peak, v);
       if (__any_sync(0xffffffffu, !(v <= t.limit))) t.move_reference(v);
-      t.add_word(make_uint4(Word16<T>::first(edge), kNone, kNone, kNone));
+      if (t.differences) t.add_pair_far(v, -INFINITY);
+      else t.add_word(make_uint4(Word16<T>::first(edge), kNone, kNone, kNone));
       if (TOP) append(edge_index >= 0, v, edge_index);
     }
-    SoftmaxPart part = t.warp_part();
-    const int far = (int)__reduce_or_sync(0xffffffffu, (uint32_t)t.far);
-    if (far && !(far == kFarDown && part.peak >= LogprobThread<T>::kLowest)) {       // (see LogprobThread)
-      part = {-INFINITY, 0.0f, 0.0f};
-      for (int c = lane; c < cols; c += 32) add_far(part, to_float(z[c]));
-      part = join_lanes<32>(part);
-    }
+    const SoftmaxPart part = t.warp_part();
     const bool empty = part.peak == -INFINITY && part.s == 0.0f;
     const float log_s = empty ? 0.0f : logf(part.s);
     if (lane == 0) {

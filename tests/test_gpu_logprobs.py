@@ -336,3 +336,38 @@ def test_refusals():
         with pytest.raises(binding.SolonError) as err:
             call()
         assert err.value.status == binding.ERR_INVALID_ARG
+
+
+HUGE = [1.2e7, 5e7, 1e9, 2e9, 3e9, 1e10, 1e12, 1e30, 1e38]
+
+
+def _rows_with(value, cols, dtype):
+    """Ordinary logits beside `value` and its neighbours (steps of 1 and of the type's spacing), a row a pattern."""
+    g = torch.Generator(device="cuda").manual_seed(13)
+    ordinary = torch.randn(cols, device="cuda", generator=g) * 3
+    full = torch.full((cols,), value, device="cuda")
+    at = torch.arange(cols, device="cuda")
+    low = torch.full((cols,), -abs(value), device="cuda")
+    step = max(1.0, abs(value) * torch.finfo(dtype).eps)
+    near = full + torch.randint(-3, 4, (cols,), device="cuda", generator=g) * step
+    far = torch.tensor([-1e38, -1e30, -1e10, -1e9, -1.2e7, -1e4, 0.0, 5.0], device="cuda")[at * 8 // cols]
+    rows = [full, near, torch.where(at < cols * 3 // 4, low, ordinary), torch.where(at < cols // 3, ordinary, low),
+            torch.where(at == cols - 1, ordinary, low), torch.where(at == cols // 2, ordinary, low), torch.where(at % 5 == 0, ordinary, near), far,
+            torch.where(at == cols // 3, full, ordinary), near.sort().values]
+    return torch.stack(rows).to(dtype)
+
+
+@pytest.mark.parametrize("rows,cols", [(10, 50), (10, 3000), (1, 70_001), (400, 16_384), (1800, 5000)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("value", [s * v for v in HUGE for s in (1, -1)] + [9.9e6, -9.9e6, -1e6])
+def test_logits_of_large_magnitude(value, dtype, rows, cols):
+    """Finite logits far from 0: masks other than the type's lowest value - throughout a row, over its first thousands of columns, all but
+    one -, and rows whose values all lie there."""
+    z = _rows_with(value, cols, TYPES[dtype][0])
+    z = z.repeat(-(-rows // len(z)), 1)[:rows] if rows > 1 else z
+    targets = torch.randint(0, cols, (len(z),), device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    targets[::3] = cols // 3
+    for part in z.split(1 if rows == 1 else rows):
+        own = targets[:len(part)]
+        for k in (0, 5, 32):
+            _check(part, own, k, binding.solon_token_logprobs(part, own, top_k=k))
