@@ -344,8 +344,9 @@ int solon_layernorm_backward(const void* dy, int64_t dy_pitch, const void* x, in
  *             likeliest tokens in falling order, of equal logits the lower token first; top_k <= SOLON_MAX_TOP, vocab
  * A logit of -infinity is a token masked out: p = 0.  A row with nothing left has peak = logp =
  * -infinity and log_sum = entropy = 0.
- * A target >= vocab is not read; its logp is NaN.  NaN or +infinity among the logits make the row's results NaN; NaN
- * ranks above every number among the likeliest tokens. */
+ * A target >= vocab is not read; its logp is NaN.  NaN or +infinity among the logits make the row's results NaN (but peak is
+ * +infinity where that is the largest and there is no NaN, and a row without target has logp 0); NaN ranks above every
+ * number among the likeliest tokens. */
 int solon_token_logprobs(const void* logits, int64_t pitch, int dtype, const int64_t* targets, int64_t rows, int64_t vocab, int top_k, float* logp,
                          float* entropy, float* peak, float* log_sum, int64_t* top_ids, float* top_logp, void* cuda_stream);
 

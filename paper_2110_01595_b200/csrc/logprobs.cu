@@ -8,8 +8,8 @@
 //
 // Edge cases, the same in both directions: a logit of -infinity has p = 0 and adds nothing (0 log 0 = 0); a row of nothing
 // but -infinity has M = logp = -infinity, log S = H = 0 and gradient 0; a negative target has logp 0 and passes no
-// gradient; a target beyond the vocabulary is not read and has logp NaN; NaN and +infinity make the row's results NaN.  A
-// probability below 2^-126 counts as 0.
+// gradient; a target beyond the vocabulary is not read and has logp NaN; NaN and +infinity make the row's results NaN, but M is
+// +infinity where that is the largest.  A probability below 2^-126 counts as 0.
 #include <math.h>
 
 #include "elements.cuh"
@@ -81,8 +81,10 @@ __device__ __forceinline__ SoftmaxPart join_parts(const SoftmaxPart& x, const So
   r.a = (has_x ? fx * fmaf(dx, x.s, x.a) : 0.0f) + (has_y ? fy * fmaf(dy, y.s, y.a) : 0.0f);
   return r;
 }
+// (the peak is NaN if one part's is; s is then NaN as well)
 template <int LANES>
 __device__ __forceinline__ SoftmaxPart join_lanes(SoftmaxPart p) {
+  const bool nan = __any_sync(0xffffffffu, p.peak != p.peak);
 #pragma unroll
   for (int off = LANES / 2; off > 0; off >>= 1) {
     SoftmaxPart o;
@@ -91,6 +93,7 @@ __device__ __forceinline__ SoftmaxPart join_lanes(SoftmaxPart p) {
     o.a = __shfl_xor_sync(0xffffffffu, p.a, off);
     p = join_parts(p, o);
   }
+  if (nan) p.peak = NAN;
   return p;
 }
 
@@ -110,17 +113,19 @@ struct LogprobThread {
   uint32_t floor;
   Float2 s, a;
   bool differences;                    // t = (z - ref) log2 e
+  bool nan;                            // one was seen (it has no part in peak)
 
   __device__ __forceinline__ void init() {
     peak = limit = -INFINITY;          // (no reference yet: every finite logit is above the limit)
     ref = 0.0f;
     floor = Word16<T>::twice(-140.0f);
     s = a = pack2(0.0f, 0.0f);
-    differences = false;
+    differences = nan = false;
   }
   // `big`: the thread's largest value of what comes next (NaN if there is one).  The whole warp calls it.
   __device__ __forceinline__ void move_reference(float big) {
     if (!(big < INFINITY)) {           // +infinity or NaN: the row has no softmax
+      nan |= big != big;
       s = pack2(NAN, NAN);
       big = -INFINITY;
     }
@@ -173,7 +178,7 @@ struct LogprobThread {
 #pragma unroll
     for (int j = 0; j < Word16<T>::kCount; j += 2) add_pair_far(x[j], x[j + 1]);
   }
-  // The warp's sums, against its largest logit.
+  // The warp's sums, against its largest logit (NaN if there is one).
   __device__ __forceinline__ SoftmaxPart warp_part() const {
     float s0, s1, a0, a1;
     unpack2(s, s0, s1);
@@ -189,6 +194,7 @@ struct LogprobThread {
       p.a = f * fmaf(d, p.s, p.a);
       p.s *= f;
     }
+    if (__any_sync(0xffffffffu, nan)) p.peak = NAN;
     return p;
   }
 };

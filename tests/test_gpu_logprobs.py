@@ -371,3 +371,26 @@ def test_logits_of_large_magnitude(value, dtype, rows, cols):
         own = targets[:len(part)]
         for k in (0, 5, 32):
             _check(part, own, k, binding.solon_token_logprobs(part, own, top_k=k))
+
+
+@pytest.mark.parametrize("rows,cols", [(4, 300), (4, 40_000), (1, 131_072), (400, 9000), (2400, 4000)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_peak_of_rows_that_hold_nan(rows, cols, dtype):
+    """The largest logit as an elementary maximum has it: NaN where there is one, +infinity where there is that."""
+    z, targets = _logits(rows, cols, dtype, 14, masked=0.3)
+    for place in (0, cols // 2, cols - 1):
+        for values, want in (([float("nan")], float("nan")), ([INF], INF), ([INF, float("nan")], float("nan")), ([-INF, float("nan")], float("nan"))):
+            q = z.clone()
+            if values[0] == -INF:
+                q[::2] = -INF
+            q[::2, place] = values[-1]
+            if values[0] == INF:
+                q[::2, cols // 3] = INF
+            for k in (0, 3):
+                got = binding.solon_token_logprobs(q, targets, top_k=k)
+                assert torch.equal(got.peak.isnan(), q.float().amax(1).isnan()) and got.peak.isnan()[::2].all() == (want != want)
+                assert torch.equal(got.peak.nan_to_num(nan=7.0, posinf=8.0), q.float().amax(1).nan_to_num(nan=7.0, posinf=8.0))
+                assert got.log_sum[::2].isnan().all() and got.entropy[::2].isnan().all() and got.logp[::2].isnan().all()
+                if rows > 1:
+                    kept = [None if x is None else x[1::2] for x in got]
+                    _check(q[1::2], targets[1::2], k, binding.TokenLogprobs(*kept))
