@@ -104,23 +104,25 @@ __device__ __forceinline__ SoftmaxPart join_lanes(SoftmaxPart p) {
 // That holds for references of logits up to 1e7.  From 2^24 / log2 e = 1.16e7 on the integers of float32 lie 2 and more apart (at 1e10
 // 1024), so the largest logit's own t can be that far from 0, which costs digits and then overflows or leaves nothing; next to
 // float16's lowest value there is no floor.  Such a row - masked with a large finite value, until something else turns up -
-// takes differences from a logit, which are exact or their 2^t is 0 (2047 x 50001 float32 71 us with every 50th row
-// all -1e9 and without).
+// takes differences from a logit, which are exact or their 2^t is 0; `limit` is NaN then, so that every iteration of such
+// a row, and of no other, is told apart behind the comparison that all make (2047 x 50001 float32 72 us with every 50th row
+// all -1e9 and without; a branch of its own in every iteration made 8192 x 32768 bfloat16 2 us longer).
 template <typename T>
 struct LogprobThread {
   static constexpr float kLowest = Word16<T>::kMinusInf == 0xFC00FC00u ? -64000.0f : -1e7f, kHighest = 1e7f;      // (float16 ends at 65504)
   float peak, ref, limit;
   uint32_t floor;
   Float2 s, a;
-  bool differences;                    // t = (z - ref) log2 e
   bool nan;                            // one was seen (it has no part in peak)
+
+  __device__ __forceinline__ bool differences() const { return limit != limit; }      // t = (z - ref) log2 e
 
   __device__ __forceinline__ void init() {
     peak = limit = -INFINITY;          // (no reference yet: every finite logit is above the limit)
     ref = 0.0f;
     floor = Word16<T>::twice(-140.0f);
     s = a = pack2(0.0f, 0.0f);
-    differences = nan = false;
+    nan = false;
   }
   // `big`: the thread's largest value of what comes next (NaN if there is one).  The whole warp calls it.
   __device__ __forceinline__ void move_reference(float big) {
@@ -130,19 +132,18 @@ struct LogprobThread {
       big = -INFINITY;
     }
     const float to = order_value(__reduce_max_sync(0xffffffffu, order_bits(big)));
-    if (!(to > limit)) return;
-    const bool far = to < kLowest || to > kHighest;
+    const bool was_far = differences(), far = to < kLowest || to > kHighest;
+    if (!(to > (was_far ? ref + 8.0f / kLog2e : limit))) return;
     const float r = far ? to : rintf(to * kLog2e);
-    if (limit > -INFINITY) {
-      float d = differences ? (far ? (ref - r) * kLog2e : fmaf(ref, kLog2e, -r)) : (far ? -fmaf(r, kLog2e, -ref) : ref - r);
+    if (was_far || limit > -INFINITY) {
+      float d = was_far ? (far ? (ref - r) * kLog2e : fmaf(ref, kLog2e, -r)) : (far ? -fmaf(r, kLog2e, -ref) : ref - r);
       d = fmaxf(d, -1e4f);             // (finite)
       const float f = exp2_fast(d);
       s = mul2(s, pack2(f, f));
       a = fma2(s, pack2(d, d), mul2(a, pack2(f, f)));
     }
-    differences = far;
     ref = r;
-    limit = to + 8.0f / kLog2e;
+    limit = far ? NAN : to + 8.0f / kLog2e;
     floor = Word16<T>::twice(to - fmaxf(140.0f, fabsf(to) * 0.015625f));
   }
   // Two elements: t = z log2 e - ref, none above the limit.
@@ -190,7 +191,7 @@ struct LogprobThread {
       p.a += __shfl_xor_sync(0xffffffffu, p.a, off);
     }
     if (p.peak > -INFINITY && p.s != 0.0f) {
-      const float d = differences ? (ref - p.peak) * kLog2e : fmaf(-p.peak, kLog2e, ref), f = exp2_fast(d);
+      const float d = differences() ? (ref - p.peak) * kLog2e : fmaf(-p.peak, kLog2e, ref), f = exp2_fast(d);
       p.a = f * fmaf(d, p.s, p.a);
       p.s *= f;
     }
@@ -574,8 +575,17 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprob_kernel(Logpr
       }
       const float biggest = largest_of<T>(w);
       t.peak = fmaxf(t.peak, biggest);
-      if (__any_sync(0xffffffffu, !(biggest <= t.limit))) t.move_reference(biggest);
-      if (t.differences) {
+      if (__any_sync(0xffffffffu, !(biggest <= t.limit))) {
+        t.move_reference(biggest);
+        if (!TOP && t.differences()) {
+#pragma unroll
+          for (int u = 0; u < kLpWords; ++u) t.add_word_far(w[u]);
+          issue(stage);
+          stage = stage + 1 == kStages ? 0 : stage + 1;
+          continue;
+        }
+      }
+      if (TOP && t.differences()) {                       // (the words are still wanted below)
 #pragma unroll
         for (int u = 0; u < kLpWords; ++u) t.add_word_far(w[u]);
       } else {
@@ -622,7 +632,7 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprob_kernel(Logpr
       t.peak = fmaxf(t.peak, v);
       if (__any_sync(0xffffffffu, !(v <= t.limit))) t.move_reference(v);
       constexpr uint32_t kNone = Word16<T>::kMinusInf;
-      if (t.differences) t.add_pair_far(v, -INFINITY);
+      if (t.differences()) t.add_pair_far(v, -INFINITY);
       else t.add_word(make_uint4(Word16<T>::first(edge), kNone, kNone, kNone));
       if (TOP && edge_index >= 0) push_candidate(count, keys, v, (uint32_t)edge_index);
     }
@@ -822,8 +832,17 @@ __global__ void __launch_bounds__(kLpThreads, (lp_warp_ctas<T, TOP>)) logprob_wa
       }
       const float biggest = largest_of<T>(w);
       t.peak = fmaxf(t.peak, biggest);
-      if (__any_sync(0xffffffffu, !(biggest <= t.limit))) t.move_reference(biggest);
-      if (t.differences) {
+      if (__any_sync(0xffffffffu, !(biggest <= t.limit))) {
+        t.move_reference(biggest);
+        if (!TOP && t.differences()) {
+#pragma unroll
+          for (int u = 0; u < kWords; ++u) t.add_word_far(w[u]);
+          issue(stage);
+          stage = stage == ring + (kStages - 1) * kChunk ? ring : stage + kChunk;
+          continue;
+        }
+      }
+      if (TOP && t.differences()) {                       // (the words are still wanted below)
 #pragma unroll
         for (int u = 0; u < kWords; ++u) t.add_word_far(w[u]);
       } else {
@@ -876,7 +895,7 @@ __global__ void __launch_bounds__(kLpThreads, (lp_warp_ctas<T, TOP>)) logprob_wa
       const float v = to_float(edge);
       t.peak = fmaxf(t.peak, v);
       if (__any_sync(0xffffffffu, !(v <= t.limit))) t.move_reference(v);
-      if (t.differences) t.add_pair_far(v, -INFINITY);
+      if (t.differences()) t.add_pair_far(v, -INFINITY);
       else t.add_word(make_uint4(Word16<T>::first(edge), kNone, kNone, kNone));
       if (TOP) append(edge_index >= 0, v, edge_index);
     }
