@@ -650,13 +650,20 @@ __global__ void __launch_bounds__(256) adam_moments_kernel(const uint4* __restri
 
 // ---- host ------------------------------------------------------------------------------------------------------------
 
+// A copy to the device that has arrived when the call returns, whichever stream the next step goes to: from pageable memory
+// cudaMemcpy alone may return when the bytes are staged, and streams made without blocking are not ordered behind it.
+static int adam_upload(void* to, const void* from, size_t bytes) {
+  if (bytes) SOLON_CUDA_TRY(cudaMemcpy(to, from, bytes, cudaMemcpyHostToDevice));
+  SOLON_CUDA_TRY(cudaDeviceSynchronize());
+  return SOLON_OK;
+}
+
 static int adam_upload_scalars(solon_adamw* o, int64_t step) {
   AdamScalars s = {};
   s.b1t = pow(o->beta1, (double)step);
   s.b2t = pow(o->beta2, (double)step);
   s.applied = step;
-  SOLON_CUDA_TRY(cudaMemcpy(o->d_scalars, &s, sizeof(s), cudaMemcpyHostToDevice));
-  return SOLON_OK;
+  return adam_upload(o->d_scalars, &s, sizeof(s));
 }
 
 static void adam_free(solon_adamw* o) {
@@ -678,8 +685,7 @@ static int adam_alloc(T** ptr, size_t count) {
 static int64_t adam_blocks(int64_t numel) { return (numel + kAdamBlock - 1) / kAdamBlock; }
 
 static int adam_upload_chunks(solon_adamw* o) {
-  if (!o->chunks.empty()) SOLON_CUDA_TRY(cudaMemcpy(o->d_chunks, o->chunks.data(), o->chunks.size() * sizeof(AdamChunk), cudaMemcpyHostToDevice));
-  return SOLON_OK;
+  return adam_upload(o->d_chunks, o->chunks.data(), o->chunks.size() * sizeof(AdamChunk));
 }
 
 static int adam_create(solon_adamw* o, const int64_t* numel, float* const* params, void* const* copies, const float* weight_decay) {

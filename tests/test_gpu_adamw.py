@@ -419,3 +419,31 @@ def test_refusals():
                 call()
             assert err.value.status == binding.ERR_INVALID_ARG
         assert opt.steps() == (0, 0)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_handles_made_bound_and_resumed_inside_another_stream(bits):
+    """What the host uploads - chunk table, bound gradients, step count - has arrived before a step that is enqueued next on a stream
+    that does not wait for the default one."""
+    flat, views, grad = _setup(SIZES, 41, 1)
+    flat2, views2, _ = _setup(SIZES, 41, 1)
+    grads = list(grad.split(SIZES))
+    other = [(-2 * g).clone() for g in grads]
+    want = binding.AdamW(views, bits=bits, seed=3)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = binding.AdamW(views2, bits=bits, seed=3)
+        for bound, count in ((grads, None), (other, None), (grads, 700), (other, 3), (grads, 0)):
+            got.bind_grads(bound)
+            if count is not None:
+                got.set_step(count)
+            got.step(None, lr=1e-2, max_norm=1.0)
+    side.synchronize()
+    for bound, count in ((grads, None), (other, None), (grads, 700), (other, 3), (grads, 0)):
+        want.bind_grads(bound)
+        if count is not None:
+            want.set_step(count)
+        want.step(None, lr=1e-2, max_norm=1.0)
+    assert want.steps() == got.steps() == (1, 0) and torch.equal(flat, flat2)
+    assert all(torch.equal(x, y) for x, y in zip(want.state, got.state) if x is not None)
