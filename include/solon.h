@@ -389,7 +389,8 @@ int solon_adamw_create(int n_tensors, const int64_t* numel, float* const* params
 int solon_adamw_destroy(solon_adamw* opt);
 
 /* Gradients that live in tensors of their own (host array of device pointers, SOLON_F32, SOLON_F64 or SOLON_BF16), read in
- * place by the steps that are given no flat gradient.  Synchronises. */
+ * place by the steps that are given no flat gradient.  Synchronises.  Refused arguments leave the earlier ones bound; if the
+ * upload fails, none are. */
 int solon_adamw_bind_grads(solon_adamw* opt, const void* const* grads, int grad_dtype);
 
 /* One step.

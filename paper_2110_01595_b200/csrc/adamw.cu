@@ -804,6 +804,7 @@ int solon_adamw_bind_grads(solon_adamw* opt, const void* const* grads, int grad_
   for (int i = 0; i < opt->n_tensors; ++i)
     if (opt->numel[(size_t)i] > 0 && (!grads[i] || ((uintptr_t)grads[i] & (size - 1)))) return SOLON_ERR_INVALID_ARG;
   SOLON_CUDA_TRY(cudaDeviceSynchronize());     // steps in flight read the table
+  opt->grads_bound = 0;                        // until the new ones have arrived: a copy that fails may leave some of each
   size_t chunk = 0;
   for (int i = 0; i < opt->n_tensors; ++i)
     for (int64_t first = 0; first < opt->numel[(size_t)i]; first += kAdamChunk) opt->chunks[chunk++].grad = static_cast<const char*>(grads[i]) + first * (int64_t)size;

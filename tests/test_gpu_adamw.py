@@ -447,3 +447,18 @@ def test_handles_made_bound_and_resumed_inside_another_stream(bits):
         want.step(None, lr=1e-2, max_norm=1.0)
     assert want.steps() == got.steps() == (1, 0) and torch.equal(flat, flat2)
     assert all(torch.equal(x, y) for x, y in zip(want.state, got.state) if x is not None)
+
+
+def test_a_refused_binding_leaves_the_earlier_one():
+    p, g = torch.zeros(3000, device="cuda"), _randn(3000, 51)
+    with binding.AdamW([p]) as opt:
+        with pytest.raises(binding.SolonError):
+            opt.bind_grads([g.half()])
+        with pytest.raises(binding.SolonError):
+            opt.step()
+        opt.bind_grads([g])
+        for refused in (lambda: opt.bind_grads([g.half()]), lambda: opt.bind_grads([g[:7]]), lambda: opt.bind_grads([])):
+            with pytest.raises((binding.SolonError, ValueError, IndexError)):
+                refused()
+        opt.step(lr=0.5)
+        assert (p.sign() == -g.sign()).all() and opt.steps() == (1, 0)
