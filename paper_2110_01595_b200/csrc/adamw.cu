@@ -38,7 +38,8 @@ struct alignas(64) AdamChunk {
   int64_t slot;              // first element in the state
   int count;                 // elements
   float weight_decay;
-  int ends;                  // 1: the tensor's first chunk, 2: its last
+  int starts;                // the tensor's first chunk
+  int behind;                // elements of the tensor behind the chunk, up to three
 };
 
 // What the update reads, written by the control kernel of the same step.
@@ -282,8 +283,8 @@ struct AdamStepArgs {
 // group is put together from the two aligned words that hold it, and parameters go back as aligned words too.  Single
 // accesses of four bytes move the same bytes in four times as many requests, which caps what is on the way: 11.2 M weights of
 // an odd offset take 63 us that way, 55 us from aligned words, 49 us where they are aligned.  The aligned words reach up to three
-// elements beyond the block, so a tensor's first and last block, and blocks that are not full, go element by element (every 32nd a
-// lane's).
+// elements beyond the block, so a tensor's first block, full blocks with fewer than three elements of the tensor behind them, and
+// blocks that are not full go element by element (every 32nd a lane's).
 enum BlockMode { kSingle, kAligned, kShifted };
 
 template <bool VEC>
@@ -616,7 +617,7 @@ __global__ void __launch_bounds__(kAdamThreads, 4) adam_step_kernel(AdamStepArgs
   const G* grad = a.flat ? static_cast<const G*>(a.flat) + ch.offset : static_cast<const G*>(ch.grad);
   const bool aligned = ((uintptr_t)ch.p & 15) == 0 && ((uintptr_t)ch.copy & 7) == 0 && ((uintptr_t)grad & (sizeof(G) < 4 ? 7 : 15)) == 0;
   const bool full = left >= kAdamBlock;
-  const bool inside = full && !(first == 0 && (ch.ends & 1)) && !(left == kAdamBlock && (ch.ends & 2));
+  const bool inside = full && !(first == 0 && ch.starts) && left - kAdamBlock + ch.behind >= 3;
   pdl_wait();
   if (left <= 0 || a.scalars->skip) return;
   if (aligned && full) adam_block<BITS, G, kAligned>(a, ch, grad, first, lane, kAdamBlock);
@@ -699,7 +700,9 @@ static int adam_create(solon_adamw* o, const int64_t* numel, float* const* param
       c.slot = o->n_blocks * kAdamBlock + first;
       c.count = (int)(numel[i] - first < kAdamChunk ? numel[i] - first : kAdamChunk);
       c.weight_decay = weight_decay ? weight_decay[i] : 0.0f;
-      c.ends = (first == 0 ? 1 : 0) | (first + kAdamChunk >= numel[i] ? 2 : 0);
+      c.starts = first == 0;
+      const int64_t behind = numel[i] - first - c.count;
+      c.behind = (int)(behind < 3 ? behind : 3);
       o->chunks.push_back(c);
     }
     o->total += numel[i];

@@ -462,3 +462,28 @@ def test_a_refused_binding_leaves_the_earlier_one():
                 refused()
         opt.step(lr=0.5)
         assert (p.sign() == -g.sign()).all() and opt.steps() == (1, 0)
+
+
+@pytest.mark.parametrize("grad_type", [torch.float32, torch.float64, torch.bfloat16])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_tensors_that_end_just_behind_a_block(bits, grad_type):
+    """Sizes of 0 to 4 elements more than whole blocks and chunks, off 16-byte boundaries: as with tensors on them, bit for bit, and
+    nothing beside them changes."""
+    for whole in (256, 512, 2048, 4096):
+        for extra in (0, 1, 2, 3, 4):
+            n = whole + extra
+            p, g = _randn(n, 61), _randn(n, 62).to(grad_type)
+            own = p.clone()
+            want = binding.AdamW([own], bits=bits, seed=9)
+            for _ in range(2):
+                want.step(g.clone(), lr=1e-2, max_norm=0.5)
+            for offset in (1, 2, 3):
+                buf, gbuf = torch.full((n + 16,), float("nan"), device="cuda"), torch.full((n + 16,), float("nan"), dtype=grad_type, device="cuda")
+                view, grad = buf[4 + offset:4 + offset + n], gbuf[8 - offset:8 - offset + n]
+                view.copy_(p)
+                grad.copy_(g)
+                with binding.AdamW([view], bits=bits, seed=9) as opt:
+                    for _ in range(2):
+                        opt.step(grad, lr=1e-2, max_norm=0.5)
+                    assert torch.equal(view, own) and all(torch.equal(x, y) for x, y in zip(opt.state, want.state) if x is not None)
+                assert buf.isnan().sum() == 16 and gbuf.isnan().sum() == 16
