@@ -276,6 +276,7 @@ struct AdamStepArgs {
   int16_t* base;               // two per block: m's, v's (8-bit states)
   const AdamScalars* scalars;
   float beta1, one_minus_beta1, beta2, one_minus_beta2, eps, lr;
+  float quotient_scale;        // a power of two on both sides of the step's quotient (eps has it already)
 };
 
 // How a warp goes through its block.  A lane has two groups of four consecutive elements; where parameters or gradients do not
@@ -400,7 +401,9 @@ __device__ __forceinline__ void store8(T* p, const T (&x)[8], int lane, int n) {
 }
 
 // The hardware's square root and quotient (one and two units in the last place): the update is rounded by far less than
-// the state's own width, and the exact forms cost a quarter of the 8-bit step's instructions.
+// the state's own width, and the exact forms cost a quarter of the 8-bit step's instructions.  The quotient asks for a denominator
+// between 2^-126 and 2^126 (above, it is 0): sqrt(v) stays below 2^64 and its factor below 2^27, so only eps can leave that range;
+// then both sides carry a power of two (solon_adamw_step).
 __device__ __forceinline__ float sqrt_fast(float x) {
   float r;
   asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -533,11 +536,11 @@ __device__ __forceinline__ void adam_block(const AdamStepArgs& a, const AdamChun
     codes.load((const uint8_t*)a.exp_avg + slot, (const uint8_t*)a.exp_avg_sq + slot, lane);
     base = load_pack<int16_t, 2>(a.base + 2 * block);
   }
-  const float inv_sqrt_bc2 = a.scalars->inv_sqrt_bc2;
+  const float inv_sqrt_bc2 = a.scalars->inv_sqrt_bc2 * a.quotient_scale;
   const Float2 grad_scale = pack2(a.scalars->grad_scale, a.scalars->grad_scale), clip = pack2(a.scalars->clip, a.scalars->clip);
   const Float2 b1 = pack2(a.beta1, a.beta1), c1 = pack2(a.one_minus_beta1, a.one_minus_beta1);
   const Float2 b2 = pack2(a.beta2, a.beta2), c2 = pack2(a.one_minus_beta2, a.one_minus_beta2);
-  const float minus_step = -a.lr * a.scalars->inv_bc1;
+  const float minus_step = -a.lr * a.scalars->inv_bc1 * a.quotient_scale;
   const float decay = 1.0f - a.lr * ch.weight_decay;
   bool simple = false;
   if constexpr (BITS == 8) {
@@ -882,7 +885,8 @@ int solon_adamw_step(solon_adamw* opt, const void* grad, int grad_dtype, double 
   a.one_minus_beta1 = (float)(1.0 - opt->beta1);
   a.beta2 = (float)opt->beta2;
   a.one_minus_beta2 = (float)(1.0 - opt->beta2);
-  a.eps = (float)opt->eps;
+  a.quotient_scale = opt->eps > 0x1p100 ? 0x1p-28f : opt->eps < 0x1p-100 ? 0x1p28f : 1.0f;      // eps: 2^-149 .. 2^128 to 2^-121 .. 2^100
+  a.eps = (float)(opt->eps * a.quotient_scale);
   a.lr = (float)lr;
   return grad_dtype == SOLON_F32 ? adam_update<float>(opt, a, stream) : grad_dtype == SOLON_F64 ? adam_update<double>(opt, a, stream)
                                                                                                  : adam_update<__nv_bfloat16>(opt, a, stream);

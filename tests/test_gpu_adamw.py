@@ -487,3 +487,20 @@ def test_tensors_that_end_just_behind_a_block(bits, grad_type):
                         opt.step(grad, lr=1e-2, max_norm=0.5)
                     assert torch.equal(view, own) and all(torch.equal(x, y) for x, y in zip(opt.state, want.state) if x is not None)
                 assert buf.isnan().sum() == 16 and gbuf.isnan().sum() == 16
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [1e-44, 1e-40, 1e-38, 1e-30, 1e30, 1e38, 3e38])
+def test_eps_at_the_ends_of_its_range(eps, bits):
+    """From a zero state the first step is lr g / (|g| + eps), whatever eps (4 u for the moments, 24 u for the quotient, as above);
+    a weight that has had no gradient stays as it is."""
+    p = torch.zeros(1024, device="cuda")
+    g = _randn(1024, 31, 1e-3 if eps < 1 else 1e18)
+    g[:100] = 0.0
+    p[:100] = 3.0
+    eps32 = float(torch.tensor(eps, dtype=torch.float32))
+    with binding.AdamW([p], bits=bits, betas=(B1, B2), eps=eps) as opt:
+        opt.step(g, lr=0.5)
+    want = -0.5 * g.double() / (g.double().abs() + eps32)
+    want[:100] = 3.0
+    _close(p, want, 32 * U * want.abs() + 2.0 ** -126, "p")
