@@ -43,9 +43,14 @@ __device__ __forceinline__ void team_barrier(int team = 0) {
   else asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "n"(TPR) : "memory");
 }
 // Sum over the team, the result in every thread.  Teams of several warps alternate between two slots, so one barrier a
-// sum is enough: a slot is written again only after everybody has passed the barrier of the sum in between.
+// sum is enough: a slot is written again only after everybody has passed the barrier of the sum in between.  (The slots are read
+// in packs of 16 bytes, which their type is aligned for.)
+template <int N>
+struct alignas(16) SumSlots {
+  float v[2 * 32 * N];
+};
 template <int TPR, int N>
-__device__ __forceinline__ void team_sum(float (&v)[N], float* slots, int& turn, int team) {
+__device__ __forceinline__ void team_sum(float (&v)[N], SumSlots<N>& slots, int& turn, int team) {
 #pragma unroll
   for (int off = 16; off > 0; off >>= 1)
 #pragma unroll
@@ -53,7 +58,7 @@ __device__ __forceinline__ void team_sum(float (&v)[N], float* slots, int& turn,
   if constexpr (TPR > 32) {
     constexpr int kWarps = TPR / 32;
     const int warp = (threadIdx.x & (TPR - 1)) >> 5;
-    float* s = slots + (turn * (blockDim.x >> 5) + team * kWarps) * N;
+    float* s = slots.v + (turn * (blockDim.x >> 5) + team * kWarps) * N;
     turn ^= 1;
     if ((threadIdx.x & 31) == 0) {
 #pragma unroll
@@ -237,7 +242,7 @@ __global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, ln_forwar
   constexpr int kStages = ln_stages<T, TPR, ELEMS, 1>;
   extern __shared__ __align__(16) uint4 ring_memory[];
   typename Row::Group* ring = reinterpret_cast<typename Row::Group*>(ring_memory);      // stages x groups x threads
-  __shared__ __align__(16) float slots[2 * 32];
+  __shared__ SumSlots<1> slots;
   const int tid = threadIdx.x & (TPR - 1), team = threadIdx.x / TPR, cols = (int)a.cols;
   const T* x = static_cast<const T*>(a.x);
   T* y = static_cast<T*>(a.y);
@@ -393,7 +398,7 @@ __global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR, TPR < 512
   constexpr int kStages = ln_stages<T, TPR, ELEMS, 2>;
   extern __shared__ __align__(16) uint4 ring_memory[];
   typename Row::Group* ring = reinterpret_cast<typename Row::Group*>(ring_memory);      // stages x 2 (x, dy) x groups x threads
-  __shared__ __align__(16) float slots[2 * 32 * 2];
+  __shared__ SumSlots<2> slots;
   const int tid = threadIdx.x & (TPR - 1), team = threadIdx.x / TPR, cols = (int)a.cols;
   const int split = blockIdx.x, part = blockIdx.y;
   const T* x = static_cast<const T*>(a.x);
@@ -519,7 +524,7 @@ __global__ void __launch_bounds__(1024) ln_backward_broad_kernel(LnBackwardArgs 
   extern __shared__ __align__(16) uint4 ring_memory[];
   Float2* weights = reinterpret_cast<Float2*>(ring_memory);                             // [kElems / 2][threads]
   typename Row::Group* ring = reinterpret_cast<typename Row::Group*>(weights + kElems / 2 * kTeam);
-  __shared__ __align__(16) float slots[2 * 32 * 2];
+  __shared__ SumSlots<2> slots;
   const int tid = threadIdx.x, cols = (int)a.cols, split = blockIdx.x, part = blockIdx.y;
   const T* x = static_cast<const T*>(a.x);
   const T* dy = static_cast<const T*>(a.dy);
@@ -660,7 +665,7 @@ constexpr int kLnWideThreads = 512;
 
 template <typename T>
 __global__ void __launch_bounds__(kLnWideThreads) ln_forward_wide_kernel(LnForwardArgs a) {
-  __shared__ float slots[2 * 32];
+  __shared__ SumSlots<1> slots;
   int turn = 0;
   const float inv_n = 1.0f / (float)a.cols;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
@@ -691,7 +696,7 @@ __global__ void __launch_bounds__(kLnWideThreads) ln_forward_wide_kernel(LnForwa
 
 template <typename T>
 __global__ void __launch_bounds__(kLnWideThreads) ln_backward_wide_kernel(LnBackwardArgs a, int64_t rows) {
-  __shared__ float slots[2 * 32 * 2];
+  __shared__ SumSlots<2> slots;
   int turn = 0;
   const float inv_n = 1.0f / (float)a.cols;
   for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {

@@ -279,3 +279,19 @@ def test_refusals():
         with pytest.raises(binding.SolonError) as err:
             call()
         assert err.value.status == binding.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("parts,n,cols,pitch,offset", [(1, 3, 16_385, 16_385, 0), (3, 2, 16_387, 16_390, 1), (2, 60, 20_000, 20_001, 3), (1, 1, 65_537, 65_537, 5)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_rows_that_pass_registers(parts, n, cols, pitch, offset, dtype):
+    """Rows of the streaming kernels, one CTA a row: every row's sums by all its warps, several rows to a CTA, in place."""
+    dt, t = TYPES[dtype]
+    x, dy = (_strided(_randn((parts * n, cols), dt, q, 1.5, 0.4), pitch, offset) for q in (5, 6))
+    w, b = _randn(cols, torch.float32, 7), _randn(cols, torch.float32, 8)
+    y, mean, rstd = binding.solon_layernorm_forward(x, w, b)
+    _check_forward(x, w, b, 1e-5, y, mean, rstd, t)
+    got = binding.solon_layernorm_backward(dy, x, mean, rstd, w, partitions=parts)
+    _check_backward(dy, x, mean, rstd, w, parts, got, t)
+    out = dy.clone()
+    inplace = binding.solon_layernorm_backward(out, x, mean, rstd, w, partitions=parts, dx=out)
+    assert inplace[0].data_ptr() == out.data_ptr() and all(torch.equal(p, q) for p, q in zip(inplace, got))
