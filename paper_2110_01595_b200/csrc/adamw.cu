@@ -46,7 +46,7 @@ struct alignas(64) AdamChunk {
 struct AdamScalars {
   double b1t, b2t;           // b1^t, b2^t of the last step that was applied
   long long applied, skipped;
-  float inv_bc1, inv_sqrt_bc2, grad_scale, clip;
+  float inv_bc1, inv_sqrt_bc2, grad_scale, clip;      // (the first two with the quotient's power of two)
   int skip;
   unsigned key;              // of the step's random words
 };
@@ -126,6 +126,7 @@ struct AdamControlArgs {
   int n_partials;              // 0: no clipping
   float* norm_out;             // nullptr: not wanted
   double grad_scale, max_norm, beta1, beta2;
+  double quotient_scale;       // a power of two for both sides of the step's quotient (its eps has it already)
   uint64_t seed;
   const int* guard_status;     // plan's status words (nullptr: no guard)
   const int* guard_t;          // per group: accepted error count, -1 undecodable
@@ -177,8 +178,8 @@ __global__ void __launch_bounds__(256) adam_control_kernel(AdamControlArgs a) {
   s->b1t = b1t;
   s->b2t = b2t;
   s->applied = t;
-  s->inv_bc1 = (float)(1.0 / (1.0 - b1t));
-  s->inv_sqrt_bc2 = (float)(1.0 / sqrt(1.0 - b2t));
+  s->inv_bc1 = (float)(a.quotient_scale / (1.0 - b1t));
+  s->inv_sqrt_bc2 = (float)(a.quotient_scale / sqrt(1.0 - b2t));
   s->grad_scale = (float)scale;
   s->clip = clip;
   s->key = mix32((uint32_t)t * 0x9E3779B1u + (uint32_t)a.seed) ^ (uint32_t)(a.seed >> 32);
@@ -276,7 +277,6 @@ struct AdamStepArgs {
   int16_t* base;               // two per block: m's, v's (8-bit states)
   const AdamScalars* scalars;
   float beta1, one_minus_beta1, beta2, one_minus_beta2, eps, lr;
-  float quotient_scale;        // a power of two on both sides of the step's quotient (eps has it already)
 };
 
 // How a warp goes through its block.  A lane has two groups of four consecutive elements; where parameters or gradients do not
@@ -536,11 +536,11 @@ __device__ __forceinline__ void adam_block(const AdamStepArgs& a, const AdamChun
     codes.load((const uint8_t*)a.exp_avg + slot, (const uint8_t*)a.exp_avg_sq + slot, lane);
     base = load_pack<int16_t, 2>(a.base + 2 * block);
   }
-  const float inv_sqrt_bc2 = a.scalars->inv_sqrt_bc2 * a.quotient_scale;
+  const float inv_sqrt_bc2 = a.scalars->inv_sqrt_bc2;
   const Float2 grad_scale = pack2(a.scalars->grad_scale, a.scalars->grad_scale), clip = pack2(a.scalars->clip, a.scalars->clip);
   const Float2 b1 = pack2(a.beta1, a.beta1), c1 = pack2(a.one_minus_beta1, a.one_minus_beta1);
   const Float2 b2 = pack2(a.beta2, a.beta2), c2 = pack2(a.one_minus_beta2, a.one_minus_beta2);
-  const float minus_step = -a.lr * a.scalars->inv_bc1 * a.quotient_scale;
+  const float minus_step = -a.lr * a.scalars->inv_bc1;
   const float decay = 1.0f - a.lr * ch.weight_decay;
   bool simple = false;
   if constexpr (BITS == 8) {
@@ -861,6 +861,7 @@ int solon_adamw_step(solon_adamw* opt, const void* grad, int grad_dtype, double 
   c.max_norm = max_norm;
   c.beta1 = opt->beta1;
   c.beta2 = opt->beta2;
+  c.quotient_scale = opt->eps > 0x1p100 ? 0x1p-28 : opt->eps < 0x1p-100 ? 0x1p28 : 1.0;      // eps: 2^-149 .. 2^128 to 2^-121 .. 2^100
   c.seed = opt->seed;
   if (guard) {
     c.guard_status = guard->d_status;
@@ -885,8 +886,7 @@ int solon_adamw_step(solon_adamw* opt, const void* grad, int grad_dtype, double 
   a.one_minus_beta1 = (float)(1.0 - opt->beta1);
   a.beta2 = (float)opt->beta2;
   a.one_minus_beta2 = (float)(1.0 - opt->beta2);
-  a.quotient_scale = opt->eps > 0x1p100 ? 0x1p-28f : opt->eps < 0x1p-100 ? 0x1p28f : 1.0f;      // eps: 2^-149 .. 2^128 to 2^-121 .. 2^100
-  a.eps = (float)(opt->eps * a.quotient_scale);
+  a.eps = (float)(opt->eps * c.quotient_scale);
   a.lr = (float)lr;
   return grad_dtype == SOLON_F32 ? adam_update<float>(opt, a, stream) : grad_dtype == SOLON_F64 ? adam_update<double>(opt, a, stream)
                                                                                                  : adam_update<__nv_bfloat16>(opt, a, stream);
