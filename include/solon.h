@@ -369,8 +369,8 @@ int solon_token_logprobs_backward(const void* logits, int64_t pitch, int dtype, 
  *   state_bits 32: exp_avg, exp_avg_sq are blocks x 256 float32; base is not used.
  *   state_bits 8:  exp_avg, exp_avg_sq are blocks x 256 bytes, base blocks x 2 int16.  Code c > 0 of a block stands for the
  *                  float32 with bits (c + base) << 20 (three mantissa bits), code 0 for 0; exp_avg's codes have seven bits
- *                  and the sign on top, base[0] is exp_avg's and base[1] exp_avg_sq's.  Rounded at random (from seed, step and
- *                  place; without bias); exp_avg values more than 15.9 binades below their block's largest become 0,
+ *                  and the sign on top, base[0] is exp_avg's and base[1] exp_avg_sq's.  Rounded at random (16 bits from seed, step
+ *                  and place; the mean is off by less than 2^-16 of the distance of two codes); exp_avg values more than 15.9 binades below their block's largest become 0,
  *                  exp_avg_sq values more than 31.9 below it the smallest code, never 0. */
 typedef struct solon_adamw solon_adamw;
 
@@ -402,8 +402,9 @@ int solon_adamw_bind_grads(solon_adamw* opt, const void* const* grads, int grad_
  *   grad_norm   device, one float32 (output; NULL: not wanted; needs max_norm > 0): the norm before clipping
  *   guard       a plan whose last decode the step depends on (NULL: none): if that decode was undecodable, or a wait in it
  *               ran out, the step changes nothing.  Enqueue the step after the decode, on its stream or ordered behind it.
- * A norm that is not finite (float64 squares: a gradient that is not) also makes the step change nothing; without clipping a gradient that is not finite goes into its
- * weight as the formulas have it.  Steps are counted on the device, only those that were applied count: a captured step may be replayed. */
+ * Gradients are taken as float32: of a float64 gradient, values beyond 3.4e38 are infinite, whatever grad_scale.  A norm that is not
+ * finite (squares in float64: a gradient that is not) also makes the step change nothing; without clipping a gradient that is not
+ * finite goes into its weight as the formulas have it.  Steps are counted on the device, only those that were applied count: a captured step may be replayed. */
 int solon_adamw_step(solon_adamw* opt, const void* grad, int grad_dtype, double grad_scale, double lr, double max_norm, float* grad_norm,
                      const solon_plan* guard, void* cuda_stream);
 

@@ -199,7 +199,8 @@ def solon_project_noalloc(received, f, rho, nu, stream=None) -> int:
 # ------------------------------------------------------------------ token-model operators (no plan needed)
 #
 # All of them enqueue on the current stream of the current device, which the tensors have to be on, and return without
-# synchronising.  Outputs may be given (to be reused from step to step) or are allocated.
+# synchronising.  Outputs may be given (to be reused from step to step) or are allocated.  Nothing is recorded for automatic
+# differentiation, whatever the inputs' requires_grad: the gradients are calls of their own.
 
 _torch_dtypes = {}
 
@@ -263,7 +264,7 @@ def _params(weight, bias, cols: int, x):
 
 def solon_layernorm_forward(x, weight=None, bias=None, eps: float = 1e-5, y=None, mean=None, rstd=None):
     """Layer norm of the rows of x (rows x cols; float32, bfloat16 or float16).  Returns (y, mean, rstd): y in x's type, the
-    rows' means and reciprocal standard deviations in float32 for the backward pass."""
+    rows' means and reciprocal standard deviations in float32 for solon_layernorm_backward.  Not recorded by autograd."""
     import torch
 
     px, x_pitch = _matrix(x, "x")
@@ -342,7 +343,7 @@ class TokenLogprobs(NamedTuple):
 
     logp: object       # rows, float32: log probability of the target (None without targets)
     entropy: object    # rows, float32
-    peak: object       # rows, float32: the largest logit
+    peak: object       # rows, float32: the largest logit (NaN if the row holds one)
     log_sum: object    # rows, float32: log sum e^(z - peak); log p = (z - peak) - log_sum
     top_ids: object    # rows x top_k, int64
     top_logp: object   # rows x top_k, float32
@@ -350,7 +351,8 @@ class TokenLogprobs(NamedTuple):
 
 def solon_token_logprobs(logits, targets=None, top_k: int = 0) -> TokenLogprobs:
     """Log probabilities of the targets (int64; negative: none in this row) under the softmax of each row of logits
-    (rows x vocabulary; float32, bfloat16 or float16), the rows' entropy and their top_k likeliest tokens."""
+    (rows x vocabulary; float32, bfloat16 or float16), the rows' entropy and their top_k likeliest tokens.  Not recorded by
+    autograd; the gradient is solon_token_logprobs_backward."""
     import torch
 
     pz, pitch = _matrix(logits, "logits")
@@ -402,7 +404,7 @@ class AdamW:
     """Owner of a solon_adamw*: AdamW over a list of float32 CUDA tensors, updated in place by step().
 
     bits: 32 or 8, the state's width.  weight_decay: one factor, or one per tensor.  copies: bfloat16 tensors of the same
-    sizes (entries may be None) that every step fills with the rounded parameters.  state: (exp_avg, exp_avg_sq, base) as
+    sizes (entries may be None) that every step fills with the rounded parameters.  Autograd does not see the updates.  state: (exp_avg, exp_avg_sq, base) as
     an earlier handle's `state` had it, taken over in place; by default zeros.  step: steps already applied to it."""
 
     def __init__(self, params, bits: int = 32, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.0, seed: int = 0, step: int = 0, copies=None,

@@ -8,9 +8,9 @@
 // after the other.  (With multiply-adds 9 to 19 codes of 50 M came out otherwise per step, and a quarter of the moments in their last bit.)
 //
 // Bound by memory: a weight with float32 gradient moves 28 bytes (32-bit states) or 16 (8-bit states) against about 20 flops.
-// Measured on 50 M weights: 32-bit states 204 us (6.9 TB/s); 8-bit states 144 us (5.6 TB/s; codes and random bits keep the integer
-// pipe busy 61 % of the time), with float64 gradients 155 us (6.4 TB/s); the norm 65 us of 400 MB of float64 gradients, 31 us of
-// float32 ones, which the update then partly finds in L2.
+// Measured on 50 M weights: 32-bit states 204 us (6.9 TB/s); 8-bit states 144 to 147 us (5.5 TB/s; codes and random bits keep the
+// integer pipe busy 61 % of the time), with float64 gradients 155 to 158 us (6.4 TB/s); the norm 65 us of 400 MB of float64
+// gradients, 31 us of float32 ones, which the update then partly finds in L2.
 //
 // Work: the state is laid out in blocks of 256 elements, every tensor starting a block of its own; one warp owns a block, one
 // CTA eight consecutive blocks of a tensor (a chunk).  Three launches at most: the gradient's squared norm (only when it is
@@ -97,8 +97,9 @@ __device__ __forceinline__ uint32_t slot_hash_start(int64_t slot) {
 // gradients for both.  Because the grid is the same for every block, a window that moves with the block's maximum
 // re-rounds nothing.
 //
-// Rounding is stochastic: adding 20 random bits before the cut is unbiased (within a binade, and across its end, a float's
-// value is linear in its bits).  Rounding to nearest would leave v standing still: with b2 = 0.999 a step moves it by up to
+// Rounding is stochastic: 16 random bits, added to the upper 16 of the 20 that are cut (within a binade, and across its end, a
+// float's value is linear in its bits).  The four lowest bits take no part, so the mean of a rounding is off by at most 15 / 2^20
+// of a grid step, towards 0.  Rounding to nearest would leave v standing still: with b2 = 0.999 a step moves it by up to
 // 0.1 %, half a grid step is 3 - 6 %.  Two exceptions: what lies below the window becomes 0 for m and the smallest code for
 // v, which is never 0 unless v is - a zero v under a moving m would divide by eps.  Non-finite values take the top code
 // and have no part in the choice of the window, so they spoil no other element of their block.
@@ -246,7 +247,8 @@ __global__ void __launch_bounds__(kAdamThreads, 4) adam_norm_flat_kernel(const G
   norm_finish(acc, partials);
 }
 
-// Gradients in tensors of their own: chunk by chunk.
+// Gradients in tensors of their own: chunk by chunk, one element a thread and access (50 M float32, step with clipping: 252 us, from
+// a flat gradient 235; 8-bit states 195 and 180).
 template <typename G>
 __global__ void __launch_bounds__(kAdamThreads) adam_norm_bound_kernel(const AdamChunk* __restrict__ chunks, int64_t n_chunks, double* __restrict__ partials) {
   pdl_trigger();

@@ -5,9 +5,10 @@
 // The variance is summed over the differences from the mean (a second sweep over values that sit in registers), not as a
 // difference of two sums; statistics and sums are float32.
 //
-// Bound by memory: 2 (forward) and 3 (backward) accesses of the matrix against about 8 and 14 flops an element.  Measured:
-// forward 16384 x 4096 bfloat16 48 us (5.6 TB/s), 8192 x 8192 float32 82 us (6.5 TB/s); backward 15 x 2048 rows of 2048 bfloat16 65 us
-// (5.8 TB/s) with 3.5 us for the partial sums, 8192 x 8192 float32 136 us (5.9 TB/s).  What keeps it from the copy rate is 16 warps
+// Bound by memory: 2 (forward) and 3 (backward) accesses of the matrix against about 8 and 14 flops an element.  Measured, call
+// after call on the same tensors, and with cold caches: forward 16384 x 4096 bfloat16 48 to 51 us (5.3 to 5.6 TB/s), 52 cold, 8192 x
+// 8192 float32 83 (6.4 TB/s), 87 cold; backward 15 x 2048 rows of 2048 bfloat16 67 us (5.6 TB/s), 73 cold, 3.5 of them for the
+// partial sums, 8192 x 8192 float32 135 (6.0 TB/s), 132 cold.  What keeps it from the copy rate is 16 warps
 // an SM (the registers of a column's parameters and sums), each with a barrier or two a row.
 //
 // Layout: a row belongs to a team of TPR threads that hold 16 or 32 elements each (fewer in short rows), so that a team's
@@ -660,6 +661,8 @@ __global__ void __launch_bounds__(WARPS < 8 ? 256 : WARPS * 32) ln_param_grad_ke
 }
 
 // ---- rows too wide for registers: one CTA a row, the row read again for every sweep (it stays in L2) ----------------------
+// (Single elements, whatever the alignment: forward 4000 x 20000 bfloat16 138 us (2.3 TB/s), 512 x 20000 23; backward 45 x 8 rows of 20000
+// 33 to 38.  No path of this library has rows this wide.)
 
 constexpr int kLnWideThreads = 512;
 

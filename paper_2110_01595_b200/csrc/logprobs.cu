@@ -18,8 +18,8 @@
 
 namespace solon {
 
-// Measured: 8192 x 32768 bfloat16 94 us (5.7 TB/s), 4096 x 32768 float32 90 us (6.0 TB/s), 2047 x 50001 float32 72 us and with 20
-// likeliest tokens 85 us; the gradient on 8192 x 32768 bfloat16 190 us (5.7 TB/s).
+// Measured: 8192 x 32768 bfloat16 91 to 100 us (5.4 to 5.9 TB/s), 4096 x 32768 float32 89 us (6.0 TB/s), 2047 x 50001 float32 72 us and
+// with 20 likeliest tokens 88 to 93 us; the gradient on 8192 x 32768 bfloat16 182 to 193 us (5.6 to 5.9 TB/s).
 //
 // Bound by memory, with the exponentials (one a logit: at 16 a clock and SM 60 % of the time that bfloat16 logits take to
 // arrive) and the instructions beside them close behind, so those are kept few: two values an instruction, one multiply-add
@@ -715,10 +715,10 @@ static bool logprob_by_warps(int64_t rows, int64_t cols, bool top, int sms) {
 constexpr int kLpWarpList = 256;               // candidates
 template <typename T>
 constexpr int lp_warp_words = 32 / Word16<T>::kCount;                    // words of a lane in an iteration: 32 elements
-// CTAs of eight warps on an SM.  Two suffice the plain sums of two-byte logits (8192 x 32768 bfloat16 takes 100 us with three, 91 with
-// two, 16384 x 16384 89 and 85: the last round of rows is fuller), and for likeliest tokens of float32 ones three would have to
-// share the memory of the lists (2047 x 50001 with 20: 91 us, 85 with two); float32 sums (2047 x 50001: 72 us, 77 with two) and
-// likeliest tokens of two-byte logits (8192 x 32768 with 8: 155 us, 168 with two) take three.
+// CTAs of eight warps on an SM.  Two suffice the plain sums of two-byte logits (8192 x 32768 bfloat16 takes 101 us with three, 91 with
+// two, 16384 x 16384 90 and 85: the last round of rows is fuller), and for likeliest tokens of float32 ones three would have to
+// share the memory of the lists (2047 x 50001 with 20, lists of half the length: 91 us, 85 with two); float32 sums (2047 x 50001: 72
+// us, 74 with two) and likeliest tokens of two-byte logits (8192 x 32768 with 8: 162 us, 164 with two) take three.
 template <typename T, bool TOP>
 constexpr int lp_warp_ctas = (sizeof(T) == 4) == TOP ? 2 : 3;
 template <typename T, bool TOP>
