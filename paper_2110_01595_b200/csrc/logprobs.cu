@@ -575,20 +575,16 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprob_kernel(Logpr
       }
       const float biggest = largest_of<T>(w);
       t.peak = fmaxf(t.peak, biggest);
+      bool added = false;
       if (__any_sync(0xffffffffu, !(biggest <= t.limit))) {
         t.move_reference(biggest);
-        if (!TOP && t.differences()) {
+        if (t.differences()) {
 #pragma unroll
           for (int u = 0; u < kLpWords; ++u) t.add_word_far(w[u]);
-          issue(stage);
-          stage = stage + 1 == kStages ? 0 : stage + 1;
-          continue;
+          added = true;
         }
       }
-      if (TOP && t.differences()) {                       // (the words are still wanted below)
-#pragma unroll
-        for (int u = 0; u < kLpWords; ++u) t.add_word_far(w[u]);
-      } else {
+      if (!added) {
 #pragma unroll
         for (int u = 0; u < kLpWords; ++u) t.add_word(w[u]);
       }
@@ -832,20 +828,16 @@ __global__ void __launch_bounds__(kLpThreads, (lp_warp_ctas<T, TOP>)) logprob_wa
       }
       const float biggest = largest_of<T>(w);
       t.peak = fmaxf(t.peak, biggest);
+      bool added = false;
       if (__any_sync(0xffffffffu, !(biggest <= t.limit))) {
         t.move_reference(biggest);
-        if (!TOP && t.differences()) {
+        if (t.differences()) {
 #pragma unroll
           for (int u = 0; u < kWords; ++u) t.add_word_far(w[u]);
-          issue(stage);
-          stage = stage == ring + (kStages - 1) * kChunk ? ring : stage + kChunk;
-          continue;
+          added = true;
         }
       }
-      if (TOP && t.differences()) {                       // (the words are still wanted below)
-#pragma unroll
-        for (int u = 0; u < kWords; ++u) t.add_word_far(w[u]);
-      } else {
+      if (!added) {
 #pragma unroll
         for (int u = 0; u < kWords; ++u) t.add_word(w[u]);
       }
