@@ -373,7 +373,7 @@ def test_logits_of_large_magnitude(value, dtype, rows, cols):
             _check(part, own, k, binding.solon_token_logprobs(part, own, top_k=k))
 
 
-@pytest.mark.parametrize("rows,cols", [(4, 300), (4, 40_000), (1, 131_072), (400, 9000), (2400, 4000)])
+@pytest.mark.parametrize("rows,cols", [(4, 300), (4, 40_000), (1, 131_072), (400, 9000), (2400, 4000), (7, 1003), (7, 30_001), (1, 100_003), (2401, 2001)])
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 def test_peak_of_rows_that_hold_nan(rows, cols, dtype):
     """The largest logit as an elementary maximum has it: NaN where there is one, +infinity where there is that."""
