@@ -44,6 +44,7 @@ typedef enum solon_status {
 #define SOLON_MAX_S 16            /* adversaries per group                                    */
 #define SOLON_MAX_PROJECTIONS 4   /* random projections K                                     */
 #define SOLON_MAX_COLS (1 << 24)  /* width of a layer norm's row; vocabulary                  */
+#define SOLON_MAX_WIDTH (1 << 22) /* width of an embedding's row, of a hidden state           */
 #define SOLON_MAX_TOP 32          /* likeliest tokens solon_token_logprobs reports            */
 #define SOLON_ADAMW_MAX_NUMEL (1LL << 36)   /* parameters of an optimizer handle, rounded up to blocks of 256 */
 
@@ -360,6 +361,28 @@ int solon_token_logprobs(const void* logits, int64_t pitch, int dtype, const int
 int solon_token_logprobs_backward(const void* logits, int64_t pitch, int dtype, const int64_t* targets, int64_t rows, int64_t vocab, const float* peak,
                                   const float* log_sum, const float* entropy, const float* grad_logp, const float* grad_entropy, void* dlogits, int64_t dlogits_pitch,
                                   void* cuda_stream);
+
+/* Embedding lookup: out_i = scale E[token_i].
+ *   weight  device, vocab x cols of `dtype` (SOLON_F32, SOLON_BF16 or SOLON_F16)
+ *   tokens  device, rows int64: a negative one gives a row of zeros, one >= vocab a row of NaN (neither is looked up)
+ *   out     device, rows x cols of `dtype` (output); scale = 1 copies the bits, otherwise one rounding
+ * cols <= SOLON_MAX_WIDTH.  rows = 0 does nothing. */
+int solon_embedding_forward(const void* weight, int64_t weight_pitch, int dtype, const int64_t* tokens, int64_t rows, int64_t cols, int64_t vocab,
+                            double scale, void* out, int64_t out_pitch, void* cuda_stream);
+
+/* Its gradient: partition k owns rows [k n, (k + 1) n), n = rows / partitions (which must divide rows), and
+ *   dweight[k * grad_pitch + v * cols + c] = scale * sum of dy[i][c] over the rows i of partition k with token v
+ * for every v < vocab - zeros for the tokens that partition k does not hold -, or, with `accumulate`, that sum added to what is
+ * there (the output matrix's gradient, where the two are tied).  Tokens outside [0, vocab) count nowhere.  Sums in float32 over the
+ * rows in an order that sizes and tokens fix: equal calls give equal bits.
+ *   dy         device, rows x cols of `dtype`            tokens  device, rows int64
+ *   dweight    device (output), elements of `grad_dtype` (SOLON_F32, SOLON_F64 or SOLON_BF16), grad_pitch >= vocab * cols: rows of the
+ *              partition-gradient matrix, for instance
+ *   workspace  device, 16-byte aligned, solon_embedding_backward_workspace(...) bytes; its contents need not survive the call */
+int64_t solon_embedding_backward_workspace(int64_t rows, int64_t cols, int partitions);
+int solon_embedding_backward(const void* dy, int64_t dy_pitch, int dtype, const int64_t* tokens, int64_t rows, int64_t cols, int64_t vocab, int partitions,
+                             double scale, void* dweight, int64_t grad_pitch, int grad_dtype, int accumulate, void* workspace, int64_t workspace_bytes,
+                             void* cuda_stream);
 
 /* AdamW over all tensors of a model at once: per weight, with g' = grad_scale * clip * gradient and t the step's number,
  *   m <- beta1 m + (1 - beta1) g'        v <- beta2 v + (1 - beta2) g'^2

@@ -88,6 +88,10 @@ SIGNATURES = {
                                      c_void_p, c_void_p]),
     "solon_token_logprobs_backward": (c_int, [c_void_p, c_int64, c_int, c_void_p, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                               c_void_p, c_int64, c_void_p]),
+    "solon_embedding_forward": (c_int, [c_void_p, c_int64, c_int, c_void_p, c_int64, c_int64, c_int64, c_double, c_void_p, c_int64, c_void_p]),
+    "solon_embedding_backward_workspace": (c_int64, [c_int64, c_int64, c_int]),
+    "solon_embedding_backward": (c_int, [c_void_p, c_int64, c_int, c_void_p, c_int64, c_int64, c_int64, c_int, c_double, c_void_p, c_int64, c_int, c_int,
+                                         c_void_p, c_int64, c_void_p]),
     "solon_adamw_state_blocks": (c_int64, [c_int, POINTER(c_int64)]),
     "solon_adamw_create": (c_int, [c_int, POINTER(c_int64), POINTER(c_void_p), POINTER(c_void_p), POINTER(c_float), c_int, c_void_p, c_void_p, c_void_p,
                                    c_double, c_double, c_double, c_uint64, POINTER(c_void_p)]),
@@ -398,6 +402,70 @@ def solon_token_logprobs_backward(logits, targets, peak, log_sum, grad_logp=None
                                                row_vector(grad_entropy, "grad_entropy"), po, out_pitch, stream),
            "solon_token_logprobs_backward")
     return out
+
+
+def solon_embedding_forward(weight, tokens, scale: float = 1.0, out=None):
+    """Rows of weight (vocabulary x cols; float32, bfloat16 or float16) by tokens (int64), times scale.  A negative token gives zeros,
+    one beyond the vocabulary NaN.  Not recorded by autograd; the gradient is solon_embedding_backward."""
+    import torch
+
+    pw, pitch = _matrix(weight, "weight")
+    vocab, cols = weight.shape
+    device = weight.device
+    stream = _current_stream(device)
+    rows = tokens.numel()
+    pt = _vector(tokens, "tokens", rows, torch.int64, device)
+    if out is None:
+        out = weight.new_empty((rows, cols))
+        po, out_pitch = out.data_ptr(), cols
+    else:
+        if out.dim() != 2 or tuple(out.shape) != (rows, cols) or out.dtype != weight.dtype or out.device != device:
+            raise ValueError(f"out: expected {rows} x {cols} {weight.dtype} on {device}, got {tuple(out.shape)} {out.dtype} on {out.device}")
+        po, out_pitch = _matrix(out, "out")
+    _check(lib().solon_embedding_forward(pw, pitch, _dtype_code(weight.dtype), pt, rows, cols, vocab, scale, po, out_pitch, stream),
+           "solon_embedding_forward")
+    return out
+
+
+@functools.lru_cache(maxsize=256)
+def _embedding_workspace(rows: int, cols: int, partitions: int) -> int:
+    return lib().solon_embedding_backward_workspace(rows, cols, partitions)
+
+
+def _partition_gradient(dweight, like, partitions: int, size: int):
+    """(tensor, pointer, pitch, type code) of a partitions x size gradient, allocated in float32 where none is given."""
+    import torch
+
+    if dweight is None:
+        dweight = like.new_empty((partitions, size), dtype=torch.float32)
+    if dweight.dim() != 2 or tuple(dweight.shape) != (partitions, size) or dweight.device != like.device:
+        raise ValueError(f"dweight: expected {partitions} x {size} on {like.device}, got {tuple(dweight.shape)} on {dweight.device}")
+    pdw, pitch = _matrix(dweight, "dweight")
+    return dweight, pdw, pitch, _dtype_code(dweight.dtype)
+
+
+def solon_embedding_backward(dy, tokens, vocab: int, partitions: int = 1, scale: float = 1.0, dweight=None, accumulate: bool = False):
+    """Gradient of solon_embedding_forward's weight.  Returns dweight, partitions x (vocab * cols): row k holds scale times the sums
+    of dy's rows by token over the rows of partition k (rows / partitions consecutive ones), zeros elsewhere.  It may be a view into
+    the partition-gradient matrix (float32 or float64, as the plan's type; or bfloat16).  accumulate: the sums are added to
+    what dweight holds.  Equal calls give equal bits."""
+    import torch
+
+    pdy, dy_pitch = _matrix(dy, "dy")
+    rows, cols = dy.shape
+    device = dy.device
+    stream = _current_stream(device)
+    pt = _vector(tokens, "tokens", rows, torch.int64, device)
+    if accumulate and dweight is None:
+        raise ValueError("accumulate needs dweight")
+    dweight, pdw, pitch, code = _partition_gradient(dweight, dy, partitions, vocab * cols)
+    n_bytes = _embedding_workspace(rows, cols, partitions)
+    if n_bytes < 0:
+        raise SolonError(n_bytes, "solon_embedding_backward_workspace")
+    workspace = dy.new_empty(n_bytes, dtype=torch.uint8)
+    _check(lib().solon_embedding_backward(pdy, dy_pitch, _dtype_code(dy.dtype), pt, rows, cols, vocab, partitions, scale, pdw, pitch, code,
+                                          1 if accumulate else 0, workspace.data_ptr() or 16, n_bytes, stream), "solon_embedding_backward")
+    return dweight
 
 
 class AdamW:

@@ -1,8 +1,8 @@
 """Closed loop on a token model: every step's partition gradients of a next-token model go through Solon and AdamW.
 
-Per step, for P partitions of n tokens each: embed -> layer norm (solon_layernorm_forward) -> logits -> log probabilities of
+Per step, for P partitions of n tokens each: embed (solon_embedding_forward) -> layer norm (solon_layernorm_forward) -> logits -> log probabilities of
 the next tokens (solon_token_logprobs) -> gradients, each partition's into its row of the P x d gradient matrix
-(solon_token_logprobs_backward, solon_layernorm_backward by partitions) -> coded vectors (solon_encode) -> an adversary
+(solon_token_logprobs_backward, solon_layernorm_backward and solon_embedding_backward by partitions) -> coded vectors (solon_encode) -> an adversary
 overwrites some nodes' rows -> robust decode (solon_decode) -> AdamW on all parameters from the decoded sum
 (solon_adamw_step), skipped on the device if the decode failed.
 
@@ -52,7 +52,7 @@ class TokenLoop:
         self.mask = torch.empty(plan.P, dtype=torch.uint8, device="cuda")
 
     def _forward(self, tokens):
-        hidden = self.embed.index_select(0, tokens)
+        hidden = binding.solon_embedding_forward(self.embed, tokens)
         normed, mean, rstd = binding.solon_layernorm_forward(hidden, self.weight, self.bias, eps=LN_EPS)
         return hidden, normed, mean, rstd, normed @ self.head.t()
 
@@ -73,10 +73,7 @@ class TokenLoop:
         torch.bmm(dlogits.view(P, n, V).transpose(1, 2), normed.view(P, n, C), out=part)
         dhidden, _, _ = binding.solon_layernorm_backward(dlogits @ self.head, hidden, mean, rstd, self.weight, partitions=P,
                                                          dweight=self.grads[:, o[1]:o[2]], dbias=self.grads[:, o[2]:o[3]])
-        part = self.grads.as_strided((P, V, C), (self.plan.d, C, 1), 0)
-        part.zero_()
-        rows = torch.arange(P, device="cuda").repeat_interleave(n)
-        part.index_put_((rows, tokens.reshape(-1)), dhidden, accumulate=True)
+        binding.solon_embedding_backward(dhidden, tokens.reshape(-1), V, partitions=P, dweight=self.grads[:, :o[1]])
         return scored.logp
 
     def step(self, tokens, targets, attackers=()):
