@@ -384,6 +384,36 @@ int solon_embedding_backward(const void* dy, int64_t dy_pitch, int dtype, const 
                              double scale, void* dweight, int64_t grad_pitch, int grad_dtype, int accumulate, void* workspace, int64_t workspace_bytes,
                              void* cuda_stream);
 
+/* solon_token_logprobs of logits = hidden * weight^T that are never in memory: log probabilities of given tokens straight from
+ * hidden states and output matrix.
+ *   hidden   device, rows x cols, weight  device, vocab x cols, both of `dtype` (SOLON_F32, SOLON_BF16 or SOLON_F16)
+ *   targets, logp, entropy, peak, log_sum  as in solon_token_logprobs
+ *   workspace  device, 256-byte aligned, solon_head_logprobs_workspace(...) bytes; `aligned`: 1 if both matrices' first elements and row
+ *              pitches are multiples of 16 bytes (other rows are copied to such a pitch first).  Its contents need not survive the call
+ * Products of the elements as they are, summed in float32 (float16 elements below 2^-14 with the precision of 2^-14); float32 elements are taken as two float16 pieces of 22 bits together (values
+ * below 2^-28 of their tensor's largest: an absolute 2^-40 of it), or multiplied as they are where rows are few (up to 16).
+ * Infinite and NaN elements reach the rows that their products enter; in two pieces infinity counts as NaN.  cols <= SOLON_MAX_WIDTH. */
+int64_t solon_head_logprobs_workspace(int64_t rows, int64_t cols, int64_t vocab, int dtype, int aligned);
+int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* weight, int64_t weight_pitch, int dtype, const int64_t* targets, int64_t rows,
+                        int64_t cols, int64_t vocab, float* logp, float* entropy, float* peak, float* log_sum, void* workspace, int64_t workspace_bytes,
+                        void* cuda_stream);
+
+/* Its gradients: with dlogits as solon_token_logprobs_backward has it (and recomputed logits),
+ *   dhidden = dlogits * weight           device, rows x cols of `dtype` (output; NULL: not wanted; not one of the inputs)
+ *   dweight_k = dlogits_k^T * hidden_k   device (output; NULL: not wanted): row k of the partition-gradient matrix from dweight[k * grad_pitch] on,
+ *                                        vocab x cols elements of `grad_dtype` (SOLON_F32, SOLON_F64 or SOLON_BF16), over the rows of partition k
+ *   peak, log_sum, entropy, grad_logp, grad_entropy  as in solon_token_logprobs_backward
+ *   workspace  device, 256-byte aligned, solon_head_logprobs_backward_workspace(...) bytes: dlogits of one piece of the vocabulary (at most
+ *              256 MB, or 256 tokens), sums of dhidden
+ * dlogits is rounded to 16 bits where the result is (dhidden of 16-bit types, bfloat16 gradients), and held in two such pieces (2^-16 of each value,
+ * 2^-22 for float32 and float16 inputs) for float32 and float64 gradients.  rows = 0: dweight becomes 0.  hidden has to be finite in rows that count in no gradient,
+ * too: they are multiplied by zeros. */
+int64_t solon_head_logprobs_backward_workspace(int64_t rows, int64_t cols, int64_t vocab, int dtype, int grad_dtype, int aligned);
+int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const void* weight, int64_t weight_pitch, int dtype, const int64_t* targets,
+                                 int64_t rows, int64_t cols, int64_t vocab, int partitions, const float* peak, const float* log_sum, const float* entropy,
+                                 const float* grad_logp, const float* grad_entropy, void* dhidden, int64_t dhidden_pitch, void* dweight, int64_t grad_pitch,
+                                 int grad_dtype, void* workspace, int64_t workspace_bytes, void* cuda_stream);
+
 /* AdamW over all tensors of a model at once: per weight, with g' = grad_scale * clip * gradient and t the step's number,
  *   m <- beta1 m + (1 - beta1) g'        v <- beta2 v + (1 - beta2) g'^2
  *   p <- p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)

@@ -92,6 +92,12 @@ SIGNATURES = {
     "solon_embedding_backward_workspace": (c_int64, [c_int64, c_int64, c_int]),
     "solon_embedding_backward": (c_int, [c_void_p, c_int64, c_int, c_void_p, c_int64, c_int64, c_int64, c_int, c_double, c_void_p, c_int64, c_int, c_int,
                                          c_void_p, c_int64, c_void_p]),
+    "solon_head_logprobs_workspace": (c_int64, [c_int64, c_int64, c_int64, c_int, c_int]),
+    "solon_head_logprobs": (c_int, [c_void_p, c_int64, c_void_p, c_int64, c_int, c_void_p, c_int64, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_void_p,
+                                    c_void_p, c_int64, c_void_p]),
+    "solon_head_logprobs_backward_workspace": (c_int64, [c_int64, c_int64, c_int64, c_int, c_int, c_int]),
+    "solon_head_logprobs_backward": (c_int, [c_void_p, c_int64, c_void_p, c_int64, c_int, c_void_p, c_int64, c_int64, c_int64, c_int, c_void_p, c_void_p,
+                                             c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_int, c_void_p, c_int64, c_void_p]),
     "solon_adamw_state_blocks": (c_int64, [c_int, POINTER(c_int64)]),
     "solon_adamw_create": (c_int, [c_int, POINTER(c_int64), POINTER(c_void_p), POINTER(c_void_p), POINTER(c_float), c_int, c_void_p, c_void_p, c_void_p,
                                    c_double, c_double, c_double, c_uint64, POINTER(c_void_p)]),
@@ -466,6 +472,90 @@ def solon_embedding_backward(dy, tokens, vocab: int, partitions: int = 1, scale:
     _check(lib().solon_embedding_backward(pdy, dy_pitch, _dtype_code(dy.dtype), pt, rows, cols, vocab, partitions, scale, pdw, pitch, code,
                                           1 if accumulate else 0, workspace.data_ptr() or 16, n_bytes, stream), "solon_embedding_backward")
     return dweight
+
+
+def _head_operands(hidden, weight):
+    """(hidden pointer, pitch, weight pointer, pitch, type code, both in 16-byte rows) of the two matrices of the head."""
+    ph, h_pitch = _matrix(hidden, "hidden")
+    pw, w_pitch = _matrix(weight, "weight")
+    if weight.shape[1] != hidden.shape[1] or weight.dtype != hidden.dtype or weight.device != hidden.device:
+        raise ValueError(f"weight: expected vocabulary x {hidden.shape[1]} {hidden.dtype} on {hidden.device}, got {tuple(weight.shape)} {weight.dtype} on "
+                         f"{weight.device}")
+    size = hidden.element_size()
+    aligned = not ((ph | pw | (h_pitch * size if hidden.shape[0] > 1 else 0) | (w_pitch * size if weight.shape[0] > 1 else 0)) & 15)
+    return ph, h_pitch, pw, w_pitch, _dtype_code(hidden.dtype), int(aligned)
+
+
+@functools.lru_cache(maxsize=256)
+def _head_workspace(rows: int, cols: int, vocab: int, code: int, aligned: int) -> int:
+    return lib().solon_head_logprobs_workspace(rows, cols, vocab, code, aligned)
+
+
+@functools.lru_cache(maxsize=256)
+def _head_backward_workspace(rows: int, cols: int, vocab: int, code: int, grad_code: int, aligned: int) -> int:
+    return lib().solon_head_logprobs_backward_workspace(rows, cols, vocab, code, grad_code, aligned)
+
+
+def solon_head_logprobs(hidden, weight, targets=None) -> TokenLogprobs:
+    """solon_token_logprobs of the logits hidden @ weight.T (rows x cols, vocabulary x cols; float32, bfloat16 or float16), which are
+    never in memory; without likeliest tokens.  Not recorded by autograd; the gradient is solon_head_logprobs_backward."""
+    import torch
+
+    ph, h_pitch, pw, w_pitch, code, aligned = _head_operands(hidden, weight)
+    (rows, cols), vocab, device = hidden.shape, weight.shape[0], hidden.device
+    stream = _current_stream(device)
+    stats = hidden.new_empty((4, rows), dtype=torch.float32)
+    base, row_bytes = stats.data_ptr(), 4 * rows
+    n_bytes = _head_workspace(rows, cols, vocab, code, aligned)
+    if n_bytes < 0:
+        raise SolonError(n_bytes, "solon_head_logprobs_workspace")
+    workspace = hidden.new_empty(n_bytes, dtype=torch.uint8)
+    _check(lib().solon_head_logprobs(ph, h_pitch, pw, w_pitch, code, None if targets is None else _vector(targets, "targets", rows, torch.int64, device),
+                                     rows, cols, vocab, None if targets is None else base, base + row_bytes, base + 2 * row_bytes, base + 3 * row_bytes,
+                                     workspace.data_ptr(), n_bytes, stream), "solon_head_logprobs")
+    logp, entropy, peak, log_sum = stats.unbind(0)
+    return TokenLogprobs(None if targets is None else logp, entropy, peak, log_sum, None, None)
+
+
+def solon_head_logprobs_backward(hidden, weight, targets, peak, log_sum, grad_logp=None, entropy=None, grad_entropy=None, partitions: int = 1, dhidden=None,
+                                 dweight=None, hidden_grad: bool = True, weight_grad: bool = True):
+    """Gradients of sum(grad_logp * logp + grad_entropy * entropy) of solon_head_logprobs.  Returns (dhidden, dweight): dhidden in
+    hidden's type; dweight partitions x (vocabulary * cols), row k over the rows of partition k (rows / partitions consecutive ones),
+    may be a view into the partition-gradient matrix (float32 or float64, as the plan's type; or bfloat16).  hidden_grad=False,
+    weight_grad=False: None in its place."""
+    import torch
+
+    ph, h_pitch, pw, w_pitch, code, aligned = _head_operands(hidden, weight)
+    (rows, cols), vocab, device = hidden.shape, weight.shape[0], hidden.device
+    stream = _current_stream(device)
+    pdh, dh_pitch = None, cols
+    if hidden_grad:
+        if dhidden is None:
+            dhidden = hidden.new_empty((rows, cols))
+            pdh = dhidden.data_ptr()
+        else:
+            pdh, dh_pitch = _matrix(dhidden, "dhidden", hidden)
+    else:
+        dhidden = None
+    pdw, grad_pitch, grad_code = None, vocab * cols, F32
+    if weight_grad:
+        dweight, pdw, grad_pitch, grad_code = _partition_gradient(dweight, hidden, partitions, vocab * cols)
+    else:
+        dweight = None
+
+    def row_vector(t, name):
+        return None if t is None else _vector(t, name, rows, torch.float32, device)
+
+    n_bytes = _head_backward_workspace(rows, cols, vocab, code, grad_code, aligned)
+    if n_bytes < 0:
+        raise SolonError(n_bytes, "solon_head_logprobs_backward_workspace")
+    workspace = hidden.new_empty(n_bytes, dtype=torch.uint8)
+    _check(lib().solon_head_logprobs_backward(ph, h_pitch, pw, w_pitch, code, None if targets is None else _vector(targets, "targets", rows, torch.int64, device),
+                                              rows, cols, vocab, partitions, row_vector(peak, "peak"), row_vector(log_sum, "log_sum"),
+                                              row_vector(entropy if grad_entropy is not None else None, "entropy"), row_vector(grad_logp, "grad_logp"),
+                                              row_vector(grad_entropy, "grad_entropy"), pdh, dh_pitch, pdw, grad_pitch, grad_code, workspace.data_ptr(),
+                                              n_bytes, stream), "solon_head_logprobs_backward")
+    return dhidden, dweight
 
 
 class AdamW:

@@ -1,0 +1,1114 @@
+// Log probabilities of given tokens straight from hidden states h (rows x cols) and output matrix W (vocab x cols), and their gradient.  The
+// logits z = h W^T are never in memory: a tile of them lives in tensor memory until its part of the result has been taken from it.
+//
+// Forward: per row M = max z, S = sum e^(z - M), A = sum e^(z - M)(z - M) by tiles of 256 tokens, joined by a second kernel; log p = (z_t - M) -
+// log S, entropy log S - A / S.  Backward, in pieces of the vocabulary: the piece's logits once more, dz = g (1[t] - p) - g_H p (log p + H) from
+// them into a workspace, then dh += dz W and dW_k = dz_k^T h_k by two more products.
+//
+// All three products run on the tensor cores (tensor_tiles.cuh).  What is multiplied is 16 bits wide:
+//   bfloat16, float16  the elements themselves; sums float32.  (Rows off 16-byte boundaries are copied to a pitch that the copies can take.)
+//   float32            two float16 pieces, x = 2^-s (hi + lo), s such that the largest of the tensor lies in [2^14, 2^15): the pieces hold 22 bits of
+//                      values down to 2^-28 of the largest, and an absolute 2^-40 of it below.  A product is three: hi lo + lo hi + hi hi; the lo lo
+//                      left out is below 2^-22 of the term.  (Three bfloat16 pieces would take six products.)
+//   dz                 one piece where what it is multiplied into is rounded to 16 bits anyway (dh of 16-bit states, bfloat16 gradients: as much
+//                      rounding again, 2^-8 or 2^-11 of each term at most, of independent signs), two for float32 and float64 gradients (2^-16 with
+//                      bfloat16 pieces, 2^-22 with float16 ones).  bfloat16 gradients of float32 states take the first piece of the states alone, too.  float16 pieces of dz are scaled by the largest |g| + |g_H| (H + 1).
+//
+// Few rows (a served token) are a matter of reading W once: a kernel of ordinary multiply-adds takes any type and alignment.
+
+#include <algorithm>
+#include <cmath>
+
+#include "elements.cuh"
+#include "solon_internal.h"
+#include "tensor_tiles.cuh"
+#include "token_args.h"
+
+namespace solon {
+
+using namespace tiles;
+
+constexpr float kLog2e = 1.44269504088896f;
+constexpr int kTile = 256;               // vocabulary tokens, or rows, of a pair's tile
+constexpr int kEpilogueWarps = 8;
+constexpr int kFirstEpilogue = 4;        // the warps before it bring blocks and multiply, and give registers to the others
+constexpr int kThreads = 32 * (kFirstEpilogue + kEpilogueWarps);
+
+enum HeadMode { kStats, kDz, kDhidden, kDweight };
+
+// ------------------------------------------------------------------------------------------------------------ scales
+
+// What the scans of a call leave behind: the bits of the largest finite magnitudes (0: nothing to scale by), and a flag of waits that ran out.
+struct HeadWords {
+  unsigned hidden, weight, dz;
+  int status;
+};
+
+__device__ __forceinline__ int scale_exponent(unsigned largest) {       // 2^s brings the largest magnitude into [2^14, 2^15)
+  return largest ? min(126, 14 - ilogbf(__uint_as_float(largest))) : 0;
+}
+__device__ __forceinline__ float power_of_two(int s) { return __int_as_float((s + 127) << 23); }       // -126 <= s <= 127
+
+// ------------------------------------------------------------------------------------------------------------ arguments
+
+struct alignas(64) HeadMaps {
+  CUtensorMap a, b, out;
+};
+
+struct HeadArgs {
+  // the product: slabs times m x n, in blocks of 64 inner indices, `products` pairs of pieces
+  int m, n, m_tiles, n_tiles, slabs;
+  int k_blocks, products;
+  int chunk;                             // blocks of 64 that are summed in tensor memory before the sum is added to the one in registers
+  int piece_a[3], piece_b[3];            // third coordinate of the tensor maps for slab 0; slab s is s further
+  int slab_a, slab_b;                    // 1: the operand has slabs
+  const HeadWords* words;
+  HeadWords* flags;
+  int scaled;                            // bits: 1 hidden, 2 weight, 4 dz carry a power of two
+  // rows
+  const int64_t* targets;
+  const float *peak, *log_sum, *entropy, *grad_logp, *grad_entropy;
+  // kStats
+  float* partial;                        // slots x 3 x rows
+  float* target_logit;                   // rows
+  // kStats, kDz: columns of the product are tokens first + n
+  int64_t first, vocab;
+  int pieces;                            // of dz
+  // kDhidden
+  float* sums;                           // rows x sums_pitch: dh of the pieces so far
+  int64_t sums_pitch;
+  int load_sums, store_sums;
+  // kDhidden, kDweight
+  void* out;
+  int64_t out_pitch, out_slab;           // elements; a slab is a partition
+  int out_wide;                          // rows of the output may be accessed four elements at a time
+};
+
+// ------------------------------------------------------------------------------------------------------------ epilogues
+
+// 32 rows x 32 columns from a register per column of a lane's row to four consecutive columns of a row: eight lanes a row.
+__device__ __forceinline__ void stage_rows(const float* v, float4* stage, int lane) {
+#pragma unroll
+  for (int i = 0; i < 8; i++) stage[lane * 8 + (i ^ (lane & 7))] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+}
+
+template <typename O>
+__device__ __forceinline__ void store4(O* p, float4 v) {
+  Pack<O, 4> w;
+  if constexpr (sizeof(O) == 8) w = {{(O)v.x, (O)v.y, (O)v.z, (O)v.w}};
+  else w = {{from_float<O>(v.x), from_float<O>(v.y), from_float<O>(v.z), from_float<O>(v.w)}};
+  if constexpr (sizeof(O) == 8) {
+    *reinterpret_cast<double2*>(p) = make_double2(w.e[0], w.e[1]);
+    *reinterpret_cast<double2*>(p + 2) = make_double2(w.e[2], w.e[3]);
+  } else store_pack(p, w);
+}
+template <typename O>
+__device__ __forceinline__ void store1(O* p, float v) {
+  if constexpr (sizeof(O) == 8) *p = (double)v;
+  else *p = from_float<O>(v);
+}
+
+// Rows [row, row + 32) and columns [col, col + 32) of an output of m x n.
+template <typename O>
+__device__ __forceinline__ void write_rows(const float4* stage, O* out, int64_t pitch, int row, int col, int m, int n, bool wide, int lane) {
+  if (wide && col + 32 <= n) {
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      const int r = i * 4 + lane / 8, c = lane % 8;
+      if (row + r < m) store4(out + (row + r) * pitch + col + c * 4, stage[r * 8 + (c ^ (r & 7))]);
+    }
+  } else {
+    const float* s = reinterpret_cast<const float*>(stage);
+#pragma unroll 8
+    for (int r = 0; r < 32; r++)
+      if (row + r < m && col + lane < n) store1(out + (row + r) * pitch + col + lane, s[(r * 8 + ((lane / 4) ^ (r & 7))) * 4 + lane % 4]);
+  }
+}
+
+struct RowSums {
+  float m, s, a;
+};
+
+// Joins two sets of logits: sums against the larger of the two largest logits.
+__device__ __forceinline__ RowSums join(const RowSums& x, const RowSums& y) {
+  RowSums r;
+  r.m = max_nan(x.m, y.m);
+  const float cx = x.m == -INFINITY ? 0.0f : x.m - r.m, cy = y.m == -INFINITY ? 0.0f : y.m - r.m;    // (no logits, or none above -infinity: s = a = 0)
+  const float ex = exp2f(cx * kLog2e), ey = exp2f(cy * kLog2e);
+  r.s = x.s * ex + y.s * ey;
+  r.a = fmaf(x.s, cx, x.a) * ex + fmaf(y.s, cy, y.a) * ey;
+  return r;
+}
+
+// Says that x is used after y is known: without it the compiler starts so many elements of a row at once that registers do not hold them.
+__device__ __forceinline__ void in_turn(Float2& x, const Float2& y) { asm volatile("" : "+l"(x.v) : "l"(y.v)); }
+
+// z = x if `yes`, in a form that no compiler turns into an indexed access: the row would have to lie in memory.
+__device__ __forceinline__ void take_if(float& z, float x, bool yes) {
+  asm("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %2, 0;\n\t@p mov.f32 %0, %1;\n\t}" : "+f"(z) : "f"(x), "r"((int)yes));
+}
+
+// Sums of one row's part of a tile: its largest logit, S and A against it.
+template <int COLUMNS>
+__device__ __forceinline__ void row_sums(const float (&v)[COLUMNS], RowSums& sums) {
+  float &m = sums.m, &s = sums.s, &a = sums.a;
+  m = v[0];
+#pragma unroll
+  for (int i = 1; i + 1 < COLUMNS; i += 2) asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(v[i]), "f"(v[i + 1]));
+  m = max_nan(m, v[COLUMNS - 1]);
+  const float ref = m == -INFINITY ? 0.0f : m;
+  Float2 minus = pack2(-ref, -ref);
+  const Float2 l2e = pack2(kLog2e, kLog2e);
+  Float2 s2[2] = {pack2(0.0f, 0.0f), pack2(0.0f, 0.0f)}, a2[2] = {s2[0], s2[0]};
+#pragma unroll
+  for (int i = 0; i < COLUMNS; i += 2) {
+    if (i % 16 == 0) in_turn(minus, a2[1]);
+    const Float2 c = add2(pack2(v[i], v[i + 1]), minus);
+    float x, y, cx, cy;
+    unpack2(mul2(c, l2e), x, y);
+    unpack2(c, cx, cy);
+    const Float2 e = pack2(exp2_fast(x), exp2_fast(y));
+    s2[i / 2 % 2] = add2(s2[i / 2 % 2], e);
+    a2[i / 2 % 2] = fma2(e, pack2(fmaxf(cx, -1e30f), fmaxf(cy, -1e30f)), a2[i / 2 % 2]);      // (0 times -infinity is not wanted; NaN is in s)
+  }
+  float x, y;
+  unpack2(add2(s2[0], s2[1]), x, y);
+  s = x + y;
+  unpack2(add2(a2[0], a2[1]), x, y);
+  a = x + y;
+}
+
+// ------------------------------------------------------------------------------------------------------------ product
+
+struct TileAt {
+  int slab, m, n;                        // first row and column
+};
+// Tiles of eight row tiles at a time, columns of those before the next eight: what runs at the same time shares rows of both operands in L2.
+__device__ __forceinline__ TileAt tile_at(const HeadArgs& a, int64_t t, int bn) {
+  const int64_t per_slab = (int64_t)a.m_tiles * a.n_tiles;
+  const int slab = (int)(t / per_slab);
+  const int64_t r = t - slab * per_slab;
+  const int group = (int)(r / (8 * a.n_tiles));
+  const int high = min(8, a.m_tiles - group * 8), in = (int)(r - (int64_t)group * 8 * a.n_tiles);
+  return {slab, (group * 8 + in % high) * kTile, in / high * bn};
+}
+
+// stages of A and B blocks, then the epilogue warps' staging, then barriers
+template <int MODE, int BN>
+struct HeadShared {
+  static constexpr int kStageBytes = (kRows + BN / 2) * kBlock * 2;
+  static constexpr int kStaging = MODE == kStats ? 0 : MODE == kDz ? 8192 : 4096;        // a warp
+  static constexpr int kStages = (232448 - 2048 - kEpilogueWarps * kStaging) / kStageBytes > 8 ? 8 : (232448 - 2048 - kEpilogueWarps * kStaging) / kStageBytes;
+  static constexpr int kBytes = 1024 + kStages * kStageBytes + kEpilogueWarps * kStaging + 512;
+};
+
+// Warp 0 of each CTA brings blocks, warp 1 of the first CTA multiplies, eight warps take finished sums from tensor memory, of which one half is read
+// while the other is being filled, and keep a tile's result in registers: 128 columns of a row a thread.
+// The tensor cores cut off what lies below an accumulator's last bit, which costs a sum of n steps of 16 about n / 2 units of 2^-25, always towards 0
+// (measured: 1.6e-8 a step).  So a result that is wanted in float32 is summed 256 inner indices at a time, and those sums are added in
+// registers, rounded to nearest.
+// Persistent: a pair takes every (pairs)-th tile.
+// Every wait ends after two seconds at the latest: the tiles of a CTA whose wait ran out are filled with NaN.
+template <int MODE, int BN, bool BF16, typename O>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_product_kernel(const __grid_constant__ HeadMaps maps, const HeadArgs a) {
+  constexpr bool kAlongA = MODE != kDweight, kAlongB = MODE == kStats || MODE == kDz;
+  using Shared = HeadShared<MODE, BN>;
+  constexpr int kStages = Shared::kStages, kStageBytes = Shared::kStageBytes;
+  constexpr int kHalf = BN / 2;              // columns of an epilogue warp
+  extern __shared__ char raw[];
+  char* smem = (char*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
+  char* staging = smem + kStages * kStageBytes;
+  uint64_t* full = (uint64_t*)(staging + kEpilogueWarps * Shared::kStaging);
+  uint64_t* empty = full + kStages;
+  uint64_t* sum_full = empty + kStages;
+  uint64_t* sum_empty = sum_full + 2;
+  uint32_t* tmem_at = (uint32_t*)(sum_empty + 2);
+  int* abort_flag = (int*)(tmem_at + 1);
+
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const uint32_t rank = cluster_rank();
+  const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+  const int64_t tiles_all = (int64_t)a.m_tiles * a.n_tiles * a.slabs;
+  const int blocks = a.products * a.k_blocks;
+  int* status = &a.flags->status;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kStages; i++) {
+      pipe::mbar_init(full + i, 1);
+      pipe::mbar_init(empty + i, 1);
+    }
+    for (int i = 0; i < 2; i++) {
+      pipe::mbar_init(sum_full + i, 1);
+      pipe::mbar_init(sum_empty + i, 2 * kEpilogueWarps);
+    }
+    *abort_flag = 0;
+    pipe::fence_barrier_init();
+  }
+  if (warp == 1) tmem_alloc<2 * BN>(tmem_at);
+  fence_before();
+  __syncthreads();
+  cluster_sync();
+  fence_after();
+  const uint32_t tmem = *tmem_at;
+
+  if (warp < kFirstEpilogue) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");        // 128 x 72 + 256 x 216 = 64512 = 384 x 168 at launch
+    if (warp == 0 && lane == 0) {
+      int s = 0;
+      uint32_t phase = 0;
+      for (int64_t t = pair; t < tiles_all; t += pairs) {
+        const TileAt at = tile_at(a, t, BN);
+        const int row = at.m + rank * kRows, col = at.n + rank * kHalf;
+        for (int p = 0; p < a.products; p++) {
+          const int za = a.piece_a[p] + at.slab * a.slab_a, zb = a.piece_b[p] + at.slab * a.slab_b;
+          for (int kb = 0; kb < a.k_blocks; kb++) {
+            pipe::mbar_wait(empty + s, phase ^ 1, abort_flag, status);
+            if (*(volatile int*)abort_flag) goto loads_done;
+            if (rank == 0) pipe::mbar_arrive_expect_tx(full + s, 2 * kStageBytes);
+            const uint32_t dst = pipe::smem_addr(smem + s * kStageBytes);
+            const int k = kb * kBlock;
+#pragma unroll
+            for (int h = 0; h < kRows / kBlock; h++)
+              load_block(dst + h * kBlockBytes, &maps.a, kAlongA ? k : row + h * kBlock, kAlongA ? row + h * kBlock : k, za, full + s);
+#pragma unroll
+            for (int h = 0; h < kHalf / kBlock; h++)
+              load_block(dst + kRows * 128 + h * kBlockBytes, &maps.b, kAlongB ? k : col + h * kBlock, kAlongB ? col + h * kBlock : k, zb, full + s);
+            if (++s == kStages) s = 0, phase ^= 1;
+          }
+        }
+      }
+    loads_done:;
+    } else if (warp == 1 && lane == 0 && rank == 0) {
+      constexpr uint32_t idesc = instruction(BF16, kAlongA, kAlongB, BN);
+      int s = 0, half = 0;
+      uint32_t phase = 0, sum_phase = 0;
+      for (int64_t t = pair; t < tiles_all; t += pairs) {
+        for (int kb = 0; kb < blocks;) {
+          pipe::mbar_wait(sum_empty + half, sum_phase ^ 1, abort_flag, status);
+          if (*(volatile int*)abort_flag) goto products_done;
+          fence_after();
+          const int first = kb, end = min(blocks, kb + a.chunk);
+          for (; kb < end; kb++) {
+            pipe::mbar_wait(full + s, phase, abort_flag, status);
+            if (*(volatile int*)abort_flag) goto products_done;
+            fence_after();
+            const uint32_t at = pipe::smem_addr(smem + s * kStageBytes);
+            const uint64_t da = operand<kAlongA>(at), db = operand<kAlongB>(at + kRows * 128);
+#pragma unroll
+            for (int k = 0; k < kBlock / 16; k++)
+              multiply(tmem + half * BN, da + k * kStep16<kAlongA>, db + k * kStep16<kAlongB>, idesc, kb > first || k > 0);
+            commit_to_both(empty + s);
+            if (++s == kStages) s = 0, phase ^= 1;
+          }
+          commit_to_both(sum_full + half);
+          if ((half ^= 1) == 0) sum_phase ^= 1;
+        }
+      }
+    products_done:;
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    const int quarter = warp % 4, side = (warp - kFirstEpilogue) / 4;
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    char* stage = staging + (warp - kFirstEpilogue) * Shared::kStaging;
+    float undo[2] = {1.0f, 1.0f};
+    if (a.scaled) {
+      const int sa = MODE == kStats || MODE == kDz ? (a.scaled & 1 ? scale_exponent(a.words->hidden) : 0) : (a.scaled & 4 ? scale_exponent(a.words->dz) : 0);
+      const int sb = MODE == kDweight ? (a.scaled & 1 ? scale_exponent(a.words->hidden) : 0) : (a.scaled & 2 ? scale_exponent(a.words->weight) : 0);
+      undo[0] = power_of_two(-sa);
+      undo[1] = power_of_two(-sb);
+    }
+    uint32_t sum_phase = 0;
+    int half = 0;
+    for (int64_t t = pair; t < tiles_all; t += pairs) {
+      const TileAt at = tile_at(a, t, BN);
+      const int row0 = at.m + rank * kRows + quarter * 32, row = row0 + lane, col = at.n + side * kHalf;
+      float v[kHalf];
+#pragma unroll
+      for (int i = 0; i < kHalf; i++) v[i] = 0.0f;
+      for (int kb = 0; kb < blocks; kb += a.chunk) {
+        pipe::mbar_wait(sum_full + half, sum_phase, abort_flag, status);
+        fence_after();
+        const uint32_t from = tmem + half * BN + side * kHalf + lanes;
+#pragma unroll
+        for (int c = 0; c < kHalf; c += 32) {
+          float more[32];
+          tmem_load32(from + c, more);
+          tmem_wait();
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            const Float2 sum = add2(pack2(v[c + i], v[c + i + 1]), pack2(more[i], more[i + 1]));
+            unpack2(sum, v[c + i], v[c + i + 1]);
+          }
+        }
+        fence_before();
+        __syncwarp();
+        if (lane == 0) arrive_at_first(sum_empty + half);
+        if ((half ^= 1) == 0) sum_phase ^= 1;
+      }
+      if (a.scaled) {
+#pragma unroll
+        for (int i = 0; i < kHalf; i++) v[i] = v[i] * undo[0] * undo[1];
+      }
+      if (*(volatile int*)abort_flag) {
+#pragma unroll
+        for (int i = 0; i < kHalf; i++) v[i] = __int_as_float(0x7FC00000);
+      }
+      if constexpr (MODE == kStats) {
+        const int inside = a.n - col;
+        if (inside < kHalf) {
+#pragma unroll
+          for (int i = 0; i < kHalf; i++)
+            if (i >= inside) v[i] = -INFINITY;
+        }
+        if (row < a.m) {
+          const int64_t token = a.targets ? a.targets[row] - a.first - col : -1;
+          if (token >= 0 && token < kHalf && token < inside) {
+            float z = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kHalf; i++) take_if(z, v[i], (int)token == i);
+            a.target_logit[row] = z;
+          }
+          RowSums sums;
+          row_sums(v, sums);
+          float* p = a.partial + (int64_t)(at.n / kHalf + side) * 3 * a.m + row;
+          p[0] = sums.m;
+          p[a.m] = sums.s;
+          p[2 * (int64_t)a.m] = sums.a;
+        }
+      } else if constexpr (MODE == kDz) {
+        float peak = 0.0f, log_sum = 0.0f, h = 0.0f, g = 0.0f, gh = 0.0f;
+        int64_t token = -1;
+        if (row < a.m) {
+          peak = a.peak[row];
+          log_sum = a.log_sum[row];
+          token = a.targets ? a.targets[row] : -1;
+          if (a.grad_logp && token >= 0) g = a.grad_logp[row];
+          if (a.grad_entropy) {
+            gh = a.grad_entropy[row];
+            h = a.entropy[row];
+          }
+        }
+        const bool active = peak != -INFINITY && (g != 0.0f || gh != 0.0f);
+        const float grow = a.scaled & 4 ? power_of_two(scale_exponent(a.words->dz)) : 1.0f;
+        g *= grow;
+        gh *= grow;
+        token -= a.first + col;
+        using Word = Word16<typename std::conditional<BF16, __nv_bfloat16, __half>::type>;
+        const int64_t inside = a.vocab - (a.first + col);
+        Float2 mp = pack2(-peak, -peak);
+        const Float2 ml = pack2(-log_sum, -log_sum), l2e = pack2(kLog2e, kLog2e), mg = pack2(-g, -g), mh = pack2(-gh, -gh), h2 = pack2(h, h);
+        const uint32_t keep = active ? ~0u : 0u;
+#pragma unroll
+        for (int c = 0; c < kHalf; c += 64) {
+          if (lane == 0) stores_read<0>();   // the blocks that were staged before have been read
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 8; i++) {
+            const int first = c + 8 * i;
+            float d[8];
+            Float2 last;
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+              Float2 lp = add2(add2(pack2(v[first + j], v[first + j + 1]), mp), ml);
+              float x, y;
+              if (a.grad_entropy) {          // (p = 0 where log p is -infinity, and no product with it)
+                unpack2(lp, x, y);
+                lp = pack2(x < -1e30f ? -1e30f : x, y < -1e30f ? -1e30f : y);
+              }
+              unpack2(mul2(lp, l2e), x, y);
+              const Float2 e = pack2(exp2_fast(x), exp2_fast(y));
+              last = a.grad_entropy ? mul2(e, fma2(add2(lp, h2), mh, mg)) : mul2(e, mg);
+              unpack2(last, d[j], d[j + 1]);
+            }
+            if (i % 2) in_turn(mp, last);
+            if (token >= first && token < first + 8) {
+#pragma unroll
+              for (int j = 0; j < 8; j++) d[j] += j == (int)token - first ? g : 0.0f;
+            }
+            if (inside < first + 8) {        // (what lies beyond is multiplied by zeros and has to be a number)
+#pragma unroll
+              for (int j = 0; j < 8; j++)
+                if (first + j >= inside) d[j] = 0.0f;
+            }
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+              hi[j] = Word::join(d[2 * j], d[2 * j + 1]) & keep;
+              float hx, hy;
+              Word::pair(hi[j], hx, hy);
+              lo[j] = Word::join(d[2 * j] - hx, d[2 * j + 1] - hy) & keep;
+            }
+            uint4* to = reinterpret_cast<uint4*>(stage) + lane * 8 + (i ^ (lane & 7));
+            to[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            if (a.pieces == 2) to[4096 / 16] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+          }
+          fence_async();
+          __syncwarp();
+          if (lane == 0) {
+            for (int p = 0; p < a.pieces; p++) store_block(&maps.out, col + c, row0, p, pipe::smem_addr(stage + p * 4096));
+            stores_commit();
+          }
+        }
+      } else {
+        float4* rows = reinterpret_cast<float4*>(stage);
+#pragma unroll
+        for (int c = 0; c < kHalf; c += 32) {
+          if (col + c >= a.n || row0 >= a.m) break;
+          __syncwarp();
+          stage_rows(v + c, rows, lane);
+          __syncwarp();
+          if constexpr (MODE == kDhidden) {
+            if (a.load_sums) {
+#pragma unroll
+              for (int i = 0; i < 8; i++) {
+                const int r = i * 4 + lane / 8, x = lane % 8;
+                if (row0 + r < a.m && col + c + x * 4 < a.sums_pitch) {
+                  const float4 was = *reinterpret_cast<const float4*>(a.sums + (row0 + r) * a.sums_pitch + col + c + x * 4);
+                  float4* at4 = rows + r * 8 + (x ^ (r & 7));
+                  *at4 = make_float4(at4->x + was.x, at4->y + was.y, at4->z + was.z, at4->w + was.w);
+                }
+              }
+              __syncwarp();
+            }
+            if (a.store_sums) write_rows(rows, a.sums, a.sums_pitch, row0, col + c, a.m, (int)a.sums_pitch, true, lane);
+            else write_rows(rows, (O*)a.out, a.out_pitch, row0, col + c, a.m, a.n, a.out_wide, lane);
+          } else {
+            write_rows(rows, (O*)a.out + at.slab * a.out_slab, a.out_pitch, row0, col + c, a.m, a.n, a.out_wide, lane);
+          }
+        }
+      }
+    }
+    if (MODE == kDz && lane == 0) stores_done();
+  }
+  if (*(volatile int*)abort_flag) pipe::drain_delay();
+  __syncwarp();
+  fence_before();
+  __syncthreads();
+  cluster_sync();
+  fence_after();
+  if (warp == 1) tmem_free<2 * BN>(tmem);
+}
+
+// ------------------------------------------------------------------------------------------------------------ few rows
+
+struct HeadRowsArgs {
+  const void *hidden, *weight;
+  int64_t hidden_pitch, weight_pitch, cols, vocab;
+  const int64_t* targets;
+  int rows, padded;                      // padded: columns of a row of hidden in shared memory
+  float *partial, *target_logit;
+};
+
+// Up to NR rows: a warp takes R rows of W at a time, E elements a lane and access, against the hidden rows in shared memory (float32; groups of
+// four columns of a lane apart, so that its reads of 16 bytes fall on all banks), and adds the products up over its lanes so that each lane ends with one
+// logit, or a part of a set of lanes.  W is read once: 4 to 16 accesses of 16 bytes a lane are on the way.
+template <typename T, int NR, int R, int E>
+__global__ void __launch_bounds__(256) head_rows_kernel(HeadRowsArgs a) {
+  extern __shared__ __align__(16) float hidden_smem[];
+  __shared__ RowSums merged[8][NR];
+  constexpr int kCount = NR * R;
+  constexpr int kGroups = E > 4 ? E / 4 : 1, kEach = E / kGroups;      // a lane's columns: kGroups runs of kEach
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  for (int i = threadIdx.x; i < NR * a.padded; i += 256) {
+    const int n = i / a.padded, k = i % a.padded;
+    const float x = n < a.rows && k < a.cols ? to_float(((const T*)a.hidden)[n * a.hidden_pitch + k]) : 0.0f;
+    const int step = k / (32 * E), in = k % (32 * E), l = in / E, g = in % E / kEach, j = in % kEach;
+    hidden_smem[n * a.padded + step * 32 * E + (g * 32 + l) * kEach + j] = x;
+  }
+  __syncthreads();
+  RowSums sums = {-INFINITY, 0.0f, 0.0f};
+  constexpr int kShift = kCount == 32 ? 0 : kCount == 16 ? 1 : 2;
+  const int index = lane >> kShift, mine_row = index / R, mine_token = index % R;
+  const bool counts = (lane & ((1 << kShift) - 1)) == 0 && mine_row < a.rows;
+  const int64_t target = counts && a.targets ? a.targets[mine_row] : -1;
+  const int64_t groups = (a.vocab + R - 1) / R;
+  for (int64_t g = (int64_t)blockIdx.x * 8 + warp; g < groups; g += (int64_t)gridDim.x * 8) {
+    const int64_t v0 = g * R;
+    float acc[kCount];
+#pragma unroll
+    for (int i = 0; i < kCount; i++) acc[i] = 0.0f;
+    const T* w[R];
+#pragma unroll
+    for (int r = 0; r < R; r++) w[r] = (const T*)a.weight + min(v0 + r, a.vocab - 1) * a.weight_pitch;
+    for (int k0 = 0; k0 < a.cols; k0 += 32 * E) {
+      const int64_t k = k0 + lane * E;
+      Pack<T, E> x[R];
+#pragma unroll
+      for (int r = 0; r < R; r++) {
+        if (k + E <= a.cols) {
+          if constexpr (sizeof(T) * E == 16) *reinterpret_cast<uint4*>(&x[r]) = load16_once(w[r] + k);
+          else x[r] = load_pack<T, E>(w[r] + k);
+        } else {
+#pragma unroll
+          for (int e = 0; e < E; e++) x[r].e[e] = k + e < a.cols ? w[r][k + e] : from_float<T>(0.0f);
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < NR; n++) {
+        float h[E];
+#pragma unroll
+        for (int q = 0; q < kGroups; q++) {
+          const Pack<float, kEach> p = load_pack<float, kEach>(hidden_smem + n * a.padded + k0 + (q * 32 + lane) * kEach);
+#pragma unroll
+          for (int j = 0; j < kEach; j++) h[q * kEach + j] = p.e[j];
+        }
+#pragma unroll
+        for (int r = 0; r < R; r++)
+#pragma unroll
+          for (int e = 0; e < E; e++) acc[n * R + r] = fmaf(to_float(x[r].e[e]), h[e], acc[n * R + r]);
+      }
+    }
+#pragma unroll
+    for (int o = 16, half = kCount / 2; o > 0; o /= 2, half /= 2) {
+      if (half > 0) {
+#pragma unroll
+        for (int i = 0; i < half; i++) {
+          const float keep = lane & o ? acc[i + half] : acc[i], give = lane & o ? acc[i] : acc[i + half];
+          acc[i] = keep + __shfl_xor_sync(~0u, give, o);
+        }
+      } else acc[0] += __shfl_xor_sync(~0u, acc[0], o);
+    }
+    const int64_t token = v0 + mine_token;
+    if (counts && token < a.vocab) {
+      if (token == target) a.target_logit[mine_row] = acc[0];
+      sums = join(sums, {acc[0], acc[0] == -INFINITY ? 0.0f : 1.0f, 0.0f});
+    }
+  }
+#pragma unroll
+  for (int o = 1; o < 32 / NR; o *= 2)
+    sums = join(sums, {__shfl_xor_sync(~0u, sums.m, o), __shfl_xor_sync(~0u, sums.s, o), __shfl_xor_sync(~0u, sums.a, o)});
+  if (lane % (32 / NR) == 0) merged[warp][lane / (32 / NR)] = sums;
+  __syncthreads();
+  if (threadIdx.x < a.rows) {
+    RowSums r = merged[0][threadIdx.x];
+    for (int i = 1; i < 8; i++) r = join(r, merged[i][threadIdx.x]);
+    float* p = a.partial + (int64_t)blockIdx.x * 3 * a.rows + threadIdx.x;
+    p[0] = r.m;
+    p[a.rows] = r.s;
+    p[2 * a.rows] = r.a;
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------ joining, scanning, splitting
+
+struct HeadJoinArgs {
+  const float *partial, *target_logit;
+  int64_t rows, slots, vocab;
+  const int64_t* targets;
+  float *logp, *entropy, *peak, *log_sum;
+};
+
+// The sums of a row's parts, 256 / ROWS threads a row, joined in an order that the sizes fix.
+template <int ROWS>
+__global__ void __launch_bounds__(256) head_join_kernel(HeadJoinArgs a) {
+  constexpr int kGroups = 256 / ROWS;
+  __shared__ RowSums part[kGroups][ROWS];
+  const int r = threadIdx.x % ROWS, group = threadIdx.x / ROWS;
+  const int64_t row = (int64_t)blockIdx.x * ROWS + r;
+  RowSums sums = {-INFINITY, 0.0f, 0.0f};
+  if (row < a.rows)
+#pragma unroll 4
+    for (int64_t s = group; s < a.slots; s += kGroups) {
+      const float* p = a.partial + s * 3 * a.rows + row;
+      sums = join(sums, {p[0], p[a.rows], p[2 * a.rows]});
+    }
+  part[group][r] = sums;
+  for (int half = kGroups / 2; half > 0; half /= 2) {
+    __syncthreads();
+    if (group < half) part[group][r] = join(part[group][r], part[group + half][r]);
+  }
+  if (group || row >= a.rows) return;
+  sums = part[0][r];
+  const bool empty = sums.m == -INFINITY;
+  const float log_sum = empty ? 0.0f : logf(sums.s);
+  if (a.peak) a.peak[row] = sums.m;
+  if (a.log_sum) a.log_sum[row] = log_sum;
+  if (a.entropy) a.entropy[row] = empty ? 0.0f : log_sum - sums.a / sums.s;
+  if (a.logp) {
+    const int64_t t = a.targets[row];
+    a.logp[row] = t < 0 ? 0.0f : t >= a.vocab ? __int_as_float(0x7FC00000) : empty ? -INFINITY : (a.target_logit[row] - sums.m) - log_sum;
+  }
+}
+
+struct HeadScanArgs {
+  const float *hidden, *weight;          // NULL: not wanted
+  int64_t hidden_pitch, weight_pitch, rows, cols, vocab;
+  const float *grad_logp, *grad_entropy, *entropy;
+  int dz;
+  HeadWords* words;
+};
+
+// Largest finite magnitudes: of the hidden states, the output matrix, and a bound of each row's dz, |g| + |g_H| (H + 1).
+__global__ void __launch_bounds__(256) head_scan_kernel(HeadScanArgs a) {
+  __shared__ unsigned most[8];
+  unsigned big = 0;
+  auto see = [&](float x) {
+    const unsigned u = __float_as_uint(x) & 0x7FFFFFFFu;
+    if (u < 0x7F800000u) big = max(big, u);
+  };
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  unsigned* word;
+  if (blockIdx.y == 2) {
+    if (!a.dz) return;
+    word = &a.words->dz;
+    for (int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x; r < a.rows; r += (int64_t)gridDim.x * 256)
+      see((a.grad_logp ? fabsf(a.grad_logp[r]) : 0.0f) + (a.grad_entropy ? fabsf(a.grad_entropy[r]) * (fabsf(a.entropy[r]) + 1.0f) : 0.0f));
+  } else {
+    const float* m = blockIdx.y ? a.weight : a.hidden;
+    if (!m) return;
+    const int64_t rows = blockIdx.y ? a.vocab : a.rows, pitch = blockIdx.y ? a.weight_pitch : a.hidden_pitch;
+    word = blockIdx.y ? &a.words->weight : &a.words->hidden;
+    const bool wide = !(((uintptr_t)m | (uintptr_t)(pitch * 4)) & 15);
+    for (int64_t r = (int64_t)blockIdx.x * 8 + warp; r < rows; r += (int64_t)gridDim.x * 8) {
+      const float* p = m + r * pitch;
+      int64_t done = 0;
+      if (wide) {
+#pragma unroll 4
+        for (int64_t c = lane; c < a.cols / 4; c += 32) {
+          const float4 x = *reinterpret_cast<const float4*>(p + 4 * c);
+          see(x.x), see(x.y), see(x.z), see(x.w);
+        }
+        done = a.cols / 4 * 4;
+      }
+#pragma unroll 4
+      for (int64_t c = done + lane; c < a.cols; c += 32) see(p[c]);
+    }
+  }
+  big = __reduce_max_sync(~0u, big);
+  if (lane == 0) most[warp] = big;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < 8; i++) big = max(big, most[i]);
+    if (big) atomicMax(word, big);
+  }
+}
+
+// Rows of a matrix at a pitch that tensor copies can take, zeros behind their ends: float32 as two float16 pieces, 16-bit elements as they are.
+template <typename T>
+__global__ void __launch_bounds__(256) head_split_kernel(const T* x, int64_t pitch, int64_t rows, int64_t cols, uint16_t* out, int64_t out_pitch,
+                                                         const unsigned* largest) {
+  const int64_t words = out_pitch / 8;
+  float scale = 1.0f;
+  if constexpr (sizeof(T) == 4) scale = power_of_two(scale_exponent(*largest));
+  const bool wide = sizeof(T) == 4 && !(((uintptr_t)x | (uintptr_t)(pitch * 4)) & 15);
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * words; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / words, c = (i - r * words) * 8;
+    const T* p = x + r * pitch + c;
+    if constexpr (sizeof(T) == 4) {
+      float v[8];
+      if (wide && c + 8 <= cols) {
+        *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(p);
+        *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<const float4*>(p + 4);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[e] = c + e < cols ? p[e] : 0.0f;
+      }
+      Pack<__half, 8> hi, lo;
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        const float y = v[e] * scale;
+        hi.e[e] = __float2half_rn(y);
+        const float rest = y - __half2float(hi.e[e]);
+        lo.e[e] = __float2half_rn(fabsf(y) < INFINITY ? rest : 0.0f);        // (infinity and NaN: the first piece alone says so)
+      }
+      store_pack((__half*)out + r * out_pitch + c, hi);
+      store_pack((__half*)out + (rows + r) * out_pitch + c, lo);
+    } else {
+      Pack<uint16_t, 8> v;
+#pragma unroll
+      for (int e = 0; e < 8; e++) v.e[e] = c + e < cols ? ((const uint16_t*)p)[e] : (uint16_t)0;
+      store_pack(out + r * out_pitch + c, v);
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------ host
+
+static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+// What a call keeps where: offsets into the workspace, in bytes.
+struct HeadPlan {
+  // few rows
+  int row_kernel;                        // 0, or the number of rows that the kernel for few rows is built for
+  int64_t slots;
+  // products
+  int pieces;                            // of hidden and weight
+  bool split;                            // hidden and weight are brought to a layout of their own
+  int64_t pitch;                         // of theirs
+  int dz_pieces;
+  int64_t width;                         // tokens of a piece of the vocabulary
+  int64_t words, partial, target_logit, hidden, weight, dz, sums, total;
+};
+
+constexpr int64_t kHeadSharedRows = 200 * 1024;       // bytes of hidden rows that the kernel for few rows holds
+constexpr int kRowBlocks = 148 * 3;
+
+static int64_t rows_padded(int64_t cols) { return up(cols, 256); }
+
+static HeadPlan head_forward_plan(int64_t rows, int64_t cols, int64_t vocab, int dtype, bool aligned) {
+  HeadPlan p = {};
+  // W has to be read once and is all there is to read: up to 8 rows the multiply-adds keep up with it, and up to 16 they cost less than
+  // splitting or copying W first would.
+  const int most = dtype == SOLON_F32 || !aligned ? 16 : 8;
+  if (rows <= most) {
+    int nr = 1;
+    while (nr < rows) nr *= 2;
+    if (nr * rows_padded(cols) * 4 <= kHeadSharedRows) p.row_kernel = nr;
+  }
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const int64_t here = at;
+    at += up(bytes, 256);
+    return here;
+  };
+  p.words = take(sizeof(HeadWords));
+  p.target_logit = take(rows * 4);
+  if (p.row_kernel) {
+    p.slots = kRowBlocks;
+  } else {
+    p.slots = 2 * ((vocab + kTile - 1) / kTile);
+    p.pieces = dtype == SOLON_F32 ? 2 : 1;
+    p.split = dtype == SOLON_F32 || !aligned;
+    p.pitch = up(cols, 8);
+    if (p.split) {
+      p.hidden = take(p.pieces * rows * p.pitch * 2);
+      p.weight = take(p.pieces * vocab * p.pitch * 2);
+    }
+  }
+  p.partial = take(p.slots * 3 * rows * 4);
+  p.total = at;
+  return p;
+}
+
+constexpr int64_t kDzBytes = 256ll << 20;
+
+static HeadPlan head_backward_plan(int64_t rows, int64_t cols, int64_t vocab, int dtype, int grad_dtype, bool aligned) {
+  HeadPlan p = {};
+  p.pieces = dtype == SOLON_F32 ? 2 : 1;
+  p.split = dtype == SOLON_F32 || !aligned;
+  p.pitch = up(cols, 8);
+  p.dz_pieces = dtype == SOLON_F32 || grad_dtype != SOLON_BF16 ? 2 : 1;
+  p.width = std::min(up(vocab, 64), std::max<int64_t>(kTile, kDzBytes / (rows * 2 * p.dz_pieces) / kTile * kTile));
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const int64_t here = at;
+    at += up(bytes, 256);
+    return here;
+  };
+  p.words = take(sizeof(HeadWords));
+  if (p.split) {
+    p.hidden = take(p.pieces * rows * p.pitch * 2);
+    p.weight = take(p.pieces * vocab * p.pitch * 2);
+  }
+  p.dz = take(p.dz_pieces * rows * p.width * 2);
+  if (p.width < vocab) p.sums = take(rows * up(cols, 4) * 4);
+  p.total = at;
+  return p;
+}
+
+static bool aligned16(const void* p, int64_t pitch, int64_t rows, int dtype) {
+  return !(((uintptr_t)p & 15) || (rows > 1 && (pitch * element_size(dtype)) & 15));
+}
+
+template <typename T, int NR, int R, int E>
+static int head_rows_launch(const HeadRowsArgs& a, cudaStream_t stream) {
+  const size_t smem = (size_t)NR * a.padded * 4;
+  SOLON_SHARED_MEMORY_ONCE((head_rows_kernel<T, NR, R, E>), kHeadSharedRows);
+  head_rows_kernel<T, NR, R, E><<<kRowBlocks, 256, smem, stream>>>(a);
+  SOLON_CUDA_TRY(cudaGetLastError());
+  return SOLON_OK;
+}
+
+template <typename T, int E>
+static int head_rows_e(const HeadRowsArgs& a, int nr, cudaStream_t stream) {
+  switch (nr) {
+    case 1: return head_rows_launch<T, 1, 8, E>(a, stream);
+    case 2: return head_rows_launch<T, 2, 8, E>(a, stream);
+    case 4: return head_rows_launch<T, 4, 8, E>(a, stream);
+    case 8: return head_rows_launch<T, 8, 4, E>(a, stream);
+    default: return head_rows_launch<T, 16, 2, E>(a, stream);
+  }
+}
+
+template <typename T>
+static int head_rows_t(const HeadRowsArgs& a, int nr, cudaStream_t stream) {
+  uintptr_t both = (uintptr_t)a.weight | (uintptr_t)(a.weight_pitch * sizeof(T));
+  if (!(both & 15)) return head_rows_e<T, 16 / sizeof(T)>(a, nr, stream);
+  if (!(both & 3) && sizeof(T) == 2) return head_rows_e<T, 2>(a, nr, stream);
+  return head_rows_e<T, 1>(a, nr, stream);
+}
+
+template <int MODE, int BN, bool BF16, typename O>
+static int head_product_launch(const HeadMaps& maps, HeadArgs a, int sms, cudaStream_t stream) {
+  auto* kernel = head_product_kernel<MODE, BN, BF16, O>;
+  constexpr int bytes = HeadShared<MODE, BN>::kBytes;
+  a.m_tiles = (a.m + kTile - 1) / kTile;
+  a.n_tiles = (a.n + BN - 1) / BN;
+  a.chunk = (MODE == kDhidden || MODE == kDweight) && sizeof(O) == 2 ? 64 : 4;
+  const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles * a.slabs;
+  const int pairs = (int)std::min<int64_t>(tiles, sms / 2);
+  SOLON_SHARED_MEMORY_ONCE(kernel, bytes);
+  kernel<<<2 * pairs, kThreads, bytes, stream>>>(maps, a);
+  SOLON_CUDA_TRY(cudaGetLastError());
+  return SOLON_OK;
+}
+
+// 256 columns a tile, or 128 where that covers the columns with a sixth less.
+template <int MODE, bool BF16, typename O>
+static int head_product(const HeadMaps& maps, const HeadArgs& a, int sms, cudaStream_t stream) {
+  if (up(a.n, 128) * 6 <= up(a.n, 256) * 5) return head_product_launch<MODE, 128, BF16, O>(maps, a, sms, stream);
+  return head_product_launch<MODE, 256, BF16, O>(maps, a, sms, stream);
+}
+
+// A matrix as the products take it: where its pieces lie.
+struct HeadOperand {
+  const char* p;
+  int64_t pitch, rows;
+  int pieces;
+};
+
+static int head_operand(const void* x, int64_t pitch, int64_t rows, int64_t cols, int dtype, const HeadPlan& plan, char* to, const unsigned* largest, int sms,
+                        cudaStream_t stream, HeadOperand* out) {
+  if (!plan.split) {
+    *out = {(const char*)x, rows > 1 ? pitch : up(cols, 8), rows, 1};
+    return SOLON_OK;
+  }
+  const int64_t words = rows * (plan.pitch / 8);
+  const unsigned blocks = (unsigned)std::min<int64_t>((words + 255) / 256, 16 * sms);
+  if (dtype == SOLON_F32)
+    head_split_kernel<float><<<blocks, 256, 0, stream>>>((const float*)x, pitch, rows, cols, (uint16_t*)to, plan.pitch, largest);
+  else
+    head_split_kernel<uint16_t><<<blocks, 256, 0, stream>>>((const uint16_t*)x, pitch, rows, cols, (uint16_t*)to, plan.pitch, nullptr);
+  SOLON_CUDA_TRY(cudaGetLastError());
+  *out = {to, plan.pitch, rows, plan.pieces};
+  return SOLON_OK;
+}
+
+static int head_scan(const HeadScanArgs& a, int sms, cudaStream_t stream) {
+  if (!a.hidden && !a.weight && !a.dz) return SOLON_OK;
+  head_scan_kernel<<<dim3(4 * sms, 3), 256, 0, stream>>>(a);
+  SOLON_CUDA_TRY(cudaGetLastError());
+  return SOLON_OK;
+}
+
+// Pairs of pieces, the smallest products first.
+static void head_pairs(HeadArgs& a, int pieces_a, int pieces_b, int step_a, int step_b) {
+  a.products = 0;
+  auto pair = [&](int x, int y) {
+    a.piece_a[a.products] = x * step_a;
+    a.piece_b[a.products++] = y * step_b;
+  };
+  if (pieces_b == 2) pair(0, 1);
+  if (pieces_a == 2) pair(1, 0);
+  pair(0, 0);
+}
+
+static bool head_sizes_ok(int64_t rows, int64_t cols, int64_t vocab) {
+  return rows >= 0 && rows <= (1 << 30) && cols >= 1 && cols <= SOLON_MAX_WIDTH && vocab >= 1 && vocab <= (1 << 30) && vocab <= (1ll << 46) / cols &&
+         (rows == 0 || vocab <= (1ll << 46) / rows);
+}
+
+static int head_stats(const HeadMaps& maps, const HeadArgs& a, bool bf16, int sms, cudaStream_t stream) {
+  if (bf16) return head_product_launch<kStats, 256, true, float>(maps, a, sms, stream);
+  return head_product_launch<kStats, 256, false, float>(maps, a, sms, stream);
+}
+
+template <bool BF16, typename H>
+static int head_backward_piece(int which, const HeadMaps& maps, const HeadArgs& a, int grad_dtype, int sms, cudaStream_t stream) {
+  if (which == kDz) return head_product_launch<kDz, 256, BF16, float>(maps, a, sms, stream);
+  if (which == kDhidden) return head_product<kDhidden, BF16, H>(maps, a, sms, stream);
+  if (grad_dtype == SOLON_F32) return head_product<kDweight, BF16, float>(maps, a, sms, stream);
+  if (grad_dtype == SOLON_F64) return head_product<kDweight, BF16, double>(maps, a, sms, stream);
+  return head_product<kDweight, BF16, __nv_bfloat16>(maps, a, sms, stream);
+}
+
+}  // namespace solon
+
+using namespace solon;
+
+extern "C" {
+
+int64_t solon_head_logprobs_workspace(int64_t rows, int64_t cols, int64_t vocab, int dtype, int aligned) {
+  if (!token_dtype(dtype) || !head_sizes_ok(rows, cols, vocab)) return SOLON_ERR_INVALID_ARG;
+  return rows == 0 ? 0 : head_forward_plan(rows, cols, vocab, dtype, aligned != 0).total;
+}
+
+int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* weight, int64_t weight_pitch, int dtype, const int64_t* targets, int64_t rows,
+                        int64_t cols, int64_t vocab, float* logp, float* entropy, float* peak, float* log_sum, void* workspace, int64_t workspace_bytes,
+                        void* cuda_stream) {
+  if (!token_dtype(dtype) || !head_sizes_ok(rows, cols, vocab)) return SOLON_ERR_INVALID_ARG;
+  if (rows == 0) return SOLON_OK;
+  if (!matrix_ok(hidden, hidden_pitch, rows, cols, dtype) || !matrix_ok(weight, weight_pitch, vocab, cols, dtype)) return SOLON_ERR_INVALID_ARG;
+  if ((logp && !targets) || ((uintptr_t)targets & 7) || (((uintptr_t)logp | (uintptr_t)entropy | (uintptr_t)peak | (uintptr_t)log_sum) & 3))
+    return SOLON_ERR_INVALID_ARG;
+  const bool aligned = aligned16(hidden, hidden_pitch, rows, dtype) && aligned16(weight, weight_pitch, vocab, dtype);
+  const HeadPlan plan = head_forward_plan(rows, cols, vocab, dtype, aligned);
+  if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < plan.total) return SOLON_ERR_INVALID_ARG;
+  int sms = 0, rc;
+  if ((rc = current_sms(&sms))) return rc;
+  cudaStream_t stream = (cudaStream_t)cuda_stream;
+  char* ws = (char*)workspace;
+  HeadWords* words = (HeadWords*)(ws + plan.words);
+  int64_t slots = plan.slots;
+  if (plan.row_kernel) {
+    const HeadRowsArgs a = {hidden, weight, hidden_pitch, vocab > 1 ? weight_pitch : cols, cols, vocab, targets, (int)rows, (int)rows_padded(cols),
+                            (float*)(ws + plan.partial), (float*)(ws + plan.target_logit)};
+    if (dtype == SOLON_F32) rc = head_rows_t<float>(a, plan.row_kernel, stream);
+    else if (dtype == SOLON_BF16) rc = head_rows_t<__nv_bfloat16>(a, plan.row_kernel, stream);
+    else rc = head_rows_t<__half>(a, plan.row_kernel, stream);
+    if (rc) return rc;
+  } else {
+    SOLON_CUDA_TRY(cudaMemsetAsync(words, 0, sizeof(HeadWords), stream));
+    if (dtype == SOLON_F32) {
+      const HeadScanArgs scan = {(const float*)hidden, (const float*)weight, hidden_pitch, weight_pitch, rows, cols, vocab, nullptr, nullptr, nullptr, 0, words};
+      if ((rc = head_scan(scan, sms, stream))) return rc;
+    }
+    HeadOperand h, w;
+    if ((rc = head_operand(hidden, hidden_pitch, rows, cols, dtype, plan, ws + plan.hidden, &words->hidden, sms, stream, &h))) return rc;
+    if ((rc = head_operand(weight, weight_pitch, vocab, cols, dtype, plan, ws + plan.weight, &words->weight, sms, stream, &w))) return rc;
+    const bool bf16 = dtype == SOLON_BF16;
+    HeadMaps maps = {};
+    if (!tensor_map(&maps.a, h.p, bf16, cols, rows, h.pieces, h.pitch, rows * h.pitch, kBlock) ||
+        !tensor_map(&maps.b, w.p, bf16, cols, vocab, w.pieces, w.pitch, vocab * w.pitch, kBlock))
+      return SOLON_ERR_CUDA;
+    HeadArgs a = {};
+    a.m = (int)rows;
+    a.n = (int)vocab;
+    a.slabs = 1;
+    a.k_blocks = (int)((cols + kBlock - 1) / kBlock);
+    head_pairs(a, h.pieces, w.pieces, 1, 1);
+    a.words = a.flags = words;
+    a.scaled = dtype == SOLON_F32 ? 3 : 0;
+    a.targets = targets;
+    a.partial = (float*)(ws + plan.partial);
+    a.target_logit = (float*)(ws + plan.target_logit);
+    a.vocab = vocab;
+    if ((rc = head_stats(maps, a, bf16, sms, stream))) return rc;
+  }
+  const HeadJoinArgs j = {(const float*)(ws + plan.partial), (const float*)(ws + plan.target_logit), rows, slots, vocab, targets, logp, entropy, peak, log_sum};
+  if (rows < 2048) head_join_kernel<1><<<(unsigned)rows, 256, 0, stream>>>(j);
+  else head_join_kernel<32><<<(unsigned)((rows + 31) / 32), 256, 0, stream>>>(j);
+  SOLON_CUDA_TRY(cudaGetLastError());
+  return SOLON_OK;
+}
+
+int64_t solon_head_logprobs_backward_workspace(int64_t rows, int64_t cols, int64_t vocab, int dtype, int grad_dtype, int aligned) {
+  if (!token_dtype(dtype) || !head_sizes_ok(rows, cols, vocab)) return SOLON_ERR_INVALID_ARG;
+  if (grad_dtype != SOLON_F32 && grad_dtype != SOLON_F64 && grad_dtype != SOLON_BF16) return SOLON_ERR_INVALID_ARG;
+  return rows == 0 ? 0 : head_backward_plan(rows, cols, vocab, dtype, grad_dtype, aligned != 0).total;
+}
+
+int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const void* weight, int64_t weight_pitch, int dtype, const int64_t* targets,
+                                 int64_t rows, int64_t cols, int64_t vocab, int partitions, const float* peak, const float* log_sum, const float* entropy,
+                                 const float* grad_logp, const float* grad_entropy, void* dhidden, int64_t dhidden_pitch, void* dweight, int64_t grad_pitch,
+                                 int grad_dtype, void* workspace, int64_t workspace_bytes, void* cuda_stream) {
+  if (!token_dtype(dtype) || !head_sizes_ok(rows, cols, vocab) || partitions < 1 || partitions > SOLON_MAX_NODES || rows % partitions)
+    return SOLON_ERR_INVALID_ARG;
+  if (grad_dtype != SOLON_F32 && grad_dtype != SOLON_F64 && grad_dtype != SOLON_BF16) return SOLON_ERR_INVALID_ARG;
+  if (dweight && !matrix_ok(dweight, grad_pitch, partitions, vocab * cols, grad_dtype)) return SOLON_ERR_INVALID_ARG;
+  cudaStream_t stream = (cudaStream_t)cuda_stream;
+  const int64_t grad_size = (int64_t)element_size(grad_dtype);
+  if (rows == 0) {
+    if (dweight)
+      SOLON_CUDA_TRY(cudaMemset2DAsync(dweight, (partitions > 1 ? grad_pitch : vocab * cols) * grad_size, 0, vocab * cols * grad_size, partitions, stream));
+    return SOLON_OK;
+  }
+  if (!matrix_ok(hidden, hidden_pitch, rows, cols, dtype) || !matrix_ok(weight, weight_pitch, vocab, cols, dtype)) return SOLON_ERR_INVALID_ARG;
+  if (dhidden && !matrix_ok(dhidden, dhidden_pitch, rows, cols, dtype)) return SOLON_ERR_INVALID_ARG;
+  if (!peak || !log_sum || (grad_logp && !targets) || (grad_entropy && !entropy) || ((uintptr_t)targets & 7) ||
+      (((uintptr_t)peak | (uintptr_t)log_sum | (uintptr_t)entropy | (uintptr_t)grad_logp | (uintptr_t)grad_entropy) & 3))
+    return SOLON_ERR_INVALID_ARG;
+  if (!dhidden && !dweight) return SOLON_OK;
+  const bool aligned = aligned16(hidden, hidden_pitch, rows, dtype) && aligned16(weight, weight_pitch, vocab, dtype);
+  const HeadPlan plan = head_backward_plan(rows, cols, vocab, dtype, grad_dtype, aligned);
+  if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < plan.total) return SOLON_ERR_INVALID_ARG;
+  int sms = 0, rc;
+  if ((rc = current_sms(&sms))) return rc;
+  char* ws = (char*)workspace;
+  HeadWords* words = (HeadWords*)(ws + plan.words);
+  const bool f32 = dtype == SOLON_F32, bf16 = dtype == SOLON_BF16;
+  SOLON_CUDA_TRY(cudaMemsetAsync(words, 0, sizeof(HeadWords), stream));
+  const HeadScanArgs scan = {f32 ? (const float*)hidden : nullptr, f32 ? (const float*)weight : nullptr, hidden_pitch, weight_pitch, rows, cols, vocab,
+                             grad_logp, grad_entropy, entropy, !bf16, words};
+  if ((rc = head_scan(scan, sms, stream))) return rc;
+  HeadOperand h, w;
+  if ((rc = head_operand(hidden, hidden_pitch, rows, cols, dtype, plan, ws + plan.hidden, &words->hidden, sms, stream, &h))) return rc;
+  if ((rc = head_operand(weight, weight_pitch, vocab, cols, dtype, plan, ws + plan.weight, &words->weight, sms, stream, &w))) return rc;
+
+  const int64_t n = rows / partitions, sums_pitch = up(cols, 4);
+  CUtensorMap map_h, map_w, map_h_parts, map_dz, map_dz_parts, map_dz_out;
+  if (!tensor_map(&map_h, h.p, bf16, cols, rows, h.pieces, h.pitch, rows * h.pitch, kBlock) ||
+      !tensor_map(&map_w, w.p, bf16, cols, vocab, w.pieces, w.pitch, vocab * w.pitch, kBlock) ||
+      !tensor_map(&map_h_parts, h.p, bf16, cols, n, (int64_t)h.pieces * partitions, h.pitch, n * h.pitch, kBlock))
+    return SOLON_ERR_CUDA;
+  HeadArgs base = {};
+  base.slabs = 1;
+  base.words = base.flags = words;
+  base.targets = targets;
+  base.peak = peak;
+  base.log_sum = log_sum;
+  base.entropy = entropy;
+  base.grad_logp = grad_logp;
+  base.grad_entropy = grad_entropy;
+  base.vocab = vocab;
+  const int dz_scaled = bf16 ? 0 : 4;
+  auto run = [&](int which, const HeadMaps& maps, const HeadArgs& a) {
+    if (f32) return head_backward_piece<false, float>(which, maps, a, grad_dtype, sms, stream);
+    if (bf16) return head_backward_piece<true, __nv_bfloat16>(which, maps, a, grad_dtype, sms, stream);
+    return head_backward_piece<false, __half>(which, maps, a, grad_dtype, sms, stream);
+  };
+  for (int64_t first = 0; first < vocab; first += plan.width) {
+    const int64_t width = std::min(plan.width, vocab - first), pitch = up(width, kBlock);
+    if (!tensor_map(&map_dz, ws + plan.dz, bf16, pitch, rows, plan.dz_pieces, pitch, rows * pitch, kBlock) ||
+        !tensor_map(&map_dz_out, ws + plan.dz, bf16, pitch, rows, plan.dz_pieces, pitch, rows * pitch, 32) ||
+        !tensor_map(&map_dz_parts, ws + plan.dz, bf16, pitch, n, (int64_t)plan.dz_pieces * partitions, pitch, n * pitch, kBlock))
+      return SOLON_ERR_CUDA;
+    CUtensorMap map_w_piece;
+    if (!tensor_map(&map_w_piece, w.p + first * w.pitch * 2, bf16, cols, width, w.pieces, w.pitch, vocab * w.pitch, kBlock)) return SOLON_ERR_CUDA;
+    HeadArgs a = base;
+    a.m = (int)rows;
+    a.n = (int)width;
+    a.first = first;
+    a.k_blocks = (int)((cols + kBlock - 1) / kBlock);
+    head_pairs(a, h.pieces, w.pieces, 1, 1);
+    a.scaled = (f32 ? 3 : 0) | dz_scaled;
+    a.pieces = plan.dz_pieces;
+    if ((rc = run(kDz, {map_h, map_w_piece, map_dz_out}, a))) return rc;
+    if (dhidden) {
+      a = base;
+      a.m = (int)rows;
+      a.n = (int)cols;
+      a.k_blocks = (int)(pitch / kBlock);
+      head_pairs(a, f32 ? 2 : 1, w.pieces, 1, 1);
+      a.scaled = (f32 ? 2 : 0) | dz_scaled;
+      a.sums = (float*)(ws + plan.sums);
+      a.sums_pitch = sums_pitch;
+      a.load_sums = first > 0;
+      a.store_sums = first + width < vocab;
+      a.out = dhidden;
+      a.out_pitch = rows > 1 ? dhidden_pitch : cols;
+      a.out_wide = !(((uintptr_t)dhidden | (uintptr_t)(a.out_pitch * element_size(dtype))) & (4 * element_size(dtype) - 1));
+      if ((rc = run(kDhidden, {map_dz, map_w_piece, map_dz}, a))) return rc;
+    }
+    if (dweight) {
+      a = base;
+      a.m = (int)width;
+      a.n = (int)cols;
+      a.slabs = partitions;
+      a.slab_a = a.slab_b = 1;
+      a.k_blocks = (int)((n + kBlock - 1) / kBlock);
+      const bool coarse = grad_dtype == SOLON_BF16;
+      head_pairs(a, coarse ? 1 : 2, coarse ? 1 : h.pieces, partitions, partitions);
+      a.scaled = (f32 ? 1 : 0) | dz_scaled;
+      a.out = (char*)dweight + first * cols * grad_size;
+      a.out_pitch = cols;
+      a.out_slab = partitions > 1 ? grad_pitch : 0;
+      a.out_wide = !(((uintptr_t)a.out | (uintptr_t)(cols * grad_size) | (uintptr_t)(a.out_slab * grad_size)) & (std::min<int64_t>(16, 4 * grad_size) - 1));
+      if ((rc = run(kDweight, {map_dz_parts, map_h_parts, map_dz}, a))) return rc;
+    }
+  }
+  return SOLON_OK;
+}
+
+}  // extern "C"

@@ -30,7 +30,7 @@ template <bool ALONG_K>
 constexpr uint32_t kStep16 = ALONG_K ? 32 >> 4 : 2048 >> 4;
 
 // Instruction descriptor: float32 accumulators, both operands bfloat16 or both float16, 256 x n.
-constexpr uint32_t instruction(bool bf16, bool a_along_k, bool b_along_k, int n) {
+__host__ __device__ constexpr uint32_t instruction(bool bf16, bool a_along_k, bool b_along_k, int n) {
   return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((a_along_k ? 0u : 1u) << 15) | ((b_along_k ? 0u : 1u) << 16) |
          ((uint32_t)(n >> 3) << 17) | ((256u >> 4) << 24);
 }
@@ -73,6 +73,14 @@ __device__ __forceinline__ void tmem_load32(uint32_t tmem, float* v) {
         "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
         "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
         "=r"(r[31])
+      : "r"(tmem));
+}
+__device__ __forceinline__ void tmem_load16(uint32_t tmem, float* v) {
+  uint32_t* r = reinterpret_cast<uint32_t*>(v);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(tmem));
 }
 __device__ __forceinline__ void tmem_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }

@@ -43,3 +43,34 @@ def test_embedding_refusals(lib):
     assert b(at, 8, 0, at, 4, 8, 10, 2, 1.0, None, 80, 0, 0, at, big, None) == BAD
     assert b(None, 8, 0, at, 4, 8, 10, 2, 1.0, at, 80, 0, 0, at, big, None) == BAD
     assert b(at, 8, 0, at, 4, 8, 1 << 45, 2, 1.0, at, 1 << 48, 0, 0, at, big, None) == BAD
+
+
+def test_head_refusals(lib):
+    at, big = 4096, 1 << 40
+    w = lib.solon_head_logprobs_workspace
+    assert w(0, 8, 10, 0, 1) == 0 and w(1, 8, 10, 0, 1) > 0 and w(1000, 64, 1000, 2, 0) > w(1000, 64, 1000, 2, 1)
+    assert w(4, 8, 10, 1, 1) == BAD and w(-1, 8, 10, 0, 1) == BAD and w(4, 0, 10, 0, 1) == BAD and w(4, 8, 0, 0, 1) == BAD and w(4, 1 << 23, 10, 0, 1) == BAD
+    f = lib.solon_head_logprobs
+    assert f(at, 8, at, 8, 1, at, 4, 8, 10, at, at, at, at, at, big, None) == BAD            # type
+    assert f(at, 7, at, 8, 0, at, 4, 8, 10, at, at, at, at, at, big, None) == BAD            # pitches
+    assert f(at, 8, at, 7, 0, at, 4, 8, 10, at, at, at, at, at, big, None) == BAD
+    assert f(at + 2, 8, at, 8, 0, at, 4, 8, 10, at, at, at, at, at, big, None) == BAD        # alignment
+    assert f(at, 8, at, 8, 0, at + 4, 4, 8, 10, at, at, at, at, at, big, None) == BAD
+    assert f(at, 8, at, 8, 0, None, 4, 8, 10, at, at, at, at, at, big, None) == BAD          # logp without targets
+    assert f(at, 8, at, 8, 0, at, 4, 8, 10, at, at, at, at, None, big, None) == BAD          # no workspace
+    assert f(at, 8, at, 8, 0, at, 4, 8, 10, at, at, at, at, at + 16, big, None) == BAD
+    assert f(at, 8, at, 8, 0, at, 4, 8, 10, at, at, at, at, at, w(4, 8, 10, 0, 1) - 1, None) == BAD
+    assert f(None, 8, None, 8, 0, None, 0, 8, 10, None, None, None, None, None, 0, None) == 0
+    v = lib.solon_head_logprobs_backward_workspace
+    assert v(0, 8, 10, 0, 0, 1) == 0 and v(4, 8, 10, 0, 3, 1) == BAD and v(4, 8, 10, 1, 0, 1) == BAD
+    assert v(100_000, 64, 50_000, 2, 0, 1) < (1 << 28) + 100_000 * 64 * 4 + 4096                # dlogits comes in pieces
+    b = lib.solon_head_logprobs_backward
+
+    def call(h=at, hp=8, m=at, mp=8, dtype=0, t=at, rows=4, cols=8, vocab=10, parts=2, peak=at, ls=at, ent=None, g=at, gh=None, dh=at, dhp=8, dw=at, dwp=80, gt=0, ws=at, n=big):
+        return b(h, hp, m, mp, dtype, t, rows, cols, vocab, parts, peak, ls, ent, g, gh, dh, dhp, dw, dwp, gt, ws, n, None)
+
+    assert call(dtype=1) == BAD and call(hp=7) == BAD and call(mp=7) == BAD and call(h=None) == BAD and call(m=at + 1) == BAD
+    assert call(parts=3) == BAD and call(parts=0) == BAD and call(peak=None) == BAD and call(ls=None) == BAD and call(t=None) == BAD
+    assert call(gh=at) == BAD and call(dhp=7) == BAD and call(dwp=79) == BAD and call(gt=3) == BAD and call(ws=None) == BAD and call(ws=at + 128) == BAD
+    assert call(n=v(4, 8, 10, 0, 0, 1) - 1) == BAD and call(cols=1 << 23) == BAD
+    assert call(dh=None, dw=None) == 0                                                          # nothing wanted
