@@ -379,7 +379,7 @@ int solon_embedding_forward(const void* weight, int64_t weight_pitch, int dtype,
  *   dweight    device (output), elements of `grad_dtype` (SOLON_F32, SOLON_F64 or SOLON_BF16), grad_pitch >= vocab * cols: rows of the
  *              partition-gradient matrix, for instance
  *   workspace  device, 16-byte aligned, solon_embedding_backward_workspace(...) bytes; its contents need not survive the call */
-int64_t solon_embedding_backward_workspace(int64_t rows, int64_t cols, int partitions);
+int64_t solon_embedding_backward_workspace(int64_t rows, int64_t cols, int64_t vocab, int partitions);
 int solon_embedding_backward(const void* dy, int64_t dy_pitch, int dtype, const int64_t* tokens, int64_t rows, int64_t cols, int64_t vocab, int partitions,
                              double scale, void* dweight, int64_t grad_pitch, int grad_dtype, int accumulate, void* workspace, int64_t workspace_bytes,
                              void* cuda_stream);

@@ -89,7 +89,7 @@ SIGNATURES = {
     "solon_token_logprobs_backward": (c_int, [c_void_p, c_int64, c_int, c_void_p, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                               c_void_p, c_int64, c_void_p]),
     "solon_embedding_forward": (c_int, [c_void_p, c_int64, c_int, c_void_p, c_int64, c_int64, c_int64, c_double, c_void_p, c_int64, c_void_p]),
-    "solon_embedding_backward_workspace": (c_int64, [c_int64, c_int64, c_int]),
+    "solon_embedding_backward_workspace": (c_int64, [c_int64, c_int64, c_int64, c_int]),
     "solon_embedding_backward": (c_int, [c_void_p, c_int64, c_int, c_void_p, c_int64, c_int64, c_int64, c_int, c_double, c_void_p, c_int64, c_int, c_int,
                                          c_void_p, c_int64, c_void_p]),
     "solon_head_logprobs_workspace": (c_int64, [c_int64, c_int64, c_int64, c_int, c_int]),
@@ -434,8 +434,8 @@ def solon_embedding_forward(weight, tokens, scale: float = 1.0, out=None):
 
 
 @functools.lru_cache(maxsize=256)
-def _embedding_workspace(rows: int, cols: int, partitions: int) -> int:
-    return lib().solon_embedding_backward_workspace(rows, cols, partitions)
+def _embedding_workspace(rows: int, cols: int, vocab: int, partitions: int) -> int:
+    return lib().solon_embedding_backward_workspace(rows, cols, vocab, partitions)
 
 
 def _partition_gradient(dweight, like, partitions: int, size: int):
@@ -465,7 +465,7 @@ def solon_embedding_backward(dy, tokens, vocab: int, partitions: int = 1, scale:
     if accumulate and dweight is None:
         raise ValueError("accumulate needs dweight")
     dweight, pdw, pitch, code = _partition_gradient(dweight, dy, partitions, vocab * cols)
-    n_bytes = _embedding_workspace(rows, cols, partitions)
+    n_bytes = _embedding_workspace(rows, cols, vocab, partitions)
     if n_bytes < 0:
         raise SolonError(n_bytes, "solon_embedding_backward_workspace")
     workspace = dy.new_empty(n_bytes, dtype=torch.uint8)
