@@ -34,7 +34,7 @@ constexpr int kEpilogueWarps = 8;
 constexpr int kFirstEpilogue = 4;        // the warps before it bring blocks and multiply, and give registers to the others
 constexpr int kThreads = 32 * (kFirstEpilogue + kEpilogueWarps);
 
-enum HeadMode { kStats, kDz, kDhidden, kDweight };
+enum HeadMode { kStats, kFewRows, kDz, kDhidden, kDweight };
 
 // ------------------------------------------------------------------------------------------------------------ scales
 
@@ -68,7 +68,7 @@ struct HeadArgs {
   // rows
   const int64_t* targets;
   const float *peak, *log_sum, *entropy, *grad_logp, *grad_entropy;
-  // kStats
+  // kStats, kFewRows (whose product is W h^T: tokens are rows of it)
   float* partial;                        // slots x 3 x rows
   float* target_logit;                   // rows
   // kStats, kDz: columns of the product are tokens first + n
@@ -198,7 +198,7 @@ template <int MODE, int BN>
 struct HeadShared {
   static constexpr int kStageBytes = (kRows + BN / 2) * kBlock * 2;
   static constexpr int kStaging = MODE == kStats ? 0 : MODE == kDz ? 8192 : 4096;        // a warp
-  static constexpr int kStages = (232448 - 2048 - kEpilogueWarps * kStaging) / kStageBytes > 8 ? 8 : (232448 - 2048 - kEpilogueWarps * kStaging) / kStageBytes;
+  static constexpr int kStages = (232448 - 2048 - kEpilogueWarps * kStaging) / kStageBytes > 12 ? 12 : (232448 - 2048 - kEpilogueWarps * kStaging) / kStageBytes;
   static constexpr int kBytes = 1024 + kStages * kStageBytes + kEpilogueWarps * kStaging + 512;
 };
 
@@ -211,10 +211,11 @@ struct HeadShared {
 // Every wait ends after two seconds at the latest: the tiles of a CTA whose wait ran out are filled with NaN.
 template <int MODE, int BN, bool BF16, typename O>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_product_kernel(const __grid_constant__ HeadMaps maps, const HeadArgs a) {
-  constexpr bool kAlongA = MODE != kDweight, kAlongB = MODE == kStats || MODE == kDz;
+  constexpr bool kAlongA = MODE != kDweight, kAlongB = MODE == kStats || MODE == kFewRows || MODE == kDz;
   using Shared = HeadShared<MODE, BN>;
   constexpr int kStages = Shared::kStages, kStageBytes = Shared::kStageBytes;
   constexpr int kHalf = BN / 2;              // columns of an epilogue warp
+  constexpr int kBurst = MODE == kFewRows ? 4 : 1;       // blocks whose rows are asked for together
   extern __shared__ char raw[];
   char* smem = (char*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
   char* staging = smem + kStages * kStageBytes;
@@ -225,6 +226,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
   uint32_t* tmem_at = (uint32_t*)(sum_empty + 2);
   int* abort_flag = (int*)(tmem_at + 1);
 
+  pdl_trigger();
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t rank = cluster_rank();
   const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
@@ -261,19 +263,29 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
         const int row = at.m + rank * kRows, col = at.n + rank * kHalf;
         for (int p = 0; p < a.products; p++) {
           const int za = a.piece_a[p] + at.slab * a.slab_a, zb = a.piece_b[p] + at.slab * a.slab_b;
-          for (int kb = 0; kb < a.k_blocks; kb++) {
-            pipe::mbar_wait(empty + s, phase ^ 1, abort_flag, status);
-            if (*(volatile int*)abort_flag) goto loads_done;
-            if (rank == 0) pipe::mbar_arrive_expect_tx(full + s, 2 * kStageBytes);
-            const uint32_t dst = pipe::smem_addr(smem + s * kStageBytes);
-            const int k = kb * kBlock;
+          for (int kb0 = 0; kb0 < a.k_blocks; kb0 += kBurst) {
+            const int burst = min(kBurst, a.k_blocks - kb0);
+            const int first = s;
+            for (int i = 0; i < burst; i++) {
+              pipe::mbar_wait(empty + s, phase ^ 1, abort_flag, status);
+              if (*(volatile int*)abort_flag) goto loads_done;
+              if (rank == 0) pipe::mbar_arrive_expect_tx(full + s, 2 * kStageBytes);
+              if (++s == kStages) s = 0, phase ^= 1;
+            }
 #pragma unroll
             for (int h = 0; h < kRows / kBlock; h++)
-              load_block(dst + h * kBlockBytes, &maps.a, kAlongA ? k : row + h * kBlock, kAlongA ? row + h * kBlock : k, za, full + s);
+              for (int i = 0; i < burst; i++) {
+                const int at_stage = first + i < kStages ? first + i : first + i - kStages, k = (kb0 + i) * kBlock;
+                load_block(pipe::smem_addr(smem + at_stage * kStageBytes) + h * kBlockBytes, &maps.a, kAlongA ? k : row + h * kBlock,
+                           kAlongA ? row + h * kBlock : k, za, full + at_stage);
+              }
 #pragma unroll
-            for (int h = 0; h < kHalf / kBlock; h++)
-              load_block(dst + kRows * 128 + h * kBlockBytes, &maps.b, kAlongB ? k : col + h * kBlock, kAlongB ? col + h * kBlock : k, zb, full + s);
-            if (++s == kStages) s = 0, phase ^= 1;
+            for (int h = 0; h < kHalf; h += kBlock)        // (fewer than 64 rows: a box of its own size)
+              for (int i = 0; i < burst; i++) {
+                const int at_stage = first + i < kStages ? first + i : first + i - kStages, k = (kb0 + i) * kBlock;
+                load_block(pipe::smem_addr(smem + at_stage * kStageBytes) + kRows * 128 + h * 128, &maps.b, kAlongB ? k : col + h, kAlongB ? col + h : k, zb,
+                           full + at_stage);
+              }
           }
         }
       }
@@ -313,13 +325,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
     char* stage = staging + (warp - kFirstEpilogue) * Shared::kStaging;
     float undo[2] = {1.0f, 1.0f};
     if (a.scaled) {
-      const int sa = MODE == kStats || MODE == kDz ? (a.scaled & 1 ? scale_exponent(a.words->hidden) : 0) : (a.scaled & 4 ? scale_exponent(a.words->dz) : 0);
+      const int sa = MODE == kStats || MODE == kFewRows || MODE == kDz ? (a.scaled & 1 ? scale_exponent(a.words->hidden) : 0) : (a.scaled & 4 ? scale_exponent(a.words->dz) : 0);
       const int sb = MODE == kDweight ? (a.scaled & 1 ? scale_exponent(a.words->hidden) : 0) : (a.scaled & 2 ? scale_exponent(a.words->weight) : 0);
       undo[0] = power_of_two(-sa);
       undo[1] = power_of_two(-sb);
     }
     uint32_t sum_phase = 0;
     int half = 0;
+    [[maybe_unused]] RowSums rows_so_far[kHalf / 32];
+    if constexpr (MODE == kFewRows) {
+#pragma unroll
+      for (int i = 0; i < kHalf / 32; i++) rows_so_far[i] = {-INFINITY, 0.0f, 0.0f};
+    }
     for (int64_t t = pair; t < tiles_all; t += pairs) {
       const TileAt at = tile_at(a, t, BN);
       const int row0 = at.m + rank * kRows + quarter * 32, row = row0 + lane, col = at.n + side * kHalf;
@@ -375,6 +392,35 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
           p[0] = sums.m;
           p[a.m] = sums.s;
           p[2 * (int64_t)a.m] = sums.a;
+        }
+      } else if constexpr (MODE == kFewRows) {
+        // lanes are tokens and columns are rows here: 32 x 32 of them are turned, so that a lane has 32 tokens of a row
+        const int inside = a.m - row0;
+        float4* turned = reinterpret_cast<float4*>(stage);
+        const float* turned1 = reinterpret_cast<const float*>(stage);
+#pragma unroll
+        for (int c = 0; c < kHalf; c += 32) {
+          if (col + c >= a.n || inside <= 0) break;
+          __syncwarp();
+          stage_rows(v + c, turned, lane);
+          __syncwarp();
+          float z[32];
+#pragma unroll
+          for (int r = 0; r < 32; r++) z[r] = turned1[(r * 8 + ((lane / 4) ^ (r & 7))) * 4 + lane % 4];
+          if (inside < 32) {
+#pragma unroll
+            for (int r = 0; r < 32; r++)
+              if (r >= inside) z[r] = -INFINITY;
+          }
+          const int mine = col + c + lane;
+          const int64_t token = mine < a.n && a.targets ? a.targets[mine] - row0 : -1;
+          if (token >= 0 && token < min(32, inside)) {
+            const int r = (int)token;
+            a.target_logit[mine] = turned1[(r * 8 + ((lane / 4) ^ (r & 7))) * 4 + lane % 4];
+          }
+          RowSums sums;
+          row_sums(z, sums);
+          rows_so_far[c / 32] = join(rows_so_far[c / 32], sums);
         }
       } else if constexpr (MODE == kDz) {
         float peak = 0.0f, log_sum = 0.0f, h = 0.0f, g = 0.0f, gh = 0.0f;
@@ -479,6 +525,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
         }
       }
     }
+    if constexpr (MODE == kFewRows) {
+#pragma unroll
+      for (int c = 0; c < kHalf; c += 32) {
+        const int mine = side * kHalf + c + lane;
+        if (mine < a.n) {
+          float* p = a.partial + (int64_t)(blockIdx.x * 4 + quarter) * 3 * a.n + mine;
+          p[0] = rows_so_far[c / 32].m;
+          p[a.n] = rows_so_far[c / 32].s;
+          p[2 * (int64_t)a.n] = rows_so_far[c / 32].a;
+        }
+      }
+    }
     if (MODE == kDz && lane == 0) stores_done();
   }
   if (*(volatile int*)abort_flag) pipe::drain_delay();
@@ -500,25 +558,22 @@ struct HeadRowsArgs {
   float *partial, *target_logit;
 };
 
-// Up to NR rows: a warp takes R rows of W at a time, E elements a lane and access, against the hidden rows in shared memory (float32; groups of
-// four columns of a lane apart, so that its reads of 16 bytes fall on all banks), and adds the products up over its lanes so that each lane ends with one
-// logit, or a part of a set of lanes.  W is read once: 4 to 16 accesses of 16 bytes a lane are on the way.
-template <typename T, int NR, int R, int E>
-__global__ void __launch_bounds__(256) head_rows_kernel(HeadRowsArgs a) {
+// Up to NR rows: a warp takes R rows of W at a time against the hidden rows in shared memory (float32), a lane G groups of EACH consecutive columns
+// 32 EACH apart, and adds the products up over its lanes so that each lane ends with one logit, or a part of a set of lanes.  W is read once; the
+// next columns are on the way while these are multiplied.
+template <typename T, int NR, int R, int EACH, int G>
+__global__ void __launch_bounds__(256, 2) head_rows_kernel(HeadRowsArgs a) {
   extern __shared__ __align__(16) float hidden_smem[];
   __shared__ RowSums merged[8][NR];
-  constexpr int kCount = NR * R;
-  constexpr int kGroups = E > 4 ? E / 4 : 1, kEach = E / kGroups;      // a lane's columns: kGroups runs of kEach
+  pdl_trigger();
+  constexpr int kCount = NR * R, kStep = 32 * EACH * G;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  for (int i = threadIdx.x; i < NR * a.padded; i += 256) {
-    const int n = i / a.padded, k = i % a.padded;
-    const float x = n < a.rows && k < a.cols ? to_float(((const T*)a.hidden)[n * a.hidden_pitch + k]) : 0.0f;
-    const int step = k / (32 * E), in = k % (32 * E), l = in / E, g = in % E / kEach, j = in % kEach;
-    hidden_smem[n * a.padded + step * 32 * E + (g * 32 + l) * kEach + j] = x;
-  }
+  for (int n = 0; n < NR; n++)
+    for (int k = threadIdx.x; k < a.padded; k += 256)
+      hidden_smem[n * a.padded + k] = n < a.rows && k < a.cols ? to_float(((const T*)a.hidden)[n * a.hidden_pitch + k]) : 0.0f;
   __syncthreads();
   RowSums sums = {-INFINITY, 0.0f, 0.0f};
-  constexpr int kShift = kCount == 32 ? 0 : kCount == 16 ? 1 : 2;
+  constexpr int kShift = kCount == 32 ? 0 : kCount == 16 ? 1 : kCount == 8 ? 2 : 3;
   const int index = lane >> kShift, mine_row = index / R, mine_token = index % R;
   const bool counts = (lane & ((1 << kShift) - 1)) == 0 && mine_row < a.rows;
   const int64_t target = counts && a.targets ? a.targets[mine_row] : -1;
@@ -531,33 +586,37 @@ __global__ void __launch_bounds__(256) head_rows_kernel(HeadRowsArgs a) {
     const T* w[R];
 #pragma unroll
     for (int r = 0; r < R; r++) w[r] = (const T*)a.weight + min(v0 + r, a.vocab - 1) * a.weight_pitch;
-    for (int k0 = 0; k0 < a.cols; k0 += 32 * E) {
-      const int64_t k = k0 + lane * E;
-      Pack<T, E> x[R];
+    Pack<T, EACH> x[R][G], next[R][G];
+    auto fetch = [&](Pack<T, EACH> (&to)[R][G], int k0) {         // (EACH divides the number of columns)
 #pragma unroll
-      for (int r = 0; r < R; r++) {
-        if (k + E <= a.cols) {
-          if constexpr (sizeof(T) * E == 16) *reinterpret_cast<uint4*>(&x[r]) = load16_once(w[r] + k);
-          else x[r] = load_pack<T, E>(w[r] + k);
-        } else {
+      for (int q = 0; q < G; q++) {
+        const int k = k0 + (q * 32 + lane) * EACH;
 #pragma unroll
-          for (int e = 0; e < E; e++) x[r].e[e] = k + e < a.cols ? w[r][k + e] : from_float<T>(0.0f);
+        for (int r = 0; r < R; r++) {
+          to[r][q] = {};
+          if (k < a.cols) to[r][q] = load_pack<T, EACH>(w[r] + k);
+        }
+      }
+    };
+    fetch(x, 0);
+    for (int k0 = 0; k0 < a.cols; k0 += kStep) {
+      if (k0 + kStep < a.cols) fetch(next, k0 + kStep);
+#pragma unroll
+      for (int q = 0; q < G; q++) {
+        const int k = k0 + (q * 32 + lane) * EACH;
+#pragma unroll
+        for (int n = 0; n < NR; n++) {
+          const Pack<float, EACH> h = load_pack<float, EACH>(hidden_smem + n * a.padded + k);
+#pragma unroll
+          for (int r = 0; r < R; r++)
+#pragma unroll
+            for (int e = 0; e < EACH; e++) acc[n * R + r] = fmaf(to_float(x[r][q].e[e]), h.e[e], acc[n * R + r]);
         }
       }
 #pragma unroll
-      for (int n = 0; n < NR; n++) {
-        float h[E];
+      for (int r = 0; r < R; r++)
 #pragma unroll
-        for (int q = 0; q < kGroups; q++) {
-          const Pack<float, kEach> p = load_pack<float, kEach>(hidden_smem + n * a.padded + k0 + (q * 32 + lane) * kEach);
-#pragma unroll
-          for (int j = 0; j < kEach; j++) h[q * kEach + j] = p.e[j];
-        }
-#pragma unroll
-        for (int r = 0; r < R; r++)
-#pragma unroll
-          for (int e = 0; e < E; e++) acc[n * R + r] = fmaf(to_float(x[r].e[e]), h[e], acc[n * R + r]);
-      }
+        for (int q = 0; q < G; q++) x[r][q] = next[r][q];
     }
 #pragma unroll
     for (int o = 16, half = kCount / 2; o > 0; o /= 2, half /= 2) {
@@ -607,6 +666,7 @@ __global__ void __launch_bounds__(256) head_join_kernel(HeadJoinArgs a) {
   const int r = threadIdx.x % ROWS, group = threadIdx.x / ROWS;
   const int64_t row = (int64_t)blockIdx.x * ROWS + r;
   RowSums sums = {-INFINITY, 0.0f, 0.0f};
+  pdl_wait();
   if (row < a.rows)
 #pragma unroll 4
     for (int64_t s = group; s < a.slots; s += kGroups) {
@@ -730,7 +790,8 @@ static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 // What a call keeps where: offsets into the workspace, in bytes.
 struct HeadPlan {
   // few rows
-  int row_kernel;                        // 0, or the number of rows that the kernel for few rows is built for
+  int row_kernel;                        // 0, or the number of rows that the kernel of multiply-adds is built for
+  bool few;                              // the product is taken the other way round
   int64_t slots;
   // products
   int pieces;                            // of hidden and weight
@@ -742,16 +803,17 @@ struct HeadPlan {
 };
 
 constexpr int64_t kHeadSharedRows = 200 * 1024;       // bytes of hidden rows that the kernel for few rows holds
-constexpr int kRowBlocks = 148 * 3;
+constexpr int kRowBlocks = 148 * 2;
+
+constexpr int kFewMost = 128;
+constexpr int kFewPairs = 74;
 
 static int64_t rows_padded(int64_t cols) { return up(cols, 256); }
 
 static HeadPlan head_forward_plan(int64_t rows, int64_t cols, int64_t vocab, int dtype, bool aligned) {
   HeadPlan p = {};
-  // W has to be read once and is all there is to read: up to 8 rows the multiply-adds keep up with it, and up to 16 they cost less than
-  // splitting or copying W first would.
-  const int most = dtype == SOLON_F32 || !aligned ? 16 : 8;
-  if (rows <= most) {
+  // W has to be read once and is all there is to read.  Up to 16 rows the multiply-adds cost less than splitting or copying W first would.
+  if (rows <= 16 && (dtype == SOLON_F32 || !aligned)) {
     int nr = 1;
     while (nr < rows) nr *= 2;
     if (nr * rows_padded(cols) * 4 <= kHeadSharedRows) p.row_kernel = nr;
@@ -767,7 +829,10 @@ static HeadPlan head_forward_plan(int64_t rows, int64_t cols, int64_t vocab, int
   if (p.row_kernel) {
     p.slots = kRowBlocks;
   } else {
-    p.slots = 2 * ((vocab + kTile - 1) / kTile);
+    // Up to 128 rows are the columns of tiles, not their rows: half the products of a tile that is mostly empty.
+    p.few = rows <= kFewMost;
+    const int64_t tiles = (vocab + kTile - 1) / kTile;
+    p.slots = p.few ? 8 * std::min<int64_t>(tiles, kFewPairs) : 2 * tiles;
     p.pieces = dtype == SOLON_F32 ? 2 : 1;
     p.split = dtype == SOLON_F32 || !aligned;
     p.pitch = up(cols, 8);
@@ -811,32 +876,37 @@ static bool aligned16(const void* p, int64_t pitch, int64_t rows, int dtype) {
   return !(((uintptr_t)p & 15) || (rows > 1 && (pitch * element_size(dtype)) & 15));
 }
 
-template <typename T, int NR, int R, int E>
+template <typename T, int NR, int R, int EACH, int G>
 static int head_rows_launch(const HeadRowsArgs& a, cudaStream_t stream) {
   const size_t smem = (size_t)NR * a.padded * 4;
-  SOLON_SHARED_MEMORY_ONCE((head_rows_kernel<T, NR, R, E>), kHeadSharedRows);
-  head_rows_kernel<T, NR, R, E><<<kRowBlocks, 256, smem, stream>>>(a);
+  SOLON_SHARED_MEMORY_ONCE((head_rows_kernel<T, NR, R, EACH, G>), kHeadSharedRows);
+  head_rows_kernel<T, NR, R, EACH, G><<<kRowBlocks, 256, smem, stream>>>(a);
   SOLON_CUDA_TRY(cudaGetLastError());
   return SOLON_OK;
 }
 
-template <typename T, int E>
+template <typename T, int EACH, int G>
 static int head_rows_e(const HeadRowsArgs& a, int nr, cudaStream_t stream) {
   switch (nr) {
-    case 1: return head_rows_launch<T, 1, 8, E>(a, stream);
-    case 2: return head_rows_launch<T, 2, 8, E>(a, stream);
-    case 4: return head_rows_launch<T, 4, 8, E>(a, stream);
-    case 8: return head_rows_launch<T, 8, 4, E>(a, stream);
-    default: return head_rows_launch<T, 16, 2, E>(a, stream);
+    case 1: return head_rows_launch<T, 1, sizeof(T) == 4 ? 8 : 4, EACH, G>(a, stream);
+    case 2: return head_rows_launch<T, 2, 4, EACH, G>(a, stream);
+    case 4: return head_rows_launch<T, 4, 4, EACH, G>(a, stream);
+    case 8: return head_rows_launch<T, 8, 4, EACH, G>(a, stream);
+    default: return head_rows_launch<T, 16, 2, EACH, G>(a, stream);
   }
 }
 
+// As many consecutive columns an access as every row's alignment and the number of columns allow, 16 to 32 bytes a row of W and lane.
 template <typename T>
 static int head_rows_t(const HeadRowsArgs& a, int nr, cudaStream_t stream) {
-  uintptr_t both = (uintptr_t)a.weight | (uintptr_t)(a.weight_pitch * sizeof(T));
-  if (!(both & 15)) return head_rows_e<T, 16 / sizeof(T)>(a, nr, stream);
-  if (!(both & 3) && sizeof(T) == 2) return head_rows_e<T, 2>(a, nr, stream);
-  return head_rows_e<T, 1>(a, nr, stream);
+  const uintptr_t both = (uintptr_t)a.weight | (uintptr_t)((a.weight_pitch | a.cols) * sizeof(T));
+  if constexpr (sizeof(T) == 4) {
+    if (!(both & 15)) return head_rows_e<T, 4, 1>(a, nr, stream);
+    return head_rows_e<T, 1, 4>(a, nr, stream);
+  } else {
+    if (!(both & 3)) return head_rows_e<T, 2, 4>(a, nr, stream);
+    return head_rows_e<T, 1, 8>(a, nr, stream);
+  }
 }
 
 template <int MODE, int BN, bool BF16, typename O>
@@ -847,7 +917,7 @@ static int head_product_launch(const HeadMaps& maps, HeadArgs a, int sms, cudaSt
   a.n_tiles = (a.n + BN - 1) / BN;
   a.chunk = (MODE == kDhidden || MODE == kDweight) && sizeof(O) == 2 ? 64 : 4;
   const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles * a.slabs;
-  const int pairs = (int)std::min<int64_t>(tiles, sms / 2);
+  const int pairs = (int)std::min<int64_t>(tiles, MODE == kFewRows ? std::min(kFewPairs, sms / 2) : sms / 2);
   SOLON_SHARED_MEMORY_ONCE(kernel, bytes);
   kernel<<<2 * pairs, kThreads, bytes, stream>>>(maps, a);
   SOLON_CUDA_TRY(cudaGetLastError());
@@ -909,7 +979,11 @@ static bool head_sizes_ok(int64_t rows, int64_t cols, int64_t vocab) {
          (rows == 0 || vocab <= (1ll << 46) / rows);
 }
 
-static int head_stats(const HeadMaps& maps, const HeadArgs& a, bool bf16, int sms, cudaStream_t stream) {
+static int head_stats(const HeadMaps& maps, const HeadArgs& a, bool few, bool bf16, int sms, cudaStream_t stream) {
+  if (few && a.n <= 64 && bf16) return head_product_launch<kFewRows, 64, true, float>(maps, a, sms, stream);
+  if (few && a.n <= 64) return head_product_launch<kFewRows, 64, false, float>(maps, a, sms, stream);
+  if (few && bf16) return head_product_launch<kFewRows, 128, true, float>(maps, a, sms, stream);
+  if (few) return head_product_launch<kFewRows, 128, false, float>(maps, a, sms, stream);
   if (bf16) return head_product_launch<kStats, 256, true, float>(maps, a, sms, stream);
   return head_product_launch<kStats, 256, false, float>(maps, a, sms, stream);
 }
@@ -947,10 +1021,10 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
   if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < plan.total) return SOLON_ERR_INVALID_ARG;
   int sms = 0, rc;
   if ((rc = current_sms(&sms))) return rc;
+  const int64_t slots = plan.few ? std::min<int64_t>(plan.slots, 8 * (sms / 2)) : plan.slots;
   cudaStream_t stream = (cudaStream_t)cuda_stream;
   char* ws = (char*)workspace;
   HeadWords* words = (HeadWords*)(ws + plan.words);
-  int64_t slots = plan.slots;
   if (plan.row_kernel) {
     const HeadRowsArgs a = {hidden, weight, hidden_pitch, vocab > 1 ? weight_pitch : cols, cols, vocab, targets, (int)rows, (int)rows_padded(cols),
                             (float*)(ws + plan.partial), (float*)(ws + plan.target_logit)};
@@ -959,8 +1033,8 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
     else rc = head_rows_t<__half>(a, plan.row_kernel, stream);
     if (rc) return rc;
   } else {
-    SOLON_CUDA_TRY(cudaMemsetAsync(words, 0, sizeof(HeadWords), stream));
     if (dtype == SOLON_F32) {
+      SOLON_CUDA_TRY(cudaMemsetAsync(words, 0, sizeof(HeadWords), stream));
       const HeadScanArgs scan = {(const float*)hidden, (const float*)weight, hidden_pitch, weight_pitch, rows, cols, vocab, nullptr, nullptr, nullptr, 0, words};
       if ((rc = head_scan(scan, sms, stream))) return rc;
     }
@@ -969,7 +1043,7 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
     if ((rc = head_operand(weight, weight_pitch, vocab, cols, dtype, plan, ws + plan.weight, &words->weight, sms, stream, &w))) return rc;
     const bool bf16 = dtype == SOLON_BF16;
     HeadMaps maps = {};
-    if (!tensor_map(&maps.a, h.p, bf16, cols, rows, h.pieces, h.pitch, rows * h.pitch, kBlock) ||
+    if (!tensor_map(&maps.a, h.p, bf16, cols, rows, h.pieces, h.pitch, rows * h.pitch, plan.few && rows <= 64 ? 32 : kBlock) ||
         !tensor_map(&maps.b, w.p, bf16, cols, vocab, w.pieces, w.pitch, vocab * w.pitch, kBlock))
       return SOLON_ERR_CUDA;
     HeadArgs a = {};
@@ -984,13 +1058,15 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
     a.partial = (float*)(ws + plan.partial);
     a.target_logit = (float*)(ws + plan.target_logit);
     a.vocab = vocab;
-    if ((rc = head_stats(maps, a, bf16, sms, stream))) return rc;
+    if (plan.few) {
+      std::swap(maps.a, maps.b);
+      std::swap(a.m, a.n);
+    }
+    if ((rc = head_stats(maps, a, plan.few, bf16, sms, stream))) return rc;
   }
   const HeadJoinArgs j = {(const float*)(ws + plan.partial), (const float*)(ws + plan.target_logit), rows, slots, vocab, targets, logp, entropy, peak, log_sum};
-  if (rows < 2048) head_join_kernel<1><<<(unsigned)rows, 256, 0, stream>>>(j);
-  else head_join_kernel<32><<<(unsigned)((rows + 31) / 32), 256, 0, stream>>>(j);
-  SOLON_CUDA_TRY(cudaGetLastError());
-  return SOLON_OK;
+  if (rows < 2048) return launch_dependent(head_join_kernel<1>, dim3((unsigned)rows), dim3(256), 0, stream, j);
+  return launch_dependent(head_join_kernel<32>, dim3((unsigned)((rows + 31) / 32)), dim3(256), 0, stream, j);
 }
 
 int64_t solon_head_logprobs_backward_workspace(int64_t rows, int64_t cols, int64_t vocab, int dtype, int grad_dtype, int aligned) {
@@ -1028,7 +1104,7 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
   char* ws = (char*)workspace;
   HeadWords* words = (HeadWords*)(ws + plan.words);
   const bool f32 = dtype == SOLON_F32, bf16 = dtype == SOLON_BF16;
-  SOLON_CUDA_TRY(cudaMemsetAsync(words, 0, sizeof(HeadWords), stream));
+  if (!bf16) SOLON_CUDA_TRY(cudaMemsetAsync(words, 0, sizeof(HeadWords), stream));
   const HeadScanArgs scan = {f32 ? (const float*)hidden : nullptr, f32 ? (const float*)weight : nullptr, hidden_pitch, weight_pitch, rows, cols, vocab,
                              grad_logp, grad_entropy, entropy, !bf16, words};
   if ((rc = head_scan(scan, sms, stream))) return rc;
