@@ -112,16 +112,20 @@ __device__ __forceinline__ void store1(O* p, float v) {
 template <typename O>
 __device__ __forceinline__ void write_rows(const float4* stage, O* out, int64_t pitch, int row, int col, int m, int n, bool wide, int lane) {
   if (wide && col + 32 <= n) {
+    const int c = lane % 8;
+    O* p = out + (row + lane / 8) * pitch + col + c * 4;
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-      const int r = i * 4 + lane / 8, c = lane % 8;
-      if (row + r < m) store4(out + (row + r) * pitch + col + c * 4, stage[r * 8 + (c ^ (r & 7))]);
+    for (int i = 0; i < 8; i++, p += 4 * pitch) {
+      const int r = i * 4 + lane / 8;
+      if (row + r < m) store4(p, stage[r * 8 + (c ^ (r & 7))]);
     }
   } else {
-    const float* s = reinterpret_cast<const float*>(stage);
+    const float* s = reinterpret_cast<const float*>(stage) + lane % 4;
+    O* p = out + row * pitch + col + lane;
+    const int rows = col + lane < n ? m - row : 0;
 #pragma unroll 8
-    for (int r = 0; r < 32; r++)
-      if (row + r < m && col + lane < n) store1(out + (row + r) * pitch + col + lane, s[(r * 8 + ((lane / 4) ^ (r & 7))) * 4 + lane % 4]);
+    for (int r = 0; r < 32; r++, p += pitch)
+      if (r < rows) store1(p, s[(r * 8 + ((lane / 4) ^ (r & 7))) * 4]);
   }
 }
 
@@ -184,13 +188,11 @@ struct TileAt {
   int slab, m, n;                        // first row and column
 };
 // Tiles of eight row tiles at a time, columns of those before the next eight: what runs at the same time shares rows of both operands in L2.
-__device__ __forceinline__ TileAt tile_at(const HeadArgs& a, int64_t t, int bn) {
-  const int64_t per_slab = (int64_t)a.m_tiles * a.n_tiles;
-  const int slab = (int)(t / per_slab);
-  const int64_t r = t - slab * per_slab;
-  const int group = (int)(r / (8 * a.n_tiles));
-  const int high = min(8, a.m_tiles - group * 8), in = (int)(r - (int64_t)group * 8 * a.n_tiles);
-  return {slab, (group * 8 + in % high) * kTile, in / high * bn};
+__device__ __forceinline__ TileAt tile_at(const HeadArgs& a, uint32_t t, int bn) {
+  const uint32_t per_slab = (uint32_t)a.m_tiles * a.n_tiles, slab = t / per_slab, r = t - slab * per_slab;
+  const uint32_t band = 8u * a.n_tiles, group = r / band, in = r - group * band;
+  const uint32_t high = min(8u, a.m_tiles - group * 8), column = in / high;
+  return {(int)slab, (int)((group * 8 + in - column * high) * kTile), (int)column * bn};
 }
 
 // stages of A and B blocks, then the epilogue warps' staging, then barriers
@@ -205,8 +207,8 @@ struct HeadShared {
 // Warp 0 of each CTA brings blocks, warp 1 of the first CTA multiplies, eight warps take finished sums from tensor memory, of which one half is read
 // while the other is being filled, and keep a tile's result in registers: 128 columns of a row a thread.
 // The tensor cores cut off what lies below an accumulator's last bit, which costs a sum of n steps of 16 about n / 2 units of 2^-25, always towards 0
-// (measured: 1.6e-8 a step).  So a result that is wanted in float32 is summed 256 inner indices at a time, and those sums are added in
-// registers, rounded to nearest.
+// (measured: 1.6e-8 a step, 2e-5 for dh of 50,001 tokens).  So a result that is wanted in float32 is summed 512 inner indices at a time, and those sums are
+// added in registers, rounded to nearest (256 at a time: 5 to 15 % slower; all at once: 1 % faster).
 // Persistent: a pair takes every (pairs)-th tile.
 // Every wait ends after two seconds at the latest: the tiles of a CTA whose wait ran out are filled with NaN.
 template <int MODE, int BN, bool BF16, typename O>
@@ -230,7 +232,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t rank = cluster_rank();
   const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
-  const int64_t tiles_all = (int64_t)a.m_tiles * a.n_tiles * a.slabs;
+  const uint32_t tiles_all = (uint32_t)a.m_tiles * a.n_tiles * a.slabs;
   const int blocks = a.products * a.k_blocks;
   int* status = &a.flags->status;
 
@@ -258,7 +260,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
     if (warp == 0 && lane == 0) {
       int s = 0;
       uint32_t phase = 0;
-      for (int64_t t = pair; t < tiles_all; t += pairs) {
+      for (uint32_t t = pair; t < tiles_all; t += pairs) {
         const TileAt at = tile_at(a, t, BN);
         const int row = at.m + rank * kRows, col = at.n + rank * kHalf;
         for (int p = 0; p < a.products; p++) {
@@ -294,7 +296,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
       constexpr uint32_t idesc = instruction(BF16, kAlongA, kAlongB, BN);
       int s = 0, half = 0;
       uint32_t phase = 0, sum_phase = 0;
-      for (int64_t t = pair; t < tiles_all; t += pairs) {
+      for (uint32_t t = pair; t < tiles_all; t += pairs) {
         for (int kb = 0; kb < blocks;) {
           pipe::mbar_wait(sum_empty + half, sum_phase ^ 1, abort_flag, status);
           if (*(volatile int*)abort_flag) goto products_done;
@@ -337,7 +339,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
 #pragma unroll
       for (int i = 0; i < kHalf / 32; i++) rows_so_far[i] = {-INFINITY, 0.0f, 0.0f};
     }
-    for (int64_t t = pair; t < tiles_all; t += pairs) {
+    for (uint32_t t = pair; t < tiles_all; t += pairs) {
       const TileAt at = tile_at(a, t, BN);
       const int row0 = at.m + rank * kRows + quarter * 32, row = row0 + lane, col = at.n + side * kHalf;
       float v[kHalf];
@@ -915,8 +917,9 @@ static int head_product_launch(const HeadMaps& maps, HeadArgs a, int sms, cudaSt
   constexpr int bytes = HeadShared<MODE, BN>::kBytes;
   a.m_tiles = (a.m + kTile - 1) / kTile;
   a.n_tiles = (a.n + BN - 1) / BN;
-  a.chunk = (MODE == kDhidden || MODE == kDweight) && sizeof(O) == 2 ? 64 : 4;
+  a.chunk = (MODE == kDhidden || MODE == kDweight) && sizeof(O) == 2 ? 64 : 8;
   const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles * a.slabs;
+  if (tiles > 0x7FFF0000) return SOLON_ERR_INVALID_ARG;
   const int pairs = (int)std::min<int64_t>(tiles, MODE == kFewRows ? std::min(kFewPairs, sms / 2) : sms / 2);
   SOLON_SHARED_MEMORY_ONCE(kernel, bytes);
   kernel<<<2 * pairs, kThreads, bytes, stream>>>(maps, a);

@@ -1,8 +1,8 @@
 """Log probabilities straight from hidden states and output matrix, and their gradient, against the formulas in float64 and against differences.
 
 Tolerances (u = 2^-24, s_iv = sum_c |h_ic w_vc|).  Products of 16-bit elements are exact in float32; the tensor cores add 16 of them to an accumulator
-and cut the result off, at most 4 u of what it holds a step, and after 16 steps (16 u s each way on average, 64 u s at most) the sum is added to
-another in float32: a logit is off by at most z_tol = (64 + cols / 256) u s.  float32 elements are two float16 pieces: 2^-22 of each factor, the
+and cut off what lies below its last bit, less than 2 u of what it holds a step, and after 32 steps (64 u s at most) the sum is added to another in
+float32, u s at most each time: a logit is off by at most z_tol = (64 + cols / 256) u s.  float32 elements are two float16 pieces: 2^-22 of each factor, the
 product of the second pieces left out (2^-22) and 2^-40 of each tensor's largest element: 2^-20 s + cols 2^-39 max|h| max|w| more.
 (Few rows: ordinary sums, (cols / 32 + 8) u s, which is below that.)
 From there the statistics are those of solon_token_logprobs: with t = max z_tol over the row, k = vocab / 256 + 72 additions and D = E|z - M| + 4
