@@ -62,6 +62,7 @@ struct HeadArgs {
   int chunk;                             // blocks of 64 that are summed in tensor memory before the sum is added to the one in registers
   int piece_a[3], piece_b[3];            // third coordinate of the tensor maps for slab 0; slab s is s further
   int slab_a, slab_b;                    // 1: the operand has slabs
+  int b_by_blocks;                       // B's map takes 128 columns a copy, where its rows lie across the inner dimension
   const HeadWords* words;
   HeadWords* flags;
   int scaled;                            // bits: 1 hidden, 2 weight, 4 dz carry a power of two
@@ -274,20 +275,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
               if (rank == 0) pipe::mbar_arrive_expect_tx(full + s, 2 * kStageBytes);
               if (++s == kStages) s = 0, phase ^= 1;
             }
+            for (int i = 0; i < burst; i++) {
+              const int at_stage = first + i < kStages ? first + i : first + i - kStages, k = (kb0 + i) * kBlock;
+              const uint32_t dst = pipe::smem_addr(smem + at_stage * kStageBytes);
+              if (kAlongA) load_block(dst, &maps.a, k, row, za, full + at_stage);
+              else load_blocks(dst, &maps.a, k, row / kBlock, za, full + at_stage);
+            }
+            for (int i = 0; i < burst; i++) {
+              const int at_stage = first + i < kStages ? first + i : first + i - kStages, k = (kb0 + i) * kBlock;
+              const uint32_t dst = pipe::smem_addr(smem + at_stage * kStageBytes) + kRows * 128;
+              if (kAlongB) load_block(dst, &maps.b, k, col, zb, full + at_stage);
+              else if (kHalf > kBlock && a.b_by_blocks) load_blocks(dst, &maps.b, k, col / kBlock, zb, full + at_stage);
+              else
 #pragma unroll
-            for (int h = 0; h < kRows / kBlock; h++)
-              for (int i = 0; i < burst; i++) {
-                const int at_stage = first + i < kStages ? first + i : first + i - kStages, k = (kb0 + i) * kBlock;
-                load_block(pipe::smem_addr(smem + at_stage * kStageBytes) + h * kBlockBytes, &maps.a, kAlongA ? k : row + h * kBlock,
-                           kAlongA ? row + h * kBlock : k, za, full + at_stage);
-              }
-#pragma unroll
-            for (int h = 0; h < kHalf; h += kBlock)        // (fewer than 64 rows: a box of its own size)
-              for (int i = 0; i < burst; i++) {
-                const int at_stage = first + i < kStages ? first + i : first + i - kStages, k = (kb0 + i) * kBlock;
-                load_block(pipe::smem_addr(smem + at_stage * kStageBytes) + kRows * 128 + h * 128, &maps.b, kAlongB ? k : col + h, kAlongB ? col + h : k, zb,
-                           full + at_stage);
-              }
+                for (int h = 0; h < kHalf; h += kBlock) load_block(dst + h * 128, &maps.b, col + h, k, zb, full + at_stage);
+            }
           }
         }
       }
@@ -837,7 +839,7 @@ static HeadPlan head_forward_plan(int64_t rows, int64_t cols, int64_t vocab, int
     p.slots = p.few ? 8 * std::min<int64_t>(tiles, kFewPairs) : 2 * tiles;
     p.pieces = dtype == SOLON_F32 ? 2 : 1;
     p.split = dtype == SOLON_F32 || !aligned;
-    p.pitch = up(cols, 8);
+    p.pitch = up(cols, kBlock);
     if (p.split) {
       p.hidden = take(p.pieces * rows * p.pitch * 2);
       p.weight = take(p.pieces * vocab * p.pitch * 2);
@@ -854,7 +856,7 @@ static HeadPlan head_backward_plan(int64_t rows, int64_t cols, int64_t vocab, in
   HeadPlan p = {};
   p.pieces = dtype == SOLON_F32 ? 2 : 1;
   p.split = dtype == SOLON_F32 || !aligned;
-  p.pitch = up(cols, 8);
+  p.pitch = up(cols, kBlock);
   p.dz_pieces = dtype == SOLON_F32 || grad_dtype != SOLON_BF16 ? 2 : 1;
   p.width = std::min(up(vocab, 64), std::max<int64_t>(kTile, kDzBytes / (rows * 2 * p.dz_pieces) / kTile * kTile));
   int64_t at = 0;
@@ -928,9 +930,11 @@ static int head_product_launch(const HeadMaps& maps, HeadArgs a, int sms, cudaSt
 }
 
 // 256 columns a tile, or 128 where that covers the columns with a sixth less.
+static bool narrow(int64_t cols) { return up(cols, 128) * 6 <= up(cols, 256) * 5; }
+
 template <int MODE, bool BF16, typename O>
 static int head_product(const HeadMaps& maps, const HeadArgs& a, int sms, cudaStream_t stream) {
-  if (up(a.n, 128) * 6 <= up(a.n, 256) * 5) return head_product_launch<MODE, 128, BF16, O>(maps, a, sms, stream);
+  if (narrow(a.n)) return head_product_launch<MODE, 128, BF16, O>(maps, a, sms, stream);
   return head_product_launch<MODE, 256, BF16, O>(maps, a, sms, stream);
 }
 
@@ -1046,8 +1050,8 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
     if ((rc = head_operand(weight, weight_pitch, vocab, cols, dtype, plan, ws + plan.weight, &words->weight, sms, stream, &w))) return rc;
     const bool bf16 = dtype == SOLON_BF16;
     HeadMaps maps = {};
-    if (!tensor_map(&maps.a, h.p, bf16, cols, rows, h.pieces, h.pitch, rows * h.pitch, plan.few && rows <= 64 ? 32 : kBlock) ||
-        !tensor_map(&maps.b, w.p, bf16, cols, vocab, w.pieces, w.pitch, vocab * w.pitch, kBlock))
+    if (!tensor_map(&maps.a, h.p, bf16, cols, rows, h.pieces, h.pitch, rows * h.pitch, !plan.few ? kRows : rows <= 64 ? 32 : 64) ||
+        !tensor_map(&maps.b, w.p, bf16, cols, vocab, w.pieces, w.pitch, vocab * w.pitch, kRows))
       return SOLON_ERR_CUDA;
     HeadArgs a = {};
     a.m = (int)rows;
@@ -1116,10 +1120,14 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
   if ((rc = head_operand(weight, weight_pitch, vocab, cols, dtype, plan, ws + plan.weight, &words->weight, sms, stream, &w))) return rc;
 
   const int64_t n = rows / partitions, sums_pitch = up(cols, 4);
-  CUtensorMap map_h, map_w, map_h_parts, map_dz, map_dz_parts, map_dz_out;
-  if (!tensor_map(&map_h, h.p, bf16, cols, rows, h.pieces, h.pitch, rows * h.pitch, kBlock) ||
-      !tensor_map(&map_w, w.p, bf16, cols, vocab, w.pieces, w.pitch, vocab * w.pitch, kBlock) ||
-      !tensor_map(&map_h_parts, h.p, bf16, cols, n, (int64_t)h.pieces * partitions, h.pitch, n * h.pitch, kBlock))
+  // as rows along the inner dimension: h and W for the logits, dz for dh; across it: W for dh, dz and h for dW
+  CUtensorMap map_h, map_w, map_w_across, map_h_across, map_dz, map_dz_across, map_dz_out;
+  const bool by_blocks = !narrow(cols) && (cols % kBlock == 0 || plan.split);
+  auto across = [&](CUtensorMap* map, const void* p, int64_t rows, int64_t slabs, int64_t pitch, int64_t slab) {
+    return by_blocks ? tensor_map_by_blocks(map, p, bf16, cols, rows, slabs, pitch, slab) : tensor_map(map, p, bf16, cols, rows, slabs, pitch, slab, kBlock);
+  };
+  if (!tensor_map(&map_h, h.p, bf16, cols, rows, h.pieces, h.pitch, rows * h.pitch, kRows) ||
+      !across(&map_h_across, h.p, n, (int64_t)h.pieces * partitions, h.pitch, n * h.pitch))
     return SOLON_ERR_CUDA;
   HeadArgs base = {};
   base.slabs = 1;
@@ -1131,6 +1139,7 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
   base.grad_logp = grad_logp;
   base.grad_entropy = grad_entropy;
   base.vocab = vocab;
+  base.b_by_blocks = by_blocks;
   const int dz_scaled = bf16 ? 0 : 4;
   auto run = [&](int which, const HeadMaps& maps, const HeadArgs& a) {
     if (f32) return head_backward_piece<false, float>(which, maps, a, grad_dtype, sms, stream);
@@ -1139,12 +1148,13 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
   };
   for (int64_t first = 0; first < vocab; first += plan.width) {
     const int64_t width = std::min(plan.width, vocab - first), pitch = up(width, kBlock);
-    if (!tensor_map(&map_dz, ws + plan.dz, bf16, pitch, rows, plan.dz_pieces, pitch, rows * pitch, kBlock) ||
+    const char* w_piece = w.p + first * w.pitch * 2;
+    if (!tensor_map(&map_dz, ws + plan.dz, bf16, pitch, rows, plan.dz_pieces, pitch, rows * pitch, kRows) ||
         !tensor_map(&map_dz_out, ws + plan.dz, bf16, pitch, rows, plan.dz_pieces, pitch, rows * pitch, 32) ||
-        !tensor_map(&map_dz_parts, ws + plan.dz, bf16, pitch, n, (int64_t)plan.dz_pieces * partitions, pitch, n * pitch, kBlock))
+        !tensor_map_by_blocks(&map_dz_across, ws + plan.dz, bf16, pitch, n, (int64_t)plan.dz_pieces * partitions, pitch, n * pitch) ||
+        !tensor_map(&map_w, w_piece, bf16, cols, width, w.pieces, w.pitch, vocab * w.pitch, kRows) ||
+        !across(&map_w_across, w_piece, width, w.pieces, w.pitch, vocab * w.pitch))
       return SOLON_ERR_CUDA;
-    CUtensorMap map_w_piece;
-    if (!tensor_map(&map_w_piece, w.p + first * w.pitch * 2, bf16, cols, width, w.pieces, w.pitch, vocab * w.pitch, kBlock)) return SOLON_ERR_CUDA;
     HeadArgs a = base;
     a.m = (int)rows;
     a.n = (int)width;
@@ -1153,7 +1163,7 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
     head_pairs(a, h.pieces, w.pieces, 1, 1);
     a.scaled = (f32 ? 3 : 0) | dz_scaled;
     a.pieces = plan.dz_pieces;
-    if ((rc = run(kDz, {map_h, map_w_piece, map_dz_out}, a))) return rc;
+    if ((rc = run(kDz, {map_h, map_w, map_dz_out}, a))) return rc;
     if (dhidden) {
       a = base;
       a.m = (int)rows;
@@ -1168,7 +1178,7 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
       a.out = dhidden;
       a.out_pitch = rows > 1 ? dhidden_pitch : cols;
       a.out_wide = !(((uintptr_t)dhidden | (uintptr_t)(a.out_pitch * element_size(dtype))) & (4 * element_size(dtype) - 1));
-      if ((rc = run(kDhidden, {map_dz, map_w_piece, map_dz}, a))) return rc;
+      if ((rc = run(kDhidden, {map_dz, map_w_across, map_dz}, a))) return rc;
     }
     if (dweight) {
       a = base;
@@ -1184,7 +1194,7 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
       a.out_pitch = cols;
       a.out_slab = partitions > 1 ? grad_pitch : 0;
       a.out_wide = !(((uintptr_t)a.out | (uintptr_t)(cols * grad_size) | (uintptr_t)(a.out_slab * grad_size)) & (std::min<int64_t>(16, 4 * grad_size) - 1));
-      if ((rc = run(kDweight, {map_dz_parts, map_h_parts, map_dz}, a))) return rc;
+      if ((rc = run(kDweight, {map_dz_across, map_h_across, map_dz}, a))) return rc;
     }
   }
   return SOLON_OK;
