@@ -205,7 +205,7 @@ struct HeadShared {
   static constexpr int kBytes = 1024 + kStages * kStageBytes + kEpilogueWarps * kStaging + 512;
 };
 
-// Warp 0 of each CTA brings blocks, warp 1 of the first CTA multiplies, eight warps take finished sums from tensor memory, of which one half is read
+// Warps 0 and 2 of each CTA bring blocks, warp 1 of the first CTA multiplies, eight warps take finished sums from tensor memory, of which one half is read
 // while the other is being filled, and keep a tile's result in registers: 128 columns of a row a thread.
 // The tensor cores cut off what lies below an accumulator's last bit, which costs a sum of n steps of 16 about n / 2 units of 2^-25, always towards 0
 // (measured: 1.6e-8 a step, 2e-5 for dh of 50,001 tokens).  So a result that is wanted in float32 is summed 512 inner indices at a time, and those sums are
@@ -218,7 +218,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
   using Shared = HeadShared<MODE, BN>;
   constexpr int kStages = Shared::kStages, kStageBytes = Shared::kStageBytes;
   constexpr int kHalf = BN / 2;              // columns of an epilogue warp
-  constexpr int kBurst = MODE == kFewRows ? 4 : 1;       // blocks whose rows are asked for together
   extern __shared__ char raw[];
   char* smem = (char*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
   char* staging = smem + kStages * kStageBytes;
@@ -258,55 +257,44 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
 
   if (warp < kFirstEpilogue) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");        // 128 x 72 + 256 x 216 = 64512 = 384 x 168 at launch
-    if (warp == 0 && lane == 0) {
+    if ((warp == 0 || warp == 2) && lane == 0) {       // warp 0 brings A's blocks, warp 2 B's
       int s = 0;
       uint32_t phase = 0;
-      for (uint32_t t = pair; t < tiles_all; t += pairs) {
+      bool fine = true;
+      for (uint32_t t = pair; t < tiles_all && fine; t += pairs) {
         const TileAt at = tile_at(a, t, BN);
         const int row = at.m + rank * kRows, col = at.n + rank * kHalf;
-        for (int p = 0; p < a.products; p++) {
-          const int za = a.piece_a[p] + at.slab * a.slab_a, zb = a.piece_b[p] + at.slab * a.slab_b;
-          for (int kb0 = 0; kb0 < a.k_blocks; kb0 += kBurst) {
-            const int burst = min(kBurst, a.k_blocks - kb0);
-            const int first = s;
-            for (int i = 0; i < burst; i++) {
-              pipe::mbar_wait(empty + s, phase ^ 1, abort_flag, status);
-              if (*(volatile int*)abort_flag) goto loads_done;
+        for (int p = 0; p < a.products && fine; p++) {
+          const int z = warp == 0 ? a.piece_a[p] + at.slab * a.slab_a : a.piece_b[p] + at.slab * a.slab_b;
+          for (int k = 0; k < a.k_blocks * kBlock; k += kBlock) {
+            if (!(fine = waited(empty + s, phase ^ 1, abort_flag, status))) break;
+            const uint32_t dst = pipe::smem_addr(smem + s * kStageBytes);
+            if (warp == 0) {
               if (rank == 0) pipe::mbar_arrive_expect_tx(full + s, 2 * kStageBytes);
-              if (++s == kStages) s = 0, phase ^= 1;
-            }
-            for (int i = 0; i < burst; i++) {
-              const int at_stage = first + i < kStages ? first + i : first + i - kStages, k = (kb0 + i) * kBlock;
-              const uint32_t dst = pipe::smem_addr(smem + at_stage * kStageBytes);
-              if (kAlongA) load_block(dst, &maps.a, k, row, za, full + at_stage);
-              else load_blocks(dst, &maps.a, k, row / kBlock, za, full + at_stage);
-            }
-            for (int i = 0; i < burst; i++) {
-              const int at_stage = first + i < kStages ? first + i : first + i - kStages, k = (kb0 + i) * kBlock;
-              const uint32_t dst = pipe::smem_addr(smem + at_stage * kStageBytes) + kRows * 128;
-              if (kAlongB) load_block(dst, &maps.b, k, col, zb, full + at_stage);
-              else if (kHalf > kBlock && a.b_by_blocks) load_blocks(dst, &maps.b, k, col / kBlock, zb, full + at_stage);
+              if (kAlongA) load_block(dst, &maps.a, k, row, z, full + s);
+              else load_blocks(dst, &maps.a, k, row / kBlock, z, full + s);
+            } else {
+              if (kAlongB) load_block(dst + kRows * 128, &maps.b, k, col, z, full + s);
+              else if (kHalf > kBlock && a.b_by_blocks) load_blocks(dst + kRows * 128, &maps.b, k, col / kBlock, z, full + s);
               else
 #pragma unroll
-                for (int h = 0; h < kHalf; h += kBlock) load_block(dst + h * 128, &maps.b, col + h, k, zb, full + at_stage);
+                for (int h = 0; h < kHalf; h += kBlock) load_block(dst + kRows * 128 + h * 128, &maps.b, col + h, k, z, full + s);
             }
+            if (++s == kStages) s = 0, phase ^= 1;
           }
         }
       }
-    loads_done:;
     } else if (warp == 1 && lane == 0 && rank == 0) {
       constexpr uint32_t idesc = instruction(BF16, kAlongA, kAlongB, BN);
       int s = 0, half = 0;
       uint32_t phase = 0, sum_phase = 0;
       for (uint32_t t = pair; t < tiles_all; t += pairs) {
         for (int kb = 0; kb < blocks;) {
-          pipe::mbar_wait(sum_empty + half, sum_phase ^ 1, abort_flag, status);
-          if (*(volatile int*)abort_flag) goto products_done;
+          if (!waited(sum_empty + half, sum_phase ^ 1, abort_flag, status)) goto products_done;
           fence_after();
           const int first = kb, end = min(blocks, kb + a.chunk);
           for (; kb < end; kb++) {
-            pipe::mbar_wait(full + s, phase, abort_flag, status);
-            if (*(volatile int*)abort_flag) goto products_done;
+            if (!waited(full + s, phase, abort_flag, status)) goto products_done;
             fence_after();
             const uint32_t at = pipe::smem_addr(smem + s * kStageBytes);
             const uint64_t da = operand<kAlongA>(at), db = operand<kAlongB>(at + kRows * 128);

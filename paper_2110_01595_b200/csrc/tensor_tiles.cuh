@@ -52,6 +52,14 @@ __device__ __forceinline__ void commit_to_both(uint64_t* bar) {
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
+// pipe::mbar_wait that says whether the phase completed: false once a wait of this CTA has run out.  (The flag is not looked at where there is nothing to wait
+// for, which is the case that the loops are made for.)
+__device__ __forceinline__ bool waited(uint64_t* bar, uint32_t parity, int* abort_flag, int* status) {
+  if (pipe::mbar_try_wait(bar, parity)) return true;
+  pipe::mbar_wait(bar, parity, abort_flag, status);
+  return !*(volatile int*)abort_flag;
+}
+
 template <int COLUMNS>
 __device__ __forceinline__ void tmem_alloc(uint32_t* where) {          // one warp of each CTA
   asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(pipe::smem_addr(where)), "n"(COLUMNS) : "memory");
