@@ -74,6 +74,10 @@ struct HeadArgs {
   float* target_logit;                   // rows
   // kStats, kDz: columns of the product are tokens first + n
   int64_t first, vocab;
+  // kDz
+  uint16_t* dz;                          // pieces x rows x dz_pitch: this piece's tokens, zeros behind them up to a multiple of 64
+  int64_t dz_piece;
+  int dz_pitch;
   int pieces;                            // of dz
   // kDhidden
   float* sums;                           // rows x sums_pitch: dh of the pieces so far
@@ -82,7 +86,8 @@ struct HeadArgs {
   // kDhidden, kDweight
   void* out;
   int64_t out_pitch, out_slab;           // elements; a slab is a partition
-  int out_wide;                          // rows of the output may be accessed four elements at a time
+  int out_by_map;                        // kDweight: the output's map can be used (16-byte aligned rows)
+  int out_wide;                          // rows of the output begin at multiples of 32 bytes
 };
 
 // ------------------------------------------------------------------------------------------------------------ epilogues
@@ -94,40 +99,50 @@ __device__ __forceinline__ void stage_rows(const float* v, float4* stage, int la
 }
 
 template <typename O>
-__device__ __forceinline__ void store4(O* p, float4 v) {
-  Pack<O, 4> w;
-  if constexpr (sizeof(O) == 8) w = {{(O)v.x, (O)v.y, (O)v.z, (O)v.w}};
-  else w = {{from_float<O>(v.x), from_float<O>(v.y), from_float<O>(v.z), from_float<O>(v.w)}};
-  if constexpr (sizeof(O) == 8) {
-    *reinterpret_cast<double2*>(p) = make_double2(w.e[0], w.e[1]);
-    *reinterpret_cast<double2*>(p + 2) = make_double2(w.e[2], w.e[3]);
-  } else store_pack(p, w);
-}
-template <typename O>
 __device__ __forceinline__ void store1(O* p, float v) {
   if constexpr (sizeof(O) == 8) *p = (double)v;
   else *p = from_float<O>(v);
 }
 
-// Rows [row, row + 32) and columns [col, col + 32) of an output of m x n.
-template <typename O>
-__device__ __forceinline__ void write_rows(const float4* stage, O* out, int64_t pitch, int row, int col, int m, int n, bool wide, int lane) {
-  if (wide && col + 32 <= n) {
-    const int c = lane % 8;
-    O* p = out + (row + lane / 8) * pitch + col + c * 4;
+__device__ __forceinline__ void store32(void* p, const uint32_t (&w)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]),
+               "r"(w[7])
+               : "memory");
+}
+__device__ __forceinline__ void load32(const float* p, float (&v)[8]) {
+  asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+               : "l"(p)
+               : "memory");
+}
+
+// N columns of a lane's row to 32-byte aligned places, 32 bytes an access.  Every lane fills whole sectors of a row of its own; bringing the rows together in
+// shared memory first made wider stretches, but there the tensor cores and the copies that feed them take all there is, and the warps waited.
+template <typename O, int N>
+__device__ __forceinline__ void store_columns(O* p, const float* v) {
+  constexpr int kEach = 32 / sizeof(O);
 #pragma unroll
-    for (int i = 0; i < 8; i++, p += 4 * pitch) {
-      const int r = i * 4 + lane / 8;
-      if (row + r < m) store4(p, stage[r * 8 + (c ^ (r & 7))]);
+  for (int i = 0; i < N; i += kEach) {
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+      if constexpr (sizeof(O) == 4) w[j] = __float_as_uint(v[i + j]);
+      else if constexpr (sizeof(O) == 2) w[j] = Word16<O>::join(v[i + 2 * j], v[i + 2 * j + 1]);
+      else w[j] = j % 2 ? __double2hiint((double)v[i + j / 2]) : __double2loint((double)v[i + j / 2]);
     }
-  } else {
-    const float* s = reinterpret_cast<const float*>(stage) + lane % 4;
-    O* p = out + row * pitch + col + lane;
-    const int rows = col + lane < n ? m - row : 0;
-#pragma unroll 8
-    for (int r = 0; r < 32; r++, p += pitch)
-      if (r < rows) store1(p, s[(r * 8 + ((lane / 4) ^ (r & 7))) * 4]);
+    store32(p + i, w);
   }
+}
+
+// Rows [row, row + 32) and columns [col, col + 32) of an output of m x n at any alignment, a column a lane.
+template <typename O>
+__device__ __forceinline__ void write_rows(const float4* stage, O* out, int64_t pitch, int row, int col, int m, int n, int lane) {
+  const float* s = reinterpret_cast<const float*>(stage) + lane % 4;
+  O* p = out + row * pitch + col + lane;
+  const int rows = col + lane < n ? m - row : 0;
+#pragma unroll 8
+  for (int r = 0; r < 32; r++, p += pitch)
+    if (r < rows) store1(p, s[(r * 8 + ((lane / 4) ^ (r & 7))) * 4]);
 }
 
 struct RowSums {
@@ -200,7 +215,7 @@ __device__ __forceinline__ TileAt tile_at(const HeadArgs& a, uint32_t t, int bn)
 template <int MODE, int BN>
 struct HeadShared {
   static constexpr int kStageBytes = (kRows + BN / 2) * kBlock * 2;
-  static constexpr int kStaging = MODE == kStats ? 0 : MODE == kDz ? 8192 : 4096;        // a warp
+  static constexpr int kStaging = MODE == kStats || MODE == kDz ? 0 : MODE == kDweight ? 8192 : 4096;        // a warp
   static constexpr int kStages = (232448 - 2048 - kEpilogueWarps * kStaging) / kStageBytes > 12 ? 12 : (232448 - 2048 - kEpilogueWarps * kStaging) / kStageBytes;
   static constexpr int kBytes = 1024 + kStages * kStageBytes + kEpilogueWarps * kStaging + 512;
 };
@@ -332,6 +347,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
     for (uint32_t t = pair; t < tiles_all; t += pairs) {
       const TileAt at = tile_at(a, t, BN);
       const int row0 = at.m + rank * kRows + quarter * 32, row = row0 + lane, col = at.n + side * kHalf;
+      [[maybe_unused]] struct {
+        float peak, log_sum, entropy, g, gh;
+        int64_t target;
+      } mine = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, -1};
+      if (MODE == kDz && row < a.m) {        // (on the way while the tile is being multiplied)
+        mine.peak = a.peak[row];
+        mine.log_sum = a.log_sum[row];
+        if (a.targets) mine.target = a.targets[row];
+        if (a.grad_logp) mine.g = a.grad_logp[row];
+        if (a.grad_entropy) {
+          mine.gh = a.grad_entropy[row];
+          mine.entropy = a.entropy[row];
+        }
+      }
+      if (MODE == kStats && row < a.m && a.targets) mine.target = a.targets[row];
       float v[kHalf];
 #pragma unroll
       for (int i = 0; i < kHalf; i++) v[i] = 0.0f;
@@ -371,7 +401,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
             if (i >= inside) v[i] = -INFINITY;
         }
         if (row < a.m) {
-          const int64_t token = a.targets ? a.targets[row] - a.first - col : -1;
+          const int64_t token = mine.target - a.first - col;
           if (token >= 0 && token < kHalf && token < inside) {
             float z = 0.0f;
 #pragma unroll
@@ -415,104 +445,120 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
           rows_so_far[c / 32] = join(rows_so_far[c / 32], sums);
         }
       } else if constexpr (MODE == kDz) {
-        float peak = 0.0f, log_sum = 0.0f, h = 0.0f, g = 0.0f, gh = 0.0f;
-        int64_t token = -1;
-        if (row < a.m) {
-          peak = a.peak[row];
-          log_sum = a.log_sum[row];
-          token = a.targets ? a.targets[row] : -1;
-          if (a.grad_logp && token >= 0) g = a.grad_logp[row];
-          if (a.grad_entropy) {
-            gh = a.grad_entropy[row];
-            h = a.entropy[row];
-          }
-        }
+        const float peak = mine.peak, log_sum = mine.log_sum, h = mine.entropy;
+        float g = mine.target >= 0 ? mine.g : 0.0f, gh = mine.gh;
+        const int64_t from = mine.target - a.first - col;
+        const int token = from >= 0 && from < kHalf ? (int)from : -1;
         const bool active = peak != -INFINITY && (g != 0.0f || gh != 0.0f);
         const float grow = a.scaled & 4 ? power_of_two(scale_exponent(a.words->dz)) : 1.0f;
         g *= grow;
         gh *= grow;
-        token -= a.first + col;
         using Word = Word16<typename std::conditional<BF16, __nv_bfloat16, __half>::type>;
-        const int64_t inside = a.vocab - (a.first + col);
+        const int inside = (int)min((int64_t)kHalf, a.vocab - (a.first + col)), padded = a.dz_pitch - col;
         Float2 mp = pack2(-peak, -peak);
-        const Float2 ml = pack2(-log_sum, -log_sum), l2e = pack2(kLog2e, kLog2e), mg = pack2(-g, -g), mh = pack2(-gh, -gh), h2 = pack2(h, h);
+        const Float2 ml = pack2(-log_sum, -log_sum), ml2 = pack2(-log_sum * kLog2e, -log_sum * kLog2e), l2e = pack2(kLog2e, kLog2e), mg = pack2(-g, -g), mh = pack2(-gh, -gh), h2 = pack2(h, h);
         const uint32_t keep = active ? ~0u : 0u;
+        // (rows beyond the last, and columns beyond the padded piece, are not there; the latter only from 64 columns on)
+        uint16_t* hi_out = a.dz + (int64_t)row * a.dz_pitch + col;
+        uint16_t* lo_out = hi_out + a.dz_piece;
+        const bool here = row < a.m;
+        uint32_t hi[8], lo[8];
 #pragma unroll
-        for (int c = 0; c < kHalf; c += 64) {
-          if (lane == 0) stores_read<0>();   // the blocks that were staged before have been read
-          __syncwarp();
+        for (int first = 0; first < kHalf; first += 8) {
+          float d[8];
+          Float2 last;
 #pragma unroll
-          for (int i = 0; i < 8; i++) {
-            const int first = c + 8 * i;
-            float d[8];
-            Float2 last;
-#pragma unroll
-            for (int j = 0; j < 8; j += 2) {
-              Float2 lp = add2(add2(pack2(v[first + j], v[first + j + 1]), mp), ml);
-              float x, y;
-              if (a.grad_entropy) {          // (p = 0 where log p is -infinity, and no product with it)
-                unpack2(lp, x, y);
-                lp = pack2(x < -1e30f ? -1e30f : x, y < -1e30f ? -1e30f : y);
-              }
-              unpack2(mul2(lp, l2e), x, y);
-              const Float2 e = pack2(exp2_fast(x), exp2_fast(y));
-              last = a.grad_entropy ? mul2(e, fma2(add2(lp, h2), mh, mg)) : mul2(e, mg);
-              unpack2(last, d[j], d[j + 1]);
-            }
-            if (i % 2) in_turn(mp, last);
-            if (token >= first && token < first + 8) {
-#pragma unroll
-              for (int j = 0; j < 8; j++) d[j] += j == (int)token - first ? g : 0.0f;
-            }
-            if (inside < first + 8) {        // (what lies beyond is multiplied by zeros and has to be a number)
-#pragma unroll
-              for (int j = 0; j < 8; j++)
-                if (first + j >= inside) d[j] = 0.0f;
-            }
-            uint32_t hi[4], lo[4];
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-              hi[j] = Word::join(d[2 * j], d[2 * j + 1]) & keep;
-              float hx, hy;
-              Word::pair(hi[j], hx, hy);
-              lo[j] = Word::join(d[2 * j] - hx, d[2 * j + 1] - hy) & keep;
-            }
-            uint4* to = reinterpret_cast<uint4*>(stage) + lane * 8 + (i ^ (lane & 7));
-            to[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-            if (a.pieces == 2) to[4096 / 16] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+          for (int j = 0; j < 8; j += 2) {
+            const Float2 c = add2(pack2(v[first + j], v[first + j + 1]), mp);
+            float x, y;
+            unpack2(fma2(c, l2e, ml2), x, y);
+            last = pack2(exp2_fast(x), exp2_fast(y));
+            if (a.grad_entropy) {            // (p = 0 where log p is -infinity, and no product with it)
+              unpack2(add2(c, ml), x, y);
+              last = mul2(last, fma2(add2(pack2(fmaxf(x, -1e30f), fmaxf(y, -1e30f)), h2), mh, mg));
+            } else last = mul2(last, mg);
+            unpack2(last, d[j], d[j + 1]);
           }
-          fence_async();
-          __syncwarp();
-          if (lane == 0) {
-            for (int p = 0; p < a.pieces; p++) store_block(&maps.out, col + c, row0, p, pipe::smem_addr(stage + p * 4096));
-            stores_commit();
+          if (first % 16) in_turn(mp, last);
+          if (token >= first && token < first + 8) {
+#pragma unroll
+            for (int j = 0; j < 8; j++) d[j] += j == token - first ? g : 0.0f;
+          }
+          if (inside < first + 8) {          // (what lies beyond is multiplied by zeros and has to be a number)
+#pragma unroll
+            for (int j = 0; j < 8; j++)
+              if (first + j >= inside) d[j] = 0.0f;
+          }
+#pragma unroll
+          for (int j = 0; j < 4; j++) {
+            const int to = first % 16 / 2 + j;
+            hi[to] = Word::join(d[2 * j], d[2 * j + 1]) & keep;
+            if (a.pieces == 2) {
+              float hx, hy;
+              Word::pair(hi[to], hx, hy);
+              lo[to] = Word::join(d[2 * j] - hx, d[2 * j + 1] - hy) & keep;
+            }
+          }
+          if (first % 16 && here && first < padded) {
+            store32(hi_out + first - 8, hi);
+            if (a.pieces == 2) store32(lo_out + first - 8, lo);
           }
         }
       } else {
-        float4* rows = reinterpret_cast<float4*>(stage);
+        if constexpr (MODE == kDhidden) {    // (the sums' pitch is a multiple of 128: room for all columns of a warp that has any)
+          float* so_far = a.sums + (int64_t)row * a.sums_pitch + col;
+          const bool here = row < a.m && col < a.n;
+          if (a.load_sums && here) {
 #pragma unroll
-        for (int c = 0; c < kHalf; c += 32) {
-          if (col + c >= a.n || row0 >= a.m) break;
-          __syncwarp();
-          stage_rows(v + c, rows, lane);
-          __syncwarp();
-          if constexpr (MODE == kDhidden) {
-            if (a.load_sums) {
+            for (int c = 0; c < kHalf; c += 32) {
+              float was[4][8];
 #pragma unroll
-              for (int i = 0; i < 8; i++) {
-                const int r = i * 4 + lane / 8, x = lane % 8;
-                if (row0 + r < a.m && col + c + x * 4 < a.sums_pitch) {
-                  const float4 was = *reinterpret_cast<const float4*>(a.sums + (row0 + r) * a.sums_pitch + col + c + x * 4);
-                  float4* at4 = rows + r * 8 + (x ^ (r & 7));
-                  *at4 = make_float4(at4->x + was.x, at4->y + was.y, at4->z + was.z, at4->w + was.w);
-                }
-              }
-              __syncwarp();
+              for (int i = 0; i < 4; i++) load32(so_far + c + 8 * i, was[i]);
+#pragma unroll
+              for (int i = 0; i < 32; i++) v[c + i] += was[i / 8][i % 8];
             }
-            if (a.store_sums) write_rows(rows, a.sums, a.sums_pitch, row0, col + c, a.m, (int)a.sums_pitch, true, lane);
-            else write_rows(rows, (O*)a.out, a.out_pitch, row0, col + c, a.m, a.n, a.out_wide, lane);
-          } else {
-            write_rows(rows, (O*)a.out + at.slab * a.out_slab, a.out_pitch, row0, col + c, a.m, a.n, a.out_wide, lane);
+          }
+          if (a.store_sums && here) store_columns<float, kHalf>(so_far, v);
+        }
+        O* out = (O*)a.out + (MODE == kDweight ? at.slab * a.out_slab : 0);
+        if (MODE == kDhidden && a.store_sums) {
+        } else if (MODE == kDweight && a.out_by_map) {
+          constexpr int kEach = 128 / sizeof(O);       // columns of a block
+#pragma unroll
+          for (int c = 0; c < kHalf; c += kEach) {
+            if (col + c >= a.n || row0 >= a.m) break;
+            uint4* block = reinterpret_cast<uint4*>(stage + (c / kEach % 2) * 4096);
+            if (lane == 0) stores_read<1>();           // the block before the last one has left its place
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+              const float* x = v + c + i * (kEach / 8);
+              uint4 w;
+              if constexpr (sizeof(O) == 4) w = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+              else if constexpr (sizeof(O) == 2)
+                w = make_uint4(Word16<O>::join(x[0], x[1]), Word16<O>::join(x[2], x[3]), Word16<O>::join(x[4], x[5]), Word16<O>::join(x[6], x[7]));
+              else
+                w = make_uint4(__double2loint((double)x[0]), __double2hiint((double)x[0]), __double2loint((double)x[1]), __double2hiint((double)x[1]));
+              block[lane * 8 + (i ^ (lane & 7))] = w;
+            }
+            fence_async();
+            __syncwarp();
+            if (lane == 0) {
+              store_block(&maps.out, col + c, row0, at.slab, pipe::smem_addr(block));
+              stores_commit();
+            }
+          }
+        } else if (a.out_wide && col + kHalf <= a.n) {
+          if (row < a.m) store_columns<O, kHalf>(out + (int64_t)row * a.out_pitch + col, v);
+        } else {
+          float4* rows = reinterpret_cast<float4*>(stage);
+#pragma unroll
+          for (int c = 0; c < kHalf; c += 32) {
+            if (col + c >= a.n || row0 >= a.m) break;
+            __syncwarp();
+            stage_rows(v + c, rows, lane);
+            __syncwarp();
+            write_rows(rows, out, a.out_pitch, row0, col + c, a.m, a.n, lane);
           }
         }
       }
@@ -529,8 +575,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
         }
       }
     }
-    if (MODE == kDz && lane == 0) stores_done();
   }
+  if (MODE == kDweight && warp >= kFirstEpilogue && lane == 0) stores_done();
   if (*(volatile int*)abort_flag) pipe::drain_delay();
   __syncwarp();
   fence_before();
@@ -859,7 +905,7 @@ static HeadPlan head_backward_plan(int64_t rows, int64_t cols, int64_t vocab, in
     p.weight = take(p.pieces * vocab * p.pitch * 2);
   }
   p.dz = take(p.dz_pieces * rows * p.width * 2);
-  if (p.width < vocab) p.sums = take(rows * up(cols, 4) * 4);
+  if (p.width < vocab) p.sums = take(rows * up(cols, 128) * 4);
   p.total = at;
   return p;
 }
@@ -1107,9 +1153,9 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
   if ((rc = head_operand(hidden, hidden_pitch, rows, cols, dtype, plan, ws + plan.hidden, &words->hidden, sms, stream, &h))) return rc;
   if ((rc = head_operand(weight, weight_pitch, vocab, cols, dtype, plan, ws + plan.weight, &words->weight, sms, stream, &w))) return rc;
 
-  const int64_t n = rows / partitions, sums_pitch = up(cols, 4);
+  const int64_t n = rows / partitions, sums_pitch = up(cols, 128);
   // as rows along the inner dimension: h and W for the logits, dz for dh; across it: W for dh, dz and h for dW
-  CUtensorMap map_h, map_w, map_w_across, map_h_across, map_dz, map_dz_across, map_dz_out;
+  CUtensorMap map_h, map_w, map_w_across, map_h_across, map_dz, map_dz_across;
   const bool by_blocks = !narrow(cols) && (cols % kBlock == 0 || plan.split);
   auto across = [&](CUtensorMap* map, const void* p, int64_t rows, int64_t slabs, int64_t pitch, int64_t slab) {
     return by_blocks ? tensor_map_by_blocks(map, p, bf16, cols, rows, slabs, pitch, slab) : tensor_map(map, p, bf16, cols, rows, slabs, pitch, slab, kBlock);
@@ -1138,7 +1184,6 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
     const int64_t width = std::min(plan.width, vocab - first), pitch = up(width, kBlock);
     const char* w_piece = w.p + first * w.pitch * 2;
     if (!tensor_map(&map_dz, ws + plan.dz, bf16, pitch, rows, plan.dz_pieces, pitch, rows * pitch, kRows) ||
-        !tensor_map(&map_dz_out, ws + plan.dz, bf16, pitch, rows, plan.dz_pieces, pitch, rows * pitch, 32) ||
         !tensor_map_by_blocks(&map_dz_across, ws + plan.dz, bf16, pitch, n, (int64_t)plan.dz_pieces * partitions, pitch, n * pitch) ||
         !tensor_map(&map_w, w_piece, bf16, cols, width, w.pieces, w.pitch, vocab * w.pitch, kRows) ||
         !across(&map_w_across, w_piece, width, w.pieces, w.pitch, vocab * w.pitch))
@@ -1151,7 +1196,10 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
     head_pairs(a, h.pieces, w.pieces, 1, 1);
     a.scaled = (f32 ? 3 : 0) | dz_scaled;
     a.pieces = plan.dz_pieces;
-    if ((rc = run(kDz, {map_h, map_w, map_dz_out}, a))) return rc;
+    a.dz = (uint16_t*)(ws + plan.dz);
+    a.dz_pitch = (int)pitch;
+    a.dz_piece = rows * pitch;
+    if ((rc = run(kDz, {map_h, map_w, {}}, a))) return rc;
     if (dhidden) {
       a = base;
       a.m = (int)rows;
@@ -1165,8 +1213,8 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
       a.store_sums = first + width < vocab;
       a.out = dhidden;
       a.out_pitch = rows > 1 ? dhidden_pitch : cols;
-      a.out_wide = !(((uintptr_t)dhidden | (uintptr_t)(a.out_pitch * element_size(dtype))) & (4 * element_size(dtype) - 1));
-      if ((rc = run(kDhidden, {map_dz, map_w_across, map_dz}, a))) return rc;
+      a.out_wide = !(((uintptr_t)dhidden | (uintptr_t)(a.out_pitch * element_size(dtype))) & 31);
+      if ((rc = run(kDhidden, {map_dz, map_w_across, {}}, a))) return rc;
     }
     if (dweight) {
       a = base;
@@ -1181,8 +1229,12 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
       a.out = (char*)dweight + first * cols * grad_size;
       a.out_pitch = cols;
       a.out_slab = partitions > 1 ? grad_pitch : 0;
-      a.out_wide = !(((uintptr_t)a.out | (uintptr_t)(cols * grad_size) | (uintptr_t)(a.out_slab * grad_size)) & (std::min<int64_t>(16, 4 * grad_size) - 1));
-      if ((rc = run(kDweight, {map_dz_across, map_h_across, map_dz}, a))) return rc;
+      a.out_wide = !(((uintptr_t)a.out | (uintptr_t)(cols * grad_size) | (uintptr_t)(a.out_slab * grad_size)) & 31);
+      HeadMaps maps = {map_dz_across, map_h_across, {}};
+      a.out_by_map = !(((uintptr_t)a.out | (uintptr_t)(cols * grad_size) | (uintptr_t)(a.out_slab * grad_size)) & 15);
+      if (a.out_by_map && !output_map(&maps.out, a.out, (int)grad_size, cols, width, partitions, cols, partitions > 1 ? a.out_slab : up(width * cols, 8)))
+        return SOLON_ERR_CUDA;
+      if ((rc = run(kDweight, maps, a))) return rc;
     }
   }
   return SOLON_OK;

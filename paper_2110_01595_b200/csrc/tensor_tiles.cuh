@@ -107,6 +107,7 @@ __device__ __forceinline__ void load_blocks(uint32_t dst, const CUtensorMap* map
       "l"(map), "r"(0), "r"(y), "r"(block), "r"(z), "r"(pipe::smem_addr(bar) & 0xFEFFFFFFu)
       : "memory");
 }
+// A block from this CTA's shared memory to where a map says; what lies outside is not written.
 __device__ __forceinline__ void store_block(const CUtensorMap* map, int x, int y, int z, uint32_t src) {
   asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(x), "r"(y), "r"(z), "r"(src)
                : "memory");
@@ -153,12 +154,24 @@ inline EncodeTiled encode_tiled() {
   return fn;
 }
 
-inline bool encode_map(CUtensorMap* map, const void* p, bool bf16, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
+inline bool encode_map(CUtensorMap* map, const void* p, CUtensorMapDataType type, int rank, const cuuint64_t* dims, const cuuint64_t* strides,
+                       const cuuint32_t* box) {
   const EncodeTiled encode = encode_tiled();
   const cuuint32_t ones[4] = {1, 1, 1, 1};
-  return encode && encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, rank, const_cast<void*>(p), dims, strides, box, ones,
+  return encode && encode(map, type, rank, const_cast<void*>(p), dims, strides, box, ones,
                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+inline CUtensorMapDataType type16(bool bf16) { return bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16; }
+
+// slabs x rows x cols elements of `size` bytes to be written in blocks of 32 rows x 128 bytes.
+inline bool output_map(CUtensorMap* map, const void* p, int size, int64_t cols, int64_t rows, int64_t slabs, int64_t pitch, int64_t slab) {
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)slabs};
+  const cuuint64_t strides[2] = {(cuuint64_t)(pitch * size), (cuuint64_t)(slab * size)};
+  const cuuint32_t box[3] = {(cuuint32_t)(128 / size), 32, 1};
+  return encode_map(map, p, size == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : size == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_FLOAT64, 3, dims,
+                    strides, box);
 }
 
 // slabs x rows x cols elements of 16 bits, row pitch and slab distance in elements (multiples of 8); boxes of box_rows x 64.  What lies outside
@@ -167,7 +180,7 @@ inline bool tensor_map(CUtensorMap* map, const void* p, bool bf16, int64_t cols,
   const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)slabs};
   const cuuint64_t strides[2] = {(cuuint64_t)pitch * 2, (cuuint64_t)slab * 2};
   const cuuint32_t box[3] = {kBlock, (cuuint32_t)box_rows, 1};
-  return encode_map(map, p, bf16, 3, dims, strides, box);
+  return encode_map(map, p, type16(bf16), 3, dims, strides, box);
 }
 
 // The same by blocks of 64 columns, two of 64 rows a box, one behind the other: one copy where there would be two.  All columns of the last block have to be
@@ -176,7 +189,7 @@ inline bool tensor_map_by_blocks(CUtensorMap* map, const void* p, bool bf16, int
   const cuuint64_t dims[4] = {kBlock, (cuuint64_t)rows, (cuuint64_t)(cols + kBlock - 1) / kBlock, (cuuint64_t)slabs};
   const cuuint64_t strides[3] = {(cuuint64_t)pitch * 2, kBlock * 2, (cuuint64_t)slab * 2};
   const cuuint32_t box[4] = {kBlock, kBlock, 2, 1};
-  return encode_map(map, p, bf16, 4, dims, strides, box);
+  return encode_map(map, p, type16(bf16), 4, dims, strides, box);
 }
 
 }  // namespace tiles
