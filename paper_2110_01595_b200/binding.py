@@ -95,7 +95,7 @@ SIGNATURES = {
     "solon_head_logprobs_workspace": (c_int64, [c_int64, c_int64, c_int64, c_int, c_int]),
     "solon_head_logprobs": (c_int, [c_void_p, c_int64, c_void_p, c_int64, c_int, c_void_p, c_int64, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_void_p,
                                     c_void_p, c_int64, c_void_p]),
-    "solon_head_logprobs_backward_workspace": (c_int64, [c_int64, c_int64, c_int64, c_int, c_int, c_int]),
+    "solon_head_logprobs_backward_workspace": (c_int64, [c_int64, c_int64, c_int64, c_int, c_int, c_int, c_int]),
     "solon_head_logprobs_backward": (c_int, [c_void_p, c_int64, c_void_p, c_int64, c_int, c_void_p, c_int64, c_int64, c_int64, c_int, c_void_p, c_void_p,
                                              c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_int, c_void_p, c_int64, c_void_p]),
     "solon_adamw_state_blocks": (c_int64, [c_int, POINTER(c_int64)]),
@@ -492,8 +492,8 @@ def _head_workspace(rows: int, cols: int, vocab: int, code: int, aligned: int) -
 
 
 @functools.lru_cache(maxsize=256)
-def _head_backward_workspace(rows: int, cols: int, vocab: int, code: int, grad_code: int, aligned: int) -> int:
-    return lib().solon_head_logprobs_backward_workspace(rows, cols, vocab, code, grad_code, aligned)
+def _head_backward_workspace(rows: int, cols: int, vocab: int, partitions: int, code: int, grad_code: int, aligned: int) -> int:
+    return lib().solon_head_logprobs_backward_workspace(rows, cols, vocab, partitions, code, grad_code, aligned)
 
 
 def solon_head_logprobs(hidden, weight, targets=None) -> TokenLogprobs:
@@ -546,7 +546,7 @@ def solon_head_logprobs_backward(hidden, weight, targets, peak, log_sum, grad_lo
     def row_vector(t, name):
         return None if t is None else _vector(t, name, rows, torch.float32, device)
 
-    n_bytes = _head_backward_workspace(rows, cols, vocab, code, grad_code, aligned)
+    n_bytes = _head_backward_workspace(rows, cols, vocab, partitions, code, grad_code, aligned)
     if n_bytes < 0:
         raise SolonError(n_bytes, "solon_head_logprobs_backward_workspace")
     workspace = hidden.new_empty(n_bytes, dtype=torch.uint8)

@@ -62,6 +62,7 @@ struct HeadArgs {
   int chunk;                             // blocks of 64 that are summed in tensor memory before the sum is added to the one in registers
   int piece_a[3], piece_b[3];            // third coordinate of the tensor maps for slab 0; slab s is s further
   int slab_a, slab_b;                    // 1: the operand has slabs
+  int splits;                            // the inner dimension is cut into so many parts of k_blocks, slabs of their own; what lies behind its end is zeros
   int b_by_blocks;                       // B's map takes 128 columns a copy, where its rows lie across the inner dimension
   const HeadWords* words;
   HeadWords* flags;
@@ -79,10 +80,10 @@ struct HeadArgs {
   int64_t dz_piece;
   int dz_pitch;
   int pieces;                            // of dz
-  // kDhidden
-  float* sums;                           // rows x sums_pitch: dh of the pieces so far
+  // kDhidden, kDweight
+  float* sums;                           // slabs x m x sums_pitch: where the result goes in float32 instead of to the output, if store_sums
   int64_t sums_pitch;
-  int load_sums, store_sums;
+  int load_sums, store_sums;             // load_sums: the result is added to what is there (kDhidden, the pieces of the vocabulary before)
   // kDhidden, kDweight
   void* out;
   int64_t out_pitch, out_slab;           // elements; a slab is a partition
@@ -280,8 +281,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
         const TileAt at = tile_at(a, t, BN);
         const int row = at.m + rank * kRows, col = at.n + rank * kHalf;
         for (int p = 0; p < a.products && fine; p++) {
-          const int z = warp == 0 ? a.piece_a[p] + at.slab * a.slab_a : a.piece_b[p] + at.slab * a.slab_b;
-          for (int k = 0; k < a.k_blocks * kBlock; k += kBlock) {
+          const int part = a.splits > 1 ? at.slab / a.splits : at.slab, from = (at.slab - part * a.splits) * a.k_blocks * kBlock;
+          const int z = warp == 0 ? a.piece_a[p] + part * a.slab_a : a.piece_b[p] + part * a.slab_b;
+          for (int k = from; k < from + a.k_blocks * kBlock; k += kBlock) {
             if (!(fine = waited(empty + s, phase ^ 1, abort_flag, status))) break;
             const uint32_t dst = pipe::smem_addr(smem + s * kStageBytes);
             if (warp == 0) {
@@ -505,23 +507,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
           }
         }
       } else {
-        if constexpr (MODE == kDhidden) {    // (the sums' pitch is a multiple of 128: room for all columns of a warp that has any)
-          float* so_far = a.sums + (int64_t)row * a.sums_pitch + col;
-          const bool here = row < a.m && col < a.n;
-          if (a.load_sums && here) {
+        // (the sums' pitch is a multiple of 128: room for all columns of a warp that has any)
+        float* so_far = a.sums + ((int64_t)at.slab * a.m + row) * a.sums_pitch + col;
+        const bool here = row < a.m && col < a.n;
+        if (MODE == kDhidden && a.load_sums && here) {
 #pragma unroll
-            for (int c = 0; c < kHalf; c += 32) {
-              float was[4][8];
+          for (int c = 0; c < kHalf; c += 32) {
+            float was[4][8];
 #pragma unroll
-              for (int i = 0; i < 4; i++) load32(so_far + c + 8 * i, was[i]);
+            for (int i = 0; i < 4; i++) load32(so_far + c + 8 * i, was[i]);
 #pragma unroll
-              for (int i = 0; i < 32; i++) v[c + i] += was[i / 8][i % 8];
-            }
+            for (int i = 0; i < 32; i++) v[c + i] += was[i / 8][i % 8];
           }
-          if (a.store_sums && here) store_columns<float, kHalf>(so_far, v);
         }
         O* out = (O*)a.out + (MODE == kDweight ? at.slab * a.out_slab : 0);
-        if (MODE == kDhidden && a.store_sums) {
+        if (a.store_sums) {
+          if (here) store_columns<float, kHalf>(so_far, v);
         } else if (MODE == kDweight && a.out_by_map) {
           constexpr int kEach = 128 / sizeof(O);       // columns of a block
 #pragma unroll
@@ -821,6 +822,30 @@ __global__ void __launch_bounds__(256) head_split_kernel(const T* x, int64_t pit
   }
 }
 
+// Adds up the parts of a product whose inner dimension was cut: parts x splits x m x pitch float32 to parts x m x n elements.
+struct HeadFinishArgs {
+  const float* sums;
+  int64_t pitch, m, n, out_pitch, out_slab;
+  int parts, splits;
+  void* out;
+};
+template <typename O>
+__global__ void __launch_bounds__(256) head_finish_kernel(HeadFinishArgs a) {
+  const int64_t words = (a.n + 3) / 4;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.parts * a.m * words; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / words, c = (i - r * words) * 4, part = r / a.m, row = r - part * a.m;
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+    for (int s = 0; s < a.splits; s++) {
+      const float4 x = __ldcg(reinterpret_cast<const float4*>(a.sums + ((part * a.splits + s) * a.m + row) * a.pitch + c));
+      sum = make_float4(sum.x + x.x, sum.y + x.y, sum.z + x.z, sum.w + x.w);
+    }
+    O* p = (O*)a.out + part * a.out_slab + row * a.out_pitch + c;
+    const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+    for (int e = 0; e < 4 && c + e < a.n; e++) store1(p + e, v[e]);
+  }
+}
+
 // ------------------------------------------------------------------------------------------------------------ host
 
 static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
@@ -837,7 +862,8 @@ struct HeadPlan {
   int64_t pitch;                         // of theirs
   int dz_pieces;
   int64_t width;                         // tokens of a piece of the vocabulary
-  int64_t words, partial, target_logit, hidden, weight, dz, sums, total;
+  int h_splits, w_splits;                // parts of the inner dimensions of dh and dW
+  int64_t words, partial, target_logit, hidden, weight, dz, sums, w_sums, total;
 };
 
 constexpr int64_t kHeadSharedRows = 200 * 1024;       // bytes of hidden rows that the kernel for few rows holds
@@ -886,13 +912,36 @@ static HeadPlan head_forward_plan(int64_t rows, int64_t cols, int64_t vocab, int
 
 constexpr int64_t kDzBytes = 256ll << 20;
 
-static HeadPlan head_backward_plan(int64_t rows, int64_t cols, int64_t vocab, int dtype, int grad_dtype, bool aligned) {
+// 256 columns a tile, or 128 where that covers the columns with a sixth less.
+static bool narrow(int64_t cols) { return up(cols, 128) * 6 <= up(cols, 256) * 5; }
+
+// Into how many parts the inner dimension of a product of `slabs` times m x n is cut, where it has too few tiles for the 74 pairs of CTAs or a last round that
+// is mostly empty.  A block of 64 indices takes a tile 0.28 us (half of that with 128 columns), a tile 1.5 us besides; parts are written and read once
+// more at 5 TB/s by a launch of their own of 4 us.  dh of 2880 x 333 over 2003 tokens: 39 us in one part, 24 in two.
+static int head_splits(int64_t slabs, int64_t m, int64_t n, int64_t k, int products, int times) {
+  const int64_t kb = (k + kBlock - 1) / kBlock;
+  const int64_t tiles = slabs * ((m + kTile - 1) / kTile) * (up(n, narrow(n) ? 128 : kTile) / (narrow(n) ? 128 : kTile));
+  const double block = (narrow(n) ? 0.15 : 0.28) * products, bytes = (double)slabs * m * up(n, 128) * 4;
+  int best = 1;
+  double least = 0.0;
+  for (int s = 1; s <= 16 && (s == 1 || kb / s >= 4); s++) {
+    const int64_t rounds = (tiles * s + 73) / 74;
+    const double cost = times * rounds * ((kb + s - 1) / s * block + 1.5) + (s > 1 ? 4.0 + s * bytes * 2 * times / 5e6 : bytes * 2 * (times - 1) / 5e6);
+    if (s == 1 || cost < 0.95 * least) best = s, least = cost;
+  }
+  return best;
+}
+
+static HeadPlan head_backward_plan(int64_t rows, int64_t cols, int64_t vocab, int partitions, int dtype, int grad_dtype, bool aligned) {
   HeadPlan p = {};
   p.pieces = dtype == SOLON_F32 ? 2 : 1;
   p.split = dtype == SOLON_F32 || !aligned;
   p.pitch = up(cols, kBlock);
   p.dz_pieces = dtype == SOLON_F32 || grad_dtype != SOLON_BF16 ? 2 : 1;
   p.width = std::min(up(vocab, 64), std::max<int64_t>(kTile, kDzBytes / (rows * 2 * p.dz_pieces) / kTile * kTile));
+  const int times = (int)((vocab + p.width - 1) / p.width);
+  p.h_splits = head_splits(1, rows, cols, std::min(vocab, p.width), dtype == SOLON_F32 ? 3 : 1, times);
+  p.w_splits = head_splits(partitions, std::min(vocab, p.width), cols, rows / partitions, grad_dtype == SOLON_BF16 ? 1 : p.pieces + 1, 1);
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
     const int64_t here = at;
@@ -905,7 +954,8 @@ static HeadPlan head_backward_plan(int64_t rows, int64_t cols, int64_t vocab, in
     p.weight = take(p.pieces * vocab * p.pitch * 2);
   }
   p.dz = take(p.dz_pieces * rows * p.width * 2);
-  if (p.width < vocab) p.sums = take(rows * up(cols, 128) * 4);
+  if (times > 1 || p.h_splits > 1) p.sums = take(p.h_splits * rows * up(cols, 128) * 4);
+  if (p.w_splits > 1) p.w_sums = take((int64_t)p.w_splits * partitions * std::min(vocab, p.width) * up(cols, 128) * 4);
   p.total = at;
   return p;
 }
@@ -963,9 +1013,6 @@ static int head_product_launch(const HeadMaps& maps, HeadArgs a, int sms, cudaSt
   return SOLON_OK;
 }
 
-// 256 columns a tile, or 128 where that covers the columns with a sixth less.
-static bool narrow(int64_t cols) { return up(cols, 128) * 6 <= up(cols, 256) * 5; }
-
 template <int MODE, bool BF16, typename O>
 static int head_product(const HeadMaps& maps, const HeadArgs& a, int sms, cudaStream_t stream) {
   if (narrow(a.n)) return head_product_launch<MODE, 128, BF16, O>(maps, a, sms, stream);
@@ -1013,6 +1060,16 @@ static void head_pairs(HeadArgs& a, int pieces_a, int pieces_b, int step_a, int 
   if (pieces_b == 2) pair(0, 1);
   if (pieces_a == 2) pair(1, 0);
   pair(0, 0);
+}
+
+static int head_finish(const HeadFinishArgs& a, int dtype, int sms, cudaStream_t stream) {
+  const unsigned blocks = (unsigned)std::min<int64_t>((a.parts * a.m * ((a.n + 3) / 4) + 255) / 256, 16 * sms);
+  if (dtype == SOLON_F32) head_finish_kernel<float><<<blocks, 256, 0, stream>>>(a);
+  else if (dtype == SOLON_F64) head_finish_kernel<double><<<blocks, 256, 0, stream>>>(a);
+  else if (dtype == SOLON_BF16) head_finish_kernel<__nv_bfloat16><<<blocks, 256, 0, stream>>>(a);
+  else head_finish_kernel<__half><<<blocks, 256, 0, stream>>>(a);
+  SOLON_CUDA_TRY(cudaGetLastError());
+  return SOLON_OK;
 }
 
 static bool head_sizes_ok(int64_t rows, int64_t cols, int64_t vocab) {
@@ -1090,7 +1147,7 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
     HeadArgs a = {};
     a.m = (int)rows;
     a.n = (int)vocab;
-    a.slabs = 1;
+    a.slabs = a.splits = 1;
     a.k_blocks = (int)((cols + kBlock - 1) / kBlock);
     head_pairs(a, h.pieces, w.pieces, 1, 1);
     a.words = a.flags = words;
@@ -1110,10 +1167,10 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
   return launch_dependent(head_join_kernel<32>, dim3((unsigned)((rows + 31) / 32)), dim3(256), 0, stream, j);
 }
 
-int64_t solon_head_logprobs_backward_workspace(int64_t rows, int64_t cols, int64_t vocab, int dtype, int grad_dtype, int aligned) {
-  if (!token_dtype(dtype) || !head_sizes_ok(rows, cols, vocab)) return SOLON_ERR_INVALID_ARG;
+int64_t solon_head_logprobs_backward_workspace(int64_t rows, int64_t cols, int64_t vocab, int partitions, int dtype, int grad_dtype, int aligned) {
+  if (!token_dtype(dtype) || !head_sizes_ok(rows, cols, vocab) || partitions < 1 || partitions > SOLON_MAX_NODES || rows % partitions) return SOLON_ERR_INVALID_ARG;
   if (grad_dtype != SOLON_F32 && grad_dtype != SOLON_F64 && grad_dtype != SOLON_BF16) return SOLON_ERR_INVALID_ARG;
-  return rows == 0 ? 0 : head_backward_plan(rows, cols, vocab, dtype, grad_dtype, aligned != 0).total;
+  return rows == 0 ? 0 : head_backward_plan(rows, cols, vocab, partitions, dtype, grad_dtype, aligned != 0).total;
 }
 
 int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const void* weight, int64_t weight_pitch, int dtype, const int64_t* targets,
@@ -1138,7 +1195,7 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
     return SOLON_ERR_INVALID_ARG;
   if (!dhidden && !dweight) return SOLON_OK;
   const bool aligned = aligned16(hidden, hidden_pitch, rows, dtype) && aligned16(weight, weight_pitch, vocab, dtype);
-  const HeadPlan plan = head_backward_plan(rows, cols, vocab, dtype, grad_dtype, aligned);
+  const HeadPlan plan = head_backward_plan(rows, cols, vocab, partitions, dtype, grad_dtype, aligned);
   if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < plan.total) return SOLON_ERR_INVALID_ARG;
   int sms = 0, rc;
   if ((rc = current_sms(&sms))) return rc;
@@ -1164,7 +1221,7 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
       !across(&map_h_across, h.p, n, (int64_t)h.pieces * partitions, h.pitch, n * h.pitch))
     return SOLON_ERR_CUDA;
   HeadArgs base = {};
-  base.slabs = 1;
+  base.slabs = base.splits = 1;
   base.words = base.flags = words;
   base.targets = targets;
   base.peak = peak;
@@ -1204,25 +1261,34 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
       a = base;
       a.m = (int)rows;
       a.n = (int)cols;
-      a.k_blocks = (int)(pitch / kBlock);
+      a.slabs = a.splits = plan.h_splits;
+      a.k_blocks = (int)((pitch / kBlock + a.splits - 1) / a.splits);
       head_pairs(a, f32 ? 2 : 1, w.pieces, 1, 1);
       a.scaled = (f32 ? 2 : 0) | dz_scaled;
       a.sums = (float*)(ws + plan.sums);
       a.sums_pitch = sums_pitch;
       a.load_sums = first > 0;
-      a.store_sums = first + width < vocab;
+      const bool last = first + width == vocab;
+      a.store_sums = !last || a.splits > 1;
       a.out = dhidden;
       a.out_pitch = rows > 1 ? dhidden_pitch : cols;
       a.out_wide = !(((uintptr_t)dhidden | (uintptr_t)(a.out_pitch * element_size(dtype))) & 31);
       if ((rc = run(kDhidden, {map_dz, map_w_across, {}}, a))) return rc;
+      if (last && a.splits > 1 &&
+          (rc = head_finish({a.sums, sums_pitch, rows, cols, a.out_pitch, 0, 1, a.splits, dhidden}, dtype, sms, stream)))
+        return rc;
     }
     if (dweight) {
       a = base;
       a.m = (int)width;
       a.n = (int)cols;
-      a.slabs = partitions;
+      a.splits = plan.w_splits;
+      a.slabs = partitions * a.splits;
       a.slab_a = a.slab_b = 1;
-      a.k_blocks = (int)((n + kBlock - 1) / kBlock);
+      a.k_blocks = (int)(((n + kBlock - 1) / kBlock + a.splits - 1) / a.splits);
+      a.sums = (float*)(ws + plan.w_sums);
+      a.sums_pitch = sums_pitch;
+      a.store_sums = a.splits > 1;
       const bool coarse = grad_dtype == SOLON_BF16;
       head_pairs(a, coarse ? 1 : 2, coarse ? 1 : h.pieces, partitions, partitions);
       a.scaled = (f32 ? 1 : 0) | dz_scaled;
@@ -1235,6 +1301,7 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
       if (a.out_by_map && !output_map(&maps.out, a.out, (int)grad_size, cols, width, partitions, cols, partitions > 1 ? a.out_slab : up(width * cols, 8)))
         return SOLON_ERR_CUDA;
       if ((rc = run(kDweight, maps, a))) return rc;
+      if (a.splits > 1 && (rc = head_finish({a.sums, sums_pitch, width, cols, cols, a.out_slab, partitions, a.splits, a.out}, grad_dtype, sms, stream))) return rc;
     }
   }
   return SOLON_OK;

@@ -62,8 +62,8 @@ def test_head_refusals(lib):
     assert f(at, 8, at, 8, 0, at, 4, 8, 10, at, at, at, at, at, w(4, 8, 10, 0, 1) - 1, None) == BAD
     assert f(None, 8, None, 8, 0, None, 0, 8, 10, None, None, None, None, None, 0, None) == 0
     v = lib.solon_head_logprobs_backward_workspace
-    assert v(0, 8, 10, 0, 0, 1) == 0 and v(4, 8, 10, 0, 3, 1) == BAD and v(4, 8, 10, 1, 0, 1) == BAD
-    assert v(100_000, 64, 50_000, 2, 0, 1) < (1 << 28) + 100_000 * 64 * 4 + 4096                # dlogits comes in pieces
+    assert v(0, 8, 10, 1, 0, 0, 1) == 0 and v(4, 8, 10, 1, 0, 3, 1) == BAD and v(4, 8, 10, 1, 1, 0, 1) == BAD and v(4, 8, 10, 3, 0, 0, 1) == BAD
+    assert v(100_000, 64, 50_000, 1, 2, 0, 1) < (1 << 28) + 100_000 * 128 * 4 + 4096                # dlogits comes in pieces
     b = lib.solon_head_logprobs_backward
 
     def call(h=at, hp=8, m=at, mp=8, dtype=0, t=at, rows=4, cols=8, vocab=10, parts=2, peak=at, ls=at, ent=None, g=at, gh=None, dh=at, dhp=8, dw=at, dwp=80, gt=0, ws=at, n=big):
@@ -72,5 +72,5 @@ def test_head_refusals(lib):
     assert call(dtype=1) == BAD and call(hp=7) == BAD and call(mp=7) == BAD and call(h=None) == BAD and call(m=at + 1) == BAD
     assert call(parts=3) == BAD and call(parts=0) == BAD and call(peak=None) == BAD and call(ls=None) == BAD and call(t=None) == BAD
     assert call(gh=at) == BAD and call(dhp=7) == BAD and call(dwp=79) == BAD and call(gt=3) == BAD and call(ws=None) == BAD and call(ws=at + 128) == BAD
-    assert call(n=v(4, 8, 10, 0, 0, 1) - 1) == BAD and call(cols=1 << 23) == BAD
+    assert call(n=v(4, 8, 10, 2, 0, 0, 1) - 1) == BAD and call(cols=1 << 23) == BAD
     assert call(dh=None, dw=None) == 0                                                          # nothing wanted
