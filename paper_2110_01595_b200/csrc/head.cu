@@ -58,11 +58,13 @@ struct alignas(64) HeadMaps {
 struct HeadArgs {
   // the product: slabs times m x n, in blocks of 64 inner indices, `products` pairs of pieces
   int m, n, m_tiles, n_tiles, slabs;
+  uint32_t per_slab_inverse, band_inverse;             // reciprocals for the tiles' numbers
   int k_blocks, products;
   int chunk;                             // blocks of 64 that are summed in tensor memory before the sum is added to the one in registers
   int piece_a[3], piece_b[3];            // third coordinate of the tensor maps for slab 0; slab s is s further
   int slab_a, slab_b;                    // 1: the operand has slabs
   int splits;                            // the inner dimension is cut into so many parts of k_blocks, slabs of their own; what lies behind its end is zeros
+  int narrow;                            // tiles of 128 columns
   int b_by_blocks;                       // B's map takes 128 columns a copy, where its rows lie across the inner dimension
   const HeadWords* words;
   HeadWords* flags;
@@ -76,9 +78,7 @@ struct HeadArgs {
   // kStats, kDz: columns of the product are tokens first + n
   int64_t first, vocab;
   // kDz
-  uint16_t* dz;                          // pieces x rows x dz_pitch: this piece's tokens, zeros behind them up to a multiple of 64
-  int64_t dz_piece;
-  int dz_pitch;
+  int dz_pitch;                          // this piece's tokens, zeros behind them up to a multiple of 64
   int pieces;                            // of dz
   // kDhidden, kDweight
   float* sums;                           // slabs x m x sums_pitch: where the result goes in float32 instead of to the output, if store_sums
@@ -173,17 +173,17 @@ __device__ __forceinline__ void take_if(float& z, float x, bool yes) {
 template <int COLUMNS>
 __device__ __forceinline__ void row_sums(const float (&v)[COLUMNS], RowSums& sums) {
   float &m = sums.m, &s = sums.s, &a = sums.a;
-  m = v[0];
+  float big[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-  for (int i = 1; i + 1 < COLUMNS; i += 2) asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(v[i]), "f"(v[i + 1]));
-  m = max_nan(m, v[COLUMNS - 1]);
+  for (int i = 4; i < COLUMNS; i += 2) asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(big[i / 2 % 4]) : "f"(v[i]), "f"(v[i + 1]));
+  m = max_nan(max_nan(big[0], big[1]), max_nan(big[2], big[3]));
   const float ref = m == -INFINITY ? 0.0f : m;
   Float2 minus = pack2(-ref, -ref);
   const Float2 l2e = pack2(kLog2e, kLog2e);
   Float2 s2[2] = {pack2(0.0f, 0.0f), pack2(0.0f, 0.0f)}, a2[2] = {s2[0], s2[0]};
 #pragma unroll
   for (int i = 0; i < COLUMNS; i += 2) {
-    if (i % 16 == 0) in_turn(minus, a2[1]);
+    if (i % 32 == 0) in_turn(minus, s2[1]);
     const Float2 c = add2(pack2(v[i], v[i + 1]), minus);
     float x, y, cx, cy;
     unpack2(mul2(c, l2e), x, y);
@@ -199,16 +199,100 @@ __device__ __forceinline__ void row_sums(const float (&v)[COLUMNS], RowSums& sum
   a = x + y;
 }
 
+struct DzRow {
+  float peak, log_sum, entropy, g, gh;
+};
+
+template <typename T>
+struct DzOut {
+  const CUtensorMap* map;
+  char* stage;                           // two blocks of 32 rows x 128 bytes
+  int col, row, columns, lane;           // first column and row of the warp, columns that there are
+  int place;                             // of the row's target (-1: not here) and its element
+  float target;
+};
+
+// -p (g + g_H (log p + H)) of N tokens of a row, from their logits: a piece of 16 bits and, with TWO, what that leaves, in blocks of 64 tokens that are
+// copied from shared memory (rows of their own are 32-byte writes, which go out at a third of the rate).  `keep` 0: zeros.
+// The forms are functions of their own so that no branch stands between the elements: with branches an element's chain of operations has nothing beside it.
+template <bool ENTROPY, bool TWO, int N, typename T>
+__device__ __forceinline__ void dz_row(const DzRow& r, const float (&v)[N], uint32_t keep, const DzOut<T>& out) {
+  using Word = Word16<T>;
+  Float2 mp = pack2(-r.peak, -r.peak);
+  const Float2 ml = pack2(-r.log_sum, -r.log_sum), ml2 = pack2(-r.log_sum * kLog2e, -r.log_sum * kLog2e), l2e = pack2(kLog2e, kLog2e);
+  const Float2 mg = pack2(-r.g, -r.g), mh = pack2(-r.gh, -r.gh), h2 = pack2(r.entropy, r.entropy);
+#pragma unroll
+  for (int c = 0; c < N; c += 64) {
+    if (c >= out.columns) break;
+    char* block[2];
+#pragma unroll
+    for (int p = 0; p < 2; p++) block[p] = out.stage + (TWO ? p : c / 64 % 2) * 4096;
+    if (out.lane == 0) {                     // the blocks that were here before have left
+      if (TWO) stores_read<0>();
+      else stores_read<1>();
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      uint32_t hi[4], lo[4];
+      Float2 d;
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        const int at = c + 8 * i + 2 * j;
+        const Float2 x2 = add2(pack2(v[at], v[at + 1]), mp);
+        float x, y;
+        unpack2(fma2(x2, l2e, ml2), x, y);
+        d = pack2(exp2_fast(x), exp2_fast(y));
+        if (ENTROPY) {                       // (p = 0 where log p is -infinity, and no product with it)
+          unpack2(add2(x2, ml), x, y);
+          d = mul2(d, fma2(add2(pack2(fmaxf(x, -1e30f), fmaxf(y, -1e30f)), h2), mh, mg));
+        } else d = mul2(d, mg);
+        unpack2(d, x, y);
+        hi[j] = Word::join(x, y) & keep;
+        if (TWO) {
+          float hx, hy;
+          Word::pair(hi[j], hx, hy);
+          lo[j] = Word::join(x - hx, y - hy) & keep;
+        }
+      }
+      if (i % 2) in_turn(mp, d);
+      const int to = out.lane * 8 + (i ^ (out.lane & 7));
+      reinterpret_cast<uint4*>(block[0])[to] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+      if (TWO) reinterpret_cast<uint4*>(block[1])[to] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
+    if (out.place >= c && out.place < c + 64) {
+      const int in = out.place - c, to = (out.lane * 8 + ((in / 8) ^ (out.lane & 7))) * 8 + in % 8;
+      const T first = from_float<T>(out.target);
+      reinterpret_cast<T*>(block[0])[to] = first;
+      if (TWO) reinterpret_cast<T*>(block[1])[to] = from_float<T>(out.target - to_float(first));
+    }
+    fence_async();
+    __syncwarp();
+    if (out.lane == 0) {
+      store_block(out.map, out.col + c, out.row, 0, pipe::smem_addr(block[0]));
+      if (TWO) store_block(out.map, out.col + c, out.row, 1, pipe::smem_addr(block[1]));
+      stores_commit();
+    }
+  }
+}
+
 // ------------------------------------------------------------------------------------------------------------ product
 
 struct TileAt {
   int slab, m, n;                        // first row and column
 };
+// t / d with the reciprocal min(2^32 - 1, 2^32 / d + 1) at hand: off by one at most before the correction, and a fifth of a division's instructions.
+__device__ __forceinline__ uint32_t quotient(uint32_t t, uint32_t d, uint32_t inverse) {
+  uint32_t q = __umulhi(t, inverse);
+  const int r = (int)(t - q * d);
+  return r < 0 ? q - 1 : r >= (int)d ? q + 1 : q;
+}
 // Tiles of eight row tiles at a time, columns of those before the next eight: what runs at the same time shares rows of both operands in L2.
 __device__ __forceinline__ TileAt tile_at(const HeadArgs& a, uint32_t t, int bn) {
-  const uint32_t per_slab = (uint32_t)a.m_tiles * a.n_tiles, slab = t / per_slab, r = t - slab * per_slab;
-  const uint32_t band = 8u * a.n_tiles, group = r / band, in = r - group * band;
-  const uint32_t high = min(8u, a.m_tiles - group * 8), column = in / high;
+  const uint32_t per_slab = (uint32_t)a.m_tiles * a.n_tiles, band = 8u * a.n_tiles;
+  const uint32_t slab = quotient(t, per_slab, a.per_slab_inverse), r = t - slab * per_slab;
+  const uint32_t group = quotient(r, band, a.band_inverse), in = r - group * band;
+  const uint32_t high = min(8u, a.m_tiles - group * 8), column = high == 8 ? in >> 3 : in / high;
   return {(int)slab, (int)((group * 8 + in - column * high) * kTile), (int)column * bn};
 }
 
@@ -216,7 +300,8 @@ __device__ __forceinline__ TileAt tile_at(const HeadArgs& a, uint32_t t, int bn)
 template <int MODE, int BN>
 struct HeadShared {
   static constexpr int kStageBytes = (kRows + BN / 2) * kBlock * 2;
-  static constexpr int kStaging = MODE == kStats || MODE == kDz ? 0 : MODE == kDweight ? 8192 : 4096;        // a warp
+  static constexpr int kBlocks = MODE == kStats ? 0 : MODE == kDz || MODE == kDweight ? 8192 : 4096;     // a warp's blocks of the result
+  static constexpr int kStaging = kBlocks + (MODE == kStats || MODE == kDz ? 1024 : 0);                   // and what the tile's rows come with
   static constexpr int kStages = (232448 - 2048 - kEpilogueWarps * kStaging) / kStageBytes > 12 ? 12 : (232448 - 2048 - kEpilogueWarps * kStaging) / kStageBytes;
   static constexpr int kBytes = 1024 + kStages * kStageBytes + kEpilogueWarps * kStaging + 512;
 };
@@ -292,7 +377,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
               else load_blocks(dst, &maps.a, k, row / kBlock, z, full + s);
             } else {
               if (kAlongB) load_block(dst + kRows * 128, &maps.b, k, col, z, full + s);
-              else if (kHalf > kBlock && a.b_by_blocks) load_blocks(dst + kRows * 128, &maps.b, k, col / kBlock, z, full + s);
+              else if (a.b_by_blocks) load_blocks(dst + kRows * 128, &maps.b, k, col / kBlock, z, full + s);
               else
 #pragma unroll
                 for (int h = 0; h < kHalf; h += kBlock) load_block(dst + kRows * 128 + h * 128, &maps.b, col + h, k, z, full + s);
@@ -349,21 +434,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
     for (uint32_t t = pair; t < tiles_all; t += pairs) {
       const TileAt at = tile_at(a, t, BN);
       const int row0 = at.m + rank * kRows + quarter * 32, row = row0 + lane, col = at.n + side * kHalf;
-      [[maybe_unused]] struct {
-        float peak, log_sum, entropy, g, gh;
-        int64_t target;
-      } mine = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, -1};
-      if (MODE == kDz && row < a.m) {        // (on the way while the tile is being multiplied)
-        mine.peak = a.peak[row];
-        mine.log_sum = a.log_sum[row];
-        if (a.targets) mine.target = a.targets[row];
-        if (a.grad_logp) mine.g = a.grad_logp[row];
-        if (a.grad_entropy) {
-          mine.gh = a.grad_entropy[row];
-          mine.entropy = a.entropy[row];
+      // what the tile's rows come with is on the way to shared memory while the tile is being multiplied
+      [[maybe_unused]] float* of_rows = reinterpret_cast<float*>(stage + Shared::kBlocks);
+      [[maybe_unused]] int64_t* of_targets = reinterpret_cast<int64_t*>(of_rows + 5 * 32);
+      if constexpr (MODE == kStats || MODE == kDz) {
+        __syncwarp();
+        const bool there = row < a.m;
+        const int64_t at_row = there ? row : 0;
+        if (a.targets) copy_async<8>(of_targets + lane, a.targets + at_row, there);
+        if constexpr (MODE == kDz) {
+          copy_async<4>(of_rows + lane, a.peak + at_row, there);
+          copy_async<4>(of_rows + 32 + lane, a.log_sum + at_row, there);
+          if (a.grad_logp) copy_async<4>(of_rows + 64 + lane, a.grad_logp + at_row, there);
+          if (a.grad_entropy) {
+            copy_async<4>(of_rows + 96 + lane, a.entropy + at_row, there);
+            copy_async<4>(of_rows + 128 + lane, a.grad_entropy + at_row, there);
+          }
         }
+        copies_commit();
       }
-      if (MODE == kStats && row < a.m && a.targets) mine.target = a.targets[row];
       float v[kHalf];
 #pragma unroll
       for (int i = 0; i < kHalf; i++) v[i] = 0.0f;
@@ -403,7 +492,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
             if (i >= inside) v[i] = -INFINITY;
         }
         if (row < a.m) {
-          const int64_t token = mine.target - a.first - col;
+          copies_wait<0>();
+          const int64_t token = a.targets ? of_targets[lane] - a.first - col : -1;
           if (token >= 0 && token < kHalf && token < inside) {
             float z = 0.0f;
 #pragma unroll
@@ -447,64 +537,41 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
           rows_so_far[c / 32] = join(rows_so_far[c / 32], sums);
         }
       } else if constexpr (MODE == kDz) {
-        const float peak = mine.peak, log_sum = mine.log_sum, h = mine.entropy;
-        float g = mine.target >= 0 ? mine.g : 0.0f, gh = mine.gh;
-        const int64_t from = mine.target - a.first - col;
-        const int token = from >= 0 && from < kHalf ? (int)from : -1;
-        const bool active = peak != -INFINITY && (g != 0.0f || gh != 0.0f);
+        using T16 = typename std::conditional<BF16, __nv_bfloat16, __half>::type;
         const float grow = a.scaled & 4 ? power_of_two(scale_exponent(a.words->dz)) : 1.0f;
-        g *= grow;
-        gh *= grow;
-        using Word = Word16<typename std::conditional<BF16, __nv_bfloat16, __half>::type>;
-        const int inside = (int)min((int64_t)kHalf, a.vocab - (a.first + col)), padded = a.dz_pitch - col;
-        Float2 mp = pack2(-peak, -peak);
-        const Float2 ml = pack2(-log_sum, -log_sum), ml2 = pack2(-log_sum * kLog2e, -log_sum * kLog2e), l2e = pack2(kLog2e, kLog2e), mg = pack2(-g, -g), mh = pack2(-gh, -gh), h2 = pack2(h, h);
+        copies_wait<0>();
+        const int64_t target = a.targets && row < a.m ? of_targets[lane] : -1;
+        DzRow r = {of_rows[lane], of_rows[32 + lane], a.grad_entropy ? of_rows[96 + lane] : 0.0f, a.grad_logp && target >= 0 ? of_rows[64 + lane] : 0.0f,
+                   a.grad_entropy ? of_rows[128 + lane] : 0.0f};
+        const bool active = r.peak != -INFINITY && (r.g != 0.0f || r.gh != 0.0f);
+        r.g *= grow;
+        r.gh *= grow;
         const uint32_t keep = active ? ~0u : 0u;
-        // (rows beyond the last, and columns beyond the padded piece, are not there; the latter only from 64 columns on)
-        uint16_t* hi_out = a.dz + (int64_t)row * a.dz_pitch + col;
-        uint16_t* lo_out = hi_out + a.dz_piece;
-        const bool here = row < a.m;
-        uint32_t hi[8], lo[8];
+        const int64_t token = target - a.first - col, inside = a.vocab - (a.first + col);
+        if (inside < kHalf) {                // (what lies beyond is multiplied by zeros and has to be a number: p = 0)
 #pragma unroll
-        for (int first = 0; first < kHalf; first += 8) {
-          float d[8];
-          Float2 last;
+          for (int i = 0; i < kHalf; i++)
+            if (i >= inside) v[i] = -INFINITY;
+        }
+        const bool hit = target >= 0 && token >= 0 && token < min((int64_t)kHalf, inside);
+        float z = 0.0f;
+        if (__any_sync(~0u, hit)) {
 #pragma unroll
-          for (int j = 0; j < 8; j += 2) {
-            const Float2 c = add2(pack2(v[first + j], v[first + j + 1]), mp);
-            float x, y;
-            unpack2(fma2(c, l2e, ml2), x, y);
-            last = pack2(exp2_fast(x), exp2_fast(y));
-            if (a.grad_entropy) {            // (p = 0 where log p is -infinity, and no product with it)
-              unpack2(add2(c, ml), x, y);
-              last = mul2(last, fma2(add2(pack2(fmaxf(x, -1e30f), fmaxf(y, -1e30f)), h2), mh, mg));
-            } else last = mul2(last, mg);
-            unpack2(last, d[j], d[j + 1]);
-          }
-          if (first % 16) in_turn(mp, last);
-          if (token >= first && token < first + 8) {
-#pragma unroll
-            for (int j = 0; j < 8; j++) d[j] += j == token - first ? g : 0.0f;
-          }
-          if (inside < first + 8) {          // (what lies beyond is multiplied by zeros and has to be a number)
-#pragma unroll
-            for (int j = 0; j < 8; j++)
-              if (first + j >= inside) d[j] = 0.0f;
-          }
-#pragma unroll
-          for (int j = 0; j < 4; j++) {
-            const int to = first % 16 / 2 + j;
-            hi[to] = Word::join(d[2 * j], d[2 * j + 1]) & keep;
-            if (a.pieces == 2) {
-              float hx, hy;
-              Word::pair(hi[to], hx, hy);
-              lo[to] = Word::join(d[2 * j] - hx, d[2 * j + 1] - hy) & keep;
-            }
-          }
-          if (first % 16 && here && first < padded) {
-            store32(hi_out + first - 8, hi);
-            if (a.pieces == 2) store32(lo_out + first - 8, lo);
-          }
+          for (int i = 0; i < kHalf; i++) take_if(z, v[i], (int)token == i);
+        }
+        float lp = 0.0f, d = 0.0f;
+        if (hit) {                           // the target's element, with its g
+          lp = (z - r.peak) - r.log_sum;
+          d = active ? fmaf(exp2_fast(lp * kLog2e), fmaf(-r.gh, lp + r.entropy, -r.g), r.g) : 0.0f;
+        }
+        const int place = hit ? (int)token : -1;
+        const DzOut<T16> out = {&maps.out, stage, col, row0, a.dz_pitch - col, lane, place, d};
+        if (a.grad_entropy) {
+          if (a.pieces == 2) dz_row<true, true, kHalf>(r, v, keep, out);
+          else dz_row<true, false, kHalf>(r, v, keep, out);
+        } else {
+          if (a.pieces == 2) dz_row<false, true, kHalf>(r, v, keep, out);
+          else dz_row<false, false, kHalf>(r, v, keep, out);
         }
       } else {
         // (the sums' pitch is a multiple of 128: room for all columns of a warp that has any)
@@ -577,7 +644,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
       }
     }
   }
-  if (MODE == kDweight && warp >= kFirstEpilogue && lane == 0) stores_done();
+  if ((MODE == kDz || MODE == kDweight) && warp >= kFirstEpilogue && lane == 0) stores_done();
   if (*(volatile int*)abort_flag) pipe::drain_delay();
   __syncwarp();
   fence_before();
@@ -912,16 +979,18 @@ static HeadPlan head_forward_plan(int64_t rows, int64_t cols, int64_t vocab, int
 
 constexpr int64_t kDzBytes = 256ll << 20;
 
-// 256 columns a tile, or 128 where that covers the columns with a sixth less.
-static bool narrow(int64_t cols) { return up(cols, 128) * 6 <= up(cols, 256) * 5; }
+// 128 columns a tile instead of 256: where there are no more, and where that covers them with a sixth less and little is multiplied (`blocks` of 64 inner
+// indices), so that writing the result is what takes time.  The tensor cores take a tile of 128 no less time than one of 256.  (Gradient of 32768 x 2048
+// over 8192 rows 1374 against 716 us, of 2003 x 333 over 45 x 64 rows 54 against 73.)
+static bool narrow(int64_t cols, int64_t blocks) { return cols <= 128 || (blocks <= 8 && up(cols, 128) * 6 <= up(cols, 256) * 5); }
 
 // Into how many parts the inner dimension of a product of `slabs` times m x n is cut, where it has too few tiles for the 74 pairs of CTAs or a last round that
-// is mostly empty.  A block of 64 indices takes a tile 0.28 us (half of that with 128 columns), a tile 1.5 us besides; parts are written and read once
-// more at 5 TB/s by a launch of their own of 4 us.  dh of 2880 x 333 over 2003 tokens: 39 us in one part, 24 in two.
+// is mostly empty.  A block of 64 indices takes a tile 0.3 us, a tile 1.5 us besides; parts are written and read once
+// more at 5 TB/s by a launch of their own of 4 us.
 static int head_splits(int64_t slabs, int64_t m, int64_t n, int64_t k, int products, int times) {
   const int64_t kb = (k + kBlock - 1) / kBlock;
-  const int64_t tiles = slabs * ((m + kTile - 1) / kTile) * (up(n, narrow(n) ? 128 : kTile) / (narrow(n) ? 128 : kTile));
-  const double block = (narrow(n) ? 0.15 : 0.28) * products, bytes = (double)slabs * m * up(n, 128) * 4;
+  const int64_t bn = narrow(n, kb * products) ? 128 : kTile, tiles = slabs * ((m + kTile - 1) / kTile) * (up(n, bn) / bn);
+  const double block = 0.3 * products, bytes = (double)slabs * m * up(n, 128) * 4;
   int best = 1;
   double least = 0.0;
   for (int s = 1; s <= 16 && (s == 1 || kb / s >= 4); s++) {
@@ -1005,7 +1074,10 @@ static int head_product_launch(const HeadMaps& maps, HeadArgs a, int sms, cudaSt
   a.n_tiles = (a.n + BN - 1) / BN;
   a.chunk = (MODE == kDhidden || MODE == kDweight) && sizeof(O) == 2 ? 64 : 8;
   const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles * a.slabs;
-  if (tiles > 0x7FFF0000) return SOLON_ERR_INVALID_ARG;
+  if (tiles > 0x3FFFFFFF) return SOLON_ERR_INVALID_ARG;
+  auto inverse = [](int64_t d) { return (uint32_t)std::min<int64_t>(0xFFFFFFFF, (1ll << 32) / d + 1); };
+  a.per_slab_inverse = inverse((int64_t)a.m_tiles * a.n_tiles);
+  a.band_inverse = inverse(8ll * a.n_tiles);
   const int pairs = (int)std::min<int64_t>(tiles, MODE == kFewRows ? std::min(kFewPairs, sms / 2) : sms / 2);
   SOLON_SHARED_MEMORY_ONCE(kernel, bytes);
   kernel<<<2 * pairs, kThreads, bytes, stream>>>(maps, a);
@@ -1015,7 +1087,7 @@ static int head_product_launch(const HeadMaps& maps, HeadArgs a, int sms, cudaSt
 
 template <int MODE, bool BF16, typename O>
 static int head_product(const HeadMaps& maps, const HeadArgs& a, int sms, cudaStream_t stream) {
-  if (narrow(a.n)) return head_product_launch<MODE, 128, BF16, O>(maps, a, sms, stream);
+  if (a.narrow) return head_product_launch<MODE, 128, BF16, O>(maps, a, sms, stream);
   return head_product_launch<MODE, 256, BF16, O>(maps, a, sms, stream);
 }
 
@@ -1212,13 +1284,16 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
 
   const int64_t n = rows / partitions, sums_pitch = up(cols, 128);
   // as rows along the inner dimension: h and W for the logits, dz for dh; across it: W for dh, dz and h for dW
-  CUtensorMap map_h, map_w, map_w_across, map_h_across, map_dz, map_dz_across;
-  const bool by_blocks = !narrow(cols) && (cols % kBlock == 0 || plan.split);
-  auto across = [&](CUtensorMap* map, const void* p, int64_t rows, int64_t slabs, int64_t pitch, int64_t slab) {
-    return by_blocks ? tensor_map_by_blocks(map, p, bf16, cols, rows, slabs, pitch, slab) : tensor_map(map, p, bf16, cols, rows, slabs, pitch, slab, kBlock);
+  CUtensorMap map_h, map_w, map_w_across, map_h_across, map_dz, map_dz_across, map_dz_out;
+  // (a map across the inner dimension goes with the tiles: copies of 128 columns need 128 of them in a CTA's tile, and whole blocks of 64 in memory)
+  const bool whole = cols % kBlock == 0 || plan.split;
+  auto across = [&](CUtensorMap* map, const void* p, int64_t rows, int64_t slabs, int64_t pitch, int64_t slab, bool narrow) {
+    return whole && !narrow ? tensor_map_by_blocks(map, p, bf16, cols, rows, slabs, pitch, slab) : tensor_map(map, p, bf16, cols, rows, slabs, pitch, slab, kBlock);
   };
+  const bool coarse = grad_dtype == SOLON_BF16;
+  const bool w_narrow = narrow(cols, (n + kBlock - 1) / kBlock * (coarse ? 1 : h.pieces + 1));
   if (!tensor_map(&map_h, h.p, bf16, cols, rows, h.pieces, h.pitch, rows * h.pitch, kRows) ||
-      !across(&map_h_across, h.p, n, (int64_t)h.pieces * partitions, h.pitch, n * h.pitch))
+      !across(&map_h_across, h.p, n, (int64_t)h.pieces * partitions, h.pitch, n * h.pitch, w_narrow))
     return SOLON_ERR_CUDA;
   HeadArgs base = {};
   base.slabs = base.splits = 1;
@@ -1230,7 +1305,6 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
   base.grad_logp = grad_logp;
   base.grad_entropy = grad_entropy;
   base.vocab = vocab;
-  base.b_by_blocks = by_blocks;
   const int dz_scaled = bf16 ? 0 : 4;
   auto run = [&](int which, const HeadMaps& maps, const HeadArgs& a) {
     if (f32) return head_backward_piece<false, float>(which, maps, a, grad_dtype, sms, stream);
@@ -1240,10 +1314,12 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
   for (int64_t first = 0; first < vocab; first += plan.width) {
     const int64_t width = std::min(plan.width, vocab - first), pitch = up(width, kBlock);
     const char* w_piece = w.p + first * w.pitch * 2;
+    const bool h_narrow = narrow(cols, pitch / kBlock * (f32 ? 3 : 1));
     if (!tensor_map(&map_dz, ws + plan.dz, bf16, pitch, rows, plan.dz_pieces, pitch, rows * pitch, kRows) ||
+        !tensor_map(&map_dz_out, ws + plan.dz, bf16, pitch, rows, plan.dz_pieces, pitch, rows * pitch, 32) ||
         !tensor_map_by_blocks(&map_dz_across, ws + plan.dz, bf16, pitch, n, (int64_t)plan.dz_pieces * partitions, pitch, n * pitch) ||
         !tensor_map(&map_w, w_piece, bf16, cols, width, w.pieces, w.pitch, vocab * w.pitch, kRows) ||
-        !across(&map_w_across, w_piece, width, w.pieces, w.pitch, vocab * w.pitch))
+        !across(&map_w_across, w_piece, width, w.pieces, w.pitch, vocab * w.pitch, h_narrow))
       return SOLON_ERR_CUDA;
     HeadArgs a = base;
     a.m = (int)rows;
@@ -1253,15 +1329,15 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
     head_pairs(a, h.pieces, w.pieces, 1, 1);
     a.scaled = (f32 ? 3 : 0) | dz_scaled;
     a.pieces = plan.dz_pieces;
-    a.dz = (uint16_t*)(ws + plan.dz);
     a.dz_pitch = (int)pitch;
-    a.dz_piece = rows * pitch;
-    if ((rc = run(kDz, {map_h, map_w, {}}, a))) return rc;
+    if ((rc = run(kDz, {map_h, map_w, map_dz_out}, a))) return rc;
     if (dhidden) {
       a = base;
       a.m = (int)rows;
       a.n = (int)cols;
       a.slabs = a.splits = plan.h_splits;
+      a.narrow = h_narrow;
+      a.b_by_blocks = whole && !h_narrow;
       a.k_blocks = (int)((pitch / kBlock + a.splits - 1) / a.splits);
       head_pairs(a, f32 ? 2 : 1, w.pieces, 1, 1);
       a.scaled = (f32 ? 2 : 0) | dz_scaled;
@@ -1285,11 +1361,12 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
       a.splits = plan.w_splits;
       a.slabs = partitions * a.splits;
       a.slab_a = a.slab_b = 1;
+      a.narrow = w_narrow;
+      a.b_by_blocks = whole && !w_narrow;
       a.k_blocks = (int)(((n + kBlock - 1) / kBlock + a.splits - 1) / a.splits);
       a.sums = (float*)(ws + plan.w_sums);
       a.sums_pitch = sums_pitch;
       a.store_sums = a.splits > 1;
-      const bool coarse = grad_dtype == SOLON_BF16;
       head_pairs(a, coarse ? 1 : 2, coarse ? 1 : h.pieces, partitions, partitions);
       a.scaled = (f32 ? 1 : 0) | dz_scaled;
       a.out = (char*)dweight + first * cols * grad_size;
