@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsolon.so")
 SOURCES = ["plan.cu", "encode.cu", "project.cu", "locate.cu", "recover.cu", "decode.cu", "lsq.cu",
-           "layernorm.cu", "logprobs.cu", "adamw.cu", "embedding.cu", "head.cu"]
+           "layernorm.cu", "logprobs.cu", "adamw.cu", "embedding.cu", "head.cu", "head_rows.cu"]
 
 
 def _nvcc() -> str:

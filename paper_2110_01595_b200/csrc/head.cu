@@ -20,6 +20,8 @@
 #include <cmath>
 
 #include "elements.cuh"
+#include "head_rows.h"
+#include "head_sums.cuh"
 #include "solon_internal.h"
 #include "tensor_tiles.cuh"
 #include "token_args.h"
@@ -28,7 +30,6 @@ namespace solon {
 
 using namespace tiles;
 
-constexpr float kLog2e = 1.44269504088896f;
 constexpr int kTile = 256;               // vocabulary tokens, or rows, of a pair's tile
 constexpr int kEpilogueWarps = 8;
 constexpr int kFirstEpilogue = 4;        // the warps before it bring blocks and multiply, and give registers to the others
@@ -144,59 +145,6 @@ __device__ __forceinline__ void write_rows(const float4* stage, O* out, int64_t 
 #pragma unroll 8
   for (int r = 0; r < 32; r++, p += pitch)
     if (r < rows) store1(p, s[(r * 8 + ((lane / 4) ^ (r & 7))) * 4]);
-}
-
-struct RowSums {
-  float m, s, a;
-};
-
-// Joins two sets of logits: sums against the larger of the two largest logits.
-__device__ __forceinline__ RowSums join(const RowSums& x, const RowSums& y) {
-  RowSums r;
-  r.m = max_nan(x.m, y.m);
-  const float cx = x.m == -INFINITY ? 0.0f : x.m - r.m, cy = y.m == -INFINITY ? 0.0f : y.m - r.m;    // (no logits, or none above -infinity: s = a = 0)
-  const float ex = exp2f(cx * kLog2e), ey = exp2f(cy * kLog2e);
-  r.s = x.s * ex + y.s * ey;
-  r.a = fmaf(x.s, cx, x.a) * ex + fmaf(y.s, cy, y.a) * ey;
-  return r;
-}
-
-// Says that x is used after y is known: without it the compiler starts so many elements of a row at once that registers do not hold them.
-__device__ __forceinline__ void in_turn(Float2& x, const Float2& y) { asm volatile("" : "+l"(x.v) : "l"(y.v)); }
-
-// z = x if `yes`, in a form that no compiler turns into an indexed access: the row would have to lie in memory.
-__device__ __forceinline__ void take_if(float& z, float x, bool yes) {
-  asm("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %2, 0;\n\t@p mov.f32 %0, %1;\n\t}" : "+f"(z) : "f"(x), "r"((int)yes));
-}
-
-// Sums of one row's part of a tile: its largest logit, S and A against it.
-template <int COLUMNS>
-__device__ __forceinline__ void row_sums(const float (&v)[COLUMNS], RowSums& sums) {
-  float &m = sums.m, &s = sums.s, &a = sums.a;
-  float big[4] = {v[0], v[1], v[2], v[3]};
-#pragma unroll
-  for (int i = 4; i < COLUMNS; i += 2) asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(big[i / 2 % 4]) : "f"(v[i]), "f"(v[i + 1]));
-  m = max_nan(max_nan(big[0], big[1]), max_nan(big[2], big[3]));
-  const float ref = m == -INFINITY ? 0.0f : m;
-  Float2 minus = pack2(-ref, -ref);
-  const Float2 l2e = pack2(kLog2e, kLog2e);
-  Float2 s2[2] = {pack2(0.0f, 0.0f), pack2(0.0f, 0.0f)}, a2[2] = {s2[0], s2[0]};
-#pragma unroll
-  for (int i = 0; i < COLUMNS; i += 2) {
-    if (i % 32 == 0) in_turn(minus, s2[1]);
-    const Float2 c = add2(pack2(v[i], v[i + 1]), minus);
-    float x, y, cx, cy;
-    unpack2(mul2(c, l2e), x, y);
-    unpack2(c, cx, cy);
-    const Float2 e = pack2(exp2_fast(x), exp2_fast(y));
-    s2[i / 2 % 2] = add2(s2[i / 2 % 2], e);
-    a2[i / 2 % 2] = fma2(e, pack2(fmaxf(cx, -1e30f), fmaxf(cy, -1e30f)), a2[i / 2 % 2]);      // (0 times -infinity is not wanted; NaN is in s)
-  }
-  float x, y;
-  unpack2(add2(s2[0], s2[1]), x, y);
-  s = x + y;
-  unpack2(add2(a2[0], a2[1]), x, y);
-  a = x + y;
 }
 
 struct DzRow {
@@ -823,22 +771,29 @@ __global__ void __launch_bounds__(256) head_scan_kernel(HeadScanArgs a) {
   } else {
     const float* m = blockIdx.y ? a.weight : a.hidden;
     if (!m) return;
-    const int64_t rows = blockIdx.y ? a.vocab : a.rows, pitch = blockIdx.y ? a.weight_pitch : a.hidden_pitch;
+    int64_t rows = blockIdx.y ? a.vocab : a.rows, pitch = blockIdx.y ? a.weight_pitch : a.hidden_pitch, cols = a.cols;
     word = blockIdx.y ? &a.words->weight : &a.words->hidden;
+    if (pitch == cols && !((uintptr_t)m & 15)) {       // one stretch: cut into rows of 2048 whatever its own are, and a last one
+      const int64_t all = rows * cols;
+      if (blockIdx.x == 0)
+        for (int64_t c = all / 2048 * 2048 + threadIdx.x; c < all; c += 256) see(m[c]);
+      rows = all / 2048;
+      cols = pitch = 2048;
+    }
     const bool wide = !(((uintptr_t)m | (uintptr_t)(pitch * 4)) & 15);
     for (int64_t r = (int64_t)blockIdx.x * 8 + warp; r < rows; r += (int64_t)gridDim.x * 8) {
       const float* p = m + r * pitch;
       int64_t done = 0;
       if (wide) {
 #pragma unroll 4
-        for (int64_t c = lane; c < a.cols / 4; c += 32) {
+        for (int64_t c = lane; c < cols / 4; c += 32) {
           const float4 x = *reinterpret_cast<const float4*>(p + 4 * c);
           see(x.x), see(x.y), see(x.z), see(x.w);
         }
-        done = a.cols / 4 * 4;
+        done = cols / 4 * 4;
       }
 #pragma unroll 4
-      for (int64_t c = done + lane; c < a.cols; c += 32) see(p[c]);
+      for (int64_t c = done + lane; c < cols; c += 32) see(p[c]);
     }
   }
   big = __reduce_max_sync(~0u, big);
@@ -922,6 +877,8 @@ struct HeadPlan {
   // few rows
   int row_kernel;                        // 0, or the number of rows that the kernel of multiply-adds is built for
   bool few;                              // the product is taken the other way round
+  int small;                             // float32: 0, or the number of rows that the kernels of head_rows.cu are built for
+  int64_t turned;
   int64_t slots;
   // products
   int pieces;                            // of hidden and weight
@@ -943,12 +900,13 @@ static int64_t rows_padded(int64_t cols) { return up(cols, 256); }
 
 static HeadPlan head_forward_plan(int64_t rows, int64_t cols, int64_t vocab, int dtype, bool aligned) {
   HeadPlan p = {};
-  // W has to be read once and is all there is to read.  Up to 16 rows the multiply-adds cost less than splitting or copying W first would.
-  if (rows <= 16 && (dtype == SOLON_F32 || !aligned)) {
-    int nr = 1;
-    while (nr < rows) nr *= 2;
+  // W has to be read once and is all there is to read.  Up to 4 rows multiply-adds keep up with that, at any type and alignment; up to 32 float32 rows they cost
+  // less than bringing W into two pieces first (65536 x 2048: 16 rows 446 us in pieces).
+  if (rows <= 4 && (dtype == SOLON_F32 || !aligned)) {
+    const int nr = rows == 3 ? 4 : (int)rows;
     if (nr * rows_padded(cols) * 4 <= kHeadSharedRows) p.row_kernel = nr;
   }
+  if (!p.row_kernel && dtype == SOLON_F32 && rows <= kSmallForward) p.small = small_rows(rows);
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
     const int64_t here = at;
@@ -959,6 +917,9 @@ static HeadPlan head_forward_plan(int64_t rows, int64_t cols, int64_t vocab, int
   p.target_logit = take(rows * 4);
   if (p.row_kernel) {
     p.slots = kRowBlocks;
+  } else if (p.small) {
+    p.slots = (vocab + small_tile() - 1) / small_tile();
+    p.turned = take(up(cols, 32) * p.small * 4);
   } else {
     // Up to 128 rows are the columns of tiles, not their rows: half the products of a tile that is mostly empty.
     p.few = rows <= kFewMost;
@@ -1008,15 +969,24 @@ static HeadPlan head_backward_plan(int64_t rows, int64_t cols, int64_t vocab, in
   p.pitch = up(cols, kBlock);
   p.dz_pieces = dtype == SOLON_F32 || grad_dtype != SOLON_BF16 ? 2 : 1;
   p.width = std::min(up(vocab, 64), std::max<int64_t>(kTile, kDzBytes / (rows * 2 * p.dz_pieces) / kTile * kTile));
-  const int times = (int)((vocab + p.width - 1) / p.width);
-  p.h_splits = head_splits(1, rows, cols, std::min(vocab, p.width), dtype == SOLON_F32 ? 3 : 1, times);
-  p.w_splits = head_splits(partitions, std::min(vocab, p.width), cols, rows / partitions, grad_dtype == SOLON_BF16 ? 1 : p.pieces + 1, 1);
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
     const int64_t here = at;
     at += up(bytes, 256);
     return here;
   };
+  if (dtype == SOLON_F32 && rows <= kSmallBackward) {      // (13 rows of 3456 over 37760 tokens: 755 us in pieces)
+    p.small = small_rows(rows);
+    p.h_splits = small_splits(cols, vocab);
+    p.turned = take(up(cols, 32) * p.small * 4);
+    p.dz = take((vocab + 64) * p.small * 4);
+    p.sums = take(p.h_splits * rows * up(cols, 128) * 4);
+    p.total = at;
+    return p;
+  }
+  const int times = (int)((vocab + p.width - 1) / p.width);
+  p.h_splits = head_splits(1, rows, cols, std::min(vocab, p.width), dtype == SOLON_F32 ? 3 : 1, times);
+  p.w_splits = head_splits(partitions, std::min(vocab, p.width), cols, rows / partitions, grad_dtype == SOLON_BF16 ? 1 : p.pieces + 1, 1);
   p.words = take(sizeof(HeadWords));
   if (p.split) {
     p.hidden = take(p.pieces * rows * p.pitch * 2);
@@ -1047,9 +1017,7 @@ static int head_rows_e(const HeadRowsArgs& a, int nr, cudaStream_t stream) {
   switch (nr) {
     case 1: return head_rows_launch<T, 1, sizeof(T) == 4 ? 8 : 4, EACH, G>(a, stream);
     case 2: return head_rows_launch<T, 2, 4, EACH, G>(a, stream);
-    case 4: return head_rows_launch<T, 4, 4, EACH, G>(a, stream);
-    case 8: return head_rows_launch<T, 8, 4, EACH, G>(a, stream);
-    default: return head_rows_launch<T, 16, 2, EACH, G>(a, stream);
+    default: return head_rows_launch<T, 4, 4, EACH, G>(a, stream);
   }
 }
 
@@ -1202,6 +1170,20 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
     else if (dtype == SOLON_BF16) rc = head_rows_t<__nv_bfloat16>(a, plan.row_kernel, stream);
     else rc = head_rows_t<__half>(a, plan.row_kernel, stream);
     if (rc) return rc;
+  } else if (plan.small) {
+    HeadSmallArgs a = {};
+    a.hidden = (const float*)hidden;
+    a.weight = (const float*)weight;
+    a.hidden_pitch = hidden_pitch;
+    a.weight_pitch = vocab > 1 ? weight_pitch : cols;
+    a.cols = cols;
+    a.vocab = vocab;
+    a.rows = (int)rows;
+    a.targets = targets;
+    a.turned = (float*)(ws + plan.turned);
+    a.partial = (float*)(ws + plan.partial);
+    a.target_logit = (float*)(ws + plan.target_logit);
+    if ((rc = small_forward(a, stream))) return rc;
   } else {
     if (dtype == SOLON_F32) {
       SOLON_CUDA_TRY(cudaMemsetAsync(words, 0, sizeof(HeadWords), stream));
@@ -1235,7 +1217,9 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
     if ((rc = head_stats(maps, a, plan.few, bf16, sms, stream))) return rc;
   }
   const HeadJoinArgs j = {(const float*)(ws + plan.partial), (const float*)(ws + plan.target_logit), rows, slots, vocab, targets, logp, entropy, peak, log_sum};
-  if (rows < 2048) return launch_dependent(head_join_kernel<1>, dim3((unsigned)rows), dim3(256), 0, stream, j);
+  // (eight neighbouring rows are a sector of each slot)
+  if (rows <= 256) return launch_dependent(head_join_kernel<1>, dim3((unsigned)rows), dim3(256), 0, stream, j);
+  if (rows <= 4096) return launch_dependent(head_join_kernel<8>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, stream, j);
   return launch_dependent(head_join_kernel<32>, dim3((unsigned)((rows + 31) / 32)), dim3(256), 0, stream, j);
 }
 
@@ -1274,6 +1258,32 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
   char* ws = (char*)workspace;
   HeadWords* words = (HeadWords*)(ws + plan.words);
   const bool f32 = dtype == SOLON_F32, bf16 = dtype == SOLON_BF16;
+  if (plan.small) {
+    HeadSmallArgs a = {};
+    a.hidden = (const float*)hidden;
+    a.weight = (const float*)weight;
+    a.hidden_pitch = hidden_pitch;
+    a.weight_pitch = vocab > 1 ? weight_pitch : cols;
+    a.cols = cols;
+    a.vocab = vocab;
+    a.rows = (int)rows;
+    a.partitions = partitions;
+    a.targets = targets;
+    a.turned = (float*)(ws + plan.turned);
+    a.peak = peak;
+    a.log_sum = log_sum;
+    a.entropy = entropy;
+    a.grad_logp = grad_logp;
+    a.grad_entropy = grad_entropy;
+    a.dz = (float*)(ws + plan.dz);
+    a.sums = dhidden ? (float*)(ws + plan.sums) : nullptr;
+    a.sums_pitch = up(cols, 128);
+    a.dweight = dweight;
+    a.grad_pitch = partitions > 1 ? grad_pitch : up(vocab * cols, 8);
+    a.grad_dtype = grad_dtype;
+    if ((rc = small_backward(a, stream)) || !dhidden) return rc;
+    return head_finish({a.sums, a.sums_pitch, rows, cols, rows > 1 ? dhidden_pitch : cols, 0, 1, plan.h_splits, dhidden}, dtype, sms, stream);
+  }
   if (!bf16) SOLON_CUDA_TRY(cudaMemsetAsync(words, 0, sizeof(HeadWords), stream));
   const HeadScanArgs scan = {f32 ? (const float*)hidden : nullptr, f32 ? (const float*)weight : nullptr, hidden_pitch, weight_pitch, rows, cols, vocab,
                              grad_logp, grad_entropy, entropy, !bf16, words};
