@@ -404,9 +404,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
       float v[kHalf];
 #pragma unroll
       for (int i = 0; i < kHalf; i++) v[i] = 0.0f;
+      const bool absent = row0 >= a.m || (MODE != kStats && col >= (MODE == kDz ? a.dz_pitch : a.n));     // nothing of the tile is this warp's
       for (int kb = 0; kb < blocks; kb += a.chunk) {
         pipe::mbar_wait(sum_full + half, sum_phase, abort_flag, status);
         fence_after();
+        if (!absent) {
         const uint32_t from = tmem + half * BN + side * kHalf + lanes;
 #pragma unroll
         for (int c = 0; c < kHalf; c += 32) {
@@ -419,11 +421,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
             unpack2(sum, v[c + i], v[c + i + 1]);
           }
         }
+        }
         fence_before();
         __syncwarp();
         if (lane == 0) arrive_at_first(sum_empty + half);
         if ((half ^= 1) == 0) sum_phase ^= 1;
       }
+      if (absent) continue;
       if (a.scaled) {
 #pragma unroll
         for (int i = 0; i < kHalf; i++) v[i] = v[i] * undo[0] * undo[1];

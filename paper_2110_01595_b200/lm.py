@@ -7,7 +7,8 @@ overwrites some nodes' rows -> robust decode (solon_decode) -> AdamW on all para
 (solon_adamw_step), skipped on the device if the decode failed.
 
 The model is the smallest that has every part: an embedding, one layer norm, one output matrix.  Products of matrices are plain
-library ones, written straight into the gradient matrix.
+library ones, written straight into the gradient matrix; with fused_head the logits are never in memory (solon_head_logprobs and its
+gradient, which goes straight into the gradient matrix too).
 """
 
 from __future__ import annotations
@@ -28,13 +29,15 @@ def parameter_count(vocab: int, width: int) -> int:
 class TokenLoop:
     """State of one run: parameters (views of one vector, in the order of the gradient), optimizer, buffers.
 
-    bits: width of AdamW's state.  max_norm: clip of the mean gradient's norm (0: none)."""
+    bits: width of AdamW's state.  max_norm: clip of the mean gradient's norm (0: none).  fused_head: loss and gradient straight
+    from hidden states and output matrix."""
 
     def __init__(self, plan: binding.Plan, vocab: int, width: int, seed: int = 0, bits: int = 32, lr: float = 1e-2, weight_decay: float = 0.0,
-                 max_norm: float = 1.0, attack: str = "flip10"):
+                 max_norm: float = 1.0, attack: str = "flip10", fused_head: bool = False):
         if plan.d != parameter_count(vocab, width) or plan.dtype != "f32":
             raise ValueError(f"the plan must be float32 with d = {parameter_count(vocab, width)}")
         self.plan, self.vocab, self.width, self.lr, self.max_norm, self.attack = plan, vocab, width, float(lr), float(max_norm), attack
+        self.fused_head = fused_head
         plan.set_fresh_projections(True)
         g = torch.Generator(device="cuda").manual_seed(seed)
         self.flat = torch.zeros(plan.d, device="cuda")
@@ -53,8 +56,7 @@ class TokenLoop:
 
     def _forward(self, tokens):
         hidden = binding.solon_embedding_forward(self.embed, tokens)
-        normed, mean, rstd = binding.solon_layernorm_forward(hidden, self.weight, self.bias, eps=LN_EPS)
-        return hidden, normed, mean, rstd, normed @ self.head.t()
+        return hidden, *binding.solon_layernorm_forward(hidden, self.weight, self.bias, eps=LN_EPS)
 
     def partition_gradients(self, tokens, targets):
         """Fills the gradient matrix with each partition's gradient of its mean loss -log p(target); returns the rows' log p.
@@ -64,14 +66,21 @@ class TokenLoop:
             raise ValueError("tokens and targets must be P x n")
         V, C = self.vocab, self.width
         flat_targets = targets.reshape(-1)
-        hidden, normed, mean, rstd, logits = self._forward(tokens.reshape(-1))
-        scored = binding.solon_token_logprobs(logits, flat_targets)
+        hidden, normed, mean, rstd = self._forward(tokens.reshape(-1))
         g = torch.full((P * n,), -1.0 / n, device="cuda")
-        dlogits = binding.solon_token_logprobs_backward(logits, flat_targets, scored.peak, scored.log_sum, g, out=logits)
         o = self.offsets
-        part = self.grads.as_strided((P, V, C), (self.plan.d, C, 1), o[3])
-        torch.bmm(dlogits.view(P, n, V).transpose(1, 2), normed.view(P, n, C), out=part)
-        dhidden, _, _ = binding.solon_layernorm_backward(dlogits @ self.head, hidden, mean, rstd, self.weight, partitions=P,
+        if self.fused_head:
+            scored = binding.solon_head_logprobs(normed, self.head, flat_targets)
+            dnormed, _ = binding.solon_head_logprobs_backward(normed, self.head, flat_targets, scored.peak, scored.log_sum, g, partitions=P,
+                                                              dweight=self.grads[:, o[3]:])
+        else:
+            logits = normed @ self.head.t()
+            scored = binding.solon_token_logprobs(logits, flat_targets)
+            dlogits = binding.solon_token_logprobs_backward(logits, flat_targets, scored.peak, scored.log_sum, g, out=logits)
+            part = self.grads.as_strided((P, V, C), (self.plan.d, C, 1), o[3])
+            torch.bmm(dlogits.view(P, n, V).transpose(1, 2), normed.view(P, n, C), out=part)
+            dnormed = dlogits @ self.head
+        dhidden, _, _ = binding.solon_layernorm_backward(dnormed, hidden, mean, rstd, self.weight, partitions=P,
                                                          dweight=self.grads[:, o[1]:o[2]], dbias=self.grads[:, o[2]:o[3]])
         binding.solon_embedding_backward(dhidden, tokens.reshape(-1), V, partitions=P, dweight=self.grads[:, :o[1]])
         return scored.logp
@@ -89,5 +98,5 @@ class TokenLoop:
 
     def next_tokens(self, tokens, top_k: int = 5):
         """What the model expects after each token: (ids, log probabilities) of the top_k likeliest, and the entropy."""
-        scored = binding.solon_token_logprobs(self._forward(tokens)[4], top_k=top_k)
+        scored = binding.solon_token_logprobs(self._forward(tokens)[1] @ self.head.t(), top_k=top_k)
         return scored.top_ids, scored.top_logp, scored.entropy
