@@ -405,8 +405,8 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
  *   peak, log_sum, entropy, grad_logp, grad_entropy  as in solon_token_logprobs_backward
  *   workspace  device, 256-byte aligned, solon_head_logprobs_backward_workspace(...) bytes: dlogits of one piece of the vocabulary (at most
  *              256 MB, or 256 tokens), sums of dhidden
- * dlogits is rounded to 16 bits where the result is (dhidden of 16-bit types, bfloat16 gradients), and held in two such pieces (2^-16 of each value,
- * 2^-22 for float32 and float16 inputs) for float32 and float64 gradients.  rows = 0: dweight becomes 0.  hidden has to be finite in rows that count in no gradient,
+ * dlogits is rounded to 16 bits where the result is (dhidden of 16-bit types, bfloat16 gradients), and held in two float16 pieces (2^-22 of each value)
+ * for float32 and float64 gradients.  rows = 0: dweight becomes 0.  hidden has to be finite in rows that count in no gradient,
  * too: they are multiplied by zeros. */
 int64_t solon_head_logprobs_backward_workspace(int64_t rows, int64_t cols, int64_t vocab, int partitions, int dtype, int grad_dtype, int aligned);
 int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const void* weight, int64_t weight_pitch, int dtype, const int64_t* targets,

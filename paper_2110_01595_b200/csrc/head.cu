@@ -11,8 +11,8 @@
 //                      values down to 2^-28 of the largest, and an absolute 2^-40 of it below.  A product is three: hi lo + lo hi + hi hi; the lo lo
 //                      left out is below 2^-22 of the term.  (Three bfloat16 pieces would take six products.)
 //   dz                 one piece where what it is multiplied into is rounded to 16 bits anyway (dh of 16-bit states, bfloat16 gradients: as much
-//                      rounding again, 2^-8 or 2^-11 of each term at most, of independent signs), two for float32 and float64 gradients (2^-16 with
-//                      bfloat16 pieces, 2^-22 with float16 ones).  bfloat16 gradients of float32 states take the first piece of the states alone, too.  float16 pieces of dz are scaled by the largest |g| + |g_H| (H + 1).
+//                      rounding again, 2^-8 or 2^-11 of each term at most, of independent signs), two float16 pieces for float32 and float64 gradients (2^-22 of each
+//                      term; bfloat16 states are taken as float16 by a power of two for that product, exactly down to 2^-28 of the largest).  bfloat16 gradients of float32 states take the first piece of the states alone, too.  float16 pieces of dz are scaled by the largest |g| + |g_H| (H + 1).
 //
 // Few rows (a served token) are a matter of reading W once: a kernel of ordinary multiply-adds takes any type and alignment.
 
@@ -80,7 +80,7 @@ struct HeadArgs {
   int64_t first, vocab;
   // kDz
   int dz_pitch;                          // this piece's tokens, zeros behind them up to a multiple of 64
-  int pieces;                            // of dz
+  int pieces;                            // of dz (3: kMixed)
   // kDhidden, kDweight
   float* sums;                           // slabs x m x sums_pitch: where the result goes in float32 instead of to the output, if store_sums
   int64_t sums_pitch;
@@ -151,6 +151,10 @@ struct DzRow {
   float peak, log_sum, entropy, g, gh;
 };
 
+// What is stored of dz: its type's nearest; with what that leaves as a second piece; or, for bfloat16 states and float32 gradients, the nearest bfloat16 (for dh) and
+// two float16 pieces (for dW).
+enum DzForm { kNearest, kPair, kMixed };
+
 template <typename T>
 struct DzOut {
   const CUtensorMap* map;
@@ -158,68 +162,90 @@ struct DzOut {
   int col, row, columns, lane;           // first column and row of the warp, columns that there are
   int place;                             // of the row's target (-1: not here) and its element
   float target;
+  float grow;                            // kMixed: the power of two of the float16 pieces
 };
 
-// -p (g + g_H (log p + H)) of N tokens of a row, from their logits: a piece of 16 bits and, with TWO, what that leaves, in blocks of 64 tokens that are
+// 64 elements of a row as 16-bit words to a block, and the target's.  Leaves what the words leave of the elements, where LEAVE.
+template <bool LEAVE, typename T>
+__device__ __forceinline__ void dz_block(float* v, float& target, uint32_t keep, float grow, int place, int lane, char* block) {
+  using Word = Word16<T>;
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      float &x = v[8 * i + 2 * j], &y = v[8 * i + 2 * j + 1];
+      w[j] = Word::join(x * grow, y * grow) & keep;
+      if (LEAVE) {
+        float wx, wy;
+        Word::pair(w[j], wx, wy);
+        x = fmaf(x, grow, -wx), y = fmaf(y, grow, -wy);
+      }
+    }
+    reinterpret_cast<uint4*>(block)[lane * 8 + (i ^ (lane & 7))] = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  if (place >= 0 && place < 64) {
+    const T nearest = from_float<T>(target * grow);
+    reinterpret_cast<T*>(block)[(lane * 8 + ((place / 8) ^ (lane & 7))) * 8 + place % 8] = nearest;
+    if (LEAVE) target = fmaf(target, grow, -to_float(nearest));
+  }
+}
+
+// -p (g + g_H (log p + H)) of N tokens of a row, from their logits, in blocks of 64 tokens that are
 // copied from shared memory (rows of their own are 32-byte writes, which go out at a third of the rate).  `keep` 0: zeros.
 // The forms are functions of their own so that no branch stands between the elements: with branches an element's chain of operations has nothing beside it.
-template <bool ENTROPY, bool TWO, int N, typename T>
-__device__ __forceinline__ void dz_row(const DzRow& r, const float (&v)[N], uint32_t keep, const DzOut<T>& out) {
-  using Word = Word16<T>;
+template <bool ENTROPY, DzForm FORM, int N, typename T>
+__device__ __forceinline__ void dz_row(const DzRow& r, float (&v)[N], uint32_t keep, const DzOut<T>& out, int& turn) {
   Float2 mp = pack2(-r.peak, -r.peak);
   const Float2 ml = pack2(-r.log_sum, -r.log_sum), ml2 = pack2(-r.log_sum * kLog2e, -r.log_sum * kLog2e), l2e = pack2(kLog2e, kLog2e);
   const Float2 mg = pack2(-r.g, -r.g), mh = pack2(-r.gh, -r.gh), h2 = pack2(r.entropy, r.entropy);
 #pragma unroll
   for (int c = 0; c < N; c += 64) {
     if (c >= out.columns) break;
-    char* block[2];
 #pragma unroll
-    for (int p = 0; p < 2; p++) block[p] = out.stage + (TWO ? p : c / 64 % 2) * 4096;
-    if (out.lane == 0) {                     // the blocks that were here before have left
-      if (TWO) stores_read<0>();
-      else stores_read<1>();
+    for (int i = c; i < c + 64; i += 2) {
+      const Float2 x2 = add2(pack2(v[i], v[i + 1]), mp);
+      float x, y;
+      unpack2(fma2(x2, l2e, ml2), x, y);
+      Float2 d = pack2(exp2_fast(x), exp2_fast(y));
+      if (ENTROPY) {                         // (p = 0 where log p is -infinity, and no product with it)
+        unpack2(add2(x2, ml), x, y);
+        d = mul2(d, fma2(add2(pack2(fmaxf(x, -1e30f), fmaxf(y, -1e30f)), h2), mh, mg));
+      } else d = mul2(d, mg);
+      unpack2(d, v[i], v[i + 1]);
+      if (i % 16 == 14) in_turn(mp, d);
     }
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-      uint32_t hi[4], lo[4];
-      Float2 d;
-#pragma unroll
-      for (int j = 0; j < 4; j++) {
-        const int at = c + 8 * i + 2 * j;
-        const Float2 x2 = add2(pack2(v[at], v[at + 1]), mp);
-        float x, y;
-        unpack2(fma2(x2, l2e, ml2), x, y);
-        d = pack2(exp2_fast(x), exp2_fast(y));
-        if (ENTROPY) {                       // (p = 0 where log p is -infinity, and no product with it)
-          unpack2(add2(x2, ml), x, y);
-          d = mul2(d, fma2(add2(pack2(fmaxf(x, -1e30f), fmaxf(y, -1e30f)), h2), mh, mg));
-        } else d = mul2(d, mg);
-        unpack2(d, x, y);
-        hi[j] = Word::join(x, y) & keep;
-        if (TWO) {
-          float hx, hy;
-          Word::pair(hi[j], hx, hy);
-          lo[j] = Word::join(x - hx, y - hy) & keep;
-        }
+    float target = out.target;
+    // the two blocks take turns: one is filled when the copy of what it held, the last but one, has read it
+    auto free_block = [&] {
+      if (out.lane == 0) stores_read<1>();
+      __syncwarp();
+      return out.stage + turn * 4096;
+    };
+    auto give = [&](int piece) {
+      fence_async();
+      __syncwarp();
+      if (out.lane == 0) {
+        store_block(out.map, out.col + c, out.row, piece, pipe::smem_addr(out.stage + turn * 4096));
+        stores_commit();
       }
-      if (i % 2) in_turn(mp, d);
-      const int to = out.lane * 8 + (i ^ (out.lane & 7));
-      reinterpret_cast<uint4*>(block[0])[to] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-      if (TWO) reinterpret_cast<uint4*>(block[1])[to] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-    }
-    if (out.place >= c && out.place < c + 64) {
-      const int in = out.place - c, to = (out.lane * 8 + ((in / 8) ^ (out.lane & 7))) * 8 + in % 8;
-      const T first = from_float<T>(out.target);
-      reinterpret_cast<T*>(block[0])[to] = first;
-      if (TWO) reinterpret_cast<T*>(block[1])[to] = from_float<T>(out.target - to_float(first));
-    }
-    fence_async();
-    __syncwarp();
-    if (out.lane == 0) {
-      store_block(out.map, out.col + c, out.row, 0, pipe::smem_addr(block[0]));
-      if (TWO) store_block(out.map, out.col + c, out.row, 1, pipe::smem_addr(block[1]));
-      stores_commit();
+      turn ^= 1;
+    };
+    if constexpr (FORM == kNearest) {
+      dz_block<false, T>(v + c, target, keep, 1.0f, out.place - c, out.lane, free_block());
+      give(0);
+    } else if constexpr (FORM == kPair) {
+      dz_block<true, T>(v + c, target, keep, 1.0f, out.place - c, out.lane, free_block());
+      give(0);
+      dz_block<false, T>(v + c, target, keep, 1.0f, out.place - c, out.lane, free_block());
+      give(1);
+    } else {
+      dz_block<false, T>(v + c, target, keep, 1.0f, out.place - c, out.lane, free_block());
+      give(0);
+      dz_block<true, __half>(v + c, target, keep, out.grow, out.place - c, out.lane, free_block());
+      give(1);
+      dz_block<false, __half>(v + c, target, keep, 1.0f, out.place - c, out.lane, free_block());
+      give(2);
     }
   }
 }
@@ -374,6 +400,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
     }
     uint32_t sum_phase = 0;
     int half = 0;
+    [[maybe_unused]] int turn = 0;           // which of the warp's two blocks of the result is filled next
     [[maybe_unused]] RowSums rows_so_far[kHalf / 32];
     if constexpr (MODE == kFewRows) {
 #pragma unroll
@@ -428,7 +455,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
         if ((half ^= 1) == 0) sum_phase ^= 1;
       }
       if (absent) continue;
-      if (a.scaled) {
+      if (MODE == kDz ? a.scaled & 3 : a.scaled) {
 #pragma unroll
         for (int i = 0; i < kHalf; i++) v[i] = v[i] * undo[0] * undo[1];
       }
@@ -490,7 +517,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
         }
       } else if constexpr (MODE == kDz) {
         using T16 = typename std::conditional<BF16, __nv_bfloat16, __half>::type;
-        const float grow = a.scaled & 4 ? power_of_two(scale_exponent(a.words->dz)) : 1.0f;
+        const float power = a.scaled & 4 ? power_of_two(scale_exponent(a.words->dz)) : 1.0f, grow = a.pieces == 3 ? 1.0f : power;
         copies_wait<0>();
         const int64_t target = a.targets && row < a.m ? of_targets[lane] : -1;
         DzRow r = {of_rows[lane], of_rows[32 + lane], a.grad_entropy ? of_rows[96 + lane] : 0.0f, a.grad_logp && target >= 0 ? of_rows[64 + lane] : 0.0f,
@@ -517,13 +544,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
           d = active ? fmaf(exp2_fast(lp * kLog2e), fmaf(-r.gh, lp + r.entropy, -r.g), r.g) : 0.0f;
         }
         const int place = hit ? (int)token : -1;
-        const DzOut<T16> out = {&maps.out, stage, col, row0, a.dz_pitch - col, lane, place, d};
+        const DzOut<T16> out = {&maps.out, stage, col, row0, a.dz_pitch - col, lane, place, d, power};
         if (a.grad_entropy) {
-          if (a.pieces == 2) dz_row<true, true, kHalf>(r, v, keep, out);
-          else dz_row<true, false, kHalf>(r, v, keep, out);
+          if (a.pieces == 1) dz_row<true, kNearest>(r, v, keep, out, turn);
+          else if (a.pieces == 2) dz_row<true, kPair>(r, v, keep, out, turn);
+          else if (BF16) dz_row<true, kMixed>(r, v, keep, out, turn);
         } else {
-          if (a.pieces == 2) dz_row<false, true, kHalf>(r, v, keep, out);
-          else dz_row<false, false, kHalf>(r, v, keep, out);
+          if (a.pieces == 1) dz_row<false, kNearest>(r, v, keep, out, turn);
+          else if (a.pieces == 2) dz_row<false, kPair>(r, v, keep, out, turn);
+          else if (BF16) dz_row<false, kMixed>(r, v, keep, out, turn);
         }
       } else {
         // (the sums' pitch is a multiple of 128: room for all columns of a warp that has any)
@@ -547,7 +576,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
 #pragma unroll
           for (int c = 0; c < kHalf; c += kEach) {
             if (col + c >= a.n || row0 >= a.m) break;
-            uint4* block = reinterpret_cast<uint4*>(stage + (c / kEach % 2) * 4096);
+            uint4* block = reinterpret_cast<uint4*>(stage + turn * 4096);
+            turn ^= 1;
             if (lane == 0) stores_read<1>();           // the block before the last one has left its place
             __syncwarp();
 #pragma unroll
@@ -751,6 +781,7 @@ __global__ void __launch_bounds__(256) head_join_kernel(HeadJoinArgs a) {
 
 struct HeadScanArgs {
   const float *hidden, *weight;          // NULL: not wanted
+  const __nv_bfloat16* hidden16;         // the same
   int64_t hidden_pitch, weight_pitch, rows, cols, vocab;
   const float *grad_logp, *grad_entropy, *entropy;
   int dz;
@@ -772,6 +803,11 @@ __global__ void __launch_bounds__(256) head_scan_kernel(HeadScanArgs a) {
     word = &a.words->dz;
     for (int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x; r < a.rows; r += (int64_t)gridDim.x * 256)
       see((a.grad_logp ? fabsf(a.grad_logp[r]) : 0.0f) + (a.grad_entropy ? fabsf(a.grad_entropy[r]) * (fabsf(a.entropy[r]) + 1.0f) : 0.0f));
+  } else if (blockIdx.y == 0 && a.hidden16) {
+    word = &a.words->hidden;
+    for (int64_t r = (int64_t)blockIdx.x * 8 + warp; r < a.rows; r += (int64_t)gridDim.x * 8)
+#pragma unroll 8
+      for (int64_t c = lane; c < a.cols; c += 32) see(__bfloat162float(a.hidden16[r * a.hidden_pitch + c]));
   } else {
     const float* m = blockIdx.y ? a.weight : a.hidden;
     if (!m) return;
@@ -809,13 +845,15 @@ __global__ void __launch_bounds__(256) head_scan_kernel(HeadScanArgs a) {
   }
 }
 
-// Rows of a matrix at a pitch that tensor copies can take, zeros behind their ends: float32 as two float16 pieces, 16-bit elements as they are.
+// Rows of a matrix at a pitch that tensor copies can take, zeros behind their ends: float32 as two float16 pieces, bfloat16 as a float16 one, 16-bit elements
+// (of type uint16_t here) as they are.
 template <typename T>
 __global__ void __launch_bounds__(256) head_split_kernel(const T* x, int64_t pitch, int64_t rows, int64_t cols, uint16_t* out, int64_t out_pitch,
                                                          const unsigned* largest) {
   const int64_t words = out_pitch / 8;
   float scale = 1.0f;
-  if constexpr (sizeof(T) == 4) scale = power_of_two(scale_exponent(*largest));
+  constexpr bool kToHalf = std::is_same<T, __nv_bfloat16>::value;
+  if constexpr (sizeof(T) == 4 || kToHalf) scale = power_of_two(scale_exponent(*largest));
   const bool wide = sizeof(T) == 4 && !(((uintptr_t)x | (uintptr_t)(pitch * 4)) & 15);
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * words; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / words, c = (i - r * words) * 8;
@@ -839,6 +877,11 @@ __global__ void __launch_bounds__(256) head_split_kernel(const T* x, int64_t pit
       }
       store_pack((__half*)out + r * out_pitch + c, hi);
       store_pack((__half*)out + (rows + r) * out_pitch + c, lo);
+    } else if constexpr (kToHalf) {
+      Pack<__half, 8> v;
+#pragma unroll
+      for (int e = 0; e < 8; e++) v.e[e] = __float2half_rn(c + e < cols ? __bfloat162float(p[e]) * scale : 0.0f);
+      store_pack((__half*)out + r * out_pitch + c, v);
     } else {
       Pack<uint16_t, 8> v;
 #pragma unroll
@@ -891,7 +934,7 @@ struct HeadPlan {
   int dz_pieces;
   int64_t width;                         // tokens of a piece of the vocabulary
   int h_splits, w_splits;                // parts of the inner dimensions of dh and dW
-  int64_t words, partial, target_logit, hidden, weight, dz, sums, w_sums, total;
+  int64_t words, partial, target_logit, hidden, weight, hidden16, dz, sums, w_sums, total;
 };
 
 constexpr int64_t kHeadSharedRows = 200 * 1024;       // bytes of hidden rows that the kernel for few rows holds
@@ -971,7 +1014,7 @@ static HeadPlan head_backward_plan(int64_t rows, int64_t cols, int64_t vocab, in
   p.pieces = dtype == SOLON_F32 ? 2 : 1;
   p.split = dtype == SOLON_F32 || !aligned;
   p.pitch = up(cols, kBlock);
-  p.dz_pieces = dtype == SOLON_F32 || grad_dtype != SOLON_BF16 ? 2 : 1;
+  p.dz_pieces = dtype == SOLON_F32 ? 2 : grad_dtype == SOLON_BF16 ? 1 : dtype == SOLON_BF16 ? 3 : 2;
   p.width = std::min(up(vocab, 64), std::max<int64_t>(kTile, kDzBytes / (rows * 2 * p.dz_pieces) / kTile * kTile));
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
@@ -996,6 +1039,7 @@ static HeadPlan head_backward_plan(int64_t rows, int64_t cols, int64_t vocab, in
     p.hidden = take(p.pieces * rows * p.pitch * 2);
     p.weight = take(p.pieces * vocab * p.pitch * 2);
   }
+  if (p.dz_pieces == 3) p.hidden16 = take(rows * p.pitch * 2);
   p.dz = take(p.dz_pieces * rows * p.width * 2);
   if (times > 1 || p.h_splits > 1) p.sums = take(p.h_splits * rows * up(cols, 128) * 4);
   if (p.w_splits > 1) p.w_sums = take((int64_t)p.w_splits * partitions * std::min(vocab, p.width) * up(cols, 128) * 4);
@@ -1088,7 +1132,7 @@ static int head_operand(const void* x, int64_t pitch, int64_t rows, int64_t cols
 }
 
 static int head_scan(const HeadScanArgs& a, int sms, cudaStream_t stream) {
-  if (!a.hidden && !a.weight && !a.dz) return SOLON_OK;
+  if (!a.hidden && !a.hidden16 && !a.weight && !a.dz) return SOLON_OK;
   head_scan_kernel<<<dim3(4 * sms, 3), 256, 0, stream>>>(a);
   SOLON_CUDA_TRY(cudaGetLastError());
   return SOLON_OK;
@@ -1191,7 +1235,7 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
   } else {
     if (dtype == SOLON_F32) {
       SOLON_CUDA_TRY(cudaMemsetAsync(words, 0, sizeof(HeadWords), stream));
-      const HeadScanArgs scan = {(const float*)hidden, (const float*)weight, hidden_pitch, weight_pitch, rows, cols, vocab, nullptr, nullptr, nullptr, 0, words};
+      const HeadScanArgs scan = {(const float*)hidden, (const float*)weight, nullptr, hidden_pitch, weight_pitch, rows, cols, vocab, nullptr, nullptr, nullptr, 0, words};
       if ((rc = head_scan(scan, sms, stream))) return rc;
     }
     HeadOperand h, w;
@@ -1288,9 +1332,10 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
     if ((rc = small_backward(a, stream)) || !dhidden) return rc;
     return head_finish({a.sums, a.sums_pitch, rows, cols, rows > 1 ? dhidden_pitch : cols, 0, 1, plan.h_splits, dhidden}, dtype, sms, stream);
   }
-  if (!bf16) SOLON_CUDA_TRY(cudaMemsetAsync(words, 0, sizeof(HeadWords), stream));
-  const HeadScanArgs scan = {f32 ? (const float*)hidden : nullptr, f32 ? (const float*)weight : nullptr, hidden_pitch, weight_pitch, rows, cols, vocab,
-                             grad_logp, grad_entropy, entropy, !bf16, words};
+  const bool mixed = plan.dz_pieces == 3 && dweight;
+  if (!bf16 || mixed) SOLON_CUDA_TRY(cudaMemsetAsync(words, 0, sizeof(HeadWords), stream));
+  const HeadScanArgs scan = {f32 ? (const float*)hidden : nullptr, f32 ? (const float*)weight : nullptr, mixed ? (const __nv_bfloat16*)hidden : nullptr,
+                             hidden_pitch, weight_pitch, rows, cols, vocab, grad_logp, grad_entropy, entropy, !bf16 || mixed, words};
   if ((rc = head_scan(scan, sms, stream))) return rc;
   HeadOperand h, w;
   if ((rc = head_operand(hidden, hidden_pitch, rows, cols, dtype, plan, ws + plan.hidden, &words->hidden, sms, stream, &h))) return rc;
@@ -1306,8 +1351,18 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
   };
   const bool coarse = grad_dtype == SOLON_BF16;
   const bool w_narrow = narrow(cols, (n + kBlock - 1) / kBlock * (coarse ? 1 : h.pieces + 1));
+  HeadOperand hw = h;                      // as it goes into dW
+  if (mixed) {
+    const int64_t items = rows * (plan.pitch / 8);
+    head_split_kernel<__nv_bfloat16><<<(unsigned)std::min<int64_t>((items + 255) / 256, 16 * sms), 256, 0, stream>>>(
+        (const __nv_bfloat16*)hidden, hidden_pitch, rows, cols, (uint16_t*)(ws + plan.hidden16), plan.pitch, &words->hidden);
+    SOLON_CUDA_TRY(cudaGetLastError());
+    hw = {ws + plan.hidden16, plan.pitch, rows, 1};
+  }
+  const bool hw_whole = whole || mixed;
   if (!tensor_map(&map_h, h.p, bf16, cols, rows, h.pieces, h.pitch, rows * h.pitch, kRows) ||
-      !across(&map_h_across, h.p, n, (int64_t)h.pieces * partitions, h.pitch, n * h.pitch, w_narrow))
+      !(hw_whole && !w_narrow ? tensor_map_by_blocks(&map_h_across, hw.p, bf16 && !mixed, cols, n, (int64_t)hw.pieces * partitions, hw.pitch, n * hw.pitch)
+                              : tensor_map(&map_h_across, hw.p, bf16 && !mixed, cols, n, (int64_t)hw.pieces * partitions, hw.pitch, n * hw.pitch, kBlock)))
     return SOLON_ERR_CUDA;
   HeadArgs base = {};
   base.slabs = base.splits = 1;
@@ -1320,6 +1375,7 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
   base.grad_entropy = grad_entropy;
   base.vocab = vocab;
   const int dz_scaled = bf16 ? 0 : 4;
+  const int dz_pieces = plan.dz_pieces == 3 && !mixed ? 1 : plan.dz_pieces;
   auto run = [&](int which, const HeadMaps& maps, const HeadArgs& a) {
     if (f32) return head_backward_piece<false, float>(which, maps, a, grad_dtype, sms, stream);
     if (bf16) return head_backward_piece<true, __nv_bfloat16>(which, maps, a, grad_dtype, sms, stream);
@@ -1329,9 +1385,10 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
     const int64_t width = std::min(plan.width, vocab - first), pitch = up(width, kBlock);
     const char* w_piece = w.p + first * w.pitch * 2;
     const bool h_narrow = narrow(cols, pitch / kBlock * (f32 ? 3 : 1));
-    if (!tensor_map(&map_dz, ws + plan.dz, bf16, pitch, rows, plan.dz_pieces, pitch, rows * pitch, kRows) ||
-        !tensor_map(&map_dz_out, ws + plan.dz, bf16, pitch, rows, plan.dz_pieces, pitch, rows * pitch, 32) ||
-        !tensor_map_by_blocks(&map_dz_across, ws + plan.dz, bf16, pitch, n, (int64_t)plan.dz_pieces * partitions, pitch, n * pitch) ||
+    const char* dz_across = ws + plan.dz + (mixed ? rows * pitch * 2 : 0);      // (the float16 pieces)
+    if (!tensor_map(&map_dz, ws + plan.dz, bf16, pitch, rows, mixed ? 1 : dz_pieces, pitch, rows * pitch, kRows) ||
+        !tensor_map(&map_dz_out, ws + plan.dz, bf16, pitch, rows, dz_pieces, pitch, rows * pitch, 32) ||
+        !tensor_map_by_blocks(&map_dz_across, dz_across, bf16 && !mixed, pitch, n, (int64_t)(mixed ? 2 : dz_pieces) * partitions, pitch, n * pitch) ||
         !tensor_map(&map_w, w_piece, bf16, cols, width, w.pieces, w.pitch, vocab * w.pitch, kRows) ||
         !across(&map_w_across, w_piece, width, w.pieces, w.pitch, vocab * w.pitch, h_narrow))
       return SOLON_ERR_CUDA;
@@ -1341,8 +1398,8 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
     a.first = first;
     a.k_blocks = (int)((cols + kBlock - 1) / kBlock);
     head_pairs(a, h.pieces, w.pieces, 1, 1);
-    a.scaled = (f32 ? 3 : 0) | dz_scaled;
-    a.pieces = plan.dz_pieces;
+    a.scaled = (f32 ? 3 : 0) | (mixed ? 4 : dz_scaled);
+    a.pieces = dz_pieces;
     a.dz_pitch = (int)pitch;
     if ((rc = run(kDz, {map_h, map_w, map_dz_out}, a))) return rc;
     if (dhidden) {
@@ -1376,13 +1433,13 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
       a.slabs = partitions * a.splits;
       a.slab_a = a.slab_b = 1;
       a.narrow = w_narrow;
-      a.b_by_blocks = whole && !w_narrow;
+      a.b_by_blocks = hw_whole && !w_narrow;
       a.k_blocks = (int)(((n + kBlock - 1) / kBlock + a.splits - 1) / a.splits);
       a.sums = (float*)(ws + plan.w_sums);
       a.sums_pitch = sums_pitch;
       a.store_sums = a.splits > 1;
       head_pairs(a, coarse ? 1 : 2, coarse ? 1 : h.pieces, partitions, partitions);
-      a.scaled = (f32 ? 1 : 0) | dz_scaled;
+      a.scaled = mixed ? 5 : (f32 ? 1 : 0) | dz_scaled;
       a.out = (char*)dweight + first * cols * grad_size;
       a.out_pitch = cols;
       a.out_slab = partitions > 1 ? grad_pitch : 0;
@@ -1391,7 +1448,7 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
       a.out_by_map = !(((uintptr_t)a.out | (uintptr_t)(cols * grad_size) | (uintptr_t)(a.out_slab * grad_size)) & 15);
       if (a.out_by_map && !output_map(&maps.out, a.out, (int)grad_size, cols, width, partitions, cols, partitions > 1 ? a.out_slab : up(width * cols, 8)))
         return SOLON_ERR_CUDA;
-      if ((rc = run(kDweight, maps, a))) return rc;
+      if ((rc = mixed ? head_backward_piece<false, __half>(kDweight, maps, a, grad_dtype, sms, stream) : run(kDweight, maps, a))) return rc;
       if (a.splits > 1 && (rc = head_finish({a.sums, sums_pitch, width, cols, cols, a.out_slab, partitions, a.splits, a.out}, grad_dtype, sms, stream))) return rc;
     }
   }

@@ -11,7 +11,8 @@ under the softmax, log S is off by (k + 2 D) u + 2 t, logp by 2 u (|z_t - M| + |
 Gradient: p is off by a relative r = (4 |log p| + 8) u + z_tol; so dz = -p (g + g_H (log p + H)) by p |g + g_H (log p + H)| (r + 4 u) + p |g_H| (z_tol + 4 u (|log p| + H));
 a product with dz is off by what that gives, by the sum's c u times its absolute terms (c = 64 + n / 256 as above; 1040 + n / 4096 where the
 result has 16 bits, as 256 steps are cut off before the sum is added to another), by dz's own rounding (half a step: 2^-8 for bfloat16, 2^-11 for
-float16 with 2^-40 of the largest bound below; squared where there are two pieces) and by half a step of the result's type.  A bfloat16 gradient
+float16 with 2^-40 of the largest bound below; float16's squared where there are two pieces, which are float16 ones for float32 gradients of any
+states, and 2^-40 of the largest bfloat16 state) and by half a step of the result's type.  A bfloat16 gradient
 of float32 states takes the first float16 piece of both factors alone, so h's rounding of half a float16 step, 2^-11 of each term, joins dz's.
 The tensor cores line a step's products up by the factors' exponents, and a float16 element below 2^-14 has the exponent of 2^-14 with zeros in front: what is
 cut off is relative to that, so such an element counts as 2^-14 in the terms of 64 u s and c u (with 2^-20 at 2e-6, six bits less are kept: 64 u becomes 2^-12)."""
@@ -153,7 +154,10 @@ def _check_backward(h, w, t, peak, log_sum, g, entropy, gh, parts, dh, dw):
         size = a.abs() @ b.abs()
         step = torch.finfo(result.dtype).eps / 2
         c = 1040 + inner_size / 4096 if result.element_size() == 2 else 64 + inner_size / 256
-        rounding = half ** pieces * (2 if pieces == 2 else 1) * size + least * b.abs().sum(-2, keepdim=True)
+        fine = pieces == 2 and h.dtype == torch.bfloat16          # bfloat16 states: dz in float16 pieces, the states as float16 elements
+        rounding = (2.0 ** -21 if pieces == 2 else half) * size + (2.0 ** -39 * bound if fine else least) * b.abs().sum(-2, keepdim=True)
+        if fine:
+            rounding = rounding + 2.0 ** -39 * b.abs().max() * a.abs().sum(-1, keepdim=True)
         tol = atol @ b.abs() + rounding + c * U * (a.abs() @ _size(factor)) + step * x.abs()
         if h.dtype == torch.float32:                              # the other factor's pieces
             tol = tol + (2.0 ** -11 if pieces == 1 else 2.0 ** -20) * size + 2.0 ** -39 * b.abs().max() * a.abs().sum(-1, keepdim=True)
