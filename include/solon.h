@@ -404,7 +404,7 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
  *                                        vocab x cols elements of `grad_dtype` (SOLON_F32, SOLON_F64 or SOLON_BF16), over the rows of partition k
  *   peak, log_sum, entropy, grad_logp, grad_entropy  as in solon_token_logprobs_backward
  *   workspace  device, 256-byte aligned, solon_head_logprobs_backward_workspace(...) bytes: dlogits of one piece of the vocabulary (at most
- *              256 MB, or 256 tokens), sums of dhidden
+ *              512 MB, or 256 tokens), sums of dhidden
  * dlogits is rounded to 16 bits where the result is (dhidden of 16-bit types, bfloat16 gradients), and held in two float16 pieces (2^-22 of each value)
  * for float32 and float64 gradients.  rows = 0: dweight becomes 0.  hidden has to be finite in rows that count in no gradient,
  * too: they are multiplied by zeros. */

@@ -63,7 +63,7 @@ def test_head_refusals(lib):
     assert f(None, 8, None, 8, 0, None, 0, 8, 10, None, None, None, None, None, 0, None) == 0
     v = lib.solon_head_logprobs_backward_workspace
     assert v(0, 8, 10, 1, 0, 0, 1) == 0 and v(4, 8, 10, 1, 0, 3, 1) == BAD and v(4, 8, 10, 1, 1, 0, 1) == BAD and v(4, 8, 10, 3, 0, 0, 1) == BAD
-    assert v(100_000, 64, 50_000, 1, 2, 0, 1) < (1 << 28) + 100_000 * 128 * 4 + 4096                # dlogits comes in pieces
+    assert v(100_000, 64, 50_000, 1, 2, 0, 1) < (1 << 29) + 100_000 * 128 * 4 + 4096                # dlogits comes in pieces
     b = lib.solon_head_logprobs_backward
 
     def call(h=at, hp=8, m=at, mp=8, dtype=0, t=at, rows=4, cols=8, vocab=10, parts=2, peak=at, ls=at, ent=None, g=at, gh=None, dh=at, dhp=8, dw=at, dwp=80, gt=0, ws=at, n=big):
