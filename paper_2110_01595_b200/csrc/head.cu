@@ -329,6 +329,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
   cluster_sync();
   fence_after();
   const uint32_t tmem = *tmem_at;
+  pdl_wait();                            // up to here nothing of the kernels before is touched
 
   if (warp < kFirstEpilogue) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");        // 128 x 72 + 256 x 216 = 64512 = 384 x 168 at launch
@@ -791,6 +792,7 @@ struct HeadScanArgs {
 // Largest finite magnitudes: of the hidden states, the output matrix, and a bound of each row's dz, |g| + |g_H| (H + 1).
 __global__ void __launch_bounds__(256) head_scan_kernel(HeadScanArgs a) {
   __shared__ unsigned most[8];
+  pdl_trigger();
   unsigned big = 0;
   auto see = [&](float x) {
     const unsigned u = __float_as_uint(x) & 0x7FFFFFFFu;
@@ -850,6 +852,8 @@ __global__ void __launch_bounds__(256) head_scan_kernel(HeadScanArgs a) {
 template <typename T>
 __global__ void __launch_bounds__(256) head_split_kernel(const T* x, int64_t pitch, int64_t rows, int64_t cols, uint16_t* out, int64_t out_pitch,
                                                          const unsigned* largest) {
+  pdl_trigger();
+  pdl_wait();
   const int64_t words = out_pitch / 8;
   float scale = 1.0f;
   constexpr bool kToHalf = std::is_same<T, __nv_bfloat16>::value;
@@ -900,6 +904,8 @@ struct HeadFinishArgs {
 };
 template <typename O>
 __global__ void __launch_bounds__(256) head_finish_kernel(HeadFinishArgs a) {
+  pdl_trigger();
+  pdl_wait();
   const int64_t words = (a.n + 3) / 4;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.parts * a.m * words; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / words, c = (i - r * words) * 4, part = r / a.m, row = r - part * a.m;
@@ -1098,9 +1104,7 @@ static int head_product_launch(const HeadMaps& maps, HeadArgs a, int sms, cudaSt
   a.band_inverse = inverse(8ll * a.n_tiles);
   const int pairs = (int)std::min<int64_t>(tiles, MODE == kFewRows ? std::min(kFewPairs, sms / 2) : sms / 2);
   SOLON_SHARED_MEMORY_ONCE(kernel, bytes);
-  kernel<<<2 * pairs, kThreads, bytes, stream>>>(maps, a);
-  SOLON_CUDA_TRY(cudaGetLastError());
-  return SOLON_OK;
+  return launch_dependent(kernel, dim3(2 * pairs), dim3(kThreads), bytes, stream, maps, a);
 }
 
 template <int MODE, bool BF16, typename O>
@@ -1124,11 +1128,11 @@ static int head_operand(const void* x, int64_t pitch, int64_t rows, int64_t cols
   }
   const int64_t words = rows * (plan.pitch / 8);
   const unsigned blocks = (unsigned)std::min<int64_t>((words + 255) / 256, 16 * sms);
-  if (dtype == SOLON_F32)
-    head_split_kernel<float><<<blocks, 256, 0, stream>>>((const float*)x, pitch, rows, cols, (uint16_t*)to, plan.pitch, largest);
-  else
-    head_split_kernel<uint16_t><<<blocks, 256, 0, stream>>>((const uint16_t*)x, pitch, rows, cols, (uint16_t*)to, plan.pitch, nullptr);
-  SOLON_CUDA_TRY(cudaGetLastError());
+  const int rc = dtype == SOLON_F32 ? launch_dependent(head_split_kernel<float>, dim3(blocks), dim3(256), 0, stream, (const float*)x, pitch, rows, cols,
+                                                       (uint16_t*)to, plan.pitch, largest)
+                                    : launch_dependent(head_split_kernel<uint16_t>, dim3(blocks), dim3(256), 0, stream, (const uint16_t*)x, pitch, rows, cols,
+                                                       (uint16_t*)to, plan.pitch, (const unsigned*)nullptr);
+  if (rc) return rc;
   *out = {to, plan.pitch, rows, plan.pieces};
   return SOLON_OK;
 }
@@ -1154,12 +1158,9 @@ static void head_pairs(HeadArgs& a, int pieces_a, int pieces_b, int step_a, int 
 
 static int head_finish(const HeadFinishArgs& a, int dtype, int sms, cudaStream_t stream) {
   const unsigned blocks = (unsigned)std::min<int64_t>((a.parts * a.m * ((a.n + 3) / 4) + 255) / 256, 16 * sms);
-  if (dtype == SOLON_F32) head_finish_kernel<float><<<blocks, 256, 0, stream>>>(a);
-  else if (dtype == SOLON_F64) head_finish_kernel<double><<<blocks, 256, 0, stream>>>(a);
-  else if (dtype == SOLON_BF16) head_finish_kernel<__nv_bfloat16><<<blocks, 256, 0, stream>>>(a);
-  else head_finish_kernel<__half><<<blocks, 256, 0, stream>>>(a);
-  SOLON_CUDA_TRY(cudaGetLastError());
-  return SOLON_OK;
+  auto* kernel = dtype == SOLON_F32 ? head_finish_kernel<float> : dtype == SOLON_F64 ? head_finish_kernel<double>
+                 : dtype == SOLON_BF16 ? head_finish_kernel<__nv_bfloat16> : head_finish_kernel<__half>;
+  return launch_dependent(kernel, dim3(blocks), dim3(256), 0, stream, a);
 }
 
 static bool head_sizes_ok(int64_t rows, int64_t cols, int64_t vocab) {
@@ -1356,9 +1357,10 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
   HeadOperand hw = h;                      // as it goes into dW
   if (mixed) {
     const int64_t items = rows * (plan.pitch / 8);
-    head_split_kernel<__nv_bfloat16><<<(unsigned)std::min<int64_t>((items + 255) / 256, 16 * sms), 256, 0, stream>>>(
-        (const __nv_bfloat16*)hidden, hidden_pitch, rows, cols, (uint16_t*)(ws + plan.hidden16), plan.pitch, &words->hidden);
-    SOLON_CUDA_TRY(cudaGetLastError());
+    if ((rc = launch_dependent(head_split_kernel<__nv_bfloat16>, dim3((unsigned)std::min<int64_t>((items + 255) / 256, 16 * sms)), dim3(256), 0, stream,
+                               (const __nv_bfloat16*)hidden, hidden_pitch, rows, cols, (uint16_t*)(ws + plan.hidden16), plan.pitch,
+                               (const unsigned*)&words->hidden)))
+      return rc;
     hw = {ws + plan.hidden16, plan.pitch, rows, 1};
   }
   const bool hw_whole = whole || mixed;
