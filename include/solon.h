@@ -399,14 +399,14 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
                         void* cuda_stream);
 
 /* Its gradients: with dlogits as solon_token_logprobs_backward has it (and recomputed logits),
- *   dhidden = dlogits * weight           device, rows x cols of `dtype` (output; NULL: not wanted; not one of the inputs)
+ *   dhidden = dlogits * weight           device, rows x cols of `dtype` (output; NULL: not wanted; neither output may be an input)
  *   dweight_k = dlogits_k^T * hidden_k   device (output; NULL: not wanted): row k of the partition-gradient matrix from dweight[k * grad_pitch] on,
  *                                        vocab x cols elements of `grad_dtype` (SOLON_F32, SOLON_F64 or SOLON_BF16), over the rows of partition k
  *   peak, log_sum, entropy, grad_logp, grad_entropy  as in solon_token_logprobs_backward
  *   workspace  device, 256-byte aligned, solon_head_logprobs_backward_workspace(...) bytes: dlogits of one piece of the vocabulary (at most
  *              512 MB, or 256 tokens), sums of dhidden
  * dlogits is rounded to 16 bits where the result is (dhidden of 16-bit types, bfloat16 gradients), and held in two float16 pieces (2^-22 of each value)
- * for float32 and float64 gradients.  rows = 0: dweight becomes 0.  hidden has to be finite in rows that count in no gradient,
+ * for float32 and float64 gradients, where bfloat16 states count as float16 times a power of two (exact down to 2^-28 of their largest).  rows = 0: dweight becomes 0.  hidden has to be finite in rows that count in no gradient,
  * too: they are multiplied by zeros. */
 int64_t solon_head_logprobs_backward_workspace(int64_t rows, int64_t cols, int64_t vocab, int partitions, int dtype, int grad_dtype, int aligned);
 int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const void* weight, int64_t weight_pitch, int dtype, const int64_t* targets,

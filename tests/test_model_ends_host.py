@@ -66,10 +66,10 @@ def test_head_refusals(lib):
     assert v(100_000, 64, 50_000, 1, 2, 0, 1) < (1 << 29) + 100_000 * 128 * 4 + 4096                # dlogits comes in pieces
     b = lib.solon_head_logprobs_backward
 
-    def call(h=at, hp=8, m=at, mp=8, dtype=0, t=at, rows=4, cols=8, vocab=10, parts=2, peak=at, ls=at, ent=None, g=at, gh=None, dh=at, dhp=8, dw=at, dwp=80, gt=0, ws=at, n=big):
+    def call(h=at + 256, hp=8, m=at + 512, mp=8, dtype=0, t=at, rows=4, cols=8, vocab=10, parts=2, peak=at, ls=at, ent=None, g=at, gh=None, dh=at, dhp=8, dw=at, dwp=80, gt=0, ws=at, n=big):
         return b(h, hp, m, mp, dtype, t, rows, cols, vocab, parts, peak, ls, ent, g, gh, dh, dhp, dw, dwp, gt, ws, n, None)
 
-    assert call(dtype=1) == BAD and call(hp=7) == BAD and call(mp=7) == BAD and call(h=None) == BAD and call(m=at + 1) == BAD
+    assert call(dtype=1) == BAD and call(hp=7) == BAD and call(mp=7) == BAD and call(h=None) == BAD and call(m=at + 1) == BAD and call(dh=at + 256) == BAD and call(dw=at + 512) == BAD and call(dh=at + 512) == BAD
     assert call(parts=3) == BAD and call(parts=0) == BAD and call(peak=None) == BAD and call(ls=None) == BAD and call(t=None) == BAD
     assert call(gh=at) == BAD and call(dhp=7) == BAD and call(dwp=79) == BAD and call(gt=3) == BAD and call(ws=None) == BAD and call(ws=at + 128) == BAD
     assert call(n=v(4, 8, 10, 2, 0, 0, 1) - 1) == BAD and call(cols=1 << 23) == BAD
