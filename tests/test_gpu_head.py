@@ -358,6 +358,52 @@ def test_on_a_stream_and_in_graphs():
             assert torch.equal(r.logp, want.logp) and torch.equal(out[0], want_dh) and torch.equal(out[1], want_dw)
 
 
+def test_two_calls_at_once():
+    """Products that each want every SM, on two streams: they may run one after the other or side by side."""
+    h, w, t = _inputs(2000, 256, 6000, "bf16", 1)
+    g = torch.full((2000,), -1.0 / 2000, device="cuda")
+    want = binding.solon_head_logprobs(h, w, t)
+    want_dh, want_dw = binding.solon_head_logprobs_backward(h, w, t, want.peak, want.log_sum, g, partitions=4)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    got = []
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(4):
+        for s in streams:
+            with torch.cuda.stream(s):
+                r = binding.solon_head_logprobs(h, w, t)
+                got.append((r, *binding.solon_head_logprobs_backward(h, w, t, r.peak, r.log_sum, g, partitions=4)))
+    torch.cuda.synchronize()
+    for r, dh, dw in got:
+        assert torch.equal(r.logp, want.logp) and torch.equal(dh, want_dh) and torch.equal(dw, want_dw)
+
+
+def test_offsets_beyond_32_bits():
+    """Gradient rows that start beyond 2^31 elements, an output matrix whose last rows do, too (in bytes)."""
+    parts, n, cols, vocab = 3, 2, 8192, 140_000
+    g = _gen(1)
+    h = torch.randn((parts * n, cols), device="cuda", generator=g).bfloat16()
+    w = torch.empty((vocab, cols), dtype=torch.bfloat16, device="cuda").normal_(0.0, cols ** -0.5, generator=g)
+    t = torch.tensor([vocab - 1, 0, 5, vocab - 2, 70_000, -1], device="cuda")
+    z = (h.float() @ w.float().t()).double()
+    lp = torch.log_softmax(z, 1)
+    got = binding.solon_head_logprobs(h, w, t)
+    assert float((got.logp[:5].double() - lp[torch.arange(5), t[:5]]).abs().max()) <= 1e-4
+    grad = torch.full((parts * n,), -1.0, device="cuda")
+    dw = torch.full((parts, vocab * cols), 9.0, dtype=torch.bfloat16, device="cuda")
+    binding.solon_head_logprobs_backward(h, w, t, got.peak, got.log_sum, grad, partitions=parts, hidden_grad=False, dweight=dw)
+    dz = lp.exp()
+    dz[torch.arange(5), t[:5]] -= 1.0
+    dz[5] = 0.0
+    for k in range(parts):
+        at = torch.tensor([0, 5, 65_535, 65_536, 70_000, vocab - 2, vocab - 1], device="cuda")
+        want = dz[k * n:(k + 1) * n, at].t() @ h[k * n:(k + 1) * n].double()
+        size = dz[k * n:(k + 1) * n, at].abs().t() @ h[k * n:(k + 1) * n].double().abs()
+        # half a bfloat16 step of each dlogit and of the result, and a logit's 1e-4 in p
+        assert ((dw[k].view(vocab, cols)[at].double() - want).abs() <= (2.0 ** -8 + 2e-4) * size + 2.0 ** -8 * want.abs()).all()
+        assert float((dw[k] == 9.0).float().mean()) < 1e-3
+
+
 def test_refusals():
     h, w = torch.zeros((4, 8), device="cuda"), torch.zeros((10, 8), device="cuda")
     t = torch.zeros(4, dtype=torch.int64, device="cuda")
