@@ -963,12 +963,13 @@ static int64_t rows_padded(int64_t cols) { return up(cols, 256); }
 static HeadPlan head_forward_plan(int64_t rows, int64_t cols, int64_t vocab, int dtype, bool aligned) {
   HeadPlan p = {};
   // W has to be read once and is all there is to read.  Up to 4 rows multiply-adds keep up with that, at any type and alignment; up to 32 float32 rows they cost
-  // less than bringing W into two pieces first (65536 x 2048: 16 rows 446 us in pieces).
+  // less than bringing W into two pieces first (65536 x 2048: 16 rows 446 us in pieces), except over a small vocabulary (9 rows of 2307 over 1702 tokens:
+  // 190 us, seven tiles one behind the other).
   if (rows <= 4 && (dtype == SOLON_F32 || !aligned)) {
     const int nr = rows == 3 ? 4 : (int)rows;
     if (nr * rows_padded(cols) * 4 <= kHeadSharedRows) p.row_kernel = nr;
   }
-  if (!p.row_kernel && dtype == SOLON_F32 && rows <= kSmallForward) p.small = small_rows(rows);
+  if (!p.row_kernel && dtype == SOLON_F32 && rows <= kSmallForward && vocab >= kSmallVocab) p.small = small_rows(rows);
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
     const int64_t here = at;
@@ -1039,7 +1040,7 @@ static HeadPlan head_backward_plan(int64_t rows, int64_t cols, int64_t vocab, in
     at += up(bytes, 256);
     return here;
   };
-  if (dtype == SOLON_F32 && rows <= kSmallBackward) {      // (13 rows of 3456 over 37760 tokens: 755 us in pieces)
+  if (dtype == SOLON_F32 && rows <= kSmallBackward && vocab >= kSmallVocab) {      // (13 rows of 3456 over 37760 tokens: 755 us in pieces)
     p.small = small_rows(rows);
     p.h_splits = small_splits(cols, vocab);
     p.turned = take(up(cols, 32) * p.small * 4);

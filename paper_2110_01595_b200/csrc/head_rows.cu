@@ -5,7 +5,7 @@
 // less than that.  Bound: reading W (and writing dW), or 2 (4) rows multiply-adds an element at 36 T/s.
 //
 // Logits: a CTA takes a tile of 128 or 256 tokens and brings 32 columns at a time into shared memory, two stages (three of 16 columns: 15 to 50 % slower); a lane owns two tokens (rows 36 floats
-// apart, so that its 16-byte reads meet no bank twice) against all rows, whose elements are broadcast.  Sums of 32 products are added to another.
+// apart, so that its 16-byte reads meet no bank twice) against all rows, whose elements are broadcast.  Sums of 16 products are added to another.
 // Backward: dz of all tokens lies in memory (vocab x rows, small); one kernel then reads W's rows once more, adds dz W to dh in registers and writes dz^T h:
 // a thread has four columns, and a CTA a share of the tokens, whose dh a further kernel adds up.
 
@@ -22,7 +22,9 @@ constexpr int kColumns = 32;             // of a stage
 constexpr int kStride = 36;              // floats between the tokens of a stage
 constexpr int kStages = 2;
 constexpr int kShareTokens = 32;         // of dz at a time
-constexpr int kSmallThreads = 128;
+constexpr int kSmallThreads = 128;       // that share a stage's tokens
+constexpr int kHalves = 2;               // sets of threads that share its columns, so that there are warps enough to hide what each waits for
+constexpr int kCtaThreads = kHalves * kSmallThreads;
 
 constexpr int kTokens = 2;               // of a lane
 constexpr int kTokenTile = kSmallThreads * kTokens;
@@ -44,11 +46,11 @@ __global__ void __launch_bounds__(256) small_turn_kernel(const float* hidden, in
 
 // BACKWARD: dz instead of statistics.  WIDE: W's rows begin at multiples of 16 bytes.
 template <int NR, bool BACKWARD, bool WIDE>
-__global__ void __launch_bounds__(kSmallThreads) small_logits_kernel(HeadSmallArgs a) {
+__global__ void __launch_bounds__(kCtaThreads, NR <= 16 ? 2 : 1) small_logits_kernel(HeadSmallArgs a) {
   constexpr int kT = kTokens, kTile = kTokenTile;
   extern __shared__ __align__(16) char small_smem[];
   SmallStage<NR>* stages = reinterpret_cast<SmallStage<NR>*>(small_smem);
-  const int t = threadIdx.x;
+  const int t = threadIdx.x % kSmallThreads, half = threadIdx.x / kSmallThreads;
   const int64_t v0 = (int64_t)blockIdx.x * kTile;
   const int here = (int)min((int64_t)kTile, a.vocab - v0);
   const float* w = a.weight + v0 * a.weight_pitch;
@@ -59,7 +61,7 @@ __global__ void __launch_bounds__(kSmallThreads) small_logits_kernel(HeadSmallAr
     const int64_t k0 = (int64_t)step * kColumns;
     if (WIDE) {
 #pragma unroll 8
-      for (int i = t; i < kTile * (kColumns / 4); i += kSmallThreads) {
+      for (int i = threadIdx.x; i < kTile * (kColumns / 4); i += kCtaThreads) {
         const int r = i / (kColumns / 4), c = i % (kColumns / 4) * 4;
         const int64_t left = a.cols - (k0 + c);      // (a group that reaches over the row's end is brought element by element)
         float* to = s.w + r * kStride + c;
@@ -71,13 +73,13 @@ __global__ void __launch_bounds__(kSmallThreads) small_logits_kernel(HeadSmallAr
       }
     } else {
 #pragma unroll 8
-      for (int i = t; i < kTile * kColumns; i += kSmallThreads) {
+      for (int i = threadIdx.x; i < kTile * kColumns; i += kCtaThreads) {
         const int r = i / kColumns, c = i % kColumns;
         const bool inside = k0 + c < a.cols;
         copy_async<4>(s.w + r * kStride + c, inside ? w + min(r, here - 1) * a.weight_pitch + k0 + c : w, inside);
       }
     }
-    for (int i = t; i < kColumns * NR / 4; i += kSmallThreads) copy16_async(s.h + 4 * i, a.turned + k0 * NR + 4 * i);
+    for (int i = threadIdx.x; i < kColumns * NR / 4; i += kCtaThreads) copy16_async(s.h + 4 * i, a.turned + k0 * NR + 4 * i);
     copies_commit();
   };
 
@@ -103,7 +105,7 @@ __global__ void __launch_bounds__(kSmallThreads) small_logits_kernel(HeadSmallAr
 #pragma unroll
       for (int n = 0; n < NR / 2; n++) sum[r][n] = pack2(0.0f, 0.0f);
 #pragma unroll 2
-    for (int k = 0; k < kColumns; k += 4) {
+    for (int k = half * (kColumns / kHalves); k < (half + 1) * (kColumns / kHalves); k += 4) {
       Pack<float, 4> x[kT];
 #pragma unroll
       for (int r = 0; r < kT; r++) x[r] = load_pack<float, 4>(s.w + (t + r * kSmallThreads) * kStride + k);
@@ -128,12 +130,33 @@ __global__ void __launch_bounds__(kSmallThreads) small_logits_kernel(HeadSmallAr
 #pragma unroll
       for (int n = 0; n < NR / 2; n++) z[r][n] = add2(z[r][n], sum[r][n]);
   }
+  // the halves' sums
   __syncthreads();
+  float* other = reinterpret_cast<float*>(small_smem);
+  if (half)
+#pragma unroll
+    for (int r = 0; r < kT; r++)
+#pragma unroll
+      for (int n = 0; n < NR / 2; n++) {
+        float x, y;
+        unpack2(z[r][n], x, y);
+        other[(t + r * kSmallThreads) * (NR + 1) + 2 * n] = x;
+        other[(t + r * kSmallThreads) * (NR + 1) + 2 * n + 1] = y;
+      }
+  __syncthreads();
+  if (!half)
+#pragma unroll
+    for (int r = 0; r < kT; r++)
+#pragma unroll
+      for (int n = 0; n < NR / 2; n++) {
+        const float* p = other + (t + r * kSmallThreads) * (NR + 1) + 2 * n;
+        z[r][n] = add2(z[r][n], pack2(p[0], p[1]));
+      }
 
   if constexpr (BACKWARD) {
     __shared__ float of_row[6][NR];                  // peak, log_sum, g, g_H, entropy, whether the row has a share
     __shared__ int64_t target[NR];
-    if (t < NR) {
+    if (!half && t < NR) {
       const bool there = t < a.rows;
       const int64_t to = there && a.targets ? a.targets[t] : -1;
       const float g = there && a.grad_logp && to >= 0 ? a.grad_logp[t] : 0.0f, gh = there && a.grad_entropy ? a.grad_entropy[t] : 0.0f;
@@ -146,6 +169,7 @@ __global__ void __launch_bounds__(kSmallThreads) small_logits_kernel(HeadSmallAr
       target[t] = to;
     }
     __syncthreads();
+    if (half) return;
 #pragma unroll
     for (int r = 0; r < kT; r++) {
       const int64_t v = v0 + t + r * kSmallThreads;
@@ -168,9 +192,10 @@ __global__ void __launch_bounds__(kSmallThreads) small_logits_kernel(HeadSmallAr
     }
   } else {
     // tokens by rows in shared memory, then a thread takes a row's share of the tile
-    constexpr int kSegments = kSmallThreads / NR, kShare = kTile / kSegments;
+    constexpr int kSegments = kCtaThreads / NR, kShare = kTile / kSegments;
     __shared__ RowSums part[kSegments][NR];
-    float* turned = reinterpret_cast<float*>(small_smem);
+    float* turned = other;                   // (every thread its own places)
+    if (!half)
 #pragma unroll
     for (int r = 0; r < kT; r++)
 #pragma unroll
@@ -181,7 +206,7 @@ __global__ void __launch_bounds__(kSmallThreads) small_logits_kernel(HeadSmallAr
         turned[(t + r * kSmallThreads) * (NR + 1) + n + 1] = y;
       }
     __syncthreads();
-    const int n = t % NR, first = t / NR * kShare, last = min(first + kShare, here);
+    const int n = threadIdx.x % NR, segment = threadIdx.x / NR, first = segment * kShare, last = min(first + kShare, here);
     RowSums sums = {-INFINITY, 0.0f, 0.0f};
     if (n < a.rows) {
       float m = -INFINITY;
@@ -196,9 +221,9 @@ __global__ void __launch_bounds__(kSmallThreads) small_logits_kernel(HeadSmallAr
       const int64_t to = a.targets ? a.targets[n] - v0 : -1;
       if (to >= first && to < last) a.target_logit[n] = turned[to * (NR + 1) + n];
     }
-    part[t / NR][n] = sums;
+    part[segment][n] = sums;
     __syncthreads();
-    if (t < a.rows) {
+    if (!half && t < a.rows) {
       RowSums all = part[0][t];
       for (int i = 1; i < kSegments; i++) all = join(all, part[i][t]);
       float* p = a.partial + (int64_t)blockIdx.x * 3 * a.rows + t;
@@ -349,10 +374,10 @@ static int small_logits(const HeadSmallArgs& a, cudaStream_t stream) {
   constexpr int kTurned = kTokenTile * (NR + 1) * 4, bytes = std::max<int>(kStages * sizeof(SmallStage<NR>), kTurned);
   if (!(((uintptr_t)a.weight | (uintptr_t)(a.weight_pitch * 4)) & 15)) {
     SOLON_SHARED_MEMORY_ONCE((small_logits_kernel<NR, BACKWARD, true>), bytes);
-    small_logits_kernel<NR, BACKWARD, true><<<tiles, kSmallThreads, bytes, stream>>>(a);
+    small_logits_kernel<NR, BACKWARD, true><<<tiles, kCtaThreads, bytes, stream>>>(a);
   } else {
     SOLON_SHARED_MEMORY_ONCE((small_logits_kernel<NR, BACKWARD, false>), bytes);
-    small_logits_kernel<NR, BACKWARD, false><<<tiles, kSmallThreads, bytes, stream>>>(a);
+    small_logits_kernel<NR, BACKWARD, false><<<tiles, kCtaThreads, bytes, stream>>>(a);
   }
   SOLON_CUDA_TRY(cudaGetLastError());
   return SOLON_OK;

@@ -25,6 +25,7 @@ struct HeadSmallArgs {
 };
 
 constexpr int kSmallForward = 32, kSmallBackward = 16;      // rows that the kernels take
+constexpr int kSmallVocab = 74 * 256;                       // tokens that they are for: fewer tiles than half the SMs are gone through too slowly
 
 int small_rows(int64_t rows);                                // the number of rows that their kernels are built for: 8, 16 or 32
 int64_t small_tile();                                        // tokens of a tile of the logits

@@ -106,7 +106,8 @@ def _check_forward(h, w, t, got):
 
 
 SHAPES = [(1, 1, 1), (1, 64, 3), (2, 7, 50), (3, 100, 257), (5, 2048, 1000), (8, 333, 5001), (9, 64, 256), (13, 40, 300), (16, 1001, 700), (17, 24, 1025), (1, 9000, 333),
-          (16, 9000, 70), (128, 128, 512), (129, 72, 513), (256, 256, 256), (257, 520, 1111), (600, 1001, 2003), (2050, 64, 3000), (40, 4096, 5000), (1, 512, 131_072), (300, 48, 50_001)]
+          (16, 9000, 70), (128, 128, 512), (129, 72, 513), (256, 256, 256), (257, 520, 1111), (600, 1001, 2003), (2050, 64, 3000), (40, 4096, 5000), (1, 512, 131_072), (300, 48, 50_001),
+          (5, 40, 19_001), (8, 520, 18_944), (9, 2049, 19_000), (16, 333, 20_003), (23, 100, 19_500), (32, 65, 30_000)]
 
 
 @pytest.mark.parametrize("rows,cols,vocab", SHAPES)
@@ -184,7 +185,7 @@ def _stats(h, w):
 
 # rows of a partition, partitions, columns, vocabulary
 BACK = [(1, 1, 1, 1), (1, 3, 8, 40), (4, 2, 24, 130), (64, 5, 333, 700), (63, 3, 64, 257), (65, 2, 128, 256), (200, 1, 129, 1000), (300, 2, 520, 999), (1, 7, 1000, 300), (2000, 1, 72, 511),
-        (512, 1, 1024, 512), (130, 1, 40, 20_000)]
+        (512, 1, 1024, 512), (130, 1, 40, 20_000), (1, 1, 520, 19_000), (4, 4, 72, 19_003), (16, 1, 333, 19_100), (1, 7, 1001, 19_001), (2, 3, 40, 20_000)]
 
 
 @pytest.mark.parametrize("n,parts,cols,vocab", BACK)
