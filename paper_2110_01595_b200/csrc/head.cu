@@ -964,7 +964,7 @@ static HeadPlan head_forward_plan(int64_t rows, int64_t cols, int64_t vocab, int
   HeadPlan p = {};
   // W has to be read once and is all there is to read.  Up to 4 rows multiply-adds keep up with that, at any type and alignment; up to 32 float32 rows they cost
   // less than bringing W into two pieces first (65536 x 2048: 16 rows 446 us in pieces), except over a small vocabulary (9 rows of 2307 over 1702 tokens:
-  // 190 us, seven tiles one behind the other).
+  // 190 us, seven tiles on seven SMs).
   if (rows <= 4 && (dtype == SOLON_F32 || !aligned)) {
     const int nr = rows == 3 ? 4 : (int)rows;
     if (nr * rows_padded(cols) * 4 <= kHeadSharedRows) p.row_kernel = nr;
