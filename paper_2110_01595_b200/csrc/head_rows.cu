@@ -5,7 +5,7 @@
 // less than that.  Bound: reading W (and writing dW), or 2 (4) rows multiply-adds an element at 36 T/s.
 //
 // Logits: a CTA takes a tile of 256 tokens and brings 32 columns at a time into shared memory, two stages (three of 16 columns: 15 to 50 % slower).  Two
-// sets of 128 threads share a stage's columns, so that more warps hide what each waits for (13 rows of 3456 over 37760 tokens: 213 us with one set, 168 with
+// sets of 128 threads share a stage's columns, so that more warps hide what each waits for (13 rows of 3456 over 37760 tokens: 213 us with one set, 168 to 176 with
 // two).  A lane owns two tokens (rows 36 floats apart, so that its 16-byte reads meet no bank twice) against all rows, whose elements are broadcast.  Sums of
 // 16 products are added to another.  A tile is gone through by one CTA from first to last column, so vocabularies of fewer tiles than half the SMs (below
 // 18,944 tokens) take the pieces instead (9 rows of 2307 over 1702 tokens: 190 us here, 60 in pieces).
