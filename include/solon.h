@@ -405,9 +405,9 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
  *   peak, log_sum, entropy, grad_logp, grad_entropy  as in solon_token_logprobs_backward
  *   workspace  device, 256-byte aligned, solon_head_logprobs_backward_workspace(...) bytes: dlogits of one piece of the vocabulary (at most
  *              512 MB, or 256 tokens), sums of dhidden
- * dlogits is rounded to 16 bits where the result is (dhidden of 16-bit types, bfloat16 gradients), and held in two float16 pieces (2^-22 of each value)
- * for float32 and float64 gradients, where bfloat16 states count as float16 times a power of two (exact down to 2^-28 of their largest).  rows = 0: dweight becomes 0.  hidden has to be finite in rows that count in no gradient,
- * too: they are multiplied by zeros. */
+ * dlogits is held in float16 times a power of two: one piece (11 bits) for dhidden of bfloat16 states and for bfloat16 gradients, two (22 bits) for dhidden of
+ * float16 and float32 states and for float32 and float64 gradients.  bfloat16 states and weights count as float16 times a power of two in the two products (exact
+ * down to 2^-28 of their largest).  rows = 0: dweight becomes 0.  hidden has to be finite in rows that count in no gradient, too: they are multiplied by zeros. */
 int64_t solon_head_logprobs_backward_workspace(int64_t rows, int64_t cols, int64_t vocab, int partitions, int dtype, int grad_dtype, int aligned);
 int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const void* weight, int64_t weight_pitch, int dtype, const int64_t* targets,
                                  int64_t rows, int64_t cols, int64_t vocab, int partitions, const float* peak, const float* log_sum, const float* entropy,

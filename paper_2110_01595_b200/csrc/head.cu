@@ -10,11 +10,10 @@
 //   float32            two float16 pieces, x = 2^-s (hi + lo), s such that the largest of the tensor lies in [2^14, 2^15): the pieces hold 22 bits of
 //                      values down to 2^-28 of the largest, and an absolute 2^-40 of it below.  A product is three: hi lo + lo hi + hi hi; the lo lo
 //                      left out is below 2^-22 of the term.  (Three bfloat16 pieces would take six products.)
-//   dz                 one piece where what it is multiplied into is rounded to 16 bits anyway (dh of 16-bit states, bfloat16 gradients: as much rounding
-//                      again, 2^-8 or 2^-11 of each term at most, of independent signs; bfloat16 gradients of float32 states take the first piece of
-//                      the states alone, too), two float16 pieces for float32 and float64 gradients (2^-22 of each term; bfloat16 states are taken as
-//                      float16 by a power of two for that product, exactly down to 2^-28 of the largest).  float16 pieces of dz carry the power of two of
-//                      the largest |g| + |g_H| (H + 1).
+//   dz                 float16 by the power of two of the largest |g| + |g_H| (H + 1), of any states (bfloat16 states and weights are taken as float16 by a power
+//                      of two for these products: eight bits of dz would put as much into a result again as its own rounding to bfloat16 does; with eleven, an
+//                      eighth of that).  One piece for dh of bfloat16 states and for bfloat16 gradients (those of float32 states take the first piece of
+//                      the states alone, too), two for dh of float16 and float32 states and for float32 and float64 gradients.
 //
 // Measured (us; of 1662 TFLOP/s in bursts, 1407 sustained): 8192 x 2048 states, 32768 tokens, bfloat16: forward 790 (1.39 PFLOP/s), backward with bfloat16
 // gradients 2345 (1.41); a library's plain products of these sizes take 660 to 730 each.  What the product is fed by and how it ends is what that came from: one
@@ -89,7 +88,7 @@ struct HeadArgs {
   int64_t first, vocab;
   // kDz
   int dz_pitch;                          // this piece's tokens, zeros behind them up to a multiple of 64
-  int pieces;                            // of dz (3: kMixed)
+  int form;                              // what is stored of dz (DzForm)
   // kDhidden, kDweight
   float* sums;                           // slabs x m x sums_pitch: where the result goes in float32 instead of to the output, if store_sums
   int64_t sums_pitch;
@@ -160,51 +159,48 @@ struct DzRow {
   float peak, log_sum, entropy, g, gh;
 };
 
-// What is stored of dz: its type's nearest; with what that leaves as a second piece; or, for bfloat16 states and float32 gradients, the nearest bfloat16 (for dh) and
-// two float16 pieces (for dW).
-enum DzForm { kNearest, kPair, kMixed };
+// What is stored of dz: the nearest float16; or that and what it leaves as a second float16.
+enum DzForm { kNearest, kPair };
 
-template <typename T>
 struct DzOut {
   const CUtensorMap* map;
   char* stage;                           // two blocks of 32 rows x 128 bytes
   int col, row, columns, lane;           // first column and row of the warp, columns that there are
   int place;                             // of the row's target (-1: not here) and its element
   float target;
-  float grow;                            // kMixed: the power of two of the float16 pieces
 };
 
-// 64 elements of a row as 16-bit words to a block, and the target's.  Leaves what the words leave of the elements, where LEAVE.
-template <bool LEAVE, typename T>
-__device__ __forceinline__ void dz_block(float* v, float& target, uint32_t keep, float grow, int place, int lane, char* block) {
-  using Word = Word16<T>;
+// 64 elements of a row as float16 to a block, and the target's.  Leaves what they leave of the elements, where LEAVE.
+template <bool LEAVE>
+__device__ __forceinline__ void dz_block(float* v, float& target, uint32_t keep, int place, int lane, char* block) {
+  using Word = Word16<__half>;
 #pragma unroll
   for (int i = 0; i < 8; i++) {
     uint32_t w[4];
 #pragma unroll
     for (int j = 0; j < 4; j++) {
       float &x = v[8 * i + 2 * j], &y = v[8 * i + 2 * j + 1];
-      w[j] = Word::join(x * grow, y * grow) & keep;
+      w[j] = Word::join(x, y) & keep;
       if (LEAVE) {
         float wx, wy;
         Word::pair(w[j], wx, wy);
-        x = fmaf(x, grow, -wx), y = fmaf(y, grow, -wy);
+        x -= wx, y -= wy;
       }
     }
     reinterpret_cast<uint4*>(block)[lane * 8 + (i ^ (lane & 7))] = make_uint4(w[0], w[1], w[2], w[3]);
   }
   if (place >= 0 && place < 64) {
-    const T nearest = from_float<T>(target * grow);
-    reinterpret_cast<T*>(block)[(lane * 8 + ((place / 8) ^ (lane & 7))) * 8 + place % 8] = nearest;
-    if (LEAVE) target = fmaf(target, grow, -to_float(nearest));
+    const __half nearest = __float2half_rn(target);
+    reinterpret_cast<__half*>(block)[(lane * 8 + ((place / 8) ^ (lane & 7))) * 8 + place % 8] = nearest;
+    if (LEAVE) target -= __half2float(nearest);
   }
 }
 
 // -p (g + g_H (log p + H)) of N tokens of a row, from their logits, in blocks of 64 tokens that are
 // copied from shared memory (rows of their own are 32-byte writes, which go out at a third of the rate).  `keep` 0: zeros.
 // The forms are functions of their own so that no branch stands between the elements: with branches an element's chain of operations has nothing beside it.
-template <bool ENTROPY, DzForm FORM, int N, typename T>
-__device__ __forceinline__ void dz_row(const DzRow& r, float (&v)[N], uint32_t keep, const DzOut<T>& out, int& turn) {
+template <bool ENTROPY, DzForm FORM, int N>
+__device__ __forceinline__ void dz_row(const DzRow& r, float (&v)[N], uint32_t keep, const DzOut& out, int& turn) {
   Float2 mp = pack2(-r.peak, -r.peak);
   const Float2 ml = pack2(-r.log_sum, -r.log_sum), ml2 = pack2(-r.log_sum * kLog2e, -r.log_sum * kLog2e), l2e = pack2(kLog2e, kLog2e);
   const Float2 mg = pack2(-r.g, -r.g), mh = pack2(-r.gh, -r.gh), h2 = pack2(r.entropy, r.entropy);
@@ -240,21 +236,11 @@ __device__ __forceinline__ void dz_row(const DzRow& r, float (&v)[N], uint32_t k
       }
       turn ^= 1;
     };
-    if constexpr (FORM == kNearest) {
-      dz_block<false, T>(v + c, target, keep, 1.0f, out.place - c, out.lane, free_block());
-      give(0);
-    } else if constexpr (FORM == kPair) {
-      dz_block<true, T>(v + c, target, keep, 1.0f, out.place - c, out.lane, free_block());
-      give(0);
-      dz_block<false, T>(v + c, target, keep, 1.0f, out.place - c, out.lane, free_block());
+    dz_block<FORM == kPair>(v + c, target, keep, out.place - c, out.lane, free_block());
+    give(0);
+    if constexpr (FORM == kPair) {
+      dz_block<false>(v + c, target, keep, out.place - c, out.lane, free_block());
       give(1);
-    } else {
-      dz_block<false, T>(v + c, target, keep, 1.0f, out.place - c, out.lane, free_block());
-      give(0);
-      dz_block<true, __half>(v + c, target, keep, out.grow, out.place - c, out.lane, free_block());
-      give(1);
-      dz_block<false, __half>(v + c, target, keep, 1.0f, out.place - c, out.lane, free_block());
-      give(2);
     }
   }
 }
@@ -465,7 +451,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
         if ((half ^= 1) == 0) sum_phase ^= 1;
       }
       if (absent) continue;
-      if (MODE == kDz ? a.scaled & 3 : a.scaled) {
+      if (a.scaled) {
 #pragma unroll
         for (int i = 0; i < kHalf; i++) v[i] = v[i] * undo[0] * undo[1];
       }
@@ -526,8 +512,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
           rows_so_far[c / 32] = join(rows_so_far[c / 32], sums);
         }
       } else if constexpr (MODE == kDz) {
-        using T16 = typename std::conditional<BF16, __nv_bfloat16, __half>::type;
-        const float power = a.scaled & 4 ? power_of_two(scale_exponent(a.words->dz)) : 1.0f, grow = a.pieces == 3 ? 1.0f : power;
+        const float grow = power_of_two(scale_exponent(a.words->dz));
         copies_wait<0>();
         const int64_t target = a.targets && row < a.m ? of_targets[lane] : -1;
         DzRow r = {of_rows[lane], of_rows[32 + lane], a.grad_entropy ? of_rows[96 + lane] : 0.0f, a.grad_logp && target >= 0 ? of_rows[64 + lane] : 0.0f,
@@ -554,15 +539,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
           d = active ? fmaf(exp2_fast(lp * kLog2e), fmaf(-r.gh, lp + r.entropy, -r.g), r.g) : 0.0f;
         }
         const int place = hit ? (int)token : -1;
-        const DzOut<T16> out = {&maps.out, stage, col, row0, a.dz_pitch - col, lane, place, d, power};
+        const DzOut out = {&maps.out, stage, col, row0, a.dz_pitch - col, lane, place, d};
         if (a.grad_entropy) {
-          if (a.pieces == 1) dz_row<true, kNearest>(r, v, keep, out, turn);
-          else if (a.pieces == 2) dz_row<true, kPair>(r, v, keep, out, turn);
-          else if (BF16) dz_row<true, kMixed>(r, v, keep, out, turn);
+          if (a.form == kNearest) dz_row<true, kNearest>(r, v, keep, out, turn);
+          else dz_row<true, kPair>(r, v, keep, out, turn);
         } else {
-          if (a.pieces == 1) dz_row<false, kNearest>(r, v, keep, out, turn);
-          else if (a.pieces == 2) dz_row<false, kPair>(r, v, keep, out, turn);
-          else if (BF16) dz_row<false, kMixed>(r, v, keep, out, turn);
+          if (a.form == kNearest) dz_row<false, kNearest>(r, v, keep, out, turn);
+          else dz_row<false, kPair>(r, v, keep, out, turn);
         }
       } else {
         // (the sums' pitch is a multiple of 128: room for all columns of a warp that has any)
@@ -791,7 +774,7 @@ __global__ void __launch_bounds__(256) head_join_kernel(HeadJoinArgs a) {
 
 struct HeadScanArgs {
   const float *hidden, *weight;          // NULL: not wanted
-  const __nv_bfloat16* hidden16;         // the same
+  const __nv_bfloat16 *hidden16, *weight16;      // the same
   int64_t hidden_pitch, weight_pitch, rows, cols, vocab;
   const float *grad_logp, *grad_entropy, *entropy;
   int dz;
@@ -814,11 +797,24 @@ __global__ void __launch_bounds__(256) head_scan_kernel(HeadScanArgs a) {
     word = &a.words->dz;
     for (int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x; r < a.rows; r += (int64_t)gridDim.x * 256)
       see((a.grad_logp ? fabsf(a.grad_logp[r]) : 0.0f) + (a.grad_entropy ? fabsf(a.grad_entropy[r]) * (fabsf(a.entropy[r]) + 1.0f) : 0.0f));
-  } else if (blockIdx.y == 0 && a.hidden16) {
-    word = &a.words->hidden;
-    for (int64_t r = (int64_t)blockIdx.x * 8 + warp; r < a.rows; r += (int64_t)gridDim.x * 8)
+  } else if (blockIdx.y ? a.weight16 : a.hidden16) {
+    const __nv_bfloat16* m = blockIdx.y ? a.weight16 : a.hidden16;
+    const int64_t rows = blockIdx.y ? a.vocab : a.rows, pitch = blockIdx.y ? a.weight_pitch : a.hidden_pitch;
+    word = blockIdx.y ? &a.words->weight : &a.words->hidden;
+    const bool wide = !(((uintptr_t)m | (uintptr_t)(pitch * 2)) & 15);
+    for (int64_t r = (int64_t)blockIdx.x * 8 + warp; r < rows; r += (int64_t)gridDim.x * 8) {
+      const __nv_bfloat16* p = m + r * pitch;
+      const int64_t done = wide ? a.cols / 8 * 8 : 0;
+#pragma unroll 4
+      for (int64_t c = lane * 8; c < done; c += 256) {
+        float x[8];
+        Word16<__nv_bfloat16>::unpack(load16_once(p + c), x);
+#pragma unroll
+        for (int e = 0; e < 8; e++) see(x[e]);
+      }
 #pragma unroll 8
-      for (int64_t c = lane; c < a.cols; c += 32) see(__bfloat162float(a.hidden16[r * a.hidden_pitch + c]));
+      for (int64_t c = done + lane; c < a.cols; c += 32) see(__bfloat162float(p[c]));
+    }
   } else {
     const float* m = blockIdx.y ? a.weight : a.hidden;
     if (!m) return;
@@ -867,7 +863,7 @@ __global__ void __launch_bounds__(256) head_split_kernel(const T* x, int64_t pit
   float scale = 1.0f;
   constexpr bool kToHalf = std::is_same<T, __nv_bfloat16>::value;
   if constexpr (sizeof(T) == 4 || kToHalf) scale = power_of_two(scale_exponent(*largest));
-  const bool wide = sizeof(T) == 4 && !(((uintptr_t)x | (uintptr_t)(pitch * 4)) & 15);
+  const bool wide = !(((uintptr_t)x | (uintptr_t)(pitch * sizeof(T))) & 15);
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * words; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / words, c = (i - r * words) * 8;
     const T* p = x + r * pitch + c;
@@ -891,10 +887,14 @@ __global__ void __launch_bounds__(256) head_split_kernel(const T* x, int64_t pit
       store_pack((__half*)out + r * out_pitch + c, hi);
       store_pack((__half*)out + (rows + r) * out_pitch + c, lo);
     } else if constexpr (kToHalf) {
-      Pack<__half, 8> v;
+      float v[8];
+      if (wide && c + 8 <= cols) Word16<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4*>(p), v);
+      else
 #pragma unroll
-      for (int e = 0; e < 8; e++) v.e[e] = __float2half_rn(c + e < cols ? __bfloat162float(p[e]) * scale : 0.0f);
-      store_pack((__half*)out + r * out_pitch + c, v);
+        for (int e = 0; e < 8; e++) v[e] = c + e < cols ? __bfloat162float(p[e]) : 0.0f;
+#pragma unroll
+      for (int e = 0; e < 8; e++) v[e] *= scale;
+      *reinterpret_cast<uint4*>(out + r * out_pitch + c) = Word16<__half>::pack(v);
     } else {
       Pack<uint16_t, 8> v;
 #pragma unroll
@@ -949,7 +949,7 @@ struct HeadPlan {
   int dz_pieces;
   int64_t width;                         // tokens of a piece of the vocabulary
   int h_splits, w_splits;                // parts of the inner dimensions of dh and dW
-  int64_t words, partial, target_logit, hidden, weight, hidden16, dz, sums, w_sums, total;
+  int64_t words, partial, target_logit, hidden, weight, hidden16, weight16, dz, sums, w_sums, total;
 };
 
 constexpr int64_t kHeadSharedRows = 200 * 1024;       // bytes of hidden rows that the kernel for few rows holds
@@ -1026,12 +1026,15 @@ static int head_splits(int64_t slabs, int64_t m, int64_t n, int64_t k, int produ
   return best;
 }
 
+// Pairs of pieces that dh is the sum of: float32 states have two of dz and of W, float16 ones two of dz, bfloat16 ones one of each.
+static int dh_products(int dtype) { return dtype == SOLON_F32 ? 3 : dtype == SOLON_F16 ? 2 : 1; }
+
 static HeadPlan head_backward_plan(int64_t rows, int64_t cols, int64_t vocab, int partitions, int dtype, int grad_dtype, bool aligned) {
   HeadPlan p = {};
   p.pieces = dtype == SOLON_F32 ? 2 : 1;
   p.split = dtype == SOLON_F32 || !aligned;
   p.pitch = up(cols, kBlock);
-  p.dz_pieces = dtype == SOLON_F32 ? 2 : grad_dtype == SOLON_BF16 ? 1 : dtype == SOLON_BF16 ? 3 : 2;
+  p.dz_pieces = dtype == SOLON_BF16 && grad_dtype == SOLON_BF16 ? 1 : 2;
   p.width = std::max<int64_t>(kTile, kDzBytes / (rows * 2 * p.dz_pieces) / kTile * kTile);
   p.width = std::min(up(vocab, 64), up((vocab + (vocab + p.width - 1) / p.width - 1) / ((vocab + p.width - 1) / p.width), kTile));     // pieces of one size
   int64_t at = 0;
@@ -1050,14 +1053,17 @@ static HeadPlan head_backward_plan(int64_t rows, int64_t cols, int64_t vocab, in
     return p;
   }
   const int times = (int)((vocab + p.width - 1) / p.width);
-  p.h_splits = head_splits(1, rows, cols, std::min(vocab, p.width), dtype == SOLON_F32 ? 3 : 1, times);
+  p.h_splits = head_splits(1, rows, cols, std::min(vocab, p.width), dh_products(dtype), times);
   p.w_splits = head_splits(partitions, std::min(vocab, p.width), cols, rows / partitions, grad_dtype == SOLON_BF16 ? 1 : p.pieces + 1, 1);
   p.words = take(sizeof(HeadWords));
   if (p.split) {
     p.hidden = take(p.pieces * rows * p.pitch * 2);
     p.weight = take(p.pieces * vocab * p.pitch * 2);
   }
-  if (p.dz_pieces == 3) p.hidden16 = take(rows * p.pitch * 2);
+  if (dtype == SOLON_BF16) {
+    p.hidden16 = take(rows * p.pitch * 2);
+    p.weight16 = take(vocab * p.pitch * 2);
+  }
   p.dz = take(p.dz_pieces * rows * p.width * 2);
   if (times > 1 || p.h_splits > 1) p.sums = take(p.h_splits * rows * up(cols, 128) * 4);
   if (p.w_splits > 1) p.w_sums = take((int64_t)p.w_splits * partitions * std::min(vocab, p.width) * up(cols, 128) * 4);
@@ -1148,7 +1154,7 @@ static int head_operand(const void* x, int64_t pitch, int64_t rows, int64_t cols
 }
 
 static int head_scan(const HeadScanArgs& a, int sms, cudaStream_t stream) {
-  if (!a.hidden && !a.hidden16 && !a.weight && !a.dz) return SOLON_OK;
+  if (!a.hidden && !a.hidden16 && !a.weight && !a.weight16 && !a.dz) return SOLON_OK;
   head_scan_kernel<<<dim3(4 * sms, 3), 256, 0, stream>>>(a);
   SOLON_CUDA_TRY(cudaGetLastError());
   return SOLON_OK;
@@ -1187,13 +1193,16 @@ static int head_stats(const HeadMaps& maps, const HeadArgs& a, bool few, bool bf
   return head_product_launch<kStats, 256, false, float>(maps, a, sms, stream);
 }
 
-template <bool BF16, typename H>
-static int head_backward_piece(int which, const HeadMaps& maps, const HeadArgs& a, int grad_dtype, int sms, cudaStream_t stream) {
-  if (which == kDz) return head_product_launch<kDz, 256, BF16, float>(maps, a, sms, stream);
-  if (which == kDhidden) return head_product<kDhidden, BF16, H>(maps, a, sms, stream);
-  if (grad_dtype == SOLON_F32) return head_product<kDweight, BF16, float>(maps, a, sms, stream);
-  if (grad_dtype == SOLON_F64) return head_product<kDweight, BF16, double>(maps, a, sms, stream);
-  return head_product<kDweight, BF16, __nv_bfloat16>(maps, a, sms, stream);
+// dh and dW are products of float16 pieces, whatever the states' type.
+static int head_dhidden(const HeadMaps& maps, const HeadArgs& a, int dtype, int sms, cudaStream_t stream) {
+  if (dtype == SOLON_F32) return head_product<kDhidden, false, float>(maps, a, sms, stream);
+  if (dtype == SOLON_BF16) return head_product<kDhidden, false, __nv_bfloat16>(maps, a, sms, stream);
+  return head_product<kDhidden, false, __half>(maps, a, sms, stream);
+}
+static int head_dweight(const HeadMaps& maps, const HeadArgs& a, int grad_dtype, int sms, cudaStream_t stream) {
+  if (grad_dtype == SOLON_F32) return head_product<kDweight, false, float>(maps, a, sms, stream);
+  if (grad_dtype == SOLON_F64) return head_product<kDweight, false, double>(maps, a, sms, stream);
+  return head_product<kDweight, false, __nv_bfloat16>(maps, a, sms, stream);
 }
 
 }  // namespace solon
@@ -1248,7 +1257,7 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
   } else {
     if (dtype == SOLON_F32) {
       SOLON_CUDA_TRY(cudaMemsetAsync(words, 0, sizeof(HeadWords), stream));
-      const HeadScanArgs scan = {(const float*)hidden, (const float*)weight, nullptr, hidden_pitch, weight_pitch, rows, cols, vocab, nullptr, nullptr, nullptr, 0, words};
+      const HeadScanArgs scan = {(const float*)hidden, (const float*)weight, nullptr, nullptr, hidden_pitch, weight_pitch, rows, cols, vocab, nullptr, nullptr, nullptr, 0, words};
       if ((rc = head_scan(scan, sms, stream))) return rc;
     }
     HeadOperand h, w;
@@ -1346,10 +1355,13 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
     if ((rc = small_backward(a, stream)) || !dhidden) return rc;
     return head_finish({a.sums, a.sums_pitch, rows, cols, rows > 1 ? dhidden_pitch : cols, 0, 1, plan.h_splits, dhidden}, dtype, sms, stream);
   }
-  const bool mixed = plan.dz_pieces == 3 && dweight;
-  if (!bf16 || mixed) SOLON_CUDA_TRY(cudaMemsetAsync(words, 0, sizeof(HeadWords), stream));
-  const HeadScanArgs scan = {f32 ? (const float*)hidden : nullptr, f32 ? (const float*)weight : nullptr, mixed ? (const __nv_bfloat16*)hidden : nullptr,
-                             hidden_pitch, weight_pitch, rows, cols, vocab, grad_logp, grad_entropy, entropy, !bf16 || mixed, words};
+  const bool coarse = grad_dtype == SOLON_BF16;          // dW from the first pieces alone
+  const int form = (dhidden && !bf16) || (dweight && !coarse) ? kPair : kNearest, dz_pieces = form == kPair ? 2 : 1;
+  const bool hidden16 = bf16 && dweight, weight16 = bf16 && dhidden;
+  SOLON_CUDA_TRY(cudaMemsetAsync(words, 0, sizeof(HeadWords), stream));
+  const HeadScanArgs scan = {f32 ? (const float*)hidden : nullptr, f32 ? (const float*)weight : nullptr, hidden16 ? (const __nv_bfloat16*)hidden : nullptr,
+                             weight16 ? (const __nv_bfloat16*)weight : nullptr, hidden_pitch, weight_pitch, rows, cols, vocab, grad_logp, grad_entropy, entropy,
+                             1, words};
   if ((rc = head_scan(scan, sms, stream))) return rc;
   HeadOperand h, w;
   if ((rc = head_operand(hidden, hidden_pitch, rows, cols, dtype, plan, ws + plan.hidden, &words->hidden, sms, stream, &h))) return rc;
@@ -1358,26 +1370,23 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
   const int64_t n = rows / partitions, sums_pitch = up(cols, 128);
   // as rows along the inner dimension: h and W for the logits, dz for dh; across it: W for dh, dz and h for dW
   CUtensorMap map_h, map_w, map_w_across, map_h_across, map_dz, map_dz_across, map_dz_out;
-  // (a map across the inner dimension goes with the tiles: copies of 128 columns need 128 of them in a CTA's tile, and whole blocks of 64 in memory)
-  const bool whole = cols % kBlock == 0 || plan.split;
-  auto across = [&](CUtensorMap* map, const void* p, int64_t rows, int64_t slabs, int64_t pitch, int64_t slab, bool narrow) {
-    return whole && !narrow ? tensor_map_by_blocks(map, p, bf16, cols, rows, slabs, pitch, slab) : tensor_map(map, p, bf16, cols, rows, slabs, pitch, slab, kBlock);
-  };
-  const bool coarse = grad_dtype == SOLON_BF16;
-  const bool w_narrow = narrow(cols, (n + kBlock - 1) / kBlock * (coarse ? 1 : h.pieces + 1));
-  HeadOperand hw = h;                      // as it goes into dW
-  if (mixed) {
+  HeadOperand hw = h, wh = w;              // as they go into dW and dh: bfloat16 as float16 by a power of two
+  auto as_half = [&](const void* x, int64_t pitch, int64_t rows, int64_t to, const unsigned* largest, HeadOperand* out) {
     const int64_t items = rows * (plan.pitch / 8);
-    if ((rc = launch_dependent(head_split_kernel<__nv_bfloat16>, dim3((unsigned)std::min<int64_t>((items + 255) / 256, 16 * sms)), dim3(256), 0, stream,
-                               (const __nv_bfloat16*)hidden, hidden_pitch, rows, cols, (uint16_t*)(ws + plan.hidden16), plan.pitch,
-                               (const unsigned*)&words->hidden)))
-      return rc;
-    hw = {ws + plan.hidden16, plan.pitch, rows, 1};
-  }
-  const bool hw_whole = whole || mixed;
+    *out = {ws + to, plan.pitch, rows, 1};
+    return launch_dependent(head_split_kernel<__nv_bfloat16>, dim3((unsigned)std::min<int64_t>((items + 255) / 256, 16 * sms)), dim3(256), 0, stream,
+                            (const __nv_bfloat16*)x, pitch, rows, cols, (uint16_t*)(ws + to), plan.pitch, largest);
+  };
+  if (hidden16 && (rc = as_half(hidden, hidden_pitch, rows, plan.hidden16, &words->hidden, &hw))) return rc;
+  if (weight16 && (rc = as_half(weight, weight_pitch, vocab, plan.weight16, &words->weight, &wh))) return rc;
+  // (a map across the inner dimension goes with the tiles: copies of 128 columns need 128 of them in a CTA's tile, and whole blocks of 64 in memory)
+  const bool whole = cols % kBlock == 0 || plan.split, hw_whole = whole || hidden16, wh_whole = whole || weight16;
+  auto across = [&](CUtensorMap* map, const void* p, bool by_blocks, int64_t rows, int64_t slabs, int64_t pitch, int64_t slab) {
+    return by_blocks ? tensor_map_by_blocks(map, p, false, cols, rows, slabs, pitch, slab) : tensor_map(map, p, false, cols, rows, slabs, pitch, slab, kBlock);
+  };
+  const bool w_narrow = narrow(cols, (n + kBlock - 1) / kBlock * (coarse ? 1 : hw.pieces + 1));
   if (!tensor_map(&map_h, h.p, bf16, cols, rows, h.pieces, h.pitch, rows * h.pitch, kRows) ||
-      !(hw_whole && !w_narrow ? tensor_map_by_blocks(&map_h_across, hw.p, bf16 && !mixed, cols, n, (int64_t)hw.pieces * partitions, hw.pitch, n * hw.pitch)
-                              : tensor_map(&map_h_across, hw.p, bf16 && !mixed, cols, n, (int64_t)hw.pieces * partitions, hw.pitch, n * hw.pitch, kBlock)))
+      !across(&map_h_across, hw.p, hw_whole && !w_narrow, n, (int64_t)hw.pieces * partitions, hw.pitch, n * hw.pitch))
     return SOLON_ERR_CUDA;
   HeadArgs base = {};
   base.slabs = base.splits = 1;
@@ -1389,23 +1398,14 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
   base.grad_logp = grad_logp;
   base.grad_entropy = grad_entropy;
   base.vocab = vocab;
-  const int dz_scaled = bf16 ? 0 : 4;
-  const int dz_pieces = plan.dz_pieces == 3 && !mixed ? 1 : plan.dz_pieces;
-  auto run = [&](int which, const HeadMaps& maps, const HeadArgs& a) {
-    if (f32) return head_backward_piece<false, float>(which, maps, a, grad_dtype, sms, stream);
-    if (bf16) return head_backward_piece<true, __nv_bfloat16>(which, maps, a, grad_dtype, sms, stream);
-    return head_backward_piece<false, __half>(which, maps, a, grad_dtype, sms, stream);
-  };
   for (int64_t first = 0; first < vocab; first += plan.width) {
     const int64_t width = std::min(plan.width, vocab - first), pitch = up(width, kBlock);
-    const char* w_piece = w.p + first * w.pitch * 2;
-    const bool h_narrow = narrow(cols, pitch / kBlock * (f32 ? 3 : 1));
-    const char* dz_across = ws + plan.dz + (mixed ? rows * pitch * 2 : 0);      // (the float16 pieces)
-    if (!tensor_map(&map_dz, ws + plan.dz, bf16, pitch, rows, mixed ? 1 : dz_pieces, pitch, rows * pitch, kRows) ||
-        !tensor_map(&map_dz_out, ws + plan.dz, bf16, pitch, rows, dz_pieces, pitch, rows * pitch, 32) ||
-        !tensor_map_by_blocks(&map_dz_across, dz_across, bf16 && !mixed, pitch, n, (int64_t)(mixed ? 2 : dz_pieces) * partitions, pitch, n * pitch) ||
-        !tensor_map(&map_w, w_piece, bf16, cols, width, w.pieces, w.pitch, vocab * w.pitch, kRows) ||
-        !across(&map_w_across, w_piece, width, w.pieces, w.pitch, vocab * w.pitch, h_narrow))
+    const bool h_narrow = narrow(cols, pitch / kBlock * dh_products(dtype));
+    if (!tensor_map(&map_dz, ws + plan.dz, false, pitch, rows, dz_pieces, pitch, rows * pitch, kRows) ||
+        !tensor_map(&map_dz_out, ws + plan.dz, false, pitch, rows, dz_pieces, pitch, rows * pitch, 32) ||
+        !tensor_map_by_blocks(&map_dz_across, ws + plan.dz, false, pitch, n, (int64_t)dz_pieces * partitions, pitch, n * pitch) ||
+        !tensor_map(&map_w, w.p + first * w.pitch * 2, bf16, cols, width, w.pieces, w.pitch, vocab * w.pitch, kRows) ||
+        !across(&map_w_across, wh.p + first * wh.pitch * 2, wh_whole && !h_narrow, width, wh.pieces, wh.pitch, vocab * wh.pitch))
       return SOLON_ERR_CUDA;
     HeadArgs a = base;
     a.m = (int)rows;
@@ -1413,20 +1413,22 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
     a.first = first;
     a.k_blocks = (int)((cols + kBlock - 1) / kBlock);
     head_pairs(a, h.pieces, w.pieces, 1, 1);
-    a.scaled = (f32 ? 3 : 0) | (mixed ? 4 : dz_scaled);
-    a.pieces = dz_pieces;
+    a.scaled = f32 ? 3 : 0;
+    a.form = form;
     a.dz_pitch = (int)pitch;
-    if ((rc = run(kDz, {map_h, map_w, map_dz_out}, a))) return rc;
+    if ((rc = bf16 ? head_product_launch<kDz, 256, true, float>({map_h, map_w, map_dz_out}, a, sms, stream)
+                   : head_product_launch<kDz, 256, false, float>({map_h, map_w, map_dz_out}, a, sms, stream)))
+      return rc;
     if (dhidden) {
       a = base;
       a.m = (int)rows;
       a.n = (int)cols;
       a.slabs = a.splits = plan.h_splits;
       a.narrow = h_narrow;
-      a.b_by_blocks = whole && !h_narrow;
+      a.b_by_blocks = wh_whole && !h_narrow;
       a.k_blocks = (int)((pitch / kBlock + a.splits - 1) / a.splits);
-      head_pairs(a, f32 ? 2 : 1, w.pieces, 1, 1);
-      a.scaled = (f32 ? 2 : 0) | dz_scaled;
+      head_pairs(a, bf16 ? 1 : 2, wh.pieces, 1, 1);
+      a.scaled = (f32 || bf16 ? 2 : 0) | 4;
       a.sums = (float*)(ws + plan.sums);
       a.sums_pitch = sums_pitch;
       a.load_sums = first > 0;
@@ -1435,7 +1437,7 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
       a.out = dhidden;
       a.out_pitch = rows > 1 ? dhidden_pitch : cols;
       a.out_wide = !(((uintptr_t)dhidden | (uintptr_t)(a.out_pitch * element_size(dtype))) & 31);
-      if ((rc = run(kDhidden, {map_dz, map_w_across, {}}, a))) return rc;
+      if ((rc = head_dhidden({map_dz, map_w_across, {}}, a, dtype, sms, stream))) return rc;
       if (last && a.splits > 1 &&
           (rc = head_finish({a.sums, sums_pitch, rows, cols, a.out_pitch, 0, 1, a.splits, dhidden}, dtype, sms, stream)))
         return rc;
@@ -1453,8 +1455,8 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
       a.sums = (float*)(ws + plan.w_sums);
       a.sums_pitch = sums_pitch;
       a.store_sums = a.splits > 1;
-      head_pairs(a, coarse ? 1 : 2, coarse ? 1 : h.pieces, partitions, partitions);
-      a.scaled = mixed ? 5 : (f32 ? 1 : 0) | dz_scaled;
+      head_pairs(a, coarse ? 1 : 2, coarse ? 1 : hw.pieces, partitions, partitions);
+      a.scaled = (f32 || bf16 ? 1 : 0) | 4;
       a.out = (char*)dweight + first * cols * grad_size;
       a.out_pitch = cols;
       a.out_slab = partitions > 1 ? grad_pitch : 0;
@@ -1463,7 +1465,7 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
       a.out_by_map = !(((uintptr_t)a.out | (uintptr_t)(cols * grad_size) | (uintptr_t)(a.out_slab * grad_size)) & 15);
       if (a.out_by_map && !output_map(&maps.out, a.out, (int)grad_size, cols, width, partitions, cols, partitions > 1 ? a.out_slab : up(width * cols, 8)))
         return SOLON_ERR_CUDA;
-      if ((rc = mixed ? head_backward_piece<false, __half>(kDweight, maps, a, grad_dtype, sms, stream) : run(kDweight, maps, a))) return rc;
+      if ((rc = head_dweight(maps, a, grad_dtype, sms, stream))) return rc;
       if (a.splits > 1 && (rc = head_finish({a.sums, sums_pitch, width, cols, cols, a.out_slab, partitions, a.splits, a.out}, grad_dtype, sms, stream))) return rc;
     }
   }

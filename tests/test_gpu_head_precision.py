@@ -1,0 +1,104 @@
+"""What the head's results may be off by, element by element, where 16-bit results, ranges of magnitudes and neighbouring rows test it.
+
+Tolerances as in test_gpu_head.py (u = 2^-24, s_iv = sum_c |h_ic w_vc|, a logit's z_tol, the gradient's dz_tol from it), with what dlogits and float32 elements are held in:
+one float16 piece is off by half a step, 2^-11 of a value, two by half a step of what the first leaves, 2^-22."""
+
+import pytest
+import torch
+
+from paper_2110_01595_b200 import binding, build
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16, "f64": torch.float64}
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    build.build()
+
+
+def _gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def _leaning(rows, cols, vocab, dtype, seed, lean=6.0):
+    """Hidden states that lean to their targets, more or less so: of some rows a few tokens carry dlogits."""
+    g = _gen(seed)
+    w = torch.randn((vocab, cols), device="cuda", generator=g) * (1.5 * cols ** -0.5)
+    t = torch.randint(0, vocab, (rows,), device="cuda", generator=g)
+    h = torch.randn((rows, cols), device="cuda", generator=g) + w[t] * (torch.rand((rows, 1), device="cuda", generator=g) * lean)
+    return h.to(TYPES[dtype]), w.to(TYPES[dtype]), t
+
+
+def _size(x):
+    return x.double().abs().clamp(min=2.0 ** -14) if x.dtype == torch.float16 else x.double().abs()
+
+
+def _logits(h, w):
+    z, s = h.double() @ w.double().t(), _size(h) @ _size(w).t()
+    return z, (64 + h.shape[1] / 256 + h.shape[1] / 32 + 8) * U * s + (2.0 ** -20 * s if h.dtype == torch.float32 else 0.0)
+
+
+def _stats(h, w):
+    z = h.double() @ w.double().t()
+    big = z.amax(1)
+    lp = torch.log_softmax(z, 1)
+    return big.float(), (torch.logsumexp(z, 1) - big).float(), (-torch.special.xlogy(lp.exp(), lp.exp()).sum(1)).float()
+
+
+def _dlogits(h, w, t, peak, log_sum, g, entropy=None, gh=None):
+    """dlogits and what they may be off by before any rounding to pieces."""
+    z, zt = _logits(h, w)
+    lp = z - peak.double()[:, None] - log_sum.double()[:, None]
+    p = lp.exp()
+    ga = torch.where(t >= 0, g.double(), 0.0)
+    gha = torch.zeros_like(ga) if gh is None else gh.double()
+    ent = torch.zeros_like(ga) if gh is None else entropy.double()
+    inner = ga[:, None] + gha[:, None] * (lp + ent[:, None])
+    dz = (-p * inner).scatter_add(1, t.clamp(min=0)[:, None], ga[:, None])
+    r = (4 * lp.abs() + 8) * U + zt
+    tol = p * inner.abs() * (r + 4 * U) + p * gha.abs()[:, None] * (zt + 4 * U * (lp.abs() + ent.abs()[:, None])) + 2 * U * dz.abs()
+    return dz, tol * 1.01 + 2.0 ** -125 * (ga.abs() + gha.abs())[:, None]
+
+
+def _close(x, y, tol, what):
+    x = x.double()
+    off = (x - y).abs()
+    bad = ~((x == y) | (off <= tol))
+    assert not bad.any(), (what, int(bad.sum()), float((off / tol.clamp(min=1e-300))[bad].max()), x[bad][:4], y[bad][:4])
+
+
+@pytest.mark.parametrize("dtype,grad", [("bf16", "f32"), ("bf16", "bf16"), ("f16", "f32"), ("f16", "bf16"), ("f32", "bf16")])
+@pytest.mark.parametrize("rows,parts,cols,vocab", [(300, 2, 128, 400), (2, 1, 72, 1000), (1000, 1, 333, 517)])
+def test_sixteen_bit_results_are_off_by_little_more_than_their_own_rounding(rows, parts, cols, vocab, dtype, grad):
+    """Half a step of the result, and what dlogits are held in: one float16 piece for dh of bfloat16 states and for bfloat16 gradients (2^-11 of a term, and as
+    much again for float32 states, of which these take one piece too), two elsewhere (2^-22); 2^-39 of the largest for what float16 does not reach, of dlogits and of
+    bfloat16 states and weights as float16."""
+    n = rows // parts
+    for entropies in (False, True):
+        h, w, t = _leaning(rows, cols, vocab, dtype, rows + cols)
+        t[::7] = -1
+        peak, log_sum, entropy = _stats(h, w)
+        g = -torch.rand(rows, device="cuda", generator=_gen(1)) / n
+        gh = torch.randn(rows, device="cuda", generator=_gen(2)) / (4 * n) if entropies else None
+        dw = torch.empty((parts, vocab * cols), dtype=TYPES[grad], device="cuda")
+        dh, _ = binding.solon_head_logprobs_backward(h, w, t, peak, log_sum, g, entropy, gh, partitions=parts, dweight=dw)
+        dz, dzt = _dlogits(h, w, t, peak, log_sum, g, entropy, gh)
+        bound = float((g.abs() + (gh.abs() * (entropy + 1) if entropies else 0.0)).max())
+
+        def check(result, a, atol, factor, held, inner, what):
+            b = factor.double()
+            x, size = a @ b, a.abs() @ b.abs()
+            c = 1040 + inner / 4096 if result.element_size() == 2 else 64 + inner / 256
+            tol = atol @ b.abs() + held * size + c * U * (a.abs() @ _size(factor)) + 2.0 ** -39 * (bound * b.abs().sum(0) + b.abs().max() * a.abs().sum(1)[:, None])
+            tol = tol + torch.finfo(result.dtype).eps / 2 * x.abs() + (2.0 ** -25 if result.dtype == torch.float16 else 0.0)
+            _close(result, x, tol, what)
+
+        pair = 2.0 ** -22 if dtype != "f32" else 2.0 ** -20
+        check(dh, dz, dzt, w, 2.0 ** -11 if dtype == "bf16" else pair, vocab, "dhidden")
+        one = 2.0 ** -11 if dtype != "f32" else 2.0 ** -10
+        for k in range(parts):
+            q = slice(k * n, (k + 1) * n)
+            check(dw[k].view(vocab, cols), dz[q].t(), dzt[q].t(), h[q], one if grad == "bf16" else pair, n, f"dweight {k}")
