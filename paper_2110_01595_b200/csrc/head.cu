@@ -1062,7 +1062,7 @@ static HeadPlan head_backward_plan(int64_t rows, int64_t cols, int64_t vocab, in
   }
   if (dtype == SOLON_BF16) {
     p.hidden16 = take(rows * p.pitch * 2);
-    p.weight16 = take(vocab * p.pitch * 2);
+    p.weight16 = take(p.width * p.pitch * 2);       // of one piece of the vocabulary
   }
   p.dz = take(p.dz_pieces * rows * p.width * 2);
   if (times > 1 || p.h_splits > 1) p.sums = take(p.h_splits * rows * up(cols, 128) * 4);
@@ -1378,7 +1378,6 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
                             (const __nv_bfloat16*)x, pitch, rows, cols, (uint16_t*)(ws + to), plan.pitch, largest);
   };
   if (hidden16 && (rc = as_half(hidden, hidden_pitch, rows, plan.hidden16, &words->hidden, &hw))) return rc;
-  if (weight16 && (rc = as_half(weight, weight_pitch, vocab, plan.weight16, &words->weight, &wh))) return rc;
   // (a map across the inner dimension goes with the tiles: copies of 128 columns need 128 of them in a CTA's tile, and whole blocks of 64 in memory)
   const bool whole = cols % kBlock == 0 || plan.split, hw_whole = whole || hidden16, wh_whole = whole || weight16;
   auto across = [&](CUtensorMap* map, const void* p, bool by_blocks, int64_t rows, int64_t slabs, int64_t pitch, int64_t slab) {
@@ -1401,11 +1400,13 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
   for (int64_t first = 0; first < vocab; first += plan.width) {
     const int64_t width = std::min(plan.width, vocab - first), pitch = up(width, kBlock);
     const bool h_narrow = narrow(cols, pitch / kBlock * dh_products(dtype));
+    if (weight16 && (rc = as_half((const __nv_bfloat16*)weight + first * weight_pitch, weight_pitch, width, plan.weight16, &words->weight, &wh))) return rc;
+    const char* w_across = wh.p + (weight16 ? 0 : first * wh.pitch * 2);
     if (!tensor_map(&map_dz, ws + plan.dz, false, pitch, rows, dz_pieces, pitch, rows * pitch, kRows) ||
         !tensor_map(&map_dz_out, ws + plan.dz, false, pitch, rows, dz_pieces, pitch, rows * pitch, 32) ||
         !tensor_map_by_blocks(&map_dz_across, ws + plan.dz, false, pitch, n, (int64_t)dz_pieces * partitions, pitch, n * pitch) ||
         !tensor_map(&map_w, w.p + first * w.pitch * 2, bf16, cols, width, w.pieces, w.pitch, vocab * w.pitch, kRows) ||
-        !across(&map_w_across, wh.p + first * wh.pitch * 2, wh_whole && !h_narrow, width, wh.pieces, wh.pitch, vocab * wh.pitch))
+        !across(&map_w_across, w_across, wh_whole && !h_narrow, width, wh.pieces, wh.pitch, wh.rows * wh.pitch))
       return SOLON_ERR_CUDA;
     HeadArgs a = base;
     a.m = (int)rows;
