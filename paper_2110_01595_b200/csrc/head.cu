@@ -776,12 +776,14 @@ struct HeadScanArgs {
   const float *hidden, *weight;          // NULL: not wanted
   const __nv_bfloat16 *hidden16, *weight16;      // the same
   int64_t hidden_pitch, weight_pitch, rows, cols, vocab;
-  const float *grad_logp, *grad_entropy, *entropy;
+  const int64_t* targets;
+  const float *peak, *grad_logp, *grad_entropy, *entropy;
   int dz;
   HeadWords* words;
 };
 
-// Largest finite magnitudes: of the hidden states, the output matrix, and a bound of each row's dz, |g| + |g_H| (H + 1).
+// Largest finite magnitudes: of the hidden states, the output matrix, and a bound of each row's dz, |g| + |g_H| (H + 1), where g counts only with a target and
+// a row of which nothing is left has no share: what padding holds says nothing about the others.
 __global__ void __launch_bounds__(256) head_scan_kernel(HeadScanArgs a) {
   __shared__ unsigned most[8];
   pdl_trigger();
@@ -796,7 +798,8 @@ __global__ void __launch_bounds__(256) head_scan_kernel(HeadScanArgs a) {
     if (!a.dz) return;
     word = &a.words->dz;
     for (int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x; r < a.rows; r += (int64_t)gridDim.x * 256)
-      see((a.grad_logp ? fabsf(a.grad_logp[r]) : 0.0f) + (a.grad_entropy ? fabsf(a.grad_entropy[r]) * (fabsf(a.entropy[r]) + 1.0f) : 0.0f));
+      if (a.peak[r] != -INFINITY)
+        see((a.grad_logp && a.targets[r] >= 0 ? fabsf(a.grad_logp[r]) : 0.0f) + (a.grad_entropy ? fabsf(a.grad_entropy[r]) * (fabsf(a.entropy[r]) + 1.0f) : 0.0f));
   } else if (blockIdx.y ? a.weight16 : a.hidden16) {
     const __nv_bfloat16* m = blockIdx.y ? a.weight16 : a.hidden16;
     const int64_t rows = blockIdx.y ? a.vocab : a.rows, pitch = blockIdx.y ? a.weight_pitch : a.hidden_pitch;
@@ -1257,7 +1260,7 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
   } else {
     if (dtype == SOLON_F32) {
       SOLON_CUDA_TRY(cudaMemsetAsync(words, 0, sizeof(HeadWords), stream));
-      const HeadScanArgs scan = {(const float*)hidden, (const float*)weight, nullptr, nullptr, hidden_pitch, weight_pitch, rows, cols, vocab, nullptr, nullptr, nullptr, 0, words};
+      const HeadScanArgs scan = {(const float*)hidden, (const float*)weight, nullptr, nullptr, hidden_pitch, weight_pitch, rows, cols, vocab, nullptr, nullptr, nullptr, nullptr, nullptr, 0, words};
       if ((rc = head_scan(scan, sms, stream))) return rc;
     }
     HeadOperand h, w;
@@ -1360,8 +1363,8 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
   const bool hidden16 = bf16 && dweight, weight16 = bf16 && dhidden;
   SOLON_CUDA_TRY(cudaMemsetAsync(words, 0, sizeof(HeadWords), stream));
   const HeadScanArgs scan = {f32 ? (const float*)hidden : nullptr, f32 ? (const float*)weight : nullptr, hidden16 ? (const __nv_bfloat16*)hidden : nullptr,
-                             weight16 ? (const __nv_bfloat16*)weight : nullptr, hidden_pitch, weight_pitch, rows, cols, vocab, grad_logp, grad_entropy, entropy,
-                             1, words};
+                             weight16 ? (const __nv_bfloat16*)weight : nullptr, hidden_pitch, weight_pitch, rows, cols, vocab, targets, peak, grad_logp,
+                             grad_entropy, entropy, 1, words};
   if ((rc = head_scan(scan, sms, stream))) return rc;
   HeadOperand h, w;
   if ((rc = head_operand(hidden, hidden_pitch, rows, cols, dtype, plan, ws + plan.hidden, &words->hidden, sms, stream, &h))) return rc;

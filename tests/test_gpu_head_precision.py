@@ -102,3 +102,29 @@ def test_sixteen_bit_results_are_off_by_little_more_than_their_own_rounding(rows
         for k in range(parts):
             q = slice(k * n, (k + 1) * n)
             check(dw[k].view(vocab, cols), dz[q].t(), dzt[q].t(), h[q], one if grad == "bf16" else pair, n, f"dweight {k}")
+
+
+@pytest.mark.parametrize("dtype,grad", [("f32", "f32"), ("f32", "bf16"), ("f16", "f32"), ("bf16", "f32"), ("bf16", "f64"), ("bf16", "bf16")])
+@pytest.mark.parametrize("rows", [8, 300])
+def test_rows_without_a_share_say_nothing_about_the_others(rows, dtype, grad):
+    """What stands in grad_logp of a row without target, or in either factor of a row of which nothing is left, counts nowhere: the same bits as with zeros there."""
+    cols, vocab, parts = 72, 19_000 if rows == 8 else 700, 2
+    h, w, t = _leaning(rows, cols, vocab, dtype, 3)
+    t[1::5] = -1
+    peak, log_sum, entropy = _stats(h, w)
+    peak[2::9] = -INF
+    g, gh = -torch.rand(rows, device="cuda", generator=_gen(1)), torch.randn(rows, device="cuda", generator=_gen(2)) / 8
+    g[1::5], g[2::9], gh[2::9] = 0.0, 0.0, 0.0
+
+    def call():
+        dw = torch.empty((parts, vocab * cols), dtype=TYPES[grad], device="cuda")
+        return binding.solon_head_logprobs_backward(h, w, t, peak, log_sum, g, entropy, gh, partitions=parts, dweight=dw)
+
+    want = call()
+    assert float(want[0].abs().max()) > 0
+    g[1::5], g[2::9], gh[2::9] = 1e12, -3e20, 1e30
+    got = call()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    g[1::5], g[2::9], gh[2::9] = NAN, INF, NAN
+    got = call()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
