@@ -391,7 +391,7 @@ int solon_embedding_backward(const void* dy, int64_t dy_pitch, int dtype, const 
  *   workspace  device, 256-byte aligned, solon_head_logprobs_workspace(...) bytes; `aligned`: 1 if both matrices' first elements and row
  *              pitches are multiples of 16 bytes (other rows are copied to such a pitch first).  Its contents need not survive the call
  * Products of the elements as they are, summed in float32 (float16 elements below 2^-14 with the precision of 2^-14); float32 elements are taken as two float16 pieces of 22 bits together (values
- * below 2^-28 of their tensor's largest: an absolute 2^-40 of it), or multiplied as they are where rows are few (up to 16).
+ * below 2^-28 of their tensor's largest: an absolute 2^-50 of it), or multiplied as they are where rows are few (up to 16).
  * Infinite and NaN elements reach the rows that their products enter; in two pieces infinity counts as NaN.  cols <= SOLON_MAX_WIDTH. */
 int64_t solon_head_logprobs_workspace(int64_t rows, int64_t cols, int64_t vocab, int dtype, int aligned);
 int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* weight, int64_t weight_pitch, int dtype, const int64_t* targets, int64_t rows,
@@ -405,8 +405,9 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
  *   peak, log_sum, entropy, grad_logp, grad_entropy  as in solon_token_logprobs_backward
  *   workspace  device, 256-byte aligned, solon_head_logprobs_backward_workspace(...) bytes: dlogits of one piece of the vocabulary (at most
  *              512 MB, or 256 tokens), sums of dhidden
- * dlogits is held in float16 times a power of two: one piece (11 bits) for dhidden of bfloat16 states and for bfloat16 gradients, two (22 bits) for dhidden of
- * float16 and float32 states and for float32 and float64 gradients.  bfloat16 states and weights count as float16 times a power of two in the two products (exact
+ * dlogits is held in float16 times a power of two: one piece (11 bits; values below 2^-28 of the call's largest |grad_logp| + |grad_entropy| (entropy + 1): an absolute
+ * 2^-40 of it) for dhidden of bfloat16 states and for bfloat16 gradients, two (22 bits; 2^-50) for dhidden of float16 and float32 states and for float32 and float64
+ * gradients.  bfloat16 states and weights count as float16 times a power of two in the two products (exact
  * down to 2^-28 of their largest).  rows = 0: dweight becomes 0.  hidden has to be finite in rows that count in no gradient, too: they are multiplied by zeros. */
 int64_t solon_head_logprobs_backward_workspace(int64_t rows, int64_t cols, int64_t vocab, int partitions, int dtype, int grad_dtype, int aligned);
 int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const void* weight, int64_t weight_pitch, int dtype, const int64_t* targets,

@@ -7,13 +7,15 @@
 //
 // All three products run on the tensor cores (tensor_tiles.cuh).  What is multiplied is 16 bits wide:
 //   bfloat16, float16  the elements themselves; sums float32.  (Rows off 16-byte boundaries are copied to a pitch that the copies can take.)
-//   float32            two float16 pieces, x = 2^-s (hi + lo), s such that the largest of the tensor lies in [2^14, 2^15): the pieces hold 22 bits of
-//                      values down to 2^-28 of the largest, and an absolute 2^-40 of it below.  A product is three: hi lo + lo hi + hi hi; the lo lo
-//                      left out is below 2^-22 of the term.  (Three bfloat16 pieces would take six products.)
+//   float32            two float16 pieces, x = 2^-s (hi + 2^-11 lo), s such that the largest of the tensor lies in [2^14, 2^15): the pieces hold 22 bits of
+//                      values down to 2^-28 of the largest, and an absolute 2^-50 of it below.  (With lo not multiplied the 22 bits ended at 2^-17: a float16's steps
+//                      end at 2^-24.)  A product is three: hi lo + lo hi, whose sum is taken times 2^-11 in registers, then hi hi; the lo lo left out is below
+//                      2^-22 of the term.  (Three bfloat16 pieces would take six products.)
 //   dz                 float16 by the power of two of the largest |g| + |g_H| (H + 1), of any states (bfloat16 states and weights are taken as float16 by a power
 //                      of two for these products: eight bits of dz would put as much into a result again as its own rounding to bfloat16 does; with eleven, an
 //                      eighth of that).  One piece for dh of bfloat16 states and for bfloat16 gradients (those of float32 states take the first piece of
-//                      the states alone, too), two for dh of float16 and float32 states and for float32 and float64 gradients.
+//                      the states alone, too): 11 bits of what lies above 2^-28 of the largest, an absolute 2^-40 of it below.  Two, the second times 2^11 as above,
+//                      for dh of float16 and float32 states and for float32 and float64 gradients: 22 bits, and 2^-50.
 //
 // Measured (us; of 1662 TFLOP/s in bursts, 1407 sustained): 8192 x 2048 states, 32768 tokens, bfloat16: forward 790 (1.39 PFLOP/s), backward with bfloat16
 // gradients 2345 (1.41); a library's plain products of these sizes take 660 to 730 each.  What the product is fed by and how it ends is what that came from: one
@@ -56,6 +58,7 @@ struct HeadWords {
 __device__ __forceinline__ int scale_exponent(unsigned largest) {       // 2^s brings the largest magnitude into [2^14, 2^15)
   return largest ? min(126, 14 - ilogbf(__uint_as_float(largest))) : 0;
 }
+constexpr float kSecond = 2048.0f;       // what a second piece is multiplied by: at most 2^3 is left of elements below 2^15, and 2^-25 of those below 2^-14
 __device__ __forceinline__ float power_of_two(int s) { return __int_as_float((s + 127) << 23); }       // -126 <= s <= 127
 
 // ------------------------------------------------------------------------------------------------------------ arguments
@@ -70,6 +73,7 @@ struct HeadArgs {
   uint32_t per_slab_inverse, band_inverse;             // reciprocals for the tiles' numbers
   int k_blocks, products;
   int chunk;                             // blocks of 64 that are summed in tensor memory before the sum is added to the one in registers
+  int low;                               // blocks of the products with a second piece, which come first: their sum is taken times 2^-11 before the others join it
   int piece_a[3], piece_b[3];            // third coordinate of the tensor maps for slab 0; slab s is s further
   int slab_a, slab_b;                    // 1: the operand has slabs
   int splits;                            // the inner dimension is cut into so many parts of k_blocks, slabs of their own; what lies behind its end is zeros
@@ -159,7 +163,7 @@ struct DzRow {
   float peak, log_sum, entropy, g, gh;
 };
 
-// What is stored of dz: the nearest float16; or that and what it leaves as a second float16.
+// What is stored of dz: the nearest float16; or that and what it leaves, times kSecond, as a second float16.
 enum DzForm { kNearest, kPair };
 
 struct DzOut {
@@ -170,7 +174,7 @@ struct DzOut {
   float target;
 };
 
-// 64 elements of a row as float16 to a block, and the target's.  Leaves what they leave of the elements, where LEAVE.
+// 64 elements of a row as float16 to a block, and the target's.  Leaves what they leave of the elements, as the second piece has it, where LEAVE.
 template <bool LEAVE>
 __device__ __forceinline__ void dz_block(float* v, float& target, uint32_t keep, int place, int lane, char* block) {
   using Word = Word16<__half>;
@@ -184,7 +188,7 @@ __device__ __forceinline__ void dz_block(float* v, float& target, uint32_t keep,
       if (LEAVE) {
         float wx, wy;
         Word::pair(w[j], wx, wy);
-        x -= wx, y -= wy;
+        x = (x - wx) * kSecond, y = (y - wy) * kSecond;
       }
     }
     reinterpret_cast<uint4*>(block)[lane * 8 + (i ^ (lane & 7))] = make_uint4(w[0], w[1], w[2], w[3]);
@@ -192,7 +196,7 @@ __device__ __forceinline__ void dz_block(float* v, float& target, uint32_t keep,
   if (place >= 0 && place < 64) {
     const __half nearest = __float2half_rn(target);
     reinterpret_cast<__half*>(block)[(lane * 8 + ((place / 8) ^ (lane & 7))) * 8 + place % 8] = nearest;
-    if (LEAVE) target -= __half2float(nearest);
+    if (LEAVE) target = (target - __half2float(nearest)) * kSecond;
   }
 }
 
@@ -264,6 +268,9 @@ __device__ __forceinline__ TileAt tile_at(const HeadArgs& a, uint32_t t, int bn)
   const uint32_t high = min(8u, a.m_tiles - group * 8), column = high == 8 ? in >> 3 : in / high;
   return {(int)slab, (int)((group * 8 + in - column * high) * kTile), (int)column * bn};
 }
+
+// Where the blocks end that are summed in tensor memory together with block kb.
+__device__ __forceinline__ int chunk_end(const HeadArgs& a, int kb, int blocks) { return min(kb < a.low ? a.low : blocks, kb + a.chunk); }
 
 // stages of A and B blocks, then the epilogue warps' staging, then barriers
 template <int MODE, int BN>
@@ -364,7 +371,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
         for (int kb = 0; kb < blocks;) {
           if (!waited(sum_empty + half, sum_phase ^ 1, abort_flag, status)) goto products_done;
           fence_after();
-          const int first = kb, end = min(blocks, kb + a.chunk);
+          const int first = kb, end = chunk_end(a, kb, blocks);
           for (; kb < end; kb++) {
             if (!waited(full + s, phase, abort_flag, status)) goto products_done;
             fence_after();
@@ -428,7 +435,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
       float v[kHalf];
 #pragma unroll
       for (int i = 0; i < kHalf; i++) v[i] = 0.0f;
-      for (int kb = 0; kb < blocks; kb += a.chunk) {
+      for (int kb = 0; kb < blocks; kb = chunk_end(a, kb, blocks)) {
+        const float so_far = kb && kb == a.low ? 1.0f / kSecond : 1.0f;
+        const Float2 so_far2 = pack2(so_far, so_far);
         pipe::mbar_wait(sum_full + half, sum_phase, abort_flag, status);
         fence_after();
         if (!absent) {
@@ -440,7 +449,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
           tmem_wait();
 #pragma unroll
           for (int i = 0; i < 32; i += 2) {
-            const Float2 sum = add2(pack2(v[c + i], v[c + i + 1]), pack2(more[i], more[i + 1]));
+            const Float2 sum = fma2(pack2(v[c + i], v[c + i + 1]), so_far2, pack2(more[i], more[i + 1]));
             unpack2(sum, v[c + i], v[c + i + 1]);
           }
         }
@@ -885,7 +894,7 @@ __global__ void __launch_bounds__(256) head_split_kernel(const T* x, int64_t pit
         const float y = v[e] * scale;
         hi.e[e] = __float2half_rn(y);
         const float rest = y - __half2float(hi.e[e]);
-        lo.e[e] = __float2half_rn(fabsf(y) < INFINITY ? rest : 0.0f);        // (infinity and NaN: the first piece alone says so)
+        lo.e[e] = __float2half_rn(fabsf(y) < INFINITY ? rest * kSecond : 0.0f);        // (infinity and NaN: the first piece alone says so)
       }
       store_pack((__half*)out + r * out_pitch + c, hi);
       store_pack((__half*)out + (rows + r) * out_pitch + c, lo);
@@ -1115,6 +1124,7 @@ static int head_product_launch(const HeadMaps& maps, HeadArgs a, int sms, cudaSt
   constexpr int bytes = HeadShared<MODE, BN>::kBytes;
   a.m_tiles = (a.m + kTile - 1) / kTile;
   a.n_tiles = (a.n + BN - 1) / BN;
+  a.low = (a.products - 1) * a.k_blocks;
   a.chunk = (MODE == kDhidden || MODE == kDweight) && sizeof(O) == 2 ? 64 : 8;
   const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles * a.slabs;
   if (tiles > 0x3FFFFFFF) return SOLON_ERR_INVALID_ARG;

@@ -128,3 +128,45 @@ def test_rows_without_a_share_say_nothing_about_the_others(rows, dtype, grad):
     g[1::5], g[2::9], gh[2::9] = NAN, INF, NAN
     got = call()
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("rows", [3, 20, 100, 300])
+def test_float32_elements_far_below_the_largest_of_their_row(rows):
+    """A row whose largest element meets zeros in the output matrix: its other elements, 2^-26 of that, keep their 22 bits (and 2^-50 of the
+    largest: 2^-24 of a weight each)."""
+    cols, vocab = 80, 500
+    h, w, t = _leaning(rows, cols, vocab, "f32", 4, 1.0)
+    h[:, 1:] *= 2.0 ** -26
+    h[:, 0] = 1.0
+    w[:, 1:] *= 2.0 ** 26
+    w[:, 0] = 0.0
+    z, tol = _logits(h, w)
+    floor = 2.0 ** -50 * float(w.abs().sum(1).max())
+    got = binding.solon_head_logprobs(h, w, t)
+    _close(got.peak, z.amax(1), tol.amax(1) + floor, "peak")
+    # a token of its own in every row, so that log p says what a single logit is
+    lp = torch.log_softmax(z, 1).gather(1, t[:, None])[:, 0]
+    _close(got.logp, lp, 2 * (tol.amax(1) + floor) + 100 * U * (1 + lp.abs()), "logp")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_gradients_of_rare_tokens_keep_their_bits(dtype):
+    """Logits that fall from token to token down to p = 2^-36: dW of each is -g p h, two pieces 2^-22 of it and 2^-50 of g h at most, next to what p is off by."""
+    rows, cols, vocab = 300, 64, 512
+    g = _gen(6)
+    h = torch.randn((rows, cols), device="cuda", generator=g) * 0.25
+    h[:, 0] = 1.0
+    w = torch.zeros((vocab, cols), device="cuda")
+    w[:, 0] = -torch.arange(vocab, device="cuda") * (25.0 / vocab)
+    h, w = h.to(TYPES[dtype]), w.to(TYPES[dtype])
+    t = torch.zeros(rows, dtype=torch.int64, device="cuda")
+    peak, log_sum, _ = _stats(h, w)
+    gl = -torch.rand(rows, device="cuda", generator=g)
+    _, dw = binding.solon_head_logprobs_backward(h, w, t, peak, log_sum, gl, hidden_grad=False)
+    dz, dzt = _dlogits(h, w, t, peak, log_sum, gl)
+    b = h.double()
+    size = dz.abs().t() @ b.abs()
+    tol = dzt.t() @ b.abs() + (2.0 ** -20 + 66 * U) * size + 2.0 ** -49 * float(gl.abs().max()) * b.abs().sum(0)
+    if dtype == "f16":
+        tol = tol + 64 * U * (dz.abs().t() @ _size(h))
+    _close(dw.view(vocab, cols), dz.t() @ b, tol, "dweight")
