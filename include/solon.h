@@ -391,7 +391,7 @@ int solon_embedding_backward(const void* dy, int64_t dy_pitch, int dtype, const 
  *   workspace  device, 256-byte aligned, solon_head_logprobs_workspace(...) bytes; `aligned`: 1 if both matrices' first elements and row
  *              pitches are multiples of 16 bytes (other rows are copied to such a pitch first).  Its contents need not survive the call
  * Products of the elements as they are, summed in float32 (float16 elements below 2^-14 with the precision of 2^-14); float32 elements are taken as two float16 pieces of 22 bits together (values
- * below 2^-28 of their tensor's largest: an absolute 2^-50 of it), or multiplied as they are where rows are few (up to 16).
+ * below 2^-28 of the largest of their row of hidden or weight: an absolute 2^-50 of it), or multiplied as they are where rows are few (up to 16).
  * Infinite and NaN elements reach the rows that their products enter; in two pieces infinity counts as NaN.  cols <= SOLON_MAX_WIDTH. */
 int64_t solon_head_logprobs_workspace(int64_t rows, int64_t cols, int64_t vocab, int dtype, int aligned);
 int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* weight, int64_t weight_pitch, int dtype, const int64_t* targets, int64_t rows,

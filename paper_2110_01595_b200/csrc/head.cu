@@ -7,8 +7,9 @@
 //
 // All three products run on the tensor cores (tensor_tiles.cuh).  What is multiplied is 16 bits wide:
 //   bfloat16, float16  the elements themselves; sums float32.  (Rows off 16-byte boundaries are copied to a pitch that the copies can take.)
-//   float32            two float16 pieces, x = 2^-s (hi + 2^-11 lo), s such that the largest of the tensor lies in [2^14, 2^15): the pieces hold 22 bits of
-//                      values down to 2^-28 of the largest, and an absolute 2^-50 of it below.  (With lo not multiplied the 22 bits ended at 2^-17: a float16's steps
+//   float32            two float16 pieces, x = 2^-s (hi + 2^-11 lo), s such that the largest lies in [2^14, 2^15): of the row for the logits, whose epilogue
+//                      undoes it, so that rows and tokens are what they are whatever stands beside them; of the whole tensor for dh and dW, which add up over them.
+//                      The pieces hold 22 bits of values down to 2^-28 of the largest, and an absolute 2^-50 of it below.  (With lo not multiplied the 22 bits ended at 2^-17: a float16's steps
 //                      end at 2^-24.)  A product is three: hi lo + lo hi, whose sum is taken times 2^-11 in registers, then hi hi; the lo lo left out is below
 //                      2^-22 of the term.  (Three bfloat16 pieces would take six products.)
 //   dz                 float16 by the power of two of the largest |g| + |g_H| (H + 1), of any states (bfloat16 states and weights are taken as float16 by a power
@@ -50,6 +51,7 @@ enum HeadMode { kStats, kFewRows, kDz, kDhidden, kDweight };
 // ------------------------------------------------------------------------------------------------------------ scales
 
 // What the scans of a call leave behind: the bits of the largest finite magnitudes (0: nothing to scale by), and a flag of waits that ran out.
+// (Of float32 rows each has its own besides, for the logits.)
 struct HeadWords {
   unsigned hidden, weight, dz;
   int status;
@@ -81,7 +83,8 @@ struct HeadArgs {
   int b_by_blocks;                       // B's map takes 128 columns a copy, where its rows lie across the inner dimension
   const HeadWords* words;
   HeadWords* flags;
-  int scaled;                            // bits: 1 hidden, 2 weight, 4 dz carry a power of two
+  int scaled;                            // kDhidden, kDweight; bits: 1 hidden, 2 weight, 4 dz carry a power of two
+  const float *undo_m, *undo_n;          // kStats, kFewRows, kDz: what the product's rows and columns are multiplied by (NULL: nothing)
   // rows
   const int64_t* targets;
   const float *peak, *log_sum, *entropy, *grad_logp, *grad_entropy;
@@ -277,7 +280,7 @@ template <int MODE, int BN>
 struct HeadShared {
   static constexpr int kStageBytes = (kRows + BN / 2) * kBlock * 2;
   static constexpr int kBlocks = MODE == kStats ? 0 : MODE == kDz || MODE == kDweight ? 8192 : 4096;     // a warp's blocks of the result
-  static constexpr int kStaging = kBlocks + (MODE == kStats || MODE == kDz ? 1024 : 0);                   // and what the tile's rows come with
+  static constexpr int kStaging = kBlocks + (MODE == kStats || MODE == kDz ? 2048 : 0);                   // and what the tile's rows and columns come with (blocks lie at multiples of 1024)
   static constexpr int kStages = (232448 - 2048 - kEpilogueWarps * kStaging) / kStageBytes > 12 ? 12 : (232448 - 2048 - kEpilogueWarps * kStaging) / kStageBytes;
   static constexpr int kBytes = 1024 + kStages * kStageBytes + kEpilogueWarps * kStaging + 512;
 };
@@ -395,11 +398,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     char* stage = staging + (warp - kFirstEpilogue) * Shared::kStaging;
     float undo[2] = {1.0f, 1.0f};
-    if (a.scaled) {
-      const int sa = MODE == kStats || MODE == kFewRows || MODE == kDz ? (a.scaled & 1 ? scale_exponent(a.words->hidden) : 0) : (a.scaled & 4 ? scale_exponent(a.words->dz) : 0);
-      const int sb = MODE == kDweight ? (a.scaled & 1 ? scale_exponent(a.words->hidden) : 0) : (a.scaled & 2 ? scale_exponent(a.words->weight) : 0);
-      undo[0] = power_of_two(-sa);
-      undo[1] = power_of_two(-sb);
+    if (MODE == kDhidden || MODE == kDweight) {
+      if (MODE == kDweight && a.scaled & 1) undo[0] = power_of_two(-scale_exponent(a.words->hidden));
+      if (MODE == kDhidden && a.scaled & 2) undo[0] = power_of_two(-scale_exponent(a.words->weight));
+      if (a.scaled & 4) undo[1] = power_of_two(-scale_exponent(a.words->dz));
     }
     uint32_t sum_phase = 0;
     int half = 0;
@@ -416,11 +418,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
       // what the tile's rows come with is on the way to shared memory while the tile is being multiplied
       [[maybe_unused]] float* of_rows = reinterpret_cast<float*>(stage + Shared::kBlocks);
       [[maybe_unused]] int64_t* of_targets = reinterpret_cast<int64_t*>(of_rows + 5 * 32);
+      [[maybe_unused]] const float* of_columns = of_rows + 256;
       if ((MODE == kStats || MODE == kDz) && !absent) {
         __syncwarp();
         const bool there = row < a.m;
         const int64_t at_row = there ? row : 0;
         if (a.targets) copy_async<8>(of_targets + lane, a.targets + at_row, there);
+        if (a.undo_n) copy16_async(of_rows + 256 + 4 * lane, a.undo_n + a.first + col + 4 * lane);      // (there are columns enough for whole tiles)
         if constexpr (MODE == kDz) {
           copy_async<4>(of_rows + lane, a.peak + at_row, there);
           copy_async<4>(of_rows + 32 + lane, a.log_sum + at_row, there);
@@ -432,6 +436,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
         }
         copies_commit();
       }
+      float undo_row = 1.0f;
+      if ((MODE == kStats || MODE == kFewRows || MODE == kDz) && a.undo_m && row < a.m) undo_row = a.undo_m[row];
       float v[kHalf];
 #pragma unroll
       for (int i = 0; i < kHalf; i++) v[i] = 0.0f;
@@ -460,9 +466,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
         if ((half ^= 1) == 0) sum_phase ^= 1;
       }
       if (absent) continue;
-      if (a.scaled) {
+      if constexpr (MODE == kDhidden || MODE == kDweight) {
 #pragma unroll
         for (int i = 0; i < kHalf; i++) v[i] = v[i] * undo[0] * undo[1];
+      } else {
+        if (MODE != kFewRows) {
+          copies_wait<0>();
+          __syncwarp();
+        }
+        if (a.undo_n) {
+          const float* columns = MODE == kFewRows ? a.undo_n + col : of_columns;
+          const Float2 by_row = pack2(undo_row, undo_row);
+#pragma unroll
+          for (int i = 0; i < kHalf; i += 4) {
+            const float4 u = *reinterpret_cast<const float4*>(columns + i);
+            unpack2(mul2(mul2(pack2(v[i], v[i + 1]), by_row), pack2(u.x, u.y)), v[i], v[i + 1]);
+            unpack2(mul2(mul2(pack2(v[i + 2], v[i + 3]), by_row), pack2(u.z, u.w)), v[i + 2], v[i + 3]);
+          }
+        }
       }
       if (*(volatile int*)abort_flag) {
 #pragma unroll
@@ -476,7 +497,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
             if (i >= inside) v[i] = -INFINITY;
         }
         if (row < a.m) {
-          copies_wait<0>();
           const int64_t token = a.targets ? of_targets[lane] - a.first - col : -1;
           if (token >= 0 && token < kHalf && token < inside) {
             float z = 0.0f;
@@ -522,7 +542,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
         }
       } else if constexpr (MODE == kDz) {
         const float grow = power_of_two(scale_exponent(a.words->dz));
-        copies_wait<0>();
         const int64_t target = a.targets && row < a.m ? of_targets[lane] : -1;
         DzRow r = {of_rows[lane], of_rows[32 + lane], a.grad_entropy ? of_rows[96 + lane] : 0.0f, a.grad_logp && target >= 0 ? of_rows[64 + lane] : 0.0f,
                    a.grad_entropy ? of_rows[128 + lane] : 0.0f};
@@ -781,82 +800,124 @@ __global__ void __launch_bounds__(256) head_join_kernel(HeadJoinArgs a) {
   }
 }
 
-struct HeadScanArgs {
-  const float *hidden, *weight;          // NULL: not wanted
-  const __nv_bfloat16 *hidden16, *weight16;      // the same
-  int64_t hidden_pitch, weight_pitch, rows, cols, vocab;
-  const int64_t* targets;
-  const float *peak, *grad_logp, *grad_entropy, *entropy;
-  int dz;
-  HeadWords* words;
-};
-
-// Largest finite magnitudes: of the hidden states, the output matrix, and a bound of each row's dz, |g| + |g_H| (H + 1), where g counts only with a target and
-// a row of which nothing is left has no share: what padding holds says nothing about the others.
-__global__ void __launch_bounds__(256) head_scan_kernel(HeadScanArgs a) {
-  __shared__ unsigned most[8];
-  pdl_trigger();
-  unsigned big = 0;
-  auto see = [&](float x) {
-    const unsigned u = __float_as_uint(x) & 0x7FFFFFFFu;
-    if (u < 0x7F800000u) big = max(big, u);
-  };
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  unsigned* word;
-  if (blockIdx.y == 2) {
-    if (!a.dz) return;
-    word = &a.words->dz;
-    for (int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x; r < a.rows; r += (int64_t)gridDim.x * 256)
-      if (a.peak[r] != -INFINITY)
-        see((a.grad_logp && a.targets[r] >= 0 ? fabsf(a.grad_logp[r]) : 0.0f) + (a.grad_entropy ? fabsf(a.grad_entropy[r]) * (fabsf(a.entropy[r]) + 1.0f) : 0.0f));
-  } else if (blockIdx.y ? a.weight16 : a.hidden16) {
-    const __nv_bfloat16* m = blockIdx.y ? a.weight16 : a.hidden16;
-    const int64_t rows = blockIdx.y ? a.vocab : a.rows, pitch = blockIdx.y ? a.weight_pitch : a.hidden_pitch;
-    word = blockIdx.y ? &a.words->weight : &a.words->hidden;
-    const bool wide = !(((uintptr_t)m | (uintptr_t)(pitch * 2)) & 15);
-    for (int64_t r = (int64_t)blockIdx.x * 8 + warp; r < rows; r += (int64_t)gridDim.x * 8) {
-      const __nv_bfloat16* p = m + r * pitch;
-      const int64_t done = wide ? a.cols / 8 * 8 : 0;
-#pragma unroll 4
-      for (int64_t c = lane * 8; c < done; c += 256) {
-        float x[8];
-        Word16<__nv_bfloat16>::unpack(load16_once(p + c), x);
-#pragma unroll
-        for (int e = 0; e < 8; e++) see(x[e]);
-      }
-#pragma unroll 8
-      for (int64_t c = done + lane; c < a.cols; c += 32) see(__bfloat162float(p[c]));
+// Eight elements of a row from column c on, zeros behind its end.  WIDE: rows lie at multiples of 16 bytes.
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, int64_t c, int64_t cols, bool wide, float (&v)[8]) {
+  if (wide && c + 8 <= cols) {
+    if constexpr (sizeof(T) == 4) {
+      *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(p + c);
+      *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<const float4*>(p + c + 4);
+    } else {
+      Word16<T>::unpack(*reinterpret_cast<const uint4*>(p + c), v);
     }
   } else {
-    const float* m = blockIdx.y ? a.weight : a.hidden;
-    if (!m) return;
-    int64_t rows = blockIdx.y ? a.vocab : a.rows, pitch = blockIdx.y ? a.weight_pitch : a.hidden_pitch, cols = a.cols;
-    word = blockIdx.y ? &a.words->weight : &a.words->hidden;
-    if (pitch == cols && !((uintptr_t)m & 15)) {       // one stretch: cut into rows of 2048 whatever its own are, and a last one
-      const int64_t all = rows * cols;
-      if (blockIdx.x == 0)
-        for (int64_t c = all / 2048 * 2048 + threadIdx.x; c < all; c += 256) see(m[c]);
-      rows = all / 2048;
-      cols = pitch = 2048;
-    }
-    const bool wide = !(((uintptr_t)m | (uintptr_t)(pitch * 4)) & 15);
-    for (int64_t r = (int64_t)blockIdx.x * 8 + warp; r < rows; r += (int64_t)gridDim.x * 8) {
-      const float* p = m + r * pitch;
-      int64_t done = 0;
-      if (wide) {
+#pragma unroll
+    for (int e = 0; e < 8; e++) v[e] = c + e < cols ? to_float(p[c + e]) : 0.0f;
+  }
+}
+// Two float16 pieces of eight elements times `scale`, `rest` elements apart.
+__device__ __forceinline__ void store_pieces(const float (&v)[8], float scale, __half* out, int64_t rest) {
+  Pack<__half, 8> hi, lo;
+#pragma unroll
+  for (int e = 0; e < 8; e++) {
+    const float y = v[e] * scale;
+    hi.e[e] = __float2half_rn(y);
+    lo.e[e] = __float2half_rn(fabsf(y) < INFINITY ? (y - __half2float(hi.e[e])) * kSecond : 0.0f);      // (infinity and NaN: the first piece alone says so)
+  }
+  store_pack(out, hi);
+  store_pack(out + rest, lo);
+}
+
+struct HeadScanSide {
+  const void* x;                         // NULL: not wanted
+  int64_t pitch, rows;
+  __half* out;                           // float32: the pieces of each row by an exponent of its own, and what they are multiplied by to undo it
+  float* undo;
+  unsigned* largest;                     // of the whole matrix (NULL: not wanted)
+};
+struct HeadScanArgs {
+  HeadScanSide side[2];                  // hidden states, output matrix
+  int64_t cols, out_pitch, rows;
+  const int64_t* targets;
+  const float *peak, *grad_logp, *grad_entropy, *entropy;
+  unsigned* dz;                          // NULL: not wanted
+};
+
+// Largest finite magnitudes: of the hidden states, of the output matrix, and of a bound of each row's dz, |g| + |g_H| (H + 1), where g counts only with a target and
+// a row of which nothing is left has no share: what padding holds says nothing about the others.
+// float32 rows leave as two pieces on the way, by TEAM threads a row, which hold its first 32 TEAM elements in registers (the rest is read twice): W comes from memory once,
+// where an exponent for the whole matrix took a pass of its own before the pieces (50001 x 1001: 116 us together), and no row's exponent is its neighbour's.
+template <typename T, int TEAM>
+__global__ void __launch_bounds__(256) head_scan_kernel(HeadScanArgs a) {
+  __shared__ unsigned most[8], row_most[8];
+  pdl_trigger();
+  unsigned big = 0;
+  auto see = [](unsigned& most, float x) {
+    const unsigned u = __float_as_uint(x) & 0x7FFFFFFFu;
+    if (u < 0x7F800000u) most = max(most, u);
+  };
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % TEAM;
+  unsigned* word = a.dz;
+  if (blockIdx.y == 2) {
+    if (!a.dz) return;
+    for (int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x; r < a.rows; r += (int64_t)gridDim.x * 256)
+      if (a.peak[r] != -INFINITY)
+        see(big, (a.grad_logp && a.targets[r] >= 0 ? fabsf(a.grad_logp[r]) : 0.0f) + (a.grad_entropy ? fabsf(a.grad_entropy[r]) * (fabsf(a.entropy[r]) + 1.0f) : 0.0f));
+  } else {
+    const HeadScanSide m = blockIdx.y ? a.side[1] : a.side[0];
+    if (!m.x) return;
+    word = m.largest;
+    const bool wide = !(((uintptr_t)m.x | (uintptr_t)(m.pitch * sizeof(T))) & 15);
+    constexpr int kTeams = 256 / TEAM, kGroups = sizeof(T) == 4 ? 4 : 1;
+    for (int64_t r = (int64_t)blockIdx.x * kTeams + threadIdx.x / TEAM; r < m.rows; r += (int64_t)gridDim.x * kTeams) {
+      const T* p = (const T*)m.x + r * m.pitch;
+      unsigned row = 0;
+      float held[kGroups][8];
+#pragma unroll
+      for (int q = 0; q < kGroups; q++) load8(p, (q * TEAM + lane) * 8, a.cols, wide, held[q]);
+#pragma unroll
+      for (int q = 0; q < kGroups; q++)
+#pragma unroll
+        for (int e = 0; e < 8; e++) see(row, held[q][e]);
 #pragma unroll 4
-        for (int64_t c = lane; c < cols / 4; c += 32) {
-          const float4 x = *reinterpret_cast<const float4*>(p + 4 * c);
-          see(x.x), see(x.y), see(x.z), see(x.w);
-        }
-        done = cols / 4 * 4;
+      for (int64_t c = (kGroups * TEAM + lane) * 8; c < a.cols; c += TEAM * 8) {
+        float v[8];
+        load8(p, c, a.cols, wide, v);
+#pragma unroll
+        for (int e = 0; e < 8; e++) see(row, v[e]);
       }
-#pragma unroll 4
-      for (int64_t c = done + lane; c < cols; c += 32) see(p[c]);
+      if constexpr (sizeof(T) == 4) {
+        row = __reduce_max_sync(~0u, row);
+        if (TEAM > 32) {
+          __syncthreads();
+          if (threadIdx.x % 32 == 0) row_most[warp] = row;
+          __syncthreads();
+#pragma unroll
+          for (int i = 0; i < 8; i++) row = max(row, row_most[i]);
+        }
+        const int exponent = scale_exponent(row);
+        const float scale = power_of_two(exponent);
+        __half* out = m.out + r * a.out_pitch;
+        const int64_t rest = m.rows * a.out_pitch;
+#pragma unroll
+        for (int q = 0; q < kGroups; q++) {
+          const int64_t c = (q * TEAM + lane) * 8;
+          if (c < a.out_pitch) store_pieces(held[q], scale, out + c, rest);
+        }
+#pragma unroll 2
+        for (int64_t c = (kGroups * TEAM + lane) * 8; c < a.out_pitch; c += TEAM * 8) {
+          float v[8];
+          load8(p, c, a.cols, wide, v);
+          store_pieces(v, scale, out + c, rest);
+        }
+        if (lane == 0) m.undo[r] = power_of_two(-exponent);
+      }
+      big = max(big, row);
     }
   }
+  if (!word) return;
   big = __reduce_max_sync(~0u, big);
-  if (lane == 0) most[warp] = big;
+  if (threadIdx.x % 32 == 0) most[warp] = big;
   __syncthreads();
   if (threadIdx.x == 0) {
     for (int i = 1; i < 8; i++) big = max(big, most[i]);
@@ -881,29 +942,11 @@ __global__ void __launch_bounds__(256) head_split_kernel(const T* x, int64_t pit
     const T* p = x + r * pitch + c;
     if constexpr (sizeof(T) == 4) {
       float v[8];
-      if (wide && c + 8 <= cols) {
-        *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(p);
-        *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<const float4*>(p + 4);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; e++) v[e] = c + e < cols ? p[e] : 0.0f;
-      }
-      Pack<__half, 8> hi, lo;
-#pragma unroll
-      for (int e = 0; e < 8; e++) {
-        const float y = v[e] * scale;
-        hi.e[e] = __float2half_rn(y);
-        const float rest = y - __half2float(hi.e[e]);
-        lo.e[e] = __float2half_rn(fabsf(y) < INFINITY ? rest * kSecond : 0.0f);        // (infinity and NaN: the first piece alone says so)
-      }
-      store_pack((__half*)out + r * out_pitch + c, hi);
-      store_pack((__half*)out + (rows + r) * out_pitch + c, lo);
+      load8(x + r * pitch, c, cols, wide, v);
+      store_pieces(v, scale, (__half*)out + r * out_pitch + c, rows * out_pitch);
     } else if constexpr (kToHalf) {
       float v[8];
-      if (wide && c + 8 <= cols) Word16<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4*>(p), v);
-      else
-#pragma unroll
-        for (int e = 0; e < 8; e++) v[e] = c + e < cols ? __bfloat162float(p[e]) : 0.0f;
+      load8(x + r * pitch, c, cols, wide, v);
 #pragma unroll
       for (int e = 0; e < 8; e++) v[e] *= scale;
       *reinterpret_cast<uint4*>(out + r * out_pitch + c) = Word16<__half>::pack(v);
@@ -961,7 +1004,9 @@ struct HeadPlan {
   int dz_pieces;
   int64_t width;                         // tokens of a piece of the vocabulary
   int h_splits, w_splits;                // parts of the inner dimensions of dh and dW
-  int64_t words, partial, target_logit, hidden, weight, hidden16, weight16, dz, sums, w_sums, total;
+  int64_t undo_hidden, undo_weight;      // float32: what the pieces' rows are multiplied by
+  int64_t hidden_w, weight_h;            // as they go into dW and, a piece of the vocabulary at a time, into dh
+  int64_t words, partial, target_logit, hidden, weight, dz, sums, w_sums, total;
 };
 
 constexpr int64_t kHeadSharedRows = 200 * 1024;       // bytes of hidden rows that the kernel for few rows holds
@@ -1006,6 +1051,10 @@ static HeadPlan head_forward_plan(int64_t rows, int64_t cols, int64_t vocab, int
     if (p.split) {
       p.hidden = take(p.pieces * rows * p.pitch * 2);
       p.weight = take(p.pieces * vocab * p.pitch * 2);
+    }
+    if (dtype == SOLON_F32) {
+      p.undo_hidden = take(up(rows, kTile) * 4);
+      p.undo_weight = take(up(vocab, kTile) * 4);
     }
   }
   p.partial = take(p.slots * 3 * rows * 4);
@@ -1072,9 +1121,13 @@ static HeadPlan head_backward_plan(int64_t rows, int64_t cols, int64_t vocab, in
     p.hidden = take(p.pieces * rows * p.pitch * 2);
     p.weight = take(p.pieces * vocab * p.pitch * 2);
   }
-  if (dtype == SOLON_BF16) {
-    p.hidden16 = take(rows * p.pitch * 2);
-    p.weight16 = take(p.width * p.pitch * 2);       // of one piece of the vocabulary
+  if (dtype == SOLON_F32) {
+    p.undo_hidden = take(up(rows, kTile) * 4);
+    p.undo_weight = take(up(vocab, kTile) * 4);
+  }
+  if (dtype != SOLON_F16) {
+    p.hidden_w = take(p.pieces * rows * p.pitch * 2);
+    p.weight_h = take(p.pieces * p.width * p.pitch * 2);
   }
   p.dz = take(p.dz_pieces * rows * p.width * 2);
   if (times > 1 || p.h_splits > 1) p.sums = take(p.h_splits * rows * up(cols, 128) * 4);
@@ -1149,26 +1202,36 @@ struct HeadOperand {
   int pieces;
 };
 
-static int head_operand(const void* x, int64_t pitch, int64_t rows, int64_t cols, int dtype, const HeadPlan& plan, char* to, const unsigned* largest, int sms,
-                        cudaStream_t stream, HeadOperand* out) {
+// The elements as they are: where they lie, or copied to a pitch that tensor copies can take.
+static int head_operand(const void* x, int64_t pitch, int64_t rows, int64_t cols, const HeadPlan& plan, char* to, int sms, cudaStream_t stream, HeadOperand* out) {
   if (!plan.split) {
     *out = {(const char*)x, rows > 1 ? pitch : up(cols, 8), rows, 1};
     return SOLON_OK;
   }
   const int64_t words = rows * (plan.pitch / 8);
-  const unsigned blocks = (unsigned)std::min<int64_t>((words + 255) / 256, 16 * sms);
-  const int rc = dtype == SOLON_F32 ? launch_dependent(head_split_kernel<float>, dim3(blocks), dim3(256), 0, stream, (const float*)x, pitch, rows, cols,
-                                                       (uint16_t*)to, plan.pitch, largest)
-                                    : launch_dependent(head_split_kernel<uint16_t>, dim3(blocks), dim3(256), 0, stream, (const uint16_t*)x, pitch, rows, cols,
-                                                       (uint16_t*)to, plan.pitch, (const unsigned*)nullptr);
-  if (rc) return rc;
-  *out = {to, plan.pitch, rows, plan.pieces};
-  return SOLON_OK;
+  *out = {to, plan.pitch, rows, 1};
+  return launch_dependent(head_split_kernel<uint16_t>, dim3((unsigned)std::min<int64_t>((words + 255) / 256, 16 * sms)), dim3(256), 0, stream, (const uint16_t*)x,
+                          pitch, rows, cols, (uint16_t*)to, plan.pitch, (const unsigned*)nullptr);
 }
 
-static int head_scan(const HeadScanArgs& a, int sms, cudaStream_t stream) {
-  if (!a.hidden && !a.hidden16 && !a.weight && !a.weight16 && !a.dz) return SOLON_OK;
-  head_scan_kernel<<<dim3(4 * sms, 3), 256, 0, stream>>>(a);
+// float32 or bfloat16 elements in as many float16 pieces as they take, all by the exponent of one number.
+static int head_pieces(const void* x, int64_t pitch, int64_t rows, int64_t cols, bool f32, const HeadPlan& plan, char* to, const unsigned* largest, int sms,
+                       cudaStream_t stream, HeadOperand* out) {
+  const int64_t words = rows * (plan.pitch / 8);
+  const dim3 blocks((unsigned)std::min<int64_t>((words + 255) / 256, 16 * sms));
+  *out = {to, plan.pitch, rows, f32 ? 2 : 1};
+  if (f32) return launch_dependent(head_split_kernel<float>, blocks, dim3(256), 0, stream, (const float*)x, pitch, rows, cols, (uint16_t*)to, plan.pitch, largest);
+  return launch_dependent(head_split_kernel<__nv_bfloat16>, blocks, dim3(256), 0, stream, (const __nv_bfloat16*)x, pitch, rows, cols, (uint16_t*)to, plan.pitch, largest);
+}
+
+// Rows wider than 8192 elements are gone through by whole CTAs.
+static int head_scan(const HeadScanArgs& a, bool f32, int sms, cudaStream_t stream) {
+  const bool whole = f32 && a.cols > 8192;
+  const int64_t rows = std::max(a.side[0].rows, a.side[1].x ? a.side[1].rows : 1);
+  const dim3 grid((unsigned)std::min<int64_t>(whole ? rows : (rows + 7) / 8, 8 * sms), a.dz ? 3 : 2);
+  if (whole) head_scan_kernel<float, 256><<<grid, 256, 0, stream>>>(a);
+  else if (f32) head_scan_kernel<float, 32><<<grid, 256, 0, stream>>>(a);
+  else head_scan_kernel<__nv_bfloat16, 32><<<grid, 256, 0, stream>>>(a);
   SOLON_CUDA_TRY(cudaGetLastError());
   return SOLON_OK;
 }
@@ -1268,14 +1331,18 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
     a.target_logit = (float*)(ws + plan.target_logit);
     if ((rc = small_forward(a, stream))) return rc;
   } else {
-    if (dtype == SOLON_F32) {
-      SOLON_CUDA_TRY(cudaMemsetAsync(words, 0, sizeof(HeadWords), stream));
-      const HeadScanArgs scan = {(const float*)hidden, (const float*)weight, nullptr, nullptr, hidden_pitch, weight_pitch, rows, cols, vocab, nullptr, nullptr, nullptr, nullptr, nullptr, 0, words};
-      if ((rc = head_scan(scan, sms, stream))) return rc;
-    }
     HeadOperand h, w;
-    if ((rc = head_operand(hidden, hidden_pitch, rows, cols, dtype, plan, ws + plan.hidden, &words->hidden, sms, stream, &h))) return rc;
-    if ((rc = head_operand(weight, weight_pitch, vocab, cols, dtype, plan, ws + plan.weight, &words->weight, sms, stream, &w))) return rc;
+    if (dtype == SOLON_F32) {
+      const HeadScanArgs scan = {{{hidden, hidden_pitch, rows, (__half*)(ws + plan.hidden), (float*)(ws + plan.undo_hidden), nullptr},
+                                  {weight, weight_pitch, vocab, (__half*)(ws + plan.weight), (float*)(ws + plan.undo_weight), nullptr}},
+                                 cols, plan.pitch, rows, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
+      if ((rc = head_scan(scan, true, sms, stream))) return rc;
+      h = {ws + plan.hidden, plan.pitch, rows, 2};
+      w = {ws + plan.weight, plan.pitch, vocab, 2};
+    } else if ((rc = head_operand(hidden, hidden_pitch, rows, cols, plan, ws + plan.hidden, sms, stream, &h)) ||
+               (rc = head_operand(weight, weight_pitch, vocab, cols, plan, ws + plan.weight, sms, stream, &w))) {
+      return rc;
+    }
     const bool bf16 = dtype == SOLON_BF16;
     HeadMaps maps = {};
     if (!tensor_map(&maps.a, h.p, bf16, cols, rows, h.pieces, h.pitch, rows * h.pitch, !plan.few ? kRows : rows <= 64 ? 32 : 64) ||
@@ -1288,7 +1355,10 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
     a.k_blocks = (int)((cols + kBlock - 1) / kBlock);
     head_pairs(a, h.pieces, w.pieces, 1, 1);
     a.words = a.flags = words;
-    a.scaled = dtype == SOLON_F32 ? 3 : 0;
+    if (dtype == SOLON_F32) {
+      a.undo_m = (const float*)(ws + plan.undo_hidden);
+      a.undo_n = (const float*)(ws + plan.undo_weight);
+    }
     a.targets = targets;
     a.partial = (float*)(ws + plan.partial);
     a.target_logit = (float*)(ws + plan.target_logit);
@@ -1296,6 +1366,7 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
     if (plan.few) {
       std::swap(maps.a, maps.b);
       std::swap(a.m, a.n);
+      std::swap(a.undo_m, a.undo_n);
     }
     if ((rc = head_stats(maps, a, plan.few, bf16, sms, stream))) return rc;
   }
@@ -1341,7 +1412,7 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
   if ((rc = current_sms(&sms))) return rc;
   char* ws = (char*)workspace;
   HeadWords* words = (HeadWords*)(ws + plan.words);
-  const bool f32 = dtype == SOLON_F32, bf16 = dtype == SOLON_BF16;
+  const bool f32 = dtype == SOLON_F32, bf16 = dtype == SOLON_BF16, f16 = dtype == SOLON_F16;
   if (plan.small) {
     HeadSmallArgs a = {};
     a.hidden = (const float*)hidden;
@@ -1370,29 +1441,26 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
   }
   const bool coarse = grad_dtype == SOLON_BF16;          // dW from the first pieces alone
   const int form = (dhidden && !bf16) || (dweight && !coarse) ? kPair : kNearest, dz_pieces = form == kPair ? 2 : 1;
-  const bool hidden16 = bf16 && dweight, weight16 = bf16 && dhidden;
+  const bool hidden_w = !f16 && dweight, weight_h = !f16 && dhidden;      // the two products take float16 pieces by an exponent of a whole matrix
   SOLON_CUDA_TRY(cudaMemsetAsync(words, 0, sizeof(HeadWords), stream));
-  const HeadScanArgs scan = {f32 ? (const float*)hidden : nullptr, f32 ? (const float*)weight : nullptr, hidden16 ? (const __nv_bfloat16*)hidden : nullptr,
-                             weight16 ? (const __nv_bfloat16*)weight : nullptr, hidden_pitch, weight_pitch, rows, cols, vocab, targets, peak, grad_logp,
-                             grad_entropy, entropy, 1, words};
-  if ((rc = head_scan(scan, sms, stream))) return rc;
-  HeadOperand h, w;
-  if ((rc = head_operand(hidden, hidden_pitch, rows, cols, dtype, plan, ws + plan.hidden, &words->hidden, sms, stream, &h))) return rc;
-  if ((rc = head_operand(weight, weight_pitch, vocab, cols, dtype, plan, ws + plan.weight, &words->weight, sms, stream, &w))) return rc;
+  const HeadScanArgs scan = {{{f32 || (bf16 && dweight) ? hidden : nullptr, hidden_pitch, rows, (__half*)(ws + plan.hidden), (float*)(ws + plan.undo_hidden),
+                               hidden_w ? &words->hidden : nullptr},
+                              {f32 || (bf16 && dhidden) ? weight : nullptr, weight_pitch, vocab, (__half*)(ws + plan.weight), (float*)(ws + plan.undo_weight),
+                               weight_h ? &words->weight : nullptr}},
+                             cols, plan.pitch, rows, targets, peak, grad_logp, grad_entropy, entropy, &words->dz};
+  if ((rc = head_scan(scan, f32, sms, stream))) return rc;
+  HeadOperand h = {ws + plan.hidden, plan.pitch, rows, 2}, w = {ws + plan.weight, plan.pitch, vocab, 2};
+  if (!f32 && ((rc = head_operand(hidden, hidden_pitch, rows, cols, plan, ws + plan.hidden, sms, stream, &h)) ||
+               (rc = head_operand(weight, weight_pitch, vocab, cols, plan, ws + plan.weight, sms, stream, &w))))
+    return rc;
 
   const int64_t n = rows / partitions, sums_pitch = up(cols, 128);
   // as rows along the inner dimension: h and W for the logits, dz for dh; across it: W for dh, dz and h for dW
   CUtensorMap map_h, map_w, map_w_across, map_h_across, map_dz, map_dz_across, map_dz_out;
-  HeadOperand hw = h, wh = w;              // as they go into dW and dh: bfloat16 as float16 by a power of two
-  auto as_half = [&](const void* x, int64_t pitch, int64_t rows, int64_t to, const unsigned* largest, HeadOperand* out) {
-    const int64_t items = rows * (plan.pitch / 8);
-    *out = {ws + to, plan.pitch, rows, 1};
-    return launch_dependent(head_split_kernel<__nv_bfloat16>, dim3((unsigned)std::min<int64_t>((items + 255) / 256, 16 * sms)), dim3(256), 0, stream,
-                            (const __nv_bfloat16*)x, pitch, rows, cols, (uint16_t*)(ws + to), plan.pitch, largest);
-  };
-  if (hidden16 && (rc = as_half(hidden, hidden_pitch, rows, plan.hidden16, &words->hidden, &hw))) return rc;
+  HeadOperand hw = h, wh = w;              // as they go into dW and dh
+  if (hidden_w && (rc = head_pieces(hidden, hidden_pitch, rows, cols, f32, plan, ws + plan.hidden_w, &words->hidden, sms, stream, &hw))) return rc;
   // (a map across the inner dimension goes with the tiles: copies of 128 columns need 128 of them in a CTA's tile, and whole blocks of 64 in memory)
-  const bool whole = cols % kBlock == 0 || plan.split, hw_whole = whole || hidden16, wh_whole = whole || weight16;
+  const bool whole = cols % kBlock == 0 || plan.split, hw_whole = whole || hidden_w, wh_whole = whole || weight_h;
   auto across = [&](CUtensorMap* map, const void* p, bool by_blocks, int64_t rows, int64_t slabs, int64_t pitch, int64_t slab) {
     return by_blocks ? tensor_map_by_blocks(map, p, false, cols, rows, slabs, pitch, slab) : tensor_map(map, p, false, cols, rows, slabs, pitch, slab, kBlock);
   };
@@ -1413,8 +1481,10 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
   for (int64_t first = 0; first < vocab; first += plan.width) {
     const int64_t width = std::min(plan.width, vocab - first), pitch = up(width, kBlock);
     const bool h_narrow = narrow(cols, pitch / kBlock * dh_products(dtype));
-    if (weight16 && (rc = as_half((const __nv_bfloat16*)weight + first * weight_pitch, weight_pitch, width, plan.weight16, &words->weight, &wh))) return rc;
-    const char* w_across = wh.p + (weight16 ? 0 : first * wh.pitch * 2);
+    if (weight_h && (rc = head_pieces((const char*)weight + first * weight_pitch * (f32 ? 4 : 2), weight_pitch, width, cols, f32, plan, ws + plan.weight_h,
+                                      &words->weight, sms, stream, &wh)))
+      return rc;
+    const char* w_across = wh.p + (weight_h ? 0 : first * wh.pitch * 2);
     if (!tensor_map(&map_dz, ws + plan.dz, false, pitch, rows, dz_pieces, pitch, rows * pitch, kRows) ||
         !tensor_map(&map_dz_out, ws + plan.dz, false, pitch, rows, dz_pieces, pitch, rows * pitch, 32) ||
         !tensor_map_by_blocks(&map_dz_across, ws + plan.dz, false, pitch, n, (int64_t)dz_pieces * partitions, pitch, n * pitch) ||
@@ -1427,7 +1497,10 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
     a.first = first;
     a.k_blocks = (int)((cols + kBlock - 1) / kBlock);
     head_pairs(a, h.pieces, w.pieces, 1, 1);
-    a.scaled = f32 ? 3 : 0;
+    if (f32) {
+      a.undo_m = (const float*)(ws + plan.undo_hidden);
+      a.undo_n = (const float*)(ws + plan.undo_weight);
+    }
     a.form = form;
     a.dz_pitch = (int)pitch;
     if ((rc = bf16 ? head_product_launch<kDz, 256, true, float>({map_h, map_w, map_dz_out}, a, sms, stream)
@@ -1442,7 +1515,7 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
       a.b_by_blocks = wh_whole && !h_narrow;
       a.k_blocks = (int)((pitch / kBlock + a.splits - 1) / a.splits);
       head_pairs(a, bf16 ? 1 : 2, wh.pieces, 1, 1);
-      a.scaled = (f32 || bf16 ? 2 : 0) | 4;
+      a.scaled = f16 ? 4 : 6;
       a.sums = (float*)(ws + plan.sums);
       a.sums_pitch = sums_pitch;
       a.load_sums = first > 0;
@@ -1470,7 +1543,7 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
       a.sums_pitch = sums_pitch;
       a.store_sums = a.splits > 1;
       head_pairs(a, coarse ? 1 : 2, coarse ? 1 : hw.pieces, partitions, partitions);
-      a.scaled = (f32 || bf16 ? 1 : 0) | 4;
+      a.scaled = f16 ? 4 : 5;
       a.out = (char*)dweight + first * cols * grad_size;
       a.out_pitch = cols;
       a.out_slab = partitions > 1 ? grad_pitch : 0;

@@ -170,3 +170,36 @@ def test_gradients_of_rare_tokens_keep_their_bits(dtype):
     if dtype == "f16":
         tol = tol + 64 * U * (dz.abs().t() @ _size(h))
     _close(dw.view(vocab, cols), dz.t() @ b, tol, "dweight")
+
+
+@pytest.mark.parametrize("rows,vocab", [(3, 700), (12, 700), (24, 19_000), (40, 700), (300, 700)])
+def test_a_large_row_or_token_leaves_the_others_alone(rows, vocab):
+    """Every logit is off by what its own row's and token's elements come to, whatever the size of their neighbours."""
+    cols = 64
+    h, w, t = _leaning(rows, cols, vocab, "f32", 9, 2.0)
+    w[:, 0] = 0.0
+    h[:, 0] = -1.0
+    t = t.clamp(min=6)
+    for what in ("row", "token"):
+        a, b = h.clone(), w.clone()
+        if what == "row":
+            a[1] *= 1e12
+        else:
+            b[5, 0] = 1e12                                        # a logit of -1e12 in every row
+        others = torch.arange(rows, device="cuda") != (1 if what == "row" else -1)
+        z, tol = _logits(a, b)
+        tokens = torch.arange(vocab, device="cuda") != (-1 if what == "row" else 5)
+        most = tol[:, tokens].amax(1)[others]
+        got = binding.solon_head_logprobs(a, b, t)
+        _close(got.peak[others], z.amax(1)[others], most + U * z.amax(1)[others].abs(), "peak")
+        lp = torch.log_softmax(z, 1).gather(1, t[:, None])[:, 0][others]
+        _close(got.logp[others], lp, 2 * most + 200 * U * (1 + lp.abs()), "logp")
+        # and in the backward pass
+        peak, log_sum, _ = _stats(a, b)
+        g = -torch.rand(rows, device="cuda", generator=_gen(1))
+        dh, _ = binding.solon_head_logprobs_backward(a, b, t, peak, log_sum, g, weight_grad=False)
+        dz, dzt = _dlogits(a, b, t, peak, log_sum, g)
+        wd = b.double()
+        size = dz.abs() @ wd.abs()
+        dtol = dzt @ wd.abs() + (2.0 ** -20 + (64 + vocab / 256) * U) * size + 2.0 ** -49 * (g.double().abs()[:, None] * wd.abs().sum(0) + wd.abs().max() * dz.abs().sum(1)[:, None])
+        _close(dh[others], (dz @ wd)[others], dtol[others], "dhidden")
