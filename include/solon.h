@@ -405,10 +405,12 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
  *   peak, log_sum, entropy, grad_logp, grad_entropy  as in solon_token_logprobs_backward
  *   workspace  device, 256-byte aligned, solon_head_logprobs_backward_workspace(...) bytes: dlogits of one piece of the vocabulary (at most
  *              512 MB, or 256 tokens), sums of dhidden
- * dlogits is held in float16 times a power of two: one piece (11 bits; values below 2^-28 of the call's largest |grad_logp| + |grad_entropy| (entropy + 1): an absolute
+ * dlogits is held in float16 times a power of two a row: one piece (11 bits; values below 2^-28 of the row's |grad_logp| + |grad_entropy| (entropy + 1): an absolute
  * 2^-40 of it) for dhidden of bfloat16 states and for bfloat16 gradients, two (22 bits; 2^-50) for dhidden of float16 and float32 states and for float32 and float64
- * gradients.  bfloat16 states and weights count as float16 times a power of two in the two products (exact
- * down to 2^-28 of their largest).  rows = 0: dweight becomes 0.  hidden has to be finite in rows that count in no gradient, too: they are multiplied by zeros. */
+ * gradients.  The other factor is taken in float16 pieces as well, as many as the elements have above (bfloat16 gradients: one): weight by a power of two of its largest in dhidden (float16
+ * as it is), hidden in dweight by powers of two that make the largest product of a row's bound and its elements in the partition the measure.  No row's dhidden depends on
+ * another row, no partition's dweight on another partition.
+ * rows = 0: dweight becomes 0.  hidden has to be finite in rows that count in no gradient, too: they are multiplied by zeros. */
 int64_t solon_head_logprobs_backward_workspace(int64_t rows, int64_t cols, int64_t vocab, int partitions, int dtype, int grad_dtype, int aligned);
 int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const void* weight, int64_t weight_pitch, int dtype, const int64_t* targets,
                                  int64_t rows, int64_t cols, int64_t vocab, int partitions, const float* peak, const float* log_sum, const float* entropy,

@@ -8,11 +8,11 @@
 // All three products run on the tensor cores (tensor_tiles.cuh).  What is multiplied is 16 bits wide:
 //   bfloat16, float16  the elements themselves; sums float32.  (Rows off 16-byte boundaries are copied to a pitch that the copies can take.)
 //   float32            two float16 pieces, x = 2^-s (hi + 2^-11 lo), s such that the largest lies in [2^14, 2^15): of the row for the logits, whose epilogue
-//                      undoes it, so that rows and tokens are what they are whatever stands beside them; of the whole tensor for dh and dW, which add up over them.
+//                      undoes it, so that rows and tokens are what they are whatever stands beside them; of all W for dh, of a partition for dW, which add up over them.
 //                      The pieces hold 22 bits of values down to 2^-28 of the largest, and an absolute 2^-50 of it below.  (With lo not multiplied the 22 bits ended at 2^-17: a float16's steps
 //                      end at 2^-24.)  A product is three: hi lo + lo hi, whose sum is taken times 2^-11 in registers, then hi hi; the lo lo left out is below
 //                      2^-22 of the term.  (Three bfloat16 pieces would take six products.)
-//   dz                 float16 by the power of two of the largest |g| + |g_H| (H + 1), of any states (bfloat16 states and weights are taken as float16 by a power
+//   dz                 float16 by the power of two of its row's |g| + |g_H| (H + 1), of any states (bfloat16 states and weights are taken as float16 by a power
 //                      of two for these products: eight bits of dz would put as much into a result again as its own rounding to bfloat16 does; with eleven, an
 //                      eighth of that).  One piece for dh of bfloat16 states and for bfloat16 gradients (those of float32 states take the first piece of
 //                      the states alone, too): 11 bits of what lies above 2^-28 of the largest, an absolute 2^-40 of it below.  Two, the second times 2^11 as above,
@@ -50,16 +50,24 @@ enum HeadMode { kStats, kFewRows, kDz, kDhidden, kDweight };
 
 // ------------------------------------------------------------------------------------------------------------ scales
 
-// What the scans of a call leave behind: the bits of the largest finite magnitudes (0: nothing to scale by), and a flag of waits that ran out.
-// (Of float32 rows each has its own besides, for the logits.)
+// Powers of two.  A float32 row of hidden states or weights has one of its own for the logits, a row's dz has one, by the largest that it can hold, and the weights
+// have one for dh.  dW of a partition adds up rows: there row i of h carries what its dz lacks to the partition's exponent, so that what counts is |dz_i| |h_i|
+// against the partition's largest, and partitions say nothing about one another.
+
+// What the scan of a call leaves behind: the bits of the weights' largest finite magnitude, and a flag of waits that ran out.  Behind it a word a partition: the
+// exponent of its largest |dz_i| |h_i| over that of dz (0: no row with a share).
 struct HeadWords {
-  unsigned hidden, weight, dz;
+  unsigned weight;
   int status;
 };
 
 __device__ __forceinline__ int scale_exponent(unsigned largest) {       // 2^s brings the largest magnitude into [2^14, 2^15)
   return largest ? min(126, 14 - ilogbf(__uint_as_float(largest))) : 0;
 }
+constexpr int kPartBias = 1024;
+__device__ __forceinline__ int part_exponent(unsigned word) { return word ? 14 + kPartBias - (int)word : 0; }      // -226 to 252
+__device__ __forceinline__ int exponent_of(float power) { return (__float_as_int(power) >> 23) - 127; }             // of a power of two
+__device__ __forceinline__ float inverse_power(float power) { return __int_as_float(0x7F000000 - __float_as_int(power)); }
 constexpr float kSecond = 2048.0f;       // what a second piece is multiplied by: at most 2^3 is left of elements below 2^15, and 2^-25 of those below 2^-14
 __device__ __forceinline__ float power_of_two(int s) { return __int_as_float((s + 127) << 23); }       // -126 <= s <= 127
 
@@ -83,11 +91,13 @@ struct HeadArgs {
   int b_by_blocks;                       // B's map takes 128 columns a copy, where its rows lie across the inner dimension
   const HeadWords* words;
   HeadWords* flags;
-  int scaled;                            // kDhidden, kDweight; bits: 1 hidden, 2 weight, 4 dz carry a power of two
-  const float *undo_m, *undo_n;          // kStats, kFewRows, kDz: what the product's rows and columns are multiplied by (NULL: nothing)
+  int weight_scaled;                     // kDhidden: the weights carry a power of two
+  const unsigned* parts;                 // kDweight: the partitions' words
+  const float *undo_m, *undo_n;          // what the product's rows and columns are multiplied by (NULL: nothing)
   // rows
   const int64_t* targets;
   const float *peak, *log_sum, *entropy, *grad_logp, *grad_entropy;
+  const float* undo_dz;                  // kDz: what a row's dz is multiplied by where it has been used (0: the row has no share)
   // kStats, kFewRows (whose product is W h^T: tokens are rows of it)
   float* partial;                        // slots x 3 x rows
   float* target_logit;                   // rows
@@ -398,11 +408,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     char* stage = staging + (warp - kFirstEpilogue) * Shared::kStaging;
     float undo[2] = {1.0f, 1.0f};
-    if (MODE == kDhidden || MODE == kDweight) {
-      if (MODE == kDweight && a.scaled & 1) undo[0] = power_of_two(-scale_exponent(a.words->hidden));
-      if (MODE == kDhidden && a.scaled & 2) undo[0] = power_of_two(-scale_exponent(a.words->weight));
-      if (a.scaled & 4) undo[1] = power_of_two(-scale_exponent(a.words->dz));
-    }
+    if (MODE == kDhidden && a.weight_scaled) undo[1] = power_of_two(-scale_exponent(a.words->weight));
     uint32_t sum_phase = 0;
     int half = 0;
     [[maybe_unused]] int turn = 0;           // which of the warp's two blocks of the result is filled next
@@ -417,7 +423,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
       const bool absent = row0 >= a.m || (MODE != kStats && col >= (MODE == kDz ? a.dz_pitch : a.n));     // nothing of the tile is this warp's
       // what the tile's rows come with is on the way to shared memory while the tile is being multiplied
       [[maybe_unused]] float* of_rows = reinterpret_cast<float*>(stage + Shared::kBlocks);
-      [[maybe_unused]] int64_t* of_targets = reinterpret_cast<int64_t*>(of_rows + 5 * 32);
+      [[maybe_unused]] int64_t* of_targets = reinterpret_cast<int64_t*>(of_rows + 6 * 32);
       [[maybe_unused]] const float* of_columns = of_rows + 256;
       if ((MODE == kStats || MODE == kDz) && !absent) {
         __syncwarp();
@@ -428,6 +434,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
         if constexpr (MODE == kDz) {
           copy_async<4>(of_rows + lane, a.peak + at_row, there);
           copy_async<4>(of_rows + 32 + lane, a.log_sum + at_row, there);
+          copy_async<4>(of_rows + 160 + lane, a.undo_dz + at_row, there);
           if (a.grad_logp) copy_async<4>(of_rows + 64 + lane, a.grad_logp + at_row, there);
           if (a.grad_entropy) {
             copy_async<4>(of_rows + 96 + lane, a.entropy + at_row, there);
@@ -437,7 +444,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
         copies_commit();
       }
       float undo_row = 1.0f;
-      if ((MODE == kStats || MODE == kFewRows || MODE == kDz) && a.undo_m && row < a.m) undo_row = a.undo_m[row];
+      if (MODE != kDweight && a.undo_m && row < a.m) undo_row = a.undo_m[row];
+      if (MODE == kDhidden) undo[0] = undo_row;
+      if (MODE == kDweight) {
+        const int exponent = part_exponent(a.parts[a.splits > 1 ? at.slab / a.splits : at.slab]);
+        undo[0] = power_of_two(-(exponent / 2));
+        undo[1] = power_of_two(exponent / 2 - exponent);
+      }
       float v[kHalf];
 #pragma unroll
       for (int i = 0; i < kHalf; i++) v[i] = 0.0f;
@@ -541,13 +554,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
           rows_so_far[c / 32] = join(rows_so_far[c / 32], sums);
         }
       } else if constexpr (MODE == kDz) {
-        const float grow = power_of_two(scale_exponent(a.words->dz));
         const int64_t target = a.targets && row < a.m ? of_targets[lane] : -1;
         DzRow r = {of_rows[lane], of_rows[32 + lane], a.grad_entropy ? of_rows[96 + lane] : 0.0f, a.grad_logp && target >= 0 ? of_rows[64 + lane] : 0.0f,
                    a.grad_entropy ? of_rows[128 + lane] : 0.0f};
-        const bool active = r.peak != -INFINITY && (r.g != 0.0f || r.gh != 0.0f);
-        r.g *= grow;
-        r.gh *= grow;
+        const float undo_dz = of_rows[160 + lane];
+        const bool active = undo_dz != 0.0f;
+        r.g *= inverse_power(undo_dz);
+        r.gh *= inverse_power(undo_dz);
         const uint32_t keep = active ? ~0u : 0u;
         const int64_t token = target - a.first - col, inside = a.vocab - (a.first + col);
         if (inside < kHalf) {                // (what lies beyond is multiplied by zeros and has to be a number: p = 0)
@@ -840,11 +853,20 @@ struct HeadScanArgs {
   int64_t cols, out_pitch, rows;
   const int64_t* targets;
   const float *peak, *grad_logp, *grad_entropy, *entropy;
-  unsigned* dz;                          // NULL: not wanted
+  float* undo_dz;                        // of each row (NULL: not wanted)
+  unsigned* parts;                       // words of the partitions of n rows (NULL: not wanted)
+  int64_t n;
 };
 
-// Largest finite magnitudes: of the hidden states, of the output matrix, and of a bound of each row's dz, |g| + |g_H| (H + 1), where g counts only with a target and
-// a row of which nothing is left has no share: what padding holds says nothing about the others.
+// What row r's dz is multiplied by where it has been used: a power of two from |g| + |g_H| (H + 1), which no element exceeds.  0 where the row has no share: g counts only
+// with a target, and nothing counts in a row of which nothing is left.
+__device__ __forceinline__ float row_share(const HeadScanArgs& a, int64_t r) {
+  const float g = a.grad_logp && a.targets[r] >= 0 ? fabsf(a.grad_logp[r]) : 0.0f, gh = a.grad_entropy ? fabsf(a.grad_entropy[r]) : 0.0f;
+  if (a.peak[r] == -INFINITY || (g == 0.0f && gh == 0.0f)) return 0.0f;
+  return power_of_two(-scale_exponent(min(__float_as_uint(gh == 0.0f ? g : g + gh * (fabsf(a.entropy[r]) + 1.0f)) & 0x7FFFFFFFu, 0x7F7FFFFFu)));
+}
+
+// Powers of two: of rows of float32 hidden states and weights, of the whole output matrix, of the rows' dz and of the partitions.
 // float32 rows leave as two pieces on the way, by TEAM threads a row, which hold its first 32 TEAM elements in registers (the rest is read twice): W comes from memory once,
 // where an exponent for the whole matrix took a pass of its own before the pieces (50001 x 1001: 116 us together), and no row's exponent is its neighbour's.
 template <typename T, int TEAM>
@@ -857,12 +879,9 @@ __global__ void __launch_bounds__(256) head_scan_kernel(HeadScanArgs a) {
     if (u < 0x7F800000u) most = max(most, u);
   };
   const int warp = threadIdx.x / 32, lane = threadIdx.x % TEAM;
-  unsigned* word = a.dz;
+  unsigned* word = nullptr;
   if (blockIdx.y == 2) {
-    if (!a.dz) return;
-    for (int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x; r < a.rows; r += (int64_t)gridDim.x * 256)
-      if (a.peak[r] != -INFINITY)
-        see(big, (a.grad_logp && a.targets[r] >= 0 ? fabsf(a.grad_logp[r]) : 0.0f) + (a.grad_entropy ? fabsf(a.grad_entropy[r]) * (fabsf(a.entropy[r]) + 1.0f) : 0.0f));
+    for (int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x; r < a.rows; r += (int64_t)gridDim.x * 256) a.undo_dz[r] = row_share(a, r);
   } else {
     const HeadScanSide m = blockIdx.y ? a.side[1] : a.side[0];
     if (!m.x) return;
@@ -886,7 +905,8 @@ __global__ void __launch_bounds__(256) head_scan_kernel(HeadScanArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; e++) see(row, v[e]);
       }
-      if constexpr (sizeof(T) == 4) {
+      const bool to_part = blockIdx.y == 0 && a.parts;
+      if (sizeof(T) == 4 || to_part) {
         row = __reduce_max_sync(~0u, row);
         if (TEAM > 32) {
           __syncthreads();
@@ -895,6 +915,13 @@ __global__ void __launch_bounds__(256) head_scan_kernel(HeadScanArgs a) {
 #pragma unroll
           for (int i = 0; i < 8; i++) row = max(row, row_most[i]);
         }
+      }
+      if (to_part && lane == 0 && row) {
+        const float share = row_share(a, r);
+        const unsigned there = share == 0.0f ? 0 : kPartBias + max(ilogbf(__uint_as_float(row)), -112) + exponent_of(share);
+        if (there > __ldcg(a.parts + r / a.n)) atomicMax(a.parts + r / a.n, there);
+      }
+      if constexpr (sizeof(T) == 4) {
         const int exponent = scale_exponent(row);
         const float scale = power_of_two(exponent);
         __half* out = m.out + r * a.out_pitch;
@@ -925,36 +952,49 @@ __global__ void __launch_bounds__(256) head_scan_kernel(HeadScanArgs a) {
   }
 }
 
-// Rows of a matrix at a pitch that tensor copies can take, zeros behind their ends: float32 as two float16 pieces, bfloat16 as a float16 one, 16-bit elements
-// (of type uint16_t here) as they are.
+// By which powers of two a matrix is taken in pieces: its own, or what each row lacks to its partition's; none for elements that stay as they are.
+struct HeadScale {
+  const unsigned* largest;
+  const float* undo_dz;
+  const unsigned* parts;
+  int64_t n;
+};
+
+// Rows of a matrix at a pitch that tensor copies can take, zeros behind their ends: float32 as two float16 pieces, bfloat16 and float16 as one, 16-bit elements
+// (of type uint16_t here) as they are.  Rows without a share are zeros.
 template <typename T>
-__global__ void __launch_bounds__(256) head_split_kernel(const T* x, int64_t pitch, int64_t rows, int64_t cols, uint16_t* out, int64_t out_pitch,
-                                                         const unsigned* largest) {
+__global__ void __launch_bounds__(256) head_split_kernel(const T* x, int64_t pitch, int64_t rows, int64_t cols, uint16_t* out, int64_t out_pitch, HeadScale by) {
   pdl_trigger();
   pdl_wait();
   const int64_t words = out_pitch / 8;
-  float scale = 1.0f;
-  constexpr bool kToHalf = std::is_same<T, __nv_bfloat16>::value;
-  if constexpr (sizeof(T) == 4 || kToHalf) scale = power_of_two(scale_exponent(*largest));
+  constexpr bool kAsIs = std::is_same<T, uint16_t>::value;
+  const float whole = by.largest ? power_of_two(scale_exponent(*by.largest)) : 1.0f;
   const bool wide = !(((uintptr_t)x | (uintptr_t)(pitch * sizeof(T))) & 15);
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * words; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / words, c = (i - r * words) * 8;
-    const T* p = x + r * pitch + c;
-    if constexpr (sizeof(T) == 4) {
-      float v[8];
-      load8(x + r * pitch, c, cols, wide, v);
-      store_pieces(v, scale, (__half*)out + r * out_pitch + c, rows * out_pitch);
-    } else if constexpr (kToHalf) {
-      float v[8];
-      load8(x + r * pitch, c, cols, wide, v);
-#pragma unroll
-      for (int e = 0; e < 8; e++) v[e] *= scale;
-      *reinterpret_cast<uint4*>(out + r * out_pitch + c) = Word16<__half>::pack(v);
-    } else {
+    if constexpr (kAsIs) {
       Pack<uint16_t, 8> v;
 #pragma unroll
-      for (int e = 0; e < 8; e++) v.e[e] = c + e < cols ? ((const uint16_t*)p)[e] : (uint16_t)0;
+      for (int e = 0; e < 8; e++) v.e[e] = c + e < cols ? x[r * pitch + c + e] : (uint16_t)0;
       store_pack(out + r * out_pitch + c, v);
+    } else {
+      float v[8], scale = whole;
+      load8(x + r * pitch, c, cols, wide, v);
+      if (by.undo_dz) {
+        const float undo = by.undo_dz[r];
+        const int exponent = undo == 0.0f ? -127 : part_exponent(by.parts[r / by.n]) + exponent_of(undo);
+        scale = exponent < -126 ? 0.0f : power_of_two(min(exponent, 126));        // (above 126 only where a row is nothing but zeros)
+        if (scale == 0.0f)
+#pragma unroll
+          for (int e = 0; e < 8; e++) v[e] = 0.0f;
+      }
+      if constexpr (sizeof(T) == 4) {
+        store_pieces(v, scale, (__half*)out + r * out_pitch + c, rows * out_pitch);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[e] *= scale;
+        *reinterpret_cast<uint4*>(out + r * out_pitch + c) = Word16<__half>::pack(v);
+      }
     }
   }
 }
@@ -1005,6 +1045,7 @@ struct HeadPlan {
   int64_t width;                         // tokens of a piece of the vocabulary
   int h_splits, w_splits;                // parts of the inner dimensions of dh and dW
   int64_t undo_hidden, undo_weight;      // float32: what the pieces' rows are multiplied by
+  int64_t undo_dz;
   int64_t hidden_w, weight_h;            // as they go into dW and, a piece of the vocabulary at a time, into dh
   int64_t words, partial, target_logit, hidden, weight, dz, sums, w_sums, total;
 };
@@ -1116,7 +1157,8 @@ static HeadPlan head_backward_plan(int64_t rows, int64_t cols, int64_t vocab, in
   const int times = (int)((vocab + p.width - 1) / p.width);
   p.h_splits = head_splits(1, rows, cols, std::min(vocab, p.width), dh_products(dtype), times);
   p.w_splits = head_splits(partitions, std::min(vocab, p.width), cols, rows / partitions, grad_dtype == SOLON_BF16 ? 1 : p.pieces + 1, 1);
-  p.words = take(sizeof(HeadWords));
+  p.words = take(sizeof(HeadWords) + partitions * 4);
+  p.undo_dz = take(rows * 4);
   if (p.split) {
     p.hidden = take(p.pieces * rows * p.pitch * 2);
     p.weight = take(p.pieces * vocab * p.pitch * 2);
@@ -1125,10 +1167,8 @@ static HeadPlan head_backward_plan(int64_t rows, int64_t cols, int64_t vocab, in
     p.undo_hidden = take(up(rows, kTile) * 4);
     p.undo_weight = take(up(vocab, kTile) * 4);
   }
-  if (dtype != SOLON_F16) {
-    p.hidden_w = take(p.pieces * rows * p.pitch * 2);
-    p.weight_h = take(p.pieces * p.width * p.pitch * 2);
-  }
+  p.hidden_w = take(p.pieces * rows * p.pitch * 2);
+  if (dtype != SOLON_F16) p.weight_h = take(p.pieces * p.width * p.pitch * 2);
   p.dz = take(p.dz_pieces * rows * p.width * 2);
   if (times > 1 || p.h_splits > 1) p.sums = take(p.h_splits * rows * up(cols, 128) * 4);
   if (p.w_splits > 1) p.w_sums = take((int64_t)p.w_splits * partitions * std::min(vocab, p.width) * up(cols, 128) * 4);
@@ -1211,27 +1251,31 @@ static int head_operand(const void* x, int64_t pitch, int64_t rows, int64_t cols
   const int64_t words = rows * (plan.pitch / 8);
   *out = {to, plan.pitch, rows, 1};
   return launch_dependent(head_split_kernel<uint16_t>, dim3((unsigned)std::min<int64_t>((words + 255) / 256, 16 * sms)), dim3(256), 0, stream, (const uint16_t*)x,
-                          pitch, rows, cols, (uint16_t*)to, plan.pitch, (const unsigned*)nullptr);
+                          pitch, rows, cols, (uint16_t*)to, plan.pitch, HeadScale{});
 }
 
-// float32 or bfloat16 elements in as many float16 pieces as they take, all by the exponent of one number.
-static int head_pieces(const void* x, int64_t pitch, int64_t rows, int64_t cols, bool f32, const HeadPlan& plan, char* to, const unsigned* largest, int sms,
+// Elements in as many float16 pieces as they take.
+static int head_pieces(const void* x, int64_t pitch, int64_t rows, int64_t cols, int dtype, const HeadPlan& plan, char* to, const HeadScale& by, int sms,
                        cudaStream_t stream, HeadOperand* out) {
   const int64_t words = rows * (plan.pitch / 8);
-  const dim3 blocks((unsigned)std::min<int64_t>((words + 255) / 256, 16 * sms));
-  *out = {to, plan.pitch, rows, f32 ? 2 : 1};
-  if (f32) return launch_dependent(head_split_kernel<float>, blocks, dim3(256), 0, stream, (const float*)x, pitch, rows, cols, (uint16_t*)to, plan.pitch, largest);
-  return launch_dependent(head_split_kernel<__nv_bfloat16>, blocks, dim3(256), 0, stream, (const __nv_bfloat16*)x, pitch, rows, cols, (uint16_t*)to, plan.pitch, largest);
+  const dim3 blocks((unsigned)std::min<int64_t>((words + 255) / 256, 16 * sms)), threads(256);
+  *out = {to, plan.pitch, rows, plan.pieces};
+  if (dtype == SOLON_F32)
+    return launch_dependent(head_split_kernel<float>, blocks, threads, 0, stream, (const float*)x, pitch, rows, cols, (uint16_t*)to, plan.pitch, by);
+  if (dtype == SOLON_BF16)
+    return launch_dependent(head_split_kernel<__nv_bfloat16>, blocks, threads, 0, stream, (const __nv_bfloat16*)x, pitch, rows, cols, (uint16_t*)to, plan.pitch, by);
+  return launch_dependent(head_split_kernel<__half>, blocks, threads, 0, stream, (const __half*)x, pitch, rows, cols, (uint16_t*)to, plan.pitch, by);
 }
 
 // Rows wider than 8192 elements are gone through by whole CTAs.
-static int head_scan(const HeadScanArgs& a, bool f32, int sms, cudaStream_t stream) {
-  const bool whole = f32 && a.cols > 8192;
-  const int64_t rows = std::max(a.side[0].rows, a.side[1].x ? a.side[1].rows : 1);
-  const dim3 grid((unsigned)std::min<int64_t>(whole ? rows : (rows + 7) / 8, 8 * sms), a.dz ? 3 : 2);
+static int head_scan(const HeadScanArgs& a, int dtype, int sms, cudaStream_t stream) {
+  const bool whole = dtype == SOLON_F32 && a.cols > 8192;
+  const int64_t rows = std::max(a.rows, a.side[1].x ? a.side[1].rows : 0);
+  const dim3 grid((unsigned)std::min<int64_t>(whole ? rows : (rows + 7) / 8, 8 * sms), a.undo_dz ? 3 : 2);
   if (whole) head_scan_kernel<float, 256><<<grid, 256, 0, stream>>>(a);
-  else if (f32) head_scan_kernel<float, 32><<<grid, 256, 0, stream>>>(a);
-  else head_scan_kernel<__nv_bfloat16, 32><<<grid, 256, 0, stream>>>(a);
+  else if (dtype == SOLON_F32) head_scan_kernel<float, 32><<<grid, 256, 0, stream>>>(a);
+  else if (dtype == SOLON_BF16) head_scan_kernel<__nv_bfloat16, 32><<<grid, 256, 0, stream>>>(a);
+  else head_scan_kernel<__half, 32><<<grid, 256, 0, stream>>>(a);
   SOLON_CUDA_TRY(cudaGetLastError());
   return SOLON_OK;
 }
@@ -1335,8 +1379,8 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
     if (dtype == SOLON_F32) {
       const HeadScanArgs scan = {{{hidden, hidden_pitch, rows, (__half*)(ws + plan.hidden), (float*)(ws + plan.undo_hidden), nullptr},
                                   {weight, weight_pitch, vocab, (__half*)(ws + plan.weight), (float*)(ws + plan.undo_weight), nullptr}},
-                                 cols, plan.pitch, rows, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
-      if ((rc = head_scan(scan, true, sms, stream))) return rc;
+                                 cols, plan.pitch, rows, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, 0};
+      if ((rc = head_scan(scan, dtype, sms, stream))) return rc;
       h = {ws + plan.hidden, plan.pitch, rows, 2};
       w = {ws + plan.weight, plan.pitch, vocab, 2};
     } else if ((rc = head_operand(hidden, hidden_pitch, rows, cols, plan, ws + plan.hidden, sms, stream, &h)) ||
@@ -1441,26 +1485,27 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
   }
   const bool coarse = grad_dtype == SOLON_BF16;          // dW from the first pieces alone
   const int form = (dhidden && !bf16) || (dweight && !coarse) ? kPair : kNearest, dz_pieces = form == kPair ? 2 : 1;
-  const bool hidden_w = !f16 && dweight, weight_h = !f16 && dhidden;      // the two products take float16 pieces by an exponent of a whole matrix
-  SOLON_CUDA_TRY(cudaMemsetAsync(words, 0, sizeof(HeadWords), stream));
-  const HeadScanArgs scan = {{{f32 || (bf16 && dweight) ? hidden : nullptr, hidden_pitch, rows, (__half*)(ws + plan.hidden), (float*)(ws + plan.undo_hidden),
-                               hidden_w ? &words->hidden : nullptr},
-                              {f32 || (bf16 && dhidden) ? weight : nullptr, weight_pitch, vocab, (__half*)(ws + plan.weight), (float*)(ws + plan.undo_weight),
+  const bool weight_h = !f16 && dhidden;
+  const int64_t n = rows / partitions, sums_pitch = up(cols, 128);
+  unsigned* parts = (unsigned*)(words + 1);
+  float* undo_dz = (float*)(ws + plan.undo_dz);
+  SOLON_CUDA_TRY(cudaMemsetAsync(words, 0, sizeof(HeadWords) + partitions * sizeof(unsigned), stream));
+  const HeadScanArgs scan = {{{f32 || dweight ? hidden : nullptr, hidden_pitch, rows, (__half*)(ws + plan.hidden), (float*)(ws + plan.undo_hidden), nullptr},
+                              {f32 || weight_h ? weight : nullptr, weight_pitch, vocab, (__half*)(ws + plan.weight), (float*)(ws + plan.undo_weight),
                                weight_h ? &words->weight : nullptr}},
-                             cols, plan.pitch, rows, targets, peak, grad_logp, grad_entropy, entropy, &words->dz};
-  if ((rc = head_scan(scan, f32, sms, stream))) return rc;
+                             cols, plan.pitch, rows, targets, peak, grad_logp, grad_entropy, entropy, undo_dz, dweight ? parts : nullptr, n};
+  if ((rc = head_scan(scan, dtype, sms, stream))) return rc;
   HeadOperand h = {ws + plan.hidden, plan.pitch, rows, 2}, w = {ws + plan.weight, plan.pitch, vocab, 2};
   if (!f32 && ((rc = head_operand(hidden, hidden_pitch, rows, cols, plan, ws + plan.hidden, sms, stream, &h)) ||
                (rc = head_operand(weight, weight_pitch, vocab, cols, plan, ws + plan.weight, sms, stream, &w))))
     return rc;
 
-  const int64_t n = rows / partitions, sums_pitch = up(cols, 128);
   // as rows along the inner dimension: h and W for the logits, dz for dh; across it: W for dh, dz and h for dW
   CUtensorMap map_h, map_w, map_w_across, map_h_across, map_dz, map_dz_across, map_dz_out;
   HeadOperand hw = h, wh = w;              // as they go into dW and dh
-  if (hidden_w && (rc = head_pieces(hidden, hidden_pitch, rows, cols, f32, plan, ws + plan.hidden_w, &words->hidden, sms, stream, &hw))) return rc;
+  if (dweight && (rc = head_pieces(hidden, hidden_pitch, rows, cols, dtype, plan, ws + plan.hidden_w, {nullptr, undo_dz, parts, n}, sms, stream, &hw))) return rc;
   // (a map across the inner dimension goes with the tiles: copies of 128 columns need 128 of them in a CTA's tile, and whole blocks of 64 in memory)
-  const bool whole = cols % kBlock == 0 || plan.split, hw_whole = whole || hidden_w, wh_whole = whole || weight_h;
+  const bool whole = cols % kBlock == 0 || plan.split, hw_whole = whole || dweight, wh_whole = whole || weight_h;
   auto across = [&](CUtensorMap* map, const void* p, bool by_blocks, int64_t rows, int64_t slabs, int64_t pitch, int64_t slab) {
     return by_blocks ? tensor_map_by_blocks(map, p, false, cols, rows, slabs, pitch, slab) : tensor_map(map, p, false, cols, rows, slabs, pitch, slab, kBlock);
   };
@@ -1478,11 +1523,13 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
   base.grad_logp = grad_logp;
   base.grad_entropy = grad_entropy;
   base.vocab = vocab;
+  base.undo_dz = undo_dz;
+  base.parts = parts;
   for (int64_t first = 0; first < vocab; first += plan.width) {
     const int64_t width = std::min(plan.width, vocab - first), pitch = up(width, kBlock);
     const bool h_narrow = narrow(cols, pitch / kBlock * dh_products(dtype));
-    if (weight_h && (rc = head_pieces((const char*)weight + first * weight_pitch * (f32 ? 4 : 2), weight_pitch, width, cols, f32, plan, ws + plan.weight_h,
-                                      &words->weight, sms, stream, &wh)))
+    if (weight_h && (rc = head_pieces((const char*)weight + first * weight_pitch * (f32 ? 4 : 2), weight_pitch, width, cols, dtype, plan, ws + plan.weight_h,
+                                      {&words->weight, nullptr, nullptr, 0}, sms, stream, &wh)))
       return rc;
     const char* w_across = wh.p + (weight_h ? 0 : first * wh.pitch * 2);
     if (!tensor_map(&map_dz, ws + plan.dz, false, pitch, rows, dz_pieces, pitch, rows * pitch, kRows) ||
@@ -1515,7 +1562,8 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
       a.b_by_blocks = wh_whole && !h_narrow;
       a.k_blocks = (int)((pitch / kBlock + a.splits - 1) / a.splits);
       head_pairs(a, bf16 ? 1 : 2, wh.pieces, 1, 1);
-      a.scaled = f16 ? 4 : 6;
+      a.weight_scaled = weight_h;
+      a.undo_m = undo_dz;
       a.sums = (float*)(ws + plan.sums);
       a.sums_pitch = sums_pitch;
       a.load_sums = first > 0;
@@ -1543,7 +1591,6 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
       a.sums_pitch = sums_pitch;
       a.store_sums = a.splits > 1;
       head_pairs(a, coarse ? 1 : 2, coarse ? 1 : hw.pieces, partitions, partitions);
-      a.scaled = f16 ? 4 : 5;
       a.out = (char*)dweight + first * cols * grad_size;
       a.out_pitch = cols;
       a.out_slab = partitions > 1 ? grad_pitch : 0;

@@ -203,3 +203,62 @@ def test_a_large_row_or_token_leaves_the_others_alone(rows, vocab):
         size = dz.abs() @ wd.abs()
         dtol = dzt @ wd.abs() + (2.0 ** -20 + (64 + vocab / 256) * U) * size + 2.0 ** -49 * (g.double().abs()[:, None] * wd.abs().sum(0) + wd.abs().max() * dz.abs().sum(1)[:, None])
         _close(dh[others], (dz @ wd)[others], dtol[others], "dhidden")
+
+
+@pytest.mark.parametrize("dtype,grad", [("f32", "f32"), ("f16", "f32"), ("bf16", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("n", [4, 150])
+def test_partitions_are_independent(n, dtype, grad):
+    """Hidden states and factors of one partition, however large, change no bit of what the others get; nor does a row's factor change another row's dh."""
+    parts, cols, vocab = 3, 72, 19_000 if n == 4 else 500
+    rows = n * parts
+    h, w, t = _leaning(rows, cols, vocab, dtype, 2)
+    peak, log_sum, _ = _stats(h, w)
+    g = -torch.rand(rows, device="cuda", generator=_gen(1))
+
+    def call():
+        dw = torch.empty((parts, vocab * cols), dtype=TYPES[grad], device="cuda")
+        return binding.solon_head_logprobs_backward(h, w, t, peak, log_sum, g, partitions=parts, dweight=dw)
+
+    dh, dw = call()
+    h[n:2 * n] *= 1e3 if dtype == "f16" else 1e10
+    g[n:2 * n] *= 1e9
+    peak[n:2 * n], log_sum[n:2 * n] = (s[n:2 * n] for s in _stats(h, w)[:2])
+    other_dh, other_dw = call()
+    keep = torch.ones(rows, dtype=torch.bool, device="cuda")
+    keep[n:2 * n] = False
+    assert torch.equal(other_dh[keep], dh[keep]) and torch.equal(other_dw[0], dw[0]) and torch.equal(other_dw[2], dw[2])
+    g[0] *= 1e9
+    last = call()[0]
+    keep[0] = False
+    assert torch.equal(last[keep], dh[keep])
+
+
+@pytest.mark.parametrize("dtype,grad", [("f32", "f32"), ("f16", "f64"), ("bf16", "f32"), ("bf16", "bf16")])
+def test_rows_of_zeros_and_partitions_without_a_share(dtype, grad):
+    """Hidden states of zeros beside tiny and large factors, a partition of such rows alone, one without a target: zeros, and the others as they are."""
+    n, parts, cols, vocab = 40, 4, 64, 300
+    rows = n * parts
+    h, w, t = _leaning(rows, cols, vocab, dtype, 7, 2.0)
+    h[3] = 0.0
+    h[n:2 * n] = 0.0
+    t[2 * n:3 * n] = -1
+    g = -torch.rand(rows, device="cuda", generator=_gen(1))
+    g[3] = 1e-36
+    g[n:2 * n:2] = 1e-30
+    g[0] = -1e6
+    h[1] *= 2.0 ** -10
+    peak, log_sum, _ = _stats(h, w)
+    dw = torch.full((parts, vocab * cols), 7.0, dtype=TYPES[grad], device="cuda")
+    dh, _ = binding.solon_head_logprobs_backward(h, w, t, peak, log_sum, g, partitions=parts, dweight=dw)
+    assert torch.isfinite(dw).all()
+    assert (dw[1:3] == 0).all() and (dh[2 * n:3 * n] == 0).all()
+    dz, _ = _dlogits(h, w, t, peak, log_sum, g)
+    for k in (0, 3):
+        want = (dz[k * n:(k + 1) * n].t() @ h[k * n:(k + 1) * n].double()).reshape(-1)
+        assert float((dw[k].double() - want).norm()) <= (2.0 ** -8 if grad == "bf16" else 1e-5) * float(want.norm())
+    want = dz @ w.double()
+    # the factor of 1e6 brings row 0 of dh to 1e6 |w| of some 2e5: beyond float16 (65504), where infinity is the nearest
+    most = torch.finfo(dh.dtype).max
+    assert torch.isfinite(dh)[want.abs() < most * (1 - 2.0 ** -8)].all()
+    some = (want.abs().amax(1) > 0) & (want.abs().amax(1) < most * (1 - 2.0 ** -8))
+    assert ((dh.double() - want).norm(dim=1)[some] <= (1e-5 if dtype == "f32" else 2.0 ** -8) * want.norm(dim=1)[some] + (2.0 ** -20 if dtype == "f16" else 0.0)).all()
