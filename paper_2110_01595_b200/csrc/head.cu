@@ -232,7 +232,7 @@ __device__ __forceinline__ void dz_row(const DzRow& r, float (&v)[N], uint32_t k
       Float2 d = pack2(exp2_fast(x), exp2_fast(y));
       if (ENTROPY) {                         // (p = 0 where log p is -infinity, and no product with it)
         unpack2(add2(x2, ml), x, y);
-        d = mul2(d, fma2(add2(pack2(fmaxf(x, -1e30f), fmaxf(y, -1e30f)), h2), mh, mg));
+        d = mul2(d, fma2(add2(pack2(fmaxf(x, kLeastLogp), fmaxf(y, kLeastLogp)), h2), mh, mg));
       } else d = mul2(d, mg);
       unpack2(d, v[i], v[i + 1]);
       if (i % 16 == 14) in_turn(mp, d);
@@ -577,7 +577,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
         float lp = 0.0f, d = 0.0f;
         if (hit) {                           // the target's element, with its g
           lp = (z - r.peak) - r.log_sum;
-          d = active ? fmaf(exp2_fast(lp * kLog2e), fmaf(-r.gh, lp + r.entropy, -r.g), r.g) : 0.0f;
+          d = active ? fmaf(exp2_fast(lp * kLog2e), fmaf(-r.gh, fmaxf(lp, kLeastLogp) + r.entropy, -r.g), r.g) : 0.0f;
         }
         const int place = hit ? (int)token : -1;
         const DzOut out = {&maps.out, stage, col, row0, a.dz_pitch - col, lane, place, d};

@@ -185,7 +185,7 @@ __global__ void __launch_bounds__(kCtaThreads, NR <= 16 ? 2 : 1) small_logits_ke
 #pragma unroll
         for (int e = 0; e < 4; e++) {
           const float g = of_row[2][n + e], lp = (d[e] - of_row[0][n + e]) - of_row[1][n + e], p = exp2_fast(lp * kLog2e);
-          float x = -p * fmaf(of_row[3][n + e], fmaxf(lp, -1e30f) + of_row[4][n + e], g);
+          float x = -p * fmaf(of_row[3][n + e], fmaxf(lp, kLeastLogp) + of_row[4][n + e], g);
           if (lp != lp) x = lp;
           if (target[n + e] == v) x += g;
           d[e] = of_row[5][n + e] != 0.0f ? x : 0.0f;

@@ -6,6 +6,7 @@
 namespace solon {
 
 constexpr float kLog2e = 1.44269504088896f;
+constexpr float kLeastLogp = -1e4f;      // p is 0 long before: log p below it makes finite products with what p is multiplied by
 
 struct RowSums {
   float m, s, a;

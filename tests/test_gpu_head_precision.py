@@ -262,3 +262,22 @@ def test_rows_of_zeros_and_partitions_without_a_share(dtype, grad):
     assert torch.isfinite(dh)[want.abs() < most * (1 - 2.0 ** -8)].all()
     some = (want.abs().amax(1) > 0) & (want.abs().amax(1) < most * (1 - 2.0 ** -8))
     assert ((dh.double() - want).norm(dim=1)[some] <= (1e-5 if dtype == "f32" else 2.0 ** -8) * want.norm(dim=1)[some] + (2.0 ** -20 if dtype == "f16" else 0.0)).all()
+
+
+@pytest.mark.parametrize("rows", [2, 300])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_a_masked_token_as_the_target(rows, dtype):
+    """A token masked by -infinity that is a row's target all the same: log p is -infinity, dz = g there."""
+    cols, vocab = 64, 500
+    h, w, t = _leaning(rows, cols, vocab, dtype, 8, 1.0)
+    h[:] = h.abs() + 0.5
+    w[7] = -INF
+    t[:] = 7
+    got = binding.solon_head_logprobs(h, w, t)
+    assert (got.logp == -INF).all() and torch.isfinite(got.log_sum).all() and torch.isfinite(got.entropy).all()
+    g = torch.full((rows,), -0.5, device="cuda")
+    for entropy, gh in ((None, None), (got.entropy, torch.zeros(rows, device="cuda")), (got.entropy, torch.full((rows,), 0.125, device="cuda"))):
+        _, dw = binding.solon_head_logprobs_backward(h, w, t, got.peak, got.log_sum, g, entropy, gh, hidden_grad=False)
+        x = -0.5 * h.double().sum(0)
+        _close(dw.view(vocab, cols)[7], x, 2.0 ** -18 * x.abs(), "dweight")
+        assert torch.isfinite(dw).all()
