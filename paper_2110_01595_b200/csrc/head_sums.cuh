@@ -16,7 +16,8 @@ struct RowSums {
 __device__ __forceinline__ RowSums join(const RowSums& x, const RowSums& y) {
   RowSums r;
   r.m = max_nan(x.m, y.m);
-  const float cx = x.m == -INFINITY ? 0.0f : x.m - r.m, cy = y.m == -INFINITY ? 0.0f : y.m - r.m;    // (no logits, or none above -infinity: s = a = 0)
+  // (no logits, or none above -infinity: s = a = 0; and a distance that leaves nothing of a set is kept finite times its sum: 0 times infinity would be NaN)
+  const float cx = x.m == -INFINITY ? 0.0f : max_nan(x.m - r.m, -1e20f), cy = y.m == -INFINITY ? 0.0f : max_nan(y.m - r.m, -1e20f);
   const float ex = exp2f(cx * kLog2e), ey = exp2f(cy * kLog2e);
   r.s = x.s * ex + y.s * ey;
   r.a = fmaf(x.s, cx, x.a) * ex + fmaf(y.s, cy, y.a) * ey;

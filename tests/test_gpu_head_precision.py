@@ -264,6 +264,37 @@ def test_rows_of_zeros_and_partitions_without_a_share(dtype, grad):
     assert ((dh.double() - want).norm(dim=1)[some] <= (1e-5 if dtype == "f32" else 2.0 ** -8) * want.norm(dim=1)[some] + (2.0 ** -20 if dtype == "f16" else 0.0)).all()
 
 
+@pytest.mark.parametrize("rows,vocab", [(1, 700), (3, 700), (20, 19_000), (40, 700), (300, 700)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_huge_finite_logits(rows, vocab, dtype):
+    """Logits of -3e37 beside ordinary ones: tokens with p = 0, no NaN (their number times their distance is beyond float32)."""
+    cols = 40
+    h, w, t = _leaning(rows, cols, vocab, dtype, 5, 1.0)
+    w[:, 0] = 0.0
+    h[:, 0] = 1.0
+    keep = torch.zeros(vocab, dtype=torch.bool, device="cuda")
+    keep[::300] = True                                            # tiles with and without an ordinary token
+    w[~keep, 0] = -3e37
+    got = binding.solon_head_logprobs(h, w, None)
+    z, tol = _logits(h, w[keep])
+    lp = torch.log_softmax(z, 1)
+    most = tol.amax(1)
+    _close(got.peak, z.amax(1), most + U * z.amax(1).abs(), "peak")
+    _close(got.log_sum, torch.logsumexp(z, 1) - z.amax(1), 2 * most + 200 * U, "log_sum")
+    _close(got.entropy, -(lp.exp() * lp).sum(1), 20 * most + 1000 * U, "entropy")
+    # gradients: none from those tokens, with entropy factors too
+    g, gh = torch.full((rows,), -0.5, device="cuda"), torch.full((rows,), 0.25, device="cuda")
+    t = torch.zeros(rows, dtype=torch.int64, device="cuda")
+    t[-1] = 1                                                     # a target with p = 0
+    _, dw = binding.solon_head_logprobs_backward(h, w, t, got.peak, got.log_sum, g, got.entropy, gh, hidden_grad=False)
+    dw = dw.view(vocab, cols)
+    assert torch.isfinite(dw).all()
+    gone = ~keep
+    gone[1] = False
+    assert (dw[gone] == 0).all()
+    _close(dw[1], -0.5 * h[-1].double(), 2.0 ** -20 * h[-1].double().abs(), "a target of p = 0")
+
+
 @pytest.mark.parametrize("rows", [2, 300])
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 def test_a_masked_token_as_the_target(rows, dtype):
