@@ -55,18 +55,23 @@ class TokenLoop:
         self.mask = torch.empty(plan.P, dtype=torch.uint8, device="cuda")
 
     def _forward(self, tokens):
+        if tokens.dtype not in (torch.int32, torch.int64) or tokens.dim() > 1:
+            raise ValueError(f"tokens must be a vector of int32 or int64, got {tuple(tokens.shape)} {tokens.dtype}")
+        tokens = tokens.reshape(-1).long().contiguous()
         hidden = binding.solon_embedding_forward(self.embed, tokens)
-        return hidden, *binding.solon_layernorm_forward(hidden, self.weight, self.bias, eps=LN_EPS)
+        return tokens, hidden, *binding.solon_layernorm_forward(hidden, self.weight, self.bias, eps=LN_EPS)
 
     def partition_gradients(self, tokens, targets):
         """Fills the gradient matrix with each partition's gradient of its mean loss -log p(target); returns the rows' log p.
-        tokens, targets: P x n int64; a negative target counts in no gradient (n still divides)."""
+        tokens: P x n int32 or int64, targets: P x n int64; a negative target counts in no gradient (n still divides).  A negative token
+        (padding) is a row of zeros before the layer norm and has no embedding to learn; what its target says to the other parameters counts, so
+        padded positions want negative targets too.  A token beyond the vocabulary makes its row, and its partition's gradient, NaN."""
         P, n = tokens.shape
         if P != self.plan.P or targets.shape != tokens.shape:
             raise ValueError("tokens and targets must be P x n")
         V, C = self.vocab, self.width
-        flat_targets = targets.reshape(-1)
-        hidden, normed, mean, rstd = self._forward(tokens.reshape(-1))
+        flat_targets = targets.reshape(-1).contiguous()
+        flat_tokens, hidden, normed, mean, rstd = self._forward(tokens.reshape(-1))
         g = torch.full((P * n,), -1.0 / n, device="cuda")
         o = self.offsets
         if self.fused_head:
@@ -82,7 +87,7 @@ class TokenLoop:
             dnormed = dlogits @ self.head
         dhidden, _, _ = binding.solon_layernorm_backward(dnormed, hidden, mean, rstd, self.weight, partitions=P,
                                                          dweight=self.grads[:, o[1]:o[2]], dbias=self.grads[:, o[2]:o[3]])
-        binding.solon_embedding_backward(dhidden, tokens.reshape(-1), V, partitions=P, dweight=self.grads[:, :o[1]])
+        binding.solon_embedding_backward(dhidden, flat_tokens, V, partitions=P, dweight=self.grads[:, :o[1]])
         return scored.logp
 
     def step(self, tokens, targets, attackers=()):
@@ -97,6 +102,7 @@ class TokenLoop:
         return logp
 
     def next_tokens(self, tokens, top_k: int = 5):
-        """What the model expects after each token: (ids, log probabilities) of the top_k likeliest, and the entropy."""
-        scored = binding.solon_token_logprobs(self._forward(tokens)[1] @ self.head.t(), top_k=top_k)
+        """What the model expects after each token: (ids, log probabilities) of the top_k likeliest, and the entropy.
+        tokens: a vector of int32 or int64, as partition_gradients takes them."""
+        scored = binding.solon_token_logprobs(self._forward(tokens)[2] @ self.head.t(), top_k=top_k)
         return scored.top_ids, scored.top_logp, scored.entropy
