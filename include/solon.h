@@ -366,7 +366,7 @@ int solon_token_logprobs_backward(const void* logits, int64_t pitch, int dtype, 
  *   weight  device, vocab x cols of `dtype` (SOLON_F32, SOLON_BF16 or SOLON_F16)
  *   tokens  device, rows int64: a negative one gives a row of zeros, one >= vocab a row of NaN (neither is looked up)
  *   out     device, rows x cols of `dtype` (output); scale = 1 copies the bits, otherwise one rounding
- * cols <= SOLON_MAX_WIDTH.  rows = 0 does nothing. */
+ * cols <= SOLON_MAX_WIDTH.  rows = 0 does nothing.  In this and the three operators below no output may share a byte with an input or another output (refused). */
 int solon_embedding_forward(const void* weight, int64_t weight_pitch, int dtype, const int64_t* tokens, int64_t rows, int64_t cols, int64_t vocab,
                             double scale, void* out, int64_t out_pitch, void* cuda_stream);
 
@@ -399,7 +399,7 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
                         void* cuda_stream);
 
 /* Its gradients: with dlogits as solon_token_logprobs_backward has it (and recomputed logits),
- *   dhidden = dlogits * weight           device, rows x cols of `dtype` (output; NULL: not wanted; neither output may be an input)
+ *   dhidden = dlogits * weight           device, rows x cols of `dtype` (output; NULL: not wanted)
  *   dweight_k = dlogits_k^T * hidden_k   device (output; NULL: not wanted): row k of the partition-gradient matrix from dweight[k * grad_pitch] on,
  *                                        vocab x cols elements of `grad_dtype` (SOLON_F32, SOLON_F64 or SOLON_BF16), over the rows of partition k
  *   peak, log_sum, entropy, grad_logp, grad_entropy  as in solon_token_logprobs_backward

@@ -562,6 +562,8 @@ int solon_embedding_forward(const void* weight, int64_t weight_pitch, int dtype,
   if (rows == 0) return SOLON_OK;
   if (!matrix_ok(weight, weight_pitch, vocab, cols, dtype) || !matrix_ok(out, out_pitch, rows, cols, dtype) || !tokens || ((uintptr_t)tokens & 7))
     return SOLON_ERR_INVALID_ARG;
+  const Extent to = extent(out, rows, cols, out_pitch, element_size(dtype));
+  if (meet(to, extent(weight, vocab, cols, weight_pitch, element_size(dtype))) || meet(to, extent(tokens, 1, rows, rows, 8))) return SOLON_ERR_INVALID_ARG;
   const EmbForwardArgs a = {weight, tokens, out, vocab > 1 ? weight_pitch : cols, rows > 1 ? out_pitch : cols, rows, cols, vocab, (float)scale, 0};
   cudaStream_t stream = (cudaStream_t)cuda_stream;
   if (dtype == SOLON_F32) return emb_forward_t<float>(a, stream);
@@ -582,6 +584,8 @@ int solon_embedding_backward(const void* dy, int64_t dy_pitch, int dtype, const 
   if (grad_dtype != SOLON_F32 && grad_dtype != SOLON_F64 && grad_dtype != SOLON_BF16) return SOLON_ERR_INVALID_ARG;
   if (!matrix_ok(dweight, grad_pitch, partitions, vocab * cols, grad_dtype)) return SOLON_ERR_INVALID_ARG;
   if (rows > 0 && (!matrix_ok(dy, dy_pitch, rows, cols, dtype) || !tokens || ((uintptr_t)tokens & 7))) return SOLON_ERR_INVALID_ARG;
+  const Extent to = extent(dweight, partitions, vocab * cols, grad_pitch, element_size(grad_dtype));
+  if (rows > 0 && (meet(to, extent(dy, rows, cols, dy_pitch, element_size(dtype))) || meet(to, extent(tokens, 1, rows, rows, 8)))) return SOLON_ERR_INVALID_ARG;
   if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < emb_back_workspace(rows, cols, vocab, partitions)) return SOLON_ERR_INVALID_ARG;
   int sms = 0, rc;
   if ((rc = current_sms(&sms))) return rc;

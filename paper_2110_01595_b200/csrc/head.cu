@@ -1344,6 +1344,10 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
   if (!matrix_ok(hidden, hidden_pitch, rows, cols, dtype) || !matrix_ok(weight, weight_pitch, vocab, cols, dtype)) return SOLON_ERR_INVALID_ARG;
   if ((logp && !targets) || ((uintptr_t)targets & 7) || (((uintptr_t)logp | (uintptr_t)entropy | (uintptr_t)peak | (uintptr_t)log_sum) & 3))
     return SOLON_ERR_INVALID_ARG;
+  for (const float* out : {logp, entropy, peak, log_sum})
+    if (meet(extent(out, 1, rows, rows, 4), extent(targets, 1, rows, rows, 8)) || meet(extent(out, 1, rows, rows, 4), extent(hidden, rows, cols, hidden_pitch, element_size(dtype))) ||
+        meet(extent(out, 1, rows, rows, 4), extent(weight, vocab, cols, weight_pitch, element_size(dtype))))
+      return SOLON_ERR_INVALID_ARG;
   const bool aligned = aligned16(hidden, hidden_pitch, rows, dtype) && aligned16(weight, weight_pitch, vocab, dtype);
   const HeadPlan plan = head_forward_plan(rows, cols, vocab, dtype, aligned);
   if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < plan.total) return SOLON_ERR_INVALID_ARG;
@@ -1448,7 +1452,14 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
       (((uintptr_t)peak | (uintptr_t)log_sum | (uintptr_t)entropy | (uintptr_t)grad_logp | (uintptr_t)grad_entropy) & 3))
     return SOLON_ERR_INVALID_ARG;
   if (!dhidden && !dweight) return SOLON_OK;
-  if ((dhidden && (dhidden == hidden || dhidden == weight)) || (dweight && (dweight == hidden || dweight == weight))) return SOLON_ERR_INVALID_ARG;
+  const Extent outs[2] = {extent(dhidden, rows, cols, dhidden_pitch, element_size(dtype)), extent(dweight, partitions, vocab * cols, grad_pitch, element_size(grad_dtype))};
+  const Extent ins[8] = {extent(hidden, rows, cols, hidden_pitch, element_size(dtype)), extent(weight, vocab, cols, weight_pitch, element_size(dtype)),
+                         extent(targets, 1, rows, rows, 8), extent(peak, 1, rows, rows, 4), extent(log_sum, 1, rows, rows, 4),
+                         extent(entropy, 1, rows, rows, 4), extent(grad_logp, 1, rows, rows, 4), extent(grad_entropy, 1, rows, rows, 4)};
+  for (const Extent& out : outs)
+    for (const Extent& in : ins)
+      if (meet(out, in)) return SOLON_ERR_INVALID_ARG;
+  if (meet(outs[0], outs[1])) return SOLON_ERR_INVALID_ARG;
   const bool aligned = aligned16(hidden, hidden_pitch, rows, dtype) && aligned16(weight, weight_pitch, vocab, dtype);
   const HeadPlan plan = head_backward_plan(rows, cols, vocab, partitions, dtype, grad_dtype, aligned);
   if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < plan.total) return SOLON_ERR_INVALID_ARG;
