@@ -417,6 +417,10 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
                                  const float* grad_logp, const float* grad_entropy, void* dhidden, int64_t dhidden_pitch, void* dweight, int64_t grad_pitch,
                                  int grad_dtype, void* workspace, int64_t workspace_bytes, void* cuda_stream);
 
+/* Health of the two calls above on the current device so far: synchronises the stream, then returns SOLON_OK, SOLON_ERR_INTERNAL (a bounded wait
+ * inside a product ran out; the results that it was for are NaN) or SOLON_ERR_CUDA. */
+int solon_head_status(void* cuda_stream);
+
 /* AdamW over all tensors of a model at once: per weight, with g' = grad_scale * clip * gradient and t the step's number,
  *   m <- beta1 m + (1 - beta1) g'        v <- beta2 v + (1 - beta2) g'^2
  *   p <- p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)

@@ -98,6 +98,7 @@ SIGNATURES = {
     "solon_head_logprobs_backward_workspace": (c_int64, [c_int64, c_int64, c_int64, c_int, c_int, c_int, c_int]),
     "solon_head_logprobs_backward": (c_int, [c_void_p, c_int64, c_void_p, c_int64, c_int, c_void_p, c_int64, c_int64, c_int64, c_int, c_void_p, c_void_p,
                                              c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_int, c_void_p, c_int64, c_void_p]),
+    "solon_head_status": (c_int, [c_void_p]),
     "solon_adamw_state_blocks": (c_int64, [c_int, POINTER(c_int64)]),
     "solon_adamw_create": (c_int, [c_int, POINTER(c_int64), POINTER(c_void_p), POINTER(c_void_p), POINTER(c_float), c_int, c_void_p, c_void_p, c_void_p,
                                    c_double, c_double, c_double, c_uint64, POINTER(c_void_p)]),
@@ -556,6 +557,14 @@ def solon_head_logprobs_backward(hidden, weight, targets, peak, log_sum, grad_lo
                                               row_vector(grad_entropy, "grad_entropy"), pdh, dh_pitch, pdw, grad_pitch, grad_code, workspace.data_ptr(),
                                               n_bytes, stream), "solon_head_logprobs_backward")
     return dhidden, dweight
+
+
+def solon_head_status() -> int:
+    """Health of solon_head_logprobs and its backward on the current device so far, after synchronising the current stream: 0, or ERR_INTERNAL if a
+    bounded wait inside a product ran out (the results that it was for are NaN)."""
+    import torch
+
+    return lib().solon_head_status(torch.cuda.current_stream().cuda_stream)
 
 
 class AdamW:

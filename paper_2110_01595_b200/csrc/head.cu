@@ -54,12 +54,14 @@ enum HeadMode { kStats, kFewRows, kDz, kDhidden, kDweight };
 // have one for dh.  dW of a partition adds up rows: there row i of h carries what its dz lacks to the partition's exponent, so that what counts is |dz_i| |h_i|
 // against the partition's largest, and partitions say nothing about one another.
 
-// What the scan of a call leaves behind: the bits of the weights' largest finite magnitude, and a flag of waits that ran out.  Behind it a word a partition: the
-// exponent of its largest |dz_i| |h_i| over that of dz (0: no row with a share).
+// What the scan of a call leaves behind: the bits of the weights' largest finite magnitude.  Behind it a word a partition: the exponent of its largest
+// |dz_i| |h_i| over that of dz (0: no row with a share).
 struct HeadWords {
   unsigned weight;
-  int status;
 };
+
+// Set by a wait that ran out, and never cleared.
+__device__ int head_wait_status;
 
 __device__ __forceinline__ int scale_exponent(unsigned largest) {       // 2^s brings the largest magnitude into [2^14, 2^15)
   return largest ? min(126, 14 - ilogbf(__uint_as_float(largest))) : 0;
@@ -90,7 +92,6 @@ struct HeadArgs {
   int narrow;                            // tiles of 128 columns
   int b_by_blocks;                       // B's map takes 128 columns a copy, where its rows lie across the inner dimension
   const HeadWords* words;
-  HeadWords* flags;
   int weight_scaled;                     // kDhidden: the weights carry a power of two
   const unsigned* parts;                 // kDweight: the partitions' words
   const float *undo_m, *undo_n;          // what the product's rows and columns are multiplied by (NULL: nothing)
@@ -324,7 +325,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
   const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
   const uint32_t tiles_all = (uint32_t)a.m_tiles * a.n_tiles * a.slabs;
   const int blocks = a.products * a.k_blocks;
-  int* status = &a.flags->status;
+  int* status = &head_wait_status;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; i++) {
@@ -1074,7 +1075,6 @@ static HeadPlan head_forward_plan(int64_t rows, int64_t cols, int64_t vocab, int
     at += up(bytes, 256);
     return here;
   };
-  p.words = take(sizeof(HeadWords));
   p.target_logit = take(rows * 4);
   if (p.row_kernel) {
     p.slots = kRowBlocks;
@@ -1331,6 +1331,15 @@ using namespace solon;
 
 extern "C" {
 
+int solon_head_status(void* cuda_stream) {
+  int status = 0;
+  void* at = nullptr;
+  SOLON_CUDA_TRY(cudaGetSymbolAddress(&at, head_wait_status));
+  SOLON_CUDA_TRY(cudaMemcpyAsync(&status, at, sizeof(int), cudaMemcpyDeviceToHost, (cudaStream_t)cuda_stream));
+  SOLON_CUDA_TRY(cudaStreamSynchronize((cudaStream_t)cuda_stream));
+  return status ? SOLON_ERR_INTERNAL : SOLON_OK;
+}
+
 int64_t solon_head_logprobs_workspace(int64_t rows, int64_t cols, int64_t vocab, int dtype, int aligned) {
   if (!token_dtype(dtype) || !head_sizes_ok(rows, cols, vocab)) return SOLON_ERR_INVALID_ARG;
   return rows == 0 ? 0 : head_forward_plan(rows, cols, vocab, dtype, aligned != 0).total;
@@ -1356,7 +1365,6 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
   const int64_t slots = plan.few ? std::min<int64_t>(plan.slots, 8 * (sms / 2)) : plan.slots;
   cudaStream_t stream = (cudaStream_t)cuda_stream;
   char* ws = (char*)workspace;
-  HeadWords* words = (HeadWords*)(ws + plan.words);
   if (plan.row_kernel) {
     const HeadRowsArgs a = {hidden, weight, hidden_pitch, vocab > 1 ? weight_pitch : cols, cols, vocab, targets, (int)rows, (int)rows_padded(cols),
                             (float*)(ws + plan.partial), (float*)(ws + plan.target_logit)};
@@ -1402,7 +1410,6 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
     a.slabs = a.splits = 1;
     a.k_blocks = (int)((cols + kBlock - 1) / kBlock);
     head_pairs(a, h.pieces, w.pieces, 1, 1);
-    a.words = a.flags = words;
     if (dtype == SOLON_F32) {
       a.undo_m = (const float*)(ws + plan.undo_hidden);
       a.undo_n = (const float*)(ws + plan.undo_weight);
@@ -1526,7 +1533,7 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
     return SOLON_ERR_CUDA;
   HeadArgs base = {};
   base.slabs = base.splits = 1;
-  base.words = base.flags = words;
+  base.words = words;
   base.targets = targets;
   base.peak = peak;
   base.log_sum = log_sum;

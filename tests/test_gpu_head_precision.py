@@ -312,3 +312,11 @@ def test_a_masked_token_as_the_target(rows, dtype):
         x = -0.5 * h.double().sum(0)
         _close(dw.view(vocab, cols)[7], x, 2.0 ** -18 * x.abs(), "dweight")
         assert torch.isfinite(dw).all()
+
+
+def test_health():
+    """No wait has run out in any call of this process (one that had would have left NaN where its results belong, and this said so)."""
+    h, w, t = _leaning(300, 64, 700, "bf16", 1)
+    r = binding.solon_head_logprobs(h, w, t)
+    binding.solon_head_logprobs_backward(h, w, t, r.peak, r.log_sum, torch.full((300,), -1.0, device="cuda"))
+    assert binding.solon_head_status() == binding.OK
