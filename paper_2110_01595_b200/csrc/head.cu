@@ -377,6 +377,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
           }
         }
       }
+      // the last products' arrivals at this CTA's barriers come before it ends
+      if (warp == 0)
+        for (int i = 0; i < kStages && fine; i++) {
+          fine = waited(empty + s, phase ^ 1, abort_flag, status);
+          if (++s == kStages) s = 0, phase ^= 1;
+        }
     } else if (warp == 1 && lane == 0 && rank == 0) {
       constexpr uint32_t idesc = instruction(BF16, kAlongA, kAlongB, BN);
       int s = 0, half = 0;
