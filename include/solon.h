@@ -410,7 +410,7 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
  * gradients.  The other factor is taken in float16 pieces as well, as many as the elements have above (bfloat16 gradients: one): weight by a power of two of its largest in dhidden (float16
  * as it is), hidden in dweight by powers of two that make the largest product of a row's bound and its elements in the partition the measure.  No row's dhidden depends on
  * another row, no partition's dweight on another partition.
- * rows = 0: dweight becomes 0.  hidden has to be finite in rows that count in no gradient, too: they are multiplied by zeros. */
+ * rows = 0: dweight becomes 0.  Rows that count in no gradient may hold anything in hidden. */
 int64_t solon_head_logprobs_backward_workspace(int64_t rows, int64_t cols, int64_t vocab, int partitions, int dtype, int grad_dtype, int aligned);
 int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const void* weight, int64_t weight_pitch, int dtype, const int64_t* targets,
                                  int64_t rows, int64_t cols, int64_t vocab, int partitions, const float* peak, const float* log_sum, const float* entropy,

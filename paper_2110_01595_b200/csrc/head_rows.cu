@@ -47,6 +47,14 @@ __global__ void __launch_bounds__(256) small_turn_kernel(const float* hidden, in
   }
 }
 
+// Row n's factors, and whether it has a share: g counts only with a target, and nothing counts in a row of which nothing is left.
+__device__ __forceinline__ bool small_share(const HeadSmallArgs& a, int n, float& g, float& gh) {
+  const bool there = n < a.rows;
+  g = there && a.grad_logp && a.targets[n] >= 0 ? a.grad_logp[n] : 0.0f;
+  gh = there && a.grad_entropy ? a.grad_entropy[n] : 0.0f;
+  return there && a.peak[n] != -INFINITY && (g != 0.0f || gh != 0.0f);
+}
+
 // BACKWARD: dz instead of statistics.  WIDE: W's rows begin at multiples of 16 bytes.
 template <int NR, bool BACKWARD, bool WIDE>
 __global__ void __launch_bounds__(kCtaThreads, NR <= 16 ? 2 : 1) small_logits_kernel(HeadSmallArgs a) {
@@ -162,13 +170,13 @@ __global__ void __launch_bounds__(kCtaThreads, NR <= 16 ? 2 : 1) small_logits_ke
     if (!half && t < NR) {
       const bool there = t < a.rows;
       const int64_t to = there && a.targets ? a.targets[t] : -1;
-      const float g = there && a.grad_logp && to >= 0 ? a.grad_logp[t] : 0.0f, gh = there && a.grad_entropy ? a.grad_entropy[t] : 0.0f;
+      float g, gh;
+      of_row[5][t] = small_share(a, t, g, gh) ? 1.0f : 0.0f;
       of_row[0][t] = there ? a.peak[t] : 0.0f;
       of_row[1][t] = there ? a.log_sum[t] : 0.0f;
       of_row[2][t] = g;
       of_row[3][t] = gh;
       of_row[4][t] = there && a.grad_entropy ? a.entropy[t] : 0.0f;
-      of_row[5][t] = there && of_row[0][t] != -INFINITY && (g != 0.0f || gh != 0.0f) ? 1.0f : 0.0f;
       target[t] = to;
     }
     __syncthreads();
@@ -250,13 +258,16 @@ __global__ void __launch_bounds__(256) small_outer_kernel(HeadSmallArgs a) {
   const int each = a.rows / a.partitions;
   float h[NR][kCols], dh[NR][kCols];
 #pragma unroll
-  for (int n = 0; n < NR; n++)
+  for (int n = 0; n < NR; n++) {
+    float g, gh;
+    const bool counts = small_share(a, n, g, gh);        // (what a row without a share holds may be no number)
 #pragma unroll
     for (int c = 0; c < kCols; c++) {
       const int64_t col = c0 + c * kApart;
-      h[n][c] = n < a.rows && col < a.cols ? a.hidden[n * a.hidden_pitch + col] : 0.0f;
+      h[n][c] = counts && col < a.cols ? a.hidden[n * a.hidden_pitch + col] : 0.0f;
       dh[n][c] = 0.0f;
     }
+  }
   auto fetch = [&](int64_t v, int stage) {
     for (int i = t; i < kShareTokens * NR / 4; i += 256) copy16_async(dz[stage] + 4 * i, a.dz + v * NR + 4 * i);      // (dz has room for whole stages)
     copies_commit();

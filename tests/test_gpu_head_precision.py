@@ -320,3 +320,26 @@ def test_health():
     r = binding.solon_head_logprobs(h, w, t)
     binding.solon_head_logprobs_backward(h, w, t, r.peak, r.log_sum, torch.full((300,), -1.0, device="cuda"))
     assert binding.solon_head_status() == binding.OK
+
+
+@pytest.mark.parametrize("dtype,grad", [("f32", "f32"), ("f32", "bf16"), ("f16", "f32"), ("bf16", "f64"), ("bf16", "bf16")])
+@pytest.mark.parametrize("rows,vocab", [(8, 19_000), (16, 700), (300, 700)])
+def test_hidden_states_of_rows_without_a_share_may_hold_anything(rows, vocab, dtype, grad):
+    """NaN and infinity where padding stands: the same bits as with numbers there."""
+    cols, parts = 72, 2
+    h, w, t = _leaning(rows, cols, vocab, dtype, 3)
+    t[1::4] = -1
+    peak, log_sum, entropy = _stats(h, w)
+    peak[2] = -INF
+    g, gh = -torch.rand(rows, device="cuda", generator=_gen(1)), torch.randn(rows, device="cuda", generator=_gen(2)) / 8
+    gh[1::4] = 0.0
+
+    def call():
+        dw = torch.empty((parts, vocab * cols), dtype=TYPES[grad], device="cuda")
+        return binding.solon_head_logprobs_backward(h, w, t, peak, log_sum, g, entropy, gh, partitions=parts, dweight=dw)
+
+    want = call()
+    h[1::4, ::3], h[1::4, 1::3], h[2] = NAN, INF, -INF
+    log_sum[1::4], entropy[1::4], log_sum[2] = NAN, NAN, INF
+    got = call()
+    assert torch.isfinite(want[1]).all() and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
