@@ -16,7 +16,8 @@
 //                      of two for these products: eight bits of dz would put as much into a result again as its own rounding to bfloat16 does; with eleven, an
 //                      eighth of that).  One piece for dh of bfloat16 states and for bfloat16 gradients (those of float32 states take the first piece of
 //                      the states alone, too): 11 bits of what lies above 2^-28 of the largest, an absolute 2^-40 of it below.  Two, the second times 2^11 as above,
-//                      for dh of float16 and float32 states and for float32 and float64 gradients: 22 bits, and 2^-50.
+//                      for dh of float16 and float32 states and for float32 and float64 gradients: 22 bits, and 2^-50.  Up to 512 bfloat16 rows it is bfloat16
+//                      instead, at any magnitude: two pieces (16 bits), or three (24) for dW in float32 and float64.
 //
 // Measured (us; of 1662 TFLOP/s in bursts, 1407 sustained): 8192 x 2048 states, 32768 tokens, bfloat16: forward 790 (1.39 PFLOP/s), backward with bfloat16
 // gradients 2345 (1.41); a library's plain products of these sizes take 660 to 730 each.  What the product is fed by and how it ends is what that came from: one
@@ -85,7 +86,8 @@ struct HeadArgs {
   uint32_t per_slab_inverse, band_inverse;             // reciprocals for the tiles' numbers
   int k_blocks, products;
   int chunk;                             // blocks of 64 that are summed in tensor memory before the sum is added to the one in registers
-  int low;                               // blocks of the products with a second piece, which come first: their sum is taken times 2^-11 before the others join it
+  int low;                               // blocks of the products with a second piece, which come first: their sum is taken times low_factor before the others join it
+  float low_factor;                      // 2^-11 for float16 pieces
   int piece_a[3], piece_b[3];            // third coordinate of the tensor maps for slab 0; slab s is s further
   int slab_a, slab_b;                    // 1: the operand has slabs
   int splits;                            // the inner dimension is cut into so many parts of k_blocks, slabs of their own; what lies behind its end is zeros
@@ -93,7 +95,7 @@ struct HeadArgs {
   int b_by_blocks;                       // B's map takes 128 columns a copy, where its rows lie across the inner dimension
   const HeadWords* words;
   int weight_scaled;                     // kDhidden: the weights carry a power of two
-  const unsigned* parts;                 // kDweight: the partitions' words
+  const unsigned* parts;                 // kDweight: the partitions' words (NULL: nothing carries a power of two)
   const float *undo_m, *undo_n;          // what the product's rows and columns are multiplied by (NULL: nothing)
   // rows
   const int64_t* targets;
@@ -177,8 +179,8 @@ struct DzRow {
   float peak, log_sum, entropy, g, gh;
 };
 
-// What is stored of dz: the nearest float16; or that and what it leaves, times kSecond, as a second float16.
-enum DzForm { kNearest, kPair };
+// What is stored of dz: the nearest float16; that and what it leaves, times kSecond, as a second float16; or the nearest bfloat16 and what it leaves in one or two more.
+enum DzForm { kNearest, kPair, kWidePair, kWideTriple };
 
 struct DzOut {
   const CUtensorMap* map;
@@ -188,10 +190,11 @@ struct DzOut {
   float target;
 };
 
-// 64 elements of a row as float16 to a block, and the target's.  Leaves what they leave of the elements, as the second piece has it, where LEAVE.
-template <bool LEAVE>
+// 64 elements of a row as 16-bit words to a block, and the target's.  Leaves what they leave of the elements, as the next piece has it, where LEAVE.
+template <typename T, bool LEAVE>
 __device__ __forceinline__ void dz_block(float* v, float& target, uint32_t keep, int place, int lane, char* block) {
-  using Word = Word16<__half>;
+  using Word = Word16<T>;
+  constexpr float kGrow = std::is_same<T, __half>::value ? kSecond : 1.0f;
 #pragma unroll
   for (int i = 0; i < 8; i++) {
     uint32_t w[4];
@@ -202,15 +205,15 @@ __device__ __forceinline__ void dz_block(float* v, float& target, uint32_t keep,
       if (LEAVE) {
         float wx, wy;
         Word::pair(w[j], wx, wy);
-        x = (x - wx) * kSecond, y = (y - wy) * kSecond;
+        x = (x - wx) * kGrow, y = (y - wy) * kGrow;
       }
     }
     reinterpret_cast<uint4*>(block)[lane * 8 + (i ^ (lane & 7))] = make_uint4(w[0], w[1], w[2], w[3]);
   }
   if (place >= 0 && place < 64) {
-    const __half nearest = __float2half_rn(target);
-    reinterpret_cast<__half*>(block)[(lane * 8 + ((place / 8) ^ (lane & 7))) * 8 + place % 8] = nearest;
-    if (LEAVE) target = (target - __half2float(nearest)) * kSecond;
+    const T nearest = from_float<T>(target);
+    reinterpret_cast<T*>(block)[(lane * 8 + ((place / 8) ^ (lane & 7))) * 8 + place % 8] = nearest;
+    if (LEAVE) target = (target - to_float(nearest)) * kGrow;
   }
 }
 
@@ -254,11 +257,17 @@ __device__ __forceinline__ void dz_row(const DzRow& r, float (&v)[N], uint32_t k
       }
       turn ^= 1;
     };
-    dz_block<FORM == kPair>(v + c, target, keep, out.place - c, out.lane, free_block());
+    using T = typename std::conditional<FORM == kNearest || FORM == kPair, __half, __nv_bfloat16>::type;
+    constexpr int kPieces = FORM == kNearest ? 1 : FORM == kWideTriple ? 3 : 2;
+    dz_block<T, (kPieces > 1)>(v + c, target, keep, out.place - c, out.lane, free_block());
     give(0);
-    if constexpr (FORM == kPair) {
-      dz_block<false>(v + c, target, keep, out.place - c, out.lane, free_block());
+    if constexpr (kPieces > 1) {
+      dz_block<T, (kPieces > 2)>(v + c, target, keep, out.place - c, out.lane, free_block());
       give(1);
+    }
+    if constexpr (kPieces > 2) {
+      dz_block<T, false>(v + c, target, keep, out.place - c, out.lane, free_block());
+      give(2);
     }
   }
 }
@@ -453,7 +462,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
       float undo_row = 1.0f;
       if (MODE != kDweight && a.undo_m && row < a.m) undo_row = a.undo_m[row];
       if (MODE == kDhidden) undo[0] = undo_row;
-      if (MODE == kDweight) {
+      if (MODE == kDweight && a.parts) {
         const int exponent = part_exponent(a.parts[a.splits > 1 ? at.slab / a.splits : at.slab]);
         undo[0] = power_of_two(-(exponent / 2));
         undo[1] = power_of_two(exponent / 2 - exponent);
@@ -462,7 +471,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
 #pragma unroll
       for (int i = 0; i < kHalf; i++) v[i] = 0.0f;
       for (int kb = 0; kb < blocks; kb = chunk_end(a, kb, blocks)) {
-        const float so_far = kb && kb == a.low ? 1.0f / kSecond : 1.0f;
+        const float so_far = kb && kb == a.low ? a.low_factor : 1.0f;
         const Float2 so_far2 = pack2(so_far, so_far);
         pipe::mbar_wait(sum_full + half, sum_phase, abort_flag, status);
         fence_after();
@@ -566,8 +575,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
                    a.grad_entropy ? of_rows[128 + lane] : 0.0f};
         const float undo_dz = of_rows[160 + lane];
         const bool active = undo_dz != 0.0f;
-        r.g *= inverse_power(undo_dz);
-        r.gh *= inverse_power(undo_dz);
+        if (a.form == kNearest || a.form == kPair) {          // (bfloat16 takes dz as it is)
+          r.g *= inverse_power(undo_dz);
+          r.gh *= inverse_power(undo_dz);
+        }
         const uint32_t keep = active ? ~0u : 0u;
         const int64_t token = target - a.first - col, inside = a.vocab - (a.first + col);
         if (inside < kHalf) {                // (what lies beyond is multiplied by zeros and has to be a number: p = 0)
@@ -588,13 +599,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
         }
         const int place = hit ? (int)token : -1;
         const DzOut out = {&maps.out, stage, col, row0, a.dz_pitch - col, lane, place, d};
-        if (a.grad_entropy) {
-          if (a.form == kNearest) dz_row<true, kNearest>(r, v, keep, out, turn);
-          else dz_row<true, kPair>(r, v, keep, out, turn);
-        } else {
-          if (a.form == kNearest) dz_row<false, kNearest>(r, v, keep, out, turn);
-          else dz_row<false, kPair>(r, v, keep, out, turn);
-        }
+        auto rows = [&](auto entropy) {
+          constexpr bool kEntropy = decltype(entropy)::value;
+          if (a.form == kPair) dz_row<kEntropy, kPair>(r, v, keep, out, turn);
+          else if constexpr (BF16) {
+            if (a.form == kNearest) dz_row<kEntropy, kNearest>(r, v, keep, out, turn);
+            else if (a.form == kWidePair) dz_row<kEntropy, kWidePair>(r, v, keep, out, turn);
+            else dz_row<kEntropy, kWideTriple>(r, v, keep, out, turn);
+          } else dz_row<kEntropy, kNearest>(r, v, keep, out, turn);
+        };
+        if (a.grad_entropy) rows(std::true_type{});
+        else rows(std::false_type{});
       } else {
         // (the sums' pitch is a multiple of 128: room for all columns of a warp that has any)
         float* so_far = a.sums + ((int64_t)at.slab * a.m + row) * a.sums_pitch + col;
@@ -851,7 +866,8 @@ __device__ __forceinline__ void store_pieces(const float (&v)[8], float scale, _
 struct HeadScanSide {
   const void* x;                         // NULL: not wanted
   int64_t pitch, rows;
-  __half* out;                           // float32: the pieces of each row by an exponent of its own, and what they are multiplied by to undo it
+  __half* out;                           // float32: the pieces of each row by an exponent of its own, and what they are multiplied by to undo it; 16-bit hidden states: a
+                                         // copy with zeros for rows without a share (NULL: not wanted)
   float* undo;
   unsigned* largest;                     // of the whole matrix (NULL: not wanted)
 };
@@ -945,6 +961,13 @@ __global__ void __launch_bounds__(256) head_scan_kernel(HeadScanArgs a) {
           store_pieces(v, scale, out + c, rest);
         }
         if (lane == 0) m.undo[r] = power_of_two(-exponent);
+      } else if (m.out) {
+        const bool counts = row_share(a, r) != 0.0f;
+        for (int64_t c = lane * 8; c < a.out_pitch; c += TEAM * 8) {
+          float v[8];
+          load8(p, c, counts ? a.cols : 0, wide, v);
+          *reinterpret_cast<uint4*>(m.out + r * a.out_pitch + c) = Word16<T>::pack(v);
+        }
       }
       big = max(big, row);
     }
@@ -1048,6 +1071,7 @@ struct HeadPlan {
   int pieces;                            // of hidden and weight
   bool split;                            // hidden and weight are brought to a layout of their own
   int64_t pitch;                         // of theirs
+  bool as_is;                            // bfloat16 states and weights go into dh and dW as they are
   int dz_pieces;
   int64_t width;                         // tokens of a piece of the vocabulary
   int h_splits, w_splits;                // parts of the inner dimensions of dh and dW
@@ -1134,15 +1158,21 @@ static int head_splits(int64_t slabs, int64_t m, int64_t n, int64_t k, int produ
   return best;
 }
 
-// Pairs of pieces that dh is the sum of: float32 states have two of dz and of W, float16 ones two of dz, bfloat16 ones one of each.
-static int dh_products(int dtype) { return dtype == SOLON_F32 ? 3 : dtype == SOLON_F16 ? 2 : 1; }
+// bfloat16 states: up to so many rows dh is taken from two bfloat16 pieces of dz and W as it lies, and dW from two or three of them.  Beyond, one float16 piece makes one
+// product of two, and W as float16 (scan, copy: three times its size, 0.9 ps an element) costs less than the other (1.4 fs an element and row).
+constexpr int kAsIsRows = 512;
+
+// Pairs of pieces that dh and dW are the sums of.
+static int dh_products(const HeadPlan& p, int dtype) { return dtype == SOLON_F32 ? 3 : dtype == SOLON_F16 || p.as_is ? 2 : 1; }
+static int dw_products(const HeadPlan& p, int grad_dtype) { return p.as_is ? (grad_dtype == SOLON_BF16 ? 2 : 3) : grad_dtype == SOLON_BF16 ? 1 : p.pieces + 1; }
 
 static HeadPlan head_backward_plan(int64_t rows, int64_t cols, int64_t vocab, int partitions, int dtype, int grad_dtype, bool aligned) {
   HeadPlan p = {};
   p.pieces = dtype == SOLON_F32 ? 2 : 1;
   p.split = dtype == SOLON_F32 || !aligned;
   p.pitch = up(cols, kBlock);
-  p.dz_pieces = dtype == SOLON_BF16 && grad_dtype == SOLON_BF16 ? 1 : 2;
+  p.as_is = dtype == SOLON_BF16 && rows <= kAsIsRows;
+  p.dz_pieces = p.as_is ? (grad_dtype == SOLON_BF16 ? 2 : 3) : dtype == SOLON_BF16 && grad_dtype == SOLON_BF16 ? 1 : 2;
   p.width = std::max<int64_t>(kTile, kDzBytes / (rows * 2 * p.dz_pieces) / kTile * kTile);
   p.width = std::min(up(vocab, 64), up((vocab + (vocab + p.width - 1) / p.width - 1) / ((vocab + p.width - 1) / p.width), kTile));     // pieces of one size
   int64_t at = 0;
@@ -1161,8 +1191,8 @@ static HeadPlan head_backward_plan(int64_t rows, int64_t cols, int64_t vocab, in
     return p;
   }
   const int times = (int)((vocab + p.width - 1) / p.width);
-  p.h_splits = head_splits(1, rows, cols, std::min(vocab, p.width), dh_products(dtype), times);
-  p.w_splits = head_splits(partitions, std::min(vocab, p.width), cols, rows / partitions, grad_dtype == SOLON_BF16 ? 1 : p.pieces + 1, 1);
+  p.h_splits = head_splits(1, rows, cols, std::min(vocab, p.width), dh_products(p, dtype), times);
+  p.w_splits = head_splits(partitions, std::min(vocab, p.width), cols, rows / partitions, dw_products(p, grad_dtype), 1);
   p.words = take(sizeof(HeadWords) + partitions * 4);
   p.undo_dz = take(rows * 4);
   if (p.split) {
@@ -1174,7 +1204,7 @@ static HeadPlan head_backward_plan(int64_t rows, int64_t cols, int64_t vocab, in
     p.undo_weight = take(up(vocab, kTile) * 4);
   }
   p.hidden_w = take(p.pieces * rows * p.pitch * 2);
-  if (dtype != SOLON_F16) p.weight_h = take(p.pieces * p.width * p.pitch * 2);
+  if (dtype != SOLON_F16 && !p.as_is) p.weight_h = take(p.pieces * p.width * p.pitch * 2);
   p.dz = take(p.dz_pieces * rows * p.width * 2);
   if (times > 1 || p.h_splits > 1) p.sums = take(p.h_splits * rows * up(cols, 128) * 4);
   if (p.w_splits > 1) p.w_sums = take((int64_t)p.w_splits * partitions * std::min(vocab, p.width) * up(cols, 128) * 4);
@@ -1224,6 +1254,7 @@ static int head_product_launch(const HeadMaps& maps, HeadArgs a, int sms, cudaSt
   a.m_tiles = (a.m + kTile - 1) / kTile;
   a.n_tiles = (a.n + BN - 1) / BN;
   a.low = (a.products - 1) * a.k_blocks;
+  if (!a.low_factor) a.low_factor = 1.0f / kSecond;
   a.chunk = (MODE == kDhidden || MODE == kDweight) && sizeof(O) == 2 ? 64 : 8;
   const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles * a.slabs;
   if (tiles > 0x3FFFFFFF) return SOLON_ERR_INVALID_ARG;
@@ -1288,13 +1319,14 @@ static int head_scan(const HeadScanArgs& a, int dtype, int sms, cudaStream_t str
 
 // Pairs of pieces, the smallest products first.
 static void head_pairs(HeadArgs& a, int pieces_a, int pieces_b, int step_a, int step_b) {
-  a.products = 0;
+  a.products = 0;                          // (three pieces of one factor go with one of the other)
   auto pair = [&](int x, int y) {
     a.piece_a[a.products] = x * step_a;
     a.piece_b[a.products++] = y * step_b;
   };
   if (pieces_b == 2) pair(0, 1);
-  if (pieces_a == 2) pair(1, 0);
+  if (pieces_a == 3) pair(2, 0);
+  if (pieces_a >= 2) pair(1, 0);
   pair(0, 0);
 }
 
@@ -1319,16 +1351,18 @@ static int head_stats(const HeadMaps& maps, const HeadArgs& a, bool few, bool bf
   return head_product_launch<kStats, 256, false, float>(maps, a, sms, stream);
 }
 
-// dh and dW are products of float16 pieces, whatever the states' type.
-static int head_dhidden(const HeadMaps& maps, const HeadArgs& a, int dtype, int sms, cudaStream_t stream) {
+// dh and dW are products of float16 pieces, whatever the states' type, but for few bfloat16 rows.
+static int head_dhidden(const HeadMaps& maps, const HeadArgs& a, int dtype, bool as_is, int sms, cudaStream_t stream) {
+  if (as_is) return head_product<kDhidden, true, __nv_bfloat16>(maps, a, sms, stream);
   if (dtype == SOLON_F32) return head_product<kDhidden, false, float>(maps, a, sms, stream);
   if (dtype == SOLON_BF16) return head_product<kDhidden, false, __nv_bfloat16>(maps, a, sms, stream);
   return head_product<kDhidden, false, __half>(maps, a, sms, stream);
 }
+template <bool BF16>
 static int head_dweight(const HeadMaps& maps, const HeadArgs& a, int grad_dtype, int sms, cudaStream_t stream) {
-  if (grad_dtype == SOLON_F32) return head_product<kDweight, false, float>(maps, a, sms, stream);
-  if (grad_dtype == SOLON_F64) return head_product<kDweight, false, double>(maps, a, sms, stream);
-  return head_product<kDweight, false, __nv_bfloat16>(maps, a, sms, stream);
+  if (grad_dtype == SOLON_F32) return head_product<kDweight, BF16, float>(maps, a, sms, stream);
+  if (grad_dtype == SOLON_F64) return head_product<kDweight, BF16, double>(maps, a, sms, stream);
+  return head_product<kDweight, BF16, __nv_bfloat16>(maps, a, sms, stream);
 }
 
 }  // namespace solon
@@ -1508,16 +1542,18 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
     return head_finish({a.sums, a.sums_pitch, rows, cols, rows > 1 ? dhidden_pitch : cols, 0, 1, plan.h_splits, dhidden}, dtype, sms, stream);
   }
   const bool coarse = grad_dtype == SOLON_BF16;          // dW from the first pieces alone
-  const int form = (dhidden && !bf16) || (dweight && !coarse) ? kPair : kNearest, dz_pieces = form == kPair ? 2 : 1;
-  const bool weight_h = !f16 && dhidden;
+  const bool as_is = plan.as_is, weight_h = !f16 && !as_is && dhidden;
+  const int form = as_is ? (dweight && !coarse ? kWideTriple : kWidePair) : (dhidden && !bf16) || (dweight && !coarse) ? kPair : kNearest;
+  const int dz_pieces = form == kNearest ? 1 : form == kWideTriple ? 3 : 2;
   const int64_t n = rows / partitions, sums_pitch = up(cols, 128);
   unsigned* parts = (unsigned*)(words + 1);
   float* undo_dz = (float*)(ws + plan.undo_dz);
-  SOLON_CUDA_TRY(cudaMemsetAsync(words, 0, sizeof(HeadWords) + partitions * sizeof(unsigned), stream));
-  const HeadScanArgs scan = {{{f32 || dweight ? hidden : nullptr, hidden_pitch, rows, (__half*)(ws + plan.hidden), (float*)(ws + plan.undo_hidden), nullptr},
-                              {f32 || weight_h ? weight : nullptr, weight_pitch, vocab, (__half*)(ws + plan.weight), (float*)(ws + plan.undo_weight),
+  if (!as_is) SOLON_CUDA_TRY(cudaMemsetAsync(words, 0, sizeof(HeadWords) + partitions * sizeof(unsigned), stream));
+  __half* const copy = f32 ? (__half*)(ws + plan.hidden) : as_is ? (__half*)(ws + plan.hidden_w) : nullptr;
+  const HeadScanArgs scan = {{{f32 || dweight ? hidden : nullptr, hidden_pitch, rows, copy, (float*)(ws + plan.undo_hidden), nullptr},
+                              {f32 || weight_h ? weight : nullptr, weight_pitch, vocab, f32 ? (__half*)(ws + plan.weight) : nullptr, (float*)(ws + plan.undo_weight),
                                weight_h ? &words->weight : nullptr}},
-                             cols, plan.pitch, rows, targets, peak, grad_logp, grad_entropy, entropy, undo_dz, dweight ? parts : nullptr, n};
+                             cols, plan.pitch, rows, targets, peak, grad_logp, grad_entropy, entropy, undo_dz, dweight && !as_is ? parts : nullptr, n};
   if ((rc = head_scan(scan, dtype, sms, stream))) return rc;
   HeadOperand h = {ws + plan.hidden, plan.pitch, rows, 2}, w = {ws + plan.weight, plan.pitch, vocab, 2};
   if (!f32 && ((rc = head_operand(hidden, hidden_pitch, rows, cols, plan, ws + plan.hidden, sms, stream, &h)) ||
@@ -1527,13 +1563,14 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
   // as rows along the inner dimension: h and W for the logits, dz for dh; across it: W for dh, dz and h for dW
   CUtensorMap map_h, map_w, map_w_across, map_h_across, map_dz, map_dz_across, map_dz_out;
   HeadOperand hw = h, wh = w;              // as they go into dW and dh
-  if (dweight && (rc = head_pieces(hidden, hidden_pitch, rows, cols, dtype, plan, ws + plan.hidden_w, {nullptr, undo_dz, parts, n}, sms, stream, &hw))) return rc;
+  if (as_is) hw = {ws + plan.hidden_w, plan.pitch, rows, 1};
+  else if (dweight && (rc = head_pieces(hidden, hidden_pitch, rows, cols, dtype, plan, ws + plan.hidden_w, {nullptr, undo_dz, parts, n}, sms, stream, &hw))) return rc;
   // (a map across the inner dimension goes with the tiles: copies of 128 columns need 128 of them in a CTA's tile, and whole blocks of 64 in memory)
   const bool whole = cols % kBlock == 0 || plan.split, hw_whole = whole || dweight, wh_whole = whole || weight_h;
   auto across = [&](CUtensorMap* map, const void* p, bool by_blocks, int64_t rows, int64_t slabs, int64_t pitch, int64_t slab) {
     return by_blocks ? tensor_map_by_blocks(map, p, false, cols, rows, slabs, pitch, slab) : tensor_map(map, p, false, cols, rows, slabs, pitch, slab, kBlock);
   };
-  const bool w_narrow = narrow(cols, (n + kBlock - 1) / kBlock * (coarse ? 1 : hw.pieces + 1));
+  const bool w_narrow = narrow(cols, (n + kBlock - 1) / kBlock * dw_products(plan, grad_dtype));
   if (!tensor_map(&map_h, h.p, bf16, cols, rows, h.pieces, h.pitch, rows * h.pitch, kRows) ||
       !across(&map_h_across, hw.p, hw_whole && !w_narrow, n, (int64_t)hw.pieces * partitions, hw.pitch, n * hw.pitch))
     return SOLON_ERR_CUDA;
@@ -1548,10 +1585,11 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
   base.grad_entropy = grad_entropy;
   base.vocab = vocab;
   base.undo_dz = undo_dz;
-  base.parts = parts;
+  base.parts = as_is ? nullptr : parts;
+  base.low_factor = as_is ? 1.0f : 1.0f / kSecond;
   for (int64_t first = 0; first < vocab; first += plan.width) {
     const int64_t width = std::min(plan.width, vocab - first), pitch = up(width, kBlock);
-    const bool h_narrow = narrow(cols, pitch / kBlock * dh_products(dtype));
+    const bool h_narrow = narrow(cols, pitch / kBlock * dh_products(plan, dtype));
     if (weight_h && (rc = head_pieces((const char*)weight + first * weight_pitch * (f32 ? 4 : 2), weight_pitch, width, cols, dtype, plan, ws + plan.weight_h,
                                       {&words->weight, nullptr, nullptr, 0}, sms, stream, &wh)))
       return rc;
@@ -1585,9 +1623,9 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
       a.narrow = h_narrow;
       a.b_by_blocks = wh_whole && !h_narrow;
       a.k_blocks = (int)((pitch / kBlock + a.splits - 1) / a.splits);
-      head_pairs(a, bf16 ? 1 : 2, wh.pieces, 1, 1);
+      head_pairs(a, bf16 && !as_is ? 1 : 2, wh.pieces, 1, 1);
       a.weight_scaled = weight_h;
-      a.undo_m = undo_dz;
+      a.undo_m = as_is ? nullptr : undo_dz;
       a.sums = (float*)(ws + plan.sums);
       a.sums_pitch = sums_pitch;
       a.load_sums = first > 0;
@@ -1596,7 +1634,7 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
       a.out = dhidden;
       a.out_pitch = rows > 1 ? dhidden_pitch : cols;
       a.out_wide = !(((uintptr_t)dhidden | (uintptr_t)(a.out_pitch * element_size(dtype))) & 31);
-      if ((rc = head_dhidden({map_dz, map_w_across, {}}, a, dtype, sms, stream))) return rc;
+      if ((rc = head_dhidden({map_dz, map_w_across, {}}, a, dtype, as_is, sms, stream))) return rc;
       if (last && a.splits > 1 &&
           (rc = head_finish({a.sums, sums_pitch, rows, cols, a.out_pitch, 0, 1, a.splits, dhidden}, dtype, sms, stream)))
         return rc;
@@ -1614,7 +1652,8 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
       a.sums = (float*)(ws + plan.w_sums);
       a.sums_pitch = sums_pitch;
       a.store_sums = a.splits > 1;
-      head_pairs(a, coarse ? 1 : 2, coarse ? 1 : hw.pieces, partitions, partitions);
+      if (as_is) head_pairs(a, coarse ? 2 : 3, 1, partitions, partitions);
+      else head_pairs(a, coarse ? 1 : 2, coarse ? 1 : hw.pieces, partitions, partitions);
       a.out = (char*)dweight + first * cols * grad_size;
       a.out_pitch = cols;
       a.out_slab = partitions > 1 ? grad_pitch : 0;
@@ -1623,7 +1662,7 @@ int solon_head_logprobs_backward(const void* hidden, int64_t hidden_pitch, const
       a.out_by_map = !(((uintptr_t)a.out | (uintptr_t)(cols * grad_size) | (uintptr_t)(a.out_slab * grad_size)) & 15);
       if (a.out_by_map && !output_map(&maps.out, a.out, (int)grad_size, cols, width, partitions, cols, partitions > 1 ? a.out_slab : up(width * cols, 8)))
         return SOLON_ERR_CUDA;
-      if ((rc = head_dweight(maps, a, grad_dtype, sms, stream))) return rc;
+      if ((rc = as_is ? head_dweight<true>(maps, a, grad_dtype, sms, stream) : head_dweight<false>(maps, a, grad_dtype, sms, stream))) return rc;
       if (a.splits > 1 && (rc = head_finish({a.sums, sums_pitch, width, cols, cols, a.out_slab, partitions, a.splits, a.out}, grad_dtype, sms, stream))) return rc;
     }
   }

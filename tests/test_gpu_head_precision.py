@@ -71,7 +71,7 @@ def _close(x, y, tol, what):
 
 
 @pytest.mark.parametrize("dtype,grad", [("bf16", "f32"), ("bf16", "bf16"), ("f16", "f32"), ("f16", "bf16"), ("f32", "bf16")])
-@pytest.mark.parametrize("rows,parts,cols,vocab", [(300, 2, 128, 400), (2, 1, 72, 1000), (1000, 1, 333, 517)])
+@pytest.mark.parametrize("rows,parts,cols,vocab", [(300, 2, 128, 400), (2, 1, 72, 1000), (512, 4, 65, 700), (1000, 1, 333, 517)])
 def test_sixteen_bit_results_are_off_by_little_more_than_their_own_rounding(rows, parts, cols, vocab, dtype, grad):
     """Half a step of the result, and what dlogits are held in: one float16 piece for dh of bfloat16 states and for bfloat16 gradients (2^-11 of a term, and as
     much again for float32 states, of which these take one piece too), two elsewhere (2^-22); 2^-39 of the largest for what float16 does not reach, of dlogits and of
@@ -149,10 +149,11 @@ def test_float32_elements_far_below_the_largest_of_their_row(rows):
     _close(got.logp, lp, 2 * (tol.amax(1) + floor) + 100 * U * (1 + lp.abs()), "logp")
 
 
+@pytest.mark.parametrize("rows", [5, 300, 513])
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
-def test_gradients_of_rare_tokens_keep_their_bits(dtype):
+def test_gradients_of_rare_tokens_keep_their_bits(dtype, rows):
     """Logits that fall from token to token down to p = 2^-36: dW of each is -g p h, two pieces 2^-22 of it and 2^-50 of g h at most, next to what p is off by."""
-    rows, cols, vocab = 300, 64, 512
+    cols, vocab = 64, 512
     g = _gen(6)
     h = torch.randn((rows, cols), device="cuda", generator=g) * 0.25
     h[:, 0] = 1.0
@@ -343,3 +344,19 @@ def test_hidden_states_of_rows_without_a_share_may_hold_anything(rows, vocab, dt
     log_sum[1::4], entropy[1::4], log_sum[2] = NAN, NAN, INF
     got = call()
     assert torch.isfinite(want[1]).all() and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("rows,vocab,pieces", [(4, 5000, False), (5, 5000, True), (8, 5000, True), (8, 19_000, False), (32, 18_944, False), (33, 18_944, True)])
+def test_where_infinity_in_float32_is_a_mask(rows, vocab, pieces):
+    """Up to 4 rows, and up to 32 from 18,944 tokens on, elements are multiplied as they are: -infinity masks a token. In two pieces its products have no sum."""
+    cols = 48
+    h, w, t = _leaning(rows, cols, vocab, "f32", 8, 1.0)
+    h[:] = h.abs() + 0.5
+    w[7] = -INF
+    t[:] = 8
+    got = binding.solon_head_logprobs(h, w, t)
+    if pieces:
+        assert got.peak.isnan().all() and got.logp.isnan().all()
+    else:
+        want = torch.log_softmax((h.double() @ w.double().t()), 1)[:, 8]
+        assert torch.isfinite(got.log_sum).all() and float((got.logp.double() - want).abs().max()) <= 1e-4
