@@ -292,8 +292,11 @@ __device__ __forceinline__ TileAt tile_at(const HeadArgs& a, uint32_t t, int bn)
   return {(int)slab, (int)((group * 8 + in - column * high) * kTile), (int)column * bn};
 }
 
+constexpr int kLowChunk = 32;            // what is cut off of the second pieces' products lies 2^-8 or 2^-11 lower
 // Where the blocks end that are summed in tensor memory together with block kb.
-__device__ __forceinline__ int chunk_end(const HeadArgs& a, int kb, int blocks) { return min(kb < a.low ? a.low : blocks, kb + a.chunk); }
+__device__ __forceinline__ int chunk_end(const HeadArgs& a, int kb, int blocks) {
+  return kb < a.low ? min(a.low, kb + kLowChunk) : min(blocks, kb + a.chunk);
+}
 
 // stages of A and B blocks, then the epilogue warps' staging, then barriers
 template <int MODE, int BN>
@@ -1255,7 +1258,10 @@ static int head_product_launch(const HeadMaps& maps, HeadArgs a, int sms, cudaSt
   a.n_tiles = (a.n + BN - 1) / BN;
   a.low = (a.products - 1) * a.k_blocks;
   if (!a.low_factor) a.low_factor = 1.0f / kSecond;
-  a.chunk = (MODE == kDhidden || MODE == kDweight) && sizeof(O) == 2 ? 64 : 8;
+  // (what is cut off of a logit is a relative error of its probability: 256 inner indices for float32, 128 in the gradient of few rows, where memory is what takes time.
+  // 45 x 64 rows x 333 float32: dW 1.7e-6 off with 512, 1.0e-6 so; 16 x 768: 1.8e-6, 6.5e-7.  One row's logits with 128: 100 us instead of 90.)
+  if (MODE == kDhidden || MODE == kDweight) a.chunk = sizeof(O) == 2 ? 64 : 8;
+  else a.chunk = MODE == kDz && a.m <= 512 ? 2 : a.products == 3 ? 4 : 8;
   const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles * a.slabs;
   if (tiles > 0x3FFFFFFF) return SOLON_ERR_INVALID_ARG;
   auto inverse = [](int64_t d) { return (uint32_t)std::min<int64_t>(0xFFFFFFFF, (1ll << 32) / d + 1); };
