@@ -913,6 +913,7 @@ __global__ void __launch_bounds__(256) head_scan_kernel(HeadScanArgs a) {
     if (!m.x) return;
     word = m.largest;
     const bool wide = !(((uintptr_t)m.x | (uintptr_t)(m.pitch * sizeof(T))) & 15);
+    if (sizeof(T) == 4 && blockIdx.x == 0 && m.rows + threadIdx.x < (m.rows + kTile - 1) / kTile * kTile) m.undo[m.rows + threadIdx.x] = 1.0f;      // (of whole tiles)
     constexpr int kTeams = 256 / TEAM, kGroups = sizeof(T) == 4 ? 4 : 1;
     for (int64_t r = (int64_t)blockIdx.x * kTeams + threadIdx.x / TEAM; r < m.rows; r += (int64_t)gridDim.x * kTeams) {
       const T* p = (const T*)m.x + r * m.pitch;

@@ -173,7 +173,7 @@ def test_gradients_of_rare_tokens_keep_their_bits(dtype, rows):
     _close(dw.view(vocab, cols), dz.t() @ b, tol, "dweight")
 
 
-@pytest.mark.parametrize("rows,vocab", [(3, 700), (12, 700), (24, 19_000), (40, 700), (300, 700)])
+@pytest.mark.parametrize("rows,vocab", [(3, 700), (12, 700), (24, 19_000), (40, 700), (300, 700), (512, 701), (513, 701), (700, 300)])
 def test_a_large_row_or_token_leaves_the_others_alone(rows, vocab):
     """Every logit is off by what its own row's and token's elements come to, whatever the size of their neighbours."""
     cols = 64
@@ -386,3 +386,33 @@ def test_float32_gradients_are_as_near_as_elementary_float32_operations(dtype, r
     for x, y, e, name in ((dh, elementary[0], exact[0], "dhidden"), (dw, elementary[1], exact[1], "dweight")):
         if x.dtype == torch.float32:
             assert float((x.double() - e).norm()) <= 2.5 * float((y.double() - e).norm()), name
+
+
+@pytest.mark.parametrize("rows", [40, 512, 513])
+def test_weights_of_zeros_and_of_very_different_sizes(rows):
+    """Tokens whose weights are zeros, 2^-60 and 2^60 of the others: float32 dh beside dW and alone, with the same bits."""
+    cols, vocab = 72, 333                                         # (not a whole block of tokens)
+    h, w, t = _leaning(rows, cols, vocab, "f32", 11, 1.0)
+    h[:, 0] = -h[:, 0].abs() - 0.5
+    w[3] = 0.0
+    w[4] *= 2.0 ** -60
+    w[vocab - 1] = 0.0
+    w[5], w[5, 0] = 0.0, 2.0 ** 60                                # p = 0
+    t[:4] = torch.tensor([3, 4, vocab - 1, 6], device="cuda")
+    peak, log_sum, entropy = _stats(h, w)
+    g, gh = -torch.rand(rows, device="cuda", generator=_gen(1)), torch.randn(rows, device="cuda", generator=_gen(2)) / 8
+    dh, dw = binding.solon_head_logprobs_backward(h, w, t, peak, log_sum, g, entropy, gh)
+    alone, _ = binding.solon_head_logprobs_backward(h, w, t, peak, log_sum, g, entropy, gh, weight_grad=False)
+    _, dw_alone = binding.solon_head_logprobs_backward(h, w, t, peak, log_sum, g, entropy, gh, hidden_grad=False)
+    assert torch.equal(alone, dh) and torch.equal(dw_alone, dw)
+    dz, dzt = _dlogits(h, w, t, peak, log_sum, g, entropy, gh)
+    dz[:, 5], dzt[:, 5] = 0.0, 0.0
+    bound = (g.abs() + gh.abs() * (entropy + 1)).double()
+    hd, wd = h.double(), w.double()
+    size = dz.abs().t() @ hd.abs()
+    tol = dzt.t() @ hd.abs() + (2.0 ** -20 + 66 * U) * size + 2.0 ** -49 * float((bound * hd.abs().amax(1)).max()) * rows
+    _close(dw.view(vocab, cols), dz.t() @ hd, tol, "dweight")
+    size = dz.abs() @ wd.abs()
+    # of dz or the weights, whichever is below 2^-28 of its largest: an absolute 2^-50 of it; here of the weights of 2^60
+    tol = dzt @ wd.abs() + (2.0 ** -20 + 66 * U) * size + 2.0 ** -49 * bound[:, None] * 2.0 ** 60 * 1.5
+    _close(dh, dz @ wd, tol, "dhidden")
