@@ -71,6 +71,7 @@ constexpr int kPartBias = 1024;
 __device__ __forceinline__ int part_exponent(unsigned word) { return word ? 14 + kPartBias - (int)word : 0; }      // -226 to 252
 __device__ __forceinline__ int exponent_of(float power) { return (__float_as_int(power) >> 23) - 127; }             // of a power of two
 __device__ __forceinline__ float inverse_power(float power) { return __int_as_float(0x7F000000 - __float_as_int(power)); }
+__device__ __forceinline__ float joint(float power, float other) { return fminf(power * other, 0x1p127f); }         // (finite: it may be that zeros are multiplied)
 constexpr float kSecond = 2048.0f;       // what a second piece is multiplied by: at most 2^3 is left of elements below 2^15, and 2^-25 of those below 2^-14
 __device__ __forceinline__ float power_of_two(int s) { return __int_as_float((s + 127) << 23); }       // -126 <= s <= 127
 
@@ -426,8 +427,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
     const int quarter = warp % 4, side = (warp - kFirstEpilogue) / 4;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     char* stage = staging + (warp - kFirstEpilogue) * Shared::kStaging;
-    float undo[2] = {1.0f, 1.0f};
-    if (MODE == kDhidden && a.weight_scaled) undo[1] = power_of_two(-scale_exponent(a.words->weight));
+    [[maybe_unused]] float undo_weight = 1.0f;
+    if (MODE == kDhidden && a.weight_scaled) undo_weight = power_of_two(-scale_exponent(a.words->weight));
     uint32_t sum_phase = 0;
     int half = 0;
     [[maybe_unused]] int turn = 0;           // which of the warp's two blocks of the result is filled next
@@ -463,8 +464,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
         copies_commit();
       }
       float undo_row = 1.0f;
+      [[maybe_unused]] float undo[2] = {1.0f, 1.0f};         // (a partition's exponent may be twice a float's)
       if (MODE != kDweight && a.undo_m && row < a.m) undo_row = a.undo_m[row];
-      if (MODE == kDhidden) undo[0] = undo_row;
       if (MODE == kDweight && a.parts) {
         const int exponent = part_exponent(a.parts[a.splits > 1 ? at.slab / a.splits : at.slab]);
         undo[0] = power_of_two(-(exponent / 2));
@@ -498,7 +499,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
         if ((half ^= 1) == 0) sum_phase ^= 1;
       }
       if (absent) continue;
-      if constexpr (MODE == kDhidden || MODE == kDweight) {
+      if constexpr (MODE == kDhidden) {
+        const float both = joint(undo_row, undo_weight);
+#pragma unroll
+        for (int i = 0; i < kHalf; i++) v[i] *= both;
+      } else if constexpr (MODE == kDweight) {
 #pragma unroll
         for (int i = 0; i < kHalf; i++) v[i] = v[i] * undo[0] * undo[1];
       } else {
@@ -508,12 +513,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) head_pr
         }
         if (a.undo_n) {
           const float* columns = MODE == kFewRows ? a.undo_n + col : of_columns;
-          const Float2 by_row = pack2(undo_row, undo_row);
 #pragma unroll
           for (int i = 0; i < kHalf; i += 4) {
             const float4 u = *reinterpret_cast<const float4*>(columns + i);
-            unpack2(mul2(mul2(pack2(v[i], v[i + 1]), by_row), pack2(u.x, u.y)), v[i], v[i + 1]);
-            unpack2(mul2(mul2(pack2(v[i + 2], v[i + 3]), by_row), pack2(u.z, u.w)), v[i + 2], v[i + 3]);
+            v[i] *= joint(undo_row, u.x), v[i + 1] *= joint(undo_row, u.y), v[i + 2] *= joint(undo_row, u.z), v[i + 3] *= joint(undo_row, u.w);
           }
         }
       }

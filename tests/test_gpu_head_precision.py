@@ -416,3 +416,26 @@ def test_weights_of_zeros_and_of_very_different_sizes(rows):
     # of dz or the weights, whichever is below 2^-28 of its largest: an absolute 2^-50 of it; here of the weights of 2^60
     tol = dzt @ wd.abs() + (2.0 ** -20 + 66 * U) * size + 2.0 ** -49 * bound[:, None] * 2.0 ** 60 * 1.5
     _close(dh, dz @ wd, tol, "dhidden")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [3, 40, 200, 600])
+@pytest.mark.parametrize("hs,ws,gs", [(1e34, 1e-34, 1e3), (1e-34, 1e34, 1.0), (1e20, 1e-20, 1e33), (1.0, 1e-30, 1e37), (1.0, 1.0, 1e-34)])
+def test_powers_of_two_near_the_ends_of_float32(hs, ws, gs, rows, dtype):
+    """Products of ordinary size from factors of any: what undoes one factor's power of two alone would be infinite, or zero. By norms: 2^-20 for float32 and
+    its gradients, half a bfloat16 step beside it for dh of bfloat16 states; ten times that where the logits' own error is part of it."""
+    cols, vocab = 64, 300
+    h, w, t = _leaning(rows, cols, vocab, "f32", 10, 1.0)
+    h, w = (h * hs).to(TYPES[dtype]), (w * ws).to(TYPES[dtype])
+    z = h.double() @ w.double().t()
+    got = binding.solon_head_logprobs(h, w, t)
+    assert float((got.peak.double() - z.amax(1)).abs().max()) <= 1e-5 * (1 + float(z.abs().max()))
+    assert float((got.logp.double() - torch.log_softmax(z, 1).gather(1, t[:, None])[:, 0]).abs().max()) <= 2e-5 * (1 + float(z.abs().max()))
+    peak, log_sum, _ = _stats(h, w)
+    g = -torch.rand(rows, device="cuda", generator=_gen(3)) * gs
+    dh, dw = binding.solon_head_logprobs_backward(h, w, t, peak, log_sum, g)
+    dz, _ = _dlogits(h, w, t, peak, log_sum, g)
+    most = torch.finfo(torch.float32).max
+    for x, e, lim in ((dh, dz @ w.double(), 1e-5 if dtype == "f32" else 2.0 ** -8), (dw.view(vocab, cols), dz.t() @ h.double(), 1e-5)):
+        if float(e.abs().max()) < most and float(e.abs().max()) > 2.0 ** -110:
+            assert float((x.double() - e).norm()) <= lim * float(e.norm())
