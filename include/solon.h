@@ -365,7 +365,7 @@ int solon_token_logprobs_backward(const void* logits, int64_t pitch, int dtype, 
 /* Embedding lookup: out_i = scale E[token_i].
  *   weight  device, vocab x cols of `dtype` (SOLON_F32, SOLON_BF16 or SOLON_F16)
  *   tokens  device, rows int64: a negative one gives a row of zeros, one >= vocab a row of NaN (neither is looked up)
- *   out     device, rows x cols of `dtype` (output); scale = 1 copies the bits, otherwise one rounding
+ *   out     device, rows x cols of `dtype` (output); scale (as float32) 1 copies the bits, otherwise one rounding of the product
  * cols <= SOLON_MAX_WIDTH.  rows = 0 does nothing.  In this and the three operators below no output may share a byte with an input or another output (refused). */
 int solon_embedding_forward(const void* weight, int64_t weight_pitch, int dtype, const int64_t* tokens, int64_t rows, int64_t cols, int64_t vocab,
                             double scale, void* out, int64_t out_pitch, void* cuda_stream);
@@ -390,9 +390,11 @@ int solon_embedding_backward(const void* dy, int64_t dy_pitch, int dtype, const 
  *   targets, logp, entropy, peak, log_sum  as in solon_token_logprobs
  *   workspace  device, 256-byte aligned, solon_head_logprobs_workspace(...) bytes; `aligned`: 1 if both matrices' first elements and row
  *              pitches are multiples of 16 bytes (other rows are copied to such a pitch first).  Its contents need not survive the call
- * Products of the elements as they are, summed in float32 (float16 elements below 2^-14 with the precision of 2^-14); float32 elements are taken as two float16 pieces of 22 bits together (values
- * below 2^-28 of the largest of their row of hidden or weight: an absolute 2^-50 of it), or multiplied as they are where rows are few (up to 16).
- * Infinite and NaN elements reach the rows that their products enter; in two pieces infinity counts as NaN.  cols <= SOLON_MAX_WIDTH. */
+ * 16-bit elements are multiplied as they are and summed in float32 (float16 elements below 2^-14 with the precision of 2^-14).  float32 elements are multiplied as they are
+ * up to 4 rows (of at most 200 KB together, their columns rounded up to 256), and up to 32 rows where vocab >= 18944; otherwise they are taken as two float16 pieces of 22
+ * bits together (values below 2^-28 of the largest of their row of hidden or weight: an absolute 2^-50 of it).  No row's results depend on another row.
+ * Infinite and NaN elements reach the rows that their products enter.  A float32 infinity in two pieces counts as NaN: an output matrix that masks tokens by -infinity
+ * does so for 16-bit types, and in float32 only where elements are multiplied as they are.  cols <= SOLON_MAX_WIDTH. */
 int64_t solon_head_logprobs_workspace(int64_t rows, int64_t cols, int64_t vocab, int dtype, int aligned);
 int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* weight, int64_t weight_pitch, int dtype, const int64_t* targets, int64_t rows,
                         int64_t cols, int64_t vocab, float* logp, float* entropy, float* peak, float* log_sum, void* workspace, int64_t workspace_bytes,
@@ -403,11 +405,12 @@ int solon_head_logprobs(const void* hidden, int64_t hidden_pitch, const void* we
  *   dweight_k = dlogits_k^T * hidden_k   device (output; NULL: not wanted): row k of the partition-gradient matrix from dweight[k * grad_pitch] on,
  *                                        vocab x cols elements of `grad_dtype` (SOLON_F32, SOLON_F64 or SOLON_BF16), over the rows of partition k
  *   peak, log_sum, entropy, grad_logp, grad_entropy  as in solon_token_logprobs_backward
- *   workspace  device, 256-byte aligned, solon_head_logprobs_backward_workspace(...) bytes: dlogits of one piece of the vocabulary (at most
- *              512 MB, or 256 tokens), sums of dhidden
+ *   workspace  device, 256-byte aligned, solon_head_logprobs_backward_workspace(...) bytes, whatever is wanted of the outputs: dlogits of one piece of the
+ *              vocabulary (at most 512 MB, or 256 tokens), sums of dhidden, pieces of hidden and (float32: twice, once of one piece of the vocabulary) weight
  * dlogits is held in float16 times a power of two a row: one piece (11 bits; values below 2^-28 of the row's |grad_logp| + |grad_entropy| (entropy + 1): an absolute
  * 2^-40 of it) for dhidden of bfloat16 states and for bfloat16 gradients, two (22 bits; 2^-50) for dhidden of float16 and float32 states and for float32 and float64
- * gradients.  The other factor is taken in float16 pieces as well, as many as the elements have above (bfloat16 gradients: one): weight by a power of two of its largest in dhidden (float16
+ * gradients; or, up to 512 bfloat16 rows, in two (16 bits) or, for float32 and float64 gradients, three (24 bits) bfloat16 pieces of any magnitude; or in float32, up to
+ * 16 float32 rows where vocab >= 18944, with no pieces of the other factor either.  The other factor is taken in float16 pieces as well, as many as the elements have above (bfloat16 gradients: one): weight by a power of two of its largest in dhidden (float16
  * as it is), hidden in dweight by powers of two that make the largest product of a row's bound and its elements in the partition the measure.  No row's dhidden depends on
  * another row, no partition's dweight on another partition.
  * rows = 0: dweight becomes 0.  Rows that count in no gradient may hold anything in hidden. */

@@ -19,13 +19,15 @@
 //                      for dh of float16 and float32 states and for float32 and float64 gradients: 22 bits, and 2^-50.  Up to 512 bfloat16 rows it is bfloat16
 //                      instead, at any magnitude: two pieces (16 bits), or three (24) for dW in float32 and float64.
 //
-// Measured (us; of 1662 TFLOP/s in bursts, 1407 sustained): 8192 x 2048 states, 32768 tokens, bfloat16: forward 790 (1.39 PFLOP/s), backward with bfloat16
-// gradients 2345 (1.41); a library's plain products of these sizes take 660 to 730 each.  What the product is fed by and how it ends is what that came from: one
+// Measured (us, the first in bursts, the second at the power limit, of 1662 and 1407 TFLOP/s): 8192 x 2048 states, 32768 tokens, bfloat16: forward 790 and 930 (1.39 and
+// 1.18 PFLOP/s), backward with bfloat16 gradients 2485 and 2910 (1.33 and 1.13, of which 100 are the scan and the copy of W as float16); a library's plain products of these sizes
+// take 660 to 730 each, so that with logits in memory the two passes take 2330 together where they take 3300 here: what this form saves is 0.5 GB of logits.  In float32,
+// whose products the library takes without tensor cores, it saves time as well: 2047 x 1001 over 50001 tokens 2280 against 10480.  What the product is fed by and how it ends is what that came from: one
 // copy for 128 rows or columns of a block (6 %), two warps that issue them (4 %), sums of 512 in registers (5 % against 256), no branch between a row's
 // elements and no store of single rows in the epilogues (a third of their time).
 //
 // Few rows (a served token) are a matter of reading W once.  Up to 128 rows the product is taken the other way round (tokens along the tile's rows): 131072 x 2048
-// bfloat16 90 us for one row (6.0 TB/s), 100 for 96.  float32 and rows off 16-byte boundaries are not brought into another form for a few rows: kernels of
+// bfloat16 90 us for one row (6.0 TB/s), 100 to 119 for 96.  float32 and rows off 16-byte boundaries are not brought into another form for a few rows: kernels of
 // multiply-adds, here for up to 4 rows of any type and alignment, in head_rows.cu for up to 32 float32 rows.
 
 #include <algorithm>
@@ -313,7 +315,7 @@ struct HeadShared {
 // while the other is being filled, and keep a tile's result in registers: 128 columns of a row a thread.
 // The tensor cores cut off what lies below an accumulator's last bit, which costs a sum of n steps of 16 about n / 2 units of 2^-25, always towards 0
 // (measured: 1.6e-8 a step, 2e-5 for dh of 50,001 tokens).  So a result that is wanted in float32 is summed 512 inner indices at a time, and those sums are
-// added in registers, rounded to nearest (256 at a time: 5 to 15 % slower; all at once: 1 % faster).
+// added in registers, rounded to nearest (256 at a time: 5 to 15 % slower; all at once: 1 % faster); logits from two pieces 256, the products with a second piece 2048.
 // Persistent: a pair takes every (pairs)-th tile.
 // Every wait ends after two seconds at the latest: the tiles of a CTA whose wait ran out are filled with NaN.
 template <int MODE, int BN, bool BF16, typename O>

@@ -1,11 +1,12 @@
 // Few float32 rows against an output matrix: logits and gradients by multiply-adds.
 //
-// The tensor cores would take float32 elements as two float16 pieces, which have to be made first: W read to find its scale, read again, written and
-// read as often as there are products.  With up to 32 rows (16 in the backward pass) the multiply-adds that W's elements go into once they are on the SM cost
-// less than that.  Bound: reading W (and writing dW), or 2 (4) rows multiply-adds an element at 36 T/s.
+// The tensor cores would take float32 elements as two float16 pieces, which have to be made first: W read, written and read as often as there are
+// products (in the backward pass twice).  With up to 32 rows (16 in the backward pass) the multiply-adds that W's elements go into once they are on the SM cost
+// less than that.  Bound: reading W (twice, and writing dW, in the backward pass), or as many multiply-adds an element as there are rows (three times as many: logits, dh,
+// dW) at 36 T/s: of 13 rows of 3456 over 37760 tokens 80 us of memory against 47 of multiply-adds.
 //
 // Logits: a CTA takes a tile of 256 tokens and brings 32 columns at a time into shared memory, two stages (three of 16 columns: 15 to 50 % slower).  Two
-// sets of 128 threads share a stage's columns, so that more warps hide what each waits for (13 rows of 3456 over 37760 tokens: 213 us with one set, 168 to 176 with
+// sets of 128 threads share a stage's columns, so that more warps hide what each waits for (13 rows of 3456 over 37760 tokens: 213 us with one set, 167 to 186 with
 // two).  A lane owns two tokens (rows 36 floats apart, so that its 16-byte reads meet no bank twice) against all rows, whose elements are broadcast.  Sums of
 // 16 products are added to another.  A tile is gone through by one CTA from first to last column, so vocabularies of fewer tiles than half the SMs (below
 // 18,944 tokens) take the pieces instead (9 rows of 2307 over 1702 tokens: 190 us here, 60 in pieces).
@@ -373,7 +374,8 @@ int64_t small_tile() { return kTokenTile; }
 
 static int64_t small_slices(int64_t cols) { return (cols + 1023) / 1024; }
 
-// Two CTAs an SM, of at least 64 tokens each.
+// 296 CTAs, of at least 64 tokens each: two an SM where the kernel takes 128 registers (up to 8 rows of a single partition at multiples of 16 bytes), otherwise one after
+// the other (140 to 148 registers; 198 to 212 up to 16 rows).
 int small_splits(int64_t cols, int64_t vocab) {
   const int64_t slices = small_slices(cols);
   return (int)std::max<int64_t>(1, std::min((2 * 148 + slices - 1) / slices, vocab / 64));
