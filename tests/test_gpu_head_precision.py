@@ -439,3 +439,38 @@ def test_powers_of_two_near_the_ends_of_float32(hs, ws, gs, rows, dtype):
     for x, e, lim in ((dh, dz @ w.double(), 1e-5 if dtype == "f32" else 2.0 ** -8), (dw.view(vocab, cols), dz.t() @ h.double(), 1e-5)):
         if float(e.abs().max()) < most and float(e.abs().max()) > 2.0 ** -110:
             assert float((x.double() - e).norm()) <= lim * float(e.norm())
+
+
+@pytest.mark.parametrize("dtype,grad", [("f32", "f32"), ("f32", "bf16"), ("f16", "f32"), ("bf16", "f32")])
+@pytest.mark.parametrize("rows,cols,vocab", [(20, 8200, 130), (600, 9001, 70), (514, 64, 20_000)])
+def test_wide_rows_and_a_graph_of_their_gradient(rows, cols, vocab, dtype, grad):
+    """Rows that a whole CTA goes through; the backward pass captured and replayed on other inputs gives the bits of a call."""
+    parts = 2
+    h, w, t = _leaning(rows, cols, vocab, dtype, 13, 2.0)
+    peak, log_sum, _ = _stats(h, w)
+    g = -torch.rand(rows, device="cuda", generator=_gen(1)) / rows
+    dw = torch.empty((parts, vocab * cols), dtype=TYPES[grad], device="cuda")
+
+    def call():
+        return binding.solon_head_logprobs_backward(h, w, t, peak, log_sum, g, partitions=parts, dweight=dw)
+
+    dh = call()[0]
+    n = rows // parts
+    dz, _ = _dlogits(h, w, t, peak, log_sum, g)
+    lim = {"f32": 1e-5, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+    e = dz @ w.double()
+    assert float((dh.double() - e).norm()) <= (lim[dtype] + 1e-5) * float(e.norm()) + (2.0 ** -25 * e.numel() ** 0.5 if dtype == "f16" else 0.0)
+    for k in range(parts):
+        e = (dz[k * n:(k + 1) * n].t() @ h[k * n:(k + 1) * n].double()).reshape(-1)
+        assert float((dw[k].double() - e).norm()) <= (1e-5 + (2.0 ** -8 if grad == "bf16" else 0.0)) * float(e.norm())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call()[0]
+    h.copy_(h.flip(0)), t.copy_(t.flip(0)), g.mul_(1e-6)
+    g[0] = 3.0
+    fresh = _stats(h, w)
+    peak.copy_(fresh[0]), log_sum.copy_(fresh[1])
+    for _ in range(2):
+        graph.replay()
+    got, got_w = out.clone(), dw.clone()
+    assert torch.equal(got, call()[0]) and torch.equal(got_w, dw)
